@@ -13,8 +13,11 @@ import sys
 HERE = os.path.dirname(os.path.abspath(__file__))
 CSRC = os.path.join(HERE, "csrc")
 LIB = os.path.join(HERE, "libcconv.so")
-SOURCES = ["kernels.cu", "direct_kernel.cu", "stem_kernel.cu", "api.cu", "host_setup.cu", "noalloc.cu", "pool.cu", "planner.cpp"]
-HEADERS = ["kernels.h", "planner.h", "host_setup.h", "ptx_sm100.cuh", "direct_issue.cuh", os.path.join("..", "..", "include", "cconv.h")]
+SOURCES = ["kernels.cu", "direct_kernel.cu", "stem_kernel.cu", "api.cu", "host_setup.cu", "noalloc.cu", "pool.cu", "planner.cpp",
+           "block_api.cu", "block_gemm.cu", "block_norm.cu", "block_quant.cu"]
+HEADERS = ["kernels.h", "planner.h", "host_setup.h", "ptx_sm100.cuh", "direct_issue.cuh",
+           "block.h", "block_device.cuh", "block_gemm.h", "block_norm.h", "block_quant.h",
+           os.path.join("..", "..", "include", "cconv_block.h"), os.path.join("..", "..", "include", "cconv.h")]
 
 
 def _nvcc() -> str:

@@ -1,0 +1,87 @@
+// Device helpers shared by the kernels of the feed-forward sub-block: element types and activations.
+#pragma once
+#include <cuda_bf16.h>
+#include <cuda_fp16.h>
+#include <cuda_runtime.h>
+
+#include <cstdint>
+
+#include "../../include/cconv_block.h"
+
+namespace cconv {
+namespace {
+
+__device__ __forceinline__ float to_f32(__nv_bfloat16 v) { return __bfloat162float(v); }
+__device__ __forceinline__ float to_f32(__half v) { return __half2float(v); }
+__device__ __forceinline__ float to_f32(float v) { return v; }
+template <typename T>
+__device__ __forceinline__ T from_f32(float v);
+template <>
+__device__ __forceinline__ __nv_bfloat16 from_f32<__nv_bfloat16>(float v) { return __float2bfloat16_rn(v); }
+template <>
+__device__ __forceinline__ __half from_f32<__half>(float v) { return __float2half_rn(v); }
+template <>
+__device__ __forceinline__ float from_f32<float>(float v) { return v; }
+
+// Two neighbouring elements of a 16-bit type as one 32-bit word (the first in the low half).
+template <typename T>
+__device__ __forceinline__ uint32_t pack2(float lo, float hi);
+template <>
+__device__ __forceinline__ uint32_t pack2<__nv_bfloat16>(float lo, float hi) {
+  const __nv_bfloat162 v = __floats2bfloat162_rn(lo, hi);
+  return *reinterpret_cast<const uint32_t*>(&v);
+}
+template <>
+__device__ __forceinline__ uint32_t pack2<__half>(float lo, float hi) {
+  const __half2 v = __floats2half2_rn(lo, hi);
+  return *reinterpret_cast<const uint32_t*>(&v);
+}
+template <typename T>
+__device__ __forceinline__ float2 unpack2(uint32_t w);
+template <>
+__device__ __forceinline__ float2 unpack2<__nv_bfloat16>(uint32_t w) {
+  return make_float2(__uint_as_float(w << 16), __uint_as_float(w & 0xffff0000u));
+}
+template <>
+__device__ __forceinline__ float2 unpack2<__half>(uint32_t w) {
+  return __half22float2(*reinterpret_cast<const __half2*>(&w));
+}
+
+// The activation's value a(g) and, if asked for, its derivative.  The exponential and the quotient
+// are the fast ones (a few units in the last place of fp32, far below a 16-bit rounding).
+//   silu       g s(g)              s(1 + g(1 - s)),          s = 1/(1 + exp(-g))
+//   gelu       g Phi(g)            Phi + g exp(-g^2/2)/sqrt(2 pi)
+//   gelu_tanh  g s(2z)             s + g s(1 - s) 2z',       z = sqrt(2/pi)(g + 0.044715 g^3)
+//   relu       max(g, 0)           g > 0
+template <bool kDerivative>
+__device__ __forceinline__ float activation(int act, float g, float& da) {
+  if (act == CCONV_ACT_SILU) {
+    const float s = __fdividef(1.0f, 1.0f + __expf(-g));
+    if (kDerivative) da = s * (1.0f + g * (1.0f - s));
+    return g * s;
+  }
+  if (act == CCONV_ACT_GELU) {
+    const float phi = 0.5f * erfcf(-0.70710678118654752f * g);
+    if (kDerivative) da = phi + g * 0.39894228040143268f * __expf(-0.5f * g * g);
+    return g * phi;
+  }
+  if (act == CCONV_ACT_GELU_TANH) {
+    const float k = 1.5957691216057308f;  // 2 sqrt(2/pi)
+    const float g2 = g * g;
+    const float s = __fdividef(1.0f, 1.0f + __expf(-k * (g + 0.044715f * g * g2)));
+    if (kDerivative) da = s + g * s * (1.0f - s) * k * (1.0f + 0.134145f * g2);
+    return g * s;
+  }
+  if (kDerivative) da = g > 0.0f ? 1.0f : 0.0f;
+  return g > 0.0f ? g : (g != g ? g : 0.0f);
+}
+
+// Sum over the 32 lanes, the same in every lane.
+__device__ __forceinline__ float warp_sum(float v) {
+#pragma unroll
+  for (int o = 16; o > 0; o >>= 1) v += __shfl_xor_sync(0xffffffffu, v, o);
+  return v;
+}
+
+}  // namespace
+}  // namespace cconv
