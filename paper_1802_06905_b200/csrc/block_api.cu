@@ -5,6 +5,7 @@
 #include <string>
 
 #include "block.h"
+#include "block_ffn.h"
 #include "block_gemm.h"
 #include "block_norm.h"
 #include "block_quant.h"
@@ -128,29 +129,6 @@ bool ffn_sizes_ok(const cconv_ffn_args& a) {
          a.act <= CCONV_ACT_RELU && double(a.T) * a.F < 1e15 && double(a.D) * a.F < 1e15 && double(a.T) * a.D < 1e15;
 }
 
-struct FfnSpace {
-  void *h = nullptr, *dg = nullptr, *du = nullptr;
-  float *s0 = nullptr, *s1 = nullptr;
-  int64_t used = 0;
-};
-
-FfnSpace ffn_space(const cconv_ffn_args& a, bool backward, void* base) {
-  FfnSpace w;
-  Carver c(base);
-  w.h = c.take(a.T * a.F * 2);
-  if (backward) {
-    w.dg = c.take(a.T * a.F * 2);
-    w.du = c.take(a.T * a.F * 2);
-  }
-  const int64_t td = a.T * a.D, tf = a.T * a.F, df = a.D * a.F;
-  int64_t most = td > tf ? td : tf;
-  if (backward && df > most) most = df;
-  w.s0 = static_cast<float*>(c.take(most * 4));
-  if (!backward) w.s1 = static_cast<float*>(c.take(tf * 4));
-  w.used = c.used();
-  return w;
-}
-
 cudaError_t zero_out(const cconv_matrix& m, int64_t rows, int64_t cols, int es, cudaStream_t s) {
   if (rows == 0 || cols == 0) return cudaSuccess;
   if (m.col_stride == 1 || cols == 1)
@@ -171,51 +149,26 @@ cudaError_t zero_out(const cconv_matrix& m, int64_t rows, int64_t cols, int es, 
     if (e_ != cudaSuccess) return block_cuda_error(e_, __func__);     \
   } while (0)
 
-int ffn_forward(const cconv_ffn_args& a, cudaStream_t s) {
-  const FfnSpace w = ffn_space(a, false, a.workspace);
-  if (a.T == 0 || a.D == 0) {
-    // no output, or pre-activations that are empty sums
-    if (a.gate_pre.data) {
-      BLOCK_CUDA(zero_out(a.gate_pre, a.T, a.F, 2, s));
-      BLOCK_CUDA(zero_out(a.up_pre, a.T, a.F, 2, s));
-    }
-    return CCONV_OK;
-  }
-  if (a.F == 0) {
+bool ffn_empty(const cconv_ffn_args& a) { return a.T == 0 || a.D == 0 || a.F == 0; }
+// Where a length is zero every result is empty or an empty sum.
+int ffn_zeros(const cconv_ffn_args& a, bool backward, cudaStream_t s) {
+  if (!backward) {
     BLOCK_CUDA(zero_out(a.out, a.T, a.D, 2, s));
+    if (a.gate_pre.data) BLOCK_CUDA(zero_out(a.gate_pre, a.T, a.F, 2, s));
+    if (a.up_pre.data) BLOCK_CUDA(zero_out(a.up_pre, a.T, a.F, 2, s));
     return CCONV_OK;
   }
-  const Mat h(w.h, a.F, 1), x(a.x);
-  BLOCK_CUDA(run_product_simple(x, Mat(a.w_gate), w.s0, a.T, a.F, a.D, a.dtype, false, s));
-  BLOCK_CUDA(run_product_simple(x, Mat(a.w_up), w.s1, a.T, a.F, a.D, a.dtype, false, s));
-  BLOCK_CUDA(finish_gated(w.s0, w.s1, Mat(a.gate_pre), Mat(a.up_pre), h, a.T, a.F, a.act, a.dtype, s));
-  BLOCK_CUDA(run_product_simple(h, Mat(a.w_down), w.s0, a.T, a.D, a.F, a.dtype, false, s));
-  BLOCK_CUDA(finish_store(w.s0, Mat(a.out), a.T, a.D, a.dtype, s));
+  BLOCK_CUDA(zero_out(a.dx, a.T, a.D, 2, s));
+  BLOCK_CUDA(zero_out(a.dw_gate, a.F, a.D, 2, s));
+  BLOCK_CUDA(zero_out(a.dw_up, a.F, a.D, 2, s));
+  BLOCK_CUDA(zero_out(a.dw_down, a.D, a.F, 2, s));
   return CCONV_OK;
 }
-
-int ffn_backward(const cconv_ffn_args& a, cudaStream_t s) {
-  const FfnSpace w = ffn_space(a, true, a.workspace);
-  if (a.T == 0 || a.D == 0 || a.F == 0) {
-    BLOCK_CUDA(zero_out(a.dx, a.T, a.D, 2, s));
-    BLOCK_CUDA(zero_out(a.dw_gate, a.F, a.D, 2, s));
-    BLOCK_CUDA(zero_out(a.dw_up, a.F, a.D, 2, s));
-    BLOCK_CUDA(zero_out(a.dw_down, a.D, a.F, 2, s));
-    return CCONV_OK;
-  }
-  const Mat dout(a.dout), x(a.x), h(w.h, a.F, 1), dg(w.dg, a.F, 1), du(w.du, a.F, 1);
-  BLOCK_CUDA(run_product_simple(dout, Mat(a.w_down).t(), w.s0, a.T, a.F, a.D, a.dtype, false, s));
-  BLOCK_CUDA(finish_gated_backward(w.s0, Mat(a.gate_pre), Mat(a.up_pre), dg, du, h, a.T, a.F, a.act, a.dtype, s));
-  BLOCK_CUDA(run_product_simple(dg, Mat(a.w_gate).t(), w.s0, a.T, a.D, a.F, a.dtype, false, s));
-  BLOCK_CUDA(run_product_simple(du, Mat(a.w_up).t(), w.s0, a.T, a.D, a.F, a.dtype, true, s));
-  BLOCK_CUDA(finish_store(w.s0, Mat(a.dx), a.T, a.D, a.dtype, s));
-  BLOCK_CUDA(run_product_simple(dg.t(), x.t(), w.s0, a.F, a.D, a.T, a.dtype, false, s));
-  BLOCK_CUDA(finish_store(w.s0, Mat(a.dw_gate), a.F, a.D, a.dtype, s));
-  BLOCK_CUDA(run_product_simple(du.t(), x.t(), w.s0, a.F, a.D, a.T, a.dtype, false, s));
-  BLOCK_CUDA(finish_store(w.s0, Mat(a.dw_up), a.F, a.D, a.dtype, s));
-  BLOCK_CUDA(run_product_simple(dout.t(), h.t(), w.s0, a.D, a.F, a.T, a.dtype, false, s));
-  BLOCK_CUDA(finish_store(w.s0, Mat(a.dw_down), a.D, a.F, a.dtype, s));
-  return CCONV_OK;
+int64_t ffn_bytes(const cconv_ffn_args* a, bool backward) {
+  if (!a || !ffn_sizes_ok(*a)) return CCONV_EINVAL;
+  const int sms = block_sm_count();
+  if (sms < 0) return sms;
+  return ffn_empty(*a) ? 0 : ffn_workspace(*a, backward, sms);
 }
 
 // ---- residual norm -------------------------------------------------------------------------------
@@ -277,15 +230,8 @@ using namespace cconv;
 
 extern "C" {
 
-int64_t cconv_ffn_forward_workspace(const cconv_ffn_args* args) {
-  if (!args || !ffn_sizes_ok(*args)) return CCONV_EINVAL;
-  return ffn_space(*args, false, nullptr).used;
-}
-
-int64_t cconv_ffn_backward_workspace(const cconv_ffn_args* args) {
-  if (!args || !ffn_sizes_ok(*args)) return CCONV_EINVAL;
-  return ffn_space(*args, true, nullptr).used;
-}
+int64_t cconv_ffn_forward_workspace(const cconv_ffn_args* args) { return ffn_bytes(args, false); }
+int64_t cconv_ffn_backward_workspace(const cconv_ffn_args* args) { return ffn_bytes(args, true); }
 
 int cconv_ffn_forward(const cconv_ffn_args* args, void* cuda_stream) {
   if (!args || !ffn_sizes_ok(*args)) return CCONV_EINVAL;
@@ -301,12 +247,14 @@ int cconv_ffn_forward(const cconv_ffn_args* args, void* cuda_stream) {
     o.out(a.gate_pre, a.T, a.F, 2);
     o.out(a.up_pre, a.T, a.F, 2);
   }
-  o.workspace(a.workspace, a.workspace_bytes, ffn_space(a, false, nullptr).used);
-  if (!o.distinct()) return CCONV_EINVAL;
+  if (!o.ok) return CCONV_EINVAL;
   const int sms = block_sm_count();
   if (sms < 0) return sms;
+  o.workspace(a.workspace, a.workspace_bytes, ffn_empty(a) ? 0 : ffn_workspace(a, false, sms));
+  if (!o.distinct()) return CCONV_EINVAL;
   note_ordinary_launch(cuda_stream);
-  return ffn_forward(a, static_cast<cudaStream_t>(cuda_stream));
+  cudaStream_t s = static_cast<cudaStream_t>(cuda_stream);
+  return ffn_empty(a) ? ffn_zeros(a, false, s) : run_ffn(a, false, sms, s);
 }
 
 int cconv_ffn_backward(const cconv_ffn_args* args, void* cuda_stream) {
@@ -324,12 +272,14 @@ int cconv_ffn_backward(const cconv_ffn_args* args, void* cuda_stream) {
   o.out(a.dw_gate, a.F, a.D, 2);
   o.out(a.dw_up, a.F, a.D, 2);
   o.out(a.dw_down, a.D, a.F, 2);
-  o.workspace(a.workspace, a.workspace_bytes, ffn_space(a, true, nullptr).used);
-  if (!o.distinct()) return CCONV_EINVAL;
+  if (!o.ok) return CCONV_EINVAL;
   const int sms = block_sm_count();
   if (sms < 0) return sms;
+  o.workspace(a.workspace, a.workspace_bytes, ffn_empty(a) ? 0 : ffn_workspace(a, true, sms));
+  if (!o.distinct()) return CCONV_EINVAL;
   note_ordinary_launch(cuda_stream);
-  return ffn_backward(a, static_cast<cudaStream_t>(cuda_stream));
+  cudaStream_t s = static_cast<cudaStream_t>(cuda_stream);
+  return ffn_empty(a) ? ffn_zeros(a, true, s) : run_ffn(a, true, sms, s);
 }
 
 int64_t cconv_residual_norm_backward_workspace(const cconv_residual_norm_args* args) {
@@ -476,7 +426,20 @@ int cconv_quantize_blocks(const cconv_quantize_args* args, void* cuda_stream) {
 
 int cconv_block_status(void* cuda_stream, int* detail_out) {
   if (detail_out) *detail_out = 0;
-  return block_cuda_error(cudaStreamSynchronize(static_cast<cudaStream_t>(cuda_stream)), "cconv_block_status");
+  const int sms = block_sm_count();
+  if (sms < 0) return sms;
+  int* word = nullptr;
+  const int rc = block_status_word(&word);
+  if (rc != CCONV_OK) return rc;
+  cudaStream_t s = static_cast<cudaStream_t>(cuda_stream);
+  int bits = 0;
+  BLOCK_CUDA(cudaMemcpyAsync(&bits, word, sizeof bits, cudaMemcpyDeviceToHost, s));
+  BLOCK_CUDA(cudaStreamSynchronize(s));
+  if (bits == 0) return CCONV_OK;
+  if (detail_out) *detail_out = bits;
+  BLOCK_CUDA(cudaMemsetAsync(word, 0, sizeof bits, s));
+  BLOCK_CUDA(cudaStreamSynchronize(s));
+  return CCONV_EDEVICE_TIMEOUT;
 }
 
 }  // extern "C"

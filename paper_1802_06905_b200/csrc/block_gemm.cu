@@ -1,20 +1,464 @@
-// Products of the feed-forward block.
+// Products of the feed-forward block on pairs of CTAs.
+//
+// C = A B^T over a 256 x block_n tile a pair: each CTA keeps 128 rows of A and half the rows of B in shared
+// memory (64 elements of k a stage), one thread of the first CTA issues the MMAs of both (M = 256), and
+// each CTA's accumulators (128 x block_n, fp32) lie in its own tensor memory, twice, so that a tile's
+// epilogue runs beside the next tile's main loop.  A pair reads (256 + block_n) rows of k from L2 for
+// 256 x block_n products, half of what two CTAs on tiles of their own would: at 128 x 256 a CTA draws 96
+// bytes a clock, a pair of CTAs at 256 x 256 64 bytes a clock each, below what L2 delivers to an SM.
+//
+// Roles: warp 0 copies (TMA), warp 1 of the first CTA issues MMAs, warp 2 owns the tensor memory, warps
+// 2-9 are the epilogue (two for each quarter of the lanes, half of the columns each).
+#include <cstdlib>
+
 #include <cuda_fp8.h>
 
 #include "block.h"
 #include "block_device.cuh"
 #include "block_gemm.h"
+#include "pair_sm100.cuh"
 
 namespace cconv {
 namespace {
 
+constexpr int kThreads = 320;
+constexpr int kEpilogueWarps = 8;
+constexpr uint32_t kABytes = 128 * 128;  // a stage of A in one CTA: 128 rows x 128 bytes of k
+constexpr uint32_t kBoxBytes = 32 * 128; // a piece that an epilogue warp stages: 32 rows x 128 bytes
+constexpr uint32_t kTmemCols = 512;
+constexpr uint32_t kSmemMost = 232448;
+constexpr uint32_t kBarrierBytes = 512;
+
+__device__ int g_block_status;
+
+struct PairParams {
+  int tiles_m, tiles_n, tiles_m0;  // tiles_m0: rows of tiles of the first stacked product
+  int splits, kb_total, kb_split, kb_seg;
+  int block_n, stages;
+  uint32_t b_bytes;                // a stage of B in one CTA
+  uint32_t a_kmajor, b_kmajor, paired;
+  uint64_t a_desc, b_desc;
+  uint32_t a_step, b_step;         // descriptor step of 16 elements of k (16-byte units)
+  uint32_t idesc;
+  int64_t M, N;
+  int act, save, more;
+  float* partial;
+  int64_t pitch, slice;
+  int* status;
+  uint64_t limit_ns;
+};
+struct PairMaps {
+  CUtensorMap a[2], b[2], out[3], in[2];
+};
+
+// Tile t of the launch: share of k, row and column of tiles.  Tiles run down groups of 8 rows of tiles,
+// so that the pairs at work at one time read few different rows of A and B.
+struct Tile {
+  int split, m, n;
+};
+__device__ __forceinline__ Tile tile_of(const PairParams& p, int t) {
+  Tile r;
+  r.split = t % p.splits;
+  t /= p.splits;
+  const int group = 8 * p.tiles_n;
+  const int first = t / group * 8;
+  const int rows = min(8, p.tiles_m - first);
+  t %= group;
+  r.m = first + t % rows;
+  r.n = t / rows;
+  return r;
+}
+
+template <int N>
+__device__ __forceinline__ void load_sums(uint32_t taddr, float (&f)[N]) {
+  static_assert(N == 32, "");
+  uint32_t v[32];
+  tmem_ld_32x32b_x32(taddr, v);
+  tmem_ld_wait();
+#pragma unroll
+  for (int i = 0; i < 32; ++i) f[i] = __uint_as_float(v[i]);
+}
+
+// 16-byte chunk c of row r of a piece staged with 128-byte swizzle.
+__device__ __forceinline__ uint32_t chunk_at(uint32_t base, int r, int c) {
+  return base + r * 128 + ((c ^ (r & 7)) << 4);
+}
+template <typename T>
+__device__ __forceinline__ void stage32(uint32_t base, int r, int c0, const float (&f)[32]) {
+#pragma unroll
+  for (int c = 0; c < 4; ++c)
+    st_shared_v4(chunk_at(base, r, c0 + c), pack2<T>(f[8 * c], f[8 * c + 1]), pack2<T>(f[8 * c + 2], f[8 * c + 3]),
+                 pack2<T>(f[8 * c + 4], f[8 * c + 5]), pack2<T>(f[8 * c + 6], f[8 * c + 7]));
+}
+template <typename T>
+__device__ __forceinline__ void unstage32(uint32_t base, int r, int c0, float (&f)[32]) {
+#pragma unroll
+  for (int c = 0; c < 4; ++c) {
+    uint32_t w[4];
+    ld_shared_v4(chunk_at(base, r, c0 + c), w[0], w[1], w[2], w[3]);
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+      const float2 v = unpack2<T>(w[i]);
+      f[8 * c + 2 * i] = v.x;
+      f[8 * c + 2 * i + 1] = v.y;
+    }
+  }
+}
+
+template <int kEpi>
+constexpr int kPieces = kEpi == kStore ? 2 : kEpi == kPartial ? 0 : 3;  // staged by an epilogue warp
+int staged_pieces(int epi) { return epi == kStore ? 2 : epi == kPartial ? 0 : 3; }
+
+// A bounded wait whose outcome is the same in all lanes, so that a warp leaves as a whole.
+__device__ __forceinline__ bool wait_all(uint32_t bar, uint32_t parity, volatile int* abort_flag, int* status, int code,
+                                         uint64_t limit_ns) {
+  return __all_sync(0xffffffffu, mbar_wait_warp(bar, parity, abort_flag, status, code, limit_ns));
+}
+
+template <int kEpi, typename T>
+__global__ void __launch_bounds__(kThreads, 1) cconv_pair_product_kernel(const __grid_constant__ PairMaps maps,
+                                                                         const PairParams p) {
+  extern __shared__ uint8_t smem_raw[];
+  const uint32_t base = (smem_u32(smem_raw) + 1023u) & ~1023u;
+  const uint32_t stage_bytes = kABytes + p.b_bytes;
+  const uint32_t staging = base + p.stages * stage_bytes;
+  const uint32_t bars = staging + kEpilogueWarps * kPieces<kEpi> * kBoxBytes;
+  const uint32_t bar_full = bars, bar_empty = bars + 8 * p.stages;
+  const uint32_t bar_tfull = bar_empty + 8 * p.stages, bar_tempty = bar_tfull + 16, bar_in = bar_tempty + 16;
+  const uint32_t slot = bar_in + 8 * kEpilogueWarps;
+  volatile int* abort_p = reinterpret_cast<volatile int*>(smem_raw + (slot + 4 - smem_u32(smem_raw)));
+
+  const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+  const uint32_t rank = cluster_ctarank();
+  const int pair = blockIdx.x >> 1, pairs = gridDim.x >> 1;
+  const int tiles = p.tiles_m * p.tiles_n * p.splits;
+
+  if (threadIdx.x == 0) {
+    *abort_p = 0;
+    for (int i = 0; i < p.stages; ++i) {
+      mbar_init(bar_full + 8 * i, 1);
+      mbar_init(bar_empty + 8 * i, 1);
+    }
+    for (int i = 0; i < 2; ++i) {
+      mbar_init(bar_tfull + 8 * i, 1);
+      mbar_init(bar_tempty + 8 * i, 2 * kEpilogueWarps);
+    }
+    for (int i = 0; i < kEpilogueWarps; ++i) mbar_init(bar_in + 8 * i, 1);
+    fence_barrier_init();
+  }
+  if (warp == 2) {
+    pair_tmem_alloc(slot, kTmemCols);
+    pair_tmem_relinquish();
+  }
+  tc_fence_before();
+  __syncthreads();
+  cluster_sync_all();  // both CTAs' barriers are initialised
+  tc_fence_after();
+  uint32_t tmem;
+  asm volatile("ld.shared.b32 %0, [%1];" : "=r"(tmem) : "r"(slot));
+
+  asm volatile("griddepcontrol.wait;" ::: "memory");
+  if (p.more) asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
+
+  if (warp == 0) {
+    if (elect_one()) {
+      uint32_t s = 0, ph = 0;
+      const uint32_t full0 = cluster_map_shared(bar_full, 0);
+      const int box_b = int(p.b_bytes) / 8192;
+      bool ok = true;
+      for (int t = pair; ok && t < tiles; t += pairs) {
+        const Tile tl = tile_of(p, t);
+        const bool second = tl.m >= p.tiles_m0;
+        const int m0 = (second ? tl.m - p.tiles_m0 : tl.m) * 256 + int(rank) * 128;
+        const int n0 = p.paired ? tl.n * 128 : tl.n * p.block_n + int(rank) * (p.block_n >> 1);
+        const int k0 = tl.split * p.kb_split, k1 = min(p.kb_total, k0 + p.kb_split);
+        for (int kb = k0; kb < k1; ++kb) {
+          if (!mbar_wait(bar_empty + 8 * s, ph ^ 1, abort_p, p.status, kStatProducerWait, p.limit_ns)) {
+            ok = false;
+            break;
+          }
+          const bool seg = kb >= p.kb_seg;
+          const int k = (seg ? kb - p.kb_seg : kb) * 64;
+          const CUtensorMap* ma = &maps.a[seg || second];
+          const CUtensorMap* mb = &maps.b[seg || (p.paired && rank)];
+          const uint32_t a = base + s * stage_bytes, b = a + kABytes, bar = full0 + 8 * s;
+          if (rank == 0) mbar_arrive_expect_tx(bar_full + 8 * s, 2 * stage_bytes);
+          if (p.a_kmajor) {
+            tma_load_2d_pair(a, ma, k, m0, bar);
+          } else {
+            tma_load_2d_pair(a, ma, m0, k, bar);
+            tma_load_2d_pair(a + 8192, ma, m0 + 64, k, bar);
+          }
+          if (p.b_kmajor) {
+            tma_load_2d_pair(b, mb, k, n0, bar);
+          } else {
+            for (int i = 0; i < box_b; ++i) tma_load_2d_pair(b + 8192 * i, mb, n0 + 64 * i, k, bar);
+          }
+          if (++s == uint32_t(p.stages)) s = 0, ph ^= 1;
+        }
+      }
+    }
+  } else if (warp == 1) {
+    if (rank == 0) {
+      const bool issue = elect_one();
+      uint32_t s = 0, ph = 0, buf = 0, bph = 0;
+      bool ok = true;
+      for (int t = pair; ok && t < tiles; t += pairs) {
+        const Tile tl = tile_of(p, t);
+        const int k0 = tl.split * p.kb_split, k1 = min(p.kb_total, k0 + p.kb_split);
+        if (!wait_all(bar_tempty + 8 * buf, bph ^ 1, abort_p, p.status, kStatMmaWaitTmem, p.limit_ns)) break;
+        tc_fence_after();
+        const uint32_t d = tmem + buf * 256;
+        for (int kb = k0; kb < k1; ++kb) {
+          if (!wait_all(bar_full + 8 * s, ph, abort_p, p.status, kStatMmaWaitFull, p.limit_ns)) {
+            ok = false;
+            break;
+          }
+          tc_fence_after();
+          const uint32_t a = base + s * stage_bytes;
+          if (issue) {
+            const uint64_t da = p.a_desc + (a >> 4), db = p.b_desc + ((a + kABytes) >> 4);
+#pragma unroll
+            for (int j = 0; j < 4; ++j)
+              pair_mma_f16(d, da + j * p.a_step, db + j * p.b_step, p.idesc, kb > k0 || j > 0);
+            pair_commit(bar_empty + 8 * s);
+          }
+          __syncwarp();
+          if (++s == uint32_t(p.stages)) s = 0, ph ^= 1;
+        }
+        if (issue && ok) pair_commit(bar_tfull + 8 * buf);
+        __syncwarp();
+        if (++buf == 2) buf = 0, bph ^= 1;
+      }
+    }
+  } else {
+    const int q = warp & 3, half = (warp - 2) >> 2;
+    const uint32_t mine = staging + (warp - 2) * kPieces<kEpi> * kBoxBytes;
+    const uint32_t in_bar = bar_in + 8 * (warp - 2);
+    const uint32_t tempty0 = cluster_map_shared(bar_tempty, 0);
+    const uint32_t lanes = tmem + (uint32_t(q * 32) << 16);
+    uint32_t buf = 0, bph = 0, in_ph = 0, piece = 0;
+    for (int t = pair; t < tiles; t += pairs) {
+      const Tile tl = tile_of(p, t);
+      const bool second = tl.m >= p.tiles_m0;
+      const int row0 = (second ? tl.m - p.tiles_m0 : tl.m) * 256 + int(rank) * 128 + q * 32;
+      const uint32_t acc = lanes + buf * 256;
+      auto wait_sums = [&]() {
+        if (!wait_all(bar_tfull + 8 * buf, bph, abort_p, p.status, kStatEpilogueWait, p.limit_ns)) return false;
+        tc_fence_after();
+        return true;
+      };
+      auto release_sums = [&]() {
+        tc_fence_before();
+        __syncwarp();
+        if (lane == 0) mbar_arrive_cluster(tempty0 + 8 * buf);
+      };
+      if constexpr (kEpi == kStore) {
+        if (!wait_sums()) break;
+        const int cols = p.block_n >> 1;
+        for (int c = 0; c < cols; c += 64) {
+          float f[32], g[32];
+          load_sums(acc + half * cols + c, f);
+          load_sums(acc + half * cols + c + 32, g);
+          if (c + 64 >= cols) release_sums();
+          const uint32_t to = mine + piece * kBoxBytes;
+          if (lane == 0) bulk_wait_group_read<1>();
+          __syncwarp();
+          stage32<T>(to, lane, 0, f);
+          stage32<T>(to, lane, 4, g);
+          fence_proxy_async_smem();
+          __syncwarp();
+          if (lane == 0) {
+            const int col = tl.n * p.block_n + half * cols + c;
+            if (row0 < p.M && col < p.N) tma_store_2d(&maps.out[second], to, col, row0);
+            bulk_commit_group();
+          }
+          piece ^= 1;
+        }
+      } else if constexpr (kEpi == kGated) {
+        if (!wait_sums()) break;
+        const int col = tl.n * 128 + half * 64;
+        if (lane == 0) bulk_wait_group_read<0>();
+        __syncwarp();
+#pragma unroll 1
+        for (int c = 0; c < 2; ++c) {
+          float g[32], u[32];
+          load_sums(acc + half * 64 + c * 32, g);
+          load_sums(acc + 128 + half * 64 + c * 32, u);
+          if (c == 1) release_sums();
+          if (p.save) {
+            stage32<T>(mine + kBoxBytes, lane, c * 4, g);
+            stage32<T>(mine + 2 * kBoxBytes, lane, c * 4, u);
+          }
+          float unused;
+#pragma unroll
+          for (int i = 0; i < 32; ++i) g[i] = activation<false>(p.act, g[i], unused) * u[i];
+          stage32<T>(mine, lane, c * 4, g);
+        }
+        fence_proxy_async_smem();
+        __syncwarp();
+        if (lane == 0) {
+          if (row0 < p.M && col < p.N) {
+            tma_store_2d(&maps.out[0], mine, col, row0);
+            if (p.save) {
+              tma_store_2d(&maps.out[1], mine + kBoxBytes, col, row0);
+              tma_store_2d(&maps.out[2], mine + 2 * kBoxBytes, col, row0);
+            }
+          }
+          bulk_commit_group();
+        }
+      } else if constexpr (kEpi == kGatedBackward) {
+        const int cols = p.block_n >> 1;
+        bool first = true, ok = true;
+        for (int c = 0; c < cols; c += 64) {
+          const int col = tl.n * p.block_n + half * cols + c;
+          if (lane == 0) {
+            bulk_wait_group_read<0>();
+            mbar_arrive_expect_tx(in_bar, 2 * kBoxBytes);
+            tma_load_2d(mine, &maps.in[0], col, row0, in_bar);
+            tma_load_2d(mine + kBoxBytes, &maps.in[1], col, row0, in_bar);
+          }
+          if (first && !(ok = wait_sums())) break;
+          first = false;
+          if (!(ok = wait_all(in_bar, in_ph, abort_p, p.status, kStatEpilogueWait, p.limit_ns))) break;
+          in_ph ^= 1;
+#pragma unroll 1
+          for (int j = 0; j < 2; ++j) {
+            float d[32], g[32], u[32];
+            load_sums(acc + half * cols + c + j * 32, d);
+            if (j == 1 && c + 64 >= cols) release_sums();
+            unstage32<T>(mine, lane, j * 4, g);
+            unstage32<T>(mine + kBoxBytes, lane, j * 4, u);
+#pragma unroll
+            for (int i = 0; i < 32; ++i) {
+              float da;
+              const float a = activation<true>(p.act, g[i], da);
+              g[i] = d[i] * u[i] * da;
+              d[i] = d[i] * a;
+              u[i] = a * u[i];
+            }
+            stage32<T>(mine, lane, j * 4, g);
+            stage32<T>(mine + kBoxBytes, lane, j * 4, d);
+            stage32<T>(mine + 2 * kBoxBytes, lane, j * 4, u);
+          }
+          fence_proxy_async_smem();
+          __syncwarp();
+          if (lane == 0) {
+            if (row0 < p.M && col < p.N) {
+              tma_store_2d(&maps.out[0], mine, col, row0);
+              tma_store_2d(&maps.out[1], mine + kBoxBytes, col, row0);
+              tma_store_2d(&maps.out[2], mine + 2 * kBoxBytes, col, row0);
+            }
+            bulk_commit_group();
+          }
+        }
+        if (!ok) break;
+      } else {  // kPartial: lanes are neighbours along the table's rows; the table covers whole tiles
+        if (!wait_sums()) break;
+        const int cols = max(p.block_n >> 1, 32);
+        float* to = p.partial + tl.split * p.slice + int64_t(tl.m) * 256 + rank * 128 + q * 32 + lane;
+        if (half * cols < p.block_n) {
+          for (int c = 0; c < cols; c += 32) {
+            float f[32];
+            load_sums(acc + half * cols + c, f);
+            const int n = tl.n * p.block_n + half * cols + c;
+#pragma unroll
+            for (int i = 0; i < 32; ++i)
+              if (n + i < p.N) to[(n + i) * p.pitch] = f[i];
+          }
+        }
+        release_sums();
+      }
+      if (++buf == 2) buf = 0, bph ^= 1;
+    }
+    if (kPieces<kEpi> > 0 && lane == 0) bulk_wait_group<0>();
+  }
+
+  // A wait that ran out raised the flag a whole limit after the last copy or MMA was issued; the other
+  // roles leave within a poll of it.  A short pause lets what they issued last come to its end.
+  __syncwarp();
+  __syncthreads();
+  if (*abort_p) {
+    const uint64_t t0 = globaltimer_ns();
+    while (globaltimer_ns() - t0 < 200000) {
+    }
+  }
+  __syncwarp();
+  tc_fence_before();
+  cluster_sync_all();  // nothing arrives at, or reads, the other CTA's shared memory any more
+  tc_fence_after();
+  if (warp == 2) pair_tmem_dealloc(tmem, kTmemCols);
+}
+
+uint64_t wait_limit_ns() {
+  const char* v = std::getenv("CCONV_WAIT_LIMIT_MS");
+  return uint64_t(v && *v ? std::atoi(v) : 1000) * 1000000ull;
+}
+
+// An ordinary launch, or one that may start while the kernel in front of it (of the same call) ends; all
+// kernels here wait for that kernel before they touch memory.
+template <typename F, typename... Args>
+cudaError_t launch(F f, dim3 grid, int threads, size_t smem, int cluster, bool chained, cudaStream_t s, Args... args) {
+  cudaLaunchConfig_t cfg = {};
+  cfg.gridDim = grid;
+  cfg.blockDim = dim3(unsigned(threads));
+  cfg.dynamicSmemBytes = smem;
+  cfg.stream = s;
+  cudaLaunchAttribute attr[2];
+  int n = 0;
+  if (chained) {
+    attr[n].id = cudaLaunchAttributeProgrammaticStreamSerialization;
+    attr[n++].val.programmaticStreamSerializationAllowed = 1;
+  }
+  if (cluster > 1) {
+    attr[n].id = cudaLaunchAttributeClusterDimension;
+    attr[n].val.clusterDim.x = unsigned(cluster);
+    attr[n].val.clusterDim.y = 1;
+    attr[n++].val.clusterDim.z = 1;
+  }
+  cfg.attrs = attr;
+  cfg.numAttrs = unsigned(n);
+  return cudaLaunchKernelEx(&cfg, f, args...);
+}
+
+template <int kEpi, typename T>
+cudaError_t launch_pair(const PairMaps& maps, const PairParams& p, int sms, bool chained, cudaStream_t s) {
+  auto f = cconv_pair_product_kernel<kEpi, T>;
+  static bool ready[64] = {};
+  int dev = 0;
+  cudaError_t e = cudaGetDevice(&dev);
+  if (e != cudaSuccess) return e;
+  if (!__atomic_load_n(&ready[dev & 63], __ATOMIC_ACQUIRE)) {
+    e = cudaFuncSetAttribute(f, cudaFuncAttributeMaxDynamicSharedMemorySize, int(kSmemMost));
+    if (e != cudaSuccess) return e;
+    __atomic_store_n(&ready[dev & 63], true, __ATOMIC_RELEASE);
+  }
+  const int tiles = p.tiles_m * p.tiles_n * p.splits;
+  const int pairs = tiles < sms / 2 ? tiles : sms / 2;
+  const size_t smem = 1024 + size_t(p.stages) * (kABytes + p.b_bytes) + kEpilogueWarps * staged_pieces(kEpi) * kBoxBytes + kBarrierBytes;
+  return launch(f, dim3(unsigned(2 * pairs)), kThreads, smem, 2, chained, s, maps, p);
+}
+
+template <typename T>
+cudaError_t launch_epilogue(int epi, const PairMaps& maps, const PairParams& p, int sms, bool chained, cudaStream_t s) {
+  if (epi == kStore) return launch_pair<kStore, T>(maps, p, sms, chained, s);
+  if (epi == kGated) return launch_pair<kGated, T>(maps, p, sms, chained, s);
+  if (epi == kGatedBackward) return launch_pair<kGatedBackward, T>(maps, p, sms, chained, s);
+  return launch_pair<kPartial, T>(maps, p, sms, chained, s);
+}
+
+int encode_operand(CUtensorMap* tm, const Operand& o, int dtype, int rows_box) {
+  return o.kmajor ? encode_map(tm, o.p, 2, dtype, o.k, o.rows, o.pitch, 64, rows_box)
+                  : encode_map(tm, o.p, 2, dtype, o.rows, o.k, o.pitch, 64, 64);
+}
+
 __device__ __forceinline__ float to_f32(__nv_fp8_e4m3 v) { return float(v); }
 
-// 64 x 64 outputs a block of 256 threads, 4 x 4 a thread; k in steps of 16 through shared memory.
-// fp8: sums of 128 products are scaled before they are added up.
-template <typename T, typename Out, bool kFp8>
-__global__ void __launch_bounds__(256) cconv_product_kernel(Mat a, Mat b, Mat sa, Mat sb, Mat c, int64_t M,
-                                                            int64_t N, int64_t K, int add) {
+// 64 x 64 outputs a block of 256 threads, 4 x 4 a thread; k in steps of 16 through shared memory.  Sums
+// of 128 products are scaled before they are added up.
+template <typename T, typename Out>
+__global__ void __launch_bounds__(256) cconv_fp8_simple_kernel(Mat a, Mat b, Mat sa, Mat sb, Mat c, int64_t M,
+                                                               int64_t N, int64_t K) {
   __shared__ float as[16][65], bs[16][65];
   const int64_t m0 = int64_t(blockIdx.y) * 64, n0 = int64_t(blockIdx.x) * 64;
   const int tx = threadIdx.x & 15, ty = threadIdx.x >> 4;
@@ -35,7 +479,7 @@ __global__ void __launch_bounds__(256) cconv_product_kernel(Mat a, Mat b, Mat sa
 #pragma unroll
         for (int j = 0; j < 4; ++j) acc[i][j] += as[k][ty * 4 + i] * bs[k][tx * 4 + j];
     __syncthreads();
-    if (kFp8 && ((k0 + 16) % 128 == 0 || k0 + 16 >= K)) {
+    if ((k0 + 16) % 128 == 0 || k0 + 16 >= K) {
       for (int i = 0; i < 4; ++i)
         for (int j = 0; j < 4; ++j) {
           const int64_t m = m0 + ty * 4 + i, n = n0 + tx * 4 + j, kb = k0 / 128;
@@ -50,108 +494,222 @@ __global__ void __launch_bounds__(256) cconv_product_kernel(Mat a, Mat b, Mat sa
   for (int i = 0; i < 4; ++i)
     for (int j = 0; j < 4; ++j) {
       const int64_t m = m0 + ty * 4 + i, n = n0 + tx * 4 + j;
-      if (m >= M || n >= N) continue;
-      float v = kFp8 ? total[i][j] : acc[i][j];
-      Out* to = C + m * c.rs + n * c.cs;
-      if (add) v += cconv::to_f32(*to);
-      *to = from_f32<Out>(v);
+      if (m < M && n < N) C[m * c.rs + n * c.cs] = from_f32<Out>(total[i][j]);
     }
 }
 
-// Finishing passes over the sums: 256 threads a block along n, a row a blockIdx.y step.
+// ---- finishing passes: four neighbouring columns a thread, a row a blockIdx.y step -----------------
+__device__ __forceinline__ void add_up(const Partial& p, int64_t at, float (&f)[4]) {
+  float4 v = *reinterpret_cast<const float4*>(p.p + at);
+  for (int s = 1; s < p.splits; ++s) {
+    const float4 w = *reinterpret_cast<const float4*>(p.p + s * p.slice + at);
+    v.x += w.x; v.y += w.y; v.z += w.z; v.w += w.w;
+  }
+  f[0] = v.x; f[1] = v.y; f[2] = v.z; f[3] = v.w;
+}
 template <typename T>
-__global__ void __launch_bounds__(256) finish_store_kernel(const float* sums, Mat out, int64_t M, int64_t N) {
-  const int64_t n = int64_t(blockIdx.x) * 256 + threadIdx.x;
+__device__ __forceinline__ void put4(const Mat& m, int64_t r, int64_t c, int64_t N, const float (&f)[4]) {
+  T* o = static_cast<T*>(const_cast<void*>(m.p)) + r * m.rs + c * m.cs;
+#pragma unroll
+  for (int i = 0; i < 4; ++i)
+    if (c + i < N) o[i * m.cs] = from_f32<T>(f[i]);
+}
+template <typename T>
+__device__ __forceinline__ void get4(const Mat& m, int64_t r, int64_t c, int64_t N, float (&f)[4]) {
+  const T* o = static_cast<const T*>(m.p) + r * m.rs + c * m.cs;
+#pragma unroll
+  for (int i = 0; i < 4; ++i) f[i] = c + i < N ? to_f32(o[i * m.cs]) : 0.0f;
+}
+#define CCONV_FINISH_PROLOGUE                                                          \
+  asm volatile("griddepcontrol.wait;" ::: "memory");                                   \
+  if (more) asm volatile("griddepcontrol.launch_dependents;" ::: "memory");            \
+  const int64_t n = (int64_t(blockIdx.x) * 128 + threadIdx.x) * 4;                     \
   if (n >= N) return;
-  T* o = static_cast<T*>(const_cast<void*>(out.p));
-  for (int64_t m = blockIdx.y; m < M; m += gridDim.y) o[m * out.rs + n * out.cs] = from_f32<T>(sums[m * N + n]);
+
+template <typename T>
+__global__ void __launch_bounds__(128) finish_store_kernel(Partial p, Mat out, int64_t M, int64_t N, int more) {
+  CCONV_FINISH_PROLOGUE
+  for (int64_t m = blockIdx.y; m < M; m += gridDim.y) {
+    float f[4];
+    add_up(p, m * p.pitch + n, f);
+    put4<T>(out, m, n, N, f);
+  }
 }
 
 template <typename T>
-__global__ void __launch_bounds__(256) finish_gated_kernel(const float* g, const float* u, Mat gate_pre, Mat up_pre,
-                                                           Mat h, int64_t M, int64_t N, int act) {
-  const int64_t n = int64_t(blockIdx.x) * 256 + threadIdx.x;
-  if (n >= N) return;
+__global__ void __launch_bounds__(128) finish_gated_kernel(Partial p, Mat gate_pre, Mat up_pre, Mat h, int64_t M,
+                                                           int64_t N, int act, int more) {
+  CCONV_FINISH_PROLOGUE
   for (int64_t m = blockIdx.y; m < M; m += gridDim.y) {
-    float da;
-    const float gv = g[m * N + n], uv = u[m * N + n];
-    static_cast<T*>(const_cast<void*>(h.p))[m * h.rs + n * h.cs] = from_f32<T>(activation<false>(act, gv, da) * uv);
+    float g[4], u[4], f[4], da;
+    add_up(p, m * p.pitch + n, g);
+    add_up(p, m * p.pitch + p.second + n, u);
+#pragma unroll
+    for (int i = 0; i < 4; ++i) f[i] = activation<false>(act, g[i], da) * u[i];
+    put4<T>(h, m, n, N, f);
     if (gate_pre.p) {
-      static_cast<T*>(const_cast<void*>(gate_pre.p))[m * gate_pre.rs + n * gate_pre.cs] = from_f32<T>(gv);
-      static_cast<T*>(const_cast<void*>(up_pre.p))[m * up_pre.rs + n * up_pre.cs] = from_f32<T>(uv);
+      put4<T>(gate_pre, m, n, N, g);
+      put4<T>(up_pre, m, n, N, u);
     }
   }
 }
 
 template <typename T>
-__global__ void __launch_bounds__(256) finish_gated_backward_kernel(const float* dh, Mat gate_pre, Mat up_pre,
-                                                                    Mat dg, Mat du, Mat h, int64_t M, int64_t N,
-                                                                    int act) {
-  const int64_t n = int64_t(blockIdx.x) * 256 + threadIdx.x;
-  if (n >= N) return;
+__global__ void __launch_bounds__(128) finish_gated_backward_kernel(Partial p, Mat gate_pre, Mat up_pre, Mat dg,
+                                                                    Mat du, Mat h, int64_t M, int64_t N, int act,
+                                                                    int more) {
+  CCONV_FINISH_PROLOGUE
   for (int64_t m = blockIdx.y; m < M; m += gridDim.y) {
-    const float g = to_f32(static_cast<const T*>(gate_pre.p)[m * gate_pre.rs + n * gate_pre.cs]);
-    const float u = to_f32(static_cast<const T*>(up_pre.p)[m * up_pre.rs + n * up_pre.cs]);
-    const float d = dh[m * N + n];
-    float da;
-    const float a = activation<true>(act, g, da);
-    static_cast<T*>(const_cast<void*>(dg.p))[m * dg.rs + n * dg.cs] = from_f32<T>(d * u * da);
-    static_cast<T*>(const_cast<void*>(du.p))[m * du.rs + n * du.cs] = from_f32<T>(d * a);
-    static_cast<T*>(const_cast<void*>(h.p))[m * h.rs + n * h.cs] = from_f32<T>(a * u);
+    float d[4], g[4], u[4], f[4];
+    get4<T>(gate_pre, m, n, N, g);
+    get4<T>(up_pre, m, n, N, u);
+    add_up(p, m * p.pitch + n, d);
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+      float da;
+      const float a = activation<true>(act, g[i], da);
+      g[i] = d[i] * u[i] * da;
+      f[i] = d[i] * a;
+      u[i] = a * u[i];
+    }
+    put4<T>(dg, m, n, N, g);
+    put4<T>(du, m, n, N, f);
+    put4<T>(h, m, n, N, u);
   }
 }
 
-dim3 product_grid(int64_t M, int64_t N) { return dim3(unsigned(cdiv64(N, 64)), unsigned(cdiv64(M, 64))); }
-dim3 finish_grid(int64_t M, int64_t N) { return dim3(unsigned(cdiv64(N, 256)), unsigned(M < 16384 ? M : 16384)); }
+// 32 x 32 elements a block through shared memory: read along the source's short stride, written along
+// the target's.
+template <typename E>
+__global__ void __launch_bounds__(256) cconv_copy_kernel(Mat from, Mat to, int64_t rows, int64_t cols, int more) {
+  __shared__ E tile[32][33];
+  asm volatile("griddepcontrol.wait;" ::: "memory");
+  if (more) asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
+  const E* src = static_cast<const E*>(from.p);
+  E* dst = static_cast<E*>(const_cast<void*>(to.p));
+  const int x = threadIdx.x & 31, y = threadIdx.x >> 5;
+  const int64_t c0 = int64_t(blockIdx.x) * 32;
+  for (int64_t r0 = int64_t(blockIdx.y) * 32; r0 < rows; r0 += int64_t(gridDim.y) * 32) {
+    const bool by_rows = from.rs < from.cs;  // neighbours in memory are rows
+    for (int i = y; i < 32; i += 8) {
+      const int r = by_rows ? x : i, c = by_rows ? i : x;
+      if (r0 + r < rows && c0 + c < cols) tile[r][c] = src[(r0 + r) * from.rs + (c0 + c) * from.cs];
+    }
+    __syncthreads();
+    const bool to_rows = to.rs < to.cs;
+    for (int i = y; i < 32; i += 8) {
+      const int r = to_rows ? x : i, c = to_rows ? i : x;
+      if (r0 + r < rows && c0 + c < cols) dst[(r0 + r) * to.rs + (c0 + c) * to.cs] = tile[r][c];
+    }
+    __syncthreads();
+  }
+}
+
+dim3 finish_grid(int64_t M, int64_t N) { return dim3(unsigned(cdiv64(N, 512)), unsigned(M < 16384 ? M : 16384)); }
 
 }  // namespace
 
-cudaError_t run_product_simple(const Mat& a, const Mat& b, float* c, int64_t M, int64_t N, int64_t K, int dtype,
-                               bool add, cudaStream_t s) {
-  const Mat cm(c, N, 1), none;
-  if (dtype == CCONV_TYPE_BF16)
-    cconv_product_kernel<__nv_bfloat16, float, false><<<product_grid(M, N), 256, 0, s>>>(a, b, none, none, cm, M, N, K, add);
-  else
-    cconv_product_kernel<__half, float, false><<<product_grid(M, N), 256, 0, s>>>(a, b, none, none, cm, M, N, K, add);
-  return cudaGetLastError();
+int block_status_word(int** word) {
+  void* p = nullptr;
+  const cudaError_t e = cudaGetSymbolAddress(&p, g_block_status);
+  *word = static_cast<int*>(p);
+  return block_cuda_error(e, "cudaGetSymbolAddress");
+}
+
+int64_t partial_rows(int64_t M, int stack) { return cdiv64(M, 256) * 256 * stack; }
+
+cudaError_t run_product(const Product& p, int sms, bool chained, bool more, cudaStream_t s, int* rc) {
+  PairMaps maps;
+  PairParams q{};
+  *rc = block_status_word(&q.status);
+  if (*rc) return cudaSuccess;
+  const int stack = p.stacked ? 2 : 1;
+  q.tiles_m0 = int(cdiv64(p.M, 256));
+  q.tiles_m = q.tiles_m0 * stack;
+  q.tiles_n = int(cdiv64(p.N, p.paired ? 128 : p.block_n));
+  q.kb_seg = int(cdiv64(p.K, 64));
+  q.kb_total = q.kb_seg * (p.segments ? 2 : 1);
+  q.kb_split = int(cdiv64(q.kb_total, p.splits));
+  q.splits = int(cdiv64(q.kb_total, q.kb_split));
+  q.block_n = p.block_n;
+  q.b_bytes = uint32_t(p.block_n / 2) * 128;
+  const uint32_t staged = kEpilogueWarps * staged_pieces(p.epilogue) * kBoxBytes;
+  q.stages = int((kSmemMost - 1024 - kBarrierBytes - staged) / (kABytes + q.b_bytes));
+  if (q.stages > 8) q.stages = 8;
+  q.a_kmajor = p.a[0].kmajor;
+  q.b_kmajor = p.b[0].kmajor;
+  q.paired = p.paired;
+  q.a_desc = swizzled_desc(p.a[0].kmajor, 8192);
+  q.b_desc = swizzled_desc(p.b[0].kmajor, 8192);
+  q.a_step = p.a[0].kmajor ? 32 >> 4 : 2048 >> 4;
+  q.b_step = p.b[0].kmajor ? 32 >> 4 : 2048 >> 4;
+  const uint32_t type = p.dtype == CCONV_TYPE_BF16 ? 1u : 0u;
+  // instruction descriptor: D fp32, types of A and B, their orders (1: rows contiguous), N / 8, M / 16
+  q.idesc = (1u << 4) | (type << 7) | (type << 10) | (uint32_t(!p.a[0].kmajor) << 15) |
+            (uint32_t(!p.b[0].kmajor) << 16) | (uint32_t(p.block_n >> 3) << 17) | (uint32_t(256 >> 4) << 24);
+  q.M = p.M;
+  q.N = p.N;
+  q.act = p.act;
+  q.save = p.save;
+  q.more = more;
+  q.partial = p.partial;
+  q.pitch = p.pitch;
+  q.slice = p.slice;
+  q.limit_ns = wait_limit_ns();
+  const int two_a = p.segments || p.stacked ? 2 : 1, two_b = p.segments || p.paired ? 2 : 1;
+  for (int i = 0; i < 2; ++i) {
+    if ((*rc = encode_operand(&maps.a[i], p.a[i < two_a ? i : 0], p.dtype, 128))) return cudaSuccess;
+    if ((*rc = encode_operand(&maps.b[i], p.b[i < two_b ? i : 0], p.dtype, p.block_n / 2))) return cudaSuccess;
+  }
+  for (int i = 0; i < 5; ++i) {
+    const Mat& m = i < 3 ? p.out[i] : p.in[i - 3];
+    CUtensorMap* tm = i < 3 ? &maps.out[i] : &maps.in[i - 3];
+    *tm = maps.a[0];
+    if (m.p && (*rc = encode_map(tm, m.p, 2, p.dtype, p.N, p.M, m.rs, 64, 32))) return cudaSuccess;
+  }
+  return p.dtype == CCONV_TYPE_BF16 ? launch_epilogue<__nv_bfloat16>(p.epilogue, maps, q, sms, chained, s)
+                                    : launch_epilogue<__half>(p.epilogue, maps, q, sms, chained, s);
 }
 
 cudaError_t run_fp8_simple(const Mat& a, const Mat& b, const Mat& sa, const Mat& sb, const Mat& c, int64_t M,
                            int64_t N, int64_t K, int dtype, cudaStream_t s) {
   using E = __nv_fp8_e4m3;
-  const dim3 grid = product_grid(M, N);
+  const dim3 grid(unsigned(cdiv64(N, 64)), unsigned(cdiv64(M, 64)));
   if (dtype == CCONV_TYPE_BF16)
-    cconv_product_kernel<E, __nv_bfloat16, true><<<grid, 256, 0, s>>>(a, b, sa, sb, c, M, N, K, 0);
+    cconv_fp8_simple_kernel<E, __nv_bfloat16><<<grid, 256, 0, s>>>(a, b, sa, sb, c, M, N, K);
   else if (dtype == CCONV_TYPE_FP16)
-    cconv_product_kernel<E, __half, true><<<grid, 256, 0, s>>>(a, b, sa, sb, c, M, N, K, 0);
+    cconv_fp8_simple_kernel<E, __half><<<grid, 256, 0, s>>>(a, b, sa, sb, c, M, N, K);
   else
-    cconv_product_kernel<E, float, true><<<grid, 256, 0, s>>>(a, b, sa, sb, c, M, N, K, 0);
+    cconv_fp8_simple_kernel<E, float><<<grid, 256, 0, s>>>(a, b, sa, sb, c, M, N, K);
   return cudaGetLastError();
 }
 
-cudaError_t finish_store(const float* sums, const Mat& out, int64_t M, int64_t N, int dtype, cudaStream_t s) {
-  if (dtype == CCONV_TYPE_BF16) finish_store_kernel<__nv_bfloat16><<<finish_grid(M, N), 256, 0, s>>>(sums, out, M, N);
-  else finish_store_kernel<__half><<<finish_grid(M, N), 256, 0, s>>>(sums, out, M, N);
-  return cudaGetLastError();
-}
-
-cudaError_t finish_gated(const float* g, const float* u, const Mat& gate_pre, const Mat& up_pre, const Mat& h,
-                         int64_t M, int64_t N, int act, int dtype, cudaStream_t s) {
+cudaError_t finish_store(const Partial& p, const Mat& out, int64_t M, int64_t N, int dtype, bool more, cudaStream_t s) {
   if (dtype == CCONV_TYPE_BF16)
-    finish_gated_kernel<__nv_bfloat16><<<finish_grid(M, N), 256, 0, s>>>(g, u, gate_pre, up_pre, h, M, N, act);
-  else
-    finish_gated_kernel<__half><<<finish_grid(M, N), 256, 0, s>>>(g, u, gate_pre, up_pre, h, M, N, act);
-  return cudaGetLastError();
+    return launch(finish_store_kernel<__nv_bfloat16>, finish_grid(M, N), 128, 0, 1, true, s, p, out, M, N, int(more));
+  return launch(finish_store_kernel<__half>, finish_grid(M, N), 128, 0, 1, true, s, p, out, M, N, int(more));
 }
 
-cudaError_t finish_gated_backward(const float* dh, const Mat& gate_pre, const Mat& up_pre, const Mat& dg,
-                                  const Mat& du, const Mat& h, int64_t M, int64_t N, int act, int dtype,
+cudaError_t finish_gated(const Partial& p, const Mat& gate_pre, const Mat& up_pre, const Mat& h, int64_t M, int64_t N,
+                         int act, int dtype, bool more, cudaStream_t s) {
+  auto f = dtype == CCONV_TYPE_BF16 ? finish_gated_kernel<__nv_bfloat16> : finish_gated_kernel<__half>;
+  return launch(f, finish_grid(M, N), 128, 0, 1, true, s, p, gate_pre, up_pre, h, M, N, act, int(more));
+}
+
+cudaError_t finish_gated_backward(const Partial& p, const Mat& gate_pre, const Mat& up_pre, const Mat& dg,
+                                  const Mat& du, const Mat& h, int64_t M, int64_t N, int act, int dtype, bool more,
                                   cudaStream_t s) {
-  if (dtype == CCONV_TYPE_BF16)
-    finish_gated_backward_kernel<__nv_bfloat16><<<finish_grid(M, N), 256, 0, s>>>(dh, gate_pre, up_pre, dg, du, h, M, N, act);
-  else
-    finish_gated_backward_kernel<__half><<<finish_grid(M, N), 256, 0, s>>>(dh, gate_pre, up_pre, dg, du, h, M, N, act);
-  return cudaGetLastError();
+  auto f = dtype == CCONV_TYPE_BF16 ? finish_gated_backward_kernel<__nv_bfloat16> : finish_gated_backward_kernel<__half>;
+  return launch(f, finish_grid(M, N), 128, 0, 1, true, s, p, gate_pre, up_pre, dg, du, h, M, N, act, int(more));
+}
+
+cudaError_t run_copy(const Mat& from, const Mat& to, int64_t rows, int64_t cols, int es, bool chained, bool more,
+                     cudaStream_t s) {
+  if (rows == 0 || cols == 0) return cudaSuccess;
+  const int64_t y = cdiv64(rows, 32);
+  const dim3 grid(unsigned(cdiv64(cols, 32)), unsigned(y < 65535 ? y : 65535));
+  if (es == 1) return launch(cconv_copy_kernel<uint8_t>, grid, 256, 0, 1, chained, s, from, to, rows, cols, int(more));
+  return launch(cconv_copy_kernel<uint16_t>, grid, 256, 0, 1, chained, s, from, to, rows, cols, int(more));
 }
 
 }  // namespace cconv
