@@ -6,6 +6,7 @@
 
 #include "block.h"
 #include "block_ffn.h"
+#include "block_fp8.h"
 #include "block_gemm.h"
 #include "block_norm.h"
 #include "block_quant.h"
@@ -223,6 +224,8 @@ bool fp8_sizes_ok(const cconv_fp8_product_args& a) {
          double(a.N) * a.K < 1e15;
 }
 
+bool fp8_empty(const cconv_fp8_product_args& a) { return a.M == 0 || a.N == 0 || a.K == 0; }
+
 }  // namespace
 }  // namespace cconv
 
@@ -375,7 +378,9 @@ int cconv_residual_norm_backward(const cconv_residual_norm_args* args, void* cud
 
 int64_t cconv_fp8_product_workspace(const cconv_fp8_product_args* args) {
   if (!args || !fp8_sizes_ok(*args)) return CCONV_EINVAL;
-  return 0;
+  const int sms = block_sm_count();
+  if (sms < 0) return sms;
+  return fp8_empty(*args) ? 0 : fp8_workspace(*args, sms);
 }
 
 int cconv_fp8_product(const cconv_fp8_product_args* args, void* cuda_stream) {
@@ -388,15 +393,15 @@ int cconv_fp8_product(const cconv_fp8_product_args* args, void* cuda_stream) {
   o.in(a.a_scale, a.M, cdiv64(a.K, 128), 4);
   o.in(a.b_scale, cdiv64(a.N, 128), cdiv64(a.K, 128), 4);
   o.out(a.c, a.M, a.N, es);
-  if (!o.distinct()) return CCONV_EINVAL;
+  if (!o.ok) return CCONV_EINVAL;
   const int sms = block_sm_count();
   if (sms < 0) return sms;
-  if (a.M == 0 || a.N == 0) return CCONV_OK;
+  o.workspace(a.workspace, a.workspace_bytes, fp8_empty(a) ? 0 : fp8_workspace(a, sms));
+  if (!o.distinct()) return CCONV_EINVAL;
   cudaStream_t s = static_cast<cudaStream_t>(cuda_stream);
   note_ordinary_launch(cuda_stream);
-  if (a.K == 0) return block_cuda_error(zero_out(a.c, a.M, a.N, es, s), "cconv_fp8_product");
-  return block_cuda_error(run_fp8_simple(Mat(a.a), Mat(a.b), Mat(a.a_scale), Mat(a.b_scale), Mat(a.c), a.M, a.N, a.K,
-                                         a.dtype, s), "cconv_fp8_product");
+  if (fp8_empty(a)) return block_cuda_error(zero_out(a.c, a.M, a.N, es, s), "cconv_fp8_product");
+  return run_fp8(a, sms, s);
 }
 
 int cconv_quantize_blocks(const cconv_quantize_args* args, void* cuda_stream) {

@@ -11,8 +11,6 @@
 // 2-9 are the epilogue (two for each quarter of the lanes, half of the columns each).
 #include <cstdlib>
 
-#include <cuda_fp8.h>
-
 #include "block.h"
 #include "block_device.cuh"
 #include "block_gemm.h"
@@ -44,6 +42,9 @@ struct PairParams {
   int act, save, more;
   float* partial;
   int64_t pitch, slice;
+  // 8-bit operands: scale of row r (or of 128 rows) and k block kb at row_scale[i * row_rs + kb * row_ks]
+  const float *row_scale, *col_scale;
+  int64_t row_rs, row_ks, col_rs, col_ks;
   int* status;
   uint64_t limit_ns;
 };
@@ -105,9 +106,29 @@ __device__ __forceinline__ void unstage32(uint32_t base, int r, int c0, float (&
   }
 }
 
+// Pieces that an epilogue warp stages.
 template <int kEpi>
-constexpr int kPieces = kEpi == kStore ? 2 : kEpi == kPartial ? 0 : 3;  // staged by an epilogue warp
-int staged_pieces(int epi) { return epi == kStore ? 2 : epi == kPartial ? 0 : 3; }
+constexpr int kPieces = kEpi == kStore || kEpi == kScaled ? 2 : kEpi == kPartial || kEpi == kScaledPartial ? 0 : 3;
+int staged_pieces(int epi) {
+  return epi == kStore || epi == kScaled ? 2 : epi == kPartial || epi == kScaledPartial ? 0 : 3;
+}
+template <int kEpi>
+constexpr bool kEightBit = kEpi == kScaled || kEpi == kScaledPartial;
+
+// Two fp32 multiply-adds in one instruction: d = a * {s, s} + d.
+__device__ __forceinline__ void fma2(float2& d, float a0, float a1, float s) {
+  asm("{\n\t.reg .b64 x, y, z;\n\t"
+      "mov.b64 x, {%2, %3};\n\tmov.b64 y, {%4, %4};\n\tmov.b64 z, {%0, %1};\n\t"
+      "fma.rn.f32x2 z, x, y, z;\n\tmov.b64 {%0, %1}, z;\n\t}"
+      : "+f"(d.x), "+f"(d.y)
+      : "f"(a0), "f"(a1), "f"(s));
+}
+__device__ __forceinline__ void stage_f32(uint32_t base, int r, const float* f) {
+#pragma unroll
+  for (int c = 0; c < 8; ++c)
+    st_shared_v4(chunk_at(base, r, c), __float_as_uint(f[4 * c]), __float_as_uint(f[4 * c + 1]),
+                 __float_as_uint(f[4 * c + 2]), __float_as_uint(f[4 * c + 3]));
+}
 
 // A bounded wait whose outcome is the same in all lanes, so that a warp leaves as a whole.
 __device__ __forceinline__ bool wait_all(uint32_t bar, uint32_t parity, volatile int* abort_flag, int* status, int code,
@@ -178,7 +199,7 @@ __global__ void __launch_bounds__(kThreads, 1) cconv_pair_product_kernel(const _
             break;
           }
           const bool seg = kb >= p.kb_seg;
-          const int k = (seg ? kb - p.kb_seg : kb) * 64;
+          const int k = (seg ? kb - p.kb_seg : kb) * (kEightBit<kEpi> ? 128 : 64);
           const CUtensorMap* ma = &maps.a[seg || second];
           const CUtensorMap* mb = &maps.b[seg || (p.paired && rank)];
           const uint32_t a = base + s * stage_bytes, b = a + kABytes, bar = full0 + 8 * s;
@@ -206,10 +227,18 @@ __global__ void __launch_bounds__(kThreads, 1) cconv_pair_product_kernel(const _
       for (int t = pair; ok && t < tiles; t += pairs) {
         const Tile tl = tile_of(p, t);
         const int k0 = tl.split * p.kb_split, k1 = min(p.kb_total, k0 + p.kb_split);
-        if (!wait_all(bar_tempty + 8 * buf, bph ^ 1, abort_p, p.status, kStatMmaWaitTmem, p.limit_ns)) break;
-        tc_fence_after();
-        const uint32_t d = tmem + buf * 256;
+        if constexpr (!kEightBit<kEpi>) {
+          if (!wait_all(bar_tempty + 8 * buf, bph ^ 1, abort_p, p.status, kStatMmaWaitTmem, p.limit_ns)) break;
+          tc_fence_after();
+        }
         for (int kb = k0; kb < k1; ++kb) {
+          if constexpr (kEightBit<kEpi>) {  // sums of one block of 128 a time
+            if (!wait_all(bar_tempty + 8 * buf, bph ^ 1, abort_p, p.status, kStatMmaWaitTmem, p.limit_ns)) {
+              ok = false;
+              break;
+            }
+          }
+          const uint32_t d = tmem + buf * 256;
           if (!wait_all(bar_full + 8 * s, ph, abort_p, p.status, kStatMmaWaitFull, p.limit_ns)) {
             ok = false;
             break;
@@ -219,16 +248,24 @@ __global__ void __launch_bounds__(kThreads, 1) cconv_pair_product_kernel(const _
           if (issue) {
             const uint64_t da = p.a_desc + (a >> 4), db = p.b_desc + ((a + kABytes) >> 4);
 #pragma unroll
-            for (int j = 0; j < 4; ++j)
-              pair_mma_f16(d, da + j * p.a_step, db + j * p.b_step, p.idesc, kb > k0 || j > 0);
+            for (int j = 0; j < 4; ++j) {
+              if constexpr (kEightBit<kEpi>) pair_mma_f8(d, da + j * 2, db + j * 2, p.idesc, j > 0);
+              else pair_mma_f16(d, da + j * p.a_step, db + j * p.b_step, p.idesc, kb > k0 || j > 0);
+            }
             pair_commit(bar_empty + 8 * s);
+            if constexpr (kEightBit<kEpi>) pair_commit(bar_tfull + 8 * buf);
           }
           __syncwarp();
+          if constexpr (kEightBit<kEpi>) {
+            if (++buf == 2) buf = 0, bph ^= 1;
+          }
           if (++s == uint32_t(p.stages)) s = 0, ph ^= 1;
         }
-        if (issue && ok) pair_commit(bar_tfull + 8 * buf);
-        __syncwarp();
-        if (++buf == 2) buf = 0, bph ^= 1;
+        if constexpr (!kEightBit<kEpi>) {
+          if (issue && ok) pair_commit(bar_tfull + 8 * buf);
+          __syncwarp();
+          if (++buf == 2) buf = 0, bph ^= 1;
+        }
       }
     }
   } else {
@@ -242,7 +279,7 @@ __global__ void __launch_bounds__(kThreads, 1) cconv_pair_product_kernel(const _
       const Tile tl = tile_of(p, t);
       const bool second = tl.m >= p.tiles_m0;
       const int row0 = (second ? tl.m - p.tiles_m0 : tl.m) * 256 + int(rank) * 128 + q * 32;
-      const uint32_t acc = lanes + buf * 256;
+      uint32_t acc = lanes + buf * 256;
       auto wait_sums = [&]() {
         if (!wait_all(bar_tfull + 8 * buf, bph, abort_p, p.status, kStatEpilogueWait, p.limit_ns)) return false;
         tc_fence_after();
@@ -353,6 +390,110 @@ __global__ void __launch_bounds__(kThreads, 1) cconv_pair_product_kernel(const _
           }
         }
         if (!ok) break;
+      } else if constexpr (kEpi == kScaled) {
+        // Each block's sums are scaled and added up in registers (a row of half the columns a thread),
+        // beside the MMAs of the next block: 128 columns are 64 two-wide multiply-adds.
+        const int cols = p.block_n >> 1;
+        const int k0 = tl.split * p.kb_split, k1 = min(p.kb_total, k0 + p.kb_split);
+        const float* sa = p.row_scale + min(int64_t(row0 + lane), p.M - 1) * p.row_rs;
+        const int64_t nb = (int64_t(tl.n) * p.block_n + half * cols) >> 7;
+        const float* sb = p.col_scale + min(nb, (p.N - 1) >> 7) * p.col_rs;
+        float2 sum[64];
+#pragma unroll
+        for (int i = 0; i < 64; ++i) sum[i] = make_float2(0.0f, 0.0f);
+        float na = sa[k0 * p.row_ks], nbs = sb[k0 * p.col_ks];
+        bool ok = true;
+        for (int kb = k0; kb < k1; ++kb) {
+          const float scale = na * nbs;
+          if (kb + 1 < k1) {
+            na = sa[(kb + 1) * p.row_ks];
+            nbs = sb[(kb + 1) * p.col_ks];
+          }
+          if (!(ok = wait_sums())) break;
+#pragma unroll
+          for (int c = 0; c < 4; ++c) {
+            if (c * 32 < cols) {
+              float f[32];
+              load_sums(acc + half * cols + c * 32, f);
+              if ((c + 1) * 32 >= cols) release_sums();
+#pragma unroll
+              for (int i = 0; i < 16; ++i) fma2(sum[c * 16 + i], f[2 * i], f[2 * i + 1], scale);
+            }
+          }
+          if (++buf == 2) buf = 0, bph ^= 1;
+          acc = lanes + buf * 256;
+        }
+        if (!ok) break;
+        constexpr int kWidth = 128 / int(sizeof(T));  // columns of a piece
+#pragma unroll
+        for (int c = 0; c < 128; c += kWidth) {
+          if (c < cols) {
+            const uint32_t to = mine + piece * kBoxBytes;
+            if (lane == 0) bulk_wait_group_read<1>();
+            __syncwarp();
+            const float* f = reinterpret_cast<const float*>(&sum[c / 2]);
+            if constexpr (sizeof(T) == 4) {
+              stage_f32(to, lane, f);
+            } else {
+#pragma unroll
+              for (int j = 0; j < 8; ++j)
+                st_shared_v4(chunk_at(to, lane, j), pack2<T>(f[8 * j], f[8 * j + 1]), pack2<T>(f[8 * j + 2], f[8 * j + 3]),
+                             pack2<T>(f[8 * j + 4], f[8 * j + 5]), pack2<T>(f[8 * j + 6], f[8 * j + 7]));
+            }
+            fence_proxy_async_smem();
+            __syncwarp();
+            if (lane == 0) {
+              const int col = tl.n * p.block_n + half * cols + c;
+              if (row0 < p.M && col < p.N) tma_store_2d(&maps.out[0], to, col, row0);
+              bulk_commit_group();
+            }
+            piece ^= 1;
+          }
+        }
+        continue;  // the buffers were handed on block by block
+      } else if constexpr (kEpi == kScaledPartial) {
+        // As kPartial, of 8-bit operands: rows are features (128 of a CTA share a scale), columns tokens
+        // (a scale each, held by one lane and passed round).
+        const int cols = max(p.block_n >> 1, 32);
+        const int k0 = tl.split * p.kb_split, k1 = min(p.kb_total, k0 + p.kb_split);
+        const bool busy = half * cols < p.block_n;
+        const int n = tl.n * p.block_n + half * cols;
+        const int64_t mb = min(int64_t(row0) >> 7, (p.M - 1) >> 7);
+        float2 sum[64];
+#pragma unroll
+        for (int i = 0; i < 64; ++i) sum[i] = make_float2(0.0f, 0.0f);
+        bool ok = true;
+        for (int kb = k0; kb < k1; ++kb) {
+          const float sb = p.row_scale[mb * p.row_rs + kb * p.row_ks];
+          float sa[4];
+#pragma unroll
+          for (int c = 0; c < 4; ++c)
+            sa[c] = c * 32 < cols ? sb * p.col_scale[min(int64_t(n + c * 32 + lane), p.N - 1) * p.col_rs + kb * p.col_ks] : 0.0f;
+          if (!(ok = wait_sums())) break;
+          if (busy) {
+#pragma unroll
+            for (int c = 0; c < 4; ++c) {
+              if (c * 32 < cols) {
+                float f[32];
+                load_sums(acc + half * cols + c * 32, f);
+#pragma unroll
+                for (int i = 0; i < 16; ++i) {
+                  sum[c * 16 + i].x += f[2 * i] * __shfl_sync(0xffffffffu, sa[c], 2 * i);
+                  sum[c * 16 + i].y += f[2 * i + 1] * __shfl_sync(0xffffffffu, sa[c], 2 * i + 1);
+                }
+              }
+            }
+          }
+          release_sums();
+          if (++buf == 2) buf = 0, bph ^= 1;
+          acc = lanes + buf * 256;
+        }
+        if (!ok) break;
+        float* to = p.partial + tl.split * p.slice + int64_t(tl.m) * 256 + rank * 128 + q * 32 + lane;
+#pragma unroll
+        for (int c = 0; c < 128; ++c)
+          if (busy && c < cols && n + c < p.N) to[(n + c) * p.pitch] = c & 1 ? sum[c / 2].y : sum[c / 2].x;
+        continue;
       } else {  // kPartial: lanes are neighbours along the table's rows; the table covers whole tiles
         if (!wait_sums()) break;
         const int cols = max(p.block_n >> 1, 32);
@@ -439,6 +580,13 @@ cudaError_t launch_pair(const PairMaps& maps, const PairParams& p, int sms, bool
   return launch(f, dim3(unsigned(2 * pairs)), kThreads, smem, 2, chained, s, maps, p);
 }
 
+template <int kEpi>
+cudaError_t launch_scaled(int dtype, const PairMaps& maps, const PairParams& p, int sms, bool chained, cudaStream_t s) {
+  if (dtype == CCONV_TYPE_BF16) return launch_pair<kEpi, __nv_bfloat16>(maps, p, sms, chained, s);
+  if (dtype == CCONV_TYPE_FP16) return launch_pair<kEpi, __half>(maps, p, sms, chained, s);
+  return launch_pair<kEpi, float>(maps, p, sms, chained, s);
+}
+
 template <typename T>
 cudaError_t launch_epilogue(int epi, const PairMaps& maps, const PairParams& p, int sms, bool chained, cudaStream_t s) {
   if (epi == kStore) return launch_pair<kStore, T>(maps, p, sms, chained, s);
@@ -447,55 +595,10 @@ cudaError_t launch_epilogue(int epi, const PairMaps& maps, const PairParams& p, 
   return launch_pair<kPartial, T>(maps, p, sms, chained, s);
 }
 
-int encode_operand(CUtensorMap* tm, const Operand& o, int dtype, int rows_box) {
+int encode_operand(CUtensorMap* tm, const Operand& o, int es, int dtype, int rows_box) {
+  if (es == 1) return encode_map(tm, o.p, 1, dtype, o.k, o.rows, o.pitch, 128, rows_box);
   return o.kmajor ? encode_map(tm, o.p, 2, dtype, o.k, o.rows, o.pitch, 64, rows_box)
                   : encode_map(tm, o.p, 2, dtype, o.rows, o.k, o.pitch, 64, 64);
-}
-
-__device__ __forceinline__ float to_f32(__nv_fp8_e4m3 v) { return float(v); }
-
-// 64 x 64 outputs a block of 256 threads, 4 x 4 a thread; k in steps of 16 through shared memory.  Sums
-// of 128 products are scaled before they are added up.
-template <typename T, typename Out>
-__global__ void __launch_bounds__(256) cconv_fp8_simple_kernel(Mat a, Mat b, Mat sa, Mat sb, Mat c, int64_t M,
-                                                               int64_t N, int64_t K) {
-  __shared__ float as[16][65], bs[16][65];
-  const int64_t m0 = int64_t(blockIdx.y) * 64, n0 = int64_t(blockIdx.x) * 64;
-  const int tx = threadIdx.x & 15, ty = threadIdx.x >> 4;
-  const T* A = static_cast<const T*>(a.p);
-  const T* B = static_cast<const T*>(b.p);
-  float total[4][4] = {}, acc[4][4] = {};
-  for (int64_t k0 = 0; k0 < K; k0 += 16) {
-    for (int i = threadIdx.x; i < 1024; i += 256) {
-      const int k = i & 15, r = i >> 4;
-      as[k][r] = m0 + r < M && k0 + k < K ? to_f32(A[(m0 + r) * a.rs + (k0 + k) * a.cs]) : 0.0f;
-      bs[k][r] = n0 + r < N && k0 + k < K ? to_f32(B[(n0 + r) * b.rs + (k0 + k) * b.cs]) : 0.0f;
-    }
-    __syncthreads();
-#pragma unroll
-    for (int k = 0; k < 16; ++k)
-#pragma unroll
-      for (int i = 0; i < 4; ++i)
-#pragma unroll
-        for (int j = 0; j < 4; ++j) acc[i][j] += as[k][ty * 4 + i] * bs[k][tx * 4 + j];
-    __syncthreads();
-    if ((k0 + 16) % 128 == 0 || k0 + 16 >= K) {
-      for (int i = 0; i < 4; ++i)
-        for (int j = 0; j < 4; ++j) {
-          const int64_t m = m0 + ty * 4 + i, n = n0 + tx * 4 + j, kb = k0 / 128;
-          if (m < M && n < N)
-            total[i][j] += acc[i][j] * (static_cast<const float*>(sa.p)[m * sa.rs + kb * sa.cs] *
-                                        static_cast<const float*>(sb.p)[n / 128 * sb.rs + kb * sb.cs]);
-          acc[i][j] = 0.0f;
-        }
-    }
-  }
-  Out* C = static_cast<Out*>(const_cast<void*>(c.p));
-  for (int i = 0; i < 4; ++i)
-    for (int j = 0; j < 4; ++j) {
-      const int64_t m = m0 + ty * 4 + i, n = n0 + tx * 4 + j;
-      if (m < M && n < N) C[m * c.rs + n * c.cs] = from_f32<Out>(total[i][j]);
-    }
 }
 
 // ---- finishing passes: four neighbouring columns a thread, a row a blockIdx.y step -----------------
@@ -627,7 +730,8 @@ cudaError_t run_product(const Product& p, int sms, bool chained, bool more, cuda
   q.tiles_m0 = int(cdiv64(p.M, 256));
   q.tiles_m = q.tiles_m0 * stack;
   q.tiles_n = int(cdiv64(p.N, p.paired ? 128 : p.block_n));
-  q.kb_seg = int(cdiv64(p.K, 64));
+  const bool eight = p.epilogue == kScaled || p.epilogue == kScaledPartial;
+  q.kb_seg = int(cdiv64(p.K, eight ? 128 : 64));
   q.kb_total = q.kb_seg * (p.segments ? 2 : 1);
   q.kb_split = int(cdiv64(q.kb_total, p.splits));
   q.splits = int(cdiv64(q.kb_total, q.kb_split));
@@ -643,7 +747,7 @@ cudaError_t run_product(const Product& p, int sms, bool chained, bool more, cuda
   q.b_desc = swizzled_desc(p.b[0].kmajor, 8192);
   q.a_step = p.a[0].kmajor ? 32 >> 4 : 2048 >> 4;
   q.b_step = p.b[0].kmajor ? 32 >> 4 : 2048 >> 4;
-  const uint32_t type = p.dtype == CCONV_TYPE_BF16 ? 1u : 0u;
+  const uint32_t type = !eight && p.dtype == CCONV_TYPE_BF16 ? 1u : 0u;  // (8 bits: 0 is e4m3)
   // instruction descriptor: D fp32, types of A and B, their orders (1: rows contiguous), N / 8, M / 16
   q.idesc = (1u << 4) | (type << 7) | (type << 10) | (uint32_t(!p.a[0].kmajor) << 15) |
             (uint32_t(!p.b[0].kmajor) << 16) | (uint32_t(p.block_n >> 3) << 17) | (uint32_t(256 >> 4) << 24);
@@ -655,39 +759,35 @@ cudaError_t run_product(const Product& p, int sms, bool chained, bool more, cuda
   q.partial = p.partial;
   q.pitch = p.pitch;
   q.slice = p.slice;
+  q.row_scale = static_cast<const float*>(p.row_scale.p);
+  q.row_rs = p.row_scale.rs;
+  q.row_ks = p.row_scale.cs;
+  q.col_scale = static_cast<const float*>(p.col_scale.p);
+  q.col_rs = p.col_scale.rs;
+  q.col_ks = p.col_scale.cs;
   q.limit_ns = wait_limit_ns();
   const int two_a = p.segments || p.stacked ? 2 : 1, two_b = p.segments || p.paired ? 2 : 1;
   for (int i = 0; i < 2; ++i) {
-    if ((*rc = encode_operand(&maps.a[i], p.a[i < two_a ? i : 0], p.dtype, 128))) return cudaSuccess;
-    if ((*rc = encode_operand(&maps.b[i], p.b[i < two_b ? i : 0], p.dtype, p.block_n / 2))) return cudaSuccess;
+    if ((*rc = encode_operand(&maps.a[i], p.a[i < two_a ? i : 0], eight ? 1 : 2, p.dtype, 128))) return cudaSuccess;
+    if ((*rc = encode_operand(&maps.b[i], p.b[i < two_b ? i : 0], eight ? 1 : 2, p.dtype, p.block_n / 2))) return cudaSuccess;
   }
   for (int i = 0; i < 5; ++i) {
     const Mat& m = i < 3 ? p.out[i] : p.in[i - 3];
     CUtensorMap* tm = i < 3 ? &maps.out[i] : &maps.in[i - 3];
     *tm = maps.a[0];
-    if (m.p && (*rc = encode_map(tm, m.p, 2, p.dtype, p.N, p.M, m.rs, 64, 32))) return cudaSuccess;
+    if (m.p && (*rc = encode_map(tm, m.p, type_bytes(p.dtype), p.dtype, p.N, p.M, m.rs, 128 / type_bytes(p.dtype), 32))) return cudaSuccess;
   }
+  if (p.epilogue == kScaled) return launch_scaled<kScaled>(p.dtype, maps, q, sms, chained, s);
+  if (p.epilogue == kScaledPartial) return launch_pair<kScaledPartial, float>(maps, q, sms, chained, s);
   return p.dtype == CCONV_TYPE_BF16 ? launch_epilogue<__nv_bfloat16>(p.epilogue, maps, q, sms, chained, s)
                                     : launch_epilogue<__half>(p.epilogue, maps, q, sms, chained, s);
 }
 
-cudaError_t run_fp8_simple(const Mat& a, const Mat& b, const Mat& sa, const Mat& sb, const Mat& c, int64_t M,
-                           int64_t N, int64_t K, int dtype, cudaStream_t s) {
-  using E = __nv_fp8_e4m3;
-  const dim3 grid(unsigned(cdiv64(N, 64)), unsigned(cdiv64(M, 64)));
-  if (dtype == CCONV_TYPE_BF16)
-    cconv_fp8_simple_kernel<E, __nv_bfloat16><<<grid, 256, 0, s>>>(a, b, sa, sb, c, M, N, K);
-  else if (dtype == CCONV_TYPE_FP16)
-    cconv_fp8_simple_kernel<E, __half><<<grid, 256, 0, s>>>(a, b, sa, sb, c, M, N, K);
-  else
-    cconv_fp8_simple_kernel<E, float><<<grid, 256, 0, s>>>(a, b, sa, sb, c, M, N, K);
-  return cudaGetLastError();
-}
-
 cudaError_t finish_store(const Partial& p, const Mat& out, int64_t M, int64_t N, int dtype, bool more, cudaStream_t s) {
-  if (dtype == CCONV_TYPE_BF16)
-    return launch(finish_store_kernel<__nv_bfloat16>, finish_grid(M, N), 128, 0, 1, true, s, p, out, M, N, int(more));
-  return launch(finish_store_kernel<__half>, finish_grid(M, N), 128, 0, 1, true, s, p, out, M, N, int(more));
+  auto f = dtype == CCONV_TYPE_BF16   ? finish_store_kernel<__nv_bfloat16>
+           : dtype == CCONV_TYPE_FP16 ? finish_store_kernel<__half>
+                                      : finish_store_kernel<float>;
+  return launch(f, finish_grid(M, N), 128, 0, 1, true, s, p, out, M, N, int(more));
 }
 
 cudaError_t finish_gated(const Partial& p, const Mat& gate_pre, const Mat& up_pre, const Mat& h, int64_t M, int64_t N,
@@ -709,6 +809,7 @@ cudaError_t run_copy(const Mat& from, const Mat& to, int64_t rows, int64_t cols,
   const int64_t y = cdiv64(rows, 32);
   const dim3 grid(unsigned(cdiv64(cols, 32)), unsigned(y < 65535 ? y : 65535));
   if (es == 1) return launch(cconv_copy_kernel<uint8_t>, grid, 256, 0, 1, chained, s, from, to, rows, cols, int(more));
+  if (es == 4) return launch(cconv_copy_kernel<uint32_t>, grid, 256, 0, 1, chained, s, from, to, rows, cols, int(more));
   return launch(cconv_copy_kernel<uint16_t>, grid, 256, 0, 1, chained, s, from, to, rows, cols, int(more));
 }
 

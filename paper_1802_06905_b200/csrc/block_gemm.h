@@ -16,6 +16,8 @@ enum : int {
   kGated = 1,          // columns are pairs g, u: out[0] = act(g) * u, and out[1] = g, out[2] = u if saved
   kGatedBackward = 2,  // sums are dh; in[0] = g, in[1] = u: out[0] = dg, out[1] = du, out[2] = h
   kPartial = 3,        // fp32 sums of a share of k go to the table of partial sums
+  kScaled = 4,         // 8-bit operands, scaled sums: out[0]
+  kScaledPartial = 5,  // 8-bit operands, scaled sums of a share of k go to the table
 };
 
 // C[m][n] = sum_k A[m][k] B[n][k] by pairs of CTAs.  With two operands a[0], a[1] (and b[0], b[1]):
@@ -30,6 +32,9 @@ struct Product {
   int dtype = 0, act = 0;
   bool save = false;
   Mat out[3], in[2];             // row-major, in place for the copy engine
+  // 8-bit operands: scale (i, kb) of rows and columns; i is a row (column) of one token, or 128 of weights:
+  // kScaled: rows are tokens; kScaledPartial: columns are
+  Mat row_scale, col_scale;
   // kPartial: share s of k of element (m, n) goes to partial[s * slice + n * pitch + m'], where m'
   // counts rows of tiles of both products when stacked
   float* partial = nullptr;
@@ -63,9 +68,5 @@ cudaError_t run_copy(const Mat& from, const Mat& to, int64_t rows, int64_t cols,
 
 // The status word that the product kernels of the current device share (device address).
 int block_status_word(int** word);
-
-// 8-bit operands with their scales.
-cudaError_t run_fp8_simple(const Mat& a, const Mat& b, const Mat& sa, const Mat& sb, const Mat& c, int64_t M,
-                           int64_t N, int64_t K, int dtype, cudaStream_t s);
 
 }  // namespace cconv
