@@ -8,7 +8,7 @@
 // bytes a clock, a pair of CTAs at 256 x 256 64 bytes a clock each, below what L2 delivers to an SM.
 //
 // Roles: warp 0 copies (TMA), warp 1 of the first CTA issues MMAs, warp 2 owns the tensor memory, warps
-// 2-9 are the epilogue (two for each quarter of the lanes, half of the columns each).
+// 4-11 are the epilogue (two for each quarter of the lanes, half of the columns each).
 #include <cstdlib>
 
 #include "block.h"
@@ -19,7 +19,7 @@
 namespace cconv {
 namespace {
 
-constexpr int kThreads = 320;
+constexpr int kThreads = 384;
 constexpr int kEpilogueWarps = 8;
 constexpr uint32_t kABytes = 128 * 128;  // a stage of A in one CTA: 128 rows x 128 bytes of k
 constexpr uint32_t kBoxBytes = 32 * 128; // a piece that an epilogue warp stages: 32 rows x 128 bytes
@@ -108,10 +108,14 @@ __device__ __forceinline__ void unstage32(uint32_t base, int r, int c0, float (&
 
 // Pieces that an epilogue warp stages.
 template <int kEpi>
-constexpr int kPieces = kEpi == kStore || kEpi == kScaled ? 2 : kEpi == kPartial || kEpi == kScaledPartial ? 0 : 3;
+constexpr int kPieces = kEpi == kStore ? 2 : kEpi == kScaled ? 1 : kEpi == kPartial || kEpi == kScaledPartial ? 0 : 3;
 int staged_pieces(int epi) {
-  return epi == kStore || epi == kScaled ? 2 : epi == kPartial || epi == kScaledPartial ? 0 : 3;
+  return epi == kStore ? 2 : epi == kScaled ? 1 : epi == kPartial || epi == kScaledPartial ? 0 : 3;
 }
+// Scales of 8-bit rows that an epilogue warp keeps: 16 blocks of k of its 32 rows and of its columns
+// (row 32), the 16 in use and the next 16; a pitch of 17 words keeps the lanes on different banks.
+constexpr uint32_t kScaleBytes = 33 * 17 * 4;
+uint32_t scale_bytes(int epi) { return epi == kScaled ? 2 * kEpilogueWarps * kScaleBytes : 0; }
 template <int kEpi>
 constexpr bool kEightBit = kEpi == kScaled || kEpi == kScaledPartial;
 
@@ -122,6 +126,14 @@ __device__ __forceinline__ void fma2(float2& d, float a0, float a1, float s) {
       "fma.rn.f32x2 z, x, y, z;\n\tmov.b64 {%0, %1}, z;\n\t}"
       : "+f"(d.x), "+f"(d.y)
       : "f"(a0), "f"(a1), "f"(s));
+}
+__device__ __forceinline__ void cp_async4(uint32_t to, const float* from) {
+  asm volatile("cp.async.ca.shared.global [%0], [%1], 4;" ::"r"(to), "l"(from) : "memory");
+}
+__device__ __forceinline__ float ld_shared_f32(uint32_t at) {
+  float f;
+  asm volatile("ld.shared.f32 %0, [%1];" : "=f"(f) : "r"(at) : "memory");
+  return f;
 }
 __device__ __forceinline__ void stage_f32(uint32_t base, int r, const float* f) {
 #pragma unroll
@@ -143,7 +155,8 @@ __global__ void __launch_bounds__(kThreads, 1) cconv_pair_product_kernel(const _
   const uint32_t base = (smem_u32(smem_raw) + 1023u) & ~1023u;
   const uint32_t stage_bytes = kABytes + p.b_bytes;
   const uint32_t staging = base + p.stages * stage_bytes;
-  const uint32_t bars = staging + kEpilogueWarps * kPieces<kEpi> * kBoxBytes;
+  const uint32_t scales = staging + kEpilogueWarps * kPieces<kEpi> * kBoxBytes;
+  const uint32_t bars = (scales + (kEpi == kScaled ? 2 * kEpilogueWarps * kScaleBytes : 0) + 7) & ~7u;
   const uint32_t bar_full = bars, bar_empty = bars + 8 * p.stages;
   const uint32_t bar_tfull = bar_empty + 8 * p.stages, bar_tempty = bar_tfull + 16, bar_in = bar_tempty + 16;
   const uint32_t slot = bar_in + 8 * kEpilogueWarps;
@@ -181,100 +194,124 @@ __global__ void __launch_bounds__(kThreads, 1) cconv_pair_product_kernel(const _
   asm volatile("griddepcontrol.wait;" ::: "memory");
   if (p.more) asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
 
-  if (warp == 0) {
-    if (elect_one()) {
-      uint32_t s = 0, ph = 0;
-      const uint32_t full0 = cluster_map_shared(bar_full, 0);
-      const int box_b = int(p.b_bytes) / 8192;
-      bool ok = true;
-      for (int t = pair; ok && t < tiles; t += pairs) {
-        const Tile tl = tile_of(p, t);
-        const bool second = tl.m >= p.tiles_m0;
-        const int m0 = (second ? tl.m - p.tiles_m0 : tl.m) * 256 + int(rank) * 128;
-        const int n0 = p.paired ? tl.n * 128 : tl.n * p.block_n + int(rank) * (p.block_n >> 1);
-        const int k0 = tl.split * p.kb_split, k1 = min(p.kb_total, k0 + p.kb_split);
-        for (int kb = k0; kb < k1; ++kb) {
-          if (!mbar_wait(bar_empty + 8 * s, ph ^ 1, abort_p, p.status, kStatProducerWait, p.limit_ns)) {
-            ok = false;
-            break;
-          }
-          const bool seg = kb >= p.kb_seg;
-          const int k = (seg ? kb - p.kb_seg : kb) * (kEightBit<kEpi> ? 128 : 64);
-          const CUtensorMap* ma = &maps.a[seg || second];
-          const CUtensorMap* mb = &maps.b[seg || (p.paired && rank)];
-          const uint32_t a = base + s * stage_bytes, b = a + kABytes, bar = full0 + 8 * s;
-          if (rank == 0) mbar_arrive_expect_tx(bar_full + 8 * s, 2 * stage_bytes);
-          if (p.a_kmajor) {
-            tma_load_2d_pair(a, ma, k, m0, bar);
-          } else {
-            tma_load_2d_pair(a, ma, m0, k, bar);
-            tma_load_2d_pair(a + 8192, ma, m0 + 64, k, bar);
-          }
-          if (p.b_kmajor) {
-            tma_load_2d_pair(b, mb, k, n0, bar);
-          } else {
-            for (int i = 0; i < box_b; ++i) tma_load_2d_pair(b + 8192 * i, mb, n0 + 64 * i, k, bar);
-          }
-          if (++s == uint32_t(p.stages)) s = 0, ph ^= 1;
-        }
-      }
-    }
-  } else if (warp == 1) {
-    if (rank == 0) {
-      const bool issue = elect_one();
-      uint32_t s = 0, ph = 0, buf = 0, bph = 0;
-      bool ok = true;
-      for (int t = pair; ok && t < tiles; t += pairs) {
-        const Tile tl = tile_of(p, t);
-        const int k0 = tl.split * p.kb_split, k1 = min(p.kb_total, k0 + p.kb_split);
-        if constexpr (!kEightBit<kEpi>) {
-          if (!wait_all(bar_tempty + 8 * buf, bph ^ 1, abort_p, p.status, kStatMmaWaitTmem, p.limit_ns)) break;
-          tc_fence_after();
-        }
-        for (int kb = k0; kb < k1; ++kb) {
-          if constexpr (kEightBit<kEpi>) {  // sums of one block of 128 a time
-            if (!wait_all(bar_tempty + 8 * buf, bph ^ 1, abort_p, p.status, kStatMmaWaitTmem, p.limit_ns)) {
+  // 8-bit: the epilogue's sums take registers that the other warps do not need (128 x 80 + 256 x 208 of
+  // the 384 x 168 that the block starts with)
+  if (warp < 4) {
+    if constexpr (kEightBit<kEpi>) asm volatile("setmaxnreg.dec.sync.aligned.u32 80;");
+    if (warp == 0) {
+      if (elect_one()) {
+        uint32_t s = 0, ph = 0;
+        const uint32_t full0 = cluster_map_shared(bar_full, 0);
+        const int box_b = int(p.b_bytes) / 8192;
+        bool ok = true;
+        for (int t = pair; ok && t < tiles; t += pairs) {
+          const Tile tl = tile_of(p, t);
+          const bool second = tl.m >= p.tiles_m0;
+          const int m0 = (second ? tl.m - p.tiles_m0 : tl.m) * 256 + int(rank) * 128;
+          const int n0 = p.paired ? tl.n * 128 : tl.n * p.block_n + int(rank) * (p.block_n >> 1);
+          const int k0 = tl.split * p.kb_split, k1 = min(p.kb_total, k0 + p.kb_split);
+          for (int kb = k0; kb < k1; ++kb) {
+            if (!mbar_wait(bar_empty + 8 * s, ph ^ 1, abort_p, p.status, kStatProducerWait, p.limit_ns)) {
               ok = false;
               break;
             }
-          }
-          const uint32_t d = tmem + buf * 256;
-          if (!wait_all(bar_full + 8 * s, ph, abort_p, p.status, kStatMmaWaitFull, p.limit_ns)) {
-            ok = false;
-            break;
-          }
-          tc_fence_after();
-          const uint32_t a = base + s * stage_bytes;
-          if (issue) {
-            const uint64_t da = p.a_desc + (a >> 4), db = p.b_desc + ((a + kABytes) >> 4);
-#pragma unroll
-            for (int j = 0; j < 4; ++j) {
-              if constexpr (kEightBit<kEpi>) pair_mma_f8(d, da + j * 2, db + j * 2, p.idesc, j > 0);
-              else pair_mma_f16(d, da + j * p.a_step, db + j * p.b_step, p.idesc, kb > k0 || j > 0);
+            const bool seg = kb >= p.kb_seg;
+            const int k = (seg ? kb - p.kb_seg : kb) * (kEightBit<kEpi> ? 128 : 64);
+            const CUtensorMap* ma = &maps.a[seg || second];
+            const CUtensorMap* mb = &maps.b[seg || (p.paired && rank)];
+            const uint32_t a = base + s * stage_bytes, b = a + kABytes, bar = full0 + 8 * s;
+            if (rank == 0) mbar_arrive_expect_tx(bar_full + 8 * s, 2 * stage_bytes);
+            if (p.a_kmajor) {
+              tma_load_2d_pair(a, ma, k, m0, bar);
+            } else {
+              tma_load_2d_pair(a, ma, m0, k, bar);
+              tma_load_2d_pair(a + 8192, ma, m0 + 64, k, bar);
             }
-            pair_commit(bar_empty + 8 * s);
-            if constexpr (kEightBit<kEpi>) pair_commit(bar_tfull + 8 * buf);
+            if (p.b_kmajor) {
+              tma_load_2d_pair(b, mb, k, n0, bar);
+            } else {
+              for (int i = 0; i < box_b; ++i) tma_load_2d_pair(b + 8192 * i, mb, n0 + 64 * i, k, bar);
+            }
+            if (++s == uint32_t(p.stages)) s = 0, ph ^= 1;
           }
-          __syncwarp();
-          if constexpr (kEightBit<kEpi>) {
+        }
+      }
+    } else if (warp == 1) {
+      if (rank == 0) {
+        const bool issue = elect_one();
+        uint32_t s = 0, ph = 0, buf = 0, bph = 0;
+        bool ok = true;
+        for (int t = pair; ok && t < tiles; t += pairs) {
+          const Tile tl = tile_of(p, t);
+          const int k0 = tl.split * p.kb_split, k1 = min(p.kb_total, k0 + p.kb_split);
+          if constexpr (!kEightBit<kEpi>) {
+            if (!wait_all(bar_tempty + 8 * buf, bph ^ 1, abort_p, p.status, kStatMmaWaitTmem, p.limit_ns)) break;
+            tc_fence_after();
+          }
+          for (int kb = k0; kb < k1; ++kb) {
+            if constexpr (kEightBit<kEpi>) {  // sums of one block of 128 a time
+              if (!wait_all(bar_tempty + 8 * buf, bph ^ 1, abort_p, p.status, kStatMmaWaitTmem, p.limit_ns)) {
+                ok = false;
+                break;
+              }
+            }
+            const uint32_t d = tmem + buf * 256;
+            if (!wait_all(bar_full + 8 * s, ph, abort_p, p.status, kStatMmaWaitFull, p.limit_ns)) {
+              ok = false;
+              break;
+            }
+            tc_fence_after();
+            const uint32_t a = base + s * stage_bytes;
+            if (issue) {
+              const uint64_t da = p.a_desc + (a >> 4), db = p.b_desc + ((a + kABytes) >> 4);
+  #pragma unroll
+              for (int j = 0; j < 4; ++j) {
+                if constexpr (kEightBit<kEpi>) pair_mma_f8(d, da + j * 2, db + j * 2, p.idesc, j > 0);
+                else pair_mma_f16(d, da + j * p.a_step, db + j * p.b_step, p.idesc, kb > k0 || j > 0);
+              }
+              pair_commit(bar_empty + 8 * s);
+              if constexpr (kEightBit<kEpi>) pair_commit(bar_tfull + 8 * buf);
+            }
+            __syncwarp();
+            if constexpr (kEightBit<kEpi>) {
+              if (++buf == 2) buf = 0, bph ^= 1;
+            }
+            if (++s == uint32_t(p.stages)) s = 0, ph ^= 1;
+          }
+          if constexpr (!kEightBit<kEpi>) {
+            if (issue && ok) pair_commit(bar_tfull + 8 * buf);
+            __syncwarp();
             if (++buf == 2) buf = 0, bph ^= 1;
           }
-          if (++s == uint32_t(p.stages)) s = 0, ph ^= 1;
-        }
-        if constexpr (!kEightBit<kEpi>) {
-          if (issue && ok) pair_commit(bar_tfull + 8 * buf);
-          __syncwarp();
-          if (++buf == 2) buf = 0, bph ^= 1;
         }
       }
     }
   } else {
-    const int q = warp & 3, half = (warp - 2) >> 2;
-    const uint32_t mine = staging + (warp - 2) * kPieces<kEpi> * kBoxBytes;
-    const uint32_t in_bar = bar_in + 8 * (warp - 2);
+    if constexpr (kEightBit<kEpi>) asm volatile("setmaxnreg.inc.sync.aligned.u32 208;");
+    const int q = warp & 3, half = (warp - 4) >> 2;
+    const uint32_t mine = staging + (warp - 4) * kPieces<kEpi> * kBoxBytes;
+    const uint32_t in_bar = bar_in + 8 * (warp - 4);
     const uint32_t tempty0 = cluster_map_shared(bar_tempty, 0);
     const uint32_t lanes = tmem + (uint32_t(q * 32) << 16);
     uint32_t buf = 0, bph = 0, in_ph = 0, piece = 0;
+    // The scales of 16 blocks of k from kb on, of tile t, on their way to half `b` of this warp's table.
+    const uint32_t my_scales = scales + (warp - 4) * 2 * kScaleBytes;
+    uint32_t sbuf = 0;
+    auto fetch_scales = [&](int t, int kb, uint32_t b) {
+      if (t < tiles) {
+        const Tile tl = tile_of(p, t);
+        const int64_t r0 = int64_t(tl.m) * 256 + int(rank) * 128 + q * 32;
+        const int64_t nb = (int64_t(tl.n) * p.block_n + half * (p.block_n >> 1)) >> 7;
+        const int k = min(kb + (lane & 15), p.kb_total - 1);
+        const uint32_t to = my_scales + b * kScaleBytes + (lane & 15) * 4;
+#pragma unroll 4
+        for (int r = lane >> 4; r < 32; r += 2)
+          cp_async4(to + r * 68, p.row_scale + min(r0 + r, p.M - 1) * p.row_rs + k * p.row_ks);
+        if (lane < 16) cp_async4(to + 32 * 68, p.col_scale + min(nb, (p.N - 1) >> 7) * p.col_rs + k * p.col_ks);
+      }
+      asm volatile("cp.async.commit_group;" ::: "memory");
+    };
+    if constexpr (kEpi == kScaled) fetch_scales(pair, 0, 0);
     for (int t = pair; t < tiles; t += pairs) {
       const Tile tl = tile_of(p, t);
       const bool second = tl.m >= p.tiles_m0;
@@ -394,30 +431,34 @@ __global__ void __launch_bounds__(kThreads, 1) cconv_pair_product_kernel(const _
         // Each block's sums are scaled and added up in registers (a row of half the columns a thread),
         // beside the MMAs of the next block: 128 columns are 64 two-wide multiply-adds.
         const int cols = p.block_n >> 1;
-        const int k0 = tl.split * p.kb_split, k1 = min(p.kb_total, k0 + p.kb_split);
-        const float* sa = p.row_scale + min(int64_t(row0 + lane), p.M - 1) * p.row_rs;
-        const int64_t nb = (int64_t(tl.n) * p.block_n + half * cols) >> 7;
-        const float* sb = p.col_scale + min(nb, (p.N - 1) >> 7) * p.col_rs;
         float2 sum[64];
 #pragma unroll
         for (int i = 0; i < 64; ++i) sum[i] = make_float2(0.0f, 0.0f);
-        float na = sa[k0 * p.row_ks], nbs = sb[k0 * p.col_ks];
         bool ok = true;
-        for (int kb = k0; kb < k1; ++kb) {
-          const float scale = na * nbs;
-          if (kb + 1 < k1) {
-            na = sa[(kb + 1) * p.row_ks];
-            nbs = sb[(kb + 1) * p.col_ks];
+        for (int kb = 0; kb < p.kb_total; ++kb) {
+          if ((kb & 15) == 0) {
+            // this half of the table has come; the other is free, as every lane is past its last use
+            asm volatile("cp.async.wait_group 0;" ::: "memory");
+            __syncwarp();
+            const bool on = kb + 16 < p.kb_total;
+            fetch_scales(on ? t : t + pairs, on ? kb + 16 : 0, sbuf ^ 1);
+            sbuf ^= 1;
           }
+          const uint32_t at = my_scales + (sbuf ^ 1) * kScaleBytes + (kb & 15) * 4;
+          const float scale = ld_shared_f32(at + lane * 68) * ld_shared_f32(at + 32 * 68);
           if (!(ok = wait_sums())) break;
+          // the next 32 columns are on their way while 32 are added up
+          uint32_t f[2][32];
+          tmem_ld_32x32b_x32(acc + half * cols, f[0]);
 #pragma unroll
           for (int c = 0; c < 4; ++c) {
             if (c * 32 < cols) {
-              float f[32];
-              load_sums(acc + half * cols + c * 32, f);
-              if ((c + 1) * 32 >= cols) release_sums();
+              tmem_ld_wait();
+              if (c < 3 && (c + 1) * 32 < cols) tmem_ld_32x32b_x32(acc + half * cols + (c + 1) * 32, f[(c + 1) & 1]);
+              else release_sums();
 #pragma unroll
-              for (int i = 0; i < 16; ++i) fma2(sum[c * 16 + i], f[2 * i], f[2 * i + 1], scale);
+              for (int i = 0; i < 16; ++i)
+                fma2(sum[c * 16 + i], __uint_as_float(f[c & 1][2 * i]), __uint_as_float(f[c & 1][2 * i + 1]), scale);
             }
           }
           if (++buf == 2) buf = 0, bph ^= 1;
@@ -428,8 +469,8 @@ __global__ void __launch_bounds__(kThreads, 1) cconv_pair_product_kernel(const _
 #pragma unroll
         for (int c = 0; c < 128; c += kWidth) {
           if (c < cols) {
-            const uint32_t to = mine + piece * kBoxBytes;
-            if (lane == 0) bulk_wait_group_read<1>();
+            const uint32_t to = mine;
+            if (lane == 0) bulk_wait_group_read<0>();
             __syncwarp();
             const float* f = reinterpret_cast<const float*>(&sum[c / 2]);
             if constexpr (sizeof(T) == 4) {
@@ -447,7 +488,6 @@ __global__ void __launch_bounds__(kThreads, 1) cconv_pair_product_kernel(const _
               if (row0 < p.M && col < p.N) tma_store_2d(&maps.out[0], to, col, row0);
               bulk_commit_group();
             }
-            piece ^= 1;
           }
         }
         continue;  // the buffers were handed on block by block
@@ -512,6 +552,7 @@ __global__ void __launch_bounds__(kThreads, 1) cconv_pair_product_kernel(const _
       }
       if (++buf == 2) buf = 0, bph ^= 1;
     }
+    if constexpr (kEpi == kScaled) asm volatile("cp.async.wait_all;" ::: "memory");
     if (kPieces<kEpi> > 0 && lane == 0) bulk_wait_group<0>();
   }
 
@@ -576,7 +617,8 @@ cudaError_t launch_pair(const PairMaps& maps, const PairParams& p, int sms, bool
   }
   const int tiles = p.tiles_m * p.tiles_n * p.splits;
   const int pairs = tiles < sms / 2 ? tiles : sms / 2;
-  const size_t smem = 1024 + size_t(p.stages) * (kABytes + p.b_bytes) + kEpilogueWarps * staged_pieces(kEpi) * kBoxBytes + kBarrierBytes;
+  const size_t smem = 1024 + size_t(p.stages) * (kABytes + p.b_bytes) + kEpilogueWarps * staged_pieces(kEpi) * kBoxBytes +
+                      scale_bytes(kEpi) + kBarrierBytes;
   return launch(f, dim3(unsigned(2 * pairs)), kThreads, smem, 2, chained, s, maps, p);
 }
 
@@ -737,7 +779,7 @@ cudaError_t run_product(const Product& p, int sms, bool chained, bool more, cuda
   q.splits = int(cdiv64(q.kb_total, q.kb_split));
   q.block_n = p.block_n;
   q.b_bytes = uint32_t(p.block_n / 2) * 128;
-  const uint32_t staged = kEpilogueWarps * staged_pieces(p.epilogue) * kBoxBytes;
+  const uint32_t staged = kEpilogueWarps * staged_pieces(p.epilogue) * kBoxBytes + scale_bytes(p.epilogue);
   q.stages = int((kSmemMost - 1024 - kBarrierBytes - staged) / (kABytes + q.b_bytes));
   if (q.stages > 8) q.stages = 8;
   q.a_kmajor = p.a[0].kmajor;

@@ -28,9 +28,11 @@ __device__ __forceinline__ void tma_store_2d(const CUtensorMap* tm, uint32_t src
                "r"(src), "r"(x), "r"(y)
                : "memory");
 }
-// Arrives at a barrier of either CTA of the pair (address from cluster_map_shared).
+// Arrives at a barrier of either CTA of the pair (address from cluster_map_shared).  Relaxed: what it
+// hands on is tensor memory that tcgen05.ld has finished reading (wait::ld, fence::before_thread_sync);
+// a release would also wait for the thread's loads from global memory that are still in flight.
 __device__ __forceinline__ void mbar_arrive_cluster(uint32_t bar) {
-  asm volatile("mbarrier.arrive.release.cluster.shared::cluster.b64 _, [%0];" ::"r"(bar) : "memory");
+  asm volatile("mbarrier.arrive.relaxed.cluster.shared::cluster.b64 _, [%0];" ::"r"(bar) : "memory");
 }
 __device__ __forceinline__ void pair_tmem_alloc(uint32_t slot_smem, uint32_t ncols) {
   asm volatile("tcgen05.alloc.cta_group::2.sync.aligned.shared::cta.b32 [%0], %1;" ::"r"(slot_smem), "r"(ncols)
