@@ -70,12 +70,26 @@ __device__ __forceinline__ Tile tile_of(const PairParams& p, int t) {
   return r;
 }
 
-template <int N>
-__device__ __forceinline__ void load_sums(uint32_t taddr, float (&f)[N]) {
-  static_assert(N == 32, "");
+// Waits for this thread's loads from tensor memory; what they brought is not used before.
+__device__ __forceinline__ void tmem_ld_wait(uint32_t (&v)[32]) {
+  asm volatile("tcgen05.wait::ld.sync.aligned;"
+               : "+r"(v[0]), "+r"(v[1]), "+r"(v[2]), "+r"(v[3]), "+r"(v[4]), "+r"(v[5]), "+r"(v[6]), "+r"(v[7]), "+r"(v[8]),
+                 "+r"(v[9]), "+r"(v[10]), "+r"(v[11]), "+r"(v[12]), "+r"(v[13]), "+r"(v[14]), "+r"(v[15]), "+r"(v[16]),
+                 "+r"(v[17]), "+r"(v[18]), "+r"(v[19]), "+r"(v[20]), "+r"(v[21]), "+r"(v[22]), "+r"(v[23]), "+r"(v[24]),
+                 "+r"(v[25]), "+r"(v[26]), "+r"(v[27]), "+r"(v[28]), "+r"(v[29]), "+r"(v[30]), "+r"(v[31])
+               :
+               : "memory");
+}
+__device__ __forceinline__ void tmem_ld_hold(uint32_t (&v)[32]) {  // as after a wait that has been made
+  asm volatile("" : "+r"(v[0]), "+r"(v[1]), "+r"(v[2]), "+r"(v[3]), "+r"(v[4]), "+r"(v[5]), "+r"(v[6]), "+r"(v[7]), "+r"(v[8]),
+                 "+r"(v[9]), "+r"(v[10]), "+r"(v[11]), "+r"(v[12]), "+r"(v[13]), "+r"(v[14]), "+r"(v[15]), "+r"(v[16]),
+                 "+r"(v[17]), "+r"(v[18]), "+r"(v[19]), "+r"(v[20]), "+r"(v[21]), "+r"(v[22]), "+r"(v[23]), "+r"(v[24]),
+                 "+r"(v[25]), "+r"(v[26]), "+r"(v[27]), "+r"(v[28]), "+r"(v[29]), "+r"(v[30]), "+r"(v[31]));
+}
+__device__ __forceinline__ void load_sums(uint32_t taddr, float (&f)[32]) {
   uint32_t v[32];
   tmem_ld_32x32b_x32(taddr, v);
-  tmem_ld_wait();
+  tmem_ld_wait(v);
 #pragma unroll
   for (int i = 0; i < 32; ++i) f[i] = __uint_as_float(v[i]);
 }
@@ -119,16 +133,22 @@ uint32_t scale_bytes(int epi) { return epi == kScaled ? 2 * kEpilogueWarps * kSc
 template <int kEpi>
 constexpr bool kEightBit = kEpi == kScaled || kEpi == kScaledPartial;
 
-// Two fp32 multiply-adds in one instruction: d = a * {s, s} + d.
-__device__ __forceinline__ void fma2(float2& d, float a0, float a1, float s) {
-  asm("{\n\t.reg .b64 x, y, z;\n\t"
-      "mov.b64 x, {%2, %3};\n\tmov.b64 y, {%4, %4};\n\tmov.b64 z, {%0, %1};\n\t"
-      "fma.rn.f32x2 z, x, y, z;\n\tmov.b64 {%0, %1}, z;\n\t}"
-      : "+f"(d.x), "+f"(d.y)
-      : "f"(a0), "f"(a1), "f"(s));
+// Pairs of fp32 values in a 64-bit register: two multiply-adds in one instruction, d = a * s + d.
+__device__ __forceinline__ uint64_t pair_of(float lo, float hi) {
+  uint64_t v;
+  asm("mov.b64 %0, {%1, %2};" : "=l"(v) : "f"(lo), "f"(hi));
+  return v;
 }
-__device__ __forceinline__ void cp_async4(uint32_t to, const float* from) {
-  asm volatile("cp.async.ca.shared.global [%0], [%1], 4;" ::"r"(to), "l"(from) : "memory");
+__device__ __forceinline__ float2 halves_of(uint64_t v) {
+  float2 f;
+  asm("mov.b64 {%0, %1}, %2;" : "=f"(f.x), "=f"(f.y) : "l"(v));
+  return f;
+}
+__device__ __forceinline__ void fma2(uint64_t& d, uint64_t a, uint64_t s) {
+  asm("fma.rn.f32x2 %0, %1, %2, %0;" : "+l"(d) : "l"(a), "l"(s));
+}
+__device__ __forceinline__ void cp_async4(uint32_t to, const float* from, bool there) {
+  asm volatile("cp.async.ca.shared.global [%0], [%1], 4, %2;" ::"r"(to), "l"(from), "r"(there ? 4 : 0) : "memory");
 }
 __device__ __forceinline__ float ld_shared_f32(uint32_t at) {
   float f;
@@ -297,23 +317,26 @@ __global__ void __launch_bounds__(kThreads, 1) cconv_pair_product_kernel(const _
     // The scales of 16 blocks of k from kb on, of tile t, on their way to half `b` of this warp's table.
     const uint32_t my_scales = scales + (warp - 4) * 2 * kScaleBytes;
     uint32_t sbuf = 0;
-    auto fetch_scales = [&](int t, int kb, uint32_t b) {
-      if (t < tiles) {
-        const Tile tl = tile_of(p, t);
-        const int64_t r0 = int64_t(tl.m) * 256 + int(rank) * 128 + q * 32;
-        const int64_t nb = (int64_t(tl.n) * p.block_n + half * (p.block_n >> 1)) >> 7;
-        const int k = min(kb + (lane & 15), p.kb_total - 1);
-        const uint32_t to = my_scales + b * kScaleBytes + (lane & 15) * 4;
-#pragma unroll 4
-        for (int r = lane >> 4; r < 32; r += 2)
-          cp_async4(to + r * 68, p.row_scale + min(r0 + r, p.M - 1) * p.row_rs + k * p.row_ks);
-        if (lane < 16) cp_async4(to + 32 * 68, p.col_scale + min(nb, (p.N - 1) >> 7) * p.col_rs + k * p.col_ks);
+    auto fetch_scales = [&](const Tile& tl, int kb, uint32_t b) {
+      const int sub = lane >> 4, k = min(kb + (lane & 15), p.kb_total - 1);
+      const int64_t r0 = int64_t(tl.m) * 256 + int(rank) * 128 + q * 32 + sub;
+      const int rows = int(min(int64_t(32), p.M - r0));  // from r0 on; what lies past them reads as 0
+      const float* from = p.row_scale + min(r0, p.M - 1) * p.row_rs + k * p.row_ks;
+      uint32_t to = my_scales + b * kScaleBytes + (lane & 15) * 4 + sub * 68;
+#pragma unroll
+      for (int r = 0; r < 32; r += 2) {
+        cp_async4(to + r * 68, from, r < rows);
+        if (r + 2 < rows) from += 2 * p.row_rs;
       }
+      const int64_t nb = min((int64_t(tl.n) * p.block_n + half * (p.block_n >> 1)) >> 7, (p.N - 1) >> 7);
+      if (sub == 0) cp_async4(to + 32 * 68, p.col_scale + nb * p.col_rs + k * p.col_ks, true);
       asm volatile("cp.async.commit_group;" ::: "memory");
     };
-    if constexpr (kEpi == kScaled) fetch_scales(pair, 0, 0);
+    Tile next = tile_of(p, pair);
+    if constexpr (kEpi == kScaled) fetch_scales(next, 0, 0);
     for (int t = pair; t < tiles; t += pairs) {
-      const Tile tl = tile_of(p, t);
+      const Tile tl = next;
+      next = tile_of(p, min(t + pairs, tiles - 1));
       const bool second = tl.m >= p.tiles_m0;
       const int row0 = (second ? tl.m - p.tiles_m0 : tl.m) * 256 + int(rank) * 128 + q * 32;
       uint32_t acc = lanes + buf * 256;
@@ -431,35 +454,48 @@ __global__ void __launch_bounds__(kThreads, 1) cconv_pair_product_kernel(const _
         // Each block's sums are scaled and added up in registers (a row of half the columns a thread),
         // beside the MMAs of the next block: 128 columns are 64 two-wide multiply-adds.
         const int cols = p.block_n >> 1;
-        float2 sum[64];
+        uint64_t sum[64];
 #pragma unroll
-        for (int i = 0; i < 64; ++i) sum[i] = make_float2(0.0f, 0.0f);
-        bool ok = true;
-        for (int kb = 0; kb < p.kb_total; ++kb) {
+        for (int i = 0; i < 64; ++i) sum[i] = 0;
+        auto scale_of = [&](int kb) {
           if ((kb & 15) == 0) {
             // this half of the table has come; the other is free, as every lane is past its last use
             asm volatile("cp.async.wait_group 0;" ::: "memory");
             __syncwarp();
             const bool on = kb + 16 < p.kb_total;
-            fetch_scales(on ? t : t + pairs, on ? kb + 16 : 0, sbuf ^ 1);
+            fetch_scales(on ? tl : next, on ? kb + 16 : 0, sbuf ^ 1);
             sbuf ^= 1;
           }
           const uint32_t at = my_scales + (sbuf ^ 1) * kScaleBytes + (kb & 15) * 4;
-          const float scale = ld_shared_f32(at + lane * 68) * ld_shared_f32(at + 32 * 68);
+          return ld_shared_f32(at + lane * 68) * ld_shared_f32(at + 32 * 68);
+        };
+        bool ok = true;
+        for (int kb = 0; kb < p.kb_total; ++kb) {
+          const float f0 = scale_of(kb);
+          const uint64_t scale = pair_of(f0, f0);
           if (!(ok = wait_sums())) break;
-          // the next 32 columns are on their way while 32 are added up
+          // 64 columns at a time; the second 64 are on their way while the first are added up
           uint32_t f[2][32];
+          auto add = [&](int c) {
+#pragma unroll
+            for (int i = 0; i < 16; ++i)
+              fma2(sum[c * 16 + i], pair_of(__uint_as_float(f[c & 1][2 * i]), __uint_as_float(f[c & 1][2 * i + 1])), scale);
+          };
           tmem_ld_32x32b_x32(acc + half * cols, f[0]);
-#pragma unroll
-          for (int c = 0; c < 4; ++c) {
-            if (c * 32 < cols) {
-              tmem_ld_wait();
-              if (c < 3 && (c + 1) * 32 < cols) tmem_ld_32x32b_x32(acc + half * cols + (c + 1) * 32, f[(c + 1) & 1]);
-              else release_sums();
-#pragma unroll
-              for (int i = 0; i < 16; ++i)
-                fma2(sum[c * 16 + i], __uint_as_float(f[c & 1][2 * i]), __uint_as_float(f[c & 1][2 * i + 1]), scale);
-            }
+          tmem_ld_32x32b_x32(acc + half * cols + 32, f[1]);
+          tmem_ld_wait(f[0]);
+          tmem_ld_hold(f[1]);
+          if (cols == 64) release_sums();
+          add(0);
+          if (cols > 64) tmem_ld_32x32b_x32(acc + half * cols + 64, f[0]);
+          add(1);
+          if (cols > 64) {
+            tmem_ld_32x32b_x32(acc + half * cols + 96, f[1]);
+            tmem_ld_wait(f[0]);
+            tmem_ld_hold(f[1]);
+            release_sums();
+            add(2);
+            add(3);
           }
           if (++buf == 2) buf = 0, bph ^= 1;
           acc = lanes + buf * 256;
@@ -472,7 +508,13 @@ __global__ void __launch_bounds__(kThreads, 1) cconv_pair_product_kernel(const _
             const uint32_t to = mine;
             if (lane == 0) bulk_wait_group_read<0>();
             __syncwarp();
-            const float* f = reinterpret_cast<const float*>(&sum[c / 2]);
+            float f[kWidth];
+#pragma unroll
+            for (int i = 0; i < kWidth / 2; ++i) {
+              const float2 v = halves_of(sum[c / 2 + i]);
+              f[2 * i] = v.x;
+              f[2 * i + 1] = v.y;
+            }
             if constexpr (sizeof(T) == 4) {
               stage_f32(to, lane, f);
             } else {
