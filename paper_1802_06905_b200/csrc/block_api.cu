@@ -214,7 +214,7 @@ cconv_matrix same_row(cconv_matrix m, int64_t rows, int64_t cols) {
 
 int64_t norm_workspace(const cconv_residual_norm_args& a, int sms) {
   if (a.T == 0 || a.D == 0) return 0;
-  const int64_t nb = norm_backward_blocks(a.T, a.D, sms);
+  const int64_t nb = norm_backward_blocks(a.T, a.D, type_bytes(a.dtype), sms);
   return round_up64(nb * 5 * a.D * 4, 256);
 }
 
@@ -371,8 +371,11 @@ int cconv_residual_norm_backward(const cconv_residual_norm_args* args, void* cud
     return CCONV_OK;
   }
   NormParams p = norm_params(a);
-  p.nb = norm_backward_blocks(a.T, a.D, sms);
+  p.nb = norm_backward_blocks(a.T, a.D, type_bytes(a.dtype), sms);
   p.part = static_cast<float*>(a.workspace);
+  const int rc = block_status_word(&p.status);
+  if (rc != CCONV_OK) return rc;
+  p.limit_ns = block_wait_limit_ns();
   return block_cuda_error(run_norm_backward(p, a.dtype, s), "cconv_residual_norm_backward");
 }
 

@@ -614,11 +614,6 @@ __global__ void __launch_bounds__(kThreads, 1) cconv_pair_product_kernel(const _
   if (warp == 2) pair_tmem_dealloc(tmem, kTmemCols);
 }
 
-uint64_t wait_limit_ns() {
-  const char* v = std::getenv("CCONV_WAIT_LIMIT_MS");
-  return uint64_t(v && *v ? std::atoi(v) : 1000) * 1000000ull;
-}
-
 // An ordinary launch, or one that may start while the kernel in front of it (of the same call) ends; all
 // kernels here wait for that kernel before they touch memory.
 template <typename F, typename... Args>
@@ -796,6 +791,11 @@ dim3 finish_grid(int64_t M, int64_t N) { return dim3(unsigned(cdiv64(N, 512)), u
 
 }  // namespace
 
+uint64_t block_wait_limit_ns() {
+  const char* v = std::getenv("CCONV_WAIT_LIMIT_MS");
+  return uint64_t(v && *v ? std::atoi(v) : 1000) * 1000000ull;
+}
+
 int block_status_word(int** word) {
   void* p = nullptr;
   const cudaError_t e = cudaGetSymbolAddress(&p, g_block_status);
@@ -849,7 +849,7 @@ cudaError_t run_product(const Product& p, int sms, bool chained, bool more, cuda
   q.col_scale = static_cast<const float*>(p.col_scale.p);
   q.col_rs = p.col_scale.rs;
   q.col_ks = p.col_scale.cs;
-  q.limit_ns = wait_limit_ns();
+  q.limit_ns = block_wait_limit_ns();
   const int two_a = p.segments || p.stacked ? 2 : 1, two_b = p.segments || p.paired ? 2 : 1;
   for (int i = 0; i < 2; ++i) {
     if ((*rc = encode_operand(&maps.a[i], p.a[i < two_a ? i : 0], eight ? 1 : 2, p.dtype, 128))) return cudaSuccess;

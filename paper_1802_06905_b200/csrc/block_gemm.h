@@ -68,5 +68,7 @@ cudaError_t run_copy(const Mat& from, const Mat& to, int64_t rows, int64_t cols,
 
 // The status word that the product kernels of the current device share (device address).
 int block_status_word(int** word);
+// Limit of every wait on the device: CCONV_WAIT_LIMIT_MS, by default a second.
+uint64_t block_wait_limit_ns();
 
 }  // namespace cconv

@@ -16,6 +16,7 @@
 #include "block_device.cuh"
 #include "block_norm.h"
 #include "host_setup.h"
+#include "ptx_sm100.cuh"
 
 namespace cconv {
 namespace {
@@ -235,10 +236,10 @@ __device__ __forceinline__ int64_t first_row(const NormParams& p, int64_t b) {
   return p.T * b / p.nb;
 }
 
-template <typename T, int E, int NV>
+// Rows that are not wide (an odd length, pitch or address): E = 1, straight from global memory.
+template <typename T, int NV>
 __global__ void __launch_bounds__(512) cconv_residual_norm_backward_kernel(const NormParams p) {
   __shared__ float2 smem[2][32];
-  using V = Vec<T, E>;
   const T* dres = static_cast<const T*>(p.dresid_out);  // may be dresid
   const T* __restrict__ dx = static_cast<const T*>(p.dnorm_out);
   const T* __restrict__ block = static_cast<const T*>(p.block);
@@ -255,174 +256,383 @@ __global__ void __launch_bounds__(512) cconv_residual_norm_backward_kernel(const
   const int64_t per = p.rows_per_gate ? p.rows_per_gate : p.T;
   float* part = p.part + int64_t(blockIdx.x) * 4 * p.D;
   int buf = 0;
-  float s_pre[NV][E], s_post[NV][E], s_gate[NV][E];
-  V vw_pre[NV], vw_post[NV], vgate[NV];
+  // Sums over rows: x rhat; S yhat of the current gate group (dgate is w_post of it); dw_post (gate times
+  // each group's S yhat, added when the group ends).
+  float s_pre[NV], s_post[NV], s_group[NV], gw[NV];  // gw: gate * w_post of the current group
 #pragma unroll
-  for (int v = 0; v < NV; ++v) {
-    const int c = (v * nt + tid) * E;
-    vw_pre[v].zero();
-    vw_post[v].zero();
-    vgate[v].zero();
-    if (c < p.D) {
-      if (w_pre) vw_pre[v].load(w_pre + c);
-      if (w_post) vw_post[v].load(w_post + c);
-    }
-#pragma unroll
-    for (int i = 0; i < E; ++i) s_pre[v][i] = s_post[v][i] = s_gate[v][i] = 0.0f;
-  }
-  int64_t group = row0 / per;
+  for (int v = 0; v < NV; ++v) s_pre[v] = s_post[v] = s_group[v] = gw[v] = 0.0f;
+  auto at = [&](const T* from, int c, float otherwise) { return from && c < p.D ? to_f32(from[c]) : otherwise; };
+  int64_t group = row0 / per, group_end = (group + 1) * per;
   const int64_t group0 = group;
-  auto load_gate = [&]() {
-    if (!gate) return;
+  auto start_group = [&]() {
 #pragma unroll
     for (int v = 0; v < NV; ++v) {
-      const int c = (v * nt + tid) * E;
-      if (c < p.D) vgate[v].load(gate + group * p.gate_rs + c);
+      const int c = v * nt + tid;
+      gw[v] = at(gate ? gate + group * p.gate_rs : nullptr, c, 1.0f) * at(w_post, c, 1.0f);
     }
   };
-  // writes the sums of the group that ends (or that the block ends in), and starts the next
-  auto flush_gate = [&]() {
-    if (!gate) return;
-    const int64_t g0 = group * per, g1 = g0 + per < p.T ? g0 + per : p.T;
+  // adds the group that ends (or that the block ends in) to dw_post and writes its part of dgate
+  auto end_group = [&]() {
+    const int64_t g0 = group * per, g1 = group_end < p.T ? group_end : p.T;
     const bool whole = g0 >= row0 && g1 <= row1;
 #pragma unroll
     for (int v = 0; v < NV; ++v) {
-      const int c = (v * nt + tid) * E;
-      if (c < p.D) {
-        if (whole) {
-          V::store(dgate + group * p.dgate_rs + c, s_gate[v]);
-        } else {
-          float* to = part + (group == group0 ? 2 : 3) * int64_t(p.D) + c;
-#pragma unroll
-          for (int i = 0; i < E; ++i) to[i] = s_gate[v][i];
-        }
-      }
-#pragma unroll
-      for (int i = 0; i < E; ++i) s_gate[v][i] = 0.0f;
-    }
-  };
-  load_gate();
-  V nr[NV], nd[NV], nx[NV], ny[NV];  // the row that is on its way
-  auto fetch = [&](int64_t t) {
-#pragma unroll
-    for (int v = 0; v < NV; ++v) {
-      const int c = (v * nt + tid) * E;
-      nr[v].zero();
-      nd[v].zero();
-      nx[v].zero();
-      ny[v].zero();
-      if (c < p.D) {
-        if (dx) {
-          nr[v].load(resid_out + t * p.resid_out_rs + c);
-          nx[v].load(dx + t * p.dnorm_out_rs + c);
-        }
-        if (dres) nd[v].load(dres + t * p.dresid_out_rs + c);
-        if (block) ny[v].load(block + t * p.block_rs + c);
+      const int c = v * nt + tid;
+      s_post[v] += at(gate ? gate + group * p.gate_rs : nullptr, c, 1.0f) * s_group[v];
+      const float f = at(w_post, c, 1.0f) * s_group[v];
+      s_group[v] = 0.0f;
+      if (gate && c < p.D) {
+        if (whole) dgate[group * p.dgate_rs + c] = from_f32<T>(f);
+        else part[(group == group0 ? 2 : 3) * int64_t(p.D) + c] = f;
       }
     }
   };
-  if (row0 < row1) fetch(row0);
+  start_group();
   for (int64_t t = row0; t < row1; ++t) {
-    if (t / per != group) {
-      flush_gate();
-      group = t / per;
-      load_gate();
+    if (t == group_end) {
+      end_group();
+      ++group;
+      group_end += per;
+      start_group();
     }
-    V r[NV], x[NV], y[NV];
-    float s[NV][E];
+    const T* row_d = dres ? dres + t * p.dresid_out_rs : nullptr;
+    const T* row_y = block ? block + t * p.block_rs : nullptr;
+    float s[NV], y[NV];
 #pragma unroll
     for (int v = 0; v < NV; ++v) {
-      r[v] = nr[v];
-      x[v] = nx[v];
-      y[v] = ny[v];
-      nd[v].get(s[v]);
+      s[v] = at(row_d, v * nt + tid, 0.0f);
+      y[v] = at(row_y, v * nt + tid, 0.0f);
     }
-    if (t + 1 < row1) fetch(t + 1);
     if (dx) {
+      const T *row_r = resid_out + t * p.resid_out_rs, *row_x = dx + t * p.dnorm_out_rs;
+      float r[NV], x[NV], w[NV];
       float srr = 0.0f, ser = 0.0f;
 #pragma unroll
       for (int v = 0; v < NV; ++v) {
-        float fr[E], fx[E], fw[E];
-        r[v].get(fr);
-        x[v].get(fx);
-        vw_pre[v].get(fw);
-#pragma unroll
-        for (int i = 0; i < E; ++i) {
-          srr += fr[i] * fr[i];
-          ser += (w_pre ? fx[i] * fw[i] : fx[i]) * fr[i];
-        }
+        const int c = v * nt + tid;
+        r[v] = at(row_r, c, 0.0f);
+        x[v] = at(row_x, c, 0.0f);
+        w[v] = at(w_pre, c, 1.0f);
+        srr += r[v] * r[v];
+        ser += x[v] * w[v] * r[v];
       }
       const float2 q = block_sum2(srr, ser, smem, buf);
       const float rho = rsqrtf(q.x * inv_d + p.eps);
       const float k = rho * rho * rho * (q.y * inv_d);
 #pragma unroll
       for (int v = 0; v < NV; ++v) {
-        float fr[E], fx[E], fw[E];
-        r[v].get(fr);
-        x[v].get(fx);
-        vw_pre[v].get(fw);
-#pragma unroll
-        for (int i = 0; i < E; ++i) {
-          s[v][i] += rho * (w_pre ? fx[i] * fw[i] : fx[i]) - k * fr[i];
-          s_pre[v][i] += fx[i] * (fr[i] * rho);
-        }
+        s[v] += rho * (x[v] * w[v]) - k * r[v];
+        s_pre[v] += x[v] * (r[v] * rho);
       }
     }
+    float syy = 0.0f, sfy = 0.0f;
 #pragma unroll
     for (int v = 0; v < NV; ++v) {
-      const int c = (v * nt + tid) * E;
-      float f[E];
-#pragma unroll
-      for (int i = 0; i < E; ++i) f[i] = p.scale * s[v][i];
-      if (c < p.D) V::store(dresid + t * p.dresid_rs + c, f);
+      const int c = v * nt + tid;
+      syy += y[v] * y[v];
+      sfy += s[v] * gw[v] * y[v];
+      if (c < p.D) dresid[t * p.dresid_rs + c] = from_f32<T>(p.scale * s[v]);
     }
     if (!block) continue;
     float rho = 1.0f, k = 0.0f;
     if (w_post) {
-      float syy = 0.0f, sfy = 0.0f;
-#pragma unroll
-      for (int v = 0; v < NV; ++v) {
-        float fy[E], fg[E], fw[E];
-        y[v].get(fy);
-        vgate[v].get(fg);
-        vw_post[v].get(fw);
-#pragma unroll
-        for (int i = 0; i < E; ++i) {
-          syy += fy[i] * fy[i];
-          sfy += s[v][i] * (gate ? fg[i] : 1.0f) * fw[i] * fy[i];
-        }
-      }
       const float2 q = block_sum2(syy, sfy, smem, buf);
       rho = rsqrtf(q.x * inv_d + p.eps);
       k = rho * rho * rho * (q.y * inv_d);
     }
 #pragma unroll
     for (int v = 0; v < NV; ++v) {
-      const int c = (v * nt + tid) * E;
-      float fy[E], fg[E], fw[E], o[E];
-      y[v].get(fy);
-      vgate[v].get(fg);
-      vw_post[v].get(fw);
-#pragma unroll
-      for (int i = 0; i < E; ++i) {
-        const float dn = gate ? fg[i] * s[v][i] : s[v][i];
-        const float yhat = fy[i] * rho;
-        if (gate) s_gate[v][i] += s[v][i] * (w_post ? yhat * fw[i] : yhat);
-        s_post[v][i] += dn * yhat;
-        o[i] = w_post ? rho * (dn * fw[i]) - k * fy[i] : dn;
-      }
-      if (c < p.D) V::store(dblock + t * p.dblock_rs + c, o);
+      const int c = v * nt + tid;
+      s_group[v] += s[v] * (y[v] * rho);
+      if (c < p.D) dblock[t * p.dblock_rs + c] = from_f32<T>(rho * (s[v] * gw[v]) - k * y[v]);
     }
   }
-  if (row0 < row1) flush_gate();
+  if (row0 < row1) end_group();
+#pragma unroll
+  for (int v = 0; v < NV; ++v) {
+    const int c = v * nt + tid;
+    if (c < p.D) {
+      part[c] = s_pre[v];
+      part[p.D + c] = s_post[v];
+    }
+  }
+}
+
+// ---- pairs of fp32 values in 64-bit registers: two operations in one instruction -----------------
+__device__ __forceinline__ uint64_t pair_of(float lo, float hi) {
+  uint64_t v;
+  asm("mov.b64 %0, {%1, %2};" : "=l"(v) : "f"(lo), "f"(hi));
+  return v;
+}
+__device__ __forceinline__ float2 halves_of(uint64_t v) {
+  float2 f;
+  asm("mov.b64 {%0, %1}, %2;" : "=f"(f.x), "=f"(f.y) : "l"(v));
+  return f;
+}
+__device__ __forceinline__ uint64_t mul2(uint64_t a, uint64_t b) {
+  uint64_t d;
+  asm("mul.rn.f32x2 %0, %1, %2;" : "=l"(d) : "l"(a), "l"(b));
+  return d;
+}
+__device__ __forceinline__ uint64_t fma2(uint64_t a, uint64_t b, uint64_t c) {
+  uint64_t d;
+  asm("fma.rn.f32x2 %0, %1, %2, %3;" : "=l"(d) : "l"(a), "l"(b), "l"(c));
+  return d;
+}
+__device__ __forceinline__ float sum_of(uint64_t v) {
+  const float2 f = halves_of(v);
+  return f.x + f.y;
+}
+// 16 bytes of elements as pairs, and back.
+template <typename T>
+__device__ __forceinline__ void get_pairs(const void* from, uint64_t (&f)[16 / sizeof(T) / 2]) {
+  const uint4 w = *static_cast<const uint4*>(from);
+  const uint32_t a[4] = {w.x, w.y, w.z, w.w};
+  if constexpr (sizeof(T) == 4) {
+    f[0] = pair_of(__uint_as_float(a[0]), __uint_as_float(a[1]));
+    f[1] = pair_of(__uint_as_float(a[2]), __uint_as_float(a[3]));
+  } else {
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+      const float2 v = unpack2<T>(a[i]);
+      f[i] = pair_of(v.x, v.y);
+    }
+  }
+}
+template <typename T>
+__device__ __forceinline__ void put_pairs(void* to, const uint64_t (&f)[16 / sizeof(T) / 2]) {
+  uint32_t a[4];
+  if constexpr (sizeof(T) == 4) {
+#pragma unroll
+    for (int i = 0; i < 2; ++i) {
+      const float2 v = halves_of(f[i]);
+      a[2 * i] = __float_as_uint(v.x);
+      a[2 * i + 1] = __float_as_uint(v.y);
+    }
+  } else {
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+      const float2 v = halves_of(f[i]);
+      a[i] = pack2<T>(v.x, v.y);
+    }
+  }
+  *static_cast<uint4*>(to) = make_uint4(a[0], a[1], a[2], a[3]);
+}
+
+// Wide rows: a ring in shared memory that bulk copies fill several rows ahead, so that no registers are
+// held for what is on its way; 16 bytes of a row a thread and access, NV of them.  The arithmetic runs on
+// pairs (8.5 operations an element instead of 17: with single ones issue slots, not HBM, set the pace).
+// kAll: every array is given and the accesses cover the row exactly, as in a training step.
+template <typename T, int NV, bool kAll>
+__global__ void __launch_bounds__(512) cconv_residual_norm_backward_ring_kernel(const NormParams p) {
+  extern __shared__ __align__(128) uint8_t ring[];
+  __shared__ float2 smem[2][32];
+  __shared__ __align__(8) uint64_t full[8];
+  __shared__ int abort_flag;
+  constexpr int E = 16 / int(sizeof(T)), P = E / 2;
+  const T* dres = static_cast<const T*>(p.dresid_out);  // may be dresid
+  const T* dx = static_cast<const T*>(p.dnorm_out);
+  const T* block = static_cast<const T*>(p.block);
+  const T* resid_out = static_cast<const T*>(p.resid_out);
+  const T* __restrict__ gate = static_cast<const T*>(p.gate);
+  const T* __restrict__ w_post = static_cast<const T*>(p.w_post);
+  const T* __restrict__ w_pre = static_cast<const T*>(p.w_pre);
+  T* dresid = static_cast<T*>(p.dresid);
+  T* dblock = static_cast<T*>(p.dblock);
+  T* dgate = static_cast<T*>(p.dgate);
+  const int nt = blockDim.x, tid = threadIdx.x;
+  const bool has_dx = kAll || dx, has_dres = kAll || dres, has_block = kAll || block;
+  const bool has_pre = kAll || w_pre, has_post = kAll || w_post, has_gate = kAll || gate;
+  auto inside = [&](int v) { return kAll || (v * nt + tid) * E < p.D; };
+  const float inv_d = 1.0f / float(p.D);
+  const int64_t row0 = first_row<T>(p, blockIdx.x), row1 = first_row<T>(p, blockIdx.x + 1);
+  const int64_t per = p.rows_per_gate ? p.rows_per_gate : p.T;
+  float* part = p.part + int64_t(blockIdx.x) * 4 * p.D;
+  const uint32_t row_bytes = uint32_t(p.D) * sizeof(T), ring0 = smem_u32(ring), full0 = smem_u32(full);
+  const uint64_t one = pair_of(1.0f, 1.0f), scale = pair_of(p.scale, p.scale);
+  int buf = 0;
+  // Sums over rows, as in the kernel above.  Those of dw_post, which change only where a group ends, lie
+  // behind the ring (each thread touches its own columns alone).
+  uint64_t s_pre[NV][P], s_group[NV][P], gw[NV][P];
+  float* s_post = reinterpret_cast<float*>(ring + p.ring_rows * 4 * row_bytes);
+#pragma unroll
+  for (int v = 0; v < NV; ++v) {
+#pragma unroll
+    for (int i = 0; i < P; ++i) s_pre[v][i] = s_group[v][i] = gw[v][i] = 0;
+    if (inside(v)) {
+#pragma unroll
+      for (int i = 0; i < E; ++i) s_post[(v * nt + tid) * E + i] = 0.0f;
+    }
+  }
+  int64_t group = row0 / per, group_end = (group + 1) * per;
+  const int64_t group0 = group;
+  auto get = [&](bool given, const T* from, int v, uint64_t (&f)[P], uint64_t otherwise) {
+    if (given && inside(v)) {
+      get_pairs<T>(from + (v * nt + tid) * E, f);
+    } else {
+#pragma unroll
+      for (int i = 0; i < P; ++i) f[i] = otherwise;
+    }
+  };
+  auto start_group = [&]() {
+#pragma unroll
+    for (int v = 0; v < NV; ++v) {
+      uint64_t fg[P], fw[P];
+      get(has_gate, gate + group * p.gate_rs, v, fg, one);
+      get(has_post, w_post, v, fw, one);
+#pragma unroll
+      for (int i = 0; i < P; ++i) gw[v][i] = mul2(fg[i], fw[i]);
+    }
+  };
+  auto end_group = [&]() {
+    const int64_t g0 = group * per, g1 = group_end < p.T ? group_end : p.T;
+    const bool whole = g0 >= row0 && g1 <= row1;
+#pragma unroll
+    for (int v = 0; v < NV; ++v) {
+      const int c = (v * nt + tid) * E;
+      uint64_t fg[P], fw[P];
+      get(has_gate, gate + group * p.gate_rs, v, fg, one);
+      get(has_post, w_post, v, fw, one);
+#pragma unroll
+      for (int i = 0; i < P; ++i) {
+        if (inside(v)) {
+          const float2 q = halves_of(mul2(fg[i], s_group[v][i]));
+          s_post[c + 2 * i] += q.x;
+          s_post[c + 2 * i + 1] += q.y;
+        }
+        fw[i] = mul2(fw[i], s_group[v][i]);
+        s_group[v][i] = 0;
+      }
+      if (has_gate && inside(v)) {
+        if (whole) {
+          put_pairs<T>(dgate + group * p.dgate_rs + c, fw);
+        } else {
+          float* to = part + (group == group0 ? 2 : 3) * int64_t(p.D) + c;
+#pragma unroll
+          for (int i = 0; i < P; ++i) *reinterpret_cast<uint64_t*>(to + 2 * i) = fw[i];
+        }
+      }
+    }
+  };
+  // arrays of a row in the ring: r', dx, dr', y (those that are given)
+  auto copy_row = [&](int64_t t) {
+    const uint32_t st = uint32_t(t - row0) % uint32_t(p.ring_rows), bar = full0 + 8 * st;
+    const uint32_t to = ring0 + st * 4 * row_bytes;
+    mbar_arrive_expect_tx(bar, row_bytes * uint32_t((has_dx ? 2 : 0) + (has_dres ? 1 : 0) + (has_block ? 1 : 0)));
+    if (has_dx) {
+      bulk_load(to, resid_out + t * p.resid_out_rs, row_bytes, bar);
+      bulk_load(to + row_bytes, dx + t * p.dnorm_out_rs, row_bytes, bar);
+    }
+    if (has_dres) bulk_load(to + 2 * row_bytes, dres + t * p.dresid_out_rs, row_bytes, bar);
+    if (has_block) bulk_load(to + 3 * row_bytes, block + t * p.block_rs, row_bytes, bar);
+  };
+  if (tid == 0) {
+    abort_flag = 0;
+    for (int i = 0; i < p.ring_rows; ++i) mbar_init(full0 + 8 * i, 1);
+    fence_barrier_init();
+    for (int64_t t = row0; t < row1 && t < row0 + p.ring_rows; ++t) copy_row(t);
+  }
+  __syncthreads();
+  start_group();
+  uint32_t st = 0, phase = 0;
+  int64_t t = row0;
+  for (; t < row1; ++t) {
+    const bool ok = mbar_wait(full0 + 8 * st, phase, &abort_flag, p.status, kStatProducerWait, p.limit_ns);
+    // every thread is past the row before: its place in the ring is free
+    if (!__syncthreads_and(ok)) break;
+    if (tid == 0 && t > row0 && t - 1 + p.ring_rows < row1) copy_row(t - 1 + p.ring_rows);
+    const T* row_r = reinterpret_cast<const T*>(ring + st * 4 * row_bytes);
+    const T *row_x = row_r + p.D, *row_d = row_x + p.D, *row_y = row_d + p.D;
+    if (++st == uint32_t(p.ring_rows)) st = 0, phase ^= 1;
+    if (t == group_end) {
+      end_group();
+      ++group;
+      group_end += per;
+      start_group();
+    }
+    uint64_t s[NV][P];
+    if (has_dx) {
+      uint64_t r[NV][P], x[NV][P], srr = 0, ser = 0;
+#pragma unroll
+      for (int v = 0; v < NV; ++v) {
+        uint64_t w[P];
+        get(true, row_r, v, r[v], 0);
+        get(true, row_x, v, x[v], 0);
+        get(has_pre, w_pre, v, w, one);
+#pragma unroll
+        for (int i = 0; i < P; ++i) {
+          srr = fma2(r[v][i], r[v][i], srr);
+          ser = fma2(mul2(x[v][i], w[i]), r[v][i], ser);
+        }
+      }
+      const float2 q = block_sum2(sum_of(srr), sum_of(ser), smem, buf);
+      const float rho1 = rsqrtf(q.x * inv_d + p.eps);
+      const float k1 = -rho1 * rho1 * rho1 * (q.y * inv_d);
+      const uint64_t rho = pair_of(rho1, rho1), k = pair_of(k1, k1);
+#pragma unroll
+      for (int v = 0; v < NV; ++v) {
+        uint64_t w[P];
+        get(has_pre, w_pre, v, w, one);
+        get(has_dres, row_d, v, s[v], 0);
+#pragma unroll
+        for (int i = 0; i < P; ++i) {
+          s[v][i] = fma2(x[v][i], mul2(w[i], rho), fma2(r[v][i], k, s[v][i]));
+          s_pre[v][i] = fma2(x[v][i], mul2(r[v][i], rho), s_pre[v][i]);
+        }
+      }
+    } else {
+#pragma unroll
+      for (int v = 0; v < NV; ++v) get(has_dres, row_d, v, s[v], 0);
+    }
+    uint64_t y[NV][P], syy = 0, sfy = 0;
+#pragma unroll
+    for (int v = 0; v < NV; ++v) {
+      uint64_t f[P];
+      get(has_block, row_y, v, y[v], 0);
+#pragma unroll
+      for (int i = 0; i < P; ++i) {
+        f[i] = mul2(scale, s[v][i]);
+        syy = fma2(y[v][i], y[v][i], syy);
+        sfy = fma2(mul2(s[v][i], gw[v][i]), y[v][i], sfy);
+      }
+      if (inside(v)) put_pairs<T>(dresid + t * p.dresid_rs + (v * nt + tid) * E, f);
+    }
+    if (!has_block) continue;
+    uint64_t rho = one, k = 0;
+    if (has_post) {
+      const float2 q = block_sum2(sum_of(syy), sum_of(sfy), smem, buf);
+      const float rho1 = rsqrtf(q.x * inv_d + p.eps);
+      const float k1 = -rho1 * rho1 * rho1 * (q.y * inv_d);
+      rho = pair_of(rho1, rho1);
+      k = pair_of(k1, k1);
+    }
+#pragma unroll
+    for (int v = 0; v < NV; ++v) {
+      uint64_t o[P];
+#pragma unroll
+      for (int i = 0; i < P; ++i) {
+        s_group[v][i] = fma2(s[v][i], mul2(y[v][i], rho), s_group[v][i]);
+        o[i] = fma2(y[v][i], k, mul2(rho, mul2(s[v][i], gw[v][i])));
+      }
+      if (inside(v)) put_pairs<T>(dblock + t * p.dblock_rs + (v * nt + tid) * E, o);
+    }
+  }
+  if (t < row1) {  // a copy did not come in time: let those on their way land
+    const uint64_t t0 = globaltimer_ns();
+    while (globaltimer_ns() - t0 < 200000) {
+    }
+    return;
+  }
+  if (row0 < row1) end_group();
 #pragma unroll
   for (int v = 0; v < NV; ++v) {
     const int c = (v * nt + tid) * E;
-    if (c < p.D) {
+    if (inside(v)) {
 #pragma unroll
-      for (int i = 0; i < E; ++i) {
-        part[c + i] = s_pre[v][i];
-        part[p.D + c + i] = s_post[v][i];
+      for (int i = 0; i < P; ++i) {
+        *reinterpret_cast<uint64_t*>(part + c + 2 * i) = s_pre[v][i];
+        part[p.D + c + 2 * i] = s_post[c + 2 * i];
+        part[p.D + c + 2 * i + 1] = s_post[c + 2 * i + 1];
       }
     }
   }
@@ -513,10 +723,10 @@ __global__ void __launch_bounds__(512) cconv_residual_norm_backward_long_kernel(
 
 // Adds up the partial table: blockIdx.y 0: dw_pre, 1: dw_post, 2 + i: a gate group that lies in
 // several blocks -- group i, or where there are more groups than blocks the one that the rows of block
-// i end in, if block i is the first that it lies in.  32 columns by 8 slices of the table a block.
+// i end in, if block i is the first that it lies in.  32 columns by 16 slices of the table a block.
 template <typename T>
-__global__ void __launch_bounds__(256) cconv_residual_norm_sums_kernel(const NormParams p) {
-  __shared__ float smem[8][33];
+__global__ void __launch_bounds__(512) cconv_residual_norm_sums_kernel(const NormParams p) {
+  __shared__ float smem[16][33];
   asm volatile("griddepcontrol.wait;" ::: "memory");
   const int c = blockIdx.x * 32 + (threadIdx.x & 31), slice = threadIdx.x >> 5;
   const int64_t per = p.rows_per_gate ? p.rows_per_gate : p.T;
@@ -537,19 +747,49 @@ __global__ void __launch_bounds__(256) cconv_residual_norm_sums_kernel(const Nor
   }
   float s = 0.0f;
   if (c < p.D) {
-    for (int b = b0 + slice; b <= b1; b += 8) {
-      int at = slot;
-      if (blockIdx.y >= 2) at = first_row<T>(p, b) / per == group ? 2 : 3;
-      s += p.part[(int64_t(b) * 4 + at) * p.D + c];
+    const float* from = p.part + int64_t(slot) * p.D + c;
+    if (blockIdx.y >= 2) {
+      // the group's rows are the last group of its first block and the first of the others, unless they
+      // begin that block
+      const int at = first_row<T>(p, b0) / per == group ? 2 : 3;
+      from = p.part + 2 * int64_t(p.D) + c;
+      if (slice == 0 && at == 3) s = from[int64_t(b0) * 4 * p.D + p.D];
+      if (at == 3) ++b0;
     }
+    const int64_t step = 4 * int64_t(p.D);
+    float a[4] = {s, 0.0f, 0.0f, 0.0f};
+    int b = b0 + slice;
+    for (; b + 48 <= b1; b += 64) {
+#pragma unroll
+      for (int i = 0; i < 4; ++i) a[i] += from[(b + 16 * i) * step];
+    }
+    for (; b <= b1; b += 16) a[0] += from[b * step];
+    s = (a[0] + a[1]) + (a[2] + a[3]);
   }
   smem[slice][threadIdx.x & 31] = s;
   __syncthreads();
   if (slice == 0 && c < p.D) {
 #pragma unroll
-    for (int i = 1; i < 8; ++i) s += smem[i][threadIdx.x];
+    for (int i = 1; i < 16; ++i) s += smem[i][threadIdx.x];
     to[c] = from_f32<T>(s);
   }
+}
+
+// Shared memory of an SM for the rings of the backward blocks on it, and what a block has besides (its own
+// few KB, and the sums of dw_post).
+constexpr int64_t kRingSmem = 216 * 1024, kRingOwn = 2048;
+int64_t ring_rows(int64_t D, int es, int64_t blocks) {
+  return (kRingSmem / blocks / 1024 * 1024 - kRingOwn - 4 * D) / (4 * D * es);
+}
+// Backward blocks that share an SM: about 512 threads of 16 elements, so that one block's row covers the
+// other's reductions while the table of partial sums stays small against the arrays (at D = 4096, bf16:
+// two blocks of 256 threads; with 8 elements a thread, two blocks of 512, it took 1.4 times as long); fewer where a
+// ring of each would not hold two rows.
+int64_t blocks_an_sm(int64_t D, int es) {
+  const int64_t threads = std::max<int64_t>(32, std::min<int64_t>(512, round_up64(cdiv64(D, 16), 32)));
+  int64_t n = std::min<int64_t>(16, 512 / threads);
+  while (n > 1 && ring_rows(D, es, n) < 2) --n;
+  return n;
 }
 
 // Threads a block and accesses a thread for rows of D elements taken E at a time: at most `held`
@@ -621,47 +861,61 @@ cudaError_t launch_forward(const NormParams& p, int sms, cudaStream_t s) {
   return cudaGetLastError();
 }
 
-template <typename T, int E, int NV>
-void launch_backward_nv(const NormParams& p, int threads, cudaStream_t s) {
-  cconv_residual_norm_backward_kernel<T, E, NV><<<unsigned(p.nb), threads, 0, s>>>(p);
+template <typename T, int NV, bool kAll>
+cudaError_t launch_ring(NormParams p, int threads, cudaStream_t s) {
+  auto f = cconv_residual_norm_backward_ring_kernel<T, NV, kAll>;
+  static bool ready[64] = {};
+  int dev = 0;
+  cudaError_t e = cudaGetDevice(&dev);
+  if (e != cudaSuccess) return e;
+  if (!__atomic_load_n(&ready[dev & 63], __ATOMIC_ACQUIRE)) {
+    e = cudaFuncSetAttribute(f, cudaFuncAttributeMaxDynamicSharedMemorySize, int(kRingSmem));
+    if (e != cudaSuccess) return e;
+    __atomic_store_n(&ready[dev & 63], true, __ATOMIC_RELEASE);
+  }
+  p.ring_rows = int(std::min<int64_t>(8, ring_rows(p.D, sizeof(T), blocks_an_sm(p.D, sizeof(T)))));
+  f<<<unsigned(p.nb), threads, size_t(p.D) * (size_t(p.ring_rows) * 4 * sizeof(T) + 4), s>>>(p);
+  return cudaGetLastError();
 }
 
 template <typename T>
 cudaError_t launch_backward(const NormParams& p, cudaStream_t s) {
   constexpr int kWide = 16 / int(sizeof(T));
-  const bool w = wide(p, sizeof(T), true);
+  const bool w = wide(p, sizeof(T), true) && ring_rows(p.D, sizeof(T), blocks_an_sm(p.D, sizeof(T))) >= 2;
   const Shape sh = shape_of(p.D, w ? kWide : 1, 16, 512);
+  const bool all = p.dnorm_out && p.dresid_out && p.block && p.w_pre && p.w_post && p.gate &&
+                   p.D == int64_t(sh.threads) * sh.nv * kWide;
+  cudaError_t e = cudaSuccess;
   if (!sh.threads) {
     cconv_residual_norm_backward_long_kernel<T><<<unsigned(p.nb), 512, 0, s>>>(p);
+    e = cudaGetLastError();
   } else if (w) {
-    if (sh.nv == 1) launch_backward_nv<T, kWide, 1>(p, sh.threads, s);
-    else if (sh.nv == 2) launch_backward_nv<T, kWide, 2>(p, sh.threads, s);
-    else launch_backward_nv<T, kWide, sizeof(T) == 4 ? 4 : 2>(p, sh.threads, s);
+    constexpr int kMost = 16 / kWide;
+    if (sh.nv == 1) e = all ? launch_ring<T, 1, true>(p, sh.threads, s) : launch_ring<T, 1, false>(p, sh.threads, s);
+    else if (sh.nv == 2) e = all ? launch_ring<T, 2, true>(p, sh.threads, s) : launch_ring<T, 2, false>(p, sh.threads, s);
+    else e = all ? launch_ring<T, kMost, true>(p, sh.threads, s) : launch_ring<T, kMost, false>(p, sh.threads, s);
   } else {
-    if (sh.nv == 1) launch_backward_nv<T, 1, 1>(p, sh.threads, s);
-    else if (sh.nv == 2) launch_backward_nv<T, 1, 2>(p, sh.threads, s);
-    else if (sh.nv == 4) launch_backward_nv<T, 1, 4>(p, sh.threads, s);
-    else if (sh.nv == 8) launch_backward_nv<T, 1, 8>(p, sh.threads, s);
-    else launch_backward_nv<T, 1, 16>(p, sh.threads, s);
+    if (sh.nv == 1) cconv_residual_norm_backward_kernel<T, 1><<<unsigned(p.nb), sh.threads, 0, s>>>(p);
+    else if (sh.nv == 2) cconv_residual_norm_backward_kernel<T, 2><<<unsigned(p.nb), sh.threads, 0, s>>>(p);
+    else if (sh.nv == 4) cconv_residual_norm_backward_kernel<T, 4><<<unsigned(p.nb), sh.threads, 0, s>>>(p);
+    else if (sh.nv == 8) cconv_residual_norm_backward_kernel<T, 8><<<unsigned(p.nb), sh.threads, 0, s>>>(p);
+    else cconv_residual_norm_backward_kernel<T, 16><<<unsigned(p.nb), sh.threads, 0, s>>>(p);
+    e = cudaGetLastError();
   }
-  cudaError_t e = cudaGetLastError();
   if (e != cudaSuccess) return e;
   NormParams q = p;
   const int64_t per = p.rows_per_gate ? p.rows_per_gate : p.T, groups = cdiv64(p.T, per);
   q.sums_by_group = groups <= p.nb;
   const int64_t items = !p.gate || per == 1 ? 0 : q.sums_by_group ? groups : p.nb - 1;
   const dim3 grid(unsigned(cdiv64(p.D, 32)), unsigned(2 + items));
-  cconv_residual_norm_sums_kernel<T><<<grid, 256, 0, s>>>(q);
+  cconv_residual_norm_sums_kernel<T><<<grid, 512, 0, s>>>(q);
   return cudaGetLastError();
 }
 
 }  // namespace
 
-int norm_backward_blocks(int64_t T, int64_t D, int sms) {
-  // about 512 threads of rows an SM: rows in flight cover the latency of HBM, and the table of
-  // partial sums stays small against the arrays
-  const int64_t threads = std::max<int64_t>(32, std::min<int64_t>(512, round_up64(cdiv64(D, 16), 32)));
-  return int(std::max<int64_t>(1, std::min<int64_t>(T, int64_t(sms) * std::min<int64_t>(16, 512 / threads))));
+int norm_backward_blocks(int64_t T, int64_t D, int es, int sms) {
+  return int(std::max<int64_t>(1, std::min<int64_t>(T, int64_t(sms) * blocks_an_sm(D, es))));
 }
 
 cudaError_t run_norm_forward(const NormParams& p, int dtype, int sms, cudaStream_t s) {

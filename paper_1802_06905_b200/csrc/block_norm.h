@@ -17,10 +17,13 @@ struct NormParams {
   int64_t resid_rs, block_rs, gate_rs, resid_out_rs, norm_out_rs, dresid_out_rs, dnorm_out_rs, dresid_rs,
       dblock_rs, dgate_rs;
   int sums_by_group;
+  int ring_rows;    // rows of the shared-memory ring
+  int* status;      // where a bounded wait that ran out is noted
+  uint64_t limit_ns;
   float* part;  // backward: [nb][4][D], and [nb][D] more for rows that registers cannot hold
 };
 
-int norm_backward_blocks(int64_t T, int64_t D, int sms);
+int norm_backward_blocks(int64_t T, int64_t D, int es, int sms);
 cudaError_t run_norm_forward(const NormParams& p, int dtype, int sms, cudaStream_t s);
 cudaError_t run_norm_backward(const NormParams& p, int dtype, cudaStream_t s);
 
