@@ -133,20 +133,6 @@ uint32_t scale_bytes(int epi) { return epi == kScaled ? 2 * kEpilogueWarps * kSc
 template <int kEpi>
 constexpr bool kEightBit = kEpi == kScaled || kEpi == kScaledPartial;
 
-// Pairs of fp32 values in a 64-bit register: two multiply-adds in one instruction, d = a * s + d.
-__device__ __forceinline__ uint64_t pair_of(float lo, float hi) {
-  uint64_t v;
-  asm("mov.b64 %0, {%1, %2};" : "=l"(v) : "f"(lo), "f"(hi));
-  return v;
-}
-__device__ __forceinline__ float2 halves_of(uint64_t v) {
-  float2 f;
-  asm("mov.b64 {%0, %1}, %2;" : "=f"(f.x), "=f"(f.y) : "l"(v));
-  return f;
-}
-__device__ __forceinline__ void fma2(uint64_t& d, uint64_t a, uint64_t s) {
-  asm("fma.rn.f32x2 %0, %1, %2, %0;" : "+l"(d) : "l"(a), "l"(s));
-}
 __device__ __forceinline__ void cp_async4(uint32_t to, const float* from, bool there) {
   asm volatile("cp.async.ca.shared.global [%0], [%1], 4, %2;" ::"r"(to), "l"(from), "r"(there ? 4 : 0) : "memory");
 }
@@ -479,7 +465,8 @@ __global__ void __launch_bounds__(kThreads, 1) cconv_pair_product_kernel(const _
           auto add = [&](int c) {
 #pragma unroll
             for (int i = 0; i < 16; ++i)
-              fma2(sum[c * 16 + i], pair_of(__uint_as_float(f[c & 1][2 * i]), __uint_as_float(f[c & 1][2 * i + 1])), scale);
+              sum[c * 16 + i] = fma2(pair_of(__uint_as_float(f[c & 1][2 * i]), __uint_as_float(f[c & 1][2 * i + 1])), scale,
+                                     sum[c * 16 + i]);
           };
           tmem_ld_32x32b_x32(acc + half * cols, f[0]);
           tmem_ld_32x32b_x32(acc + half * cols + 32, f[1]);

@@ -3,10 +3,8 @@
 //   scale = max|x| / 448,  q = e4m3(x / scale), nearest, ties to even
 //
 // One pass: the values of a block stay in registers between its maximum and its rounding.  Bound by HBM:
-// 2 bytes read and 1 written an element (16-bit x).  Both quotients are IEEE divisions, so that
-// the result is the definition's bit for bit.
-#include <cuda_fp8.h>
-
+// 2 bytes read and 1 written an element (16-bit x).  Both quotients are correctly rounded, so that the
+// result is the definition's bit for bit.
 #include <algorithm>
 
 #include "block.h"
@@ -18,101 +16,196 @@ namespace {
 
 constexpr float kMax = 448.0f;
 
-// max that keeps a NaN (fmaxf would drop it)
-__device__ __forceinline__ float max_nan(float a, float b) { return (a > b || a != a) ? a : b; }
-
-__device__ __forceinline__ uint32_t e4m3x4(float a, float b, float c, float d) {
-  const __nv_fp8x2_storage_t lo = __nv_cvt_float2_to_fp8x2(make_float2(a, b), __NV_SATFINITE, __NV_E4M3);
-  const __nv_fp8x2_storage_t hi = __nv_cvt_float2_to_fp8x2(make_float2(c, d), __NV_SATFINITE, __NV_E4M3);
+// Four values as e4m3, nearest (ties to even), at most +-448 in size.
+__device__ __forceinline__ uint32_t e4m3x4(uint64_t ab, uint64_t cd) {
+  const float2 x = halves_of(ab), y = halves_of(cd);
+  uint16_t lo, hi;
+  asm("cvt.rn.satfinite.e4m3x2.f32 %0, %1, %2;" : "=h"(lo) : "f"(x.y), "f"(x.x));
+  asm("cvt.rn.satfinite.e4m3x2.f32 %0, %1, %2;" : "=h"(hi) : "f"(y.y), "f"(y.x));
   return uint32_t(lo) | uint32_t(hi) << 16;
 }
 
-// Eight elements from p, of which the first n are in range (kWide: all or, n <= 0, none).
+// x / s, correctly rounded, for one s and many x.  A quotient of its own for each element keeps the
+// reciprocal unit busier than HBM (8192 x 4096 bf16: 39 us).  Markstein's method instead (IBM J. Res. Dev. 34, 1990):
+// with y = 1/s correctly rounded, q + (x - q s) y is correctly rounded once q is within an ulp, which one
+// such step from x y makes it; the residuals are exact in a fused multiply-add.  It needs scales whose
+// reciprocal and residuals neither overflow nor underflow; others (and NaN) divide.
+__device__ __noinline__ uint64_t divide_pair(uint64_t f, float s) {
+  const float2 v = halves_of(f);
+  return pair_of(__fdiv_rn(v.x, s), __fdiv_rn(v.y, s));
+}
+struct Divisor {
+  float s;
+  uint64_t y2, minus_s2;
+  bool quick;
+  // of a scale and its reciprocal (a scale of 0, of a block of zeros, divides by 1)
+  __device__ __forceinline__ Divisor(float scale, float y) {
+    s = scale == 0.0f ? 1.0f : scale;
+    y2 = pair_of(y, y);
+    minus_s2 = pair_of(-s, -s);
+    quick = s > 1e-25f && s < 1e25f;
+  }
+  __device__ __forceinline__ void divide(uint64_t (&f)[4]) const {
+    if (quick) {
+#pragma unroll
+      for (int i = 0; i < 4; ++i) {
+        uint64_t q = mul2(f[i], y2);
+        q = fma2(fma2(q, minus_s2, f[i]), y2, q);
+        f[i] = fma2(fma2(q, minus_s2, f[i]), y2, q);
+      }
+    } else {
+#pragma unroll
+      for (int i = 0; i < 4; ++i) f[i] = divide_pair(f[i], s);
+    }
+  }
+};
+
+// The size of a value as an integer of the same order, in which a NaN is the largest.
+__device__ __forceinline__ uint32_t size_of(float v) { return __float_as_uint(v) & 0x7fffffffu; }
+
+// Eight elements of a row: packed (16-bit types, 16 bytes at once) or one by one.
 template <typename T, bool kWide>
-__device__ __forceinline__ void load8(float (&f)[8], const T* p, int64_t cs, int64_t n) {
-  if constexpr (kWide && sizeof(T) == 2) {
-    uint4 w = make_uint4(0, 0, 0, 0);
-    if (n > 0) w = *reinterpret_cast<const uint4*>(p);
-    const float2 a = unpack2<T>(w.x), b = unpack2<T>(w.y), c = unpack2<T>(w.z), d = unpack2<T>(w.w);
-    f[0] = a.x; f[1] = a.y; f[2] = b.x; f[3] = b.y; f[4] = c.x; f[5] = c.y; f[6] = d.x; f[7] = d.y;
-  } else {
+struct Eight {
+  float f[8];
+  __device__ __forceinline__ void load(const T* p, int64_t cs, int64_t n) {  // the first n are in range
 #pragma unroll
     for (int i = 0; i < 8; ++i) f[i] = i < n ? to_f32(p[i * cs]) : 0.0f;
   }
-}
+  __device__ __forceinline__ void get(uint64_t (&o)[4]) const {
+#pragma unroll
+    for (int i = 0; i < 4; ++i) o[i] = pair_of(f[2 * i], f[2 * i + 1]);
+  }
+  __device__ __forceinline__ uint32_t largest() const {  // as size_of
+    uint32_t m = 0;
+#pragma unroll
+    for (int i = 0; i < 8; ++i) m = max(m, size_of(f[i]));
+    return m;
+  }
+};
+template <typename T>
+struct Eight<T, true> {
+  uint4 w;
+  __device__ __forceinline__ void load(const T* p, int64_t, int64_t n) {  // all are in range or, n <= 0, none
+    w = make_uint4(0, 0, 0, 0);
+    if (n > 0) w = *reinterpret_cast<const uint4*>(p);
+  }
+  __device__ __forceinline__ void get(uint64_t (&f)[4]) const {
+    const float2 a = unpack2<T>(w.x), b = unpack2<T>(w.y), c = unpack2<T>(w.z), d = unpack2<T>(w.w);
+    f[0] = pair_of(a.x, a.y);
+    f[1] = pair_of(b.x, b.y);
+    f[2] = pair_of(c.x, c.y);
+    f[3] = pair_of(d.x, d.y);
+  }
+  __device__ __forceinline__ uint32_t largest() const {
+    constexpr uint32_t k = 0x7fff7fffu;  // sizes of both halves order like 15-bit integers
+    const uint32_t m = __vmaxu2(__vmaxu2(w.x & k, w.y & k), __vmaxu2(w.z & k, w.w & k));
+    const float2 v = unpack2<T>(m);
+    return max(size_of(v.x), size_of(v.y));
+  }
+};
 
-// 16 lanes a 128-channel group, 8 channels a lane; kRows groups (rows) a lane: 1 (a block is one token's
-// group) or 8 (a CTA of 256 threads takes 16 x 8 = 128 rows).
-template <typename T, int kRows, bool kWide>
-__global__ void __launch_bounds__(256) cconv_quantize_kernel(const QuantParams p) {
-  __shared__ float smem[8];
+// kLanes lanes a row of 128 channels (pieces of 8 channels, 8 kLanes apart), U rows a lane.  kBlock = 1:
+// each row has a scale, 256 threads.  kBlock = 128: 512 threads take 128 rows and one scale.
+// What a row costs besides its elements (the reduction, the scale, its addresses) keeps the issue slots
+// busier than the elements do; 8 lanes a row share it among fewer threads than 16 (tokens 8192 x 4096
+// bf16: 28.5 us with 16).
+template <typename T, int kBlock, int kLanes, int U, bool kWide>
+__global__ void __launch_bounds__(kBlock == 1 ? 256 : 512, U == 2 ? 4 : 1) cconv_quantize_kernel(const QuantParams p) {
+  constexpr int kAcross = (kBlock == 1 ? 256 : 512) / kLanes, kPieces = 16 / kLanes;
+  static_assert(kBlock == 1 || U * kAcross == 128, "");
+  __shared__ uint32_t smem[16];
   const T* x = static_cast<const T*>(p.x);
-  const int sub = threadIdx.x & 15, row_in = threadIdx.x >> 4;
-  for (int64_t b = blockIdx.x; b < p.blocks; b += gridDim.x) {
-    const int64_t cb = b % p.col_blocks, rb = b / p.col_blocks;
-    const int64_t c = cb * 128 + sub * 8;
-    float f[kRows][8];
-    float m = 0.0f;
+  const int sub = threadIdx.x % kLanes, row_in = threadIdx.x / kLanes;
+  const int64_t cb = blockIdx.x, c = cb * 128 + sub * 8;
+  const int cols = int(min(p.D - c, int64_t(128)));  // from c on; may be negative
+  for (int64_t rb = blockIdx.y; rb < p.row_blocks; rb += gridDim.y) {
+    const int64_t t0 = rb * U * kAcross + row_in;
+    const int rows = int(min(int64_t(U * kAcross), p.T - t0));  // from t0 on; may be negative
+    const T* from = x + t0 * p.x_rs + c * p.x_cs;
+    uint8_t* q = p.q + t0 * p.q_rs + c * p.q_cs;
+    float* scales = p.scale + (kBlock == 1 ? t0 : rb) * p.scale_rs + cb * p.scale_cs;
+    Eight<T, kWide> v[U][kPieces];
+    uint32_t m[U];
 #pragma unroll
-    for (int i = 0; i < kRows; ++i) {
-      const int64_t t = (rb * kRows + i) * 16 + row_in;
-      load8<T, kWide>(f[i], x + t * p.x_rs + c * p.x_cs, p.x_cs, t < p.T ? p.D - c : 0);
+    for (int i = 0; i < U; ++i)
 #pragma unroll
-      for (int j = 0; j < 8; ++j) m = max_nan(fabsf(f[i][j]), m);
+      for (int j = 0; j < kPieces; ++j)
+        v[i][j].load(from + i * (kAcross * p.x_rs) + j * (8 * kLanes * p.x_cs), p.x_cs, i * kAcross < rows ? cols - j * 8 * kLanes : 0);
+#pragma unroll
+    for (int i = 0; i < U; ++i) {
+      m[i] = v[i][0].largest();
+      if (kPieces == 2) m[i] = max(m[i], v[i][kPieces - 1].largest());
     }
+    if constexpr (kBlock == 1) {
 #pragma unroll
-    for (int o = 8; o > 0; o >>= 1) m = max_nan(__shfl_xor_sync(0xffffffffu, m, o), m);
-    if (kRows > 1) {
-      m = max_nan(__shfl_xor_sync(0xffffffffu, m, 16), m);
-      if ((threadIdx.x & 31) == 0) smem[threadIdx.x >> 5] = m;
+      for (int o = kLanes / 2; o > 0; o >>= 1)
+#pragma unroll
+        for (int i = 0; i < U; ++i) m[i] = max(m[i], __shfl_xor_sync(0xffffffffu, m[i], o));
+    } else {
+#pragma unroll
+      for (int i = 1; i < U; ++i) m[0] = max(m[0], m[i]);
+      m[0] = __reduce_max_sync(0xffffffffu, m[0]);
+      if ((threadIdx.x & 31) == 0) smem[threadIdx.x >> 5] = m[0];
       __syncthreads();
-#pragma unroll
-      for (int i = 0; i < 8; ++i) m = max_nan(smem[i], m);
+      m[0] = __reduce_max_sync(0xffffffffu, smem[threadIdx.x & 15]);
       __syncthreads();
     }
-    const float scale = __fdiv_rn(m, kMax);
-    const float by = scale == 0.0f ? 1.0f : scale;
-    if (kRows > 1) {
-      if (threadIdx.x == 0) p.scale[rb * p.scale_rs + cb * p.scale_cs] = scale;
-    } else if (sub == 0 && rb * 16 + row_in < p.T) {
-      p.scale[(rb * 16 + row_in) * p.scale_rs + cb * p.scale_cs] = scale;
+    // Each lane divides for one row, and the rows' scales go round.
+    uint32_t mine = m[0];
+    if (kBlock == 1) {
+#pragma unroll
+      for (int i = 1; i < U; ++i) mine = (sub & 3) == i ? m[i] : mine;
     }
+    const float my_scale = __fdiv_rn(__uint_as_float(mine), kMax);
+    const float my_recip = __fdiv_rn(1.0f, my_scale == 0.0f ? 1.0f : my_scale);
+    if (kBlock == 1 ? sub < U && sub * kAcross < rows : threadIdx.x == 0)
+      scales[kBlock == 1 ? sub * (kAcross * p.scale_rs) : 0] = my_scale;
 #pragma unroll
-    for (int i = 0; i < kRows; ++i) {
-      const int64_t t = (rb * kRows + i) * 16 + row_in;
-      if (t >= p.T) continue;
+    for (int i = 0; i < U; ++i) {
+      const float scale = kBlock == 1 ? __shfl_sync(0xffffffffu, my_scale, i, 4) : my_scale;
+      const float recip = kBlock == 1 ? __shfl_sync(0xffffffffu, my_recip, i, 4) : my_recip;
+      const Divisor by(scale, recip);
 #pragma unroll
-      for (int j = 0; j < 8; ++j) f[i][j] = __fdiv_rn(f[i][j], by);
-      const uint32_t lo = e4m3x4(f[i][0], f[i][1], f[i][2], f[i][3]);
-      const uint32_t hi = e4m3x4(f[i][4], f[i][5], f[i][6], f[i][7]);
-      uint8_t* q = p.q + t * p.q_rs + c * p.q_cs;
-      if (kWide) {
-        if (c < p.D) *reinterpret_cast<uint2*>(q) = make_uint2(lo, hi);
-      } else {
+      for (int j = 0; j < kPieces; ++j) {
+        uint64_t f[4];
+        v[i][j].get(f);
+        by.divide(f);
+        const int n = i * kAcross < rows ? cols - j * 8 * kLanes : 0;  // of eight channels, in range
+        const uint32_t lo = e4m3x4(f[0], f[1]), hi = e4m3x4(f[2], f[3]);
+        uint8_t* to = q + i * (kAcross * p.q_rs) + j * (8 * kLanes * p.q_cs);
+        if (kWide) {
+          if (n > 0) *reinterpret_cast<uint2*>(to) = make_uint2(lo, hi);
+        } else {
 #pragma unroll
-        for (int j = 0; j < 8; ++j)
-          if (c + j < p.D) q[j * p.q_cs] = uint8_t((j < 4 ? lo : hi) >> (8 * (j & 3)));
+          for (int e = 0; e < 8; ++e)
+            if (e < n) to[e * p.q_cs] = uint8_t((e < 4 ? lo : hi) >> (8 * (e & 3)));
+        }
       }
     }
   }
 }
 
+template <typename T, int kBlock, int kLanes, int U, bool kWide>
+cudaError_t launch_as(QuantParams p, cudaStream_t s) {
+  p.row_blocks = cdiv64(p.T, kBlock == 1 ? 256 / kLanes * U : 128);
+  const dim3 grid(unsigned(cdiv64(p.D, 128)), unsigned(std::min<int64_t>(p.row_blocks, 65535)));
+  cconv_quantize_kernel<T, kBlock, kLanes, U, kWide><<<grid, kBlock == 1 ? 256 : 512, 0, s>>>(p);
+  return cudaGetLastError();
+}
+
 template <typename T>
-cudaError_t launch(QuantParams p, int block_rows, int sms, cudaStream_t s) {
+cudaError_t launch(const QuantParams& p, int block_rows, int sms, cudaStream_t s) {
   const uintptr_t in = reinterpret_cast<uintptr_t>(p.x) | uintptr_t(p.x_rs * int64_t(sizeof(T)));
   const uintptr_t out = reinterpret_cast<uintptr_t>(p.q) | uintptr_t(p.q_rs);
   const bool wide = sizeof(T) == 2 && p.D % 8 == 0 && p.x_cs == 1 && p.q_cs == 1 && (in & 15) == 0 && (out & 7) == 0;
-  p.col_blocks = cdiv64(p.D, 128);
-  p.blocks = p.col_blocks * cdiv64(p.T, block_rows == 1 ? 16 : 128);
-  const unsigned grid = unsigned(std::min<int64_t>(p.blocks, int64_t(sms) * 64));
-  if (block_rows == 1) {
-    if (wide) cconv_quantize_kernel<T, 1, true><<<grid, 256, 0, s>>>(p);
-    else cconv_quantize_kernel<T, 1, false><<<grid, 256, 0, s>>>(p);
-  } else {
-    if (wide) cconv_quantize_kernel<T, 8, true><<<grid, 256, 0, s>>>(p);
-    else cconv_quantize_kernel<T, 8, false><<<grid, 256, 0, s>>>(p);
+  if constexpr (sizeof(T) == 2) {
+    if (wide && block_rows == 128) return launch_as<T, 128, 16, 4, true>(p, s);
+    // two rows a lane where that still fills the SMs (loads on their way cover HBM's latency), else one
+    if (wide && cdiv64(p.T, 64) * cdiv64(p.D, 128) >= 4 * sms) return launch_as<T, 1, 8, 2, true>(p, s);
+    if (wide) return launch_as<T, 1, 16, 1, true>(p, s);
   }
-  return cudaGetLastError();
+  if (block_rows == 128) return launch_as<T, 128, 16, 4, false>(p, s);
+  return launch_as<T, 1, 16, 1, false>(p, s);
 }
 
 }  // namespace

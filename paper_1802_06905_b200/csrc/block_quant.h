@@ -12,7 +12,7 @@ struct QuantParams {
   uint8_t* q;
   float* scale;
   int64_t x_rs, x_cs, q_rs, q_cs, scale_rs, scale_cs;
-  int64_t col_blocks, blocks;  // filled in by the launcher
+  int64_t row_blocks;  // filled in by the launcher
 };
 
 cudaError_t run_quantize(const QuantParams& p, int dtype, int block_rows, int sms, cudaStream_t s);
