@@ -16,6 +16,7 @@
 #include <algorithm>
 
 #include "block.h"
+#include "block_few.h"
 #include "block_gemm.h"
 
 namespace cconv {
@@ -32,6 +33,15 @@ class Runner {
   void forward() {
     const int64_t T = a_.T, D = a_.D, F = a_.F;
     const Mat h = scratch(T, F);
+    if (T <= kFewTokens && few_readable(Mat(a_.x), T, D, 2) && few_readable(Mat(a_.w_gate), F, D, 2) &&
+        few_readable(Mat(a_.w_up), F, D, 2)) {
+      finish([&](bool more) {
+        return run_few_gated(Mat(a_.x), Mat(a_.w_gate), Mat(a_.w_up), Mat(a_.gate_pre), Mat(a_.up_pre), h, T, F, D, a_.act,
+                             a_.dtype, more, s_);
+      });
+      down(h);
+      return;
+    }
     Result gate_pre, up_pre;
     const bool save = a_.gate_pre.data != nullptr;
     const int64_t tiles = cdiv64(T, 256) * cdiv64(F, 128);
@@ -65,8 +75,7 @@ class Runner {
       }
       launch(p);
     }
-    Operand hk = in_place(h, T, F);
-    store(&hk, nullptr, nullptr, nullptr, h, Mat(a_.w_down), T, D, F, a_.out);
+    down(h);
     place(gate_pre, T, F);
     place(up_pre, T, F);
   }
@@ -101,13 +110,13 @@ class Runner {
     Operand kg = in_place(dg, T, F), ku = in_place(du, T, F);
     Operand wg = operand(Mat(a_.w_gate).t(), D, F), wu = operand(Mat(a_.w_up).t(), D, F, wg.kmajor);
     same_order(wg, wu, Mat(a_.w_gate).t(), Mat(a_.w_up).t());
-    store(&kg, &ku, &wg, &wu, Mat(), Mat(), T, D, F, a_.dx);
+    store(&kg, &ku, &wg, &wu, Mat(), T, D, F, a_.dx);
     Operand xt = operand(x.t(), D, T);
     Operand gt = in_place(dg.t(), F, T), ut = in_place(du.t(), F, T);
     const int64_t wtiles = cdiv64(F, 256) * cdiv64(D, 128);
     if (4 * wtiles <= pairs()) {
-      store(&gt, nullptr, &xt, nullptr, Mat(), Mat(), F, D, T, a_.dw_gate);
-      store(&ut, nullptr, &xt, nullptr, Mat(), Mat(), F, D, T, a_.dw_up);
+      store(&gt, nullptr, &xt, nullptr, Mat(), F, D, T, a_.dw_gate);
+      store(&ut, nullptr, &xt, nullptr, Mat(), F, D, T, a_.dw_up);
     } else {
       Product p = base(F, D, T);
       p.stacked = true;
@@ -123,7 +132,7 @@ class Runner {
       place(u, F, D);
     }
     Operand dt = operand(dout.t(), D, T), ht = in_place(h.t(), F, T);
-    store(&dt, nullptr, &ht, nullptr, Mat(), Mat(), D, F, T, a_.dw_down);
+    store(&dt, nullptr, &ht, nullptr, Mat(), D, F, T, a_.dw_down);
   }
 
  private:
@@ -134,6 +143,19 @@ class Runner {
 
   int pairs() const { return sms_ / 2; }
   static bool few(int64_t T) { return T <= 128; }
+
+  // y = h Wd^T
+  void down(const Mat& h) {
+    const int64_t T = a_.T, D = a_.D, F = a_.F;
+    if (T <= kFewTokens && few_readable(Mat(a_.w_down), D, F, 2)) {  // (F % 8 == 0: h is readable too)
+      finish([&](bool more) {
+        return run_few_product(h, Mat(a_.w_down), Mat(a_.out), T, D, F, a_.dtype, made > 0, more, s_);
+      });
+      return;
+    }
+    const Operand hk = in_place(h, T, F);
+    store(&hk, nullptr, nullptr, nullptr, Mat(a_.w_down), T, D, F, a_.out);
+  }
 
   Product base(int64_t M, int64_t N, int64_t K) const {
     Product p;
@@ -232,10 +254,9 @@ class Runner {
     return Partial{p.partial, p.pitch, p.slice, p.splits, p.pitch / stack};
   }
 
-  // out = A B^T (+ A1 B1^T): A given or `ma`, B given or `mb`.  M x N results with K (each) terms.
-  void store(const Operand* a0, const Operand* a1, const Operand* b0, const Operand* b1, const Mat& ma, const Mat& mb,
+  // out = A B^T (+ A1 B1^T): B given or `mb`.  M x N results with K (each) terms.
+  void store(const Operand* a0, const Operand* a1, const Operand* b0, const Operand* b1, const Mat& mb,
              int64_t M, int64_t N, int64_t K, const cconv_matrix& out) {
-    (void)ma;
     const int64_t tiles = cdiv64(M, 256) * cdiv64(N, 128);
     const int64_t kb = cdiv64(K, 64) * (a1 ? 2 : 1);
     if (few(M) || (2 * tiles <= pairs() && kb >= 8)) {

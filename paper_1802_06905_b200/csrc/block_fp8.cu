@@ -8,6 +8,7 @@
 #include <algorithm>
 
 #include "block.h"
+#include "block_few.h"
 #include "block_gemm.h"
 
 namespace cconv {
@@ -25,6 +26,12 @@ class Runner {
     const int pairs = sms_ / 2;
     const int64_t M = a_.M, N = a_.N, K = a_.K, kb = cdiv64(K, 128);
     const int64_t tiles = cdiv64(M, 256) * cdiv64(N, 128);
+    if (M <= kFewTokens && few_readable(Mat(a_.a), M, K, 1) && few_readable(Mat(a_.b), N, K, 1)) {
+      launch([&](bool) {
+        return run_few_fp8(Mat(a_.a), Mat(a_.b), Mat(a_.a_scale), Mat(a_.b_scale), Mat(a_.c), M, N, K, a_.dtype, s_);
+      });
+      return;
+    }
     Product p;
     p.K = K;
     p.dtype = a_.dtype;
