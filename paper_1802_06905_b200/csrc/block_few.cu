@@ -1,8 +1,9 @@
 // Products of at most 16 tokens: the weights are read once, straight into the registers that multiply them.
 //
 // What bounds them is HBM (a token costs 2 flops a weight), so the kernels are made of loads in flight: a
-// block takes 16 rows of weights (8 of each matrix of the gated pair) and splits k over its 8 warps, every
-// lane has 16 loads of 16 bytes on their way, and all blocks of a served layer are resident at once.  The
+// tile is 16 rows of weights (8 of each matrix of the gated pair, or 8 of one where 16 would leave SMs
+// idle), k is split over the 8 warps of a block, and a block goes through its tiles with the next 8 loads of
+// 16 bytes of every lane on their way while the last 8 are multiplied, also across tiles.  The
 // products run on warp-wide matrix instructions (m16n8: 16 rows of weights by 8 tokens) because they
 // take operands from registers as they come from memory; tcgen05 would want them in shared memory first, for
 // tiles that a few tokens leave almost empty.
@@ -12,6 +13,7 @@
 #include "block_few.h"
 
 #include <algorithm>
+#include <type_traits>
 
 #include "block_device.cuh"
 #include "block_launch.h"
@@ -92,128 +94,145 @@ __device__ __forceinline__ void put(const Mat& m, int dtype, int64_t r, int64_t 
   else reinterpret_cast<float*>(p)[at] = v;
 }
 
-// 16-bit types.  kPair: rows 0-7 of the tile are 8 rows of w0, rows 8-15 the same rows of w1, else 16 rows of w0.
-// B: blocks of 8 tokens.  A step is 64 bytes of k a row (32 elements).
-template <typename T, bool kPair, int B>
-__global__ void __launch_bounds__(kWarps * 32) cconv_few_kernel(const FewParams p) {
-  __shared__ float smem[kWarps][B * 128];
-  constexpr int kSteps = 8;  // loaded together
+// The rows of a tile: 8 of w0 and the same 8 of w1, 16 of w0, or 8 of w0.
+enum Rows { kPair, kSixteen, kEight };
+
+// A block's tiles are blockIdx.x, blockIdx.x + gridDim.x, ...; every warp takes the same number of batches of
+// each.  A step is 64 bytes of k a row (32 elements of 16 bits, or 64 of 8, two of which make a block that
+// shares a scale); a batch is 8 loads a lane.
+template <typename T, Rows kRows, int B>
+__global__ void __launch_bounds__(kWarps * 32, 2) cconv_few_kernel(const FewParams p) {
+  __shared__ float smem[2][kWarps][B * 128];
+  constexpr bool kFp8 = std::is_same<T, E4m3>::value;
+  constexpr int kSteps = kRows == kEight ? 8 : 4, kHalf = kRows == kEight ? 1 : 2;
+  constexpr int kTile = kRows == kSixteen ? 16 : 8;
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, g = lane >> 2, q = lane & 3;
-  const int64_t n0 = int64_t(blockIdx.x) * (kPair ? 8 : 16), last = p.N - 1;
-  const char* w0 = p.w0 + min(n0 + g, last) * p.w0_rs + q * 16;
-  const char* w1 = kPair ? p.w1 + min(n0 + g, last) * p.w1_rs + q * 16 : p.w0 + min(n0 + 8 + g, last) * p.w0_rs + q * 16;
-  const int64_t steps = (p.k_bytes + 63) / 64, per = (steps + kWarps - 1) / kWarps;
-  const int64_t s0 = warp * per, s1 = min(steps, s0 + per);
-  float acc[B][4] = {};
+  const int tiles = int((p.N + kTile - 1) / kTile);
+  const int steps = int((p.k_bytes + 63) / 64), unit = kFp8 ? 2 : 1;
+  const int per = ((steps + unit - 1) / unit + kWarps - 1) / kWarps * unit;  // steps of a warp
+  const int s0 = warp * per, s1 = min(steps, s0 + per), batches = (per + kSteps - 1) / kSteps;
+  const int mine = int(blockIdx.x) < tiles ? (tiles - 1 - int(blockIdx.x)) / int(gridDim.x) + 1 : 0;
   const uint4 none = make_uint4(0, 0, 0, 0);
-  bool waited = false;
-  for (int64_t s = s0; s < s1 || !waited; s += kSteps) {
-    uint4 a[kSteps], c[kSteps];
-#pragma unroll
-    for (int i = 0; i < kSteps; ++i) {
-      const int64_t at = (s + i) * 64;
-      const bool in = s + i < s1 && at + q * 16 < p.k_bytes;
-      a[i] = in ? load_weights(w0 + at) : none;
-      c[i] = in ? load_weights(w1 + at) : none;
-    }
-    if (!waited) {
-      // the weights were there before this call; the tokens may come from the kernel in front
-      asm volatile("griddepcontrol.wait;" ::: "memory");
-      if (p.more) asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
-      waited = true;
-    }
-#pragma unroll
-    for (int b = 0; b < B; ++b) {
-      const int t = b * 8 + g;
-      const char* x = p.x + min(t, p.T - 1) * p.x_rs + q * 16;
+  uint4 w[2][8];
+
+  // where the next batch comes from
+  int lt = blockIdx.x, lb = 0;
+  auto load = [&](uint4 (&a)[8]) {
+    if (lt < tiles) {
+      const int64_t r = int64_t(lt) * kTile + g, last = p.N - 1;
+      const char* w0 = p.w0 + min(r, last) * p.w0_rs + q * 16;
+      const char* w1 = kRows == kPair ? p.w1 + min(r, last) * p.w1_rs + q * 16 : p.w0 + min(r + 8, last) * p.w0_rs + q * 16;
 #pragma unroll
       for (int i = 0; i < kSteps; ++i) {
-        const int64_t at = (s + i) * 64;
-        const uint4 v = t < p.T && s + i < s1 && at + q * 16 < p.k_bytes ? load_tokens(x + at) : none;
-        mma<T>(acc[b], a[i].x, c[i].x, a[i].y, c[i].y, v.x, v.y);
-        mma<T>(acc[b], a[i].z, c[i].z, a[i].w, c[i].w, v.z, v.w);
+        const int s = s0 + lb * kSteps + i;
+        const int64_t at = int64_t(s) * 64;
+        const bool in = s < s1 && at + q * 16 < p.k_bytes;
+        a[i * kHalf] = in ? load_weights(w0 + at) : none;
+        if (kHalf == 2) a[i * 2 + 1] = in ? load_weights(w1 + at) : none;
       }
     }
-  }
-  gather<B>(smem, acc, warp, lane);
-  const int dtype = sizeof(T) == 2 && p.out_dtype == CCONV_TYPE_BF16 ? CCONV_TYPE_BF16 : CCONV_TYPE_FP16;
-  if (kPair) {
-    const int r = threadIdx.x & 7, t = threadIdx.x >> 3;
-    if (t < p.T && t < 8 * B && n0 + r < p.N) {
-      const float gate = gathered<B>(smem, r, t), up = gathered<B>(smem, r + 8, t);
-      float unused;
-      put(p.out, dtype, t, n0 + r, activation<false>(p.act, gate, unused) * up);
-      if (p.gate_pre.p) {
-        put(p.gate_pre, dtype, t, n0 + r, gate);
-        put(p.up_pre, dtype, t, n0 + r, up);
-      }
-    }
-  } else {
-    const int r = threadIdx.x & 15, t = threadIdx.x >> 4;
-    if (t < p.T && t < 8 * B && n0 + r < p.N) put(p.out, dtype, t, n0 + r, gathered<B>(smem, r, t));
-  }
-}
+    if (++lb == batches) lb = 0, lt += gridDim.x;
+  };
 
-// 8-bit operands: a step is 64 bytes = 64 elements of k a row, two steps a block of 128, whose sums are
-// scaled before they are added up.  The 16 rows share their scale.
-template <int B>
-__global__ void __launch_bounds__(kWarps * 32) cconv_few_fp8_kernel(const FewParams p) {
-  __shared__ float smem[kWarps][B * 128];
-  constexpr int kBlocks = 4;  // loaded together
-  const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, g = lane >> 2, q = lane & 3;
-  const int64_t n0 = int64_t(blockIdx.x) * 16, last = p.N - 1;
-  const char* w0 = p.w0 + min(n0 + g, last) * p.w0_rs + q * 16;
-  const char* w1 = p.w0 + min(n0 + 8 + g, last) * p.w0_rs + q * 16;
-  const float* sb = p.sb + (n0 >> 7) * p.sb_rs;
-  const int64_t kbs = (p.k_bytes + 127) / 128, per = (kbs + kWarps - 1) / kWarps;
-  const int64_t k0 = warp * per, k1 = min(kbs, k0 + per);
-  float total[B][4] = {};
-  const uint4 none = make_uint4(0, 0, 0, 0);
-  for (int64_t kb = k0; kb < k1; kb += kBlocks) {
-    uint4 a[2 * kBlocks], c[2 * kBlocks];
-#pragma unroll
-    for (int i = 0; i < 2 * kBlocks; ++i) {
-      const int64_t at = kb * 128 + i * 64;
-      const bool in = kb + i / 2 < k1 && at + q * 16 < p.k_bytes;
-      a[i] = in ? load_weights(w0 + at) : none;
-      c[i] = in ? load_weights(w1 + at) : none;
-    }
+  load(w[0]);
+  // the weights were there before this call; the tokens may come from the kernel in front
+  asm volatile("griddepcontrol.wait;" ::: "memory");
+  if (p.more) asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
+
+  float acc[B][4] = {};
+  int tile = blockIdx.x, batch = 0, parity = 0;
+  auto use = [&](const uint4 (&a)[8]) {
+    const int sb = s0 + batch * kSteps;
 #pragma unroll
     for (int b = 0; b < B; ++b) {
       const int t = b * 8 + g;
       const char* x = p.x + min(t, p.T - 1) * p.x_rs + q * 16;
-      const int t0 = b * 8 + 2 * q;  // the two tokens whose sums this lane holds
+      uint4 v[kSteps];
 #pragma unroll
-      for (int j = 0; j < kBlocks; ++j) {
-        if (kb + j >= k1) break;
-        float acc[4] = {};
+      for (int i = 0; i < kSteps; ++i) {
+        const int64_t at = int64_t(sb + i) * 64;
+        v[i] = t < p.T && sb + i < s1 && at + q * 16 < p.k_bytes ? load_tokens(x + at) : none;
+      }
+      if constexpr (!kFp8) {
 #pragma unroll
-        for (int i = 2 * j; i < 2 * j + 2; ++i) {
-          const int64_t at = kb * 128 + i * 64;
-          const uint4 v = t < p.T && at + q * 16 < p.k_bytes ? load_tokens(x + at) : none;
-          mma<E4m3>(acc, a[i].x, c[i].x, a[i].y, c[i].y, v.x, v.y);
-          mma<E4m3>(acc, a[i].z, c[i].z, a[i].w, c[i].w, v.z, v.w);
+        for (int i = 0; i < kSteps; ++i) {
+          const uint4 a0 = a[i * kHalf], a1 = kHalf == 2 ? a[i * kHalf + kHalf - 1] : none;
+          mma<T>(acc[b], a0.x, a1.x, a0.y, a1.y, v[i].x, v[i].y);
+          mma<T>(acc[b], a0.z, a1.z, a0.w, a1.w, v[i].z, v[i].w);
         }
-        const float s = sb[(kb + j) * p.sb_ks];
-        const float s0 = s * p.sa[min(t0, p.T - 1) * p.sa_rs + (kb + j) * p.sa_ks];
-        const float s1 = s * p.sa[min(t0 + 1, p.T - 1) * p.sa_rs + (kb + j) * p.sa_ks];
-        total[b][0] += s0 * acc[0];
-        total[b][1] += s1 * acc[1];
-        total[b][2] += s0 * acc[2];
-        total[b][3] += s1 * acc[3];
+      } else {
+        // the sums of a block of 128 are scaled before they are added up; the rows of a tile share their scale
+        const int64_t nb = int64_t(tile) * kTile >> 7;
+        const int t0 = min(b * 8 + 2 * q, p.T - 1), t1 = min(b * 8 + 2 * q + 1, p.T - 1);
+#pragma unroll
+        for (int j = 0; j < kSteps / 2; ++j) {
+          if (sb + 2 * j < s1) {
+            const int64_t kb = (sb >> 1) + j;
+            const float s = p.sb[nb * p.sb_rs + kb * p.sb_ks];
+            const float sa0 = s * p.sa[t0 * p.sa_rs + kb * p.sa_ks], sa1 = s * p.sa[t1 * p.sa_rs + kb * p.sa_ks];
+            float d[4] = {};
+#pragma unroll
+            for (int i = 2 * j; i < 2 * j + 2; ++i) {
+              const uint4 a0 = a[i * kHalf], a1 = kHalf == 2 ? a[i * kHalf + kHalf - 1] : none;
+              mma<T>(d, a0.x, a1.x, a0.y, a1.y, v[i].x, v[i].y);
+              mma<T>(d, a0.z, a1.z, a0.w, a1.w, v[i].z, v[i].w);
+            }
+            acc[b][0] += sa0 * d[0];
+            acc[b][1] += sa1 * d[1];
+            acc[b][2] += sa0 * d[2];
+            acc[b][3] += sa1 * d[3];
+          }
+        }
       }
     }
+    if (++batch < batches) return;
+    batch = 0;
+    gather<B>(smem[parity], acc, warp, lane);
+#pragma unroll
+    for (int b = 0; b < B; ++b)
+#pragma unroll
+      for (int i = 0; i < 4; ++i) acc[b][i] = 0.0f;
+    const int64_t n0 = int64_t(tile) * kTile;
+    const int r = threadIdx.x % kTile, t = threadIdx.x / kTile;
+    if (t < p.T && t < 8 * B && n0 + r < p.N) {
+      const float f = gathered<B>(smem[parity], r, t);
+      if constexpr (kRows == kPair) {
+        const float up = gathered<B>(smem[parity], r + 8, t);
+        float unused;
+        put(p.out, p.out_dtype, t, n0 + r, activation<false>(p.act, f, unused) * up);
+        if (p.gate_pre.p) {
+          put(p.gate_pre, p.out_dtype, t, n0 + r, f);
+          put(p.up_pre, p.out_dtype, t, n0 + r, up);
+        }
+      } else {
+        put(p.out, p.out_dtype, t, n0 + r, f);
+      }
+    }
+    parity ^= 1;
+    tile += gridDim.x;
+  };
+  const int total = mine * batches;
+  for (int it = 0; it < total; it += 2) {
+    load(w[1]);
+    use(w[0]);
+    if (it + 1 < total) {
+      load(w[0]);
+      use(w[1]);
+    }
   }
-  gather<B>(smem, total, warp, lane);
-  const int r = threadIdx.x & 15, t = threadIdx.x >> 4;
-  if (t < p.T && t < 8 * B && n0 + r < p.N) put(p.out, p.out_dtype, t, n0 + r, gathered<B>(smem, r, t));
 }
 
-template <typename T, bool kPair>
-cudaError_t launch_few(const FewParams& p, bool chained, cudaStream_t s) {
-  const dim3 grid(unsigned(cdiv64(p.N, kPair ? 8 : 16)));
-  return p.T <= 8 ? launch(cconv_few_kernel<T, kPair, 1>, grid, kWarps * 32, 0, 1, chained, s, p)
-                  : launch(cconv_few_kernel<T, kPair, 2>, grid, kWarps * 32, 0, 1, chained, s, p);
+template <typename T, Rows kRows>
+cudaError_t launch_rows(const FewParams& p, int sms, bool chained, cudaStream_t s) {
+  const int64_t tiles = cdiv64(p.N, kRows == kSixteen ? 16 : 8);
+  const dim3 grid(unsigned(std::min<int64_t>(tiles, 2 * sms)));
+  return p.T <= 8 ? launch(cconv_few_kernel<T, kRows, 1>, grid, kWarps * 32, 0, 1, chained, s, p)
+                  : launch(cconv_few_kernel<T, kRows, 2>, grid, kWarps * 32, 0, 1, chained, s, p);
+}
+
+template <typename T>
+cudaError_t launch_single(const FewParams& p, int sms, bool chained, cudaStream_t s) {
+  return p.N >= 32 * int64_t(sms) ? launch_rows<T, kSixteen>(p, sms, chained, s) : launch_rows<T, kEight>(p, sms, chained, s);
 }
 
 FewParams params(const Mat& x, const Mat& w, const Mat& out, int64_t T, int64_t N, int64_t K, int es, int dtype) {
@@ -239,7 +258,7 @@ bool few_readable(const Mat& m, int64_t rows, int64_t k, int es) {
 }
 
 cudaError_t run_few_gated(const Mat& x, const Mat& wg, const Mat& wu, const Mat& gate_pre, const Mat& up_pre,
-                          const Mat& h, int64_t T, int64_t F, int64_t D, int act, int dtype, bool more, cudaStream_t s) {
+                          const Mat& h, int64_t T, int64_t F, int64_t D, int act, int dtype, int sms, bool more, cudaStream_t s) {
   FewParams p = params(x, wg, h, T, F, D, 2, dtype);
   p.w1 = static_cast<const char*>(wu.p);
   p.w1_rs = wu.rs * 2;
@@ -247,19 +266,20 @@ cudaError_t run_few_gated(const Mat& x, const Mat& wg, const Mat& wu, const Mat&
   p.up_pre = up_pre;
   p.act = act;
   p.more = more;
-  return dtype == CCONV_TYPE_BF16 ? launch_few<__nv_bfloat16, true>(p, false, s) : launch_few<__half, true>(p, false, s);
+  return dtype == CCONV_TYPE_BF16 ? launch_rows<__nv_bfloat16, kPair>(p, sms, false, s)
+                                  : launch_rows<__half, kPair>(p, sms, false, s);
 }
 
 cudaError_t run_few_product(const Mat& x, const Mat& w, const Mat& out, int64_t T, int64_t N, int64_t K, int dtype,
-                            bool chained, bool more, cudaStream_t s) {
+                            int sms, bool chained, bool more, cudaStream_t s) {
   FewParams p = params(x, w, out, T, N, K, 2, dtype);
   p.more = more;
-  return dtype == CCONV_TYPE_BF16 ? launch_few<__nv_bfloat16, false>(p, chained, s)
-                                  : launch_few<__half, false>(p, chained, s);
+  return dtype == CCONV_TYPE_BF16 ? launch_single<__nv_bfloat16>(p, sms, chained, s)
+                                  : launch_single<__half>(p, sms, chained, s);
 }
 
 cudaError_t run_few_fp8(const Mat& x, const Mat& w, const Mat& sa, const Mat& sb, const Mat& out, int64_t T, int64_t N,
-                        int64_t K, int dtype, cudaStream_t s) {
+                        int64_t K, int dtype, int sms, cudaStream_t s) {
   FewParams p = params(x, w, out, T, N, K, 1, dtype);
   p.sa = static_cast<const float*>(sa.p);
   p.sa_rs = sa.rs;
@@ -267,9 +287,7 @@ cudaError_t run_few_fp8(const Mat& x, const Mat& w, const Mat& sa, const Mat& sb
   p.sb = static_cast<const float*>(sb.p);
   p.sb_rs = sb.rs;
   p.sb_ks = sb.cs;
-  const dim3 grid(unsigned(cdiv64(N, 16)));
-  return T <= 8 ? launch(cconv_few_fp8_kernel<1>, grid, kWarps * 32, 0, 1, false, s, p)
-                : launch(cconv_few_fp8_kernel<2>, grid, kWarps * 32, 0, 1, false, s, p);
+  return launch_single<E4m3>(p, sms, false, s);
 }
 
 }  // namespace cconv

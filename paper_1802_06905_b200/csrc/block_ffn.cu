@@ -37,7 +37,7 @@ class Runner {
         few_readable(Mat(a_.w_up), F, D, 2)) {
       finish([&](bool more) {
         return run_few_gated(Mat(a_.x), Mat(a_.w_gate), Mat(a_.w_up), Mat(a_.gate_pre), Mat(a_.up_pre), h, T, F, D, a_.act,
-                             a_.dtype, more, s_);
+                             a_.dtype, sms_, more, s_);
       });
       down(h);
       return;
@@ -149,7 +149,7 @@ class Runner {
     const int64_t T = a_.T, D = a_.D, F = a_.F;
     if (T <= kFewTokens && few_readable(Mat(a_.w_down), D, F, 2)) {  // (F % 8 == 0: h is readable too)
       finish([&](bool more) {
-        return run_few_product(h, Mat(a_.w_down), Mat(a_.out), T, D, F, a_.dtype, made > 0, more, s_);
+        return run_few_product(h, Mat(a_.w_down), Mat(a_.out), T, D, F, a_.dtype, sms_, made > 0, more, s_);
       });
       return;
     }

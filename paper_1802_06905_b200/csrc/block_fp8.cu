@@ -28,7 +28,7 @@ class Runner {
     const int64_t tiles = cdiv64(M, 256) * cdiv64(N, 128);
     if (M <= kFewTokens && few_readable(Mat(a_.a), M, K, 1) && few_readable(Mat(a_.b), N, K, 1)) {
       launch([&](bool) {
-        return run_few_fp8(Mat(a_.a), Mat(a_.b), Mat(a_.a_scale), Mat(a_.b_scale), Mat(a_.c), M, N, K, a_.dtype, s_);
+        return run_few_fp8(Mat(a_.a), Mat(a_.b), Mat(a_.a_scale), Mat(a_.b_scale), Mat(a_.c), M, N, K, a_.dtype, sms_, s_);
       });
       return;
     }
