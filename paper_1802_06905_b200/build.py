@@ -16,7 +16,7 @@ LIB = os.path.join(HERE, "libcconv.so")
 SOURCES = ["kernels.cu", "direct_kernel.cu", "stem_kernel.cu", "api.cu", "host_setup.cu", "noalloc.cu", "pool.cu", "planner.cpp",
            "block_api.cu", "block_few.cu", "block_ffn.cu", "block_fp8.cu", "block_gemm.cu", "block_tma.cu", "block_norm.cu", "block_quant.cu"]
 HEADERS = ["kernels.h", "planner.h", "host_setup.h", "ptx_sm100.cuh", "direct_issue.cuh",
-           "block.h", "block_device.cuh", "block_few.h", "block_ffn.h", "block_fp8.h", "block_launch.h", "block_gemm.h", "block_tma.h", "pair_sm100.cuh", "block_norm.h", "block_quant.h",
+           "block.h", "block_device.cuh", "block_few.h", "block_ffn.h", "block_fp8.h", "block_launch.h", "block_steps.h", "block_gemm.h", "block_tma.h", "pair_sm100.cuh", "block_norm.h", "block_quant.h",
            os.path.join("..", "..", "include", "cconv_block.h"), os.path.join("..", "..", "include", "cconv.h")]
 
 

@@ -7,8 +7,14 @@
 // 256 x block_n products, half of what two CTAs on tiles of their own would: at 128 x 256 a CTA draws 96
 // bytes a clock, a pair of CTAs at 256 x 256 64 bytes a clock each, below what L2 delivers to an SM.
 //
+// A product with fewer tiles than pairs is cut along k: a cluster of 2 or 4 pairs shares a tile, each pair
+// sums a part of k, and the pairs then exchange their accumulators through distributed shared memory, so
+// that each finishes its own share of the columns (in the order of the parts: the result does not depend
+// on who is first).  One launch, no table of partial sums in memory.
+//
 // Roles: warp 0 copies (TMA), warp 1 of the first CTA issues MMAs, warp 2 owns the tensor memory, warps
 // 4-11 are the epilogue (two for each quarter of the lanes, half of the columns each).
+#include <algorithm>
 #include <cstdlib>
 
 #include "block.h"
@@ -27,44 +33,71 @@ constexpr uint32_t kBoxBytes = 32 * 128; // a piece that an epilogue warp stages
 constexpr uint32_t kTmemCols = 512;
 constexpr uint32_t kSmemMost = 232448;
 constexpr uint32_t kBarrierBytes = 512;
+constexpr int kMostStages = 10;
 
 __device__ int g_block_status;
 
-struct PairParams {
-  int tiles_m, tiles_n, tiles_m0;  // tiles_m0: rows of tiles of the first stacked product
-  int splits, kb_total, kb_split, kb_seg;
-  int block_n, stages;
-  uint32_t b_bytes;                // a stage of B in one CTA
-  uint32_t a_kmajor, b_kmajor, paired;
-  uint64_t a_desc, b_desc;
-  uint32_t a_step, b_step;         // descriptor step of 16 elements of k (16-byte units)
+// A product of the launch, as the kernel sees it.
+struct ProductParams {
+  int tiles_m, tiles_n, first;  // first: tiles of the products before it
+  int kb_total, kb_seg, kb_part;  // k blocks: all, of the first segment, of a pair's part
+  int block_n;
+  uint32_t b_bytes;             // a stage of B in one CTA
+  uint32_t a_kmajor, b_kmajor;
+  uint32_t a_step, b_step;      // descriptor step of 16 elements of k (16-byte units)
   uint32_t idesc;
+  uint64_t a_desc, b_desc;
   int64_t M, N;
-  int act, save, more;
-  float* partial;
-  int64_t pitch, slice;
-  // 8-bit operands: scale of row r (or of 128 rows) and k block kb at row_scale[i * row_rs + kb * row_ks]
+};
+template <int kProducts>
+struct PairParams {
+  ProductParams of[kProducts];
+  int count, tiles, splits, stages;
+  uint32_t stage_bytes;
+  int paired, act, save, more;
+  // cut: where results go and come from (in elements)
+  char* out[3];
+  int64_t out_rs[3], out_cs[3];
+  const char* in[2];
+  int64_t in_rs[2];
+  // 8-bit: scale of row r (of 128 rows of B) and k block kb
   const float *row_scale, *col_scale;
   int64_t row_rs, row_ks, col_rs, col_ks;
   int* status;
   uint64_t limit_ns;
 };
+struct ProductMaps {
+  CUtensorMap a[2], b[2], out;
+};
+template <int kProducts>
 struct PairMaps {
-  CUtensorMap a[2], b[2], out[3], in[2];
+  ProductMaps of[kProducts];
 };
+template <>
+struct PairMaps<1> {
+  ProductMaps of[1];
+  CUtensorMap out1, out2, in[2];
+};
+template <int kEpi>
+constexpr int kProductsOf = kEpi == kStore ? kMostProducts : 1;
 
-// Tile t of the launch: share of k, row and column of tiles.  Tiles run down groups of 8 rows of tiles,
-// so that the pairs at work at one time read few different rows of A and B.
+// Tile t of the launch: product, row and column of tiles.  Tiles run down groups of 8 rows of tiles, so that
+// the pairs at work at one time read few different rows of A and B.
 struct Tile {
-  int split, m, n;
+  int of, m, n;
 };
-__device__ __forceinline__ Tile tile_of(const PairParams& p, int t) {
+template <int kProducts>
+__device__ __forceinline__ Tile tile_of(const PairParams<kProducts>& p, int t) {
   Tile r;
-  r.split = t % p.splits;
-  t /= p.splits;
-  const int group = 8 * p.tiles_n;
+  r.of = 0;
+  if (kProducts > 1) {
+    while (r.of + 1 < p.count && t >= p.of[r.of + 1].first) ++r.of;
+    t -= p.of[r.of].first;
+  }
+  const int tiles_n = p.of[r.of].tiles_n, tiles_m = p.of[r.of].tiles_m;
+  const int group = 8 * tiles_n;
   const int first = t / group * 8;
-  const int rows = min(8, p.tiles_m - first);
+  const int rows = min(8, tiles_m - first);
   t %= group;
   r.m = first + t % rows;
   r.n = t / rows;
@@ -123,16 +156,12 @@ __device__ __forceinline__ void unstage32(uint32_t base, int r, int c0, float (&
 
 // Pieces that an epilogue warp stages.
 template <int kEpi>
-constexpr int kPieces = kEpi == kStore ? 2 : kEpi == kScaled ? 1 : kEpi == kPartial || kEpi == kScaledPartial ? 0 : 3;
-int staged_pieces(int epi) {
-  return epi == kStore ? 2 : epi == kScaled ? 1 : epi == kPartial || epi == kScaledPartial ? 0 : 3;
-}
+constexpr int kPieces = kEpi == kStore ? 2 : kEpi == kScaled ? 1 : 3;
+int staged_pieces(int epi) { return epi == kStore ? 2 : epi == kScaled ? 1 : 3; }
 // Scales of 8-bit rows that an epilogue warp keeps: 16 blocks of k of its 32 rows and of its columns
 // (row 32), the 16 in use and the next 16; a pitch of 17 words keeps the lanes on different banks.
 constexpr uint32_t kScaleBytes = 33 * 17 * 4;
 uint32_t scale_bytes(int epi) { return epi == kScaled ? 2 * kEpilogueWarps * kScaleBytes : 0; }
-template <int kEpi>
-constexpr bool kEightBit = kEpi == kScaled || kEpi == kScaledPartial;
 
 __device__ __forceinline__ void cp_async4(uint32_t to, const float* from, bool there) {
   asm volatile("cp.async.ca.shared.global [%0], [%1], 4, %2;" ::"r"(to), "l"(from), "r"(there ? 4 : 0) : "memory");
@@ -155,24 +184,111 @@ __device__ __forceinline__ bool wait_all(uint32_t bar, uint32_t parity, volatile
   return __all_sync(0xffffffffu, mbar_wait_warp(bar, parity, abort_flag, status, code, limit_ns));
 }
 
+// ---- cut along k: exchange of accumulators and results straight to memory -------------------------
+// A piece of 32 columns by 128 rows, as the other pairs send it: 16 bytes of a row next to those of the next
+// row, so that lanes (rows) write and read neighbouring addresses.
+constexpr uint32_t kShareBytes = 128 * 32 * 4;
+__device__ __forceinline__ void send32(uint32_t to, int row, const float (&f)[32]) {
+#pragma unroll
+  for (int c = 0; c < 8; ++c)
+    st_cluster_v4(to + (c * 128 + row) * 16, __float_as_uint(f[4 * c]), __float_as_uint(f[4 * c + 1]),
+                  __float_as_uint(f[4 * c + 2]), __float_as_uint(f[4 * c + 3]));
+}
+__device__ __forceinline__ void add32(uint32_t from, int row, float (&f)[32]) {
+#pragma unroll
+  for (int c = 0; c < 8; ++c) {
+    uint32_t w[4];
+    ld_shared_v4(from + (c * 128 + row) * 16, w[0], w[1], w[2], w[3]);
+#pragma unroll
+    for (int i = 0; i < 4; ++i) f[4 * c + i] += __uint_as_float(w[i]);
+  }
+}
+// The sum of all pairs' parts in their order; f holds this pair's.  Piece `local` of `each` a pair lies at
+// from + (slot * each + local) pieces, slots being the other pairs in order.
+__device__ __forceinline__ void join32(uint32_t from, int row, int splits, int share, int each, int local, float (&f)[32]) {
+  float own[32];
+#pragma unroll
+  for (int i = 0; i < 32; ++i) {
+    own[i] = f[i];
+    f[i] = 0.0f;
+  }
+  for (int s = 0; s < splits; ++s) {
+    if (s == share) {
+#pragma unroll
+      for (int i = 0; i < 32; ++i) f[i] += own[i];
+    } else {
+      add32(from + uint32_t((s < share ? s : s - 1) * each + local) * kShareBytes, row, f);
+    }
+  }
+}
+// 32 columns of a row of a result, the first n of them in range.
+template <typename T>
+__device__ __forceinline__ void write32(char* base, int64_t rs, int64_t cs, int64_t row, int64_t col, int n, const float (&f)[32]) {
+  T* to = reinterpret_cast<T*>(base) + row * rs + col * cs;
+  constexpr int E = 16 / int(sizeof(T));
+  if (cs == 1 && (reinterpret_cast<uintptr_t>(to) & 15u) == 0) {
+#pragma unroll
+    for (int c = 0; c < 32; c += E) {
+      if (c + E <= n) {
+        uint4 w;
+        if constexpr (sizeof(T) == 4) {
+          w = make_uint4(__float_as_uint(f[c]), __float_as_uint(f[c + 1]), __float_as_uint(f[c + 2]), __float_as_uint(f[c + 3]));
+        } else {
+          w = make_uint4(pack2<T>(f[c], f[c + 1]), pack2<T>(f[c + 2], f[c + 3]), pack2<T>(f[c + 4], f[c + 5]), pack2<T>(f[c + 6], f[c + 7]));
+        }
+        *reinterpret_cast<uint4*>(to + c) = w;
+      } else {
+#pragma unroll
+        for (int i = 0; i < E; ++i)
+          if (c + i < n) to[c + i] = from_f32<T>(f[c + i]);
+      }
+    }
+  } else {
+#pragma unroll
+    for (int i = 0; i < 32; ++i)
+      if (i < n) to[i * cs] = from_f32<T>(f[i]);
+  }
+}
+template <typename T>
+__device__ __forceinline__ void read32(const char* base, int64_t rs, int64_t row, int64_t col, int n, float (&f)[32]) {
+  const T* from = reinterpret_cast<const T*>(base) + row * rs + col;
+#pragma unroll
+  for (int c = 0; c < 32; c += 8) {
+    if (c + 8 <= n && (reinterpret_cast<uintptr_t>(from) & 15u) == 0) {
+      const uint4 w = *reinterpret_cast<const uint4*>(from + c);
+      const uint32_t a[4] = {w.x, w.y, w.z, w.w};
+#pragma unroll
+      for (int i = 0; i < 4; ++i) {
+        const float2 v = unpack2<T>(a[i]);
+        f[c + 2 * i] = v.x;
+        f[c + 2 * i + 1] = v.y;
+      }
+    } else {
+#pragma unroll
+      for (int i = 0; i < 8; ++i) f[c + i] = c + i < n ? to_f32(from[c + i]) : 0.0f;
+    }
+  }
+}
+
 template <int kEpi, typename T>
-__global__ void __launch_bounds__(kThreads, 1) cconv_pair_product_kernel(const __grid_constant__ PairMaps maps,
-                                                                         const PairParams p) {
+__global__ void __launch_bounds__(kThreads, 1) cconv_pair_product_kernel(
+    const __grid_constant__ PairMaps<kProductsOf<kEpi>> maps, const __grid_constant__ PairParams<kProductsOf<kEpi>> p) {
   extern __shared__ uint8_t smem_raw[];
+  constexpr bool kEightBit = kEpi == kScaled;
   const uint32_t base = (smem_u32(smem_raw) + 1023u) & ~1023u;
-  const uint32_t stage_bytes = kABytes + p.b_bytes;
-  const uint32_t staging = base + p.stages * stage_bytes;
+  const uint32_t staging = base + p.stages * p.stage_bytes;
   const uint32_t scales = staging + kEpilogueWarps * kPieces<kEpi> * kBoxBytes;
-  const uint32_t bars = (scales + (kEpi == kScaled ? 2 * kEpilogueWarps * kScaleBytes : 0) + 7) & ~7u;
+  const uint32_t bars = (scales + (kEightBit ? 2 * kEpilogueWarps * kScaleBytes : 0) + 7) & ~7u;
   const uint32_t bar_full = bars, bar_empty = bars + 8 * p.stages;
   const uint32_t bar_tfull = bar_empty + 8 * p.stages, bar_tempty = bar_tfull + 16, bar_in = bar_tempty + 16;
   const uint32_t slot = bar_in + 8 * kEpilogueWarps;
   volatile int* abort_p = reinterpret_cast<volatile int*>(smem_raw + (slot + 4 - smem_u32(smem_raw)));
 
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
-  const uint32_t rank = cluster_ctarank();
-  const int pair = blockIdx.x >> 1, pairs = gridDim.x >> 1;
-  const int tiles = p.tiles_m * p.tiles_n * p.splits;
+  const uint32_t in_cluster = cluster_ctarank(), rank = in_cluster & 1, leader = in_cluster & ~1u;
+  // uncut: the cluster is a pair, which goes through its tiles.  Cut: the cluster's pairs share one tile.
+  const int share = int(in_cluster >> 1), cluster = int(blockIdx.x) / (2 * p.splits);
+  const int stride = p.splits > 1 ? p.tiles : int(gridDim.x >> 1);
 
   if (threadIdx.x == 0) {
     *abort_p = 0;
@@ -193,7 +309,7 @@ __global__ void __launch_bounds__(kThreads, 1) cconv_pair_product_kernel(const _
   }
   tc_fence_before();
   __syncthreads();
-  cluster_sync_all();  // both CTAs' barriers are initialised
+  cluster_sync_all();  // all CTAs' barriers are initialised
   tc_fence_after();
   uint32_t tmem;
   asm volatile("ld.shared.b32 %0, [%1];" : "=r"(tmem) : "r"(slot));
@@ -204,37 +320,38 @@ __global__ void __launch_bounds__(kThreads, 1) cconv_pair_product_kernel(const _
   // 8-bit: the epilogue's sums take registers that the other warps do not need (128 x 80 + 256 x 208 of
   // the 384 x 168 that the block starts with)
   if (warp < 4) {
-    if constexpr (kEightBit<kEpi>) asm volatile("setmaxnreg.dec.sync.aligned.u32 80;");
+    if constexpr (kEightBit) asm volatile("setmaxnreg.dec.sync.aligned.u32 80;");
     if (warp == 0) {
       if (elect_one()) {
         uint32_t s = 0, ph = 0;
-        const uint32_t full0 = cluster_map_shared(bar_full, 0);
-        const int box_b = int(p.b_bytes) / 8192;
+        const uint32_t full0 = cluster_map_shared(bar_full, leader);
         bool ok = true;
-        for (int t = pair; ok && t < tiles; t += pairs) {
+        for (int t = cluster; ok && t < p.tiles; t += stride) {
           const Tile tl = tile_of(p, t);
-          const bool second = tl.m >= p.tiles_m0;
-          const int m0 = (second ? tl.m - p.tiles_m0 : tl.m) * 256 + int(rank) * 128;
-          const int n0 = p.paired ? tl.n * 128 : tl.n * p.block_n + int(rank) * (p.block_n >> 1);
-          const int k0 = tl.split * p.kb_split, k1 = min(p.kb_total, k0 + p.kb_split);
+          const ProductParams& o = p.of[tl.of];
+          const ProductMaps& om = maps.of[tl.of];
+          const int m0 = tl.m * 256 + int(rank) * 128;
+          const int n0 = p.paired ? tl.n * 128 : tl.n * o.block_n + int(rank) * (o.block_n >> 1);
+          const int k0 = share * o.kb_part, k1 = min(o.kb_total, k0 + o.kb_part);
+          const int box_b = int(o.b_bytes) / 8192;
           for (int kb = k0; kb < k1; ++kb) {
             if (!mbar_wait(bar_empty + 8 * s, ph ^ 1, abort_p, p.status, kStatProducerWait, p.limit_ns)) {
               ok = false;
               break;
             }
-            const bool seg = kb >= p.kb_seg;
-            const int k = (seg ? kb - p.kb_seg : kb) * (kEightBit<kEpi> ? 128 : 64);
-            const CUtensorMap* ma = &maps.a[seg || second];
-            const CUtensorMap* mb = &maps.b[seg || (p.paired && rank)];
-            const uint32_t a = base + s * stage_bytes, b = a + kABytes, bar = full0 + 8 * s;
-            if (rank == 0) mbar_arrive_expect_tx(bar_full + 8 * s, 2 * stage_bytes);
-            if (p.a_kmajor) {
+            const bool seg = kb >= o.kb_seg;
+            const int k = (seg ? kb - o.kb_seg : kb) * (kEightBit ? 128 : 64);
+            const CUtensorMap* ma = &om.a[seg];
+            const CUtensorMap* mb = &om.b[seg || (p.paired && rank)];
+            const uint32_t a = base + s * p.stage_bytes, b = a + kABytes, bar = full0 + 8 * s;
+            if (rank == 0) mbar_arrive_expect_tx(bar_full + 8 * s, 2 * (kABytes + o.b_bytes));
+            if (o.a_kmajor) {
               tma_load_2d_pair(a, ma, k, m0, bar);
             } else {
               tma_load_2d_pair(a, ma, m0, k, bar);
               tma_load_2d_pair(a + 8192, ma, m0 + 64, k, bar);
             }
-            if (p.b_kmajor) {
+            if (o.b_kmajor) {
               tma_load_2d_pair(b, mb, k, n0, bar);
             } else {
               for (int i = 0; i < box_b; ++i) tma_load_2d_pair(b + 8192 * i, mb, n0 + 64 * i, k, bar);
@@ -246,17 +363,21 @@ __global__ void __launch_bounds__(kThreads, 1) cconv_pair_product_kernel(const _
     } else if (warp == 1) {
       if (rank == 0) {
         const bool issue = elect_one();
+        const uint16_t both = uint16_t(3u << leader);
         uint32_t s = 0, ph = 0, buf = 0, bph = 0;
         bool ok = true;
-        for (int t = pair; ok && t < tiles; t += pairs) {
+        for (int t = cluster; ok && t < p.tiles; t += stride) {
           const Tile tl = tile_of(p, t);
-          const int k0 = tl.split * p.kb_split, k1 = min(p.kb_total, k0 + p.kb_split);
-          if constexpr (!kEightBit<kEpi>) {
+          const ProductParams& o = p.of[tl.of];
+          const int k0 = share * o.kb_part, k1 = min(o.kb_total, k0 + o.kb_part);
+          const uint64_t a_desc = o.a_desc, b_desc = o.b_desc;
+          const uint32_t a_step = o.a_step, b_step = o.b_step, idesc = o.idesc;
+          if constexpr (!kEightBit) {
             if (!wait_all(bar_tempty + 8 * buf, bph ^ 1, abort_p, p.status, kStatMmaWaitTmem, p.limit_ns)) break;
             tc_fence_after();
           }
           for (int kb = k0; kb < k1; ++kb) {
-            if constexpr (kEightBit<kEpi>) {  // sums of one block of 128 a time
+            if constexpr (kEightBit) {  // sums of one block of 128 a time
               if (!wait_all(bar_tempty + 8 * buf, bph ^ 1, abort_p, p.status, kStatMmaWaitTmem, p.limit_ns)) {
                 ok = false;
                 break;
@@ -268,64 +389,72 @@ __global__ void __launch_bounds__(kThreads, 1) cconv_pair_product_kernel(const _
               break;
             }
             tc_fence_after();
-            const uint32_t a = base + s * stage_bytes;
+            const uint32_t a = base + s * p.stage_bytes;
             if (issue) {
-              const uint64_t da = p.a_desc + (a >> 4), db = p.b_desc + ((a + kABytes) >> 4);
-  #pragma unroll
+              const uint64_t da = a_desc + (a >> 4), db = b_desc + ((a + kABytes) >> 4);
+#pragma unroll
               for (int j = 0; j < 4; ++j) {
-                if constexpr (kEightBit<kEpi>) pair_mma_f8(d, da + j * 2, db + j * 2, p.idesc, j > 0);
-                else pair_mma_f16(d, da + j * p.a_step, db + j * p.b_step, p.idesc, kb > k0 || j > 0);
+                if constexpr (kEightBit) pair_mma_f8(d, da + j * 2, db + j * 2, idesc, j > 0);
+                else pair_mma_f16(d, da + j * a_step, db + j * b_step, idesc, kb > k0 || j > 0);
               }
-              pair_commit(bar_empty + 8 * s);
-              if constexpr (kEightBit<kEpi>) pair_commit(bar_tfull + 8 * buf);
+              pair_commit(bar_empty + 8 * s, both);
+              if constexpr (kEightBit) pair_commit(bar_tfull + 8 * buf, both);
             }
             __syncwarp();
-            if constexpr (kEightBit<kEpi>) {
+            if constexpr (kEightBit) {
               if (++buf == 2) buf = 0, bph ^= 1;
             }
             if (++s == uint32_t(p.stages)) s = 0, ph ^= 1;
           }
-          if constexpr (!kEightBit<kEpi>) {
-            if (issue && ok) pair_commit(bar_tfull + 8 * buf);
+          if constexpr (!kEightBit) {
+            if (issue && ok) pair_commit(bar_tfull + 8 * buf, both);
             __syncwarp();
             if (++buf == 2) buf = 0, bph ^= 1;
           }
         }
       }
     }
+    if (p.splits > 1) {  // (see the epilogue)
+      __syncwarp();
+      cluster_sync_all();
+      cluster_sync_all();
+    }
   } else {
-    if constexpr (kEightBit<kEpi>) asm volatile("setmaxnreg.inc.sync.aligned.u32 208;");
+    if constexpr (kEightBit) asm volatile("setmaxnreg.inc.sync.aligned.u32 208;");
     const int q = warp & 3, half = (warp - 4) >> 2;
     const uint32_t mine = staging + (warp - 4) * kPieces<kEpi> * kBoxBytes;
     const uint32_t in_bar = bar_in + 8 * (warp - 4);
-    const uint32_t tempty0 = cluster_map_shared(bar_tempty, 0);
+    const uint32_t tempty0 = cluster_map_shared(bar_tempty, leader);
     const uint32_t lanes = tmem + (uint32_t(q * 32) << 16);
     uint32_t buf = 0, bph = 0, in_ph = 0, piece = 0;
     // The scales of 16 blocks of k from kb on, of tile t, on their way to half `b` of this warp's table.
     const uint32_t my_scales = scales + (warp - 4) * 2 * kScaleBytes;
     uint32_t sbuf = 0;
     auto fetch_scales = [&](const Tile& tl, int kb, uint32_t b) {
-      const int sub = lane >> 4, k = min(kb + (lane & 15), p.kb_total - 1);
+      const ProductParams& o = p.of[0];
+      const int sub = lane >> 4, k = min(kb + (lane & 15), o.kb_total - 1);
       const int64_t r0 = int64_t(tl.m) * 256 + int(rank) * 128 + q * 32 + sub;
-      const int rows = int(min(int64_t(32), p.M - r0));  // from r0 on; what lies past them reads as 0
-      const float* from = p.row_scale + min(r0, p.M - 1) * p.row_rs + k * p.row_ks;
+      const int rows = int(min(int64_t(32), o.M - r0));  // from r0 on; what lies past them reads as 0
+      const float* from = p.row_scale + min(r0, o.M - 1) * p.row_rs + k * p.row_ks;
       uint32_t to = my_scales + b * kScaleBytes + (lane & 15) * 4 + sub * 68;
 #pragma unroll
       for (int r = 0; r < 32; r += 2) {
         cp_async4(to + r * 68, from, r < rows);
         if (r + 2 < rows) from += 2 * p.row_rs;
       }
-      const int64_t nb = min((int64_t(tl.n) * p.block_n + half * (p.block_n >> 1)) >> 7, (p.N - 1) >> 7);
+      const int64_t nb = min((int64_t(tl.n) * o.block_n + half * (o.block_n >> 1)) >> 7, (o.N - 1) >> 7);
       if (sub == 0) cp_async4(to + 32 * 68, p.col_scale + nb * p.col_rs + k * p.col_ks, true);
       asm volatile("cp.async.commit_group;" ::: "memory");
     };
-    Tile next = tile_of(p, pair);
-    if constexpr (kEpi == kScaled) fetch_scales(next, 0, 0);
-    for (int t = pair; t < tiles; t += pairs) {
+    bool met = false;  // the cluster's two meetings are behind this warp
+    Tile next = tile_of(p, cluster);
+    if constexpr (kEightBit) fetch_scales(next, share * p.of[0].kb_part, 0);
+    for (int t = cluster; t < p.tiles; t += stride) {
       const Tile tl = next;
-      next = tile_of(p, min(t + pairs, tiles - 1));
-      const bool second = tl.m >= p.tiles_m0;
-      const int row0 = (second ? tl.m - p.tiles_m0 : tl.m) * 256 + int(rank) * 128 + q * 32;
+      next = tile_of(p, min(t + stride, p.tiles - 1));
+      const ProductParams& o = p.of[tl.of];
+      const CUtensorMap* out_map = &maps.of[tl.of].out;
+      const int row0 = tl.m * 256 + int(rank) * 128 + q * 32;
       uint32_t acc = lanes + buf * 256;
       auto wait_sums = [&]() {
         if (!wait_all(bar_tfull + 8 * buf, bph, abort_p, p.status, kStatEpilogueWait, p.limit_ns)) return false;
@@ -337,13 +466,83 @@ __global__ void __launch_bounds__(kThreads, 1) cconv_pair_product_kernel(const _
         __syncwarp();
         if (lane == 0) mbar_arrive_cluster(tempty0 + 8 * buf);
       };
+      if constexpr (!kEightBit) {
+        if (p.splits > 1) {
+          // Columns go in pieces of 32; the pair `owner` finishes `each` neighbouring ones (of both
+          // g and u when paired).  The two halves of the warps take turns.
+          if (!wait_sums()) break;
+          const int all = p.paired ? 4 : o.block_n >> 5, each = all / p.splits, sent = p.paired ? 2 * each : each;
+          const int row = q * 32 + lane;
+          cluster_sync_all();  // every pair's operands are used up: their place takes the pieces
+          for (int i = half; i < all; i += 2) {
+            const int owner = i / each;
+            if (owner == share) continue;
+            const uint32_t to = cluster_map_shared(base, uint32_t(2 * owner) + rank) +
+                                uint32_t((share < owner ? share : share - 1) * sent + i - owner * each) * kShareBytes;
+            float f[32];
+            load_sums(acc + i * 32, f);
+            send32(to, row, f);
+            if (p.paired) {
+              load_sums(acc + 128 + i * 32, f);
+              send32(to + each * kShareBytes, row, f);
+            }
+          }
+          cluster_sync_all();  // all pieces have come
+          met = true;
+          for (int i = share * each + half; i < (share + 1) * each; i += 2) {
+            const int local = i - share * each;
+            const int64_t r = row0 + lane, col = int64_t(tl.n) * (p.paired ? 128 : o.block_n) + i * 32;
+            const int n = r < o.M ? int(min(int64_t(32), o.N - col)) : 0;
+            float f[32];
+            load_sums(acc + i * 32, f);
+            join32(base, row, p.splits, share, sent, local, f);
+            if constexpr (kEpi == kStore) {
+              write32<T>(p.out[0], p.out_rs[0], p.out_cs[0], r, col, n, f);
+            } else if constexpr (kEpi == kGated) {
+              float u[32];
+              load_sums(acc + 128 + i * 32, u);
+              join32(base, row, p.splits, share, sent, each + local, u);
+              if (p.save) {
+                write32<T>(p.out[1], p.out_rs[1], p.out_cs[1], r, col, n, f);
+                write32<T>(p.out[2], p.out_rs[2], p.out_cs[2], r, col, n, u);
+              }
+              float unused;
+#pragma unroll
+              for (int j = 0; j < 32; ++j) f[j] = activation<false>(p.act, f[j], unused) * u[j];
+              write32<T>(p.out[0], p.out_rs[0], p.out_cs[0], r, col, n, f);
+            } else {
+              float g[32], u[32];
+              read32<T>(p.in[0], p.in_rs[0], r, col, n, g);
+              read32<T>(p.in[1], p.in_rs[1], r, col, n, u);
+#pragma unroll
+              for (int j = 0; j < 32; ++j) {
+                float da;
+                const float a = activation<true>(p.act, g[j], da);
+                g[j] = f[j] * u[j] * da;
+                f[j] = f[j] * a;
+                u[j] = a * u[j];
+              }
+              write32<T>(p.out[0], p.out_rs[0], p.out_cs[0], r, col, n, g);
+              write32<T>(p.out[1], p.out_rs[1], p.out_cs[1], r, col, n, f);
+              write32<T>(p.out[2], p.out_rs[2], p.out_cs[2], r, col, n, u);
+            }
+          }
+          break;  // the cluster has one tile
+        }
+      }
       if constexpr (kEpi == kStore) {
         if (!wait_sums()) break;
-        const int cols = p.block_n >> 1;
+        const int cols = o.block_n >> 1;
         for (int c = 0; c < cols; c += 64) {
+          const bool narrow = cols < 64;  // 64 columns a tile: one half of the warps takes them all
+          if (narrow && half) {
+            release_sums();
+            break;
+          }
+          const int at = narrow ? 0 : half * cols + c;
           float f[32], g[32];
-          load_sums(acc + half * cols + c, f);
-          load_sums(acc + half * cols + c + 32, g);
+          load_sums(acc + at, f);
+          load_sums(acc + at + 32, g);
           if (c + 64 >= cols) release_sums();
           const uint32_t to = mine + piece * kBoxBytes;
           if (lane == 0) bulk_wait_group_read<1>();
@@ -353,8 +552,8 @@ __global__ void __launch_bounds__(kThreads, 1) cconv_pair_product_kernel(const _
           fence_proxy_async_smem();
           __syncwarp();
           if (lane == 0) {
-            const int col = tl.n * p.block_n + half * cols + c;
-            if (row0 < p.M && col < p.N) tma_store_2d(&maps.out[second], to, col, row0);
+            const int col = tl.n * o.block_n + at;
+            if (row0 < o.M && col < o.N) tma_store_2d(out_map, to, col, row0);
             bulk_commit_group();
           }
           piece ^= 1;
@@ -382,20 +581,20 @@ __global__ void __launch_bounds__(kThreads, 1) cconv_pair_product_kernel(const _
         fence_proxy_async_smem();
         __syncwarp();
         if (lane == 0) {
-          if (row0 < p.M && col < p.N) {
-            tma_store_2d(&maps.out[0], mine, col, row0);
+          if (row0 < o.M && col < o.N) {
+            tma_store_2d(out_map, mine, col, row0);
             if (p.save) {
-              tma_store_2d(&maps.out[1], mine + kBoxBytes, col, row0);
-              tma_store_2d(&maps.out[2], mine + 2 * kBoxBytes, col, row0);
+              tma_store_2d(&maps.out1, mine + kBoxBytes, col, row0);
+              tma_store_2d(&maps.out2, mine + 2 * kBoxBytes, col, row0);
             }
           }
           bulk_commit_group();
         }
       } else if constexpr (kEpi == kGatedBackward) {
-        const int cols = p.block_n >> 1;
+        const int cols = o.block_n >> 1;
         bool first = true, ok = true;
         for (int c = 0; c < cols; c += 64) {
-          const int col = tl.n * p.block_n + half * cols + c;
+          const int col = tl.n * o.block_n + half * cols + c;
           if (lane == 0) {
             bulk_wait_group_read<0>();
             mbar_arrive_expect_tx(in_bar, 2 * kBoxBytes);
@@ -428,36 +627,37 @@ __global__ void __launch_bounds__(kThreads, 1) cconv_pair_product_kernel(const _
           fence_proxy_async_smem();
           __syncwarp();
           if (lane == 0) {
-            if (row0 < p.M && col < p.N) {
-              tma_store_2d(&maps.out[0], mine, col, row0);
-              tma_store_2d(&maps.out[1], mine + kBoxBytes, col, row0);
-              tma_store_2d(&maps.out[2], mine + 2 * kBoxBytes, col, row0);
+            if (row0 < o.M && col < o.N) {
+              tma_store_2d(out_map, mine, col, row0);
+              tma_store_2d(&maps.out1, mine + kBoxBytes, col, row0);
+              tma_store_2d(&maps.out2, mine + 2 * kBoxBytes, col, row0);
             }
             bulk_commit_group();
           }
         }
         if (!ok) break;
-      } else if constexpr (kEpi == kScaled) {
+      } else {
         // Each block's sums are scaled and added up in registers (a row of half the columns a thread),
         // beside the MMAs of the next block: 128 columns are 64 two-wide multiply-adds.
-        const int cols = p.block_n >> 1;
+        const int cols = o.block_n >> 1;
+        const int k0 = share * o.kb_part, k1 = min(o.kb_total, k0 + o.kb_part);
         uint64_t sum[64];
 #pragma unroll
         for (int i = 0; i < 64; ++i) sum[i] = 0;
         auto scale_of = [&](int kb) {
-          if ((kb & 15) == 0) {
+          if (((kb - k0) & 15) == 0) {
             // this half of the table has come; the other is free, as every lane is past its last use
             asm volatile("cp.async.wait_group 0;" ::: "memory");
             __syncwarp();
-            const bool on = kb + 16 < p.kb_total;
-            fetch_scales(on ? tl : next, on ? kb + 16 : 0, sbuf ^ 1);
+            const bool on = kb + 16 < k1;
+            fetch_scales(on ? tl : next, on ? kb + 16 : k0, sbuf ^ 1);
             sbuf ^= 1;
           }
-          const uint32_t at = my_scales + (sbuf ^ 1) * kScaleBytes + (kb & 15) * 4;
+          const uint32_t at = my_scales + (sbuf ^ 1) * kScaleBytes + ((kb - k0) & 15) * 4;
           return ld_shared_f32(at + lane * 68) * ld_shared_f32(at + 32 * 68);
         };
         bool ok = true;
-        for (int kb = 0; kb < p.kb_total; ++kb) {
+        for (int kb = k0; kb < k1; ++kb) {
           const float f0 = scale_of(kb);
           const uint64_t scale = pair_of(f0, f0);
           if (!(ok = wait_sums())) break;
@@ -489,101 +689,78 @@ __global__ void __launch_bounds__(kThreads, 1) cconv_pair_product_kernel(const _
           acc = lanes + buf * 256;
         }
         if (!ok) break;
+        auto piece32 = [&](int c, float (&f)[32]) {
+#pragma unroll
+          for (int i = 0; i < 16; ++i) {
+            const float2 v = halves_of(sum[c * 16 + i]);
+            f[2 * i] = v.x;
+            f[2 * i + 1] = v.y;
+          }
+        };
+        if (p.splits > 1) {  // as above, with the sums in registers
+          const int each = (o.block_n >> 5) / p.splits, row = q * 32 + lane, first = half * (cols >> 5);
+          cluster_sync_all();
+#pragma unroll
+          for (int c = 0; c < 4; ++c) {
+            const int i = first + c, owner = i / each;
+            if (c * 32 < cols && owner != share) {
+              float f[32];
+              piece32(c, f);
+              send32(cluster_map_shared(base, uint32_t(2 * owner) + rank) +
+                         uint32_t((share < owner ? share : share - 1) * each + i - owner * each) * kShareBytes,
+                     row, f);
+            }
+          }
+          cluster_sync_all();
+          met = true;
+#pragma unroll
+          for (int c = 0; c < 4; ++c) {
+            const int i = first + c;
+            if (c * 32 < cols && i / each == share) {
+              float f[32];
+              piece32(c, f);
+              join32(base, row, p.splits, share, each, i - share * each, f);
+              const int64_t r = row0 + lane, col = int64_t(tl.n) * o.block_n + i * 32;
+              write32<T>(p.out[0], p.out_rs[0], p.out_cs[0], r, col, r < o.M ? int(min(int64_t(32), o.N - col)) : 0, f);
+            }
+          }
+          break;
+        }
         constexpr int kWidth = 128 / int(sizeof(T));  // columns of a piece
 #pragma unroll
         for (int c = 0; c < 128; c += kWidth) {
           if (c < cols) {
-            const uint32_t to = mine;
             if (lane == 0) bulk_wait_group_read<0>();
             __syncwarp();
-            float f[kWidth];
-#pragma unroll
-            for (int i = 0; i < kWidth / 2; ++i) {
-              const float2 v = halves_of(sum[c / 2 + i]);
-              f[2 * i] = v.x;
-              f[2 * i + 1] = v.y;
-            }
+            float f[32];
+            piece32(c / 32, f);
             if constexpr (sizeof(T) == 4) {
-              stage_f32(to, lane, f);
+              stage_f32(mine, lane, f);
             } else {
-#pragma unroll
-              for (int j = 0; j < 8; ++j)
-                st_shared_v4(chunk_at(to, lane, j), pack2<T>(f[8 * j], f[8 * j + 1]), pack2<T>(f[8 * j + 2], f[8 * j + 3]),
-                             pack2<T>(f[8 * j + 4], f[8 * j + 5]), pack2<T>(f[8 * j + 6], f[8 * j + 7]));
+              stage32<T>(mine, lane, 0, f);
+              piece32(c / 32 + 1, f);
+              stage32<T>(mine, lane, 4, f);
             }
             fence_proxy_async_smem();
             __syncwarp();
             if (lane == 0) {
-              const int col = tl.n * p.block_n + half * cols + c;
-              if (row0 < p.M && col < p.N) tma_store_2d(&maps.out[0], to, col, row0);
+              const int col = tl.n * o.block_n + half * cols + c;
+              if (row0 < o.M && col < o.N) tma_store_2d(out_map, mine, col, row0);
               bulk_commit_group();
             }
           }
         }
         continue;  // the buffers were handed on block by block
-      } else if constexpr (kEpi == kScaledPartial) {
-        // As kPartial, of 8-bit operands: rows are features (128 of a CTA share a scale), columns tokens
-        // (a scale each, held by one lane and passed round).
-        const int cols = max(p.block_n >> 1, 32);
-        const int k0 = tl.split * p.kb_split, k1 = min(p.kb_total, k0 + p.kb_split);
-        const bool busy = half * cols < p.block_n;
-        const int n = tl.n * p.block_n + half * cols;
-        const int64_t mb = min(int64_t(row0) >> 7, (p.M - 1) >> 7);
-        float2 sum[64];
-#pragma unroll
-        for (int i = 0; i < 64; ++i) sum[i] = make_float2(0.0f, 0.0f);
-        bool ok = true;
-        for (int kb = k0; kb < k1; ++kb) {
-          const float sb = p.row_scale[mb * p.row_rs + kb * p.row_ks];
-          float sa[4];
-#pragma unroll
-          for (int c = 0; c < 4; ++c)
-            sa[c] = c * 32 < cols ? sb * p.col_scale[min(int64_t(n + c * 32 + lane), p.N - 1) * p.col_rs + kb * p.col_ks] : 0.0f;
-          if (!(ok = wait_sums())) break;
-          if (busy) {
-#pragma unroll
-            for (int c = 0; c < 4; ++c) {
-              if (c * 32 < cols) {
-                float f[32];
-                load_sums(acc + half * cols + c * 32, f);
-#pragma unroll
-                for (int i = 0; i < 16; ++i) {
-                  sum[c * 16 + i].x += f[2 * i] * __shfl_sync(0xffffffffu, sa[c], 2 * i);
-                  sum[c * 16 + i].y += f[2 * i + 1] * __shfl_sync(0xffffffffu, sa[c], 2 * i + 1);
-                }
-              }
-            }
-          }
-          release_sums();
-          if (++buf == 2) buf = 0, bph ^= 1;
-          acc = lanes + buf * 256;
-        }
-        if (!ok) break;
-        float* to = p.partial + tl.split * p.slice + int64_t(tl.m) * 256 + rank * 128 + q * 32 + lane;
-#pragma unroll
-        for (int c = 0; c < 128; ++c)
-          if (busy && c < cols && n + c < p.N) to[(n + c) * p.pitch] = c & 1 ? sum[c / 2].y : sum[c / 2].x;
-        continue;
-      } else {  // kPartial: lanes are neighbours along the table's rows; the table covers whole tiles
-        if (!wait_sums()) break;
-        const int cols = max(p.block_n >> 1, 32);
-        float* to = p.partial + tl.split * p.slice + int64_t(tl.m) * 256 + rank * 128 + q * 32 + lane;
-        if (half * cols < p.block_n) {
-          for (int c = 0; c < cols; c += 32) {
-            float f[32];
-            load_sums(acc + half * cols + c, f);
-            const int n = tl.n * p.block_n + half * cols + c;
-#pragma unroll
-            for (int i = 0; i < 32; ++i)
-              if (n + i < p.N) to[(n + i) * p.pitch] = f[i];
-          }
-        }
-        release_sums();
       }
       if (++buf == 2) buf = 0, bph ^= 1;
     }
-    if constexpr (kEpi == kScaled) asm volatile("cp.async.wait_all;" ::: "memory");
-    if (kPieces<kEpi> > 0 && lane == 0) bulk_wait_group<0>();
+    if (p.splits > 1 && !met) {  // gave up on the way: the others are not kept waiting
+      __syncwarp();
+      cluster_sync_all();
+      cluster_sync_all();
+    }
+    if constexpr (kEightBit) asm volatile("cp.async.wait_all;" ::: "memory");
+    if (lane == 0) bulk_wait_group<0>();
   }
 
   // A wait that ran out raised the flag a whole limit after the last copy or MMA was issued; the other
@@ -597,13 +774,14 @@ __global__ void __launch_bounds__(kThreads, 1) cconv_pair_product_kernel(const _
   }
   __syncwarp();
   tc_fence_before();
-  cluster_sync_all();  // nothing arrives at, or reads, the other CTA's shared memory any more
+  cluster_sync_all();  // nothing arrives at, or reads, another CTA's shared memory any more
   tc_fence_after();
   if (warp == 2) pair_tmem_dealloc(tmem, kTmemCols);
 }
 
 template <int kEpi, typename T>
-cudaError_t launch_pair(const PairMaps& maps, const PairParams& p, int sms, bool chained, cudaStream_t s) {
+cudaError_t launch_pair(const PairMaps<kProductsOf<kEpi>>& maps, const PairParams<kProductsOf<kEpi>>& p, int sms, bool chained,
+                        cudaStream_t s) {
   auto f = cconv_pair_product_kernel<kEpi, T>;
   static bool ready[64] = {};
   int dev = 0;
@@ -614,26 +792,10 @@ cudaError_t launch_pair(const PairMaps& maps, const PairParams& p, int sms, bool
     if (e != cudaSuccess) return e;
     __atomic_store_n(&ready[dev & 63], true, __ATOMIC_RELEASE);
   }
-  const int tiles = p.tiles_m * p.tiles_n * p.splits;
-  const int pairs = tiles < sms / 2 ? tiles : sms / 2;
-  const size_t smem = 1024 + size_t(p.stages) * (kABytes + p.b_bytes) + kEpilogueWarps * staged_pieces(kEpi) * kBoxBytes +
+  const int pairs = p.splits > 1 ? p.tiles * p.splits : p.tiles < sms / 2 ? p.tiles : sms / 2;
+  const size_t smem = 1024 + size_t(p.stages) * p.stage_bytes + kEpilogueWarps * staged_pieces(kEpi) * kBoxBytes +
                       scale_bytes(kEpi) + kBarrierBytes;
-  return launch(f, dim3(unsigned(2 * pairs)), kThreads, smem, 2, chained, s, maps, p);
-}
-
-template <int kEpi>
-cudaError_t launch_scaled(int dtype, const PairMaps& maps, const PairParams& p, int sms, bool chained, cudaStream_t s) {
-  if (dtype == CCONV_TYPE_BF16) return launch_pair<kEpi, __nv_bfloat16>(maps, p, sms, chained, s);
-  if (dtype == CCONV_TYPE_FP16) return launch_pair<kEpi, __half>(maps, p, sms, chained, s);
-  return launch_pair<kEpi, float>(maps, p, sms, chained, s);
-}
-
-template <typename T>
-cudaError_t launch_epilogue(int epi, const PairMaps& maps, const PairParams& p, int sms, bool chained, cudaStream_t s) {
-  if (epi == kStore) return launch_pair<kStore, T>(maps, p, sms, chained, s);
-  if (epi == kGated) return launch_pair<kGated, T>(maps, p, sms, chained, s);
-  if (epi == kGatedBackward) return launch_pair<kGatedBackward, T>(maps, p, sms, chained, s);
-  return launch_pair<kPartial, T>(maps, p, sms, chained, s);
+  return launch(f, dim3(unsigned(2 * pairs)), kThreads, smem, 2 * p.splits, chained, s, maps, p);
 }
 
 int encode_operand(CUtensorMap* tm, const Operand& o, int es, int dtype, int rows_box) {
@@ -642,84 +804,124 @@ int encode_operand(CUtensorMap* tm, const Operand& o, int es, int dtype, int row
                   : encode_map(tm, o.p, 2, dtype, o.rows, o.k, o.pitch, 64, 64);
 }
 
-// ---- finishing passes: four neighbouring columns a thread, a row a blockIdx.y step -----------------
-__device__ __forceinline__ void add_up(const Partial& p, int64_t at, float (&f)[4]) {
-  float4 v = *reinterpret_cast<const float4*>(p.p + at);
-  for (int s = 1; s < p.splits; ++s) {
-    const float4 w = *reinterpret_cast<const float4*>(p.p + s * p.slice + at);
-    v.x += w.x; v.y += w.y; v.z += w.z; v.w += w.w;
-  }
-  f[0] = v.x; f[1] = v.y; f[2] = v.z; f[3] = v.w;
-}
-template <typename T>
-__device__ __forceinline__ void put4(const Mat& m, int64_t r, int64_t c, int64_t N, const float (&f)[4]) {
-  T* o = static_cast<T*>(const_cast<void*>(m.p)) + r * m.rs + c * m.cs;
-#pragma unroll
-  for (int i = 0; i < 4; ++i)
-    if (c + i < N) o[i * m.cs] = from_f32<T>(f[i]);
-}
-template <typename T>
-__device__ __forceinline__ void get4(const Mat& m, int64_t r, int64_t c, int64_t N, float (&f)[4]) {
-  const T* o = static_cast<const T*>(m.p) + r * m.rs + c * m.cs;
-#pragma unroll
-  for (int i = 0; i < 4; ++i) f[i] = c + i < N ? to_f32(o[i * m.cs]) : 0.0f;
-}
-#define CCONV_FINISH_PROLOGUE                                                          \
-  asm volatile("griddepcontrol.wait;" ::: "memory");                                   \
-  if (more) asm volatile("griddepcontrol.launch_dependents;" ::: "memory");            \
-  const int64_t n = (int64_t(blockIdx.x) * 128 + threadIdx.x) * 4;                     \
-  if (n >= N) return;
-
-template <typename T>
-__global__ void __launch_bounds__(128) finish_store_kernel(Partial p, Mat out, int64_t M, int64_t N, int more) {
-  CCONV_FINISH_PROLOGUE
-  for (int64_t m = blockIdx.y; m < M; m += gridDim.y) {
-    float f[4];
-    add_up(p, m * p.pitch + n, f);
-    put4<T>(out, m, n, N, f);
-  }
-}
-
-template <typename T>
-__global__ void __launch_bounds__(128) finish_gated_kernel(Partial p, Mat gate_pre, Mat up_pre, Mat h, int64_t M,
-                                                           int64_t N, int act, int more) {
-  CCONV_FINISH_PROLOGUE
-  for (int64_t m = blockIdx.y; m < M; m += gridDim.y) {
-    float g[4], u[4], f[4], da;
-    add_up(p, m * p.pitch + n, g);
-    add_up(p, m * p.pitch + p.second + n, u);
-#pragma unroll
-    for (int i = 0; i < 4; ++i) f[i] = activation<false>(act, g[i], da) * u[i];
-    put4<T>(h, m, n, N, f);
-    if (gate_pre.p) {
-      put4<T>(gate_pre, m, n, N, g);
-      put4<T>(up_pre, m, n, N, u);
+template <int kEpi>
+int run_as(const Launch& l, int sms, bool chained, bool more, cudaStream_t s) {
+  constexpr int kProducts = kProductsOf<kEpi>;
+  constexpr bool kEight = kEpi == kScaled;
+  PairMaps<kProducts> maps;
+  PairParams<kProducts> q;
+  int rc = block_status_word(&q.status);
+  if (rc != CCONV_OK) return rc;
+  const int es = type_bytes(l.dtype);
+  uint32_t b_most = 0;
+  q.tiles = 0;
+  q.count = l.count;
+  q.splits = l.splits;
+  for (int i = 0; i < l.count; ++i) {
+    const Product& p = l.of[i];
+    ProductParams& o = q.of[i];
+    ProductMaps& m = maps.of[i];
+    o.tiles_m = int(cdiv64(p.M, 256));
+    o.tiles_n = int(cdiv64(p.N, p.paired ? 128 : p.block_n));
+    o.first = q.tiles;
+    q.tiles += o.tiles_m * o.tiles_n;
+    o.kb_seg = int(cdiv64(p.K, kEight ? 128 : 64));
+    o.kb_total = o.kb_seg * (p.segments ? 2 : 1);
+    o.kb_part = int(cdiv64(o.kb_total, l.splits));
+    o.block_n = p.block_n;
+    o.b_bytes = uint32_t(p.block_n / 2) * 128;
+    if (o.b_bytes > b_most) b_most = o.b_bytes;
+    o.a_kmajor = p.a[0].kmajor;
+    o.b_kmajor = p.b[0].kmajor;
+    o.a_desc = swizzled_desc(p.a[0].kmajor, 8192);
+    o.b_desc = swizzled_desc(p.b[0].kmajor, 8192);
+    o.a_step = p.a[0].kmajor ? 32 >> 4 : 2048 >> 4;
+    o.b_step = p.b[0].kmajor ? 32 >> 4 : 2048 >> 4;
+    const uint32_t type = !kEight && l.dtype == CCONV_TYPE_BF16 ? 1u : 0u;  // (8 bits: 0 is e4m3)
+    // instruction descriptor: D fp32, types of A and B, their orders (1: rows contiguous), N / 8, M / 16
+    o.idesc = (1u << 4) | (type << 7) | (type << 10) | (uint32_t(!p.a[0].kmajor) << 15) |
+              (uint32_t(!p.b[0].kmajor) << 16) | (uint32_t(p.block_n >> 3) << 17) | (uint32_t(256 >> 4) << 24);
+    o.M = p.M;
+    o.N = p.N;
+    for (int j = 0; j < 2 && rc == CCONV_OK; ++j) {
+      if (j == 0 || p.segments) rc = encode_operand(&m.a[j], p.a[j], kEight ? 1 : 2, l.dtype, 128);
+      if (rc == CCONV_OK && (j == 0 || p.segments || p.paired)) rc = encode_operand(&m.b[j], p.b[j], kEight ? 1 : 2, l.dtype, p.block_n / 2);
     }
+    if (rc == CCONV_OK && l.splits == 1) rc = encode_map(&m.out, p.out[0].p, es, l.dtype, p.N, p.M, p.out[0].rs, 128 / es, 32);
+    if (rc != CCONV_OK) return rc;
   }
+  const Product& p = l.of[0];
+  for (int i = 0; i < 3; ++i) {
+    q.out[i] = static_cast<char*>(const_cast<void*>(p.out[i].p));
+    q.out_rs[i] = p.out[i].rs;
+    q.out_cs[i] = p.out[i].cs;
+  }
+  for (int i = 0; i < 2; ++i) {
+    q.in[i] = static_cast<const char*>(p.in[i].p);
+    q.in_rs[i] = p.in[i].rs;
+  }
+  if constexpr (kEpi == kGated || kEpi == kGatedBackward) {
+    CUtensorMap* more_maps[4] = {&maps.out1, &maps.out2, &maps.in[0], &maps.in[1]};
+    const Mat* mats[4] = {&p.out[1], &p.out[2], &p.in[0], &p.in[1]};
+    for (int i = 0; i < 4 && l.splits == 1; ++i)
+      if (mats[i]->p && (rc = encode_map(more_maps[i], mats[i]->p, es, l.dtype, p.N, p.M, mats[i]->rs, 64, 32))) return rc;
+  }
+  q.stage_bytes = kABytes + b_most;
+  const uint32_t staged = kEpilogueWarps * staged_pieces(kEpi) * kBoxBytes + scale_bytes(kEpi);
+  q.stages = int((kSmemMost - 1024 - kBarrierBytes - staged) / q.stage_bytes);
+  if (q.stages > kMostStages) q.stages = kMostStages;
+  q.paired = p.paired;
+  q.act = l.act;
+  q.save = l.save;
+  q.more = more;
+  q.row_scale = static_cast<const float*>(l.row_scale.p);
+  q.row_rs = l.row_scale.rs;
+  q.row_ks = l.row_scale.cs;
+  q.col_scale = static_cast<const float*>(l.col_scale.p);
+  q.col_rs = l.col_scale.rs;
+  q.col_ks = l.col_scale.cs;
+  q.limit_ns = block_wait_limit_ns();
+  cudaError_t e;
+  if (l.dtype == CCONV_TYPE_BF16) e = launch_pair<kEpi, __nv_bfloat16>(maps, q, sms, chained, s);
+  else if (l.dtype == CCONV_TYPE_FP16) e = launch_pair<kEpi, __half>(maps, q, sms, chained, s);
+  else if constexpr (kEight) e = launch_pair<kEpi, float>(maps, q, sms, chained, s);
+  else return CCONV_EUNSUPPORTED;
+  return block_cuda_error(e, "cconv_pair_product_kernel");
 }
 
-template <typename T>
-__global__ void __launch_bounds__(128) finish_gated_backward_kernel(Partial p, Mat gate_pre, Mat up_pre, Mat dg,
-                                                                    Mat du, Mat h, int64_t M, int64_t N, int act,
-                                                                    int more) {
-  CCONV_FINISH_PROLOGUE
-  for (int64_t m = blockIdx.y; m < M; m += gridDim.y) {
-    float d[4], g[4], u[4], f[4];
-    get4<T>(gate_pre, m, n, N, g);
-    get4<T>(up_pre, m, n, N, u);
-    add_up(p, m * p.pitch + n, d);
+// Clocks of one product's tile: its k blocks at the slower of the tensor cores (block_n * 2 clocks a block and
+// pair) and of L2 (about 60 bytes a clock and SM while all draw), and what begins and ends it.
+double tile_clocks(const Product& p, int splits, int es) {
+  const double kb = double(cdiv64(cdiv64(p.K, 128 / es) * (p.segments ? 2 : 1), splits));
+  const double rows = double(p.M < 256 ? p.M : 256) + p.block_n;
+  const double block = std::max(2.0 * p.block_n * (es == 1 ? 1.7 : 1.0) + 30.0, rows * 128.0 / 120.0);
+  return kb * block + (splits > 1 ? 4000.0 : 600.0);
+}
+
+// Rows of `pieces` accesses of type E, both sides contiguous: 64 threads by 4 rows a block, 4 accesses a thread.
+template <typename E>
+__global__ void __launch_bounds__(256) cconv_copy_rows_kernel(Mat from, Mat to, int64_t rows, int64_t pieces, int more) {
+  asm volatile("griddepcontrol.wait;" ::: "memory");
+  if (more) asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
+  const int64_t x0 = int64_t(blockIdx.x) * 256 + (threadIdx.x & 63);
+  for (int64_t r = int64_t(blockIdx.y) * 4 + (threadIdx.x >> 6); r < rows; r += int64_t(gridDim.y) * 4) {
+    const E* src = reinterpret_cast<const E*>(static_cast<const char*>(from.p) + r * from.rs);
+    E* dst = reinterpret_cast<E*>(static_cast<char*>(const_cast<void*>(to.p)) + r * to.rs);
+    E v[4];
 #pragma unroll
-    for (int i = 0; i < 4; ++i) {
-      float da;
-      const float a = activation<true>(act, g[i], da);
-      g[i] = d[i] * u[i] * da;
-      f[i] = d[i] * a;
-      u[i] = a * u[i];
-    }
-    put4<T>(dg, m, n, N, g);
-    put4<T>(du, m, n, N, f);
-    put4<T>(h, m, n, N, u);
+    for (int i = 0; i < 4; ++i)
+      if (x0 + 64 * i < pieces) v[i] = src[x0 + 64 * i];
+#pragma unroll
+    for (int i = 0; i < 4; ++i)
+      if (x0 + 64 * i < pieces) dst[x0 + 64 * i] = v[i];
   }
+}
+template <typename E>
+cudaError_t copy_rows(const Mat& from, const Mat& to, int64_t rows, int64_t cols, int es, bool chained, bool more, cudaStream_t s) {
+  const int64_t pieces = cols * es / int64_t(sizeof(E)), y = cdiv64(rows, 4);
+  const dim3 grid(unsigned(cdiv64(pieces, 256)), unsigned(y < 65535 ? y : 65535));
+  return launch(cconv_copy_rows_kernel<E>, grid, 256, 0, 1, chained, s, Mat(from.p, from.rs * es, 1), Mat(to.p, to.rs * es, 1),
+                rows, pieces, int(more));
 }
 
 // 32 x 32 elements a block through shared memory: read along the source's short stride, written along
@@ -749,8 +951,6 @@ __global__ void __launch_bounds__(256) cconv_copy_kernel(Mat from, Mat to, int64
   }
 }
 
-dim3 finish_grid(int64_t M, int64_t N) { return dim3(unsigned(cdiv64(N, 512)), unsigned(M < 16384 ? M : 16384)); }
-
 }  // namespace
 
 uint64_t block_wait_limit_ns() {
@@ -759,99 +959,78 @@ uint64_t block_wait_limit_ns() {
 }
 
 int block_status_word(int** word) {
+  static int* words[64] = {};
+  int dev = 0;
+  cudaError_t e = cudaGetDevice(&dev);
+  if (e != cudaSuccess) return block_cuda_error(e, "cudaGetDevice");
+  *word = __atomic_load_n(&words[dev & 63], __ATOMIC_ACQUIRE);
+  if (*word) return CCONV_OK;
   void* p = nullptr;
-  const cudaError_t e = cudaGetSymbolAddress(&p, g_block_status);
+  e = cudaGetSymbolAddress(&p, g_block_status);
   *word = static_cast<int*>(p);
+  if (e == cudaSuccess) __atomic_store_n(&words[dev & 63], *word, __ATOMIC_RELEASE);
   return block_cuda_error(e, "cudaGetSymbolAddress");
 }
 
-int64_t partial_rows(int64_t M, int stack) { return cdiv64(M, 256) * 256 * stack; }
-
-cudaError_t run_product(const Product& p, int sms, bool chained, bool more, cudaStream_t s, int* rc) {
-  PairMaps maps;
-  PairParams q{};
-  *rc = block_status_word(&q.status);
-  if (*rc) return cudaSuccess;
-  const int stack = p.stacked ? 2 : 1;
-  q.tiles_m0 = int(cdiv64(p.M, 256));
-  q.tiles_m = q.tiles_m0 * stack;
-  q.tiles_n = int(cdiv64(p.N, p.paired ? 128 : p.block_n));
-  const bool eight = p.epilogue == kScaled || p.epilogue == kScaledPartial;
-  q.kb_seg = int(cdiv64(p.K, eight ? 128 : 64));
-  q.kb_total = q.kb_seg * (p.segments ? 2 : 1);
-  q.kb_split = int(cdiv64(q.kb_total, p.splits));
-  q.splits = int(cdiv64(q.kb_total, q.kb_split));
-  q.block_n = p.block_n;
-  q.b_bytes = uint32_t(p.block_n / 2) * 128;
-  const uint32_t staged = kEpilogueWarps * staged_pieces(p.epilogue) * kBoxBytes + scale_bytes(p.epilogue);
-  q.stages = int((kSmemMost - 1024 - kBarrierBytes - staged) / (kABytes + q.b_bytes));
-  if (q.stages > 8) q.stages = 8;
-  q.a_kmajor = p.a[0].kmajor;
-  q.b_kmajor = p.b[0].kmajor;
-  q.paired = p.paired;
-  q.a_desc = swizzled_desc(p.a[0].kmajor, 8192);
-  q.b_desc = swizzled_desc(p.b[0].kmajor, 8192);
-  q.a_step = p.a[0].kmajor ? 32 >> 4 : 2048 >> 4;
-  q.b_step = p.b[0].kmajor ? 32 >> 4 : 2048 >> 4;
-  const uint32_t type = !eight && p.dtype == CCONV_TYPE_BF16 ? 1u : 0u;  // (8 bits: 0 is e4m3)
-  // instruction descriptor: D fp32, types of A and B, their orders (1: rows contiguous), N / 8, M / 16
-  q.idesc = (1u << 4) | (type << 7) | (type << 10) | (uint32_t(!p.a[0].kmajor) << 15) |
-            (uint32_t(!p.b[0].kmajor) << 16) | (uint32_t(p.block_n >> 3) << 17) | (uint32_t(256 >> 4) << 24);
-  q.M = p.M;
-  q.N = p.N;
-  q.act = p.act;
-  q.save = p.save;
-  q.more = more;
-  q.partial = p.partial;
-  q.pitch = p.pitch;
-  q.slice = p.slice;
-  q.row_scale = static_cast<const float*>(p.row_scale.p);
-  q.row_rs = p.row_scale.rs;
-  q.row_ks = p.row_scale.cs;
-  q.col_scale = static_cast<const float*>(p.col_scale.p);
-  q.col_rs = p.col_scale.rs;
-  q.col_ks = p.col_scale.cs;
-  q.limit_ns = block_wait_limit_ns();
-  const int two_a = p.segments || p.stacked ? 2 : 1, two_b = p.segments || p.paired ? 2 : 1;
-  for (int i = 0; i < 2; ++i) {
-    if ((*rc = encode_operand(&maps.a[i], p.a[i < two_a ? i : 0], eight ? 1 : 2, p.dtype, 128))) return cudaSuccess;
-    if ((*rc = encode_operand(&maps.b[i], p.b[i < two_b ? i : 0], eight ? 1 : 2, p.dtype, p.block_n / 2))) return cudaSuccess;
+double launch_clocks(const Launch& l, int sms) {
+  const int es = l.epilogue == kScaled ? 1 : 2;
+  // clusters that run at one time: of 4 and 8 CTAs some SMs of a GPC are left over
+  const int slots = l.splits == 1 ? sms / 2 : l.splits == 2 ? sms / 4 - 1 : sms / 8 - 2;
+  double all = 0, longest = 0;
+  int64_t tiles = 0;
+  for (int i = 0; i < l.count; ++i) {
+    const Product& p = l.of[i];
+    const int64_t n = cdiv64(p.M, 256) * cdiv64(p.N, p.paired ? 128 : p.block_n);
+    const double c = tile_clocks(p, l.splits, es);
+    tiles += n;
+    all += double(n) * c;
+    longest = std::max(longest, c);
   }
-  for (int i = 0; i < 5; ++i) {
-    const Mat& m = i < 3 ? p.out[i] : p.in[i - 3];
-    CUtensorMap* tm = i < 3 ? &maps.out[i] : &maps.in[i - 3];
-    *tm = maps.a[0];
-    if (m.p && (*rc = encode_map(tm, m.p, type_bytes(p.dtype), p.dtype, p.N, p.M, m.rs, 128 / type_bytes(p.dtype), 32))) return cudaSuccess;
+  if (l.count == 1) return double(cdiv64(tiles, slots)) * longest + 5000.0;
+  return std::max(longest, all / slots + 0.5 * longest) + 5000.0;
+}
+
+void choose_cut(Launch* l, int sms, bool few_columns) {
+  Product& p = l->of[0];
+  const int es = l->epilogue == kScaled ? 1 : 2;
+  const int64_t kb = cdiv64(p.K, 128 / es) * (p.segments ? 2 : 1);
+  double best = 0;
+  int best_n = 0, best_s = 1;
+  for (int n = 256; n >= 64; n /= 2) {
+    if (p.paired && n != 256) continue;
+    if (n == 64 && (!few_columns || !p.b[0].kmajor)) continue;
+    for (int s = 1; s <= 4; s *= 2) {
+      if (s > 1 && (s - 1) * cdiv64(kb, s) >= kb) continue;      // every pair has a part
+      if ((p.paired ? 128 : n) / 32 < s) continue;                // and 32 columns to finish
+      p.block_n = n;
+      l->splits = s;
+      const double c = launch_clocks(*l, sms);
+      if (best_n == 0 || c < best) best = c, best_n = n, best_s = s;
+    }
   }
-  if (p.epilogue == kScaled) return launch_scaled<kScaled>(p.dtype, maps, q, sms, chained, s);
-  if (p.epilogue == kScaledPartial) return launch_pair<kScaledPartial, float>(maps, q, sms, chained, s);
-  return p.dtype == CCONV_TYPE_BF16 ? launch_epilogue<__nv_bfloat16>(p.epilogue, maps, q, sms, chained, s)
-                                    : launch_epilogue<__half>(p.epilogue, maps, q, sms, chained, s);
+  p.block_n = best_n;
+  l->splits = best_s;
 }
 
-cudaError_t finish_store(const Partial& p, const Mat& out, int64_t M, int64_t N, int dtype, bool more, cudaStream_t s) {
-  auto f = dtype == CCONV_TYPE_BF16   ? finish_store_kernel<__nv_bfloat16>
-           : dtype == CCONV_TYPE_FP16 ? finish_store_kernel<__half>
-                                      : finish_store_kernel<float>;
-  return launch(f, finish_grid(M, N), 128, 0, 1, true, s, p, out, M, N, int(more));
-}
-
-cudaError_t finish_gated(const Partial& p, const Mat& gate_pre, const Mat& up_pre, const Mat& h, int64_t M, int64_t N,
-                         int act, int dtype, bool more, cudaStream_t s) {
-  auto f = dtype == CCONV_TYPE_BF16 ? finish_gated_kernel<__nv_bfloat16> : finish_gated_kernel<__half>;
-  return launch(f, finish_grid(M, N), 128, 0, 1, true, s, p, gate_pre, up_pre, h, M, N, act, int(more));
-}
-
-cudaError_t finish_gated_backward(const Partial& p, const Mat& gate_pre, const Mat& up_pre, const Mat& dg,
-                                  const Mat& du, const Mat& h, int64_t M, int64_t N, int act, int dtype, bool more,
-                                  cudaStream_t s) {
-  auto f = dtype == CCONV_TYPE_BF16 ? finish_gated_backward_kernel<__nv_bfloat16> : finish_gated_backward_kernel<__half>;
-  return launch(f, finish_grid(M, N), 128, 0, 1, true, s, p, gate_pre, up_pre, dg, du, h, M, N, act, int(more));
+int run_products(const Launch& l, int sms, bool chained, bool more, cudaStream_t s) {
+  if (l.epilogue == kStore) return run_as<kStore>(l, sms, chained, more, s);
+  if (l.epilogue == kGated) return run_as<kGated>(l, sms, chained, more, s);
+  if (l.epilogue == kGatedBackward) return run_as<kGatedBackward>(l, sms, chained, more, s);
+  return run_as<kScaled>(l, sms, chained, more, s);
 }
 
 cudaError_t run_copy(const Mat& from, const Mat& to, int64_t rows, int64_t cols, int es, bool chained, bool more,
                      cudaStream_t s) {
   if (rows == 0 || cols == 0) return cudaSuccess;
+  if (from.cs == 1 && to.cs == 1) {
+    const uintptr_t all = reinterpret_cast<uintptr_t>(from.p) | reinterpret_cast<uintptr_t>(to.p) | uintptr_t(cols * es) |
+                          (rows > 1 ? uintptr_t(from.rs * es) | uintptr_t(to.rs * es) : 0);
+    if ((all & 15) == 0) return copy_rows<uint4>(from, to, rows, cols, es, chained, more, s);
+    if ((all & 7) == 0) return copy_rows<uint2>(from, to, rows, cols, es, chained, more, s);
+    if ((all & 3) == 0) return copy_rows<uint32_t>(from, to, rows, cols, es, chained, more, s);
+    if ((all & 1) == 0) return copy_rows<uint16_t>(from, to, rows, cols, es, chained, more, s);
+    return copy_rows<uint8_t>(from, to, rows, cols, es, chained, more, s);
+  }
   const int64_t y = cdiv64(rows, 32);
   const dim3 grid(unsigned(cdiv64(cols, 32)), unsigned(y < 65535 ? y : 65535));
   if (es == 1) return launch(cconv_copy_kernel<uint8_t>, grid, 256, 0, 1, chained, s, from, to, rows, cols, int(more));

@@ -1,0 +1,104 @@
+// A call as a sequence of launches: operands that the kernels can read in place or copies of them, products
+// with their cuts, results that the copy engine can write or a place for them.
+#pragma once
+#include <functional>
+#include <vector>
+
+#include "block.h"
+#include "block_gemm.h"
+
+namespace cconv {
+
+class Steps {
+ public:
+  // With no base the workspace is only measured, and nothing may be run.
+  Steps(void* base, int sms, int es, int dtype) : ws_(base), sms_(sms), es_(es), dtype_(dtype) {}
+
+  int64_t bytes() const { return ws_.used(); }
+  int sms() const { return sms_; }
+
+  // A step: launches something (chained: not the first; more: not the last) and gives a status code.
+  using Step = std::function<int(bool chained, bool more, cudaStream_t s)>;
+  void add(Step f) { steps_.push_back(std::move(f)); }
+  int run(cudaStream_t s) const {
+    for (size_t i = 0; i < steps_.size(); ++i) {
+      const int rc = steps_[i](i > 0, i + 1 < steps_.size(), s);
+      if (rc != CCONV_OK) return rc;
+    }
+    return CCONV_OK;
+  }
+
+  // rows x cols elements of `es` bytes, 16-byte aligned rows.
+  Mat scratch(int64_t rows, int64_t cols, int es) {
+    const int64_t pitch = round_up64(cols, 16 / es);
+    return Mat(ws_.take(rows * pitch * es), pitch, 1);
+  }
+  void copy(const Mat& from, const Mat& to, int64_t rows, int64_t cols, int es) {
+    add([=](bool chained, bool more, cudaStream_t s) {
+      return block_cuda_error(run_copy(from, to, rows, cols, es, chained, more, s), "cconv_copy_kernel");
+    });
+  }
+
+  // An operand of a product (rows x k) as it lies, or a copy of it with k contiguous.
+  Operand copied(const Mat& m, int64_t rows, int64_t k) {
+    const Mat to = scratch(rows, k, es_);
+    copy(m, to, rows, k, es_);
+    Operand o;
+    o.p = to.p;
+    o.pitch = to.rs;
+    o.kmajor = true;
+    o.rows = rows;
+    o.k = k;
+    return o;
+  }
+  Operand operand(const Mat& m, int64_t rows, int64_t k, bool want_kmajor = false) {
+    Operand o;
+    return operand_in_place(m, rows, k, es_, !want_kmajor && es_ == 2, &o) ? o : copied(m, rows, k);
+  }
+  // Two operands of one product, in the same order.
+  void operands(const Mat& a, const Mat& b, int64_t rows, int64_t k, Operand* oa, Operand* ob) {
+    *oa = operand(a, rows, k);
+    *ob = operand(b, rows, k, oa->kmajor);
+    if (oa->kmajor != ob->kmajor) *oa = copied(a, rows, k);
+  }
+  // A matrix that is read row by row.
+  Mat readable(const cconv_matrix& m, int64_t rows, int64_t cols) {
+    Operand o;
+    if (operand_in_place(Mat(m), rows, cols, es_, false, &o)) return Mat(o.p, o.pitch, 1);
+    const Mat to = scratch(rows, cols, es_);
+    copy(Mat(m), to, rows, cols, es_);
+    return to;
+  }
+
+  // Adds a launch.  `to[i]` is where out[i] of the i-th product (or of the only one) belongs; what the
+  // copy engine cannot write there in place goes to the workspace first.
+  void launch(Launch l, const Mat* to) {
+    struct Move { Mat from, to; int64_t M, N; };
+    std::vector<Move> moves;
+    const int es = type_bytes(dtype_);
+    for (int i = 0; i < (l.count > 1 ? l.count : 3); ++i) {
+      if (!to[i].p) continue;
+      Product& p = l.of[l.count > 1 ? i : 0];
+      Mat& out = p.out[l.count > 1 ? 0 : i];
+      out = to[i];
+      Operand o;
+      if (l.splits > 1) continue;  // written straight to any layout
+      if (operand_in_place(to[i], p.M, p.N, es, false, &o)) {
+        out = Mat(o.p, o.pitch, 1);
+      } else {
+        out = scratch(p.M, p.N, es);
+        moves.push_back({out, to[i], p.M, p.N});
+      }
+    }
+    const int sms = sms_;
+    add([=](bool chained, bool more, cudaStream_t s) { return run_products(l, sms, chained, more, s); });
+    for (const Move& m : moves) copy(m.from, m.to, m.M, m.N, es);
+  }
+
+ private:
+  Carver ws_;
+  const int sms_, es_, dtype_;
+  std::vector<Step> steps_;
+};
+
+}  // namespace cconv

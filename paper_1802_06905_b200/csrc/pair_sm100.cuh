@@ -61,11 +61,12 @@ __device__ __forceinline__ void pair_mma_f8(uint32_t d, uint64_t a, uint64_t b, 
       "l"(a), "l"(b), "r"(idesc), "r"(accumulate)
       : "memory");
 }
-// Arrives at the barrier at this offset in both CTAs once every MMA issued so far has completed.
-__device__ __forceinline__ void pair_commit(uint32_t bar) {
+// Arrives at the barrier at this offset in the CTAs of the mask (bits: ranks in the cluster) once every MMA
+// issued so far has completed.
+__device__ __forceinline__ void pair_commit(uint32_t bar, uint16_t mask) {
   asm volatile(
       "tcgen05.commit.cta_group::2.mbarrier::arrive::one.shared::cluster.multicast::cluster.b64 [%0], %1;" ::"r"(bar),
-      "h"(uint16_t(3))
+      "h"(mask)
       : "memory");
 }
 
