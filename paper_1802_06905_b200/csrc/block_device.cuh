@@ -47,33 +47,73 @@ __device__ __forceinline__ float2 unpack2<__half>(uint32_t w) {
   return __half22float2(*reinterpret_cast<const __half2*>(&w));
 }
 
-// The activation's value a(g) and, if asked for, its derivative.  The exponential and the quotient
-// are the fast ones (a few units in the last place of fp32, far below a 16-bit rounding).
+// The activation's value a(g) and, if asked for, its derivative.  The exponential, the quotient and gelu's
+// error function are fast ones (1e-7 of 1, far below a 16-bit rounding).
 //   silu       g s(g)              s(1 + g(1 - s)),          s = 1/(1 + exp(-g))
 //   gelu       g Phi(g)            Phi + g exp(-g^2/2)/sqrt(2 pi)
 //   gelu_tanh  g s(2z)             s + g s(1 - s) 2z',       z = sqrt(2/pi)(g + 0.044715 g^3)
 //   relu       max(g, 0)           g > 0
-template <bool kDerivative>
-__device__ __forceinline__ float activation(int act, float g, float& da) {
-  if (act == CCONV_ACT_SILU) {
+template <int kAct, bool kDerivative>
+__device__ __forceinline__ float activation_of(float g, float& da) {
+  if constexpr (kAct == CCONV_ACT_SILU) {
     const float s = __fdividef(1.0f, 1.0f + __expf(-g));
     if (kDerivative) da = s * (1.0f + g * (1.0f - s));
     return g * s;
-  }
-  if (act == CCONV_ACT_GELU) {
-    const float phi = 0.5f * erfcf(-0.70710678118654752f * g);
-    if (kDerivative) da = phi + g * 0.39894228040143268f * __expf(-0.5f * g * g);
+  } else if constexpr (kAct == CCONV_ACT_GELU) {
+    // Abramowitz and Stegun 7.1.26: erfc(x) = t (a1 + t (a2 + ...)) exp(-x^2), t = 1 / (1 + 0.3275911 x), for
+    // x >= 0, within 1.5e-7; its exponential is the derivative's (x = |g| / sqrt 2)
+    const float e = __expf(-0.5f * g * g), t = __fdividef(1.0f, 1.0f + 0.23164190f * fabsf(g));
+    const float poly = t * (0.254829592f + t * (-0.284496736f + t * (1.421413741f + t * (-1.453152027f + t * 1.061405429f))));
+    const float tail = 0.5f * poly * e;  // Phi(-|g|)
+    const float phi = g > 0.0f ? 1.0f - tail : tail;
+    if (kDerivative) da = phi + g * 0.39894228040143268f * e;
     return g * phi;
-  }
-  if (act == CCONV_ACT_GELU_TANH) {
+  } else if constexpr (kAct == CCONV_ACT_GELU_TANH) {
     const float k = 1.5957691216057308f;  // 2 sqrt(2/pi)
     const float g2 = g * g;
     const float s = __fdividef(1.0f, 1.0f + __expf(-k * (g + 0.044715f * g * g2)));
     if (kDerivative) da = s + g * s * (1.0f - s) * k * (1.0f + 0.134145f * g2);
     return g * s;
+  } else {
+    if (kDerivative) da = g > 0.0f ? 1.0f : 0.0f;
+    return g > 0.0f ? g : (g != g ? g : 0.0f);
   }
-  if (kDerivative) da = g > 0.0f ? 1.0f : 0.0f;
-  return g > 0.0f ? g : (g != g ? g : 0.0f);
+}
+// h = a(g) u for N elements, in the place of g.  The choice is made once, not for each element: unrolled code
+// for all four would not fit the instruction cache.
+template <int kAct, int N>
+__device__ __forceinline__ void gate_as(float (&g)[N], const float (&u)[N]) {
+#pragma unroll
+  for (int i = 0; i < N; ++i) {
+    float unused;
+    g[i] = activation_of<kAct, false>(g[i], unused) * u[i];
+  }
+}
+template <int N>
+__device__ __forceinline__ void gate(int act, float (&g)[N], const float (&u)[N]) {
+  if (act == CCONV_ACT_SILU) gate_as<CCONV_ACT_SILU>(g, u);
+  else if (act == CCONV_ACT_GELU) gate_as<CCONV_ACT_GELU>(g, u);
+  else if (act == CCONV_ACT_GELU_TANH) gate_as<CCONV_ACT_GELU_TANH>(g, u);
+  else gate_as<CCONV_ACT_RELU>(g, u);
+}
+// From d = dL/dh, g and u: dL/dg in the place of g, dL/du in the place of d, h in the place of u.
+template <int kAct, int N>
+__device__ __forceinline__ void gate_backward_as(float (&d)[N], float (&g)[N], float (&u)[N]) {
+#pragma unroll
+  for (int i = 0; i < N; ++i) {
+    float da;
+    const float a = activation_of<kAct, true>(g[i], da);
+    g[i] = d[i] * u[i] * da;
+    d[i] = d[i] * a;
+    u[i] = a * u[i];
+  }
+}
+template <int N>
+__device__ __forceinline__ void gate_backward(int act, float (&d)[N], float (&g)[N], float (&u)[N]) {
+  if (act == CCONV_ACT_SILU) gate_backward_as<CCONV_ACT_SILU>(d, g, u);
+  else if (act == CCONV_ACT_GELU) gate_backward_as<CCONV_ACT_GELU>(d, g, u);
+  else if (act == CCONV_ACT_GELU_TANH) gate_backward_as<CCONV_ACT_GELU_TANH>(d, g, u);
+  else gate_backward_as<CCONV_ACT_RELU>(d, g, u);
 }
 
 // Pairs of fp32 values in a 64-bit register: two operations in one instruction.

@@ -198,8 +198,10 @@ __global__ void __launch_bounds__(kWarps * 32, 2) cconv_few_kernel(const FewPara
       const float f = gathered<B>(smem[parity], r, t);
       if constexpr (kRows == kPair) {
         const float up = gathered<B>(smem[parity], r + 8, t);
-        float unused;
-        put(p.out, p.out_dtype, t, n0 + r, activation<false>(p.act, f, unused) * up);
+        float h[1] = {f};
+        const float u[1] = {up};
+        gate(p.act, h, u);
+        put(p.out, p.out_dtype, t, n0 + r, h[0]);
         if (p.gate_pre.p) {
           put(p.gate_pre, p.out_dtype, t, n0 + r, f);
           put(p.up_pre, p.out_dtype, t, n0 + r, up);

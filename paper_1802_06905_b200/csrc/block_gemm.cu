@@ -12,7 +12,7 @@
 // that each finishes its own share of the columns (in the order of the parts: the result does not depend
 // on who is first).  One launch, no table of partial sums in memory.
 //
-// Roles: warp 0 copies (TMA), warp 1 of the first CTA issues MMAs, warp 2 owns the tensor memory, warps
+// Roles: warps 0 and 3 copy (TMA), warp 1 of the first CTA issues MMAs, warp 2 owns the tensor memory, warps
 // 4-11 are the epilogue (two for each quarter of the lanes, half of the columns each).
 #include <algorithm>
 #include <cstdlib>
@@ -33,7 +33,7 @@ constexpr uint32_t kBoxBytes = 32 * 128; // a piece that an epilogue warp stages
 constexpr uint32_t kTmemCols = 512;
 constexpr uint32_t kSmemMost = 232448;
 constexpr uint32_t kBarrierBytes = 512;
-constexpr int kMostStages = 10;
+constexpr int kMostStages = 16;
 
 __device__ int g_block_status;
 
@@ -42,7 +42,8 @@ struct ProductParams {
   int tiles_m, tiles_n, first;  // first: tiles of the products before it
   int kb_total, kb_seg, kb_part;  // k blocks: all, of the first segment, of a pair's part
   int block_n;
-  uint32_t b_bytes;             // a stage of B in one CTA
+  uint32_t a_bytes, b_bytes;    // what a stage brings of A and B to one CTA
+  uint32_t one_sided;           // the rows of A are all the first CTA's
   uint32_t a_kmajor, b_kmajor;
   uint32_t a_step, b_step;      // descriptor step of 16 elements of k (16-byte units)
   uint32_t idesc;
@@ -53,9 +54,11 @@ template <int kProducts>
 struct PairParams {
   ProductParams of[kProducts];
   int count, tiles, splits, stages;
-  uint32_t stage_bytes;
+  uint32_t a_stage, stage_bytes; // room of a stage's A; of the whole stage
+  uint32_t pieces;              // staged by an epilogue warp
   int paired, act, save, more;
-  // cut: where results go and come from (in elements)
+  int direct;  // results straight to memory (cut)
+  // direct: where results go and come from (in elements)
   char* out[3];
   int64_t out_rs[3], out_cs[3];
   const char* in[2];
@@ -128,6 +131,21 @@ __device__ __forceinline__ void load_sums(uint32_t taddr, float (&f)[32]) {
   for (int i = 0; i < 32; ++i) f[i] = __uint_as_float(v[i]);
 }
 
+// Eight columns (cut along k, where code that a launch fetches cold and runs once had better be short).
+__device__ __forceinline__ void load_sums8(uint32_t taddr, float (&f)[8]) {
+  uint32_t v[8];
+  asm volatile("tcgen05.ld.sync.aligned.32x32b.x8.b32 {%0, %1, %2, %3, %4, %5, %6, %7}, [%8];"
+               : "=r"(v[0]), "=r"(v[1]), "=r"(v[2]), "=r"(v[3]), "=r"(v[4]), "=r"(v[5]), "=r"(v[6]), "=r"(v[7])
+               : "r"(taddr)
+               : "memory");
+  asm volatile("tcgen05.wait::ld.sync.aligned;"
+               : "+r"(v[0]), "+r"(v[1]), "+r"(v[2]), "+r"(v[3]), "+r"(v[4]), "+r"(v[5]), "+r"(v[6]), "+r"(v[7])
+               :
+               : "memory");
+#pragma unroll
+  for (int i = 0; i < 8; ++i) f[i] = __uint_as_float(v[i]);
+}
+
 // 16-byte chunk c of row r of a piece staged with 128-byte swizzle.
 __device__ __forceinline__ uint32_t chunk_at(uint32_t base, int r, int c) {
   return base + r * 128 + ((c ^ (r & 7)) << 4);
@@ -140,28 +158,54 @@ __device__ __forceinline__ void stage32(uint32_t base, int r, int c0, const floa
                  pack2<T>(f[8 * c + 4], f[8 * c + 5]), pack2<T>(f[8 * c + 6], f[8 * c + 7]));
 }
 template <typename T>
+__device__ __forceinline__ uint4 pack8(const float (&f)[8]) {
+  return make_uint4(pack2<T>(f[0], f[1]), pack2<T>(f[2], f[3]), pack2<T>(f[4], f[5]), pack2<T>(f[6], f[7]));
+}
+template <typename T>
+__device__ __forceinline__ void unpack8(const uint4& w, float (&f)[8]) {
+  const uint32_t a[4] = {w.x, w.y, w.z, w.w};
+#pragma unroll
+  for (int i = 0; i < 4; ++i) {
+    const float2 v = unpack2<T>(a[i]);
+    f[2 * i] = v.x;
+    f[2 * i + 1] = v.y;
+  }
+}
+template <typename T>
 __device__ __forceinline__ void unstage32(uint32_t base, int r, int c0, float (&f)[32]) {
 #pragma unroll
   for (int c = 0; c < 4; ++c) {
-    uint32_t w[4];
-    ld_shared_v4(chunk_at(base, r, c0 + c), w[0], w[1], w[2], w[3]);
+    uint4 w;
+    ld_shared_v4(chunk_at(base, r, c0 + c), w.x, w.y, w.z, w.w);
+    float v[8];
+    unpack8<T>(w, v);
 #pragma unroll
-    for (int i = 0; i < 4; ++i) {
-      const float2 v = unpack2<T>(w[i]);
-      f[8 * c + 2 * i] = v.x;
-      f[8 * c + 2 * i + 1] = v.y;
-    }
+    for (int i = 0; i < 8; ++i) f[8 * c + i] = v[i];
   }
 }
 
 // Pieces that an epilogue warp stages.
-template <int kEpi>
-constexpr int kPieces = kEpi == kStore ? 2 : kEpi == kScaled ? 1 : 3;
-int staged_pieces(int epi) { return epi == kStore ? 2 : epi == kScaled ? 1 : 3; }
+int pieces_of(const Launch& l) {
+  if (l.direct) return 0;
+  return l.epilogue == kStore ? 2 : l.epilogue == kScaled || (l.epilogue == kGated && !l.save) ? 1 : 3;
+}
 // Scales of 8-bit rows that an epilogue warp keeps: 16 blocks of k of its 32 rows and of its columns
 // (row 32), the 16 in use and the next 16; a pitch of 17 words keeps the lanes on different banks.
 constexpr uint32_t kScaleBytes = 33 * 17 * 4;
 uint32_t scale_bytes(int epi) { return epi == kScaled ? 2 * kEpilogueWarps * kScaleBytes : 0; }
+// Rows of A that a stage brings to a CTA: 128, or fewer where the product has fewer (the tensor cores then
+// read what lies behind them for rows that nobody stores).  A stage of a few tokens is mostly weights, so that
+// more of those are on their way.
+int a_rows_of(const Product& p) {
+  const int least = p.a[0].kmajor ? 16 : 64;
+  int rows = 128;
+  while (rows > least && p.M <= rows / 2) rows /= 2;
+  return rows;
+}
+int stages_of(const Launch& l, uint32_t a_bytes, uint32_t b_bytes) {
+  const uint32_t other = 1024 + kBarrierBytes + kEpilogueWarps * pieces_of(l) * kBoxBytes + scale_bytes(l.epilogue) + kABytes - a_bytes;
+  return std::min(kMostStages, int((kSmemMost - other) / (a_bytes + b_bytes)));
+}
 
 __device__ __forceinline__ void cp_async4(uint32_t to, const float* from, bool there) {
   asm volatile("cp.async.ca.shared.global [%0], [%1], 4, %2;" ::"r"(to), "l"(from), "r"(there ? 4 : 0) : "memory");
@@ -184,89 +228,64 @@ __device__ __forceinline__ bool wait_all(uint32_t bar, uint32_t parity, volatile
   return __all_sync(0xffffffffu, mbar_wait_warp(bar, parity, abort_flag, status, code, limit_ns));
 }
 
-// ---- cut along k: exchange of accumulators and results straight to memory -------------------------
+// ---- exchange of accumulators (cut along k) and results straight to memory -------------------------
 // A piece of 32 columns by 128 rows, as the other pairs send it: 16 bytes of a row next to those of the next
 // row, so that lanes (rows) write and read neighbouring addresses.
 constexpr uint32_t kShareBytes = 128 * 32 * 4;
-__device__ __forceinline__ void send32(uint32_t to, int row, const float (&f)[32]) {
+__device__ __forceinline__ void send8(uint32_t to, int row, int c8, const float (&f)[8]) {
 #pragma unroll
-  for (int c = 0; c < 8; ++c)
-    st_cluster_v4(to + (c * 128 + row) * 16, __float_as_uint(f[4 * c]), __float_as_uint(f[4 * c + 1]),
+  for (int c = 0; c < 2; ++c)
+    st_cluster_v4(to + ((2 * c8 + c) * 128 + row) * 16, __float_as_uint(f[4 * c]), __float_as_uint(f[4 * c + 1]),
                   __float_as_uint(f[4 * c + 2]), __float_as_uint(f[4 * c + 3]));
-}
-__device__ __forceinline__ void add32(uint32_t from, int row, float (&f)[32]) {
-#pragma unroll
-  for (int c = 0; c < 8; ++c) {
-    uint32_t w[4];
-    ld_shared_v4(from + (c * 128 + row) * 16, w[0], w[1], w[2], w[3]);
-#pragma unroll
-    for (int i = 0; i < 4; ++i) f[4 * c + i] += __uint_as_float(w[i]);
-  }
 }
 // The sum of all pairs' parts in their order; f holds this pair's.  Piece `local` of `each` a pair lies at
 // from + (slot * each + local) pieces, slots being the other pairs in order.
-__device__ __forceinline__ void join32(uint32_t from, int row, int splits, int share, int each, int local, float (&f)[32]) {
-  float own[32];
+__device__ __forceinline__ void join8(uint32_t from, int row, int c8, int splits, int share, int each, int local, float (&f)[8]) {
+  float own[8];
 #pragma unroll
-  for (int i = 0; i < 32; ++i) {
+  for (int i = 0; i < 8; ++i) {
     own[i] = f[i];
     f[i] = 0.0f;
   }
   for (int s = 0; s < splits; ++s) {
     if (s == share) {
 #pragma unroll
-      for (int i = 0; i < 32; ++i) f[i] += own[i];
+      for (int i = 0; i < 8; ++i) f[i] += own[i];
     } else {
-      add32(from + uint32_t((s < share ? s : s - 1) * each + local) * kShareBytes, row, f);
+      const uint32_t at = from + uint32_t((s < share ? s : s - 1) * each + local) * kShareBytes + (2 * c8 * 128 + row) * 16;
+      uint32_t w[8];
+      ld_shared_v4(at, w[0], w[1], w[2], w[3]);
+      ld_shared_v4(at + 128 * 16, w[4], w[5], w[6], w[7]);
+#pragma unroll
+      for (int i = 0; i < 8; ++i) f[i] += __uint_as_float(w[i]);
     }
   }
 }
-// 32 columns of a row of a result, the first n of them in range.
+// Eight columns of a row of a result, the first n of them in range.
 template <typename T>
-__device__ __forceinline__ void write32(char* base, int64_t rs, int64_t cs, int64_t row, int64_t col, int n, const float (&f)[32]) {
+__device__ __forceinline__ void write8(char* base, int64_t rs, int64_t cs, int64_t row, int64_t col, int n, const float (&f)[8]) {
   T* to = reinterpret_cast<T*>(base) + row * rs + col * cs;
-  constexpr int E = 16 / int(sizeof(T));
-  if (cs == 1 && (reinterpret_cast<uintptr_t>(to) & 15u) == 0) {
-#pragma unroll
-    for (int c = 0; c < 32; c += E) {
-      if (c + E <= n) {
-        uint4 w;
-        if constexpr (sizeof(T) == 4) {
-          w = make_uint4(__float_as_uint(f[c]), __float_as_uint(f[c + 1]), __float_as_uint(f[c + 2]), __float_as_uint(f[c + 3]));
-        } else {
-          w = make_uint4(pack2<T>(f[c], f[c + 1]), pack2<T>(f[c + 2], f[c + 3]), pack2<T>(f[c + 4], f[c + 5]), pack2<T>(f[c + 6], f[c + 7]));
-        }
-        *reinterpret_cast<uint4*>(to + c) = w;
-      } else {
-#pragma unroll
-        for (int i = 0; i < E; ++i)
-          if (c + i < n) to[c + i] = from_f32<T>(f[c + i]);
-      }
+  if (n >= 8 && cs == 1 && (reinterpret_cast<uintptr_t>(to) & 15u) == 0) {
+    if constexpr (sizeof(T) == 4) {
+      reinterpret_cast<float4*>(to)[0] = make_float4(f[0], f[1], f[2], f[3]);
+      reinterpret_cast<float4*>(to)[1] = make_float4(f[4], f[5], f[6], f[7]);
+    } else {
+      *reinterpret_cast<uint4*>(to) = pack8<T>(f);
     }
   } else {
 #pragma unroll
-    for (int i = 0; i < 32; ++i)
+    for (int i = 0; i < 8; ++i)
       if (i < n) to[i * cs] = from_f32<T>(f[i]);
   }
 }
 template <typename T>
-__device__ __forceinline__ void read32(const char* base, int64_t rs, int64_t row, int64_t col, int n, float (&f)[32]) {
-  const T* from = reinterpret_cast<const T*>(base) + row * rs + col;
+__device__ __forceinline__ void read8(const char* base, int64_t rs, int64_t row, int64_t col, int n, float (&f)[8]) {
+  const T* from = reinterpret_cast<const T*>(base) + row * rs + col;  // rows are 16-byte aligned, col a multiple of 8
+  if (n >= 8) {
+    unpack8<T>(*reinterpret_cast<const uint4*>(from), f);
+  } else {
 #pragma unroll
-  for (int c = 0; c < 32; c += 8) {
-    if (c + 8 <= n && (reinterpret_cast<uintptr_t>(from) & 15u) == 0) {
-      const uint4 w = *reinterpret_cast<const uint4*>(from + c);
-      const uint32_t a[4] = {w.x, w.y, w.z, w.w};
-#pragma unroll
-      for (int i = 0; i < 4; ++i) {
-        const float2 v = unpack2<T>(a[i]);
-        f[c + 2 * i] = v.x;
-        f[c + 2 * i + 1] = v.y;
-      }
-    } else {
-#pragma unroll
-      for (int i = 0; i < 8; ++i) f[c + i] = c + i < n ? to_f32(from[c + i]) : 0.0f;
-    }
+    for (int i = 0; i < 8; ++i) f[i] = i < n ? to_f32(from[i]) : 0.0f;
   }
 }
 
@@ -277,7 +296,7 @@ __global__ void __launch_bounds__(kThreads, 1) cconv_pair_product_kernel(
   constexpr bool kEightBit = kEpi == kScaled;
   const uint32_t base = (smem_u32(smem_raw) + 1023u) & ~1023u;
   const uint32_t staging = base + p.stages * p.stage_bytes;
-  const uint32_t scales = staging + kEpilogueWarps * kPieces<kEpi> * kBoxBytes;
+  const uint32_t scales = staging + kEpilogueWarps * p.pieces * kBoxBytes;
   const uint32_t bars = (scales + (kEightBit ? 2 * kEpilogueWarps * kScaleBytes : 0) + 7) & ~7u;
   const uint32_t bar_full = bars, bar_empty = bars + 8 * p.stages;
   const uint32_t bar_tfull = bar_empty + 8 * p.stages, bar_tempty = bar_tfull + 16, bar_in = bar_tempty + 16;
@@ -321,7 +340,9 @@ __global__ void __launch_bounds__(kThreads, 1) cconv_pair_product_kernel(
   // the 384 x 168 that the block starts with)
   if (warp < 4) {
     if constexpr (kEightBit) asm volatile("setmaxnreg.dec.sync.aligned.u32 80;");
-    if (warp == 0) {
+    if (warp == 0 || warp == 3) {
+      // One thread copies A, one B: a copy costs its thread some 150 clocks to issue, and a stage has two or three.
+      const bool of_a = warp == 0;
       if (elect_one()) {
         uint32_t s = 0, ph = 0;
         const uint32_t full0 = cluster_map_shared(bar_full, leader);
@@ -330,33 +351,41 @@ __global__ void __launch_bounds__(kThreads, 1) cconv_pair_product_kernel(
           const Tile tl = tile_of(p, t);
           const ProductParams& o = p.of[tl.of];
           const ProductMaps& om = maps.of[tl.of];
-          const int m0 = tl.m * 256 + int(rank) * 128;
-          const int n0 = p.paired ? tl.n * 128 : tl.n * o.block_n + int(rank) * (o.block_n >> 1);
-          const int k0 = share * o.kb_part, k1 = min(o.kb_total, k0 + o.kb_part);
-          const int box_b = int(o.b_bytes) / 8192;
+          const int row = of_a ? tl.m * 256 + int(rank) * 128
+                               : p.paired ? tl.n * 128 : tl.n * o.block_n + int(rank) * (o.block_n >> 1);
+          const int k0 = share * o.kb_part, k1 = min(o.kb_total, k0 + o.kb_part), kb_seg = o.kb_seg;
+          const uint32_t bytes = of_a ? o.a_bytes : o.b_bytes;
+          const bool kmajor = of_a ? o.a_kmajor : o.b_kmajor;
+          const int boxes = kmajor ? 1 : int(bytes >> 13);
+          const bool none = of_a && o.one_sided && rank;  // its rows are past the end
+          const uint32_t expected = (o.one_sided ? 1 : 2) * o.a_bytes + 2 * o.b_bytes;
+          const CUtensorMap* map0 = of_a ? &om.a[0] : &om.b[p.paired && rank];
+          const CUtensorMap* map1 = of_a ? &om.a[1] : &om.b[1];
+          uint32_t to = base + s * p.stage_bytes + (of_a ? 0 : p.a_stage);
           for (int kb = k0; kb < k1; ++kb) {
-            if (!mbar_wait(bar_empty + 8 * s, ph ^ 1, abort_p, p.status, kStatProducerWait, p.limit_ns)) {
+            if (!mbar_try_wait(bar_empty + 8 * s, ph ^ 1) &&
+                !mbar_wait_slow(bar_empty + 8 * s, ph ^ 1, abort_p, p.status, kStatProducerWait, p.limit_ns)) {
               ok = false;
               break;
             }
-            const bool seg = kb >= o.kb_seg;
-            const int k = (seg ? kb - o.kb_seg : kb) * (kEightBit ? 128 : 64);
-            const CUtensorMap* ma = &om.a[seg];
-            const CUtensorMap* mb = &om.b[seg || (p.paired && rank)];
-            const uint32_t a = base + s * p.stage_bytes, b = a + kABytes, bar = full0 + 8 * s;
-            if (rank == 0) mbar_arrive_expect_tx(bar_full + 8 * s, 2 * (kABytes + o.b_bytes));
-            if (o.a_kmajor) {
-              tma_load_2d_pair(a, ma, k, m0, bar);
-            } else {
-              tma_load_2d_pair(a, ma, m0, k, bar);
-              tma_load_2d_pair(a + 8192, ma, m0 + 64, k, bar);
+            const bool seg = kb >= kb_seg;
+            const int k = (seg ? kb - kb_seg : kb) * (kEightBit ? 128 : 64);
+            const CUtensorMap* map = seg ? map1 : map0;
+            const uint32_t bar = full0 + 8 * s;
+            if (of_a && rank == 0) mbar_arrive_expect_tx(bar_full + 8 * s, expected);
+            if (!none) {
+              if (kmajor) {
+                tma_load_2d_pair(to, map, k, row, bar);
+              } else {
+                for (int i = 0; i < boxes; ++i) tma_load_2d_pair(to + 8192 * i, map, row + 64 * i, k, bar);
+              }
             }
-            if (o.b_kmajor) {
-              tma_load_2d_pair(b, mb, k, n0, bar);
-            } else {
-              for (int i = 0; i < box_b; ++i) tma_load_2d_pair(b + 8192 * i, mb, n0 + 64 * i, k, bar);
+            to += p.stage_bytes;
+            if (++s == uint32_t(p.stages)) {
+              s = 0;
+              ph ^= 1;
+              to -= p.stages * p.stage_bytes;
             }
-            if (++s == uint32_t(p.stages)) s = 0, ph ^= 1;
           }
         }
       }
@@ -391,7 +420,7 @@ __global__ void __launch_bounds__(kThreads, 1) cconv_pair_product_kernel(
             tc_fence_after();
             const uint32_t a = base + s * p.stage_bytes;
             if (issue) {
-              const uint64_t da = a_desc + (a >> 4), db = b_desc + ((a + kABytes) >> 4);
+              const uint64_t da = a_desc + (a >> 4), db = b_desc + ((a + p.a_stage) >> 4);
 #pragma unroll
               for (int j = 0; j < 4; ++j) {
                 if constexpr (kEightBit) pair_mma_f8(d, da + j * 2, db + j * 2, idesc, j > 0);
@@ -422,7 +451,7 @@ __global__ void __launch_bounds__(kThreads, 1) cconv_pair_product_kernel(
   } else {
     if constexpr (kEightBit) asm volatile("setmaxnreg.inc.sync.aligned.u32 208;");
     const int q = warp & 3, half = (warp - 4) >> 2;
-    const uint32_t mine = staging + (warp - 4) * kPieces<kEpi> * kBoxBytes;
+    const uint32_t mine = staging + (warp - 4) * p.pieces * kBoxBytes;
     const uint32_t in_bar = bar_in + 8 * (warp - 4);
     const uint32_t tempty0 = cluster_map_shared(bar_tempty, leader);
     const uint32_t lanes = tmem + (uint32_t(q * 32) << 16);
@@ -467,67 +496,66 @@ __global__ void __launch_bounds__(kThreads, 1) cconv_pair_product_kernel(
         if (lane == 0) mbar_arrive_cluster(tempty0 + 8 * buf);
       };
       if constexpr (!kEightBit) {
-        if (p.splits > 1) {
+        if (p.direct) {
           // Columns go in pieces of 32; the pair `owner` finishes `each` neighbouring ones (of both
           // g and u when paired).  The two halves of the warps take turns.
           if (!wait_sums()) break;
           const int all = p.paired ? 4 : o.block_n >> 5, each = all / p.splits, sent = p.paired ? 2 * each : each;
           const int row = q * 32 + lane;
-          cluster_sync_all();  // every pair's operands are used up: their place takes the pieces
-          for (int i = half; i < all; i += 2) {
+          if (p.splits > 1) cluster_sync_all();  // every pair's operands are used up: their place takes the pieces
+          for (int i = half; p.splits > 1 && i < all; i += 2) {
             const int owner = i / each;
             if (owner == share) continue;
             const uint32_t to = cluster_map_shared(base, uint32_t(2 * owner) + rank) +
                                 uint32_t((share < owner ? share : share - 1) * sent + i - owner * each) * kShareBytes;
-            float f[32];
-            load_sums(acc + i * 32, f);
-            send32(to, row, f);
-            if (p.paired) {
-              load_sums(acc + 128 + i * 32, f);
-              send32(to + each * kShareBytes, row, f);
+#pragma unroll 1
+            for (int c = 0; c < 4; ++c) {
+              float f[8];
+              load_sums8(acc + i * 32 + c * 8, f);
+              send8(to, row, c, f);
+              if (p.paired) {
+                load_sums8(acc + 128 + i * 32 + c * 8, f);
+                send8(to + each * kShareBytes, row, c, f);
+              }
             }
           }
-          cluster_sync_all();  // all pieces have come
+          if (p.splits > 1) cluster_sync_all();  // all pieces have come
           met = true;
           for (int i = share * each + half; i < (share + 1) * each; i += 2) {
             const int local = i - share * each;
             const int64_t r = row0 + lane, col = int64_t(tl.n) * (p.paired ? 128 : o.block_n) + i * 32;
-            const int n = r < o.M ? int(min(int64_t(32), o.N - col)) : 0;
-            float f[32];
-            load_sums(acc + i * 32, f);
-            join32(base, row, p.splits, share, sent, local, f);
-            if constexpr (kEpi == kStore) {
-              write32<T>(p.out[0], p.out_rs[0], p.out_cs[0], r, col, n, f);
-            } else if constexpr (kEpi == kGated) {
-              float u[32];
-              load_sums(acc + 128 + i * 32, u);
-              join32(base, row, p.splits, share, sent, each + local, u);
-              if (p.save) {
-                write32<T>(p.out[1], p.out_rs[1], p.out_cs[1], r, col, n, f);
-                write32<T>(p.out[2], p.out_rs[2], p.out_cs[2], r, col, n, u);
+            const int cols = r < o.M ? int(min(int64_t(32), o.N - col)) : 0;
+#pragma unroll 1
+            for (int c = 0; c < 4; ++c) {
+              const int64_t at = col + c * 8;
+              const int n = cols - c * 8;
+              float f[8];
+              load_sums8(acc + i * 32 + c * 8, f);
+              if (p.splits > 1) join8(base, row, c, p.splits, share, sent, local, f);
+              if constexpr (kEpi == kStore) {
+                write8<T>(p.out[0], p.out_rs[0], p.out_cs[0], r, at, n, f);
+              } else if constexpr (kEpi == kGated) {
+                float u[8];
+                load_sums8(acc + 128 + i * 32 + c * 8, u);
+                if (p.splits > 1) join8(base, row, c, p.splits, share, sent, each + local, u);
+                if (p.save) {
+                  write8<T>(p.out[1], p.out_rs[1], p.out_cs[1], r, at, n, f);
+                  write8<T>(p.out[2], p.out_rs[2], p.out_cs[2], r, at, n, u);
+                }
+                gate(p.act, f, u);
+                write8<T>(p.out[0], p.out_rs[0], p.out_cs[0], r, at, n, f);
+              } else {
+                float g[8], u[8];
+                read8<T>(p.in[0], p.in_rs[0], r, at, n, g);
+                read8<T>(p.in[1], p.in_rs[1], r, at, n, u);
+                gate_backward(p.act, f, g, u);
+                write8<T>(p.out[0], p.out_rs[0], p.out_cs[0], r, at, n, g);
+                write8<T>(p.out[1], p.out_rs[1], p.out_cs[1], r, at, n, f);
+                write8<T>(p.out[2], p.out_rs[2], p.out_cs[2], r, at, n, u);
               }
-              float unused;
-#pragma unroll
-              for (int j = 0; j < 32; ++j) f[j] = activation<false>(p.act, f[j], unused) * u[j];
-              write32<T>(p.out[0], p.out_rs[0], p.out_cs[0], r, col, n, f);
-            } else {
-              float g[32], u[32];
-              read32<T>(p.in[0], p.in_rs[0], r, col, n, g);
-              read32<T>(p.in[1], p.in_rs[1], r, col, n, u);
-#pragma unroll
-              for (int j = 0; j < 32; ++j) {
-                float da;
-                const float a = activation<true>(p.act, g[j], da);
-                g[j] = f[j] * u[j] * da;
-                f[j] = f[j] * a;
-                u[j] = a * u[j];
-              }
-              write32<T>(p.out[0], p.out_rs[0], p.out_cs[0], r, col, n, g);
-              write32<T>(p.out[1], p.out_rs[1], p.out_cs[1], r, col, n, f);
-              write32<T>(p.out[2], p.out_rs[2], p.out_cs[2], r, col, n, u);
             }
           }
-          break;  // the cluster has one tile
+          break;  // there is one tile
         }
       }
       if constexpr (kEpi == kStore) {
@@ -573,9 +601,7 @@ __global__ void __launch_bounds__(kThreads, 1) cconv_pair_product_kernel(
             stage32<T>(mine + kBoxBytes, lane, c * 4, g);
             stage32<T>(mine + 2 * kBoxBytes, lane, c * 4, u);
           }
-          float unused;
-#pragma unroll
-          for (int i = 0; i < 32; ++i) g[i] = activation<false>(p.act, g[i], unused) * u[i];
+          gate(p.act, g, u);
           stage32<T>(mine, lane, c * 4, g);
         }
         fence_proxy_async_smem();
@@ -612,14 +638,7 @@ __global__ void __launch_bounds__(kThreads, 1) cconv_pair_product_kernel(
             if (j == 1 && c + 64 >= cols) release_sums();
             unstage32<T>(mine, lane, j * 4, g);
             unstage32<T>(mine + kBoxBytes, lane, j * 4, u);
-#pragma unroll
-            for (int i = 0; i < 32; ++i) {
-              float da;
-              const float a = activation<true>(p.act, g[i], da);
-              g[i] = d[i] * u[i] * da;
-              d[i] = d[i] * a;
-              u[i] = a * u[i];
-            }
+            gate_backward(p.act, d, g, u);
             stage32<T>(mine, lane, j * 4, g);
             stage32<T>(mine + kBoxBytes, lane, j * 4, d);
             stage32<T>(mine + 2 * kBoxBytes, lane, j * 4, u);
@@ -697,31 +716,46 @@ __global__ void __launch_bounds__(kThreads, 1) cconv_pair_product_kernel(
             f[2 * i + 1] = v.y;
           }
         };
-        if (p.splits > 1) {  // as above, with the sums in registers
+        auto piece8 = [&](int c, float (&f)[8]) {
+#pragma unroll
+          for (int i = 0; i < 4; ++i) {
+            const float2 v = halves_of(sum[c * 4 + i]);
+            f[2 * i] = v.x;
+            f[2 * i + 1] = v.y;
+          }
+        };
+        if (p.direct) {  // as above, with the sums in registers
           const int each = (o.block_n >> 5) / p.splits, row = q * 32 + lane, first = half * (cols >> 5);
-          cluster_sync_all();
+          if (p.splits > 1) cluster_sync_all();
 #pragma unroll
           for (int c = 0; c < 4; ++c) {
             const int i = first + c, owner = i / each;
-            if (c * 32 < cols && owner != share) {
-              float f[32];
-              piece32(c, f);
-              send32(cluster_map_shared(base, uint32_t(2 * owner) + rank) +
-                         uint32_t((share < owner ? share : share - 1) * each + i - owner * each) * kShareBytes,
-                     row, f);
+            if (p.splits > 1 && c * 32 < cols && owner != share) {
+              const uint32_t to = cluster_map_shared(base, uint32_t(2 * owner) + rank) +
+                                  uint32_t((share < owner ? share : share - 1) * each + i - owner * each) * kShareBytes;
+#pragma unroll
+              for (int e = 0; e < 4; ++e) {
+                float f[8];
+                piece8(c * 4 + e, f);
+                send8(to, row, e, f);
+              }
             }
           }
-          cluster_sync_all();
+          if (p.splits > 1) cluster_sync_all();
           met = true;
 #pragma unroll
           for (int c = 0; c < 4; ++c) {
             const int i = first + c;
             if (c * 32 < cols && i / each == share) {
-              float f[32];
-              piece32(c, f);
-              join32(base, row, p.splits, share, each, i - share * each, f);
               const int64_t r = row0 + lane, col = int64_t(tl.n) * o.block_n + i * 32;
-              write32<T>(p.out[0], p.out_rs[0], p.out_cs[0], r, col, r < o.M ? int(min(int64_t(32), o.N - col)) : 0, f);
+              const int n = r < o.M ? int(min(int64_t(32), o.N - col)) : 0;
+#pragma unroll
+              for (int e = 0; e < 4; ++e) {
+                float f[8];
+                piece8(c * 4 + e, f);
+                if (p.splits > 1) join8(base, row, e, p.splits, share, each, i - share * each, f);
+                write8<T>(p.out[0], p.out_rs[0], p.out_cs[0], r, col + e * 8, n - e * 8, f);
+              }
             }
           }
           break;
@@ -793,7 +827,7 @@ cudaError_t launch_pair(const PairMaps<kProductsOf<kEpi>>& maps, const PairParam
     __atomic_store_n(&ready[dev & 63], true, __ATOMIC_RELEASE);
   }
   const int pairs = p.splits > 1 ? p.tiles * p.splits : p.tiles < sms / 2 ? p.tiles : sms / 2;
-  const size_t smem = 1024 + size_t(p.stages) * p.stage_bytes + kEpilogueWarps * staged_pieces(kEpi) * kBoxBytes +
+  const size_t smem = 1024 + size_t(p.stages) * p.stage_bytes + kABytes - p.a_stage + kEpilogueWarps * p.pieces * kBoxBytes +
                       scale_bytes(kEpi) + kBarrierBytes;
   return launch(f, dim3(unsigned(2 * pairs)), kThreads, smem, 2 * p.splits, chained, s, maps, p);
 }
@@ -813,7 +847,7 @@ int run_as(const Launch& l, int sms, bool chained, bool more, cudaStream_t s) {
   int rc = block_status_word(&q.status);
   if (rc != CCONV_OK) return rc;
   const int es = type_bytes(l.dtype);
-  uint32_t b_most = 0;
+  uint32_t a_most = 0, b_most = 0;
   q.tiles = 0;
   q.count = l.count;
   q.splits = l.splits;
@@ -830,7 +864,10 @@ int run_as(const Launch& l, int sms, bool chained, bool more, cudaStream_t s) {
     o.kb_part = int(cdiv64(o.kb_total, l.splits));
     o.block_n = p.block_n;
     o.b_bytes = uint32_t(p.block_n / 2) * 128;
-    if (o.b_bytes > b_most) b_most = o.b_bytes;
+    o.a_bytes = uint32_t(a_rows_of(p)) * 128;
+    o.one_sided = p.M <= 128;
+    a_most = std::max(a_most, o.a_bytes);
+    b_most = std::max(b_most, o.b_bytes);
     o.a_kmajor = p.a[0].kmajor;
     o.b_kmajor = p.b[0].kmajor;
     o.a_desc = swizzled_desc(p.a[0].kmajor, 8192);
@@ -844,10 +881,10 @@ int run_as(const Launch& l, int sms, bool chained, bool more, cudaStream_t s) {
     o.M = p.M;
     o.N = p.N;
     for (int j = 0; j < 2 && rc == CCONV_OK; ++j) {
-      if (j == 0 || p.segments) rc = encode_operand(&m.a[j], p.a[j], kEight ? 1 : 2, l.dtype, 128);
+      if (j == 0 || p.segments) rc = encode_operand(&m.a[j], p.a[j], kEight ? 1 : 2, l.dtype, a_rows_of(p));
       if (rc == CCONV_OK && (j == 0 || p.segments || p.paired)) rc = encode_operand(&m.b[j], p.b[j], kEight ? 1 : 2, l.dtype, p.block_n / 2);
     }
-    if (rc == CCONV_OK && l.splits == 1) rc = encode_map(&m.out, p.out[0].p, es, l.dtype, p.N, p.M, p.out[0].rs, 128 / es, 32);
+    if (rc == CCONV_OK && !l.direct) rc = encode_map(&m.out, p.out[0].p, es, l.dtype, p.N, p.M, p.out[0].rs, 128 / es, 32);
     if (rc != CCONV_OK) return rc;
   }
   const Product& p = l.of[0];
@@ -863,13 +900,14 @@ int run_as(const Launch& l, int sms, bool chained, bool more, cudaStream_t s) {
   if constexpr (kEpi == kGated || kEpi == kGatedBackward) {
     CUtensorMap* more_maps[4] = {&maps.out1, &maps.out2, &maps.in[0], &maps.in[1]};
     const Mat* mats[4] = {&p.out[1], &p.out[2], &p.in[0], &p.in[1]};
-    for (int i = 0; i < 4 && l.splits == 1; ++i)
+    for (int i = 0; i < 4 && !l.direct; ++i)
       if (mats[i]->p && (rc = encode_map(more_maps[i], mats[i]->p, es, l.dtype, p.N, p.M, mats[i]->rs, 64, 32))) return rc;
   }
-  q.stage_bytes = kABytes + b_most;
-  const uint32_t staged = kEpilogueWarps * staged_pieces(kEpi) * kBoxBytes + scale_bytes(kEpi);
-  q.stages = int((kSmemMost - 1024 - kBarrierBytes - staged) / q.stage_bytes);
-  if (q.stages > kMostStages) q.stages = kMostStages;
+  q.a_stage = a_most;
+  q.stage_bytes = a_most + b_most;
+  q.direct = l.direct;
+  q.pieces = uint32_t(pieces_of(l));
+  q.stages = stages_of(l, a_most, b_most);
   q.paired = p.paired;
   q.act = l.act;
   q.save = l.save;
@@ -889,13 +927,19 @@ int run_as(const Launch& l, int sms, bool chained, bool more, cudaStream_t s) {
   return block_cuda_error(e, "cconv_pair_product_kernel");
 }
 
-// Clocks of one product's tile: its k blocks at the slower of the tensor cores (block_n * 2 clocks a block and
-// pair) and of L2 (about 60 bytes a clock and SM while all draw), and what begins and ends it.
-double tile_clocks(const Product& p, int splits, int es) {
-  const double kb = double(cdiv64(cdiv64(p.K, 128 / es) * (p.segments ? 2 : 1), splits));
+// Clocks of one product's tile: its k blocks at the slowest of the tensor cores (block_n * 2 clocks a block and
+// pair; 8-bit sums are scaled at 1.7 times that), of L2 (about 60 bytes a clock and SM while all draw) and of
+// a ring of stages that waits for memory (3500 clocks where every tile reads rows of B of its own, which then
+// come from HBM, 1500 where others have brought them to L2); and what begins and ends it (measured: with an
+// exchange 8 us a tile, without 5 us a launch).
+double tile_clocks(const Launch& l, const Product& p) {
+  const int es = l.epilogue == kScaled ? 1 : 2;
+  const double kb = double(cdiv64(cdiv64(p.K, 128 / es) * (p.segments ? 2 : 1), l.splits));
   const double rows = double(p.M < 256 ? p.M : 256) + p.block_n;
-  const double block = std::max(2.0 * p.block_n * (es == 1 ? 1.7 : 1.0) + 30.0, rows * 128.0 / 120.0);
-  return kb * block + (splits > 1 ? 4000.0 : 600.0);
+  const double stages = stages_of(l, uint32_t(a_rows_of(p)) * 128, uint32_t(p.block_n / 2) * 128);
+  const double block = std::max({2.0 * p.block_n * (es == 1 ? 1.7 : 1.0) + 30.0, rows * 128.0 / 120.0,
+                                 (p.M <= 256 ? 3500.0 : 1500.0) / stages});
+  return kb * block + (l.splits > 1 ? 15000.0 : 600.0);
 }
 
 // Rows of `pieces` accesses of type E, both sides contiguous: 64 threads by 4 rows a block, 4 accesses a thread.
@@ -972,23 +1016,65 @@ int block_status_word(int** word) {
   return block_cuda_error(e, "cudaGetSymbolAddress");
 }
 
+namespace {
+// Clusters of 2 * splits CTAs that run at one time: GPCs whose SMs a cluster does not divide leave some over
+// (a B200 with 148 SMs: 74 of 2, 33 of 4, 15 of 8).
+int cluster_slots(int splits, int sms) {
+  static int known[64][3] = {};
+  int dev = 0;
+  const int which = splits == 1 ? 0 : splits == 2 ? 1 : 2, guess = std::max(1, sms / (2 * splits) - (splits > 1 ? 1 << which : 0));
+  if (cudaGetDevice(&dev) != cudaSuccess) return guess;
+  int n = __atomic_load_n(&known[dev & 63][which], __ATOMIC_RELAXED);
+  if (n == 0) {
+    auto f = cconv_pair_product_kernel<kStore, __nv_bfloat16>;
+    cudaLaunchConfig_t cfg = {};
+    cfg.gridDim = dim3(unsigned(2 * splits * sms));
+    cfg.blockDim = dim3(kThreads);
+    cfg.dynamicSmemBytes = kSmemMost;
+    cudaLaunchAttribute attr[1];
+    attr[0].id = cudaLaunchAttributeClusterDimension;
+    attr[0].val.clusterDim.x = unsigned(2 * splits);
+    attr[0].val.clusterDim.y = attr[0].val.clusterDim.z = 1;
+    cfg.attrs = attr;
+    cfg.numAttrs = 1;
+    if (cudaFuncSetAttribute(f, cudaFuncAttributeMaxDynamicSharedMemorySize, int(kSmemMost)) != cudaSuccess ||
+        cudaOccupancyMaxActiveClusters(&n, f, &cfg) != cudaSuccess || n <= 0) {
+      cudaGetLastError();
+      n = guess;
+    }
+    __atomic_store_n(&known[dev & 63][which], n, __ATOMIC_RELAXED);
+  }
+  return n;
+}
+}  // namespace
+
 double launch_clocks(const Launch& l, int sms) {
   const int es = l.epilogue == kScaled ? 1 : 2;
-  // clusters that run at one time: of 4 and 8 CTAs some SMs of a GPC are left over
-  const int slots = l.splits == 1 ? sms / 2 : l.splits == 2 ? sms / 4 - 1 : sms / 8 - 2;
-  double all = 0, longest = 0;
+  const int slots = cluster_slots(l.splits, sms);
+  double all = 0, longest = 0, bytes = 0;
   int64_t tiles = 0;
   for (int i = 0; i < l.count; ++i) {
     const Product& p = l.of[i];
     const int64_t n = cdiv64(p.M, 256) * cdiv64(p.N, p.paired ? 128 : p.block_n);
-    const double c = tile_clocks(p, l.splits, es);
+    const double c = tile_clocks(l, p);
     tiles += n;
     all += double(n) * c;
     longest = std::max(longest, c);
+    bytes += double(es) * (double(p.M + p.N * (p.paired ? 2 : 1)) * double(p.K) * (p.segments ? 2 : 1) + double(p.M) * double(p.N));
   }
-  if (l.count == 1) return double(cdiv64(tiles, slots)) * longest + 5000.0;
-  return std::max(longest, all / slots + 0.5 * longest) + 5000.0;
+  const double least = bytes / 3500.0;  // HBM, per clock
+  if (l.count == 1) return std::max(least, double(cdiv64(tiles, slots)) * longest) + (l.splits > 1 ? 0.0 : 9000.0);
+  return std::max(least, std::max(longest, all / slots + 0.5 * longest)) + 9000.0;
 }
+
+namespace {
+void cut(Launch* l, int block_n, int splits) {
+  Product& p = l->of[0];
+  p.block_n = block_n;
+  l->splits = splits;
+  l->direct = splits > 1;
+}
+}  // namespace
 
 void choose_cut(Launch* l, int sms, bool few_columns) {
   Product& p = l->of[0];
@@ -1002,14 +1088,12 @@ void choose_cut(Launch* l, int sms, bool few_columns) {
     for (int s = 1; s <= 4; s *= 2) {
       if (s > 1 && (s - 1) * cdiv64(kb, s) >= kb) continue;      // every pair has a part
       if ((p.paired ? 128 : n) / 32 < s) continue;                // and 32 columns to finish
-      p.block_n = n;
-      l->splits = s;
+      cut(l, n, s);
       const double c = launch_clocks(*l, sms);
       if (best_n == 0 || c < best) best = c, best_n = n, best_s = s;
     }
   }
-  p.block_n = best_n;
-  l->splits = best_s;
+  cut(l, best_n, best_s);
 }
 
 int run_products(const Launch& l, int sms, bool chained, bool more, cudaStream_t s) {
