@@ -31,15 +31,20 @@ EXPORTS = (
     "cconv_fp8_product_workspace", "cconv_fp8_product", "cconv_quantize_blocks", "cconv_block_status",
 )
 
-# The argument structures of the C ABI, field for field (P: address, q: 64-bit, i: 32-bit, f: float).
+# The argument structures of the C ABI, field for field (P: address, q: 64-bit, i: 32-bit, f: float), without
+# the workspace's address and size that end all but the last.
 _MAT = "Pqq"
-_FFN = struct.Struct("qqqii" + _MAT * 12 + "PQ")
-_NORM = struct.Struct("qqiffxxxxq" + _MAT * 3 + "PP" + _MAT * 7 + "PPPQ")
-_FP8 = struct.Struct("qqqii" + _MAT * 5 + "PQ")
+_FFN = struct.Struct("qqqii" + _MAT * 12)
+_NORM = struct.Struct("qqiffxxxxq" + _MAT * 3 + "PP" + _MAT * 7 + "PP")
+_FP8 = struct.Struct("qqqii" + _MAT * 5)
 _QUANT = struct.Struct("qqii" + _MAT * 3)
+_SPACE = struct.Struct("PQ")
+_NO_SPACE = _SPACE.pack(0, 0)
 _NONE = (0, 0, 0)
 
 _fn = {}
+_current_device = torch._C._cuda_getDevice
+_current_stream = torch._C._cuda_getCurrentRawStream
 
 
 def _f(name):
@@ -57,95 +62,103 @@ def _f(name):
     return f
 
 
-def _mat(t, shape, dtype, device, name):
-    """(address, row stride, column stride) of a matrix operand, checked."""
-    if t.shape != shape or t.dtype is not dtype or t.device != device:
-        raise ValueError(f"{name} must be a {dtype} tensor of shape {tuple(shape)} on {device}, "
+def _mat(t, shape, dtype, dev, name):
+    """(address, row stride, column stride) of a matrix operand, checked; dev: the device's index."""
+    if t.dtype is not dtype or t.get_device() != dev or t.shape != shape:
+        raise ValueError(f"{name} must be a {dtype} tensor of shape {tuple(shape)} on cuda:{dev}, "
                          f"got {t.dtype} {tuple(t.shape)} on {t.device}")
-    return (t.data_ptr(), *t.stride())
+    rows, cols = t.stride()
+    return t.data_ptr(), rows, cols
 
 
-def _row(t, shape, dtype, device, name):
+def _row(t, shape, dtype, dev, name):
     """As _mat, of a matrix whose rows are contiguous."""
-    m = _mat(t, shape, dtype, device, name)
+    m = _mat(t, shape, dtype, dev, name)
     if m[2] != 1 and shape[1] > 1:
         raise ValueError(f"{name} must have contiguous rows, got strides {t.stride()}")
     return m
 
 
-def _vec(t, n, dtype, device, name):
+def _vec(t, n, dtype, dev, name):
     """Address of a vector operand (0: absent), checked."""
     if t is None:
         return 0
-    if t.shape != (n,) or t.dtype is not dtype or t.device != device or (n > 1 and t.stride(0) != 1):
-        raise ValueError(f"{name} must be a contiguous {dtype} tensor of shape {(n,)} on {device}, "
+    if t.dtype is not dtype or t.get_device() != dev or t.shape != (n,) or (n > 1 and t.stride(0) != 1):
+        raise ValueError(f"{name} must be a contiguous {dtype} tensor of shape {(n,)} on cuda:{dev}, "
                          f"got {t.dtype} {tuple(t.shape)} on {t.device}")
     return t.data_ptr()
 
 
 def _type(t, name, allowed=_TYPES):
-    if t.device.type != "cuda":
+    """(type code, device index) of a matrix that gives a call its type and device."""
+    dev = t.get_device()
+    if dev < 0:
         raise ValueError(f"{name} must be a CUDA tensor")
     ty = allowed.get(t.dtype)
     if ty is None:
         raise ValueError(f"{name} has type {t.dtype}; supported: {', '.join(str(d) for d in allowed)}")
     if t.dim() != 2:
         raise ValueError(f"{name} must be a matrix, got shape {tuple(t.shape)}")
-    return ty
+    return ty, dev
 
 
 _HALF_TYPES = {torch.bfloat16: TYPE_BF16, torch.float16: TYPE_FP16}
 
 
-def _call(name, args, device, stream):
-    """Runs the entry point on ``stream``, with the operands' device current."""
-    index = device.index
-    raw = torch._C._cuda_getCurrentRawStream(index) if stream is None else stream.cuda_stream
-    if torch.cuda.current_device() == index:
-        rc = _f(name)(args, raw)
+def _need(name, args, dev):
+    """Bytes of workspace of the call with these arguments."""
+    f = _fn.get(name) or _f(name)
+    if _current_device() == dev:
+        n = f(args + _NO_SPACE)
     else:
-        with torch.cuda.device(index):
-            rc = _f(name)(args, raw)
-    if rc != OK:
-        raise CconvError(rc, name)
-
-
-def _need(name, args, device):
-    if torch.cuda.current_device() == device.index:
-        n = _f(name)(args)
-    else:
-        with torch.cuda.device(device):
-            n = _f(name)(args)
+        with torch.cuda.device(dev):
+            n = f(args + _NO_SPACE)
     if n < 0:
         raise CconvError(n, name)
     return n
 
 
-def _space(nbytes, workspace, device, stream):
-    """(address, bytes, tensor to keep until the call is made) of the workspace."""
-    if workspace is not None:
-        if workspace.device != device or not workspace.is_contiguous():
-            raise ValueError(f"workspace must be a contiguous tensor on {device}")
-        return workspace.data_ptr(), workspace.numel() * workspace.element_size(), workspace
-    if nbytes == 0:
-        return 0, 0, None
-    if stream is None:
-        w = torch.empty(nbytes, dtype=torch.uint8, device=device)
+def _call(name, args, dev, stream):
+    """Runs the entry point on ``stream``, with the operands' device current."""
+    f = _fn.get(name) or _f(name)
+    raw = _current_stream(dev) if stream is None else stream.cuda_stream
+    if _current_device() == dev:
+        rc = f(args, raw)
     else:
-        with torch.cuda.stream(stream):  # memory of that stream: it is reused in its order
-            w = torch.empty(nbytes, dtype=torch.uint8, device=device)
-    return w.data_ptr(), nbytes, w
+        with torch.cuda.device(dev):
+            rc = f(args, raw)
+    if rc != OK:
+        raise CconvError(rc, name)
+
+
+def _call_with_space(name, need, args, dev, workspace, stream):
+    """_call with a workspace: the caller's, or one from torch's allocator (which reuses the memory in the
+    order of the stream that it was taken on)."""
+    if workspace is not None:
+        if workspace.get_device() != dev or not workspace.is_contiguous():
+            raise ValueError(f"workspace must be a contiguous tensor on cuda:{dev}")
+        _call(name, args + _SPACE.pack(workspace.data_ptr(), workspace.numel() * workspace.element_size()), dev, stream)
+        return
+    n = _need(need, args, dev)
+    if n == 0:
+        _call(name, args + _NO_SPACE, dev, stream)
+        return
+    if stream is None:
+        w = torch.empty(n, dtype=torch.uint8, device=dev)
+    else:
+        with torch.cuda.stream(stream):
+            w = torch.empty(n, dtype=torch.uint8, device=dev)
+    _call(name, args + _SPACE.pack(w.data_ptr(), n), dev, stream)
 
 
 # ---- gated feed-forward block ---------------------------------------------------------------------
 
 def _ffn_common(x, w_gate, w_up, w_down):
-    dtype = _type(x, "x", _HALF_TYPES)
+    dtype, dev = _type(x, "x", _HALF_TYPES)
     T, D = x.shape
     if w_gate.dim() != 2:
         raise ValueError(f"w_gate must be a matrix, got shape {tuple(w_gate.shape)}")
-    F = w_gate.shape[0]
-    dt, dev = x.dtype, x.device
+    F, dt = w_gate.shape[0], x.dtype
     mats = (x.data_ptr(), *x.stride(), *_mat(w_gate, (F, D), dt, dev, "w_gate"), *_mat(w_up, (F, D), dt, dev, "w_up"),
             *_mat(w_down, (D, F), dt, dev, "w_down"))
     return T, D, F, dtype, dt, dev, mats
@@ -158,13 +171,13 @@ def _ffn_forward_args(x, w_gate, w_up, w_down, out, act, gate_pre, up_pre):
     pre = _NONE + _NONE
     if gate_pre is not None:
         pre = _mat(gate_pre, (T, F), dt, dev, "gate_pre") + _mat(up_pre, (T, F), dt, dev, "up_pre")
-    return (T, D, F, dtype, act, *mats, *pre, *_mat(out, (T, D), dt, dev, "out"), *(_NONE * 5)), dev
+    return _FFN.pack(T, D, F, dtype, act, *mats, *pre, *_mat(out, (T, D), dt, dev, "out"), *(_NONE * 5)), dev
 
 
 def ffn_forward_workspace(x, w_gate, w_up, w_down, out, act=ACT_SILU, gate_pre=None, up_pre=None):
     """cconv_ffn_forward_workspace: bytes of workspace of the call with these tensors."""
     args, dev = _ffn_forward_args(x, w_gate, w_up, w_down, out, act, gate_pre, up_pre)
-    return _need("cconv_ffn_forward_workspace", _FFN.pack(*args, 0, 0), dev)
+    return _need("cconv_ffn_forward_workspace", args, dev)
 
 
 def ffn_forward(x, w_gate, w_up, w_down, out, act=ACT_SILU, gate_pre=None, up_pre=None, workspace=None, stream=None):
@@ -173,15 +186,13 @@ def ffn_forward(x, w_gate, w_up, w_down, out, act=ACT_SILU, gate_pre=None, up_pr
     x, out [T, D]; w_gate, w_up [F, D]; w_down [D, F]; bf16 or fp16, any strides.  Given ``gate_pre`` and
     ``up_pre`` [T, F], the pre-activations are written there for ffn_backward."""
     args, dev = _ffn_forward_args(x, w_gate, w_up, w_down, out, act, gate_pre, up_pre)
-    need = _need("cconv_ffn_forward_workspace", _FFN.pack(*args, 0, 0), dev) if workspace is None else 0
-    at, size, _keep = _space(need, workspace, dev, stream)
-    _call("cconv_ffn_forward", _FFN.pack(*args, at, size), dev, stream)
+    _call_with_space("cconv_ffn_forward", "cconv_ffn_forward_workspace", args, dev, workspace, stream)
     return out
 
 
 def _ffn_backward_args(dout, x, w_gate, w_up, w_down, gate_pre, up_pre, dx, dw_gate, dw_up, dw_down, act):
     T, D, F, dtype, dt, dev, mats = _ffn_common(x, w_gate, w_up, w_down)
-    return (T, D, F, dtype, act, *mats, *_mat(gate_pre, (T, F), dt, dev, "gate_pre"),
+    return _FFN.pack(T, D, F, dtype, act, *mats, *_mat(gate_pre, (T, F), dt, dev, "gate_pre"),
             *_mat(up_pre, (T, F), dt, dev, "up_pre"), *_NONE, *_mat(dout, (T, D), dt, dev, "dout"),
             *_mat(dx, (T, D), dt, dev, "dx"), *_mat(dw_gate, (F, D), dt, dev, "dw_gate"),
             *_mat(dw_up, (F, D), dt, dev, "dw_up"), *_mat(dw_down, (D, F), dt, dev, "dw_down")), dev
@@ -190,7 +201,7 @@ def _ffn_backward_args(dout, x, w_gate, w_up, w_down, gate_pre, up_pre, dx, dw_g
 def ffn_backward_workspace(dout, x, w_gate, w_up, w_down, gate_pre, up_pre, dx, dw_gate, dw_up, dw_down, act=ACT_SILU):
     """cconv_ffn_backward_workspace: bytes of workspace of the call with these tensors."""
     args, dev = _ffn_backward_args(dout, x, w_gate, w_up, w_down, gate_pre, up_pre, dx, dw_gate, dw_up, dw_down, act)
-    return _need("cconv_ffn_backward_workspace", _FFN.pack(*args, 0, 0), dev)
+    return _need("cconv_ffn_backward_workspace", args, dev)
 
 
 def ffn_backward(dout, x, w_gate, w_up, w_down, gate_pre, up_pre, dx, dw_gate, dw_up, dw_down, act=ACT_SILU,
@@ -198,9 +209,7 @@ def ffn_backward(dout, x, w_gate, w_up, w_down, gate_pre, up_pre, dx, dw_gate, d
     """cconv_ffn_backward: the gradients dx, dw_gate, dw_up, dw_down (all written) for dout = dL/dy and
     the pre-activations that ffn_forward saved."""
     args, dev = _ffn_backward_args(dout, x, w_gate, w_up, w_down, gate_pre, up_pre, dx, dw_gate, dw_up, dw_down, act)
-    need = _need("cconv_ffn_backward_workspace", _FFN.pack(*args, 0, 0), dev) if workspace is None else 0
-    at, size, _keep = _space(need, workspace, dev, stream)
-    _call("cconv_ffn_backward", _FFN.pack(*args, at, size), dev, stream)
+    _call_with_space("cconv_ffn_backward", "cconv_ffn_backward_workspace", args, dev, workspace, stream)
     return dx, dw_gate, dw_up, dw_down
 
 
@@ -222,31 +231,29 @@ def residual_norm_forward(resid, resid_out, norm_out=None, block=None, w_post=No
     residual is scaled; without ``w_post`` the block is not normed; without ``gate`` it counts in full;
     without ``norm_out`` there is no second norm.  ``gate`` [ceil(T / rows_per_gate), D] has a row for
     each ``rows_per_gate`` tokens (0: one row for all).  ``resid_out`` may be ``resid``."""
-    dtype = _type(resid, "resid")
-    T, D = resid.shape
-    dt, dev = resid.dtype, resid.device
-    shape = (T, D)
+    dtype, dev = _type(resid, "resid")
+    shape = T, D = resid.shape
+    dt = resid.dtype
     args = _NORM.pack(
         T, D, dtype, scale, eps, rows_per_gate, *_row(resid, shape, dt, dev, "resid"),
         *(_NONE if block is None else _row(block, shape, dt, dev, "block")),
         *_gate(gate, T, D, rows_per_gate, dt, dev, "gate"), _vec(w_post, D, dt, dev, "w_post"),
         _vec(w_pre, D, dt, dev, "w_pre"), *_row(resid_out, shape, dt, dev, "resid_out"),
         *(_NONE if norm_out is None else _row(norm_out, shape, dt, dev, "norm_out")),
-        0, 0, 0, 0, 0, 0, 0, 0, 0, 0, 0, 0, 0, 0, 0, 0, 0, 0, 0)
-    _call("cconv_residual_norm_forward", args, dev, stream)
+        0, 0, 0, 0, 0, 0, 0, 0, 0, 0, 0, 0, 0, 0, 0, 0, 0)
+    _call("cconv_residual_norm_forward", args + _NO_SPACE, dev, stream)
     return resid_out, norm_out
 
 
 def _norm_backward_args(dresid_out, dnorm_out, resid_out, dresid, block, dblock, w_post, dw_post, gate, dgate, w_pre,
                         dw_pre, rows_per_gate, scale, eps):
-    dtype = _type(dresid, "dresid")
-    T, D = dresid.shape
-    dt, dev = dresid.dtype, dresid.device
-    shape = (T, D)
+    dtype, dev = _type(dresid, "dresid")
+    shape = T, D = dresid.shape
+    dt = dresid.dtype
 
     def opt(t, name):
         return _NONE if t is None else _row(t, shape, dt, dev, name)
-    return (T, D, dtype, scale, eps, rows_per_gate, *_NONE, *opt(block, "block"),
+    return _NORM.pack(T, D, dtype, scale, eps, rows_per_gate, *_NONE, *opt(block, "block"),
             *_gate(gate, T, D, rows_per_gate, dt, dev, "gate"), _vec(w_post, D, dt, dev, "w_post"),
             _vec(w_pre, D, dt, dev, "w_pre"), *opt(resid_out, "resid_out"), *_NONE, *opt(dresid_out, "dresid_out"),
             *opt(dnorm_out, "dnorm_out"), *_row(dresid, shape, dt, dev, "dresid"), *opt(dblock, "dblock"),
@@ -260,7 +267,7 @@ def residual_norm_backward_workspace(dresid_out, dnorm_out, resid_out, dresid, b
     """cconv_residual_norm_backward_workspace: bytes of workspace of the call with these tensors."""
     args, dev = _norm_backward_args(dresid_out, dnorm_out, resid_out, dresid, block, dblock, w_post, dw_post, gate,
                                     dgate, w_pre, dw_pre, rows_per_gate, scale, eps)
-    return _need("cconv_residual_norm_backward_workspace", _NORM.pack(*args, 0, 0), dev)
+    return _need("cconv_residual_norm_backward_workspace", args, dev)
 
 
 def residual_norm_backward(dresid_out, dnorm_out, resid_out, dresid, block=None, dblock=None, w_post=None, dw_post=None,
@@ -274,24 +281,20 @@ def residual_norm_backward(dresid_out, dnorm_out, resid_out, dresid, block=None,
     ``dresid`` may be ``dresid_out``."""
     args, dev = _norm_backward_args(dresid_out, dnorm_out, resid_out, dresid, block, dblock, w_post, dw_post, gate,
                                     dgate, w_pre, dw_pre, rows_per_gate, scale, eps)
-    need = 0
-    if workspace is None:
-        need = _need("cconv_residual_norm_backward_workspace", _NORM.pack(*args, 0, 0), dev)
-    at, size, _keep = _space(need, workspace, dev, stream)
-    _call("cconv_residual_norm_backward", _NORM.pack(*args, at, size), dev, stream)
+    _call_with_space("cconv_residual_norm_backward", "cconv_residual_norm_backward_workspace", args, dev, workspace, stream)
     return dresid, dblock, dw_post, dgate, dw_pre
 
 
 # ---- 8-bit product and quantisation -----------------------------------------------------------------
 
 def _fp8_args(a, a_scale, b, b_scale, out):
-    dtype = _type(out, "out")
+    dtype, dev = _type(out, "out")
     M, N = out.shape
     if a.dim() != 2:
         raise ValueError(f"a must be a matrix, got shape {tuple(a.shape)}")
-    K, dev, e4m3, f32 = a.shape[1], out.device, torch.float8_e4m3fn, torch.float32
+    K, e4m3, f32 = a.shape[1], torch.float8_e4m3fn, torch.float32
     kb = (K + 127) // 128
-    return (M, N, K, dtype, 0, *_mat(a, (M, K), e4m3, dev, "a"), *_mat(b, (N, K), e4m3, dev, "b"),
+    return _FP8.pack(M, N, K, dtype, 0, *_mat(a, (M, K), e4m3, dev, "a"), *_mat(b, (N, K), e4m3, dev, "b"),
             *_mat(a_scale, (M, kb), f32, dev, "a_scale"), *_mat(b_scale, ((N + 127) // 128, kb), f32, dev, "b_scale"),
             out.data_ptr(), *out.stride()), dev
 
@@ -299,7 +302,7 @@ def _fp8_args(a, a_scale, b, b_scale, out):
 def fp8_product_workspace(a, a_scale, b, b_scale, out):
     """cconv_fp8_product_workspace: bytes of workspace of the call with these tensors."""
     args, dev = _fp8_args(a, a_scale, b, b_scale, out)
-    return _need("cconv_fp8_product_workspace", _FP8.pack(*args, 0, 0), dev)
+    return _need("cconv_fp8_product_workspace", args, dev)
 
 
 def fp8_product(a, a_scale, b, b_scale, out, workspace=None, stream=None):
@@ -308,18 +311,15 @@ def fp8_product(a, a_scale, b, b_scale, out, workspace=None, stream=None):
     a [M, K], b [N, K] float8_e4m3fn; a_scale [M, ceil(K/128)], b_scale [ceil(N/128), ceil(K/128)] fp32;
     out [M, N] bf16, fp16 or fp32; any strides."""
     args, dev = _fp8_args(a, a_scale, b, b_scale, out)
-    need = _need("cconv_fp8_product_workspace", _FP8.pack(*args, 0, 0), dev) if workspace is None else 0
-    at, size, _keep = _space(need, workspace, dev, stream)
-    _call("cconv_fp8_product", _FP8.pack(*args, at, size), dev, stream)
+    _call_with_space("cconv_fp8_product", "cconv_fp8_product_workspace", args, dev, workspace, stream)
     return out
 
 
 def quantize_blocks(x, q, scale, block_rows=1, stream=None):
     """cconv_quantize_blocks: q = x / scale in float8_e4m3fn, scale = max|x| / 448 of each block of
     ``block_rows`` (1 or 128) x 128 elements, fp32 [ceil(T/block_rows), ceil(D/128)]."""
-    dtype = _type(x, "x")
+    dtype, dev = _type(x, "x")
     T, D = x.shape
-    dev = x.device
     if block_rows not in (1, 128):
         raise ValueError(f"block_rows must be 1 or 128, got {block_rows}")
     args = _QUANT.pack(T, D, dtype, block_rows, x.data_ptr(), *x.stride(), *_mat(q, (T, D), torch.float8_e4m3fn, dev, "q"),

@@ -72,6 +72,18 @@ class Operands {
     }
     push({static_cast<const char*>(p), static_cast<const char*>(p) + need, 0, 0}, true);
   }
+  // Tells the stream's bookkeeping that a call with these operands is under way: its kernels wait for the work
+  // in front of them, but let the next be put in place, so that a convolution whose arrays meet these (their
+  // hulls, which may take in more) has to wait for it too.
+  void note(void* stream, int sms) const {
+    CallSpans c;
+    for (int i = 0; i < n_; ++i) {
+      Span& s = written_[i] ? c.out : c.image;
+      if (!s.lo || range_[i].lo < s.lo) s.lo = range_[i].lo;
+      if (!s.hi || range_[i].hi > s.hi) s.hi = range_[i].hi;
+    }
+    note_call(stream, c, Overlap::kInputsEarly, sms);
+  }
   // No output meets another output or an input; `same` names a pair that may be one matrix.
   bool distinct(const void* same_in = nullptr, const void* same_out = nullptr) const {
     for (int i = 0; i < n_; ++i)
@@ -255,7 +267,7 @@ int cconv_ffn_forward(const cconv_ffn_args* args, void* cuda_stream) {
   if (sms < 0) return sms;
   o.workspace(a.workspace, a.workspace_bytes, ffn_empty(a) ? 0 : ffn_workspace(a, false, sms));
   if (!o.distinct()) return CCONV_EINVAL;
-  note_ordinary_launch(cuda_stream);
+  o.note(cuda_stream, sms);
   cudaStream_t s = static_cast<cudaStream_t>(cuda_stream);
   return ffn_empty(a) ? ffn_zeros(a, false, s) : run_ffn(a, false, sms, s);
 }
@@ -280,7 +292,7 @@ int cconv_ffn_backward(const cconv_ffn_args* args, void* cuda_stream) {
   if (sms < 0) return sms;
   o.workspace(a.workspace, a.workspace_bytes, ffn_empty(a) ? 0 : ffn_workspace(a, true, sms));
   if (!o.distinct()) return CCONV_EINVAL;
-  note_ordinary_launch(cuda_stream);
+  o.note(cuda_stream, sms);
   cudaStream_t s = static_cast<cudaStream_t>(cuda_stream);
   return ffn_empty(a) ? ffn_zeros(a, true, s) : run_ffn(a, true, sms, s);
 }
@@ -317,7 +329,7 @@ int cconv_residual_norm_forward(const cconv_residual_norm_args* args, void* cuda
   const int sms = block_sm_count();
   if (sms < 0) return sms;
   if (a.T == 0 || a.D == 0) return CCONV_OK;
-  note_ordinary_launch(cuda_stream);
+  o.note(cuda_stream, sms);
   return block_cuda_error(run_norm_forward(norm_params(a), a.dtype, sms, static_cast<cudaStream_t>(cuda_stream)),
                           "cconv_residual_norm_forward");
 }
@@ -363,7 +375,7 @@ int cconv_residual_norm_backward(const cconv_residual_norm_args* args, void* cud
   if (!o.distinct(same ? a.dresid_out.data : nullptr, a.dresid.data)) return CCONV_EINVAL;
   if (a.D == 0) return CCONV_OK;
   cudaStream_t s = static_cast<cudaStream_t>(cuda_stream);
-  note_ordinary_launch(cuda_stream);
+  o.note(cuda_stream, sms);
   if (a.T == 0) {
     if (a.dgate.data) BLOCK_CUDA(zero_out(a.dgate, gate_rows(a), a.D, es, s));
     if (a.dw_post) BLOCK_CUDA(cudaMemsetAsync(a.dw_post, 0, size_t(a.D * es), s));
@@ -402,7 +414,7 @@ int cconv_fp8_product(const cconv_fp8_product_args* args, void* cuda_stream) {
   o.workspace(a.workspace, a.workspace_bytes, fp8_empty(a) ? 0 : fp8_workspace(a, sms));
   if (!o.distinct()) return CCONV_EINVAL;
   cudaStream_t s = static_cast<cudaStream_t>(cuda_stream);
-  note_ordinary_launch(cuda_stream);
+  o.note(cuda_stream, sms);
   if (fp8_empty(a)) return block_cuda_error(zero_out(a.c, a.M, a.N, es, s), "cconv_fp8_product");
   return run_fp8(a, sms, s);
 }
@@ -427,7 +439,7 @@ int cconv_quantize_blocks(const cconv_quantize_args* args, void* cuda_stream) {
   p.x = a.x.data; p.x_rs = a.x.row_stride; p.x_cs = a.x.col_stride;
   p.q = static_cast<uint8_t*>(a.q.data); p.q_rs = a.q.row_stride; p.q_cs = a.q.col_stride;
   p.scale = static_cast<float*>(a.scale.data); p.scale_rs = a.scale.row_stride; p.scale_cs = a.scale.col_stride;
-  note_ordinary_launch(cuda_stream);
+  o.note(cuda_stream, sms);
   return block_cuda_error(run_quantize(p, a.dtype, a.block_rows, sms, static_cast<cudaStream_t>(cuda_stream)),
                           "cconv_quantize_blocks");
 }

@@ -23,6 +23,14 @@ __device__ __forceinline__ __half from_f32<__half>(float v) { return __float2hal
 template <>
 __device__ __forceinline__ float from_f32<float>(float v) { return v; }
 
+// Every kernel of the sub-block is launched so that it may start while the kernel in front of it on its
+// stream still runs, and begins with this: it touches memory only once that kernel is complete (which had
+// waited for the one before it), and lets the next one be put in place.
+__device__ __forceinline__ void start_in_order() {
+  asm volatile("griddepcontrol.wait;" ::: "memory");
+  asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
+}
+
 // Two neighbouring elements of a 16-bit type as one 32-bit word (the first in the low half).
 template <typename T>
 __device__ __forceinline__ uint32_t pack2(float lo, float hi);

@@ -1,4 +1,4 @@
-// Products of at most 16 tokens: the weights are read once, straight into the registers that multiply them.
+// Products of at most 8 tokens: the weights are read once, straight into the registers that multiply them.
 //
 // What bounds them is HBM (a token costs 2 flops a weight), so the kernels are made of loads in flight: a
 // tile is 16 rows of weights (8 of each matrix of the gated pair, or 8 of one where 16 would leave SMs
@@ -61,25 +61,21 @@ struct FewParams {
   const char *x, *w0, *w1;        // tokens; weights (w1: the second matrix of a pair)
   int64_t x_rs, w0_rs, w1_rs;     // bytes
   int64_t k_bytes, N;
-  int T, act, more;
+  int T, act, weights_there;
   Mat out, gate_pre, up_pre;
   const float *sa, *sb;
   int64_t sa_rs, sa_ks, sb_rs, sb_ks;
   int out_dtype;
 };
 
-// Sums of the block's warps: element (row r, token t) of the 16 x 8 B tile.
-template <int B>
-__device__ __forceinline__ void gather(float (*smem)[B * 128], const float (&acc)[B][4], int warp, int lane) {
+// Sums of the block's warps: element (row r, token t) of the 16 x 8 tile.
+__device__ __forceinline__ void gather(float (*smem)[128], const float (&acc)[4], int warp, int lane) {
 #pragma unroll
-  for (int b = 0; b < B; ++b)
-#pragma unroll
-    for (int i = 0; i < 4; ++i) smem[warp][b * 128 + i * 32 + lane] = acc[b][i];
+  for (int i = 0; i < 4; ++i) smem[warp][i * 32 + lane] = acc[i];
   __syncthreads();
 }
-template <int B>
-__device__ __forceinline__ float gathered(float (*smem)[B * 128], int r, int t) {
-  const int at = (t >> 3) * 128 + ((r >> 3) * 2 + (t & 1)) * 32 + (r & 7) * 4 + ((t & 7) >> 1);
+__device__ __forceinline__ float gathered(float (*smem)[128], int r, int t) {
+  const int at = ((r >> 3) * 2 + (t & 1)) * 32 + (r & 7) * 4 + (t >> 1);
   float s = 0.0f;
 #pragma unroll
   for (int w = 0; w < kWarps; ++w) s += smem[w][at];
@@ -100,9 +96,9 @@ enum Rows { kPair, kSixteen, kEight };
 // A block's tiles are blockIdx.x, blockIdx.x + gridDim.x, ...; every warp takes the same number of batches of
 // each.  A step is 64 bytes of k a row (32 elements of 16 bits, or 64 of 8, two of which make a block that
 // shares a scale); a batch is 8 loads a lane.
-template <typename T, Rows kRows, int B>
+template <typename T, Rows kRows>
 __global__ void __launch_bounds__(kWarps * 32, 2) cconv_few_kernel(const FewParams p) {
-  __shared__ float smem[2][kWarps][B * 128];
+  __shared__ float smem[2][kWarps][128];
   constexpr bool kFp8 = std::is_same<T, E4m3>::value;
   constexpr int kSteps = kRows == kEight ? 8 : 4, kHalf = kRows == kEight ? 1 : 2;
   constexpr int kTile = kRows == kSixteen ? 16 : 8;
@@ -134,70 +130,64 @@ __global__ void __launch_bounds__(kWarps * 32, 2) cconv_few_kernel(const FewPara
     if (++lb == batches) lb = 0, lt += gridDim.x;
   };
 
-  load(w[0]);
-  // the weights were there before this call; the tokens may come from the kernel in front
-  asm volatile("griddepcontrol.wait;" ::: "memory");
-  if (p.more) asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
+  // Behind a kernel of the same call, which had waited for everything before the call, the weights are there
+  // already, and only the tokens may still be on their way.
+  if (p.weights_there) load(w[0]);
+  start_in_order();
+  if (!p.weights_there) load(w[0]);
 
-  float acc[B][4] = {};
+  float acc[4] = {};
   int tile = blockIdx.x, batch = 0, parity = 0;
   auto use = [&](const uint4 (&a)[8]) {
     const int sb = s0 + batch * kSteps;
+    const char* x = p.x + min(g, p.T - 1) * p.x_rs + q * 16;
+    uint4 v[kSteps];
 #pragma unroll
-    for (int b = 0; b < B; ++b) {
-      const int t = b * 8 + g;
-      const char* x = p.x + min(t, p.T - 1) * p.x_rs + q * 16;
-      uint4 v[kSteps];
+    for (int i = 0; i < kSteps; ++i) {
+      const int64_t at = int64_t(sb + i) * 64;
+      v[i] = g < p.T && sb + i < s1 && at + q * 16 < p.k_bytes ? load_tokens(x + at) : none;
+    }
+    if constexpr (!kFp8) {
 #pragma unroll
       for (int i = 0; i < kSteps; ++i) {
-        const int64_t at = int64_t(sb + i) * 64;
-        v[i] = t < p.T && sb + i < s1 && at + q * 16 < p.k_bytes ? load_tokens(x + at) : none;
+        const uint4 a0 = a[i * kHalf], a1 = kHalf == 2 ? a[i * kHalf + kHalf - 1] : none;
+        mma<T>(acc, a0.x, a1.x, a0.y, a1.y, v[i].x, v[i].y);
+        mma<T>(acc, a0.z, a1.z, a0.w, a1.w, v[i].z, v[i].w);
       }
-      if constexpr (!kFp8) {
+    } else {
+      // the sums of a block of 128 are scaled before they are added up; the rows of a tile share their scale
+      const int64_t nb = int64_t(tile) * kTile >> 7;
+      const int t0 = min(2 * q, p.T - 1), t1 = min(2 * q + 1, p.T - 1);  // the tokens whose sums this lane holds
 #pragma unroll
-        for (int i = 0; i < kSteps; ++i) {
-          const uint4 a0 = a[i * kHalf], a1 = kHalf == 2 ? a[i * kHalf + kHalf - 1] : none;
-          mma<T>(acc[b], a0.x, a1.x, a0.y, a1.y, v[i].x, v[i].y);
-          mma<T>(acc[b], a0.z, a1.z, a0.w, a1.w, v[i].z, v[i].w);
-        }
-      } else {
-        // the sums of a block of 128 are scaled before they are added up; the rows of a tile share their scale
-        const int64_t nb = int64_t(tile) * kTile >> 7;
-        const int t0 = min(b * 8 + 2 * q, p.T - 1), t1 = min(b * 8 + 2 * q + 1, p.T - 1);
+      for (int j = 0; j < kSteps / 2; ++j) {
+        if (sb + 2 * j < s1) {
+          const int64_t kb = (sb >> 1) + j;
+          const float s = p.sb[nb * p.sb_rs + kb * p.sb_ks];
+          const float sa0 = s * p.sa[t0 * p.sa_rs + kb * p.sa_ks], sa1 = s * p.sa[t1 * p.sa_rs + kb * p.sa_ks];
+          float d[4] = {};
 #pragma unroll
-        for (int j = 0; j < kSteps / 2; ++j) {
-          if (sb + 2 * j < s1) {
-            const int64_t kb = (sb >> 1) + j;
-            const float s = p.sb[nb * p.sb_rs + kb * p.sb_ks];
-            const float sa0 = s * p.sa[t0 * p.sa_rs + kb * p.sa_ks], sa1 = s * p.sa[t1 * p.sa_rs + kb * p.sa_ks];
-            float d[4] = {};
-#pragma unroll
-            for (int i = 2 * j; i < 2 * j + 2; ++i) {
-              const uint4 a0 = a[i * kHalf], a1 = kHalf == 2 ? a[i * kHalf + kHalf - 1] : none;
-              mma<T>(d, a0.x, a1.x, a0.y, a1.y, v[i].x, v[i].y);
-              mma<T>(d, a0.z, a1.z, a0.w, a1.w, v[i].z, v[i].w);
-            }
-            acc[b][0] += sa0 * d[0];
-            acc[b][1] += sa1 * d[1];
-            acc[b][2] += sa0 * d[2];
-            acc[b][3] += sa1 * d[3];
+          for (int i = 2 * j; i < 2 * j + 2; ++i) {
+            const uint4 a0 = a[i * kHalf], a1 = kHalf == 2 ? a[i * kHalf + kHalf - 1] : none;
+            mma<T>(d, a0.x, a1.x, a0.y, a1.y, v[i].x, v[i].y);
+            mma<T>(d, a0.z, a1.z, a0.w, a1.w, v[i].z, v[i].w);
           }
+          acc[0] += sa0 * d[0];
+          acc[1] += sa1 * d[1];
+          acc[2] += sa0 * d[2];
+          acc[3] += sa1 * d[3];
         }
       }
     }
     if (++batch < batches) return;
     batch = 0;
-    gather<B>(smem[parity], acc, warp, lane);
-#pragma unroll
-    for (int b = 0; b < B; ++b)
-#pragma unroll
-      for (int i = 0; i < 4; ++i) acc[b][i] = 0.0f;
+    gather(smem[parity], acc, warp, lane);
+    acc[0] = acc[1] = acc[2] = acc[3] = 0.0f;
     const int64_t n0 = int64_t(tile) * kTile;
     const int r = threadIdx.x % kTile, t = threadIdx.x / kTile;
-    if (t < p.T && t < 8 * B && n0 + r < p.N) {
-      const float f = gathered<B>(smem[parity], r, t);
+    if (t < p.T && n0 + r < p.N) {
+      const float f = gathered(smem[parity], r, t);
       if constexpr (kRows == kPair) {
-        const float up = gathered<B>(smem[parity], r + 8, t);
+        const float up = gathered(smem[parity], r + 8, t);
         float h[1] = {f};
         const float u[1] = {up};
         gate(p.act, h, u);
@@ -225,16 +215,15 @@ __global__ void __launch_bounds__(kWarps * 32, 2) cconv_few_kernel(const FewPara
 }
 
 template <typename T, Rows kRows>
-cudaError_t launch_rows(const FewParams& p, int sms, bool chained, cudaStream_t s) {
+cudaError_t launch_rows(const FewParams& p, int sms, cudaStream_t s) {
   const int64_t tiles = cdiv64(p.N, kRows == kSixteen ? 16 : 8);
   const dim3 grid(unsigned(std::min<int64_t>(tiles, 2 * sms)));
-  return p.T <= 8 ? launch(cconv_few_kernel<T, kRows, 1>, grid, kWarps * 32, 0, 1, chained, s, p)
-                  : launch(cconv_few_kernel<T, kRows, 2>, grid, kWarps * 32, 0, 1, chained, s, p);
+  return launch(cconv_few_kernel<T, kRows>, grid, kWarps * 32, 0, 1, s, p);
 }
 
 template <typename T>
-cudaError_t launch_single(const FewParams& p, int sms, bool chained, cudaStream_t s) {
-  return p.N >= 32 * int64_t(sms) ? launch_rows<T, kSixteen>(p, sms, chained, s) : launch_rows<T, kEight>(p, sms, chained, s);
+cudaError_t launch_single(const FewParams& p, int sms, cudaStream_t s) {
+  return p.N >= 32 * int64_t(sms) ? launch_rows<T, kSixteen>(p, sms, s) : launch_rows<T, kEight>(p, sms, s);
 }
 
 FewParams params(const Mat& x, const Mat& w, const Mat& out, int64_t T, int64_t N, int64_t K, int es, int dtype) {
@@ -260,24 +249,23 @@ bool few_readable(const Mat& m, int64_t rows, int64_t k, int es) {
 }
 
 cudaError_t run_few_gated(const Mat& x, const Mat& wg, const Mat& wu, const Mat& gate_pre, const Mat& up_pre,
-                          const Mat& h, int64_t T, int64_t F, int64_t D, int act, int dtype, int sms, bool more, cudaStream_t s) {
+                          const Mat& h, int64_t T, int64_t F, int64_t D, int act, int dtype, int sms, cudaStream_t s) {
   FewParams p = params(x, wg, h, T, F, D, 2, dtype);
   p.w1 = static_cast<const char*>(wu.p);
   p.w1_rs = wu.rs * 2;
   p.gate_pre = gate_pre;
   p.up_pre = up_pre;
   p.act = act;
-  p.more = more;
-  return dtype == CCONV_TYPE_BF16 ? launch_rows<__nv_bfloat16, kPair>(p, sms, false, s)
-                                  : launch_rows<__half, kPair>(p, sms, false, s);
+  return dtype == CCONV_TYPE_BF16 ? launch_rows<__nv_bfloat16, kPair>(p, sms, s)
+                                  : launch_rows<__half, kPair>(p, sms, s);
 }
 
 cudaError_t run_few_product(const Mat& x, const Mat& w, const Mat& out, int64_t T, int64_t N, int64_t K, int dtype,
-                            int sms, bool chained, bool more, cudaStream_t s) {
+                            int sms, bool weights_there, cudaStream_t s) {
   FewParams p = params(x, w, out, T, N, K, 2, dtype);
-  p.more = more;
-  return dtype == CCONV_TYPE_BF16 ? launch_single<__nv_bfloat16>(p, sms, chained, s)
-                                  : launch_single<__half>(p, sms, chained, s);
+  p.weights_there = weights_there;
+  return dtype == CCONV_TYPE_BF16 ? launch_single<__nv_bfloat16>(p, sms, s)
+                                  : launch_single<__half>(p, sms, s);
 }
 
 cudaError_t run_few_fp8(const Mat& x, const Mat& w, const Mat& sa, const Mat& sb, const Mat& out, int64_t T, int64_t N,
@@ -289,7 +277,7 @@ cudaError_t run_few_fp8(const Mat& x, const Mat& w, const Mat& sa, const Mat& sb
   p.sb = static_cast<const float*>(sb.p);
   p.sb_rs = sb.rs;
   p.sb_ks = sb.cs;
-  return launch_single<E4m3>(p, sms, false, s);
+  return launch_single<E4m3>(p, sms, s);
 }
 
 }  // namespace cconv

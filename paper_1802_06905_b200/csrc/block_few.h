@@ -15,13 +15,12 @@ constexpr int64_t kFewTokens = 8;
 bool few_readable(const Mat& m, int64_t rows, int64_t k, int es);
 
 // h[t][f] = act(x[t] . wg[f]) * (x[t] . wu[f]), T <= kFewTokens; the dot products too, if asked for.
-// chained: may start while the kernel in front of it in the same call ends; more: another one follows.
 cudaError_t run_few_gated(const Mat& x, const Mat& wg, const Mat& wu, const Mat& gate_pre, const Mat& up_pre,
-                          const Mat& h, int64_t T, int64_t F, int64_t D, int act, int dtype, int sms, bool more,
+                          const Mat& h, int64_t T, int64_t F, int64_t D, int act, int dtype, int sms,
                           cudaStream_t s);
-// out[t][n] = x[t] . w[n]; w was there before the call that this launch belongs to.
+// out[t][n] = x[t] . w[n].  weights_there: a kernel of the same call is in front, which does not write w.
 cudaError_t run_few_product(const Mat& x, const Mat& w, const Mat& out, int64_t T, int64_t N, int64_t K, int dtype,
-                            int sms, bool chained, bool more, cudaStream_t s);
+                            int sms, bool weights_there, cudaStream_t s);
 // out[t][n] = sum_kb sa[t][kb] sb[n/128][kb] (x[t] . w[n])_kb of 8-bit x and w.
 cudaError_t run_few_fp8(const Mat& x, const Mat& w, const Mat& sa, const Mat& sb, const Mat& out, int64_t T, int64_t N,
                         int64_t K, int dtype, int sms, cudaStream_t s);

@@ -20,8 +20,6 @@
 namespace cconv {
 namespace {
 
-constexpr double kLaunch = 4000.0;  // clocks that another launch costs
-
 Product product(int64_t M, int64_t N, int64_t K) {
   Product p;
   p.M = M;
@@ -51,8 +49,8 @@ void forward(Steps& st, const cconv_ffn_args& a) {
   const Mat h = st.scratch(T, F, 2), x(a.x), wg(a.w_gate), wu(a.w_up), wd(a.w_down), gate_pre(a.gate_pre), up_pre(a.up_pre),
             out(a.out);
   if (T <= kFewTokens && few_readable(x, T, D, 2) && few_readable(wg, F, D, 2) && few_readable(wu, F, D, 2)) {
-    st.add([=](bool, bool more, cudaStream_t s) {  // always the first
-      return block_cuda_error(run_few_gated(x, wg, wu, gate_pre, up_pre, h, T, F, D, act, dtype, sms, more, s), "cconv_few_kernel");
+    st.add([=](bool, cudaStream_t s) {
+      return block_cuda_error(run_few_gated(x, wg, wu, gate_pre, up_pre, h, T, F, D, act, dtype, sms, s), "cconv_few_kernel");
     });
   } else {
     Product p = product(T, F, D);
@@ -66,8 +64,8 @@ void forward(Steps& st, const cconv_ffn_args& a) {
     st.launch(l, to);
   }
   if (T <= kFewTokens && few_readable(wd, D, F, 2)) {  // (F % 8 == 0: h is readable too)
-    st.add([=](bool chained, bool more, cudaStream_t s) {
-      return block_cuda_error(run_few_product(h, wd, out, T, D, F, dtype, sms, chained, more, s), "cconv_few_kernel");
+    st.add([=](bool first, cudaStream_t s) {
+      return block_cuda_error(run_few_product(h, wd, out, T, D, F, dtype, sms, !first, s), "cconv_few_kernel");
     });
     return;
   }
@@ -115,7 +113,7 @@ void backward(Steps& st, const cconv_ffn_args& a) {
   for (int i = 0; i < 4; ++i) {
     single[i] = launch_of(a, ps[i], kStore);
     choose_cut(&single[i], sms, false);
-    apart[i] = launch_clocks(single[i], sms) + kLaunch;
+    apart[i] = launch_clocks(single[i], sms);
   }
   // the products first .. 3 together, uncut, at the tile that suits them best
   auto group_of = [&](int first, double* clocks) {
@@ -127,7 +125,7 @@ void backward(Steps& st, const cconv_ffn_args& a) {
         l.of[i - first] = ps[i];
         l.of[i - first].block_n = n;
       }
-      const double c = launch_clocks(l, sms) + kLaunch;
+      const double c = launch_clocks(l, sms);
       if (n == 256 || c < *clocks) best = l, *clocks = c;
     }
     return best;

@@ -56,7 +56,7 @@ struct PairParams {
   int count, tiles, splits, stages;
   uint32_t a_stage, stage_bytes; // room of a stage's A; of the whole stage
   uint32_t pieces;              // staged by an epilogue warp
-  int paired, act, save, more;
+  int paired, act, save;
   int direct;  // results straight to memory (cut)
   // direct: where results go and come from (in elements)
   char* out[3];
@@ -333,8 +333,7 @@ __global__ void __launch_bounds__(kThreads, 1) cconv_pair_product_kernel(
   uint32_t tmem;
   asm volatile("ld.shared.b32 %0, [%1];" : "=r"(tmem) : "r"(slot));
 
-  asm volatile("griddepcontrol.wait;" ::: "memory");
-  if (p.more) asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
+  start_in_order();
 
   // 8-bit: the epilogue's sums take registers that the other warps do not need (128 x 80 + 256 x 208 of
   // the 384 x 168 that the block starts with)
@@ -814,7 +813,7 @@ __global__ void __launch_bounds__(kThreads, 1) cconv_pair_product_kernel(
 }
 
 template <int kEpi, typename T>
-cudaError_t launch_pair(const PairMaps<kProductsOf<kEpi>>& maps, const PairParams<kProductsOf<kEpi>>& p, int sms, bool chained,
+cudaError_t launch_pair(const PairMaps<kProductsOf<kEpi>>& maps, const PairParams<kProductsOf<kEpi>>& p, int sms,
                         cudaStream_t s) {
   auto f = cconv_pair_product_kernel<kEpi, T>;
   static bool ready[64] = {};
@@ -829,7 +828,7 @@ cudaError_t launch_pair(const PairMaps<kProductsOf<kEpi>>& maps, const PairParam
   const int pairs = p.splits > 1 ? p.tiles * p.splits : p.tiles < sms / 2 ? p.tiles : sms / 2;
   const size_t smem = 1024 + size_t(p.stages) * p.stage_bytes + kABytes - p.a_stage + kEpilogueWarps * p.pieces * kBoxBytes +
                       scale_bytes(kEpi) + kBarrierBytes;
-  return launch(f, dim3(unsigned(2 * pairs)), kThreads, smem, 2 * p.splits, chained, s, maps, p);
+  return launch(f, dim3(unsigned(2 * pairs)), kThreads, smem, 2 * p.splits, s, maps, p);
 }
 
 int encode_operand(CUtensorMap* tm, const Operand& o, int es, int dtype, int rows_box) {
@@ -839,7 +838,7 @@ int encode_operand(CUtensorMap* tm, const Operand& o, int es, int dtype, int row
 }
 
 template <int kEpi>
-int run_as(const Launch& l, int sms, bool chained, bool more, cudaStream_t s) {
+int run_as(const Launch& l, int sms, cudaStream_t s) {
   constexpr int kProducts = kProductsOf<kEpi>;
   constexpr bool kEight = kEpi == kScaled;
   PairMaps<kProducts> maps;
@@ -911,7 +910,6 @@ int run_as(const Launch& l, int sms, bool chained, bool more, cudaStream_t s) {
   q.paired = p.paired;
   q.act = l.act;
   q.save = l.save;
-  q.more = more;
   q.row_scale = static_cast<const float*>(l.row_scale.p);
   q.row_rs = l.row_scale.rs;
   q.row_ks = l.row_scale.cs;
@@ -920,33 +918,31 @@ int run_as(const Launch& l, int sms, bool chained, bool more, cudaStream_t s) {
   q.col_ks = l.col_scale.cs;
   q.limit_ns = block_wait_limit_ns();
   cudaError_t e;
-  if (l.dtype == CCONV_TYPE_BF16) e = launch_pair<kEpi, __nv_bfloat16>(maps, q, sms, chained, s);
-  else if (l.dtype == CCONV_TYPE_FP16) e = launch_pair<kEpi, __half>(maps, q, sms, chained, s);
-  else if constexpr (kEight) e = launch_pair<kEpi, float>(maps, q, sms, chained, s);
+  if (l.dtype == CCONV_TYPE_BF16) e = launch_pair<kEpi, __nv_bfloat16>(maps, q, sms, s);
+  else if (l.dtype == CCONV_TYPE_FP16) e = launch_pair<kEpi, __half>(maps, q, sms, s);
+  else if constexpr (kEight) e = launch_pair<kEpi, float>(maps, q, sms, s);
   else return CCONV_EUNSUPPORTED;
   return block_cuda_error(e, "cconv_pair_product_kernel");
 }
 
-// Clocks of one product's tile: its k blocks at the slowest of the tensor cores (block_n * 2 clocks a block and
-// pair; 8-bit sums are scaled at 1.7 times that), of L2 (about 60 bytes a clock and SM while all draw) and of
-// a ring of stages that waits for memory (3500 clocks where every tile reads rows of B of its own, which then
-// come from HBM, 1500 where others have brought them to L2); and what begins and ends it (measured: with an
-// exchange 8 us a tile, without 5 us a launch).
-double tile_clocks(const Launch& l, const Product& p) {
-  const int es = l.epilogue == kScaled ? 1 : 2;
-  const double kb = double(cdiv64(cdiv64(p.K, 128 / es) * (p.segments ? 2 : 1), l.splits));
-  const double rows = double(p.M < 256 ? p.M : 256) + p.block_n;
-  const double stages = stages_of(l, uint32_t(a_rows_of(p)) * 128, uint32_t(p.block_n / 2) * 128);
-  const double block = std::max({2.0 * p.block_n * (es == 1 ? 1.7 : 1.0) + 30.0, rows * 128.0 / 120.0,
-                                 (p.M <= 256 ? 3500.0 : 1500.0) / stages});
-  return kb * block + (l.splits > 1 ? 15000.0 : 600.0);
+// Clocks of a k block of a tile, and of what begins and ends a launch or, where cut, a round of tiles, as
+// measured on products of 64 to 2048 rows (back to back, operands in L2): a block costs the tensor cores'
+// 2 clocks a column, or 340 (390 with rows of B contiguous) that a stage takes to come and go; 8-bit sums are
+// scaled at 3.5 clocks a column with 220 a block.  8 us a launch, 11 and 12.5 a round of 2 and 4 pairs a tile.
+double block_clocks(const Launch& l, const Product& p) {
+  if (l.epilogue == kScaled) return 220.0 + 2.65 * p.block_n;
+  return std::max(2.0 * p.block_n, p.b[0].kmajor ? 340.0 : 390.0);
+}
+double fixed_clocks(const Launch& l, int block_n) {
+  const double epilogue = l.epilogue == kGatedBackward ? (block_n == 256 ? 11000.0 : 5000.0)
+                          : l.epilogue == kScaled && l.splits > 1 ? 8000.0 : 0.0;
+  return (l.splits == 1 ? 14600.0 : l.splits == 2 ? 20000.0 : 23000.0) + epilogue;
 }
 
 // Rows of `pieces` accesses of type E, both sides contiguous: 64 threads by 4 rows a block, 4 accesses a thread.
 template <typename E>
-__global__ void __launch_bounds__(256) cconv_copy_rows_kernel(Mat from, Mat to, int64_t rows, int64_t pieces, int more) {
-  asm volatile("griddepcontrol.wait;" ::: "memory");
-  if (more) asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
+__global__ void __launch_bounds__(256) cconv_copy_rows_kernel(Mat from, Mat to, int64_t rows, int64_t pieces) {
+  start_in_order();
   const int64_t x0 = int64_t(blockIdx.x) * 256 + (threadIdx.x & 63);
   for (int64_t r = int64_t(blockIdx.y) * 4 + (threadIdx.x >> 6); r < rows; r += int64_t(gridDim.y) * 4) {
     const E* src = reinterpret_cast<const E*>(static_cast<const char*>(from.p) + r * from.rs);
@@ -961,20 +957,19 @@ __global__ void __launch_bounds__(256) cconv_copy_rows_kernel(Mat from, Mat to, 
   }
 }
 template <typename E>
-cudaError_t copy_rows(const Mat& from, const Mat& to, int64_t rows, int64_t cols, int es, bool chained, bool more, cudaStream_t s) {
+cudaError_t copy_rows(const Mat& from, const Mat& to, int64_t rows, int64_t cols, int es, cudaStream_t s) {
   const int64_t pieces = cols * es / int64_t(sizeof(E)), y = cdiv64(rows, 4);
   const dim3 grid(unsigned(cdiv64(pieces, 256)), unsigned(y < 65535 ? y : 65535));
-  return launch(cconv_copy_rows_kernel<E>, grid, 256, 0, 1, chained, s, Mat(from.p, from.rs * es, 1), Mat(to.p, to.rs * es, 1),
-                rows, pieces, int(more));
+  return launch(cconv_copy_rows_kernel<E>, grid, 256, 0, 1, s, Mat(from.p, from.rs * es, 1), Mat(to.p, to.rs * es, 1), rows,
+                pieces);
 }
 
 // 32 x 32 elements a block through shared memory: read along the source's short stride, written along
 // the target's.
 template <typename E>
-__global__ void __launch_bounds__(256) cconv_copy_kernel(Mat from, Mat to, int64_t rows, int64_t cols, int more) {
+__global__ void __launch_bounds__(256) cconv_copy_kernel(Mat from, Mat to, int64_t rows, int64_t cols) {
   __shared__ E tile[32][33];
-  asm volatile("griddepcontrol.wait;" ::: "memory");
-  if (more) asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
+  start_in_order();
   const E* src = static_cast<const E*>(from.p);
   E* dst = static_cast<E*>(const_cast<void*>(to.p));
   const int x = threadIdx.x & 31, y = threadIdx.x >> 5;
@@ -1056,15 +1051,17 @@ double launch_clocks(const Launch& l, int sms) {
   for (int i = 0; i < l.count; ++i) {
     const Product& p = l.of[i];
     const int64_t n = cdiv64(p.M, 256) * cdiv64(p.N, p.paired ? 128 : p.block_n);
-    const double c = tile_clocks(l, p);
+    const double c = double(cdiv64(cdiv64(p.K, 128 / es) * (p.segments ? 2 : 1), l.splits)) * block_clocks(l, p) + 600.0;
     tiles += n;
     all += double(n) * c;
     longest = std::max(longest, c);
     bytes += double(es) * (double(p.M + p.N * (p.paired ? 2 : 1)) * double(p.K) * (p.segments ? 2 : 1) + double(p.M) * double(p.N));
   }
   const double least = bytes / 3500.0;  // HBM, per clock
-  if (l.count == 1) return std::max(least, double(cdiv64(tiles, slots)) * longest) + (l.splits > 1 ? 0.0 : 9000.0);
-  return std::max(least, std::max(longest, all / slots + 0.5 * longest)) + 9000.0;
+  const double fixed = fixed_clocks(l, l.of[0].block_n), rounds = double(cdiv64(tiles, slots));
+  if (l.splits > 1) return std::max(least, rounds * (longest + fixed));
+  if (l.count == 1) return std::max(least, rounds * longest) + fixed;
+  return std::max(least, all / slots + 0.9 * longest) + fixed;
 }
 
 namespace {
@@ -1096,30 +1093,30 @@ void choose_cut(Launch* l, int sms, bool few_columns) {
   cut(l, best_n, best_s);
 }
 
-int run_products(const Launch& l, int sms, bool chained, bool more, cudaStream_t s) {
-  if (l.epilogue == kStore) return run_as<kStore>(l, sms, chained, more, s);
-  if (l.epilogue == kGated) return run_as<kGated>(l, sms, chained, more, s);
-  if (l.epilogue == kGatedBackward) return run_as<kGatedBackward>(l, sms, chained, more, s);
-  return run_as<kScaled>(l, sms, chained, more, s);
+int run_products(const Launch& l, int sms, cudaStream_t s) {
+  if (l.epilogue == kStore) return run_as<kStore>(l, sms, s);
+  if (l.epilogue == kGated) return run_as<kGated>(l, sms, s);
+  if (l.epilogue == kGatedBackward) return run_as<kGatedBackward>(l, sms, s);
+  return run_as<kScaled>(l, sms, s);
 }
 
-cudaError_t run_copy(const Mat& from, const Mat& to, int64_t rows, int64_t cols, int es, bool chained, bool more,
+cudaError_t run_copy(const Mat& from, const Mat& to, int64_t rows, int64_t cols, int es,
                      cudaStream_t s) {
   if (rows == 0 || cols == 0) return cudaSuccess;
   if (from.cs == 1 && to.cs == 1) {
     const uintptr_t all = reinterpret_cast<uintptr_t>(from.p) | reinterpret_cast<uintptr_t>(to.p) | uintptr_t(cols * es) |
                           (rows > 1 ? uintptr_t(from.rs * es) | uintptr_t(to.rs * es) : 0);
-    if ((all & 15) == 0) return copy_rows<uint4>(from, to, rows, cols, es, chained, more, s);
-    if ((all & 7) == 0) return copy_rows<uint2>(from, to, rows, cols, es, chained, more, s);
-    if ((all & 3) == 0) return copy_rows<uint32_t>(from, to, rows, cols, es, chained, more, s);
-    if ((all & 1) == 0) return copy_rows<uint16_t>(from, to, rows, cols, es, chained, more, s);
-    return copy_rows<uint8_t>(from, to, rows, cols, es, chained, more, s);
+    if ((all & 15) == 0) return copy_rows<uint4>(from, to, rows, cols, es, s);
+    if ((all & 7) == 0) return copy_rows<uint2>(from, to, rows, cols, es, s);
+    if ((all & 3) == 0) return copy_rows<uint32_t>(from, to, rows, cols, es, s);
+    if ((all & 1) == 0) return copy_rows<uint16_t>(from, to, rows, cols, es, s);
+    return copy_rows<uint8_t>(from, to, rows, cols, es, s);
   }
   const int64_t y = cdiv64(rows, 32);
   const dim3 grid(unsigned(cdiv64(cols, 32)), unsigned(y < 65535 ? y : 65535));
-  if (es == 1) return launch(cconv_copy_kernel<uint8_t>, grid, 256, 0, 1, chained, s, from, to, rows, cols, int(more));
-  if (es == 4) return launch(cconv_copy_kernel<uint32_t>, grid, 256, 0, 1, chained, s, from, to, rows, cols, int(more));
-  return launch(cconv_copy_kernel<uint16_t>, grid, 256, 0, 1, chained, s, from, to, rows, cols, int(more));
+  if (es == 1) return launch(cconv_copy_kernel<uint8_t>, grid, 256, 0, 1, s, from, to, rows, cols);
+  if (es == 4) return launch(cconv_copy_kernel<uint32_t>, grid, 256, 0, 1, s, from, to, rows, cols);
+  return launch(cconv_copy_kernel<uint16_t>, grid, 256, 0, 1, s, from, to, rows, cols);
 }
 
 }  // namespace cconv

@@ -42,16 +42,14 @@ struct Launch {
   Mat row_scale, col_scale;     // kScaled: scale (row, kb) of A, (row / 128, kb) of B
 };
 
-// chained: may start while the kernel in front of it in the same call ends; more: another one follows.
-int run_products(const Launch& l, int sms, bool chained, bool more, cudaStream_t s);
+int run_products(const Launch& l, int sms, cudaStream_t s);
 
 // An estimate of the launch's time in clocks, and the cut that makes it least (`few_columns`: 64 is allowed).
 double launch_clocks(const Launch& l, int sms);
 void choose_cut(Launch* l, int sms, bool few_columns);
 
 // Copies rows x cols elements of es bytes between any two layouts.
-cudaError_t run_copy(const Mat& from, const Mat& to, int64_t rows, int64_t cols, int es, bool chained, bool more,
-                     cudaStream_t s);
+cudaError_t run_copy(const Mat& from, const Mat& to, int64_t rows, int64_t cols, int es, cudaStream_t s);
 
 // The status word that the product kernels of the current device share (device address).
 int block_status_word(int** word);

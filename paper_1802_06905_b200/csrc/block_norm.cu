@@ -14,6 +14,7 @@
 
 #include "block.h"
 #include "block_device.cuh"
+#include "block_launch.h"
 #include "block_norm.h"
 #include "host_setup.h"
 #include "ptx_sm100.cuh"
@@ -76,6 +77,7 @@ __device__ __forceinline__ float2 block_sum2(float a, float b, float2 (*smem)[32
 template <typename T, int E, int NV>
 __global__ void __launch_bounds__(1024) cconv_residual_norm_kernel(const NormParams p) {
   __shared__ float2 smem[2][32];
+  start_in_order();
   using V = Vec<T, E>;
   const T* resid = static_cast<const T*>(p.resid);  // may be resid_out
   const T* __restrict__ block = static_cast<const T*>(p.block);
@@ -176,6 +178,7 @@ __global__ void __launch_bounds__(1024) cconv_residual_norm_kernel(const NormPar
 template <typename T>
 __global__ void __launch_bounds__(1024) cconv_residual_norm_long_kernel(const NormParams p) {
   __shared__ float2 smem[2][32];
+  start_in_order();
   const T* resid = static_cast<const T*>(p.resid);
   const T* block = static_cast<const T*>(p.block);
   const T* gate = static_cast<const T*>(p.gate);
@@ -240,6 +243,7 @@ __device__ __forceinline__ int64_t first_row(const NormParams& p, int64_t b) {
 template <typename T, int NV>
 __global__ void __launch_bounds__(512) cconv_residual_norm_backward_kernel(const NormParams p) {
   __shared__ float2 smem[2][32];
+  start_in_order();
   const T* dres = static_cast<const T*>(p.dresid_out);  // may be dresid
   const T* __restrict__ dx = static_cast<const T*>(p.dnorm_out);
   const T* __restrict__ block = static_cast<const T*>(p.block);
@@ -408,6 +412,7 @@ __global__ void __launch_bounds__(512) cconv_residual_norm_backward_ring_kernel(
   __shared__ float2 smem[2][32];
   __shared__ __align__(8) uint64_t full[8];
   __shared__ int abort_flag;
+  start_in_order();
   constexpr int E = 16 / int(sizeof(T)), P = E / 2;
   const T* dres = static_cast<const T*>(p.dresid_out);  // may be dresid
   const T* dx = static_cast<const T*>(p.dnorm_out);
@@ -622,6 +627,7 @@ __global__ void __launch_bounds__(512) cconv_residual_norm_backward_ring_kernel(
 template <typename T>
 __global__ void __launch_bounds__(512) cconv_residual_norm_backward_long_kernel(const NormParams p) {
   __shared__ float2 smem[2][32];
+  start_in_order();
   const T* dres = static_cast<const T*>(p.dresid_out);
   const T* dx = static_cast<const T*>(p.dnorm_out);
   const T* block = static_cast<const T*>(p.block);
@@ -706,7 +712,7 @@ __global__ void __launch_bounds__(512) cconv_residual_norm_backward_long_kernel(
 template <typename T>
 __global__ void __launch_bounds__(512) cconv_residual_norm_sums_kernel(const NormParams p) {
   __shared__ float smem[16][33];
-  asm volatile("griddepcontrol.wait;" ::: "memory");
+  start_in_order();
   const int c = blockIdx.x * 32 + (threadIdx.x & 31), slice = threadIdx.x >> 5;
   const int64_t per = p.rows_per_gate ? p.rows_per_gate : p.T;
   int b0 = 0, b1 = p.nb - 1, slot = int(blockIdx.y);
@@ -813,31 +819,28 @@ bool wide(const NormParams& p, int es, bool backward) {
 }
 
 template <typename T, int E, int NV>
-void launch_forward_nv(const NormParams& p, int threads, int64_t grid, cudaStream_t s) {
-  cconv_residual_norm_kernel<T, E, NV><<<unsigned(grid), threads, 0, s>>>(p);
+cudaError_t launch_forward_nv(const NormParams& p, int threads, int64_t grid, cudaStream_t s) {
+  return launch(cconv_residual_norm_kernel<T, E, NV>, dim3(unsigned(grid)), threads, 0, 1, s, p);
 }
 
 template <typename T>
 cudaError_t launch_forward(const NormParams& p, int sms, cudaStream_t s) {
-  constexpr int kWide = 16 / int(sizeof(T));
+  constexpr int kWide = 16 / int(sizeof(T)), kMost = sizeof(T) == 4 ? 4 : 2;
   const bool w = wide(p, sizeof(T), false);
   const Shape sh = shape_of(p.D, w ? kWide : 1, 16, 1024);
   const int threads = sh.threads ? sh.threads : 1024;
   const int64_t grid = std::min<int64_t>(p.T, int64_t(sms) * std::max(1, std::min(32, 1024 / threads)));
-  if (!sh.threads) {
-    cconv_residual_norm_long_kernel<T><<<unsigned(grid), threads, 0, s>>>(p);
-  } else if (w) {
-    if (sh.nv == 1) launch_forward_nv<T, kWide, 1>(p, threads, grid, s);
-    else if (sh.nv == 2) launch_forward_nv<T, kWide, 2>(p, threads, grid, s);
-    else launch_forward_nv<T, kWide, sizeof(T) == 4 ? 4 : 2>(p, threads, grid, s);
-  } else {
-    if (sh.nv == 1) launch_forward_nv<T, 1, 1>(p, threads, grid, s);
-    else if (sh.nv == 2) launch_forward_nv<T, 1, 2>(p, threads, grid, s);
-    else if (sh.nv == 4) launch_forward_nv<T, 1, 4>(p, threads, grid, s);
-    else if (sh.nv == 8) launch_forward_nv<T, 1, 8>(p, threads, grid, s);
-    else launch_forward_nv<T, 1, 16>(p, threads, grid, s);
+  if (!sh.threads) return launch(cconv_residual_norm_long_kernel<T>, dim3(unsigned(grid)), threads, 0, 1, s, p);
+  if (w) {
+    if (sh.nv == 1) return launch_forward_nv<T, kWide, 1>(p, threads, grid, s);
+    if (sh.nv == 2) return launch_forward_nv<T, kWide, 2>(p, threads, grid, s);
+    return launch_forward_nv<T, kWide, kMost>(p, threads, grid, s);
   }
-  return cudaGetLastError();
+  if (sh.nv == 1) return launch_forward_nv<T, 1, 1>(p, threads, grid, s);
+  if (sh.nv == 2) return launch_forward_nv<T, 1, 2>(p, threads, grid, s);
+  if (sh.nv == 4) return launch_forward_nv<T, 1, 4>(p, threads, grid, s);
+  if (sh.nv == 8) return launch_forward_nv<T, 1, 8>(p, threads, grid, s);
+  return launch_forward_nv<T, 1, 16>(p, threads, grid, s);
 }
 
 template <typename T, int NV, bool kAll>
@@ -853,8 +856,12 @@ cudaError_t launch_ring(NormParams p, int threads, cudaStream_t s) {
     __atomic_store_n(&ready[dev & 63], true, __ATOMIC_RELEASE);
   }
   p.ring_rows = int(std::min<int64_t>(8, ring_rows(p.D, sizeof(T), blocks_an_sm(p.D, sizeof(T)))));
-  f<<<unsigned(p.nb), threads, size_t(p.D) * (size_t(p.ring_rows) * 4 * sizeof(T) + 4), s>>>(p);
-  return cudaGetLastError();
+  return launch(f, dim3(unsigned(p.nb)), threads, size_t(p.D) * (size_t(p.ring_rows) * 4 * sizeof(T) + 4), 1, s, p);
+}
+
+template <typename T, int NV>
+cudaError_t launch_plain(const NormParams& p, int threads, cudaStream_t s) {
+  return launch(cconv_residual_norm_backward_kernel<T, NV>, dim3(unsigned(p.nb)), threads, 0, 1, s, p);
 }
 
 template <typename T>
@@ -866,20 +873,18 @@ cudaError_t launch_backward(const NormParams& p, cudaStream_t s) {
                    p.D == int64_t(sh.threads) * sh.nv * kWide;
   cudaError_t e = cudaSuccess;
   if (!sh.threads) {
-    cconv_residual_norm_backward_long_kernel<T><<<unsigned(p.nb), 512, 0, s>>>(p);
-    e = cudaGetLastError();
+    e = launch(cconv_residual_norm_backward_long_kernel<T>, dim3(unsigned(p.nb)), 512, 0, 1, s, p);
   } else if (w) {
     constexpr int kMost = 16 / kWide;
     if (sh.nv == 1) e = all ? launch_ring<T, 1, true>(p, sh.threads, s) : launch_ring<T, 1, false>(p, sh.threads, s);
     else if (sh.nv == 2) e = all ? launch_ring<T, 2, true>(p, sh.threads, s) : launch_ring<T, 2, false>(p, sh.threads, s);
     else e = all ? launch_ring<T, kMost, true>(p, sh.threads, s) : launch_ring<T, kMost, false>(p, sh.threads, s);
   } else {
-    if (sh.nv == 1) cconv_residual_norm_backward_kernel<T, 1><<<unsigned(p.nb), sh.threads, 0, s>>>(p);
-    else if (sh.nv == 2) cconv_residual_norm_backward_kernel<T, 2><<<unsigned(p.nb), sh.threads, 0, s>>>(p);
-    else if (sh.nv == 4) cconv_residual_norm_backward_kernel<T, 4><<<unsigned(p.nb), sh.threads, 0, s>>>(p);
-    else if (sh.nv == 8) cconv_residual_norm_backward_kernel<T, 8><<<unsigned(p.nb), sh.threads, 0, s>>>(p);
-    else cconv_residual_norm_backward_kernel<T, 16><<<unsigned(p.nb), sh.threads, 0, s>>>(p);
-    e = cudaGetLastError();
+    if (sh.nv == 1) e = launch_plain<T, 1>(p, sh.threads, s);
+    else if (sh.nv == 2) e = launch_plain<T, 2>(p, sh.threads, s);
+    else if (sh.nv == 4) e = launch_plain<T, 4>(p, sh.threads, s);
+    else if (sh.nv == 8) e = launch_plain<T, 8>(p, sh.threads, s);
+    else e = launch_plain<T, 16>(p, sh.threads, s);
   }
   if (e != cudaSuccess) return e;
   NormParams q = p;
@@ -887,8 +892,7 @@ cudaError_t launch_backward(const NormParams& p, cudaStream_t s) {
   q.sums_by_group = groups <= p.nb;
   const int64_t items = !p.gate || per == 1 ? 0 : q.sums_by_group ? groups : p.nb - 1;
   const dim3 grid(unsigned(cdiv64(p.D, 32)), unsigned(2 + items));
-  cconv_residual_norm_sums_kernel<T><<<grid, 512, 0, s>>>(q);
-  return cudaGetLastError();
+  return launch(cconv_residual_norm_sums_kernel<T>, grid, 512, 0, 1, s, q);
 }
 
 }  // namespace

@@ -9,6 +9,7 @@
 
 #include "block.h"
 #include "block_device.cuh"
+#include "block_launch.h"
 #include "block_quant.h"
 
 namespace cconv {
@@ -114,6 +115,7 @@ __global__ void __launch_bounds__(kBlock == 1 ? 256 : 512, U == 2 ? 4 : 1) cconv
   constexpr int kAcross = (kBlock == 1 ? 256 : 512) / kLanes, kPieces = 16 / kLanes;
   static_assert(kBlock == 1 || U * kAcross == 128, "");
   __shared__ uint32_t smem[16];
+  start_in_order();
   const T* x = static_cast<const T*>(p.x);
   const int sub = threadIdx.x % kLanes, row_in = threadIdx.x / kLanes;
   const int64_t cb = blockIdx.x, c = cb * 128 + sub * 8;
@@ -189,8 +191,7 @@ template <typename T, int kBlock, int kLanes, int U, bool kWide>
 cudaError_t launch_as(QuantParams p, cudaStream_t s) {
   p.row_blocks = cdiv64(p.T, kBlock == 1 ? 256 / kLanes * U : 128);
   const dim3 grid(unsigned(cdiv64(p.D, 128)), unsigned(std::min<int64_t>(p.row_blocks, 65535)));
-  cconv_quantize_kernel<T, kBlock, kLanes, U, kWide><<<grid, kBlock == 1 ? 256 : 512, 0, s>>>(p);
-  return cudaGetLastError();
+  return launch(cconv_quantize_kernel<T, kBlock, kLanes, U, kWide>, grid, kBlock == 1 ? 256 : 512, 0, 1, s, p);
 }
 
 template <typename T>

@@ -17,12 +17,12 @@ class Steps {
   int64_t bytes() const { return ws_.used(); }
   int sms() const { return sms_; }
 
-  // A step: launches something (chained: not the first; more: not the last) and gives a status code.
-  using Step = std::function<int(bool chained, bool more, cudaStream_t s)>;
+  // A step: launches something (first: of the call) and gives a status code.
+  using Step = std::function<int(bool first, cudaStream_t s)>;
   void add(Step f) { steps_.push_back(std::move(f)); }
   int run(cudaStream_t s) const {
     for (size_t i = 0; i < steps_.size(); ++i) {
-      const int rc = steps_[i](i > 0, i + 1 < steps_.size(), s);
+      const int rc = steps_[i](i == 0, s);
       if (rc != CCONV_OK) return rc;
     }
     return CCONV_OK;
@@ -34,8 +34,8 @@ class Steps {
     return Mat(ws_.take(rows * pitch * es), pitch, 1);
   }
   void copy(const Mat& from, const Mat& to, int64_t rows, int64_t cols, int es) {
-    add([=](bool chained, bool more, cudaStream_t s) {
-      return block_cuda_error(run_copy(from, to, rows, cols, es, chained, more, s), "cconv_copy_kernel");
+    add([=](bool, cudaStream_t s) {
+      return block_cuda_error(run_copy(from, to, rows, cols, es, s), "cconv_copy_kernel");
     });
   }
 
@@ -91,7 +91,7 @@ class Steps {
       }
     }
     const int sms = sms_;
-    add([=](bool chained, bool more, cudaStream_t s) { return run_products(l, sms, chained, more, s); });
+    add([=](bool, cudaStream_t s) { return run_products(l, sms, s); });
     for (const Move& m : moves) copy(m.from, m.to, m.M, m.N, es);
   }
 
