@@ -329,8 +329,12 @@ int cconv_residual_norm_forward(const cconv_residual_norm_args* args, void* cuda
   const int sms = block_sm_count();
   if (sms < 0) return sms;
   if (a.T == 0 || a.D == 0) return CCONV_OK;
+  NormParams p = norm_params(a);
+  const int rc = block_status_word(&p.status);
+  if (rc != CCONV_OK) return rc;
+  p.limit_ns = block_wait_limit_ns();
   o.note(cuda_stream, sms);
-  return block_cuda_error(run_norm_forward(norm_params(a), a.dtype, sms, static_cast<cudaStream_t>(cuda_stream)),
+  return block_cuda_error(run_norm_forward(p, a.dtype, sms, static_cast<cudaStream_t>(cuda_stream)),
                           "cconv_residual_norm_forward");
 }
 

@@ -74,6 +74,8 @@ __device__ __forceinline__ float2 block_sum2(float a, float b, float2 (*smem)[32
 }
 
 // ---- forward -----------------------------------------------------------------------------------
+// A block a row (and the row gridDim.x further on, ...): few rows, whose latency counts, or rows that are not
+// wide.  Everything that a row needs is asked for before its first reduction.
 template <typename T, int E, int NV>
 __global__ void __launch_bounds__(1024) cconv_residual_norm_kernel(const NormParams p) {
   __shared__ float2 smem[2][32];
@@ -89,87 +91,76 @@ __global__ void __launch_bounds__(1024) cconv_residual_norm_kernel(const NormPar
   const int nt = blockDim.x, tid = threadIdx.x;
   const float inv_d = 1.0f / float(p.D);
   int buf = 0;
-  V r[NV], y[NV];
-  auto fetch = [&](int64_t t) {
+  V vpost[NV], vpre[NV];
+  auto fetch = [&](V& v, const T* from, int c) {
+    v.zero();
+    if (from && c < p.D) v.load(from + c);
+  };
+#pragma unroll
+  for (int v = 0; v < NV; ++v) {
+    fetch(vpost[v], w_post, (v * nt + tid) * E);
+    fetch(vpre[v], w_pre, (v * nt + tid) * E);
+  }
+  for (int64_t t = blockIdx.x; t < p.T; t += gridDim.x) {
+    const T* row_r = resid + t * p.resid_rs;
+    const T* row_y = block ? block + t * p.block_rs : nullptr;
+    const T* row_g = gate ? gate + (p.rows_per_gate ? t / p.rows_per_gate : 0) * p.gate_rs : nullptr;
+    V r[NV], y[NV], g[NV];
 #pragma unroll
     for (int v = 0; v < NV; ++v) {
       const int c = (v * nt + tid) * E;
-      r[v].zero();
-      y[v].zero();
-      if (c < p.D) {
-        r[v].load(resid + t * p.resid_rs + c);
-        if (block) y[v].load(block + t * p.block_rs + c);
-      }
+      fetch(r[v], row_r, c);
+      fetch(y[v], row_y, c);
+      fetch(g[v], row_g, c);
     }
-  };
-  int64_t t = blockIdx.x;
-  if (t < p.T) fetch(t);
-  for (; t < p.T; t += gridDim.x) {
-    float o[NV][E], n[NV][E];
-    float ss = 0.0f;
+    float rho = 1.0f;
+    if (block && w_post) {
+      float ss = 0.0f;
+#pragma unroll
+      for (int v = 0; v < NV; ++v) {
+        float f[E];
+        y[v].get(f);
+#pragma unroll
+        for (int i = 0; i < E; ++i) ss += f[i] * f[i];
+      }
+      rho = rsqrtf(block_sum2(ss, 0.0f, smem, buf).x * inv_d + p.eps);
+    }
+    float o[NV][E], ss = 0.0f;
 #pragma unroll
     for (int v = 0; v < NV; ++v) {
+      const int c = (v * nt + tid) * E;
+      float f[E];
       r[v].get(o[v]);
-      y[v].get(n[v]);
+      y[v].get(f);
+      if (w_post) {
+        float w[E];
+        vpost[v].get(w);
+#pragma unroll
+        for (int i = 0; i < E; ++i) f[i] *= rho * w[i];
+      }
+      if (gate) {
+        float w[E];
+        g[v].get(w);
+#pragma unroll
+        for (int i = 0; i < E; ++i) f[i] *= w[i];
+      }
 #pragma unroll
       for (int i = 0; i < E; ++i) {
-        o[v][i] *= p.scale;
-        ss += n[v][i] * n[v][i];
+        o[v][i] = p.scale * o[v][i] + f[i];
+        ss += o[v][i] * o[v][i];
       }
+      if (c < p.D) V::store(resid_out + t * p.resid_out_rs + c, o[v]);
     }
-    // the next row of this block is on its way while this one is reduced
-    if (t + gridDim.x < p.T) fetch(t + gridDim.x);
-    if (block) {
-      float rho = 1.0f;
-      if (w_post) rho = rsqrtf(block_sum2(ss, 0.0f, smem, buf).x * inv_d + p.eps);
-      const T* g = gate ? gate + (p.rows_per_gate ? t / p.rows_per_gate : 0) * p.gate_rs : nullptr;
-#pragma unroll
-      for (int v = 0; v < NV; ++v) {
-        const int c = (v * nt + tid) * E;
-        if (c >= p.D) continue;
-        float f[E];
-        if (w_post) {
-          V w;
-          w.load(w_post + c);
-          w.get(f);
-#pragma unroll
-          for (int i = 0; i < E; ++i) n[v][i] *= rho * f[i];
-        }
-        if (g) {
-          V w;
-          w.load(g + c);
-          w.get(f);
-#pragma unroll
-          for (int i = 0; i < E; ++i) n[v][i] *= f[i];
-        }
-#pragma unroll
-        for (int i = 0; i < E; ++i) o[v][i] += n[v][i];
-      }
-    }
-    ss = 0.0f;
+    if (!norm_out) continue;
+    rho = rsqrtf(block_sum2(ss, 0.0f, smem, buf).x * inv_d + p.eps);
 #pragma unroll
     for (int v = 0; v < NV; ++v) {
       const int c = (v * nt + tid) * E;
-      if (c < p.D) V::store(resid_out + t * p.resid_out_rs + c, o[v]);
+      float w[E];
+      vpre[v].get(w);
 #pragma unroll
-      for (int i = 0; i < E; ++i) ss += o[v][i] * o[v][i];
-    }
-    if (norm_out) {
-      const float rho = rsqrtf(block_sum2(ss, 0.0f, smem, buf).x * inv_d + p.eps);
-#pragma unroll
-      for (int v = 0; v < NV; ++v) {
-        const int c = (v * nt + tid) * E;
-        if (c >= p.D) continue;
-        float f[E];
-        if (w_pre) {
-          V w;
-          w.load(w_pre + c);
-          w.get(f);
-        }
-#pragma unroll
-        for (int i = 0; i < E; ++i) o[v][i] *= w_pre ? rho * f[i] : rho;
-        V::store(norm_out + t * p.norm_out_rs + c, o[v]);
-      }
+      for (int i = 0; i < E; ++i) o[v][i] *= w_pre ? rho * w[i] : rho;
+      if (c < p.D) V::store(norm_out + t * p.norm_out_rs + c, o[v]);
     }
   }
 }
@@ -622,6 +613,122 @@ __global__ void __launch_bounds__(512) cconv_residual_norm_backward_ring_kernel(
   }
 }
 
+// The forward direction of many wide rows, the same way: r and y through a ring, pairs of operations, the
+// weights in registers.
+template <typename T, int NV, bool kAll>
+__global__ void __launch_bounds__(512) cconv_residual_norm_ring_kernel(const NormParams p) {
+  extern __shared__ __align__(128) uint8_t ring[];
+  __shared__ float2 smem[2][32];
+  __shared__ __align__(8) uint64_t full[8];
+  __shared__ int abort_flag;
+  start_in_order();
+  constexpr int E = 16 / int(sizeof(T)), P = E / 2;
+  const T* resid = static_cast<const T*>(p.resid);  // may be resid_out
+  const T* block = static_cast<const T*>(p.block);
+  const T* __restrict__ gate = static_cast<const T*>(p.gate);
+  const T* __restrict__ w_post = static_cast<const T*>(p.w_post);
+  const T* __restrict__ w_pre = static_cast<const T*>(p.w_pre);
+  T* resid_out = static_cast<T*>(p.resid_out);
+  T* norm_out = static_cast<T*>(p.norm_out);
+  const int nt = blockDim.x, tid = threadIdx.x;
+  const bool has_block = kAll || block, has_post = kAll || w_post, has_norm = kAll || norm_out;
+  auto inside = [&](int v) { return kAll || (v * nt + tid) * E < p.D; };
+  const float inv_d = 1.0f / float(p.D);
+  const int64_t row0 = first_row<T>(p, blockIdx.x), row1 = first_row<T>(p, blockIdx.x + 1);
+  const int64_t per = p.rows_per_gate ? p.rows_per_gate : p.T;
+  const uint32_t row_bytes = uint32_t(p.D) * sizeof(T), ring0 = smem_u32(ring), full0 = smem_u32(full);
+  const uint64_t one = pair_of(1.0f, 1.0f), scale = pair_of(p.scale, p.scale);
+  int buf = 0;
+  auto get = [&](bool given, const T* from, int v, uint64_t (&f)[P], uint64_t otherwise) {
+    if (given && inside(v)) {
+      get_pairs<T>(from + (v * nt + tid) * E, f);
+    } else {
+#pragma unroll
+      for (int i = 0; i < P; ++i) f[i] = otherwise;
+    }
+  };
+  auto copy_row = [&](int64_t t) {
+    const uint32_t st = uint32_t(t - row0) % uint32_t(p.ring_rows), bar = full0 + 8 * st;
+    const uint32_t to = ring0 + st * 2 * row_bytes;
+    mbar_arrive_expect_tx(bar, row_bytes * (has_block ? 2u : 1u));
+    bulk_load(to, resid + t * p.resid_rs, row_bytes, bar);
+    if (has_block) bulk_load(to + row_bytes, block + t * p.block_rs, row_bytes, bar);
+  };
+  if (tid == 0) {
+    abort_flag = 0;
+    for (int i = 0; i < p.ring_rows; ++i) mbar_init(full0 + 8 * i, 1);
+    fence_barrier_init();
+    for (int64_t t = row0; t < row1 && t < row0 + p.ring_rows; ++t) copy_row(t);
+  }
+  __syncthreads();
+  uint64_t gw[NV][P], wpre[NV][P];  // gate * w_post of the current group; w_pre
+#pragma unroll
+  for (int v = 0; v < NV; ++v) get(kAll || w_pre, w_pre, v, wpre[v], one);
+  int64_t group_end = row0;
+  uint32_t st = 0, phase = 0;
+  int64_t t = row0;
+  for (; t < row1; ++t) {
+    if (t == group_end || t == row0) {
+      const int64_t group = t / per;
+      group_end = (group + 1) * per;
+#pragma unroll
+      for (int v = 0; v < NV; ++v) {
+        uint64_t fg[P];
+        get(kAll || gate, gate + group * p.gate_rs, v, fg, one);
+        get(has_post, w_post, v, gw[v], one);
+#pragma unroll
+        for (int i = 0; i < P; ++i) gw[v][i] = mul2(gw[v][i], fg[i]);
+      }
+    }
+    const bool ok = mbar_wait(full0 + 8 * st, phase, &abort_flag, p.status, kStatProducerWait, p.limit_ns);
+    // every thread is past the row before: its place in the ring is free
+    if (!__syncthreads_and(ok)) break;
+    if (tid == 0 && t > row0 && t - 1 + p.ring_rows < row1) copy_row(t - 1 + p.ring_rows);
+    const T* row_r = reinterpret_cast<const T*>(ring + st * 2 * row_bytes);
+    const T* row_y = row_r + p.D;
+    if (++st == uint32_t(p.ring_rows)) st = 0, phase ^= 1;
+    uint64_t o[NV][P], sum = 0;
+    float rho1 = 1.0f;
+    if (has_block) {
+#pragma unroll
+      for (int v = 0; v < NV; ++v) {
+        get(true, row_y, v, o[v], 0);
+#pragma unroll
+        for (int i = 0; i < P; ++i) sum = fma2(o[v][i], o[v][i], sum);
+      }
+      if (has_post) rho1 = rsqrtf(block_sum2(sum_of(sum), 0.0f, smem, buf).x * inv_d + p.eps);
+    }
+    uint64_t rho = pair_of(rho1, rho1);
+    sum = 0;
+#pragma unroll
+    for (int v = 0; v < NV; ++v) {
+      uint64_t r[P];
+      get(true, row_r, v, r, 0);
+#pragma unroll
+      for (int i = 0; i < P; ++i) {
+        r[i] = mul2(scale, r[i]);
+        o[v][i] = has_block ? fma2(o[v][i], mul2(rho, gw[v][i]), r[i]) : r[i];
+        sum = fma2(o[v][i], o[v][i], sum);
+      }
+      if (inside(v)) put_pairs<T>(resid_out + t * p.resid_out_rs + (v * nt + tid) * E, o[v]);
+    }
+    if (!has_norm) continue;
+    rho1 = rsqrtf(block_sum2(sum_of(sum), 0.0f, smem, buf).x * inv_d + p.eps);
+    rho = pair_of(rho1, rho1);
+#pragma unroll
+    for (int v = 0; v < NV; ++v) {
+#pragma unroll
+      for (int i = 0; i < P; ++i) o[v][i] = mul2(o[v][i], mul2(rho, wpre[v][i]));
+      if (inside(v)) put_pairs<T>(norm_out + t * p.norm_out_rs + (v * nt + tid) * E, o[v]);
+    }
+  }
+  if (t < row1) {  // a copy did not come in time: let those on their way land
+    const uint64_t t0 = globaltimer_ns();
+    while (globaltimer_ns() - t0 < 200000) {
+    }
+  }
+}
+
 // Rows too long for registers: column sums live in the partial table (5 rows a block here; the fifth
 // holds the sums of a gate group that is complete within the block until it is written).
 template <typename T>
@@ -818,17 +925,52 @@ bool wide(const NormParams& p, int es, bool backward) {
   return ((all | uintptr_t(strides)) & 15u) == 0;
 }
 
+template <typename F>
+cudaError_t allow_ring(F f, bool (&ready)[64]) {
+  int dev = 0;
+  cudaError_t e = cudaGetDevice(&dev);
+  if (e != cudaSuccess) return e;
+  if (!__atomic_load_n(&ready[dev & 63], __ATOMIC_ACQUIRE)) {
+    e = cudaFuncSetAttribute(f, cudaFuncAttributeMaxDynamicSharedMemorySize, int(kRingSmem));
+    if (e != cudaSuccess) return e;
+    __atomic_store_n(&ready[dev & 63], true, __ATOMIC_RELEASE);
+  }
+  return cudaSuccess;
+}
+
 template <typename T, int E, int NV>
 cudaError_t launch_forward_nv(const NormParams& p, int threads, int64_t grid, cudaStream_t s) {
   return launch(cconv_residual_norm_kernel<T, E, NV>, dim3(unsigned(grid)), threads, 0, 1, s, p);
 }
 
+template <typename T, int NV, bool kAll>
+cudaError_t launch_forward_ring(const NormParams& p, int threads, cudaStream_t s) {
+  auto f = cconv_residual_norm_ring_kernel<T, NV, kAll>;
+  static bool ready[64] = {};
+  const cudaError_t e = allow_ring(f, ready);
+  if (e != cudaSuccess) return e;
+  return launch(f, dim3(unsigned(p.nb)), threads, size_t(p.D) * p.ring_rows * 2 * sizeof(T), 1, s, p);
+}
+
 template <typename T>
-cudaError_t launch_forward(const NormParams& p, int sms, cudaStream_t s) {
-  constexpr int kWide = 16 / int(sizeof(T)), kMost = sizeof(T) == 4 ? 4 : 2;
+cudaError_t launch_forward(NormParams p, int sms, cudaStream_t s) {
+  constexpr int kWide = 16 / int(sizeof(T)), kMost = 16 / kWide;
   const bool w = wide(p, sizeof(T), false);
   const Shape sh = shape_of(p.D, w ? kWide : 1, 16, 1024);
   const int threads = sh.threads ? sh.threads : 1024;
+  // Many wide rows: blocks of about 1024 threads an SM go through rows of their own, fewer where their rings
+  // would not hold two rows each.
+  int64_t an_sm = std::max(1, std::min(16, 1024 / threads));
+  auto rows = [&](int64_t blocks) { return (kRingSmem / blocks / 1024 * 1024 - kRingOwn) / (2 * p.D * int64_t(sizeof(T))); };
+  while (an_sm > 1 && rows(an_sm) < 2) --an_sm;
+  if (w && sh.threads && sh.threads <= 512 && rows(an_sm) >= 2 && p.T >= 4 * an_sm * sms) {
+    p.nb = int(an_sm * sms);
+    p.ring_rows = int(std::min<int64_t>(8, rows(an_sm)));
+    const bool all = p.block && p.w_post && p.w_pre && p.gate && p.norm_out && p.D == int64_t(sh.threads) * sh.nv * kWide;
+    if (sh.nv == 1) return all ? launch_forward_ring<T, 1, true>(p, threads, s) : launch_forward_ring<T, 1, false>(p, threads, s);
+    if (sh.nv == 2) return all ? launch_forward_ring<T, 2, true>(p, threads, s) : launch_forward_ring<T, 2, false>(p, threads, s);
+    return all ? launch_forward_ring<T, kMost, true>(p, threads, s) : launch_forward_ring<T, kMost, false>(p, threads, s);
+  }
   const int64_t grid = std::min<int64_t>(p.T, int64_t(sms) * std::max(1, std::min(32, 1024 / threads)));
   if (!sh.threads) return launch(cconv_residual_norm_long_kernel<T>, dim3(unsigned(grid)), threads, 0, 1, s, p);
   if (w) {
@@ -847,14 +989,8 @@ template <typename T, int NV, bool kAll>
 cudaError_t launch_ring(NormParams p, int threads, cudaStream_t s) {
   auto f = cconv_residual_norm_backward_ring_kernel<T, NV, kAll>;
   static bool ready[64] = {};
-  int dev = 0;
-  cudaError_t e = cudaGetDevice(&dev);
+  const cudaError_t e = allow_ring(f, ready);
   if (e != cudaSuccess) return e;
-  if (!__atomic_load_n(&ready[dev & 63], __ATOMIC_ACQUIRE)) {
-    e = cudaFuncSetAttribute(f, cudaFuncAttributeMaxDynamicSharedMemorySize, int(kRingSmem));
-    if (e != cudaSuccess) return e;
-    __atomic_store_n(&ready[dev & 63], true, __ATOMIC_RELEASE);
-  }
   p.ring_rows = int(std::min<int64_t>(8, ring_rows(p.D, sizeof(T), blocks_an_sm(p.D, sizeof(T)))));
   return launch(f, dim3(unsigned(p.nb)), threads, size_t(p.D) * (size_t(p.ring_rows) * 4 * sizeof(T) + 4), 1, s, p);
 }

@@ -9,7 +9,7 @@ namespace cconv {
 struct NormParams {
   int64_t T;
   int D;
-  int nb;  // backward: blocks, at most T
+  int nb;  // blocks that have rows of their own (backward: at most T)
   float scale, eps;
   int64_t rows_per_gate;  // 0: one gate row for all tokens
   const void *resid, *block, *gate, *w_post, *w_pre, *dresid_out, *dnorm_out;
