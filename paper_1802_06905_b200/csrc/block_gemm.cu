@@ -826,8 +826,9 @@ cudaError_t launch_pair(const PairMaps<kProductsOf<kEpi>>& maps, const PairParam
     __atomic_store_n(&ready[dev & 63], true, __ATOMIC_RELEASE);
   }
   const int pairs = p.splits > 1 ? p.tiles * p.splits : p.tiles < sms / 2 ? p.tiles : sms / 2;
-  const size_t smem = 1024 + size_t(p.stages) * p.stage_bytes + kABytes - p.a_stage + kEpilogueWarps * p.pieces * kBoxBytes +
-                      scale_bytes(kEpi) + kBarrierBytes;
+  // All of an SM's shared memory, needed or not: no other block may share the SM, as it could hold the tensor
+  // memory that one CTA of a cluster waits for while that block's kernel waits for another CTA of the cluster.
+  const size_t smem = kSmemMost;
   return launch(f, dim3(unsigned(2 * pairs)), kThreads, smem, 2 * p.splits, s, maps, p);
 }
 
