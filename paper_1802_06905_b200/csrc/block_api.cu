@@ -40,7 +40,7 @@ int block_sm_count() {
 
 namespace {
 
-constexpr int64_t kMaxLength = int64_t(1) << 31;  // of one dimension
+constexpr int64_t kMaxLength = (int64_t(1) << 31) - 1024;  // of one dimension: coordinates of tiles are 32 bits
 constexpr int64_t kMaxStride = int64_t(1) << 40;
 
 // The bytes of an operand: [lo, hi), and where they are rows at a pitch, `width` bytes of every `pitch`.
@@ -135,6 +135,16 @@ class Operands {
 
 bool length_ok(int64_t n) { return n >= 0 && n < kMaxLength; }
 
+// Runs the body of an entry point; nothing is thrown through the C boundary.
+template <typename F>
+auto guarded(F f) noexcept -> decltype(f()) {
+  try {
+    return f();
+  } catch (...) {  // host memory ran out: nothing else here throws
+    return CCONV_ENOMEM;
+  }
+}
+
 // ---- feed-forward --------------------------------------------------------------------------------
 bool ffn_sizes_ok(const cconv_ffn_args& a) {
   return length_ok(a.T) && length_ok(a.D) && length_ok(a.F) &&
@@ -159,7 +169,7 @@ cudaError_t zero_out(const cconv_matrix& m, int64_t rows, int64_t cols, int es, 
 #define BLOCK_CUDA(call)                                              \
   do {                                                                \
     const cudaError_t e_ = (call);                                    \
-    if (e_ != cudaSuccess) return block_cuda_error(e_, __func__);     \
+    if (e_ != cudaSuccess) return block_cuda_error(e_, "feed-forward sub-block");     \
   } while (0)
 
 bool ffn_empty(const cconv_ffn_args& a) { return a.T == 0 || a.D == 0 || a.F == 0; }
@@ -245,225 +255,249 @@ using namespace cconv;
 
 extern "C" {
 
-int64_t cconv_ffn_forward_workspace(const cconv_ffn_args* args) { return ffn_bytes(args, false); }
-int64_t cconv_ffn_backward_workspace(const cconv_ffn_args* args) { return ffn_bytes(args, true); }
+int64_t cconv_ffn_forward_workspace(const cconv_ffn_args* args) {
+  return guarded([&] { return ffn_bytes(args, false); });
+}
+int64_t cconv_ffn_backward_workspace(const cconv_ffn_args* args) {
+  return guarded([&] { return ffn_bytes(args, true); });
+}
 
 int cconv_ffn_forward(const cconv_ffn_args* args, void* cuda_stream) {
-  if (!args || !ffn_sizes_ok(*args)) return CCONV_EINVAL;
-  const cconv_ffn_args& a = *args;
-  if (!a.gate_pre.data != !a.up_pre.data && a.T && a.F) return CCONV_EINVAL;
-  Operands o;
-  o.in(a.x, a.T, a.D, 2);
-  o.in(a.w_gate, a.F, a.D, 2);
-  o.in(a.w_up, a.F, a.D, 2);
-  o.in(a.w_down, a.D, a.F, 2);
-  o.out(a.out, a.T, a.D, 2);
-  if (a.gate_pre.data) {
-    o.out(a.gate_pre, a.T, a.F, 2);
-    o.out(a.up_pre, a.T, a.F, 2);
-  }
-  if (!o.ok) return CCONV_EINVAL;
-  const int sms = block_sm_count();
-  if (sms < 0) return sms;
-  o.workspace(a.workspace, a.workspace_bytes, ffn_empty(a) ? 0 : ffn_workspace(a, false, sms));
-  if (!o.distinct()) return CCONV_EINVAL;
-  o.note(cuda_stream, sms);
-  cudaStream_t s = static_cast<cudaStream_t>(cuda_stream);
-  return ffn_empty(a) ? ffn_zeros(a, false, s) : run_ffn(a, false, sms, s);
+  return guarded([&]() -> int {
+    if (!args || !ffn_sizes_ok(*args)) return CCONV_EINVAL;
+    const cconv_ffn_args& a = *args;
+    if (!a.gate_pre.data != !a.up_pre.data && a.T && a.F) return CCONV_EINVAL;
+    Operands o;
+    o.in(a.x, a.T, a.D, 2);
+    o.in(a.w_gate, a.F, a.D, 2);
+    o.in(a.w_up, a.F, a.D, 2);
+    o.in(a.w_down, a.D, a.F, 2);
+    o.out(a.out, a.T, a.D, 2);
+    if (a.gate_pre.data) {
+      o.out(a.gate_pre, a.T, a.F, 2);
+      o.out(a.up_pre, a.T, a.F, 2);
+    }
+    if (!o.distinct()) return CCONV_EINVAL;
+    const int sms = block_sm_count();
+    if (sms < 0) return sms;
+    o.workspace(a.workspace, a.workspace_bytes, ffn_empty(a) ? 0 : ffn_workspace(a, false, sms));
+    if (!o.distinct()) return CCONV_EINVAL;
+    o.note(cuda_stream, sms);
+    cudaStream_t s = static_cast<cudaStream_t>(cuda_stream);
+    return ffn_empty(a) ? ffn_zeros(a, false, s) : run_ffn(a, false, sms, s);
+  });
 }
 
 int cconv_ffn_backward(const cconv_ffn_args* args, void* cuda_stream) {
-  if (!args || !ffn_sizes_ok(*args)) return CCONV_EINVAL;
-  const cconv_ffn_args& a = *args;
-  Operands o;
-  o.in(a.dout, a.T, a.D, 2);
-  o.in(a.x, a.T, a.D, 2);
-  o.in(a.w_gate, a.F, a.D, 2);
-  o.in(a.w_up, a.F, a.D, 2);
-  o.in(a.w_down, a.D, a.F, 2);
-  o.in(a.gate_pre, a.T, a.F, 2);
-  o.in(a.up_pre, a.T, a.F, 2);
-  o.out(a.dx, a.T, a.D, 2);
-  o.out(a.dw_gate, a.F, a.D, 2);
-  o.out(a.dw_up, a.F, a.D, 2);
-  o.out(a.dw_down, a.D, a.F, 2);
-  if (!o.ok) return CCONV_EINVAL;
-  const int sms = block_sm_count();
-  if (sms < 0) return sms;
-  o.workspace(a.workspace, a.workspace_bytes, ffn_empty(a) ? 0 : ffn_workspace(a, true, sms));
-  if (!o.distinct()) return CCONV_EINVAL;
-  o.note(cuda_stream, sms);
-  cudaStream_t s = static_cast<cudaStream_t>(cuda_stream);
-  return ffn_empty(a) ? ffn_zeros(a, true, s) : run_ffn(a, true, sms, s);
+  return guarded([&]() -> int {
+    if (!args || !ffn_sizes_ok(*args)) return CCONV_EINVAL;
+    const cconv_ffn_args& a = *args;
+    Operands o;
+    o.in(a.dout, a.T, a.D, 2);
+    o.in(a.x, a.T, a.D, 2);
+    o.in(a.w_gate, a.F, a.D, 2);
+    o.in(a.w_up, a.F, a.D, 2);
+    o.in(a.w_down, a.D, a.F, 2);
+    o.in(a.gate_pre, a.T, a.F, 2);
+    o.in(a.up_pre, a.T, a.F, 2);
+    o.out(a.dx, a.T, a.D, 2);
+    o.out(a.dw_gate, a.F, a.D, 2);
+    o.out(a.dw_up, a.F, a.D, 2);
+    o.out(a.dw_down, a.D, a.F, 2);
+    if (!o.distinct()) return CCONV_EINVAL;
+    const int sms = block_sm_count();
+    if (sms < 0) return sms;
+    o.workspace(a.workspace, a.workspace_bytes, ffn_empty(a) ? 0 : ffn_workspace(a, true, sms));
+    if (!o.distinct()) return CCONV_EINVAL;
+    o.note(cuda_stream, sms);
+    cudaStream_t s = static_cast<cudaStream_t>(cuda_stream);
+    return ffn_empty(a) ? ffn_zeros(a, true, s) : run_ffn(a, true, sms, s);
+  });
 }
 
 int64_t cconv_residual_norm_backward_workspace(const cconv_residual_norm_args* args) {
-  if (!args || !norm_sizes_ok(*args)) return CCONV_EINVAL;
-  const int sms = block_sm_count();
-  if (sms < 0) return sms;
-  return norm_workspace(*args, sms);
+  return guarded([&]() -> int64_t {
+    if (!args || !norm_sizes_ok(*args)) return CCONV_EINVAL;
+    const int sms = block_sm_count();
+    if (sms < 0) return sms;
+    return norm_workspace(*args, sms);
+  });
 }
 
 int cconv_residual_norm_forward(const cconv_residual_norm_args* args, void* cuda_stream) {
-  if (!args || !norm_sizes_ok(*args)) return CCONV_EINVAL;
-  cconv_residual_norm_args a = *args;
-  const int es = type_bytes(a.dtype);
-  a.resid = same_row(a.resid, a.T, a.D);
-  a.block = same_row(a.block, a.T, a.D);
-  a.gate = same_row(a.gate, gate_rows(a), a.D);
-  a.resid_out = same_row(a.resid_out, a.T, a.D);
-  a.norm_out = same_row(a.norm_out, a.T, a.D);
-  if (!unit(a.resid, a.D) || !unit(a.block, a.D) || !unit(a.gate, a.D) || !unit(a.resid_out, a.D) || !unit(a.norm_out, a.D))
-    return CCONV_EINVAL;
-  if (a.T && a.D && ((!a.block.data && (a.gate.data || a.w_post)) || (!a.norm_out.data && a.w_pre))) return CCONV_EINVAL;
-  Operands o;
-  o.in(a.resid, a.T, a.D, es);
-  if (a.block.data) o.in(a.block, a.T, a.D, es);
-  if (a.gate.data) o.in(a.gate, gate_rows(a), a.D, es);
-  if (a.w_post) o.in(a.w_post, a.D, es);
-  if (a.w_pre) o.in(a.w_pre, a.D, es);
-  o.out(a.resid_out, a.T, a.D, es);
-  if (a.norm_out.data) o.out(a.norm_out, a.T, a.D, es);
-  const bool same = a.resid.row_stride == a.resid_out.row_stride;
-  if (!o.distinct(same ? a.resid.data : nullptr, a.resid_out.data)) return CCONV_EINVAL;
-  const int sms = block_sm_count();
-  if (sms < 0) return sms;
-  if (a.T == 0 || a.D == 0) return CCONV_OK;
-  NormParams p = norm_params(a);
-  const int rc = block_status_word(&p.status);
-  if (rc != CCONV_OK) return rc;
-  p.limit_ns = block_wait_limit_ns();
-  o.note(cuda_stream, sms);
-  return block_cuda_error(run_norm_forward(p, a.dtype, sms, static_cast<cudaStream_t>(cuda_stream)),
-                          "cconv_residual_norm_forward");
+  return guarded([&]() -> int {
+    if (!args || !norm_sizes_ok(*args)) return CCONV_EINVAL;
+    cconv_residual_norm_args a = *args;
+    const int es = type_bytes(a.dtype);
+    a.resid = same_row(a.resid, a.T, a.D);
+    a.block = same_row(a.block, a.T, a.D);
+    a.gate = same_row(a.gate, gate_rows(a), a.D);
+    a.resid_out = same_row(a.resid_out, a.T, a.D);
+    a.norm_out = same_row(a.norm_out, a.T, a.D);
+    if (!unit(a.resid, a.D) || !unit(a.block, a.D) || !unit(a.gate, a.D) || !unit(a.resid_out, a.D) || !unit(a.norm_out, a.D))
+      return CCONV_EINVAL;
+    if (a.T && a.D && ((!a.block.data && (a.gate.data || a.w_post)) || (!a.norm_out.data && a.w_pre))) return CCONV_EINVAL;
+    Operands o;
+    o.in(a.resid, a.T, a.D, es);
+    if (a.block.data) o.in(a.block, a.T, a.D, es);
+    if (a.gate.data) o.in(a.gate, gate_rows(a), a.D, es);
+    if (a.w_post) o.in(a.w_post, a.D, es);
+    if (a.w_pre) o.in(a.w_pre, a.D, es);
+    o.out(a.resid_out, a.T, a.D, es);
+    if (a.norm_out.data) o.out(a.norm_out, a.T, a.D, es);
+    const bool same = a.resid.row_stride == a.resid_out.row_stride;
+    if (!o.distinct(same ? a.resid.data : nullptr, a.resid_out.data)) return CCONV_EINVAL;
+    const int sms = block_sm_count();
+    if (sms < 0) return sms;
+    if (a.T == 0 || a.D == 0) return CCONV_OK;
+    NormParams p = norm_params(a);
+    const int rc = block_status_word(&p.status);
+    if (rc != CCONV_OK) return rc;
+    p.limit_ns = block_wait_limit_ns();
+    o.note(cuda_stream, sms);
+    return block_cuda_error(run_norm_forward(p, a.dtype, sms, static_cast<cudaStream_t>(cuda_stream)),
+                            "cconv_residual_norm_forward");
+  });
 }
 
 int cconv_residual_norm_backward(const cconv_residual_norm_args* args, void* cuda_stream) {
-  if (!args || !norm_sizes_ok(*args)) return CCONV_EINVAL;
-  cconv_residual_norm_args a = *args;
-  const int es = type_bytes(a.dtype);
-  a.block = same_row(a.block, a.T, a.D);
-  a.gate = same_row(a.gate, gate_rows(a), a.D);
-  a.resid_out = same_row(a.resid_out, a.T, a.D);
-  a.dresid_out = same_row(a.dresid_out, a.T, a.D);
-  a.dnorm_out = same_row(a.dnorm_out, a.T, a.D);
-  a.dresid = same_row(a.dresid, a.T, a.D);
-  a.dblock = same_row(a.dblock, a.T, a.D);
-  a.dgate = same_row(a.dgate, gate_rows(a), a.D);
-  for (const cconv_matrix* m : {&a.block, &a.gate, &a.resid_out, &a.dresid_out, &a.dnorm_out, &a.dresid, &a.dblock, &a.dgate})
-    if (!unit(*m, a.D)) return CCONV_EINVAL;
-  if (a.T && a.D) {
-    if (!a.block.data && (a.gate.data || a.w_post)) return CCONV_EINVAL;
-    if (!a.block.data != !a.dblock.data) return CCONV_EINVAL;
-    if (!a.dnorm_out.data && !a.dresid_out.data) return CCONV_EINVAL;
-  }
-  if (a.D && (!a.gate.data != !a.dgate.data || !a.w_post != !a.dw_post)) return CCONV_EINVAL;
-  if (a.D && (a.w_pre && (a.dnorm_out.data || a.T == 0)) != (a.dw_pre != nullptr)) return CCONV_EINVAL;
-  const int sms = block_sm_count();
-  if (sms < 0) return sms;
-  Operands o;
-  if (a.block.data) o.in(a.block, a.T, a.D, es);
-  if (a.gate.data) o.in(a.gate, gate_rows(a), a.D, es);
-  if (a.w_post) o.in(a.w_post, a.D, es);
-  if (a.w_pre) o.in(a.w_pre, a.D, es);
-  if (a.dnorm_out.data) o.in(a.resid_out, a.T, a.D, es);
-  if (a.dresid_out.data) o.in(a.dresid_out, a.T, a.D, es);
-  if (a.dnorm_out.data) o.in(a.dnorm_out, a.T, a.D, es);
-  o.out(a.dresid, a.T, a.D, es);
-  if (a.dblock.data) o.out(a.dblock, a.T, a.D, es);
-  if (a.dgate.data) o.out(a.dgate, gate_rows(a), a.D, es);
-  if (a.dw_post) o.out(a.dw_post, a.D, es);
-  if (a.dw_pre) o.out(a.dw_pre, a.D, es);
-  o.workspace(a.workspace, a.workspace_bytes, norm_workspace(a, sms));
-  const bool same = a.dresid_out.row_stride == a.dresid.row_stride;
-  if (!o.distinct(same ? a.dresid_out.data : nullptr, a.dresid.data)) return CCONV_EINVAL;
-  if (a.D == 0) return CCONV_OK;
-  cudaStream_t s = static_cast<cudaStream_t>(cuda_stream);
-  o.note(cuda_stream, sms);
-  if (a.T == 0) {
-    if (a.dgate.data) BLOCK_CUDA(zero_out(a.dgate, gate_rows(a), a.D, es, s));
-    if (a.dw_post) BLOCK_CUDA(cudaMemsetAsync(a.dw_post, 0, size_t(a.D * es), s));
-    if (a.dw_pre) BLOCK_CUDA(cudaMemsetAsync(a.dw_pre, 0, size_t(a.D * es), s));
-    return CCONV_OK;
-  }
-  NormParams p = norm_params(a);
-  p.nb = norm_backward_blocks(a.T, a.D, type_bytes(a.dtype), sms);
-  p.part = static_cast<float*>(a.workspace);
-  const int rc = block_status_word(&p.status);
-  if (rc != CCONV_OK) return rc;
-  p.limit_ns = block_wait_limit_ns();
-  return block_cuda_error(run_norm_backward(p, a.dtype, s), "cconv_residual_norm_backward");
+  return guarded([&]() -> int {
+    if (!args || !norm_sizes_ok(*args)) return CCONV_EINVAL;
+    cconv_residual_norm_args a = *args;
+    const int es = type_bytes(a.dtype);
+    a.block = same_row(a.block, a.T, a.D);
+    a.gate = same_row(a.gate, gate_rows(a), a.D);
+    a.resid_out = same_row(a.resid_out, a.T, a.D);
+    a.dresid_out = same_row(a.dresid_out, a.T, a.D);
+    a.dnorm_out = same_row(a.dnorm_out, a.T, a.D);
+    a.dresid = same_row(a.dresid, a.T, a.D);
+    a.dblock = same_row(a.dblock, a.T, a.D);
+    a.dgate = same_row(a.dgate, gate_rows(a), a.D);
+    for (const cconv_matrix* m : {&a.block, &a.gate, &a.resid_out, &a.dresid_out, &a.dnorm_out, &a.dresid, &a.dblock, &a.dgate})
+      if (!unit(*m, a.D)) return CCONV_EINVAL;
+    if (a.T && a.D) {
+      if (!a.block.data && (a.gate.data || a.w_post)) return CCONV_EINVAL;
+      if (!a.block.data != !a.dblock.data) return CCONV_EINVAL;
+      if (!a.dnorm_out.data && !a.dresid_out.data) return CCONV_EINVAL;
+    }
+    if (a.D && (!a.gate.data != !a.dgate.data || !a.w_post != !a.dw_post)) return CCONV_EINVAL;
+    if (a.D && (a.w_pre && (a.dnorm_out.data || a.T == 0)) != (a.dw_pre != nullptr)) return CCONV_EINVAL;
+    Operands o;
+    if (a.block.data) o.in(a.block, a.T, a.D, es);
+    if (a.gate.data) o.in(a.gate, gate_rows(a), a.D, es);
+    if (a.w_post) o.in(a.w_post, a.D, es);
+    if (a.w_pre) o.in(a.w_pre, a.D, es);
+    if (a.dnorm_out.data) o.in(a.resid_out, a.T, a.D, es);
+    if (a.dresid_out.data) o.in(a.dresid_out, a.T, a.D, es);
+    if (a.dnorm_out.data) o.in(a.dnorm_out, a.T, a.D, es);
+    o.out(a.dresid, a.T, a.D, es);
+    if (a.dblock.data) o.out(a.dblock, a.T, a.D, es);
+    if (a.dgate.data) o.out(a.dgate, gate_rows(a), a.D, es);
+    if (a.dw_post) o.out(a.dw_post, a.D, es);
+    if (a.dw_pre) o.out(a.dw_pre, a.D, es);
+    const bool same = a.dresid_out.row_stride == a.dresid.row_stride;
+    const void* same_in = same ? a.dresid_out.data : nullptr;
+    if (!o.distinct(same_in, a.dresid.data)) return CCONV_EINVAL;
+    const int sms = block_sm_count();
+    if (sms < 0) return sms;
+    o.workspace(a.workspace, a.workspace_bytes, norm_workspace(a, sms));
+    if (!o.distinct(same_in, a.dresid.data)) return CCONV_EINVAL;
+    if (a.D == 0) return CCONV_OK;
+    cudaStream_t s = static_cast<cudaStream_t>(cuda_stream);
+    o.note(cuda_stream, sms);
+    if (a.T == 0) {
+      if (a.dgate.data) BLOCK_CUDA(zero_out(a.dgate, gate_rows(a), a.D, es, s));
+      if (a.dw_post) BLOCK_CUDA(cudaMemsetAsync(a.dw_post, 0, size_t(a.D * es), s));
+      if (a.dw_pre) BLOCK_CUDA(cudaMemsetAsync(a.dw_pre, 0, size_t(a.D * es), s));
+      return CCONV_OK;
+    }
+    NormParams p = norm_params(a);
+    p.nb = norm_backward_blocks(a.T, a.D, type_bytes(a.dtype), sms);
+    p.part = static_cast<float*>(a.workspace);
+    const int rc = block_status_word(&p.status);
+    if (rc != CCONV_OK) return rc;
+    p.limit_ns = block_wait_limit_ns();
+    return block_cuda_error(run_norm_backward(p, a.dtype, s), "cconv_residual_norm_backward");
+  });
 }
 
 int64_t cconv_fp8_product_workspace(const cconv_fp8_product_args* args) {
-  if (!args || !fp8_sizes_ok(*args)) return CCONV_EINVAL;
-  const int sms = block_sm_count();
-  if (sms < 0) return sms;
-  return fp8_empty(*args) ? 0 : fp8_workspace(*args, sms);
+  return guarded([&]() -> int64_t {
+    if (!args || !fp8_sizes_ok(*args)) return CCONV_EINVAL;
+    const int sms = block_sm_count();
+    if (sms < 0) return sms;
+    return fp8_empty(*args) ? 0 : fp8_workspace(*args, sms);
+  });
 }
 
 int cconv_fp8_product(const cconv_fp8_product_args* args, void* cuda_stream) {
-  if (!args || !fp8_sizes_ok(*args)) return CCONV_EINVAL;
-  const cconv_fp8_product_args& a = *args;
-  const int es = type_bytes(a.dtype);
-  Operands o;
-  o.in(a.a, a.M, a.K, 1);
-  o.in(a.b, a.N, a.K, 1);
-  o.in(a.a_scale, a.M, cdiv64(a.K, 128), 4);
-  o.in(a.b_scale, cdiv64(a.N, 128), cdiv64(a.K, 128), 4);
-  o.out(a.c, a.M, a.N, es);
-  if (!o.ok) return CCONV_EINVAL;
-  const int sms = block_sm_count();
-  if (sms < 0) return sms;
-  o.workspace(a.workspace, a.workspace_bytes, fp8_empty(a) ? 0 : fp8_workspace(a, sms));
-  if (!o.distinct()) return CCONV_EINVAL;
-  cudaStream_t s = static_cast<cudaStream_t>(cuda_stream);
-  o.note(cuda_stream, sms);
-  if (fp8_empty(a)) return block_cuda_error(zero_out(a.c, a.M, a.N, es, s), "cconv_fp8_product");
-  return run_fp8(a, sms, s);
+  return guarded([&]() -> int {
+    if (!args || !fp8_sizes_ok(*args)) return CCONV_EINVAL;
+    const cconv_fp8_product_args& a = *args;
+    const int es = type_bytes(a.dtype);
+    Operands o;
+    o.in(a.a, a.M, a.K, 1);
+    o.in(a.b, a.N, a.K, 1);
+    o.in(a.a_scale, a.M, cdiv64(a.K, 128), 4);
+    o.in(a.b_scale, cdiv64(a.N, 128), cdiv64(a.K, 128), 4);
+    o.out(a.c, a.M, a.N, es);
+    if (!o.distinct()) return CCONV_EINVAL;
+    const int sms = block_sm_count();
+    if (sms < 0) return sms;
+    o.workspace(a.workspace, a.workspace_bytes, fp8_empty(a) ? 0 : fp8_workspace(a, sms));
+    if (!o.distinct()) return CCONV_EINVAL;
+    cudaStream_t s = static_cast<cudaStream_t>(cuda_stream);
+    o.note(cuda_stream, sms);
+    if (fp8_empty(a)) return block_cuda_error(zero_out(a.c, a.M, a.N, es, s), "cconv_fp8_product");
+    return run_fp8(a, sms, s);
+  });
 }
 
 int cconv_quantize_blocks(const cconv_quantize_args* args, void* cuda_stream) {
-  if (!args) return CCONV_EINVAL;
-  const cconv_quantize_args& a = *args;
-  if (!length_ok(a.T) || !length_ok(a.D) || a.dtype < CCONV_TYPE_BF16 || a.dtype > CCONV_TYPE_FP32 ||
-      (a.block_rows != 1 && a.block_rows != 128) || double(a.T) * a.D >= 1e15)
-    return CCONV_EINVAL;
-  Operands o;
-  o.in(a.x, a.T, a.D, type_bytes(a.dtype));
-  o.out(a.q, a.T, a.D, 1);
-  o.out(a.scale, cdiv64(a.T, a.block_rows), cdiv64(a.D, 128), 4);
-  if (!o.distinct()) return CCONV_EINVAL;
-  const int sms = block_sm_count();
-  if (sms < 0) return sms;
-  if (a.T == 0 || a.D == 0) return CCONV_OK;
-  QuantParams p{};
-  p.T = a.T;
-  p.D = a.D;
-  p.x = a.x.data; p.x_rs = a.x.row_stride; p.x_cs = a.x.col_stride;
-  p.q = static_cast<uint8_t*>(a.q.data); p.q_rs = a.q.row_stride; p.q_cs = a.q.col_stride;
-  p.scale = static_cast<float*>(a.scale.data); p.scale_rs = a.scale.row_stride; p.scale_cs = a.scale.col_stride;
-  o.note(cuda_stream, sms);
-  return block_cuda_error(run_quantize(p, a.dtype, a.block_rows, sms, static_cast<cudaStream_t>(cuda_stream)),
-                          "cconv_quantize_blocks");
+  return guarded([&]() -> int {
+    if (!args) return CCONV_EINVAL;
+    const cconv_quantize_args& a = *args;
+    if (!length_ok(a.T) || !length_ok(a.D) || a.dtype < CCONV_TYPE_BF16 || a.dtype > CCONV_TYPE_FP32 ||
+        (a.block_rows != 1 && a.block_rows != 128) || double(a.T) * a.D >= 1e15)
+      return CCONV_EINVAL;
+    Operands o;
+    o.in(a.x, a.T, a.D, type_bytes(a.dtype));
+    o.out(a.q, a.T, a.D, 1);
+    o.out(a.scale, cdiv64(a.T, a.block_rows), cdiv64(a.D, 128), 4);
+    if (!o.distinct()) return CCONV_EINVAL;
+    const int sms = block_sm_count();
+    if (sms < 0) return sms;
+    if (a.T == 0 || a.D == 0) return CCONV_OK;
+    QuantParams p{};
+    p.T = a.T;
+    p.D = a.D;
+    p.x = a.x.data; p.x_rs = a.x.row_stride; p.x_cs = a.x.col_stride;
+    p.q = static_cast<uint8_t*>(a.q.data); p.q_rs = a.q.row_stride; p.q_cs = a.q.col_stride;
+    p.scale = static_cast<float*>(a.scale.data); p.scale_rs = a.scale.row_stride; p.scale_cs = a.scale.col_stride;
+    o.note(cuda_stream, sms);
+    return block_cuda_error(run_quantize(p, a.dtype, a.block_rows, sms, static_cast<cudaStream_t>(cuda_stream)),
+                            "cconv_quantize_blocks");
+  });
 }
 
 int cconv_block_status(void* cuda_stream, int* detail_out) {
-  if (detail_out) *detail_out = 0;
-  const int sms = block_sm_count();
-  if (sms < 0) return sms;
-  int* word = nullptr;
-  const int rc = block_status_word(&word);
-  if (rc != CCONV_OK) return rc;
-  cudaStream_t s = static_cast<cudaStream_t>(cuda_stream);
-  int bits = 0;
-  BLOCK_CUDA(cudaMemcpyAsync(&bits, word, sizeof bits, cudaMemcpyDeviceToHost, s));
-  BLOCK_CUDA(cudaStreamSynchronize(s));
-  if (bits == 0) return CCONV_OK;
-  if (detail_out) *detail_out = bits;
-  BLOCK_CUDA(cudaMemsetAsync(word, 0, sizeof bits, s));
-  BLOCK_CUDA(cudaStreamSynchronize(s));
-  return CCONV_EDEVICE_TIMEOUT;
+  return guarded([&]() -> int {
+    if (detail_out) *detail_out = 0;
+    const int sms = block_sm_count();
+    if (sms < 0) return sms;
+    int* word = nullptr;
+    const int rc = block_status_word(&word);
+    if (rc != CCONV_OK) return rc;
+    cudaStream_t s = static_cast<cudaStream_t>(cuda_stream);
+    int bits = 0;
+    BLOCK_CUDA(cudaMemcpyAsync(&bits, word, sizeof bits, cudaMemcpyDeviceToHost, s));
+    BLOCK_CUDA(cudaStreamSynchronize(s));
+    if (bits == 0) return CCONV_OK;
+    if (detail_out) *detail_out = bits;
+    BLOCK_CUDA(cudaMemsetAsync(word, 0, sizeof bits, s));
+    BLOCK_CUDA(cudaStreamSynchronize(s));
+    return CCONV_EDEVICE_TIMEOUT;
+  });
 }
 
 }  // extern "C"

@@ -15,6 +15,7 @@
 // Roles: warps 0 and 3 copy (TMA), warp 1 of the first CTA issues MMAs, warp 2 owns the tensor memory, warps
 // 4-11 are the epilogue (two for each quarter of the lanes, half of the columns each).
 #include <algorithm>
+#include <cstdio>
 #include <cstdlib>
 
 #include "block.h"
@@ -417,7 +418,8 @@ __global__ void __launch_bounds__(kThreads, 1) cconv_pair_product_kernel(
               break;
             }
             tc_fence_after();
-            const uint32_t a = base + s * p.stage_bytes;
+            // (a descriptor takes 18 bits of an address; above them lies the CTA's rank in its cluster)
+            const uint32_t a = (base + s * p.stage_bytes) & 0x3ffffu;
             if (issue) {
               const uint64_t da = a_desc + (a >> 4), db = b_desc + ((a + p.a_stage) >> 4);
 #pragma unroll
@@ -1078,6 +1080,9 @@ void choose_cut(Launch* l, int sms, bool few_columns) {
   Product& p = l->of[0];
   const int es = l->epilogue == kScaled ? 1 : 2;
   const int64_t kb = cdiv64(p.K, 128 / es) * (p.segments ? 2 : 1);
+  int force_n = 0, force_s = 0;  // diagnostics: columns of a tile, pairs that share it
+  if (const char* v = std::getenv("CCONV_BLOCK_CUT"))
+    if (std::sscanf(v, "%d,%d", &force_n, &force_s) != 2) force_n = force_s = 0;
   double best = 0;
   int best_n = 0, best_s = 1;
   for (int n = 256; n >= 64; n /= 2) {
@@ -1087,7 +1092,9 @@ void choose_cut(Launch* l, int sms, bool few_columns) {
       if (s > 1 && (s - 1) * cdiv64(kb, s) >= kb) continue;      // every pair has a part
       if ((p.paired ? 128 : n) / 32 < s) continue;                // and 32 columns to finish
       cut(l, n, s);
-      const double c = launch_clocks(*l, sms);
+      double c = launch_clocks(*l, sms);
+      if (n == force_n) c *= 1e-3;
+      if (s == force_s) c *= 1e-3;
       if (best_n == 0 || c < best) best = c, best_n = n, best_s = s;
     }
   }

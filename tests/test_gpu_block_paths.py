@@ -1,0 +1,178 @@
+"""The feed-forward sub-block where its pieces meet: every cut of a product, offsets past 32 bits, the order of
+a stream that convolutions share, other devices' streams, and the command that runs all of it together."""
+import pytest
+import torch
+
+from paper_1802_06905_b200 import binding, block
+from test_gpu_block import BF16, E4M3, FP16, FP32, Ffn, Norm, close, fp8_check, fp8_operands, gen, normal, poisoned
+
+pytestmark = pytest.mark.gpu
+
+
+# T, D, F that take: cuts of a tile over 2 and 4 pairs (few tiles, long k), 64-column tiles, several rounds of
+# tiles, the gradients together and apart, tokens of one CTA only and of two
+@pytest.mark.parametrize("T,D,F", [(16, 2048, 4096), (48, 512, 8192), (100, 4096, 256), (130, 264, 8200), (200, 128, 6000),
+                                   (260, 8192, 128), (700, 1000, 2600), (1500, 72, 4000), (2000, 2048, 136), (4100, 512, 520),
+                                   (4096, 64, 64)])
+def test_ffn_cuts(T, D, F):
+    f = Ffn(T, D, F, BF16 if T % 3 else FP16, "silu")
+    f.check_forward(*f.forward(True), "forward")
+    f.check_backward(*f.backward(), "backward")
+    assert block.status() == (0, 0)
+
+
+@pytest.mark.parametrize("M,N,K", [(12, 128, 16384), (50, 300, 8192), (150, 1000, 4096), (300, 128, 10000), (600, 4096, 256),
+                                   (2000, 2100, 520), (1100, 136, 130), (20, 8192, 144)])
+def test_fp8_cuts(M, N, K):
+    a, sa, b, sb = fp8_operands(M, N, K)
+    for dtype in (BF16, FP32):
+        out = poisoned((M, N), dtype)
+        block.fp8_product(a, sa, b, sb, out)
+        fp8_check(a, sa, b, sb, out)
+    assert block.status() == (0, 0)
+
+
+def far_rows(t, pitch):
+    """The same values in rows `pitch` elements apart, so that offsets pass 2^31 elements."""
+    buf = torch.empty(pitch * (t.shape[0] - 1) + t.shape[1], dtype=t.dtype, device="cuda")
+    v = buf.as_strided(t.shape, (pitch, 1))
+    v.copy_(t)
+    return v
+
+
+def test_offsets_past_32_bits():
+    pitch = (1 << 30) + 64
+    f = Ffn(4, 256, 384)
+    f.x = far_rows(f.x, pitch)
+    f.check_forward(*f.forward(True))
+    f.check_backward(*f.backward())
+    del f
+    torch.cuda.empty_cache()
+    n = Norm(4, 256, BF16, "all")
+    n.r, n.y = far_rows(n.r, pitch), n.y
+    n.check(*n.run())
+    out = far_rows(torch.zeros(4, 256, device="cuda", dtype=BF16), pitch)
+    n.check(*n.run(out=out))
+    del n, out
+    torch.cuda.empty_cache()
+    x = far_rows(normal(gen(1), (4, 256), BF16), pitch)
+    q, s = torch.empty((4, 256), device="cuda", dtype=E4M3), poisoned((4, 2), FP32)
+    block.quantize_blocks(x, q, s)
+    q2, s2 = torch.empty_like(q), poisoned((4, 2), FP32)
+    block.quantize_blocks(x.contiguous(), q2, s2)
+    assert torch.equal(q.float(), q2.float()) and torch.equal(s, s2)
+
+
+def conv_chain(T, steps, sync):
+    """A convolution whose Image a residual norm writes and whose Out a quantisation and the next norm read,
+    over and over in the same buffers; with a synchronisation after each call, or none."""
+    B, C, K = 64, 64, 128
+    g = gen(4)
+    rows = normal(g, (9 * C, B), BF16)            # the Image [3][3][C][B] as rows of B
+    w = normal(g, (B,), BF16)
+    filt = normal(g, (K, 3, 3, C), BF16, (9 * C) ** -0.5)
+    image = torch.empty((9 * C, B), dtype=BF16, device="cuda")
+    out = torch.empty((K, 1, 1, B), dtype=BF16, device="cuda")
+    q, s = torch.empty((K, B), dtype=E4M3, device="cuda"), torch.empty((K, 1), device="cuda")
+    got = []
+
+    def done():
+        if sync:
+            torch.cuda.synchronize()
+    for i in range(steps):
+        block.residual_norm_forward(rows, rows, image, w_pre=w, scale=0.9)
+        done()
+        binding.conv_forward(image.view(3, 3, C, B), filt, out, B, C, K, 1, 1, 3, 3)
+        done()
+        block.quantize_blocks(out.view(K, B), q, s)
+        done()
+        block.residual_norm_forward(out.view(K, B), rows[:K], w_pre=None, scale=1.25)
+        done()
+        if i % 8 == 7:
+            got.append((image.clone(), out.clone(), q.float(), s.clone(), rows.clone()))
+            done()
+    torch.cuda.synchronize()
+    return got
+
+
+def test_stream_order_with_convolutions():
+    want = conv_chain(0, 40, True)
+    for _ in range(5):
+        for a, b in zip(want, conv_chain(0, 40, False)):
+            for x, y in zip(a, b):
+                assert torch.equal(x, y)
+
+
+def test_a_chain_of_calls_without_waiting_equals_one_with():
+    """Quantise, product, norm, feed-forward in shared buffers: every call reads what the one in front wrote."""
+    g = gen(8)
+    T, D, F = 24, 256, 512
+    w8, s8 = torch.empty((D, D), device="cuda", dtype=E4M3), poisoned((2, 2), FP32)
+    wq = normal(g, (D, D), BF16, D ** -0.5)
+    wg, wu, wd = normal(g, (F, D), BF16, D ** -0.5), normal(g, (F, D), BF16, D ** -0.5), normal(g, (D, F), BF16, F ** -0.5)
+    w = normal(g, (D,), BF16)
+
+    def chain(tokens, sync):
+        x = normal(gen(9), (tokens, D), BF16)
+        res, q, s = x.clone(), torch.empty((tokens, D), device="cuda", dtype=E4M3), poisoned((tokens, 2), FP32)
+        y = torch.empty_like(x)
+        for _ in range(25):
+            for call in (lambda: block.quantize_blocks(wq, w8, s8, block_rows=128), lambda: block.quantize_blocks(x, q, s),
+                         lambda: block.fp8_product(q, s, w8, s8, y), lambda: block.ffn_forward(y, wg, wu, wd, x),
+                         lambda: block.residual_norm_forward(res, res, y, block=x, w_post=w, w_pre=w, scale=0.5),
+                         lambda: block.ffn_forward(y, wg, wu, wd, x)):
+                call()
+                if sync:
+                    torch.cuda.synchronize()
+        torch.cuda.synchronize()
+        return x, y, res, q.float(), s
+    for tokens in (1, 5, T, 300):
+        want = chain(tokens, True)
+        for _ in range(3):
+            for a, b in zip(want, chain(tokens, False)):
+                assert torch.equal(a, b)
+
+
+def test_two_streams_at_once():
+    f, h = Ffn(300, 512, 1408), Ffn(40, 1024, 2048, seed=3)
+    want = f.forward(True) + h.forward(True)
+    a, b = torch.cuda.Stream(), torch.cuda.Stream()
+    torch.cuda.synchronize()
+    for _ in range(10):
+        with torch.cuda.stream(a):
+            p = f.forward(True)
+        with torch.cuda.stream(b):
+            q = h.forward(True)
+        torch.cuda.synchronize()
+        for x, y in zip(want, p + q):
+            assert torch.equal(x, y)
+    assert block.status() == (0, 0)
+
+
+def test_the_command_runs_a_block():
+    from paper_1802_06905_b200 import ffn_block
+    r = ffn_block.run(tokens=96, channels=256, hidden=512, steps=6, serve=3)
+    assert r["loss"][-1] < 0.9 * r["loss"][0]
+    assert r["serve_error"] < 0.1                   # 8-bit operands: 2^-4 of a factor at worst, less on average
+
+
+@pytest.mark.parametrize("cut", ["256,1", "256,2", "256,4", "128,1", "128,2", "128,4", "64,1", "64,2"])
+def test_every_cut_in_every_storage_order(cut, monkeypatch):
+    """The diagnostic switch makes every product take the cut where it can; operands in both orders."""
+    monkeypatch.setenv("CCONV_BLOCK_CUT", cut)
+    flip = lambda t: t.t().contiguous().t()  # noqa: E731
+    for T, D, F, dtype in ((24, 512, 640, BF16), (300, 520, 1032, FP16)):
+        f = Ffn(T, D, F, dtype, "gelu")
+        for names in ((), ("x", "dy"), ("wg", "wu", "wd"), ("x", "wg", "wu", "wd", "dy")):
+            h = Ffn(T, D, F, dtype, "gelu")
+            for n in names:
+                setattr(h, n, flip(getattr(f, n)))
+            h.check_forward(*h.forward(True), f"{cut} {names}")
+            h.check_backward(*h.backward(), f"{cut} {names}")
+    for M, N, K in ((20, 300, 1100), (300, 520, 2048)):
+        a, sa, b, sb = fp8_operands(M, N, K)
+        for dtype in (BF16, FP32):
+            out = poisoned((M, N), dtype)
+            block.fp8_product(a, sa, b, sb, out)
+            fp8_check(a, sa, b, sb, out, cut)
+    assert block.status() == (0, 0)
