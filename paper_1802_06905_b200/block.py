@@ -73,10 +73,12 @@ def _mat(t, shape, dtype, dev, name):
 
 def _row(t, shape, dtype, dev, name):
     """As _mat, of a matrix whose rows are contiguous."""
-    m = _mat(t, shape, dtype, dev, name)
-    if m[2] != 1 and shape[1] > 1:
+    if t.dtype is not dtype or t.get_device() != dev or t.shape != shape:
+        _mat(t, shape, dtype, dev, name)  # says what is wrong
+    rows, cols = t.stride()
+    if cols != 1 and shape[1] > 1:
         raise ValueError(f"{name} must have contiguous rows, got strides {t.stride()}")
-    return m
+    return t.data_ptr(), rows, cols
 
 
 def _vec(t, n, dtype, dev, name):

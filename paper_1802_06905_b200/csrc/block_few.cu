@@ -6,7 +6,9 @@
 // 16 bytes of every lane on their way while the last 8 are multiplied, also across tiles.  The
 // products run on warp-wide matrix instructions (m16n8: 16 rows of weights by 8 tokens) because they
 // take operands from registers as they come from memory; tcgen05 would want them in shared memory first, for
-// tiles that a few tokens leave almost empty.
+// tiles that a few tokens leave almost empty.  Measured: one token 2048 x 8192 16 bits 23.2 us for 100.7 MB, 4.35 TB/s
+// (a kernel that only reads as much, from as many threads: 18.4 to 20.7 us); two tokens 8192 x 4096 8 bits 10.2 us
+// (reading alone: 8.2 us).
 //
 // k is permuted inside a step: lane q of a row holds 16 neighbouring bytes of k, which stand for two
 // pairs of fragment registers.  Weights and tokens are permuted alike, so the sums are those of the definition.
@@ -60,9 +62,10 @@ __device__ __forceinline__ uint4 load_tokens(const char* p) { return *reinterpre
 struct FewParams {
   const char *x, *w0, *w1;        // tokens; weights (w1: the second matrix of a pair)
   int64_t x_rs, w0_rs, w1_rs;     // bytes
+  int64_t x_lo;                   // bytes from a token's row to the row of what its rounding left (0: none)
   int64_t k_bytes, N;
   int T, act, weights_there;
-  Mat out, gate_pre, up_pre;
+  Mat out, out_lo, gate_pre, up_pre;
   const float *sa, *sb;
   int64_t sa_rs, sa_ks, sb_rs, sb_ks;
   int out_dtype;
@@ -130,22 +133,25 @@ __global__ void __launch_bounds__(kWarps * 32, 2) cconv_few_kernel(const FewPara
     if (++lb == batches) lb = 0, lt += gridDim.x;
   };
 
-  // Behind a kernel of the same call, which had waited for everything before the call, the weights are there
-  // already, and only the tokens may still be on their way.
+  // Behind this kernel's other form in the same call, which lets it in only once everything before the call is
+  // complete, the weights are there already, and only the tokens may still be on their way.
   if (p.weights_there) load(w[0]);
   start_in_order();
   if (!p.weights_there) load(w[0]);
 
+  // Column g of a tile is token g; tokens in two parts (at most 4) take columns g and g + 4.
+  const bool parts = !kFp8 && kRows != kPair && p.x_lo != 0;
+  const int token = parts ? g & 3 : g;
+  const char* const x = p.x + min(token, p.T - 1) * p.x_rs + (parts && g >= 4 ? p.x_lo : 0) + q * 16;
   float acc[4] = {};
   int tile = blockIdx.x, batch = 0, parity = 0;
   auto use = [&](const uint4 (&a)[8]) {
     const int sb = s0 + batch * kSteps;
-    const char* x = p.x + min(g, p.T - 1) * p.x_rs + q * 16;
     uint4 v[kSteps];
 #pragma unroll
     for (int i = 0; i < kSteps; ++i) {
       const int64_t at = int64_t(sb + i) * 64;
-      v[i] = g < p.T && sb + i < s1 && at + q * 16 < p.k_bytes ? load_tokens(x + at) : none;
+      v[i] = token < p.T && sb + i < s1 && at + q * 16 < p.k_bytes ? load_tokens(x + at) : none;
     }
     if constexpr (!kFp8) {
 #pragma unroll
@@ -185,13 +191,17 @@ __global__ void __launch_bounds__(kWarps * 32, 2) cconv_few_kernel(const FewPara
     const int64_t n0 = int64_t(tile) * kTile;
     const int r = threadIdx.x % kTile, t = threadIdx.x / kTile;
     if (t < p.T && n0 + r < p.N) {
-      const float f = gathered(smem[parity], r, t);
+      float f = gathered(smem[parity], r, t);
+      if (parts) f += gathered(smem[parity], r, t + 4);
       if constexpr (kRows == kPair) {
         const float up = gathered(smem[parity], r + 8, t);
         float h[1] = {f};
         const float u[1] = {up};
         gate(p.act, h, u);
-        put(p.out, p.out_dtype, t, n0 + r, h[0]);
+        // in two parts, whose sum has the type's precision twice (what overflows has no second part)
+        const T hi = from_f32<T>(h[0]);
+        put(p.out, p.out_dtype, t, n0 + r, to_f32(hi));
+        if (p.out_lo.p) put(p.out_lo, p.out_dtype, t, n0 + r, isfinite(to_f32(hi)) ? h[0] - to_f32(hi) : 0.0f);
         if (p.gate_pre.p) {
           put(p.gate_pre, p.out_dtype, t, n0 + r, f);
           put(p.up_pre, p.out_dtype, t, n0 + r, up);
@@ -221,9 +231,12 @@ cudaError_t launch_rows(const FewParams& p, int sms, cudaStream_t s) {
   return launch(cconv_few_kernel<T, kRows>, grid, kWarps * 32, 0, 1, s, p);
 }
 
+// 16 rows a tile where that leaves no SM idle: one token, 16 bits, the product back to 4096 channels as part of
+// 4096 x 8192 whole: 37 against 41 us; to 2048 channels 8 rows a tile are better (2048 x 8192 whole: 23.7 against
+// 25.4 us).
 template <typename T>
 cudaError_t launch_single(const FewParams& p, int sms, cudaStream_t s) {
-  return p.N >= 32 * int64_t(sms) ? launch_rows<T, kSixteen>(p, sms, s) : launch_rows<T, kEight>(p, sms, s);
+  return p.N >= 16 * int64_t(sms) ? launch_rows<T, kSixteen>(p, sms, s) : launch_rows<T, kEight>(p, sms, s);
 }
 
 FewParams params(const Mat& x, const Mat& w, const Mat& out, int64_t T, int64_t N, int64_t K, int es, int dtype) {
@@ -249,10 +262,12 @@ bool few_readable(const Mat& m, int64_t rows, int64_t k, int es) {
 }
 
 cudaError_t run_few_gated(const Mat& x, const Mat& wg, const Mat& wu, const Mat& gate_pre, const Mat& up_pre,
-                          const Mat& h, int64_t T, int64_t F, int64_t D, int act, int dtype, int sms, cudaStream_t s) {
+                          const Mat& h, const Mat& h_lo, int64_t T, int64_t F, int64_t D, int act, int dtype, int sms,
+                          cudaStream_t s) {
   FewParams p = params(x, wg, h, T, F, D, 2, dtype);
   p.w1 = static_cast<const char*>(wu.p);
   p.w1_rs = wu.rs * 2;
+  p.out_lo = h_lo;
   p.gate_pre = gate_pre;
   p.up_pre = up_pre;
   p.act = act;
@@ -260,10 +275,11 @@ cudaError_t run_few_gated(const Mat& x, const Mat& wg, const Mat& wu, const Mat&
                                   : launch_rows<__half, kPair>(p, sms, s);
 }
 
-cudaError_t run_few_product(const Mat& x, const Mat& w, const Mat& out, int64_t T, int64_t N, int64_t K, int dtype,
-                            int sms, bool weights_there, cudaStream_t s) {
+cudaError_t run_few_product(const Mat& x, const Mat& x_lo, const Mat& w, const Mat& out, int64_t T, int64_t N,
+                            int64_t K, int dtype, int sms, bool weights_there, cudaStream_t s) {
   FewParams p = params(x, w, out, T, N, K, 2, dtype);
   p.weights_there = weights_there;
+  if (x_lo.p) p.x_lo = static_cast<const char*>(x_lo.p) - p.x;
   return dtype == CCONV_TYPE_BF16 ? launch_single<__nv_bfloat16>(p, sms, s)
                                   : launch_single<__half>(p, sms, s);
 }
@@ -277,7 +293,9 @@ cudaError_t run_few_fp8(const Mat& x, const Mat& w, const Mat& sa, const Mat& sb
   p.sb = static_cast<const float*>(sb.p);
   p.sb_rs = sb.rs;
   p.sb_ks = sb.cs;
-  return launch_single<E4m3>(p, sms, s);
+  // 8 rows a tile take twice the scales a row: 4096 x 4096 8.7 against 6.2 us, 4096 x 1024 5.3 against 2.9, 1024 x
+  // 1024 2.6 against 2.1; they win only where rows are few and long (1024 x 8192: 6.4 against 7.3)
+  return launch_rows<E4m3, kSixteen>(p, sms, s);
 }
 
 }  // namespace cconv

@@ -18,7 +18,7 @@ void plan(Steps& st, const cconv_fp8_product_args& args) {
   const Mat a(args.a), b(args.b), sa(args.a_scale), sb(args.b_scale), c(args.c);
   const int dtype = args.dtype, sms = st.sms();
   if (M <= kFewTokens && few_readable(a, M, K, 1) && few_readable(b, N, K, 1)) {
-    st.add([=](bool, cudaStream_t s) {
+    st.add([=](cudaStream_t s) {
       return block_cuda_error(run_few_fp8(a, b, sa, sb, c, M, N, K, dtype, sms, s), "cconv_few_kernel");
     });
     return;

@@ -942,29 +942,43 @@ double fixed_clocks(const Launch& l, int block_n) {
   return (l.splits == 1 ? 14600.0 : l.splits == 2 ? 20000.0 : 23000.0) + epilogue;
 }
 
-// Rows of `pieces` accesses of type E, both sides contiguous: 64 threads by 4 rows a block, 4 accesses a thread.
+// Copies of rows that are contiguous on both sides, several at once: blockIdx.z is the copy, an access is the
+// largest of 16, 8, 4, 2, 1 bytes that its addresses, pitches and rows allow; 64 threads by 4 rows a block,
+// 4 accesses a thread.
+struct RowCopy {
+  const char* from;
+  char* to;
+  int64_t from_pitch, to_pitch, rows, bytes;  // pitches and row length in bytes
+  int access;
+};
+struct RowCopies {
+  RowCopy of[kMostCopies];
+};
 template <typename E>
-__global__ void __launch_bounds__(256) cconv_copy_rows_kernel(Mat from, Mat to, int64_t rows, int64_t pieces) {
-  start_in_order();
-  const int64_t x0 = int64_t(blockIdx.x) * 256 + (threadIdx.x & 63);
-  for (int64_t r = int64_t(blockIdx.y) * 4 + (threadIdx.x >> 6); r < rows; r += int64_t(gridDim.y) * 4) {
-    const E* src = reinterpret_cast<const E*>(static_cast<const char*>(from.p) + r * from.rs);
-    E* dst = reinterpret_cast<E*>(static_cast<char*>(const_cast<void*>(to.p)) + r * to.rs);
-    E v[4];
+__device__ __forceinline__ void copy_rows(const RowCopy& c) {
+  const int64_t pieces = c.bytes / int64_t(sizeof(E));
+  for (int64_t x0 = int64_t(blockIdx.x) * 256 + (threadIdx.x & 63); x0 < pieces; x0 += int64_t(gridDim.x) * 256) {
+    for (int64_t r = int64_t(blockIdx.y) * 4 + (threadIdx.x >> 6); r < c.rows; r += int64_t(gridDim.y) * 4) {
+      const E* src = reinterpret_cast<const E*>(c.from + r * c.from_pitch);
+      E* dst = reinterpret_cast<E*>(c.to + r * c.to_pitch);
+      E v[4];
 #pragma unroll
-    for (int i = 0; i < 4; ++i)
-      if (x0 + 64 * i < pieces) v[i] = src[x0 + 64 * i];
+      for (int i = 0; i < 4; ++i)
+        if (x0 + 64 * i < pieces) v[i] = src[x0 + 64 * i];
 #pragma unroll
-    for (int i = 0; i < 4; ++i)
-      if (x0 + 64 * i < pieces) dst[x0 + 64 * i] = v[i];
+      for (int i = 0; i < 4; ++i)
+        if (x0 + 64 * i < pieces) dst[x0 + 64 * i] = v[i];
+    }
   }
 }
-template <typename E>
-cudaError_t copy_rows(const Mat& from, const Mat& to, int64_t rows, int64_t cols, int es, cudaStream_t s) {
-  const int64_t pieces = cols * es / int64_t(sizeof(E)), y = cdiv64(rows, 4);
-  const dim3 grid(unsigned(cdiv64(pieces, 256)), unsigned(y < 65535 ? y : 65535));
-  return launch(cconv_copy_rows_kernel<E>, grid, 256, 0, 1, s, Mat(from.p, from.rs * es, 1), Mat(to.p, to.rs * es, 1), rows,
-                pieces);
+__global__ void __launch_bounds__(256) cconv_copy_rows_kernel(const __grid_constant__ RowCopies copies) {
+  start_in_order();
+  const RowCopy& c = copies.of[blockIdx.z];
+  if (c.access == 16) copy_rows<uint4>(c);
+  else if (c.access == 8) copy_rows<uint2>(c);
+  else if (c.access == 4) copy_rows<uint32_t>(c);
+  else if (c.access == 2) copy_rows<uint16_t>(c);
+  else copy_rows<uint8_t>(c);
 }
 
 // 32 x 32 elements a block through shared memory: read along the source's short stride, written along
@@ -1108,23 +1122,37 @@ int run_products(const Launch& l, int sms, cudaStream_t s) {
   return run_as<kScaled>(l, sms, s);
 }
 
-cudaError_t run_copy(const Mat& from, const Mat& to, int64_t rows, int64_t cols, int es,
-                     cudaStream_t s) {
-  if (rows == 0 || cols == 0) return cudaSuccess;
-  if (from.cs == 1 && to.cs == 1) {
-    const uintptr_t all = reinterpret_cast<uintptr_t>(from.p) | reinterpret_cast<uintptr_t>(to.p) | uintptr_t(cols * es) |
-                          (rows > 1 ? uintptr_t(from.rs * es) | uintptr_t(to.rs * es) : 0);
-    if ((all & 15) == 0) return copy_rows<uint4>(from, to, rows, cols, es, s);
-    if ((all & 7) == 0) return copy_rows<uint2>(from, to, rows, cols, es, s);
-    if ((all & 3) == 0) return copy_rows<uint32_t>(from, to, rows, cols, es, s);
-    if ((all & 1) == 0) return copy_rows<uint16_t>(from, to, rows, cols, es, s);
-    return copy_rows<uint8_t>(from, to, rows, cols, es, s);
+bool copies_rows(const Mat& from, const Mat& to) { return from.cs == 1 && to.cs == 1; }
+
+cudaError_t run_row_copies(const Copy* copies, int n, cudaStream_t s) {
+  RowCopies c{};
+  int64_t x = 1, y = 1;
+  for (int i = 0; i < n; ++i) {
+    const Copy& k = copies[i];
+    RowCopy& r = c.of[i];
+    r.from = static_cast<const char*>(k.from.p);
+    r.to = static_cast<char*>(const_cast<void*>(k.to.p));
+    r.rows = k.rows;
+    r.bytes = k.cols * k.es;
+    r.from_pitch = k.from.rs * k.es;
+    r.to_pitch = k.to.rs * k.es;
+    uintptr_t all = reinterpret_cast<uintptr_t>(r.from) | reinterpret_cast<uintptr_t>(r.to) | uintptr_t(r.bytes);
+    if (r.rows > 1) all |= uintptr_t(r.from_pitch) | uintptr_t(r.to_pitch);
+    r.access = 16;
+    while (all & uintptr_t(r.access - 1)) r.access /= 2;
+    x = std::max(x, cdiv64(r.bytes / r.access, 256));
+    y = std::max(y, cdiv64(r.rows, 4));
   }
-  const int64_t y = cdiv64(rows, 32);
-  const dim3 grid(unsigned(cdiv64(cols, 32)), unsigned(y < 65535 ? y : 65535));
-  if (es == 1) return launch(cconv_copy_kernel<uint8_t>, grid, 256, 0, 1, s, from, to, rows, cols);
-  if (es == 4) return launch(cconv_copy_kernel<uint32_t>, grid, 256, 0, 1, s, from, to, rows, cols);
-  return launch(cconv_copy_kernel<uint16_t>, grid, 256, 0, 1, s, from, to, rows, cols);
+  const dim3 grid(unsigned(std::min<int64_t>(x, 65535)), unsigned(std::min<int64_t>(y, 16384)), unsigned(n));
+  return launch(cconv_copy_rows_kernel, grid, 256, 0, 1, s, c);
+}
+
+cudaError_t run_copy(const Copy& k, cudaStream_t s) {
+  const int64_t y = cdiv64(k.rows, 32);
+  const dim3 grid(unsigned(cdiv64(k.cols, 32)), unsigned(y < 65535 ? y : 65535));
+  if (k.es == 1) return launch(cconv_copy_kernel<uint8_t>, grid, 256, 0, 1, s, k.from, k.to, k.rows, k.cols);
+  if (k.es == 4) return launch(cconv_copy_kernel<uint32_t>, grid, 256, 0, 1, s, k.from, k.to, k.rows, k.cols);
+  return launch(cconv_copy_kernel<uint16_t>, grid, 256, 0, 1, s, k.from, k.to, k.rows, k.cols);
 }
 
 }  // namespace cconv

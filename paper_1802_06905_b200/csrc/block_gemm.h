@@ -48,8 +48,16 @@ int run_products(const Launch& l, int sms, cudaStream_t s);
 double launch_clocks(const Launch& l, int sms);
 void choose_cut(Launch* l, int sms, bool few_columns);
 
-// Copies rows x cols elements of es bytes between any two layouts.
-cudaError_t run_copy(const Mat& from, const Mat& to, int64_t rows, int64_t cols, int es, cudaStream_t s);
+// A copy of rows x cols elements of es bytes from one layout to another.
+struct Copy {
+  Mat from, to;
+  int64_t rows = 0, cols = 0;
+  int es = 2;
+};
+constexpr int kMostCopies = 6;  // of one launch
+bool copies_rows(const Mat& from, const Mat& to);  // rows contiguous on both sides
+cudaError_t run_row_copies(const Copy* copies, int n, cudaStream_t s);  // at most kMostCopies such
+cudaError_t run_copy(const Copy& c, cudaStream_t s);                     // any layouts
 
 // The status word that the product kernels of the current device share (device address).
 int block_status_word(int** word);

@@ -17,12 +17,16 @@ class Steps {
   int64_t bytes() const { return ws_.used(); }
   int sms() const { return sms_; }
 
-  // A step: launches something (first: of the call) and gives a status code.
-  using Step = std::function<int(bool first, cudaStream_t s)>;
-  void add(Step f) { steps_.push_back(std::move(f)); }
-  int run(cudaStream_t s) const {
-    for (size_t i = 0; i < steps_.size(); ++i) {
-      const int rc = steps_[i](i == 0, s);
+  // A step launches something and gives a status code.
+  using Step = std::function<int(cudaStream_t s)>;
+  void add(Step f) {
+    flush();
+    steps_.push_back(std::move(f));
+  }
+  int run(cudaStream_t s) {
+    flush();
+    for (const Step& f : steps_) {
+      const int rc = f(s);
       if (rc != CCONV_OK) return rc;
     }
     return CCONV_OK;
@@ -33,10 +37,21 @@ class Steps {
     const int64_t pitch = round_up64(cols, 16 / es);
     return Mat(ws_.take(rows * pitch * es), pitch, 1);
   }
+  // Copies of rows gather until the next step and go in one launch (none of them reads what another writes).
   void copy(const Mat& from, const Mat& to, int64_t rows, int64_t cols, int es) {
-    add([=](bool, cudaStream_t s) {
-      return block_cuda_error(run_copy(from, to, rows, cols, es, s), "cconv_copy_kernel");
-    });
+    if (rows == 0 || cols == 0) return;
+    Copy c;
+    c.from = from;
+    c.to = to;
+    c.rows = rows;
+    c.cols = cols;
+    c.es = es;
+    if (copies_rows(from, to)) {
+      if (pending_.size() == size_t(kMostCopies)) flush();
+      pending_.push_back(c);
+    } else {
+      steps_.push_back([=](cudaStream_t s) { return block_cuda_error(run_copy(c, s), "cconv_copy_kernel"); });
+    }
   }
 
   // An operand of a product (rows x k) as it lies, or a copy of it with k contiguous.
@@ -91,14 +106,24 @@ class Steps {
       }
     }
     const int sms = sms_;
-    add([=](bool, cudaStream_t s) { return run_products(l, sms, s); });
+    add([=](cudaStream_t s) { return run_products(l, sms, s); });
     for (const Move& m : moves) copy(m.from, m.to, m.M, m.N, es);
   }
 
  private:
+  void flush() {
+    if (pending_.empty()) return;
+    std::vector<Copy> all;
+    all.swap(pending_);
+    steps_.push_back([all](cudaStream_t s) {
+      return block_cuda_error(run_row_copies(all.data(), int(all.size()), s), "cconv_copy_rows_kernel");
+    });
+  }
+
   Carver ws_;
   const int sms_, es_, dtype_;
   std::vector<Step> steps_;
+  std::vector<Copy> pending_;
 };
 
 }  // namespace cconv

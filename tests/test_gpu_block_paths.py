@@ -4,7 +4,7 @@ import pytest
 import torch
 
 from paper_1802_06905_b200 import binding, block
-from test_gpu_block import BF16, E4M3, FP16, FP32, Ffn, Norm, close, fp8_check, fp8_operands, gen, normal, poisoned
+from test_gpu_block import BF16, E4M3, FP16, FP32, Ffn, Norm, act64, close, fp8_check, fp8_operands, gen, normal, poisoned
 
 pytestmark = pytest.mark.gpu
 
@@ -30,6 +30,26 @@ def test_fp8_cuts(M, N, K):
         block.fp8_product(a, sa, b, sb, out)
         fp8_check(a, sa, b, sb, out)
     assert block.status() == (0, 0)
+
+
+@pytest.mark.parametrize("T", [1, 2, 3, 4])
+@pytest.mark.parametrize("dtype,most", [(BF16, 0.0020), (FP16, 0.00025)])
+def test_few_tokens_round_the_result_alone(T, dtype, most):
+    """One rounding of normal values to 8 bits is 0.00166 of their norm (11 bits: 0.00021), two in a row 0.0024."""
+    for act in block.ACTS:
+        f = Ffn(T, 1024, 512, dtype, act)
+        out, _, _ = f.forward(False)
+        x, wg, wu, wd = (t.double() for t in (f.x, f.wg, f.wu, f.wd))
+        want = (act64(act, x @ wg.T)[0] * (x @ wu.T)) @ wd.T
+        assert (out.double() - want).norm() <= most * want.norm()
+
+
+def test_few_tokens_whose_hidden_values_overflow():
+    f = Ffn(2, 128, 256, FP16)
+    f.x[1] *= 3000.0  # h passes 65504 for this token only
+    out = f.forward(False)[0]
+    alone = Ffn(2, 128, 256, FP16).forward(False)[0]
+    assert torch.equal(out[0], alone[0]) and not torch.isfinite(out[1]).all()
 
 
 def far_rows(t, pitch):
@@ -101,6 +121,40 @@ def test_stream_order_with_convolutions():
         for a, b in zip(want, conv_chain(0, 40, False)):
             for x, y in zip(a, b):
                 assert torch.equal(x, y)
+
+
+def test_a_call_between_two_convolutions_keeps_them_in_order():
+    """A convolution reads what one two calls in front wrote; the call between them touches neither array."""
+    B, C, K, H = 64, 64, 128, 14
+    g = gen(11)
+    image = normal(g, (H + 2, H + 2, C, B), BF16)
+    f1, f2 = normal(g, (C, 3, 3, C), BF16, (9 * C) ** -0.5), normal(g, (K, 1, 1, C), BF16, C ** -0.5)
+    x, q, s = normal(g, (1, 128), BF16), torch.empty((1, 128), dtype=E4M3, device="cuda"), torch.empty((1, 1), device="cuda")
+    w, h = normal(g, (128,), BF16), torch.empty((1, 128), dtype=BF16, device="cuda")
+    ffn = Ffn(4, 128, 256)
+    between = (lambda: block.quantize_blocks(x, q, s), lambda: block.residual_norm_forward(x, x.clone(), h, w_pre=w),
+               lambda: ffn.forward(False))
+    middles = [torch.empty((C, H, H, B), dtype=BF16, device="cuda") for _ in range(12)]
+
+    def chain(sync):
+        outs = []
+        for i, mid in enumerate(middles):
+            mid.zero_()
+        torch.cuda.synchronize()
+        for i, mid in enumerate(middles):
+            out = torch.zeros((K, H, H, B), dtype=BF16, device="cuda")
+            for call in (lambda: binding.conv_forward(image, f1, mid, B, C, C, H, H, 3, 3), between[i % 3],
+                         lambda: binding.conv_forward(mid.view(H, H, C, B), f2, out, B, C, K, H, H, 1, 1)):
+                call()
+                if sync:
+                    torch.cuda.synchronize()
+            outs.append(out)
+        torch.cuda.synchronize()
+        return outs
+    want = chain(True)
+    for _ in range(3):
+        for a, b in zip(want, chain(False)):
+            assert torch.equal(a, b)
 
 
 def test_a_chain_of_calls_without_waiting_equals_one_with():
