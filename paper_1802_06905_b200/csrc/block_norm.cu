@@ -13,6 +13,7 @@
 // at the rate of a copy); backward 149 us, 5.4 TB/s (6 arrays: 123 us), 135 of them the first kernel.  One token
 // of 4096 channels: 2.5 us on the device.
 #include <algorithm>
+#include <type_traits>
 
 #include "block.h"
 #include "block_device.cuh"
@@ -73,6 +74,107 @@ __device__ __forceinline__ float2 block_sum2(float a, float b, float2 (*smem)[32
   const float2 v = lane < warps ? smem[buf][lane] : make_float2(0.0f, 0.0f);
   buf ^= 1;
   return make_float2(warp_sum(v.x), warp_sum(v.y));
+}
+
+// Block b of the kernels that take neighbouring rows has the rows [T b / nb, T (b+1) / nb).
+template <typename T>
+__device__ __forceinline__ int64_t first_row(const NormParams& p, int64_t b) {
+  return p.T * b / p.nb;
+}
+
+// A ring in shared memory for rows that begin anywhere: a bulk copy brings the 16-byte pieces that a row lies
+// in, so that its first element lies as far behind the slot's start as in memory behind a multiple of 16.  Pieces
+// that reach out of the whole array (of its first and last row) stay behind; complete() fetches their elements.
+template <typename T, int kArrays>
+struct RowRing {
+  struct Span {
+    uintptr_t row, end, lo, hi;  // of the row; of the pieces that are copied
+  };
+  const T* base[kArrays];  // null: absent
+  int64_t rs[kArrays];
+  int64_t rows_of_all, row0, row1;
+  uint32_t row_bytes, slot, ring0, full0, stages;
+
+  __device__ __forceinline__ Span span(int a, int64_t t) const {
+    Span s;
+    const uintptr_t first = reinterpret_cast<uintptr_t>(base[a]);
+    s.row = first + uintptr_t(t * rs[a]) * sizeof(T);
+    s.end = s.row + row_bytes;
+    s.lo = s.row & ~uintptr_t(15);
+    s.hi = (s.end + 15) & ~uintptr_t(15);
+    if (s.lo < first) s.lo += 16;
+    if (s.hi > first + uintptr_t((rows_of_all - 1) * rs[a]) * sizeof(T) + row_bytes) s.hi -= 16;
+    return s;
+  }
+  __device__ __forceinline__ void copy(int64_t t) const {  // one thread
+    const uint32_t st = uint32_t(t - row0) % stages, bar = full0 + 8 * st, to = ring0 + st * kArrays * slot;
+    uint32_t bytes = 0;
+#pragma unroll
+    for (int a = 0; a < kArrays; ++a) {
+      if (!base[a]) continue;
+      const Span s = span(a, t);
+      bytes += uint32_t(s.hi - s.lo);
+    }
+    mbar_arrive_expect_tx(bar, bytes);
+#pragma unroll
+    for (int a = 0; a < kArrays; ++a) {
+      if (!base[a]) continue;
+      const Span s = span(a, t);
+      bulk_load(to + a * slot + uint32_t(s.lo - (s.row & ~uintptr_t(15))), reinterpret_cast<const void*>(s.lo),
+                uint32_t(s.hi - s.lo), bar);
+    }
+  }
+  __device__ __forceinline__ void begin() const {  // one thread
+    for (uint32_t i = 0; i < stages; ++i) mbar_init(full0 + 8 * i, 1);
+    fence_barrier_init();
+    for (int64_t t = row0; t < row1 && t < row0 + int64_t(stages); ++t) copy(t);
+  }
+  // Array a of row t, which lies in stage st.
+  __device__ __forceinline__ T* row(uint8_t* ring, int a, uint32_t st, int64_t t) const {
+    const uintptr_t at = reinterpret_cast<uintptr_t>(base[a] + t * rs[a]);
+    return reinterpret_cast<T*>(ring + (st * kArrays + a) * slot + (at & 15));
+  }
+  // All threads, once the copies of row t have landed.
+  __device__ __forceinline__ void complete(uint8_t* ring, uint32_t st, int64_t t) const {
+    if (t != 0 && t != rows_of_all - 1) return;
+#pragma unroll
+    for (int a = 0; a < kArrays; ++a) {
+      if (!base[a]) continue;
+      const Span s = span(a, t);
+      const uint32_t n = row_bytes / sizeof(T), head = s.lo > s.row ? uint32_t(s.lo - s.row) / sizeof(T) : 0,
+                     tail = s.end > s.hi ? uint32_t(s.end - s.hi) / sizeof(T) : 0;
+      if (threadIdx.x < head) row(ring, a, st, t)[threadIdx.x] = base[a][t * rs[a] + threadIdx.x];
+      if (threadIdx.x < tail) row(ring, a, st, t)[n - 1 - threadIdx.x] = base[a][t * rs[a] + n - 1 - threadIdx.x];
+    }
+    fence_proxy_async_smem();  // the next copy into the slot comes after
+    __syncthreads();
+  }
+};
+
+// Rows of which a thread takes the elements v nt + tid.  kThreads: the threads of a block, if known when compiled;
+// a row then has more than kThreads NV 2/3 elements (NV = 12 and 16), so that most need no comparison.
+template <int NV, int kThreads>
+struct Across {
+  static constexpr int kSure = kThreads && NV > 8 ? NV - 4 : 0;  // elements that every thread has
+  static __device__ __forceinline__ int nt() { return kThreads ? kThreads : blockDim.x; }
+  static __device__ __forceinline__ int column(int v) { return v * nt() + int(threadIdx.x); }
+  static __device__ __forceinline__ bool inside(int v, int D) { return v < kSure || column(v) < D; }
+};
+// Elements of a row (`otherwise` where it ends, or where there is none): loads without conditions, so that all are on
+// their way together.  kSpare: memory goes on behind the row.
+template <int kThreads, bool kSpare, typename T, int NV>
+__device__ __forceinline__ void load_across(float (&f)[NV], const T* from, int D, float otherwise) {
+  using A = Across<NV, kThreads>;
+  if (from) {
+    T raw[NV];
+#pragma unroll
+    for (int v = 0; v < NV; ++v) raw[v] = from[kSpare || v < A::kSure ? A::column(v) : min(A::column(v), D - 1)];
+#pragma unroll
+    for (int v = 0; v < NV; ++v) f[v] = A::inside(v, D) ? to_f32(raw[v]) : otherwise;
+  } else {
+#pragma unroll
+    for (int v = 0; v < NV; ++v) f[v] = otherwise;
+  }
 }
 
 // ---- forward -----------------------------------------------------------------------------------
@@ -222,22 +324,109 @@ __global__ void __launch_bounds__(1024) cconv_residual_norm_long_kernel(const No
   }
 }
 
+// Many rows that are not wide, through the ring above (16384 x 4095 bf16: 131 us, 224 with a block size known at
+// the launch; with a block a row and everything from global memory 516 us).
+template <typename T, int NV, int kThreads>
+__global__ void __launch_bounds__(kThreads) cconv_residual_norm_narrow_kernel(const NormParams p) {
+  extern __shared__ __align__(128) uint8_t ring[];
+  __shared__ float2 smem[2][32];
+  __shared__ __align__(8) uint64_t full[8];
+  __shared__ int abort_flag;
+  start_in_order();
+  const T* block = static_cast<const T*>(p.block);
+  const T* __restrict__ gate = static_cast<const T*>(p.gate);
+  const T* __restrict__ w_post = static_cast<const T*>(p.w_post);
+  const T* __restrict__ w_pre = static_cast<const T*>(p.w_pre);
+  T* resid_out = static_cast<T*>(p.resid_out);
+  T* norm_out = static_cast<T*>(p.norm_out);
+  using A = Across<NV, kThreads>;
+  const int tid = threadIdx.x;
+  const float inv_d = 1.0f / float(p.D);
+  const int64_t row0 = first_row<T>(p, blockIdx.x), row1 = first_row<T>(p, blockIdx.x + 1);
+  const int64_t per = p.rows_per_gate ? p.rows_per_gate : p.T;
+  const RowRing<T, 2> rows = {{static_cast<const T*>(p.resid), block}, {p.resid_rs, p.block_rs}, p.T, row0, row1,
+                              uint32_t(p.D * sizeof(T)), p.ring_slot, smem_u32(ring), smem_u32(full), uint32_t(p.ring_rows)};
+  if (tid == 0) {
+    abort_flag = 0;
+    rows.begin();
+  }
+  __syncthreads();
+  float gw[NV], wpre[NV];  // gate * w_post of the current group; w_pre
+  load_across<kThreads, false>(wpre, w_pre, p.D, 1.0f);
+  int64_t group_end = row0;
+  uint32_t st = 0, phase = 0;
+  int buf = 0;
+  int64_t t = row0;
+  for (; t < row1; ++t) {
+    if (t == group_end || t == row0) {
+      const int64_t group = t / per;
+      group_end = (group + 1) * per;
+      float g[NV];
+      load_across<kThreads, false>(g, gate ? gate + group * p.gate_rs : nullptr, p.D, 1.0f);
+      load_across<kThreads, false>(gw, w_post, p.D, 1.0f);
+#pragma unroll
+      for (int v = 0; v < NV; ++v) gw[v] *= g[v];
+    }
+    const bool ok = mbar_wait(rows.full0 + 8 * st, phase, &abort_flag, p.status, kStatProducerWait, p.limit_ns);
+    // every thread is past the row before: its place in the ring is free
+    if (!__syncthreads_and(ok)) break;
+    if (tid == 0 && t > row0 && t - 1 + p.ring_rows < row1) rows.copy(t - 1 + p.ring_rows);
+    rows.complete(ring, st, t);
+    const T* row_r = rows.row(ring, 0, st, t);
+    const T* row_y = block ? rows.row(ring, 1, st, t) : nullptr;
+    if (++st == uint32_t(p.ring_rows)) st = 0, phase ^= 1;
+    float rho = 1.0f, ss = 0.0f;
+    float o[NV];
+    load_across<kThreads, true>(o, row_y, p.D, 0.0f);
+    if (block && w_post) {
+#pragma unroll
+      for (int v = 0; v < NV; ++v) ss += o[v] * o[v];
+      rho = rsqrtf(block_sum2(ss, 0.0f, smem, buf).x * inv_d + p.eps);
+      ss = 0.0f;
+    }
+    float r[NV];
+    load_across<kThreads, true>(r, row_r, p.D, 0.0f);
+    T* to = resid_out + t * p.resid_out_rs;
+#pragma unroll
+    for (int v = 0; v < NV; ++v) {
+      o[v] = p.scale * r[v] + o[v] * (rho * gw[v]);
+      ss += o[v] * o[v];
+      if (A::inside(v, p.D)) to[A::column(v)] = from_f32<T>(o[v]);
+    }
+    if (!norm_out) continue;
+    rho = rsqrtf(block_sum2(ss, 0.0f, smem, buf).x * inv_d + p.eps);
+    to = norm_out + t * p.norm_out_rs;
+#pragma unroll
+    for (int v = 0; v < NV; ++v)
+      if (A::inside(v, p.D)) to[A::column(v)] = from_f32<T>(o[v] * (rho * wpre[v]));
+  }
+  if (t < row1) {  // a copy did not come in time: let those on their way land
+    const uint64_t t0 = globaltimer_ns();
+    while (globaltimer_ns() - t0 < 200000) {
+    }
+  }
+}
+
 // ---- backward ----------------------------------------------------------------------------------
-// Block b takes the rows [T b / nb, T (b+1) / nb) in order and keeps its share of the column sums
+// A block takes its rows in order and keeps its share of the column sums
 // (dw_pre, dw_post, dgate of the current group) in registers.  At the end they go to its rows of the
 // partial table part[b][4][D] (dw_pre, dw_post, gate group of its first row, gate group of its last
 // row), which a second kernel adds up in a fixed order.  A gate group that lies inside one block's
 // rows is complete there and written at once.
-template <typename T>
-__device__ __forceinline__ int64_t first_row(const NormParams& p, int64_t b) {
-  return p.T * b / p.nb;
-}
-
-// Rows that are not wide (an odd length, pitch or address): E = 1, straight from global memory.
-template <typename T, int NV>
-__global__ void __launch_bounds__(512) cconv_residual_norm_backward_kernel(const NormParams p) {
+// Rows that are not wide (an odd length, pitch or address): element v nt + tid is the thread's, so that the
+// narrow accesses of a warp are neighbours.  kThreads: rows come through the ring above, and a block's size is
+// known when compiled, which leaves accesses no address arithmetic of their own (16384 x 4095 bf16: 245 us, and 490
+// with a size known at the launch); 0: straight from global memory, where rows are few or the ring has no room for
+// two (1118 us).
+template <typename T, int NV, int kThreads>
+__global__ void __launch_bounds__(kThreads ? kThreads : 512, 512 / (kThreads ? kThreads : 512)) cconv_residual_norm_backward_kernel(const NormParams p) {
+  extern __shared__ __align__(128) uint8_t ring[];
   __shared__ float2 smem[2][32];
+  __shared__ __align__(8) uint64_t full[8];
+  __shared__ int abort_flag;
   start_in_order();
+  using A = Across<NV, kThreads>;
+  constexpr bool kRing = kThreads != 0;
   const T* dres = static_cast<const T*>(p.dresid_out);  // may be dresid
   const T* __restrict__ dx = static_cast<const T*>(p.dnorm_out);
   const T* __restrict__ block = static_cast<const T*>(p.block);
@@ -248,7 +437,7 @@ __global__ void __launch_bounds__(512) cconv_residual_norm_backward_kernel(const
   T* dresid = static_cast<T*>(p.dresid);
   T* dblock = static_cast<T*>(p.dblock);
   T* dgate = static_cast<T*>(p.dgate);
-  const int nt = blockDim.x, tid = threadIdx.x;
+  const int tid = threadIdx.x;
   const float inv_d = 1.0f / float(p.D);
   const int64_t row0 = first_row<T>(p, blockIdx.x), row1 = first_row<T>(p, blockIdx.x + 1);
   const int64_t per = p.rows_per_gate ? p.rows_per_gate : p.T;
@@ -256,82 +445,123 @@ __global__ void __launch_bounds__(512) cconv_residual_norm_backward_kernel(const
   int buf = 0;
   // Sums over rows: x rhat; S yhat of the current gate group (dgate is w_post of it); dw_post (gate times
   // each group's S yhat, added when the group ends).
-  float s_pre[NV], s_post[NV], s_group[NV], gw[NV];  // gw: gate * w_post of the current group
+  // Those of dw_post, which change only where a group ends, lie in the partial table (each thread touches its own
+  // columns alone).
+  float s_pre[NV], s_group[NV], gw[NV];  // gw: gate * w_post of the current group
 #pragma unroll
-  for (int v = 0; v < NV; ++v) s_pre[v] = s_post[v] = s_group[v] = gw[v] = 0.0f;
-  auto at = [&](const T* from, int c, float otherwise) { return from && c < p.D ? to_f32(from[c]) : otherwise; };
+  for (int v = 0; v < NV; ++v) {
+    s_pre[v] = s_group[v] = gw[v] = 0.0f;
+    if (A::inside(v, p.D)) part[p.D + A::column(v)] = 0.0f;
+  }
   int64_t group = row0 / per, group_end = (group + 1) * per;
   const int64_t group0 = group;
   auto start_group = [&]() {
+    float g[NV];
+    load_across<kThreads, false>(g, gate ? gate + group * p.gate_rs : nullptr, p.D, 1.0f);
+    load_across<kThreads, false>(gw, w_post, p.D, 1.0f);
 #pragma unroll
-    for (int v = 0; v < NV; ++v) {
-      const int c = v * nt + tid;
-      gw[v] = at(gate ? gate + group * p.gate_rs : nullptr, c, 1.0f) * at(w_post, c, 1.0f);
-    }
+    for (int v = 0; v < NV; ++v) gw[v] *= g[v];
   };
   // adds the group that ends (or that the block ends in) to dw_post and writes its part of dgate
   auto end_group = [&]() {
     const int64_t g0 = group * per, g1 = group_end < p.T ? group_end : p.T;
     const bool whole = g0 >= row0 && g1 <= row1;
+    float g[NV], w[NV];
+    load_across<kThreads, false>(g, gate ? gate + group * p.gate_rs : nullptr, p.D, 1.0f);
+    load_across<kThreads, false>(w, w_post, p.D, 1.0f);
 #pragma unroll
     for (int v = 0; v < NV; ++v) {
-      const int c = v * nt + tid;
-      s_post[v] += at(gate ? gate + group * p.gate_rs : nullptr, c, 1.0f) * s_group[v];
-      const float f = at(w_post, c, 1.0f) * s_group[v];
+      const int c = A::column(v);
+      if (A::inside(v, p.D)) part[p.D + c] += g[v] * s_group[v];
+      const float f = w[v] * s_group[v];
       s_group[v] = 0.0f;
-      if (gate && c < p.D) {
+      if (gate && A::inside(v, p.D)) {
         if (whole) dgate[group * p.dgate_rs + c] = from_f32<T>(f);
         else part[(group == group0 ? 2 : 3) * int64_t(p.D) + c] = f;
       }
     }
   };
+  RowRing<T, 4> rows;  // r', dx, dr', y
+  const T* pre = w_pre;
+  if (kRing) {
+    rows = {{dx ? resid_out : nullptr, dx, dres, block},
+            {p.resid_out_rs, p.dnorm_out_rs, p.dresid_out_rs, p.block_rs},
+            p.T, row0, row1, uint32_t(p.D * sizeof(T)), p.ring_slot, smem_u32(ring), smem_u32(full), uint32_t(p.ring_rows)};
+    if (tid == 0) {
+      abort_flag = 0;
+      rows.begin();
+    }
+    if (w_pre) {  // a copy behind the ring
+      T* w = reinterpret_cast<T*>(ring + p.ring_rows * 4 * p.ring_slot);
+      for (int c = tid; c < p.D; c += kThreads) w[c] = w_pre[c];
+      pre = w;
+    }
+    __syncthreads();
+  }
   start_group();
-  for (int64_t t = row0; t < row1; ++t) {
+  uint32_t st = 0, phase = 0;
+  int64_t t = row0;
+  for (; t < row1; ++t) {
+    const T* row_d = dres ? dres + t * p.dresid_out_rs : nullptr;
+    const T* row_y = block ? block + t * p.block_rs : nullptr;
+    const T* row_r = dx ? resid_out + t * p.resid_out_rs : nullptr;
+    const T* row_x = dx ? dx + t * p.dnorm_out_rs : nullptr;
+    if (kRing) {
+      const bool ok = mbar_wait(rows.full0 + 8 * st, phase, &abort_flag, p.status, kStatProducerWait, p.limit_ns);
+      // every thread is past the row before: its place in the ring is free
+      if (!__syncthreads_and(ok)) break;
+      if (tid == 0 && t > row0 && t - 1 + p.ring_rows < row1) rows.copy(t - 1 + p.ring_rows);
+      rows.complete(ring, st, t);
+      if (dx) row_r = rows.row(ring, 0, st, t), row_x = rows.row(ring, 1, st, t);
+      if (dres) row_d = rows.row(ring, 2, st, t);
+      if (block) row_y = rows.row(ring, 3, st, t);
+      if (++st == uint32_t(p.ring_rows)) st = 0, phase ^= 1;
+    }
     if (t == group_end) {
       end_group();
       ++group;
       group_end += per;
       start_group();
     }
-    const T* row_d = dres ? dres + t * p.dresid_out_rs : nullptr;
-    const T* row_y = block ? block + t * p.block_rs : nullptr;
-    float s[NV], y[NV];
-#pragma unroll
-    for (int v = 0; v < NV; ++v) {
-      s[v] = at(row_d, v * nt + tid, 0.0f);
-      y[v] = at(row_y, v * nt + tid, 0.0f);
-    }
+    float s[NV];
     if (dx) {
-      const T *row_r = resid_out + t * p.resid_out_rs, *row_x = dx + t * p.dnorm_out_rs;
-      float r[NV], x[NV], w[NV];
-      float srr = 0.0f, ser = 0.0f;
+      float r[NV], x[NV], w[NV], srr = 0.0f, ser = 0.0f;
+      load_across<kThreads, kRing>(r, row_r, p.D, 0.0f);
+      load_across<kThreads, kRing>(x, row_x, p.D, 0.0f);
+      load_across<kThreads, kRing>(w, pre, p.D, 1.0f);
 #pragma unroll
       for (int v = 0; v < NV; ++v) {
-        const int c = v * nt + tid;
-        r[v] = at(row_r, c, 0.0f);
-        x[v] = at(row_x, c, 0.0f);
-        w[v] = at(w_pre, c, 1.0f);
         srr += r[v] * r[v];
         ser += x[v] * w[v] * r[v];
       }
       const float2 q = block_sum2(srr, ser, smem, buf);
       const float rho = rsqrtf(q.x * inv_d + p.eps);
       const float k = rho * rho * rho * (q.y * inv_d);
+      // (read again: the reduction would hold them in registers that the sums need)
+      load_across<kThreads, kRing>(r, row_r, p.D, 0.0f);
+      load_across<kThreads, kRing>(x, row_x, p.D, 0.0f);
+      load_across<kThreads, kRing>(w, pre, p.D, 1.0f);
+      load_across<kThreads, kRing>(s, row_d, p.D, 0.0f);
 #pragma unroll
       for (int v = 0; v < NV; ++v) {
         s[v] += rho * (x[v] * w[v]) - k * r[v];
         s_pre[v] += x[v] * (r[v] * rho);
       }
+    } else {
+      load_across<kThreads, kRing>(s, row_d, p.D, 0.0f);
     }
-    float syy = 0.0f, sfy = 0.0f;
+    T* const to_r = dresid + t * p.dresid_rs;
+    float y[NV], syy = 0.0f, sfy = 0.0f;
+    load_across<kThreads, kRing>(y, row_y, p.D, 0.0f);
 #pragma unroll
     for (int v = 0; v < NV; ++v) {
-      const int c = v * nt + tid;
+      const int c = A::column(v);
       syy += y[v] * y[v];
       sfy += s[v] * gw[v] * y[v];
-      if (c < p.D) dresid[t * p.dresid_rs + c] = from_f32<T>(p.scale * s[v]);
+      if (A::inside(v, p.D)) to_r[c] = from_f32<T>(p.scale * s[v]);
     }
     if (!block) continue;
+    T* const to_y = dblock + t * p.dblock_rs;
     float rho = 1.0f, k = 0.0f;
     if (w_post) {
       const float2 q = block_sum2(syy, sfy, smem, buf);
@@ -340,19 +570,22 @@ __global__ void __launch_bounds__(512) cconv_residual_norm_backward_kernel(const
     }
 #pragma unroll
     for (int v = 0; v < NV; ++v) {
-      const int c = v * nt + tid;
+      const int c = A::column(v);
       s_group[v] += s[v] * (y[v] * rho);
-      if (c < p.D) dblock[t * p.dblock_rs + c] = from_f32<T>(rho * (s[v] * gw[v]) - k * y[v]);
+      if (A::inside(v, p.D)) to_y[c] = from_f32<T>(rho * (s[v] * gw[v]) - k * y[v]);
     }
+  }
+  if (t < row1) {  // a copy did not come in time: let those on their way land
+    const uint64_t t0 = globaltimer_ns();
+    while (globaltimer_ns() - t0 < 200000) {
+    }
+    return;
   }
   if (row0 < row1) end_group();
 #pragma unroll
   for (int v = 0; v < NV; ++v) {
-    const int c = v * nt + tid;
-    if (c < p.D) {
-      part[c] = s_pre[v];
-      part[p.D + c] = s_post[v];
-    }
+    const int c = A::column(v);
+    if (A::inside(v, p.D)) part[c] = s_pre[v];
   }
 }
 
@@ -968,6 +1201,35 @@ cudaError_t launch_forward_ring(const NormParams& p, int threads, cudaStream_t s
   return launch(f, dim3(unsigned(p.nb)), threads, size_t(p.D) * p.ring_rows * 2 * sizeof(T), 1, s, p);
 }
 
+// Shared memory of a row of one array in the ring of rows that begin anywhere.
+int64_t narrow_slot(int64_t row_bytes) { return round_up64(row_bytes, 16) + 16; }
+// Threads and elements a thread there: 64 to 512 threads, 12 or 16 elements (8 where D is at most 512).
+Shape narrow_shape(int64_t D) {
+  if (D <= 512) return {64, 8};
+  for (int threads = 64; threads <= 512; threads *= 2) {
+    if (D <= threads * 12) return {threads, 12};
+    if (D <= threads * 16) return {threads, 16};
+  }
+  return {0, 0};
+}
+// Calls f with the shape's numbers as constants: f(elements, threads).
+template <typename F>
+cudaError_t with_narrow_shape(const Shape& n, F f) {
+  auto elements = [&](auto threads) {
+    if (n.nv == 12) return f(std::integral_constant<int, 12>(), threads);
+    return f(std::integral_constant<int, 16>(), threads);
+  };
+  if (n.nv == 8) return f(std::integral_constant<int, 8>(), std::integral_constant<int, 64>());
+  if (n.threads == 64) return elements(std::integral_constant<int, 64>());
+  if (n.threads == 128) return elements(std::integral_constant<int, 128>());
+  if (n.threads == 256) return elements(std::integral_constant<int, 256>());
+  return elements(std::integral_constant<int, 512>());
+}
+// Whether the rows of an array can go through it: none but the first and last touch its ends.
+bool narrow_fits(const void* q, int64_t rs, const NormParams& p, int es) {
+  return !q || (rs * es >= 16 && p.D * es >= 64);
+}
+
 template <typename T>
 cudaError_t launch_forward(NormParams p, int sms, cudaStream_t s) {
   constexpr int kWide = 16 / int(sizeof(T)), kMost = 16 / kWide;
@@ -994,6 +1256,26 @@ cudaError_t launch_forward(NormParams p, int sms, cudaStream_t s) {
     if (sh.nv == 2) return launch_forward_nv<T, kWide, 2>(p, threads, grid, s);
     return launch_forward_nv<T, kWide, kMost>(p, threads, grid, s);
   }
+  // many rows that are not wide: the same with their own ring
+  const Shape n = narrow_shape(p.D);
+  if (n.threads && narrow_fits(p.resid, p.resid_rs, p, sizeof(T)) && narrow_fits(p.block, p.block_rs, p, sizeof(T))) {
+    const int64_t es = sizeof(T), slot = narrow_slot(p.D * es), spare = n.threads * n.nv * es;
+    an_sm = 1024 / n.threads;
+    auto narrow_rows = [&](int64_t blocks) { return (kRingSmem / blocks / 1024 * 1024 - kRingOwn - spare) / (2 * slot); };
+    while (an_sm > 1 && narrow_rows(an_sm) < 2) --an_sm;
+    if (narrow_rows(an_sm) >= 2 && p.T >= 4 * an_sm * sms) {
+      p.nb = int(an_sm * sms);
+      p.ring_rows = int(std::min<int64_t>(8, narrow_rows(an_sm)));
+      p.ring_slot = uint32_t(slot);
+      return with_narrow_shape(n, [&](auto nv, auto nt) {
+        auto f = cconv_residual_norm_narrow_kernel<T, decltype(nv)::value, decltype(nt)::value>;
+        static bool ready[64] = {};
+        const cudaError_t e = allow_ring(f, ready);
+        if (e != cudaSuccess) return e;
+        return launch(f, dim3(unsigned(p.nb)), nt, size_t(p.ring_rows) * 2 * slot + spare, 1, s, p);
+      });
+    }
+  }
   if (sh.nv == 1) return launch_forward_nv<T, 1, 1>(p, threads, grid, s);
   if (sh.nv == 2) return launch_forward_nv<T, 1, 2>(p, threads, grid, s);
   if (sh.nv == 4) return launch_forward_nv<T, 1, 4>(p, threads, grid, s);
@@ -1013,18 +1295,45 @@ cudaError_t launch_ring(NormParams p, int threads, cudaStream_t s) {
 
 template <typename T, int NV>
 cudaError_t launch_plain(const NormParams& p, int threads, cudaStream_t s) {
-  return launch(cconv_residual_norm_backward_kernel<T, NV>, dim3(unsigned(p.nb)), threads, 0, 1, s, p);
+  return launch(cconv_residual_norm_backward_kernel<T, NV, 0>, dim3(unsigned(p.nb)), threads, 0, 1, s, p);
+}
+
+// The same with rows through the ring, where they are many and it has room: fewer blocks then, if need be.
+template <typename T>
+bool use_narrow_ring(NormParams* p, Shape* n) {
+  const int64_t es = sizeof(T), slot = narrow_slot(p->D * es);
+  *n = narrow_shape(p->D);
+  if (!n->threads) return false;
+  const int64_t an_sm = 512 / n->threads, spare = n->threads * n->nv * es;  // w_pre, and what lies behind the last row
+  const int64_t rows = (kRingSmem / an_sm / 1024 * 1024 - kRingOwn - spare) / (4 * slot);
+  if (p->T < 4 * int64_t(p->nb) || rows < 2 || !narrow_fits(p->dnorm_out, p->dnorm_out_rs, *p, es) ||
+      !narrow_fits(p->dnorm_out ? p->resid_out : nullptr, p->resid_out_rs, *p, es) ||
+      !narrow_fits(p->dresid_out, p->dresid_out_rs, *p, es) || !narrow_fits(p->block, p->block_rs, *p, es))
+    return false;
+  p->nb = int(std::min<int64_t>(p->nb, std::max<int64_t>(1, p->nb * an_sm / blocks_an_sm(p->D, es))));
+  p->ring_rows = int(std::min<int64_t>(8, rows));
+  p->ring_slot = uint32_t(slot);
+  return true;
 }
 
 template <typename T>
-cudaError_t launch_backward(const NormParams& p, cudaStream_t s) {
+cudaError_t launch_backward(NormParams p, cudaStream_t s) {
   constexpr int kWide = 16 / int(sizeof(T));
   const bool w = wide(p, sizeof(T), true) && ring_rows(p.D, sizeof(T), blocks_an_sm(p.D, sizeof(T))) >= 2;
   const Shape sh = shape_of(p.D, w ? kWide : 1, 16, 512);
   const bool all = p.dnorm_out && p.dresid_out && p.block && p.w_pre && p.w_post && p.gate &&
                    p.D == int64_t(sh.threads) * sh.nv * kWide;
   cudaError_t e = cudaSuccess;
-  if (!sh.threads) {
+  Shape n;
+  if (!w && use_narrow_ring<T>(&p, &n)) {
+    e = with_narrow_shape(n, [&](auto nv, auto nt) {
+      auto f = cconv_residual_norm_backward_kernel<T, decltype(nv)::value, decltype(nt)::value>;
+      static bool ready[64] = {};
+      const cudaError_t e = allow_ring(f, ready);
+      if (e != cudaSuccess) return e;
+      return launch(f, dim3(unsigned(p.nb)), nt, size_t(p.ring_rows) * 4 * p.ring_slot + nt * nv * sizeof(T), 1, s, p);
+    });
+  } else if (!sh.threads) {
     e = launch(cconv_residual_norm_backward_long_kernel<T>, dim3(unsigned(p.nb)), 512, 0, 1, s, p);
   } else if (w) {
     constexpr int kMost = 16 / kWide;

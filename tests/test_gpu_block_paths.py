@@ -230,3 +230,49 @@ def test_every_cut_in_every_storage_order(cut, monkeypatch):
             block.fp8_product(a, sa, b, sb, out)
             fp8_check(a, sa, b, sb, out, cut)
     assert block.status() == (0, 0)
+
+
+def shifted(t, pitch, by):
+    """The same values in rows `pitch` apart, `by` elements behind an allocation's start."""
+    buf = torch.full((by + pitch * t.shape[0] + 8,), float("nan"), dtype=t.dtype, device="cuda")
+    v = buf.as_strided(t.shape, (pitch, 1), by)
+    v.copy_(t)
+    return v
+
+
+# rows that begin anywhere, enough of them for the ring: T >= 4 rows a block of up to 16 blocks on 148 SMs
+@pytest.mark.parametrize("T,D,dtype,gate,rows", [
+    (2400, 4095, BF16, "groups", 300), (2500, 2049, FP16, "all", 0), (9600, 1001, BF16, "groups", 1), (9600, 67, FP16, "groups", 777),
+    (9500, 700, BF16, "none", 0), (4800, 1999, BF16, "groups", 5000), (1200, 5001, FP32, "none", 0), (4800, 1026, FP32, "all", 0),
+    (1250, 8190, BF16, "groups", 1250), (4800, 1500, BF16, "groups", 7), (9600, 33, FP32, "groups", 1)])
+@pytest.mark.parametrize("by,pad", [(0, 0), (3, 0), (1, 5)])
+def test_norms_of_many_rows_that_begin_anywhere(T, D, dtype, gate, rows, by, pad):
+    n = Norm(T, D, dtype, gate, rows, scale=0.75)
+    for name in ("r", "y", "dr", "dx"):
+        setattr(n, name, shifted(getattr(n, name), D + pad, by))
+    n.check(*n.run(), "forward")
+    inplace = shifted(n.r, D + pad, by)
+    want = n.run()
+    block.residual_norm_forward(inplace, inplace, torch.empty_like(want[1]), block=n.y, w_post=n.wpost, gate=n.gate,
+                                w_pre=n.wpre, rows_per_gate=n.rows, scale=n.scale, eps=n.eps)
+    assert torch.equal(inplace, want[0])
+    got = n.run_backward()
+    n.check_backward(got)
+    inplace = shifted(n.dr, D + pad, by)
+    like = lambda t: None if t is None else torch.empty_like(t)  # noqa: E731
+    block.residual_norm_backward(inplace, n.dx, n.o, inplace, block=n.y, dblock=like(got[1]), w_post=n.wpost,
+                                 dw_post=like(got[2]), gate=n.gate, dgate=like(got[3]), w_pre=n.wpre, dw_pre=like(got[4]),
+                                 rows_per_gate=n.rows, scale=n.scale, eps=n.eps)
+    assert torch.equal(inplace, got[0])
+    assert block.status() == (0, 0)
+
+
+def test_norms_of_many_rows_with_parts_left_out():
+    for kw in (dict(blk=False), dict(post=False), dict(pre=False), dict(gate="all", post=False)):
+        n = Norm(2600, 1001, BF16, **kw)
+        n.check(*n.run(), f"{kw}")
+        n.check(*n.run(norm=False), f"{kw} without the second norm")
+        n.check_backward(n.run_backward())
+        n.check_backward(n.run_backward(use_dr=False), use_dr=False)
+        n.check_backward(n.run_backward(use_dx=False), use_dx=False)
+    assert block.status() == (0, 0)
