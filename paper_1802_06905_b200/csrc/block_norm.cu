@@ -415,34 +415,56 @@ __global__ void __launch_bounds__(kThreads) cconv_residual_norm_narrow_kernel(co
 // rows is complete there and written at once.
 // Rows that are not wide (an odd length, pitch or address): element v nt + tid is the thread's, so that the
 // narrow accesses of a warp are neighbours.  kThreads: rows come through the ring above, and a block's size is
-// known when compiled, which leaves accesses no address arithmetic of their own (16384 x 4095 bf16: 245 us, and 490
+// known when compiled, which leaves accesses no address arithmetic of their own (16384 x 4095 bf16: 260 us, and 490
 // with a size known at the launch); 0: straight from global memory, where rows are few or the ring has no room for
-// two (1118 us).
-template <typename T, int NV, int kThreads>
+// two (1118 us).  kCluster: rows too long for one block's registers are shared by the 2, 4 or 8 blocks of a
+// cluster, a range of columns each, which exchange their sums through distributed shared memory (4096 x 16384
+// bf16: 357 us; with sums in memory, cconv_residual_norm_backward_long_kernel, 2860 us).
+constexpr int kMostParts = 8;
+template <typename T, int NV, int kThreads, bool kCluster = false>
 __global__ void __launch_bounds__(kThreads ? kThreads : 512, 512 / (kThreads ? kThreads : 512)) cconv_residual_norm_backward_kernel(const NormParams p) {
   extern __shared__ __align__(128) uint8_t ring[];
   __shared__ float2 smem[2][32];
   __shared__ __align__(8) uint64_t full[8];
   __shared__ int abort_flag;
+  __shared__ float2 shares[2][kMostParts];
   start_in_order();
   using A = Across<NV, kThreads>;
   constexpr bool kRing = kThreads != 0;
-  const T* dres = static_cast<const T*>(p.dresid_out);  // may be dresid
-  const T* __restrict__ dx = static_cast<const T*>(p.dnorm_out);
-  const T* __restrict__ block = static_cast<const T*>(p.block);
-  const T* __restrict__ resid_out = static_cast<const T*>(p.resid_out);
-  const T* __restrict__ gate = static_cast<const T*>(p.gate);
-  const T* __restrict__ w_post = static_cast<const T*>(p.w_post);
-  const T* __restrict__ w_pre = static_cast<const T*>(p.w_pre);
-  T* dresid = static_cast<T*>(p.dresid);
-  T* dblock = static_cast<T*>(p.dblock);
-  T* dgate = static_cast<T*>(p.dgate);
+  const int parts = kCluster ? p.parts : 1, rank = kCluster ? int(cluster_ctarank()) : 0;
+  const int b = kCluster ? int(blockIdx.x) / parts : int(blockIdx.x);
+  const int c0 = kCluster ? int(int64_t(p.D) * rank / parts) : 0;
+  const int D = kCluster ? int(int64_t(p.D) * (rank + 1) / parts) - c0 : p.D;  // the block's columns, from c0 on
+  auto columns = [&](const void* q) { return static_cast<const T*>(q) + (kCluster && q ? c0 : 0); };
+  const T* dres = columns(p.dresid_out);  // may be dresid
+  const T* __restrict__ dx = columns(p.dnorm_out);
+  const T* __restrict__ block = columns(p.block);
+  const T* __restrict__ resid_out = columns(p.resid_out);
+  const T* __restrict__ gate = columns(p.gate);
+  const T* __restrict__ w_post = columns(p.w_post);
+  const T* __restrict__ w_pre = columns(p.w_pre);
+  T* dresid = static_cast<T*>(p.dresid) + c0;
+  T* dblock = static_cast<T*>(p.dblock) + c0;
+  T* dgate = static_cast<T*>(p.dgate) + c0;
   const int tid = threadIdx.x;
   const float inv_d = 1.0f / float(p.D);
-  const int64_t row0 = first_row<T>(p, blockIdx.x), row1 = first_row<T>(p, blockIdx.x + 1);
+  const int64_t row0 = first_row<T>(p, b), row1 = first_row<T>(p, b + 1);
   const int64_t per = p.rows_per_gate ? p.rows_per_gate : p.T;
-  float* part = p.part + int64_t(blockIdx.x) * 4 * p.D;
-  int buf = 0;
+  float* part = p.part + int64_t(b) * 4 * p.D + c0;
+  int buf = 0, shares_of = 0;
+  // Sums over the whole row: of the block, and then, in the order of the ranks, of the cluster.
+  auto row_sum2 = [&](float f, float g) {
+    float2 q = block_sum2(f, g, smem, buf);
+    if (kCluster) {
+      if (tid < parts) st_cluster_v2(cluster_map_shared(smem_u32(&shares[shares_of][rank]), tid), q.x, q.y);
+      __syncwarp();
+      cluster_sync_all();
+      q = shares[shares_of][0];
+      for (int i = 1; i < parts; ++i) q.x += shares[shares_of][i].x, q.y += shares[shares_of][i].y;
+      shares_of ^= 1;
+    }
+    return q;
+  };
   // Sums over rows: x rhat; S yhat of the current gate group (dgate is w_post of it); dw_post (gate times
   // each group's S yhat, added when the group ends).
   // Those of dw_post, which change only where a group ends, lie in the partial table (each thread touches its own
@@ -451,14 +473,14 @@ __global__ void __launch_bounds__(kThreads ? kThreads : 512, 512 / (kThreads ? k
 #pragma unroll
   for (int v = 0; v < NV; ++v) {
     s_pre[v] = s_group[v] = gw[v] = 0.0f;
-    if (A::inside(v, p.D)) part[p.D + A::column(v)] = 0.0f;
+    if (A::inside(v, D)) part[p.D + A::column(v)] = 0.0f;
   }
   int64_t group = row0 / per, group_end = (group + 1) * per;
   const int64_t group0 = group;
   auto start_group = [&]() {
     float g[NV];
-    load_across<kThreads, false>(g, gate ? gate + group * p.gate_rs : nullptr, p.D, 1.0f);
-    load_across<kThreads, false>(gw, w_post, p.D, 1.0f);
+    load_across<kThreads, false>(g, gate ? gate + group * p.gate_rs : nullptr, D, 1.0f);
+    load_across<kThreads, false>(gw, w_post, D, 1.0f);
 #pragma unroll
     for (int v = 0; v < NV; ++v) gw[v] *= g[v];
   };
@@ -467,15 +489,15 @@ __global__ void __launch_bounds__(kThreads ? kThreads : 512, 512 / (kThreads ? k
     const int64_t g0 = group * per, g1 = group_end < p.T ? group_end : p.T;
     const bool whole = g0 >= row0 && g1 <= row1;
     float g[NV], w[NV];
-    load_across<kThreads, false>(g, gate ? gate + group * p.gate_rs : nullptr, p.D, 1.0f);
-    load_across<kThreads, false>(w, w_post, p.D, 1.0f);
+    load_across<kThreads, false>(g, gate ? gate + group * p.gate_rs : nullptr, D, 1.0f);
+    load_across<kThreads, false>(w, w_post, D, 1.0f);
 #pragma unroll
     for (int v = 0; v < NV; ++v) {
       const int c = A::column(v);
-      if (A::inside(v, p.D)) part[p.D + c] += g[v] * s_group[v];
+      if (A::inside(v, D)) part[p.D + c] += g[v] * s_group[v];
       const float f = w[v] * s_group[v];
       s_group[v] = 0.0f;
-      if (gate && A::inside(v, p.D)) {
+      if (gate && A::inside(v, D)) {
         if (whole) dgate[group * p.dgate_rs + c] = from_f32<T>(f);
         else part[(group == group0 ? 2 : 3) * int64_t(p.D) + c] = f;
       }
@@ -486,20 +508,22 @@ __global__ void __launch_bounds__(kThreads ? kThreads : 512, 512 / (kThreads ? k
   if (kRing) {
     rows = {{dx ? resid_out : nullptr, dx, dres, block},
             {p.resid_out_rs, p.dnorm_out_rs, p.dresid_out_rs, p.block_rs},
-            p.T, row0, row1, uint32_t(p.D * sizeof(T)), p.ring_slot, smem_u32(ring), smem_u32(full), uint32_t(p.ring_rows)};
+            p.T, row0, row1, uint32_t(D * sizeof(T)), p.ring_slot, smem_u32(ring), smem_u32(full), uint32_t(p.ring_rows)};
     if (tid == 0) {
       abort_flag = 0;
       rows.begin();
     }
     if (w_pre) {  // a copy behind the ring
       T* w = reinterpret_cast<T*>(ring + p.ring_rows * 4 * p.ring_slot);
-      for (int c = tid; c < p.D; c += kThreads) w[c] = w_pre[c];
+      for (int c = tid; c < D; c += kThreads) w[c] = w_pre[c];
       pre = w;
     }
     __syncthreads();
+    if (kCluster) cluster_sync_all();  // the others' shared memory is there
   }
   start_group();
   uint32_t st = 0, phase = 0;
+  bool dead = false;  // a copy did not come in time: a cluster's blocks go on, for the others wait for them
   int64_t t = row0;
   for (; t < row1; ++t) {
     const T* row_d = dres ? dres + t * p.dresid_out_rs : nullptr;
@@ -507,10 +531,13 @@ __global__ void __launch_bounds__(kThreads ? kThreads : 512, 512 / (kThreads ? k
     const T* row_r = dx ? resid_out + t * p.resid_out_rs : nullptr;
     const T* row_x = dx ? dx + t * p.dnorm_out_rs : nullptr;
     if (kRing) {
-      const bool ok = mbar_wait(rows.full0 + 8 * st, phase, &abort_flag, p.status, kStatProducerWait, p.limit_ns);
+      const bool ok = (kCluster && dead) || mbar_wait(rows.full0 + 8 * st, phase, &abort_flag, p.status, kStatProducerWait, p.limit_ns);
       // every thread is past the row before: its place in the ring is free
-      if (!__syncthreads_and(ok)) break;
-      if (tid == 0 && t > row0 && t - 1 + p.ring_rows < row1) rows.copy(t - 1 + p.ring_rows);
+      if (!__syncthreads_and(ok)) {
+        if (!kCluster) break;
+        dead = true;
+      }
+      if (tid == 0 && !(kCluster && dead) && t > row0 && t - 1 + p.ring_rows < row1) rows.copy(t - 1 + p.ring_rows);
       rows.complete(ring, st, t);
       if (dx) row_r = rows.row(ring, 0, st, t), row_x = rows.row(ring, 1, st, t);
       if (dres) row_d = rows.row(ring, 2, st, t);
@@ -526,45 +553,45 @@ __global__ void __launch_bounds__(kThreads ? kThreads : 512, 512 / (kThreads ? k
     float s[NV];
     if (dx) {
       float r[NV], x[NV], w[NV], srr = 0.0f, ser = 0.0f;
-      load_across<kThreads, kRing>(r, row_r, p.D, 0.0f);
-      load_across<kThreads, kRing>(x, row_x, p.D, 0.0f);
-      load_across<kThreads, kRing>(w, pre, p.D, 1.0f);
+      load_across<kThreads, kRing>(r, row_r, D, 0.0f);
+      load_across<kThreads, kRing>(x, row_x, D, 0.0f);
+      load_across<kThreads, kRing>(w, pre, D, 1.0f);
 #pragma unroll
       for (int v = 0; v < NV; ++v) {
         srr += r[v] * r[v];
         ser += x[v] * w[v] * r[v];
       }
-      const float2 q = block_sum2(srr, ser, smem, buf);
+      const float2 q = row_sum2(srr, ser);
       const float rho = rsqrtf(q.x * inv_d + p.eps);
       const float k = rho * rho * rho * (q.y * inv_d);
       // (read again: the reduction would hold them in registers that the sums need)
-      load_across<kThreads, kRing>(r, row_r, p.D, 0.0f);
-      load_across<kThreads, kRing>(x, row_x, p.D, 0.0f);
-      load_across<kThreads, kRing>(w, pre, p.D, 1.0f);
-      load_across<kThreads, kRing>(s, row_d, p.D, 0.0f);
+      load_across<kThreads, kRing>(r, row_r, D, 0.0f);
+      load_across<kThreads, kRing>(x, row_x, D, 0.0f);
+      load_across<kThreads, kRing>(w, pre, D, 1.0f);
+      load_across<kThreads, kRing>(s, row_d, D, 0.0f);
 #pragma unroll
       for (int v = 0; v < NV; ++v) {
         s[v] += rho * (x[v] * w[v]) - k * r[v];
         s_pre[v] += x[v] * (r[v] * rho);
       }
     } else {
-      load_across<kThreads, kRing>(s, row_d, p.D, 0.0f);
+      load_across<kThreads, kRing>(s, row_d, D, 0.0f);
     }
     T* const to_r = dresid + t * p.dresid_rs;
     float y[NV], syy = 0.0f, sfy = 0.0f;
-    load_across<kThreads, kRing>(y, row_y, p.D, 0.0f);
+    load_across<kThreads, kRing>(y, row_y, D, 0.0f);
 #pragma unroll
     for (int v = 0; v < NV; ++v) {
       const int c = A::column(v);
       syy += y[v] * y[v];
       sfy += s[v] * gw[v] * y[v];
-      if (A::inside(v, p.D)) to_r[c] = from_f32<T>(p.scale * s[v]);
+      if (A::inside(v, D)) to_r[c] = from_f32<T>(p.scale * s[v]);
     }
     if (!block) continue;
     T* const to_y = dblock + t * p.dblock_rs;
     float rho = 1.0f, k = 0.0f;
     if (w_post) {
-      const float2 q = block_sum2(syy, sfy, smem, buf);
+      const float2 q = row_sum2(syy, sfy);
       rho = rsqrtf(q.x * inv_d + p.eps);
       k = rho * rho * rho * (q.y * inv_d);
     }
@@ -572,10 +599,10 @@ __global__ void __launch_bounds__(kThreads ? kThreads : 512, 512 / (kThreads ? k
     for (int v = 0; v < NV; ++v) {
       const int c = A::column(v);
       s_group[v] += s[v] * (y[v] * rho);
-      if (A::inside(v, p.D)) to_y[c] = from_f32<T>(rho * (s[v] * gw[v]) - k * y[v]);
+      if (A::inside(v, D)) to_y[c] = from_f32<T>(rho * (s[v] * gw[v]) - k * y[v]);
     }
   }
-  if (t < row1) {  // a copy did not come in time: let those on their way land
+  if (t < row1 || dead) {  // let the copies that are on their way land
     const uint64_t t0 = globaltimer_ns();
     while (globaltimer_ns() - t0 < 200000) {
     }
@@ -585,7 +612,7 @@ __global__ void __launch_bounds__(kThreads ? kThreads : 512, 512 / (kThreads ? k
 #pragma unroll
   for (int v = 0; v < NV; ++v) {
     const int c = A::column(v);
-    if (A::inside(v, p.D)) part[c] = s_pre[v];
+    if (A::inside(v, D)) part[c] = s_pre[v];
   }
 }
 
@@ -1316,6 +1343,30 @@ bool use_narrow_ring(NormParams* p, Shape* n) {
   return true;
 }
 
+// Rows of more than 8192: 512 threads a block, 12 or 16 columns a thread, which a block must have at least 8 or 12 of
+// (Across::kSure), and a ring of two rows.  Not every SM finds others for a cluster of more than 2.
+template <typename T>
+bool use_cluster(NormParams* p, Shape* n) {
+  const int64_t es = sizeof(T);
+  if (p->T < 2 || !narrow_fits(p->dnorm_out, p->dnorm_out_rs, *p, es) ||
+      !narrow_fits(p->dnorm_out ? p->resid_out : nullptr, p->resid_out_rs, *p, es) ||
+      !narrow_fits(p->dresid_out, p->dresid_out_rs, *p, es) || !narrow_fits(p->block, p->block_rs, *p, es))
+    return false;
+  for (int parts = 2; parts <= kMostParts; parts *= 2) {
+    const int64_t columns = cdiv64(p->D, parts), slot = narrow_slot(columns * es);
+    const int nv = columns <= 512 * 12 ? 12 : 16;
+    const int64_t rows = (kRingSmem - kRingOwn - 512 * nv * es) / (4 * slot);
+    if (columns > 512 * 16 || p->D / parts < 512 * (nv - 4) || rows < 2) continue;
+    *n = {512, nv};
+    p->parts = parts;
+    p->nb = std::max(1, parts == 2 ? p->nb / 2 : p->nb * 5 / (6 * parts));
+    p->ring_rows = int(std::min<int64_t>(8, rows));
+    p->ring_slot = uint32_t(slot);
+    return true;
+  }
+  return false;
+}
+
 template <typename T>
 cudaError_t launch_backward(NormParams p, cudaStream_t s) {
   constexpr int kWide = 16 / int(sizeof(T));
@@ -1325,7 +1376,17 @@ cudaError_t launch_backward(NormParams p, cudaStream_t s) {
                    p.D == int64_t(sh.threads) * sh.nv * kWide;
   cudaError_t e = cudaSuccess;
   Shape n;
-  if (!w && use_narrow_ring<T>(&p, &n)) {
+  if (!sh.threads && use_cluster<T>(&p, &n)) {
+    auto run = [&](auto nv) {
+      auto f = cconv_residual_norm_backward_kernel<T, decltype(nv)::value, 512, true>;
+      static bool ready[64] = {};
+      const cudaError_t e = allow_ring(f, ready);
+      if (e != cudaSuccess) return e;
+      return launch(f, dim3(unsigned(p.nb * p.parts)), 512, size_t(p.ring_rows) * 4 * p.ring_slot + 512 * nv * sizeof(T), p.parts,
+                    s, p);
+    };
+    e = n.nv == 12 ? run(std::integral_constant<int, 12>()) : run(std::integral_constant<int, 16>());
+  } else if (!w && use_narrow_ring<T>(&p, &n)) {
     e = with_narrow_shape(n, [&](auto nv, auto nt) {
       auto f = cconv_residual_norm_backward_kernel<T, decltype(nv)::value, decltype(nt)::value>;
       static bool ready[64] = {};

@@ -18,6 +18,7 @@ struct NormParams {
       dblock_rs, dgate_rs;
   int sums_by_group;
   int ring_rows;    // rows of the shared-memory ring
+  int parts;        // blocks of a cluster that share a row
   uint32_t ring_slot;  // bytes of a row of one array there, where rows begin anywhere
   int* status;      // where a bounded wait that ran out is noted
   uint64_t limit_ns;

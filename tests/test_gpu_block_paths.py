@@ -276,3 +276,23 @@ def test_norms_of_many_rows_with_parts_left_out():
         n.check_backward(n.run_backward(use_dr=False), use_dr=False)
         n.check_backward(n.run_backward(use_dx=False), use_dx=False)
     assert block.status() == (0, 0)
+
+
+# rows shared by the 2, 4 and 8 blocks of a cluster, the shortest and longest of each; rows that no cluster takes
+@pytest.mark.parametrize("T,D,dtype,gate,rows", [
+    (300, 8193, BF16, "groups", 33), (40, 16384, BF16, "all", 0), (37, 16385, FP16, "groups", 1), (150, 32768, BF16, "none", 0),
+    (5, 32769, BF16, "groups", 2), (160, 65536, FP16, "groups", 160), (3, 65537, BF16, "all", 0), (200, 9999, FP32, "groups", 7),
+    (6, 14000, FP32, "all", 0), (33, 20000, FP32, "groups", 33), (2, 12288, BF16, "groups", 1), (1, 16384, BF16, "all", 0)])
+@pytest.mark.parametrize("by,pad", [(0, 0), (1, 3)])
+def test_norm_gradients_of_long_rows(T, D, dtype, gate, rows, by, pad):
+    n = Norm(T, D, dtype, gate, rows, scale=0.75)
+    for name in ("r", "y", "dr", "dx"):
+        setattr(n, name, shifted(getattr(n, name), D + pad, by))
+    got = n.run_backward()
+    n.check_backward(got)
+    for again in range(3):  # sums in a fixed order
+        for a, b in zip(got, n.run_backward()):
+            assert a is b or torch.equal(a, b)
+    n.check_backward(n.run_backward(use_dr=False), use_dr=False)
+    n.check_backward(n.run_backward(use_dx=False), use_dx=False)
+    assert block.status() == (0, 0)
