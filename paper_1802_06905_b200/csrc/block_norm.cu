@@ -1161,14 +1161,14 @@ int64_t blocks_an_sm(int64_t D, int es) {
 }
 
 // Threads a block and accesses a thread for rows of D elements taken E at a time: at most `held`
-// elements a thread, whole warps, one access a thread as long as that leaves 256 threads or fewer.
+// elements a thread, whole warps, one access a thread as long as that leaves `few` threads or fewer.
 struct Shape {
   int threads, nv;
 };
-Shape shape_of(int64_t D, int E, int held, int most) {
+Shape shape_of(int64_t D, int E, int held, int most, int few = 256) {
   const int64_t acc = cdiv64(D, E);
   int nv = 1;
-  while (nv * E < held && acc > int64_t(nv) * 256) nv *= 2;
+  while (nv * E < held && acc > int64_t(nv) * few) nv *= 2;
   const int64_t threads = round_up64(cdiv64(acc, nv), 32);
   return threads <= most ? Shape{int(threads), nv} : Shape{0, 0};
 }
@@ -1371,7 +1371,9 @@ template <typename T>
 cudaError_t launch_backward(NormParams p, cudaStream_t s) {
   constexpr int kWide = 16 / int(sizeof(T));
   const bool w = wide(p, sizeof(T), true) && ring_rows(p.D, sizeof(T), blocks_an_sm(p.D, sizeof(T))) >= 2;
-  const Shape sh = shape_of(p.D, w ? kWide : 1, 16, 512);
+  // Many wide rows: all of 16 elements a thread, for which blocks_an_sm counts (16384 x 1000 bf16: 64 us, with
+  // 8 elements, of whose blocks not all fit, 73 us).
+  const Shape sh = shape_of(p.D, w ? kWide : 1, 16, 512, w && p.T >= 4 * int64_t(p.nb) ? 32 : 256);
   const bool all = p.dnorm_out && p.dresid_out && p.block && p.w_pre && p.w_post && p.gate &&
                    p.D == int64_t(sh.threads) * sh.nv * kWide;
   cudaError_t e = cudaSuccess;
