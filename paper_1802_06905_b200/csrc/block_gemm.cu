@@ -952,43 +952,72 @@ double fixed_clocks(const Launch& l, int block_n) {
   return (l.splits == 1 ? 14600.0 : l.splits == 2 ? 20000.0 : 23000.0) + epilogue;
 }
 
-// Copies of rows that are contiguous on both sides, several at once: blockIdx.z is the copy, an access is the
-// largest of 16, 8, 4, 2, 1 bytes that its addresses, pitches and rows allow; 64 threads by 4 rows a block,
-// 4 accesses a thread.
+// Copies of rows that are contiguous on both sides, several at once: blockIdx.z is the copy, 64 threads by 4
+// rows a block, 4 pieces of 16 bytes a thread.  Rows that begin anywhere are written in the target's pieces,
+// each from the five words of the source that it lies in; pieces that a row's ends cut, and those whose words would
+// reach out of the source, go byte by byte (two operands of 4000 x 4095 and 4095 x 4095 bytes: 35 us; with the
+// widest accesses that both sides' alignment allows, which is a byte there, 70 us).
 struct RowCopy {
   const char* from;
   char* to;
   int64_t from_pitch, to_pitch, rows, bytes;  // pitches and row length in bytes
-  int access;
+  int aligned;                                // all of them, and the addresses, to 16 bytes
 };
 struct RowCopies {
   RowCopy of[kMostCopies];
 };
-template <typename E>
-__device__ __forceinline__ void copy_rows(const RowCopy& c) {
-  const int64_t pieces = c.bytes / int64_t(sizeof(E));
-  for (int64_t x0 = int64_t(blockIdx.x) * 256 + (threadIdx.x & 63); x0 < pieces; x0 += int64_t(gridDim.x) * 256) {
-    for (int64_t r = int64_t(blockIdx.y) * 4 + (threadIdx.x >> 6); r < c.rows; r += int64_t(gridDim.y) * 4) {
-      const E* src = reinterpret_cast<const E*>(c.from + r * c.from_pitch);
-      E* dst = reinterpret_cast<E*>(c.to + r * c.to_pitch);
-      E v[4];
+__device__ __forceinline__ void copy_aligned_row(const RowCopy& c, int64_t r, int64_t x0) {
+  const uint4* src = reinterpret_cast<const uint4*>(c.from + r * c.from_pitch);
+  uint4* dst = reinterpret_cast<uint4*>(c.to + r * c.to_pitch);
+  uint4 v[4];
 #pragma unroll
-      for (int i = 0; i < 4; ++i)
-        if (x0 + 64 * i < pieces) v[i] = src[x0 + 64 * i];
+  for (int i = 0; i < 4; ++i)
+    if (x0 + 64 * i < c.bytes / 16) v[i] = src[x0 + 64 * i];
 #pragma unroll
-      for (int i = 0; i < 4; ++i)
-        if (x0 + 64 * i < pieces) dst[x0 + 64 * i] = v[i];
+  for (int i = 0; i < 4; ++i)
+    if (x0 + 64 * i < c.bytes / 16) dst[x0 + 64 * i] = v[i];
+}
+__device__ __forceinline__ void copy_row(const RowCopy& c, int64_t r, int64_t x0) {
+  const char* src = c.from + r * c.from_pitch;
+  char* dst = c.to + r * c.to_pitch;
+  const uintptr_t first = reinterpret_cast<uintptr_t>(c.from),
+                  last = first + uintptr_t((c.rows - 1) * c.from_pitch + c.bytes);  // the source, all of it
+  const int64_t lead = int64_t(reinterpret_cast<uintptr_t>(dst) & 15);
+  uint32_t w[4][5];
+  bool whole[4];
+#pragma unroll
+  for (int i = 0; i < 4; ++i) {
+    const int64_t at = (x0 + 64 * i) * 16 - lead;  // of the piece, from the row's start
+    const uintptr_t a = reinterpret_cast<uintptr_t>(src + at), words = a & ~uintptr_t(3);
+    whole[i] = at >= 0 && at + 16 <= c.bytes && words >= first && words + 20 <= last;
+    if (whole[i]) {
+#pragma unroll
+      for (int k = 0; k < 5; ++k) w[i][k] = reinterpret_cast<const uint32_t*>(words)[k];
+    }
+  }
+#pragma unroll
+  for (int i = 0; i < 4; ++i) {
+    const int64_t at = (x0 + 64 * i) * 16 - lead;
+    if (whole[i]) {
+      const uint32_t by = uint32_t(reinterpret_cast<uintptr_t>(src + at) & 3) * 8;
+      *reinterpret_cast<uint4*>(dst + at) =
+          make_uint4(__funnelshift_r(w[i][0], w[i][1], by), __funnelshift_r(w[i][1], w[i][2], by),
+                     __funnelshift_r(w[i][2], w[i][3], by), __funnelshift_r(w[i][3], w[i][4], by));
+    } else {
+      for (int64_t k = max(at, int64_t(0)); k < min(at + 16, c.bytes); ++k) dst[k] = src[k];
     }
   }
 }
 __global__ void __launch_bounds__(256) cconv_copy_rows_kernel(const __grid_constant__ RowCopies copies) {
   start_in_order();
   const RowCopy& c = copies.of[blockIdx.z];
-  if (c.access == 16) copy_rows<uint4>(c);
-  else if (c.access == 8) copy_rows<uint2>(c);
-  else if (c.access == 4) copy_rows<uint32_t>(c);
-  else if (c.access == 2) copy_rows<uint16_t>(c);
-  else copy_rows<uint8_t>(c);
+  const int64_t pieces = (c.bytes + (c.aligned ? 15 : 30)) / 16;  // unaligned: at most
+  for (int64_t x0 = int64_t(blockIdx.x) * 256 + (threadIdx.x & 63); x0 < pieces; x0 += int64_t(gridDim.x) * 256) {
+    for (int64_t r = int64_t(blockIdx.y) * 4 + (threadIdx.x >> 6); r < c.rows; r += int64_t(gridDim.y) * 4) {
+      if (c.aligned) copy_aligned_row(c, r, x0);
+      else copy_row(c, r, x0);
+    }
+  }
 }
 
 // 32 x 32 elements a block through shared memory: read along the source's short stride, written along
@@ -1148,9 +1177,8 @@ cudaError_t run_row_copies(const Copy* copies, int n, cudaStream_t s) {
     r.to_pitch = k.to.rs * k.es;
     uintptr_t all = reinterpret_cast<uintptr_t>(r.from) | reinterpret_cast<uintptr_t>(r.to) | uintptr_t(r.bytes);
     if (r.rows > 1) all |= uintptr_t(r.from_pitch) | uintptr_t(r.to_pitch);
-    r.access = 16;
-    while (all & uintptr_t(r.access - 1)) r.access /= 2;
-    x = std::max(x, cdiv64(r.bytes / r.access, 256));
+    r.aligned = (all & 15) == 0;
+    x = std::max(x, cdiv64((r.bytes + 30) / 16, 256));
     y = std::max(y, cdiv64(r.rows, 4));
   }
   const dim3 grid(unsigned(std::min<int64_t>(x, 65535)), unsigned(std::min<int64_t>(y, 16384)), unsigned(n));
