@@ -54,27 +54,43 @@ class Steps {
     }
   }
 
-  // An operand of a product (rows x k) as it lies, or a copy of it with k contiguous.
-  Operand copied(const Mat& m, int64_t rows, int64_t k) {
-    const Mat to = scratch(rows, k, es_);
-    copy(m, to, rows, k, es_);
+  // An operand of a product (rows x k) as it lies, or a copy of it: in its own order, where the product takes that
+  // and the copies need not transpose, else with k contiguous.  A matrix that is copied in one order serves
+  // for both (dout and its transpose).
+  Operand copied(const Mat& m, int64_t rows, int64_t k, bool want_kmajor) {
+    const bool kmajor = want_kmajor || es_ != 2 || m.rs != 1 || m.cs == 1;
+    const Mat from = kmajor ? m : m.t();
+    const int64_t outer = kmajor ? rows : k, inner = kmajor ? k : rows;
+    Mat to;
+    for (const Copy& c : copies_)
+      if (m.p && c.from.p == from.p && c.from.rs == from.rs && c.from.cs == from.cs && c.rows == outer && c.cols == inner) to = c.to;
+    if (!to.rs) {
+      to = scratch(outer, inner, es_);
+      copy(from, to, outer, inner, es_);
+      Copy c;
+      c.from = from;
+      c.to = to;
+      c.rows = outer;
+      c.cols = inner;
+      copies_.push_back(c);
+    }
     Operand o;
     o.p = to.p;
     o.pitch = to.rs;
-    o.kmajor = true;
+    o.kmajor = kmajor;
     o.rows = rows;
     o.k = k;
     return o;
   }
   Operand operand(const Mat& m, int64_t rows, int64_t k, bool want_kmajor = false) {
     Operand o;
-    return operand_in_place(m, rows, k, es_, !want_kmajor && es_ == 2, &o) ? o : copied(m, rows, k);
+    return operand_in_place(m, rows, k, es_, !want_kmajor && es_ == 2, &o) ? o : copied(m, rows, k, want_kmajor);
   }
   // Two operands of one product, in the same order.
   void operands(const Mat& a, const Mat& b, int64_t rows, int64_t k, Operand* oa, Operand* ob) {
     *oa = operand(a, rows, k);
     *ob = operand(b, rows, k, oa->kmajor);
-    if (oa->kmajor != ob->kmajor) *oa = copied(a, rows, k);
+    if (oa->kmajor != ob->kmajor) *oa = copied(a, rows, k, true);
   }
   // A matrix that is read row by row.
   Mat readable(const cconv_matrix& m, int64_t rows, int64_t cols) {
@@ -123,7 +139,7 @@ class Steps {
   Carver ws_;
   const int sms_, es_, dtype_;
   std::vector<Step> steps_;
-  std::vector<Copy> pending_;
+  std::vector<Copy> pending_, copies_;  // to be launched; made for operands
 };
 
 }  // namespace cconv
