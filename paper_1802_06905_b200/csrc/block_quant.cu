@@ -3,8 +3,8 @@
 //   scale = max|x| / 448,  q = e4m3(x / scale), nearest, ties to even
 //
 // One pass: the values of a block stay in registers between its maximum and its rounding.  3 bytes an element
-// (16-bit x) pass through HBM, and about 13 instructions of a lane take as long to issue: tokens 8192 x 4096
-// bf16 21.8 us, 4.6 TB/s (the bytes alone: 15.4 us); weights 2600 x 2000 5.5 us.  Both quotients are correctly rounded, so
+// (16-bit x) pass through HBM, and about 12 instructions of a lane take as long to issue: tokens 8192 x 4096
+// bf16 20.6 us, 4.9 TB/s (the bytes alone: 15.4 us); weights 2600 x 2000 5.5 us.  Both quotients are correctly rounded, so
 // that the result is the definition's bit for bit.
 #include <algorithm>
 
@@ -79,13 +79,13 @@ struct Two<__half> {
   using type = __half2;
 };
 
-// Eight elements of a row: packed (16-bit types, 16 bytes at once) or one by one.
+// Eight elements of a row: packed (16-bit types, 16 bytes at once) or one by one, `step` apart in memory.
 template <typename T, bool kWide>
 struct Eight {
   float f[8];
-  __device__ __forceinline__ void load(const T* p, int64_t cs, int64_t n) {  // the first n are in range
+  __device__ __forceinline__ void load(const T* p, int64_t step, int64_t n) {  // the first n are in range
 #pragma unroll
-    for (int i = 0; i < 8; ++i) f[i] = i < n ? to_f32(p[i * cs]) : 0.0f;
+    for (int i = 0; i < 8; ++i) f[i] = i < n ? to_f32(p[i * step]) : 0.0f;
   }
   __device__ __forceinline__ void get(uint64_t (&o)[4]) const {
 #pragma unroll
@@ -121,13 +121,15 @@ struct Eight<T, true> {
   }
 };
 
-// kLanes lanes a row of 128 channels (pieces of 8 channels, 8 kLanes apart), U rows a lane.  kBlock = 1:
+// kLanes lanes a row of 128 channels, U rows a lane: pieces of 8 channels, 8 kLanes apart, or, where accesses are of
+// one element, every 16th channel, so that the lanes' are neighbours (8192 x 4095 bf16: 44 us; 8 channels a lane:
+// 95 us).  kBlock = 1:
 // each row has a scale, 256 threads.  kBlock = 128: 512 threads take 128 rows and one scale.
 // What a row costs besides its elements (the reduction, the scale, its addresses) keeps the issue slots
 // busier than the elements do; 8 lanes a row share it among fewer threads than 16 (tokens 8192 x 4096
 // bf16: 1.2 times as long with 16).  Blocks that stay and load their next rows while they work on these
 // were no faster (22.6 us with 3 an SM, 24.8 with 4, 23.7 with 4 rows a lane and 2).
-template <typename T, int kBlock, int kLanes, int U, bool kWide>
+template <typename T, int kBlock, int kLanes, int U, bool kWide, bool kUnit>
 __global__ void __launch_bounds__(kBlock == 1 ? 256 : 512, U == 2 ? 4 : 1) cconv_quantize_kernel(const QuantParams p) {
   constexpr int kAcross = (kBlock == 1 ? 256 : 512) / kLanes, kPieces = 16 / kLanes;
   static_assert(kBlock == 1 || U * kAcross == 128, "");
@@ -135,13 +137,16 @@ __global__ void __launch_bounds__(kBlock == 1 ? 256 : 512, U == 2 ? 4 : 1) cconv
   start_in_order();
   const T* x = static_cast<const T*>(p.x);
   const int sub = threadIdx.x % kLanes, row_in = threadIdx.x / kLanes;
-  const int64_t cb = blockIdx.x, c = cb * 128 + sub * 8;
-  const int cols = int(min(p.D - c, int64_t(128)));  // from c on; may be negative
+  constexpr int kStep = kWide ? 1 : kLanes;  // from one of a lane's channels to its next
+  const int64_t x_cs = kUnit ? 1 : p.x_cs, q_cs = kUnit ? 1 : p.q_cs;
+  static_assert(kWide || kPieces == 1, "");
+  const int64_t cb = blockIdx.x, c = cb * 128 + sub * (kWide ? 8 : 1);
+  const int cols = (int(min(p.D - c, int64_t(128))) + kStep - 1) / kStep;  // of a lane, from c on; may be negative
   for (int64_t rb = blockIdx.y; rb < p.row_blocks; rb += gridDim.y) {
     const int64_t t0 = rb * U * kAcross + row_in;
     const int rows = int(min(int64_t(U * kAcross), p.T - t0));  // from t0 on; may be negative
-    const T* from = x + t0 * p.x_rs + c * p.x_cs;
-    uint8_t* q = p.q + t0 * p.q_rs + c * p.q_cs;
+    const T* from = x + t0 * p.x_rs + c * x_cs;
+    uint8_t* q = p.q + t0 * p.q_rs + c * q_cs;
     float* scales = p.scale + (kBlock == 1 ? t0 : rb) * p.scale_rs + cb * p.scale_cs;
     Eight<T, kWide> v[U][kPieces];
     uint32_t m[U];
@@ -149,7 +154,7 @@ __global__ void __launch_bounds__(kBlock == 1 ? 256 : 512, U == 2 ? 4 : 1) cconv
     for (int i = 0; i < U; ++i)
 #pragma unroll
       for (int j = 0; j < kPieces; ++j)
-        v[i][j].load(from + i * (kAcross * p.x_rs) + j * (8 * kLanes * p.x_cs), p.x_cs, i * kAcross < rows ? cols - j * 8 * kLanes : 0);
+        v[i][j].load(from + i * (kAcross * p.x_rs) + j * (8 * kLanes * x_cs), kStep * x_cs, i * kAcross < rows ? cols - j * 8 * kLanes : 0);
 #pragma unroll
     for (int i = 0; i < U; ++i) {
       m[i] = v[i][0].largest();
@@ -191,24 +196,24 @@ __global__ void __launch_bounds__(kBlock == 1 ? 256 : 512, U == 2 ? 4 : 1) cconv
         by.template divide<sizeof(T) == 2 ? 1 : 2>(f);
         const int n = i * kAcross < rows ? cols - j * 8 * kLanes : 0;  // of eight channels, in range
         const uint32_t lo = e4m3x4(f[0], f[1]), hi = e4m3x4(f[2], f[3]);
-        uint8_t* to = q + i * (kAcross * p.q_rs) + j * (8 * kLanes * p.q_cs);
+        uint8_t* to = q + i * (kAcross * p.q_rs) + j * (8 * kLanes * q_cs);
         if (kWide) {
           if (n > 0) *reinterpret_cast<uint2*>(to) = make_uint2(lo, hi);
         } else {
 #pragma unroll
           for (int e = 0; e < 8; ++e)
-            if (e < n) to[e * p.q_cs] = uint8_t((e < 4 ? lo : hi) >> (8 * (e & 3)));
+            if (e < n) to[e * kStep * q_cs] = uint8_t((e < 4 ? lo : hi) >> (8 * (e & 3)));
         }
       }
     }
   }
 }
 
-template <typename T, int kBlock, int kLanes, int U, bool kWide>
+template <typename T, int kBlock, int kLanes, int U, bool kWide, bool kUnit>
 cudaError_t launch_as(QuantParams p, cudaStream_t s) {
   p.row_blocks = cdiv64(p.T, kBlock == 1 ? 256 / kLanes * U : 128);
   const dim3 grid(unsigned(cdiv64(p.D, 128)), unsigned(std::min<int64_t>(p.row_blocks, 65535)));
-  return launch(cconv_quantize_kernel<T, kBlock, kLanes, U, kWide>, grid, kBlock == 1 ? 256 : 512, 0, 1, s, p);
+  return launch(cconv_quantize_kernel<T, kBlock, kLanes, U, kWide, kUnit>, grid, kBlock == 1 ? 256 : 512, 0, 1, s, p);
 }
 
 template <typename T>
@@ -217,13 +222,17 @@ cudaError_t launch(const QuantParams& p, int block_rows, int sms, cudaStream_t s
   const uintptr_t out = reinterpret_cast<uintptr_t>(p.q) | uintptr_t(p.q_rs);
   const bool wide = sizeof(T) == 2 && p.D % 8 == 0 && p.x_cs == 1 && p.q_cs == 1 && (in & 15) == 0 && (out & 7) == 0;
   if constexpr (sizeof(T) == 2) {
-    if (wide && block_rows == 128) return launch_as<T, 128, 16, 4, true>(p, s);
+    if (wide && block_rows == 128) return launch_as<T, 128, 16, 4, true, true>(p, s);
     // two rows a lane where that still fills the SMs (loads on their way cover HBM's latency), else one
-    if (wide && cdiv64(p.T, 64) * cdiv64(p.D, 128) >= 4 * sms) return launch_as<T, 1, 8, 2, true>(p, s);
-    if (wide) return launch_as<T, 1, 16, 1, true>(p, s);
+    if (wide && cdiv64(p.T, 64) * cdiv64(p.D, 128) >= 4 * sms) return launch_as<T, 1, 8, 2, true, true>(p, s);
+    if (wide) return launch_as<T, 1, 16, 1, true, true>(p, s);
   }
-  if (block_rows == 128) return launch_as<T, 128, 16, 4, false>(p, s);
-  return launch_as<T, 1, 16, 1, false>(p, s);
+  if (p.x_cs == 1 && p.q_cs == 1) {  // (rows of an odd length: no multiplications for their addresses)
+    if (block_rows == 128) return launch_as<T, 128, 16, 4, false, true>(p, s);
+    return launch_as<T, 1, 16, 1, false, true>(p, s);
+  }
+  if (block_rows == 128) return launch_as<T, 128, 16, 4, false, false>(p, s);
+  return launch_as<T, 1, 16, 1, false, false>(p, s);
 }
 
 }  // namespace
