@@ -1,4 +1,4 @@
-// Products of at most 8 tokens: the weights are read once, straight into the registers that multiply them.
+// Products of at most 16 tokens: the weights are read once, straight into the registers that multiply them.
 //
 // What bounds them is HBM (a token costs 2 flops a weight), so the kernels are made of loads in flight: a
 // tile is 16 rows of weights (8 of each matrix of the gated pair, or 8 of one where 16 would leave SMs
@@ -8,7 +8,8 @@
 // take operands from registers as they come from memory; tcgen05 would want them in shared memory first, for
 // tiles that a few tokens leave almost empty.  Measured: one token 2048 x 8192 16 bits 23.2 us for 100.7 MB, 4.35 TB/s
 // (a kernel that only reads as much, from as many threads: 18.4 to 20.7 us); two tokens 8192 x 4096 8 bits 10.2 us
-// (reading alone: 8.2 us).
+// (reading alone: 8.2 us).  9 to 16 tokens take two such instructions a step (kEights = 2): 2048 x 8192 30 us and 512 x
+// 1408 5.3, on pairs of CTAs 39 and 15; 8 bits 4096 x 4096 9.0, on pairs 14.4, and 8192 x 4096 16 on both.
 //
 // k is permuted inside a step: lane q of a row holds 16 neighbouring bytes of k, which stand for two
 // pairs of fragment registers.  Weights and tokens are permuted alike, so the sums are those of the definition.
@@ -71,12 +72,8 @@ struct FewParams {
   int out_dtype;
 };
 
-// Sums of the block's warps: element (row r, token t) of the 16 x 8 tile.
-__device__ __forceinline__ void gather(float (*smem)[128], const float (&acc)[4], int warp, int lane) {
-#pragma unroll
-  for (int i = 0; i < 4; ++i) smem[warp][i * 32 + lane] = acc[i];
-  __syncthreads();
-}
+// The sum of the block's warps for element (row r, token t) of a 16 x 8 tile, of which each wrote accumulator i of
+// lane l at [i * 32 + l].
 __device__ __forceinline__ float gathered(float (*smem)[128], int r, int t) {
   const int at = ((r >> 3) * 2 + (t & 1)) * 32 + (r & 7) * 4 + (t >> 1);
   float s = 0.0f;
@@ -99,9 +96,9 @@ enum Rows { kPair, kSixteen, kEight };
 // A block's tiles are blockIdx.x, blockIdx.x + gridDim.x, ...; every warp takes the same number of batches of
 // each.  A step is 64 bytes of k a row (32 elements of 16 bits, or 64 of 8, two of which make a block that
 // shares a scale); a batch is 8 loads a lane.
-template <typename T, Rows kRows>
+template <typename T, Rows kRows, int kEights>
 __global__ void __launch_bounds__(kWarps * 32, 2) cconv_few_kernel(const FewParams p) {
-  __shared__ float smem[2][kWarps][128];
+  __shared__ float smem[2][kEights][kWarps][128];
   constexpr bool kFp8 = std::is_same<T, E4m3>::value;
   constexpr int kSteps = kRows == kEight ? 8 : 4, kHalf = kRows == kEight ? 1 : 2;
   constexpr int kTile = kRows == kSixteen ? 16 : 8;
@@ -140,61 +137,68 @@ __global__ void __launch_bounds__(kWarps * 32, 2) cconv_few_kernel(const FewPara
   if (!p.weights_there) load(w[0]);
 
   // Column g of a tile is token g; tokens in two parts (at most 4) take columns g and g + 4.
-  const bool parts = !kFp8 && kRows != kPair && p.x_lo != 0;
-  const int token = parts ? g & 3 : g;
-  const char* const x = p.x + min(token, p.T - 1) * p.x_rs + (parts && g >= 4 ? p.x_lo : 0) + q * 16;
-  float acc[4] = {};
+  const bool parts = !kFp8 && kRows != kPair && kEights == 1 && p.x_lo != 0;
+  float acc[kEights][4] = {};
   int tile = blockIdx.x, batch = 0, parity = 0;
   auto use = [&](const uint4 (&a)[8]) {
     const int sb = s0 + batch * kSteps;
-    uint4 v[kSteps];
 #pragma unroll
-    for (int i = 0; i < kSteps; ++i) {
-      const int64_t at = int64_t(sb + i) * 64;
-      v[i] = token < p.T && sb + i < s1 && at + q * 16 < p.k_bytes ? load_tokens(x + at) : none;
-    }
-    if constexpr (!kFp8) {
+    for (int e = 0; e < kEights; ++e) {
+      const int token = parts ? g & 3 : g + 8 * e;
+      const char* const x = p.x + min(token, p.T - 1) * p.x_rs + (parts && g >= 4 ? p.x_lo : 0) + q * 16;
+      uint4 v[kSteps];
 #pragma unroll
       for (int i = 0; i < kSteps; ++i) {
-        const uint4 a0 = a[i * kHalf], a1 = kHalf == 2 ? a[i * kHalf + kHalf - 1] : none;
-        mma<T>(acc, a0.x, a1.x, a0.y, a1.y, v[i].x, v[i].y);
-        mma<T>(acc, a0.z, a1.z, a0.w, a1.w, v[i].z, v[i].w);
+        const int64_t at = int64_t(sb + i) * 64;
+        v[i] = token < p.T && sb + i < s1 && at + q * 16 < p.k_bytes ? load_tokens(x + at) : none;
       }
-    } else {
-      // the sums of a block of 128 are scaled before they are added up; the rows of a tile share their scale
-      const int64_t nb = int64_t(tile) * kTile >> 7;
-      const int t0 = min(2 * q, p.T - 1), t1 = min(2 * q + 1, p.T - 1);  // the tokens whose sums this lane holds
+      if constexpr (!kFp8) {
 #pragma unroll
-      for (int j = 0; j < kSteps / 2; ++j) {
-        if (sb + 2 * j < s1) {
-          const int64_t kb = (sb >> 1) + j;
-          const float s = p.sb[nb * p.sb_rs + kb * p.sb_ks];
-          const float sa0 = s * p.sa[t0 * p.sa_rs + kb * p.sa_ks], sa1 = s * p.sa[t1 * p.sa_rs + kb * p.sa_ks];
-          float d[4] = {};
+        for (int i = 0; i < kSteps; ++i) {
+          const uint4 a0 = a[i * kHalf], a1 = kHalf == 2 ? a[i * kHalf + kHalf - 1] : none;
+          mma<T>(acc[e], a0.x, a1.x, a0.y, a1.y, v[i].x, v[i].y);
+          mma<T>(acc[e], a0.z, a1.z, a0.w, a1.w, v[i].z, v[i].w);
+        }
+      } else {
+        // the sums of a block of 128 are scaled before they are added up; the rows of a tile share their scale
+        const int64_t nb = int64_t(tile) * kTile >> 7;
+        const int t0 = min(8 * e + 2 * q, p.T - 1), t1 = min(8 * e + 2 * q + 1, p.T - 1);  // whose sums this lane holds
 #pragma unroll
-          for (int i = 2 * j; i < 2 * j + 2; ++i) {
-            const uint4 a0 = a[i * kHalf], a1 = kHalf == 2 ? a[i * kHalf + kHalf - 1] : none;
-            mma<T>(d, a0.x, a1.x, a0.y, a1.y, v[i].x, v[i].y);
-            mma<T>(d, a0.z, a1.z, a0.w, a1.w, v[i].z, v[i].w);
+        for (int j = 0; j < kSteps / 2; ++j) {
+          if (sb + 2 * j < s1) {
+            const int64_t kb = (sb >> 1) + j;
+            const float s = p.sb[nb * p.sb_rs + kb * p.sb_ks];
+            const float sa0 = s * p.sa[t0 * p.sa_rs + kb * p.sa_ks], sa1 = s * p.sa[t1 * p.sa_rs + kb * p.sa_ks];
+            float d[4] = {};
+#pragma unroll
+            for (int i = 2 * j; i < 2 * j + 2; ++i) {
+              const uint4 a0 = a[i * kHalf], a1 = kHalf == 2 ? a[i * kHalf + kHalf - 1] : none;
+              mma<T>(d, a0.x, a1.x, a0.y, a1.y, v[i].x, v[i].y);
+              mma<T>(d, a0.z, a1.z, a0.w, a1.w, v[i].z, v[i].w);
+            }
+            acc[e][0] += sa0 * d[0];
+            acc[e][1] += sa1 * d[1];
+            acc[e][2] += sa0 * d[2];
+            acc[e][3] += sa1 * d[3];
           }
-          acc[0] += sa0 * d[0];
-          acc[1] += sa1 * d[1];
-          acc[2] += sa0 * d[2];
-          acc[3] += sa1 * d[3];
         }
       }
     }
     if (++batch < batches) return;
     batch = 0;
-    gather(smem[parity], acc, warp, lane);
-    acc[0] = acc[1] = acc[2] = acc[3] = 0.0f;
+#pragma unroll
+    for (int e = 0; e < kEights; ++e) {
+#pragma unroll
+      for (int i = 0; i < 4; ++i) smem[parity][e][warp][i * 32 + lane] = acc[e][i], acc[e][i] = 0.0f;
+    }
+    __syncthreads();
     const int64_t n0 = int64_t(tile) * kTile;
     const int r = threadIdx.x % kTile, t = threadIdx.x / kTile;
     if (t < p.T && n0 + r < p.N) {
-      float f = gathered(smem[parity], r, t);
-      if (parts) f += gathered(smem[parity], r, t + 4);
+      float f = gathered(smem[parity][t >> 3 & (kEights - 1)], r, t & 7);
+      if (parts) f += gathered(smem[parity][0], r, t + 4);
       if constexpr (kRows == kPair) {
-        const float up = gathered(smem[parity], r + 8, t);
+        const float up = gathered(smem[parity][t >> 3 & (kEights - 1)], r + 8, t & 7);
         float h[1] = {f};
         const float u[1] = {up};
         gate(p.act, h, u);
@@ -224,11 +228,16 @@ __global__ void __launch_bounds__(kWarps * 32, 2) cconv_few_kernel(const FewPara
   }
 }
 
-template <typename T, Rows kRows>
-cudaError_t launch_rows(const FewParams& p, int sms, cudaStream_t s) {
+template <typename T, Rows kRows, int kEights>
+cudaError_t launch_eights(const FewParams& p, int sms, cudaStream_t s) {
   const int64_t tiles = cdiv64(p.N, kRows == kSixteen ? 16 : 8);
   const dim3 grid(unsigned(std::min<int64_t>(tiles, 2 * sms)));
-  return launch(cconv_few_kernel<T, kRows>, grid, kWarps * 32, 0, 1, s, p);
+  return launch(cconv_few_kernel<T, kRows, kEights>, grid, kWarps * 32, 0, 1, s, p);
+}
+template <typename T, Rows kRows>
+cudaError_t launch_rows(const FewParams& p, int sms, cudaStream_t s) {
+  if (p.T > 8) return launch_eights<T, kRows, 2>(p, sms, s);
+  return launch_eights<T, kRows, 1>(p, sms, s);
 }
 
 // 16 rows a tile where that leaves no SM idle: one token, 16 bits, the product back to 4096 channels as part of

@@ -8,7 +8,7 @@
 
 namespace cconv {
 
-constexpr int64_t kFewTokens = 8, kFewTokensInParts = 4;
+constexpr int64_t kFewTokens = 16, kFewTokensInParts = 4;
 
 // Whether rows x k weights (es bytes an element) and tokens can be read by these kernels: k contiguous in
 // pieces of 16 bytes, addresses and pitches multiples of 16 bytes.

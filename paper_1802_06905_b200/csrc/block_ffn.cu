@@ -7,7 +7,7 @@
 //             dWg = dg^T x, dWu = du^T x, dWd = dy^T h
 //             the last four in one launch where their tiles together fill the SMs better than apart
 //
-// Up to 8 tokens go through the kernels that stream the weights instead (forward).
+// Up to 16 tokens go through the kernels that stream the weights instead (forward).
 #include "block_ffn.h"
 
 #include <algorithm>

@@ -2,7 +2,7 @@
 //
 // C[m][n] = sum_kb sa[m][kb] sb[n/128][kb] (A B^T)_kb: the tensor cores form the sums of one block of 128
 // (one stage: 128 bytes of k a row), which the epilogue warps scale and add up in fp32 registers while the
-// next block's are formed.  Up to 8 tokens go through the kernel that streams the weights instead.
+// next block's are formed.  Up to 16 tokens go through the kernel that streams the weights instead.
 #include "block_fp8.h"
 
 #include "block.h"

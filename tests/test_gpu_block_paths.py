@@ -44,6 +44,30 @@ def test_few_tokens_round_the_result_alone(T, dtype, most):
         assert (out.double() - want).norm() <= most * want.norm()
 
 
+@pytest.mark.parametrize("T", [5, 8, 9, 11, 15, 16, 17])
+@pytest.mark.parametrize("D,F", [(512, 1408), (2400, 520), (72, 2400), (8, 16)])
+def test_few_tokens_either_side_of_their_limits(T, D, F):
+    for dtype, save in ((BF16, True), (FP16, False)):
+        f = Ffn(T, D, F, dtype, "gelu_tanh")
+        f.check_forward(*f.forward(save), "forward")
+        wide = Ffn(T, D, F, dtype, "gelu_tanh")
+        for n in ("x", "wg", "wu", "wd"):
+            v = getattr(f, n)
+            setattr(wide, n, shifted(v, v.shape[1] + 16, 8))
+        wide.check_forward(*wide.forward(save), "rows with a pitch")
+
+
+@pytest.mark.parametrize("M", [5, 8, 9, 13, 16, 17])
+@pytest.mark.parametrize("N,K", [(1408, 512), (4800, 144), (24, 4096), (130, 16)])
+def test_few_tokens_in_8_bits_either_side_of_their_limits(M, N, K):
+    a, sa, b, sb = fp8_operands(M, N, K)
+    for dtype in (BF16, FP16, FP32):
+        out = poisoned((M, N), dtype)
+        block.fp8_product(a, sa, b, sb, out)
+        fp8_check(a, sa, b, sb, out)
+    assert block.status() == (0, 0)
+
+
 def test_few_tokens_whose_hidden_values_overflow():
     f = Ffn(2, 128, 256, FP16)
     f.x[1] *= 3000.0  # h passes 65504 for this token only
