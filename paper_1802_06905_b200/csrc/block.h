@@ -42,4 +42,7 @@ class Carver {
 int block_sm_count();
 int block_cuda_error(cudaError_t e, const char* where);
 
+// Kernels and memsets that this host thread has put into streams for the sub-block, so far.
+int64_t& block_launches();
+
 }  // namespace cconv

@@ -38,6 +38,11 @@ int block_sm_count() {
   return n;
 }
 
+int64_t& block_launches() {
+  static thread_local int64_t n = 0;
+  return n;
+}
+
 namespace {
 
 constexpr int64_t kMaxLength = (int64_t(1) << 31) - 1024;  // of one dimension: coordinates of tiles are 32 bits
@@ -72,17 +77,22 @@ class Operands {
     }
     push({static_cast<const char*>(p), static_cast<const char*>(p) + need, 0, 0}, true);
   }
-  // Tells the stream's bookkeeping that a call with these operands is under way: its kernels wait for the work
-  // in front of them, but let the next be put in place, so that a convolution whose arrays meet these (their
-  // hulls, which may take in more) has to wait for it too.
-  void note(void* stream, int sms) const {
-    CallSpans c;
-    for (int i = 0; i < n_; ++i) {
-      Span& s = written_[i] ? c.out : c.image;
-      if (!s.lo || range_[i].lo < s.lo) s.lo = range_[i].lo;
-      if (!s.hi || range_[i].hi > s.hi) s.hi = range_[i].hi;
-    }
-    note_call(stream, c, Overlap::kInputsEarly, sms);
+  // Whether any result has an element.  A call without one launches nothing and needs no device.
+  bool writes() const {
+    for (int i = 0; i < n_; ++i)
+      if (written_[i]) return true;
+    return false;
+  }
+  // Runs the launches of a call with these operands, and then tells the stream's bookkeeping that it is under
+  // way: its kernels wait for the work in front of them (which the bookkeeping may forget from now on), but let
+  // the next be put in place, so that a convolution whose arrays meet these (their hulls, which may take in
+  // more) has to wait for it too.  A call that failed before its first launch waits for nothing: no entry.
+  template <typename F>
+  int run(void* stream, int sms, F launches) const {
+    const int64_t before = block_launches();
+    const int rc = launches();
+    if (block_launches() != before) note(stream, sms);
+    return rc;
   }
   // No output meets another output or an input; `same` names a pair that may be one matrix.
   bool distinct(const void* same_in = nullptr, const void* same_out = nullptr) const {
@@ -97,6 +107,15 @@ class Operands {
   }
 
  private:
+  void note(void* stream, int sms) const {
+    CallSpans c;
+    for (int i = 0; i < n_; ++i) {
+      Span& s = written_[i] ? c.out : c.image;
+      if (!s.lo || range_[i].lo < s.lo) s.lo = range_[i].lo;
+      if (!s.hi || range_[i].hi > s.hi) s.hi = range_[i].hi;
+    }
+    note_call(stream, c, Overlap::kInputsEarly, sms);
+  }
   static cconv_matrix vec(const void* v, int64_t n) { return cconv_matrix{const_cast<void*>(v), n, 1}; }
   void push(Bytes b, bool written) {
     range_[n_] = b;
@@ -152,15 +171,17 @@ bool ffn_sizes_ok(const cconv_ffn_args& a) {
          a.act <= CCONV_ACT_RELU && double(a.T) * a.F < 1e15 && double(a.D) * a.F < 1e15 && double(a.T) * a.D < 1e15;
 }
 
+cudaError_t zero_rows(void* p, int64_t pitch, int64_t bytes, int64_t rows, cudaStream_t s) {
+  const cudaError_t e = cudaMemset2DAsync(p, size_t(pitch), 0, size_t(bytes), size_t(rows), s);
+  block_launches() += e == cudaSuccess;
+  return e;
+}
 cudaError_t zero_out(const cconv_matrix& m, int64_t rows, int64_t cols, int es, cudaStream_t s) {
   if (rows == 0 || cols == 0) return cudaSuccess;
-  if (m.col_stride == 1 || cols == 1)
-    return cudaMemset2DAsync(m.data, size_t((rows == 1 ? cols : m.row_stride) * es), 0, size_t(cols * es), size_t(rows), s);
-  if (m.row_stride == 1 || rows == 1)
-    return cudaMemset2DAsync(m.data, size_t((cols == 1 ? rows : m.col_stride) * es), 0, size_t(rows * es), size_t(cols), s);
+  if (m.col_stride == 1 || cols == 1) return zero_rows(m.data, (rows == 1 ? cols : m.row_stride) * es, cols * es, rows, s);
+  if (m.row_stride == 1 || rows == 1) return zero_rows(m.data, (cols == 1 ? rows : m.col_stride) * es, rows * es, cols, s);
   for (int64_t r = 0; r < rows; ++r) {
-    cudaError_t e = cudaMemset2DAsync(static_cast<char*>(m.data) + r * m.row_stride * es, size_t(m.col_stride * es), 0,
-                                      size_t(es), size_t(cols), s);
+    const cudaError_t e = zero_rows(static_cast<char*>(m.data) + r * m.row_stride * es, m.col_stride * es, es, cols, s);
     if (e != cudaSuccess) return e;
   }
   return cudaSuccess;
@@ -278,13 +299,13 @@ int cconv_ffn_forward(const cconv_ffn_args* args, void* cuda_stream) {
       o.out(a.up_pre, a.T, a.F, 2);
     }
     if (!o.distinct()) return CCONV_EINVAL;
+    if (!o.writes()) return CCONV_OK;
     const int sms = block_sm_count();
     if (sms < 0) return sms;
     o.workspace(a.workspace, a.workspace_bytes, ffn_empty(a) ? 0 : ffn_workspace(a, false, sms));
     if (!o.distinct()) return CCONV_EINVAL;
-    o.note(cuda_stream, sms);
     cudaStream_t s = static_cast<cudaStream_t>(cuda_stream);
-    return ffn_empty(a) ? ffn_zeros(a, false, s) : run_ffn(a, false, sms, s);
+    return o.run(cuda_stream, sms, [&] { return ffn_empty(a) ? ffn_zeros(a, false, s) : run_ffn(a, false, sms, s); });
   });
 }
 
@@ -305,13 +326,13 @@ int cconv_ffn_backward(const cconv_ffn_args* args, void* cuda_stream) {
     o.out(a.dw_up, a.F, a.D, 2);
     o.out(a.dw_down, a.D, a.F, 2);
     if (!o.distinct()) return CCONV_EINVAL;
+    if (!o.writes()) return CCONV_OK;
     const int sms = block_sm_count();
     if (sms < 0) return sms;
     o.workspace(a.workspace, a.workspace_bytes, ffn_empty(a) ? 0 : ffn_workspace(a, true, sms));
     if (!o.distinct()) return CCONV_EINVAL;
-    o.note(cuda_stream, sms);
     cudaStream_t s = static_cast<cudaStream_t>(cuda_stream);
-    return ffn_empty(a) ? ffn_zeros(a, true, s) : run_ffn(a, true, sms, s);
+    return o.run(cuda_stream, sms, [&] { return ffn_empty(a) ? ffn_zeros(a, true, s) : run_ffn(a, true, sms, s); });
   });
 }
 
@@ -347,16 +368,17 @@ int cconv_residual_norm_forward(const cconv_residual_norm_args* args, void* cuda
     if (a.norm_out.data) o.out(a.norm_out, a.T, a.D, es);
     const bool same = a.resid.row_stride == a.resid_out.row_stride;
     if (!o.distinct(same ? a.resid.data : nullptr, a.resid_out.data)) return CCONV_EINVAL;
+    if (!o.writes()) return CCONV_OK;
     const int sms = block_sm_count();
     if (sms < 0) return sms;
-    if (a.T == 0 || a.D == 0) return CCONV_OK;
     NormParams p = norm_params(a);
     const int rc = block_status_word(&p.status);
     if (rc != CCONV_OK) return rc;
     p.limit_ns = block_wait_limit_ns();
-    o.note(cuda_stream, sms);
-    return block_cuda_error(run_norm_forward(p, a.dtype, sms, static_cast<cudaStream_t>(cuda_stream)),
-                            "cconv_residual_norm_forward");
+    return o.run(cuda_stream, sms, [&] {
+      return block_cuda_error(run_norm_forward(p, a.dtype, sms, static_cast<cudaStream_t>(cuda_stream)),
+                              "cconv_residual_norm_forward");
+    });
   });
 }
 
@@ -398,18 +420,19 @@ int cconv_residual_norm_backward(const cconv_residual_norm_args* args, void* cud
     const bool same = a.dresid_out.row_stride == a.dresid.row_stride;
     const void* same_in = same ? a.dresid_out.data : nullptr;
     if (!o.distinct(same_in, a.dresid.data)) return CCONV_EINVAL;
+    if (!o.writes()) return CCONV_OK;
     const int sms = block_sm_count();
     if (sms < 0) return sms;
     o.workspace(a.workspace, a.workspace_bytes, norm_workspace(a, sms));
     if (!o.distinct(same_in, a.dresid.data)) return CCONV_EINVAL;
-    if (a.D == 0) return CCONV_OK;
     cudaStream_t s = static_cast<cudaStream_t>(cuda_stream);
-    o.note(cuda_stream, sms);
     if (a.T == 0) {
-      if (a.dgate.data) BLOCK_CUDA(zero_out(a.dgate, gate_rows(a), a.D, es, s));
-      if (a.dw_post) BLOCK_CUDA(cudaMemsetAsync(a.dw_post, 0, size_t(a.D * es), s));
-      if (a.dw_pre) BLOCK_CUDA(cudaMemsetAsync(a.dw_pre, 0, size_t(a.D * es), s));
-      return CCONV_OK;
+      return o.run(cuda_stream, sms, [&]() -> int {
+        if (a.dgate.data) BLOCK_CUDA(zero_out(a.dgate, gate_rows(a), a.D, es, s));
+        if (a.dw_post) BLOCK_CUDA(zero_rows(a.dw_post, a.D * es, a.D * es, 1, s));
+        if (a.dw_pre) BLOCK_CUDA(zero_rows(a.dw_pre, a.D * es, a.D * es, 1, s));
+        return CCONV_OK;
+      });
     }
     NormParams p = norm_params(a);
     p.nb = norm_backward_blocks(a.T, a.D, type_bytes(a.dtype), sms);
@@ -417,7 +440,9 @@ int cconv_residual_norm_backward(const cconv_residual_norm_args* args, void* cud
     const int rc = block_status_word(&p.status);
     if (rc != CCONV_OK) return rc;
     p.limit_ns = block_wait_limit_ns();
-    return block_cuda_error(run_norm_backward(p, a.dtype, s), "cconv_residual_norm_backward");
+    return o.run(cuda_stream, sms, [&] {
+      return block_cuda_error(run_norm_backward(p, a.dtype, s), "cconv_residual_norm_backward");
+    });
   });
 }
 
@@ -442,14 +467,15 @@ int cconv_fp8_product(const cconv_fp8_product_args* args, void* cuda_stream) {
     o.in(a.b_scale, cdiv64(a.N, 128), cdiv64(a.K, 128), 4);
     o.out(a.c, a.M, a.N, es);
     if (!o.distinct()) return CCONV_EINVAL;
+    if (!o.writes()) return CCONV_OK;
     const int sms = block_sm_count();
     if (sms < 0) return sms;
     o.workspace(a.workspace, a.workspace_bytes, fp8_empty(a) ? 0 : fp8_workspace(a, sms));
     if (!o.distinct()) return CCONV_EINVAL;
     cudaStream_t s = static_cast<cudaStream_t>(cuda_stream);
-    o.note(cuda_stream, sms);
-    if (fp8_empty(a)) return block_cuda_error(zero_out(a.c, a.M, a.N, es, s), "cconv_fp8_product");
-    return run_fp8(a, sms, s);
+    return o.run(cuda_stream, sms, [&] {
+      return fp8_empty(a) ? block_cuda_error(zero_out(a.c, a.M, a.N, es, s), "cconv_fp8_product") : run_fp8(a, sms, s);
+    });
   });
 }
 
@@ -465,18 +491,19 @@ int cconv_quantize_blocks(const cconv_quantize_args* args, void* cuda_stream) {
     o.out(a.q, a.T, a.D, 1);
     o.out(a.scale, cdiv64(a.T, a.block_rows), cdiv64(a.D, 128), 4);
     if (!o.distinct()) return CCONV_EINVAL;
+    if (!o.writes()) return CCONV_OK;
     const int sms = block_sm_count();
     if (sms < 0) return sms;
-    if (a.T == 0 || a.D == 0) return CCONV_OK;
     QuantParams p{};
     p.T = a.T;
     p.D = a.D;
     p.x = a.x.data; p.x_rs = a.x.row_stride; p.x_cs = a.x.col_stride;
     p.q = static_cast<uint8_t*>(a.q.data); p.q_rs = a.q.row_stride; p.q_cs = a.q.col_stride;
     p.scale = static_cast<float*>(a.scale.data); p.scale_rs = a.scale.row_stride; p.scale_cs = a.scale.col_stride;
-    o.note(cuda_stream, sms);
-    return block_cuda_error(run_quantize(p, a.dtype, a.block_rows, sms, static_cast<cudaStream_t>(cuda_stream)),
-                            "cconv_quantize_blocks");
+    return o.run(cuda_stream, sms, [&] {
+      return block_cuda_error(run_quantize(p, a.dtype, a.block_rows, sms, static_cast<cudaStream_t>(cuda_stream)),
+                              "cconv_quantize_blocks");
+    });
   });
 }
 

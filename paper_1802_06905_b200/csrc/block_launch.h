@@ -2,6 +2,8 @@
 #pragma once
 #include <cuda_runtime.h>
 
+#include "block.h"
+
 namespace cconv {
 namespace {
 
@@ -23,7 +25,9 @@ cudaError_t launch(F f, dim3 grid, int threads, size_t smem, int cluster, cudaSt
   attr[1].val.clusterDim.z = 1;
   cfg.attrs = attr;
   cfg.numAttrs = cluster > 1 ? 2 : 1;
-  return cudaLaunchKernelEx(&cfg, f, args...);
+  const cudaError_t e = cudaLaunchKernelEx(&cfg, f, args...);
+  block_launches() += e == cudaSuccess;
+  return e;
 }
 
 }  // namespace

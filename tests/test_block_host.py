@@ -150,3 +150,57 @@ def test_column_slices_of_one_array_are_distinct(lib):
     if not torch.cuda.is_available():
         s = ffn(lib, gate_pre=(at, 64, 1), up_pre=(at + 64, 64, 1))
         assert f(ctypes.addressof(s), None) in (binding.ECUDA, binding.EUNSUPPORTED)
+
+
+def call(lib, name, struct, stream=None, **kw):
+    """The code of entry point `name` with these arguments; tuples are matrices (address, strides)."""
+    s = struct_of(struct)()
+    for k, v in kw.items():
+        if isinstance(v, tuple):
+            m = getattr(s, k)
+            m.data, m.row_stride, m.col_stride = v
+        else:
+            setattr(s, k, v)
+    f = getattr(lib, name)
+    f.restype, f.argtypes = ctypes.c_int, [ctypes.c_void_p, ctypes.c_void_p]
+    return f(ctypes.addressof(s), stream)
+
+
+def at(i, pitch=256):
+    return (i << 20, pitch, 1)
+
+
+EMPTY = [
+    ("cconv_ffn_forward", "cconv_ffn_args",
+     dict(T=0, D=16, F=32, x=at(1), w_gate=at(2), w_up=at(3), w_down=at(4), out=at(5), gate_pre=at(6), up_pre=at(7))),
+    ("cconv_ffn_forward", "cconv_ffn_args", dict(T=4, D=0, F=32, x=at(1), w_gate=at(2), w_up=at(3), w_down=at(4), out=at(5))),
+    ("cconv_ffn_backward", "cconv_ffn_args",
+     dict(T=4, D=0, F=32, x=at(1), dout=at(2), gate_pre=at(3), up_pre=at(4), dx=at(5), dw_gate=at(6), dw_up=at(7), dw_down=at(8))),
+    ("cconv_ffn_backward", "cconv_ffn_args", dict(T=0, D=16, F=0, dx=at(1))),
+    ("cconv_residual_norm_forward", "cconv_residual_norm_args",
+     dict(T=0, D=256, scale=1.0, eps=1e-6, resid=at(1), resid_out=at(2), norm_out=at(3))),
+    ("cconv_residual_norm_backward", "cconv_residual_norm_args",
+     dict(T=0, D=256, scale=1.0, eps=1e-6, resid_out=at(1), dnorm_out=at(2), dresid=at(3))),
+    ("cconv_residual_norm_backward", "cconv_residual_norm_args",
+     dict(T=4, D=0, scale=1.0, eps=1e-6, resid_out=at(1), dnorm_out=at(2), dresid=at(3))),
+    ("cconv_fp8_product", "cconv_fp8_product_args",
+     dict(M=0, N=256, K=256, a=at(1), b=at(2), a_scale=at(3, 2), b_scale=at(4, 2), c=at(5))),
+    ("cconv_fp8_product", "cconv_fp8_product_args",
+     dict(M=4, N=0, K=256, a=at(1), b=at(2), a_scale=at(3, 2), b_scale=at(4, 2), c=at(5))),
+    ("cconv_quantize_blocks", "cconv_quantize_args", dict(T=0, D=256, block_rows=1, x=at(1), q=at(2), scale=at(3, 2))),
+]
+
+
+@pytest.mark.parametrize("name,struct,args", EMPTY)
+def test_a_call_without_results_leaves_the_stream_alone(lib, name, struct, args):
+    """It launches nothing, so that it needs no device and completes nothing: a convolution in front of it may
+    still be running afterwards, and one that reads its Out has to wait."""
+    key = 0x7E560000 + 256 * EMPTY.index((name, struct, args))
+    far = 1 << 40
+
+    def probe(image, out):
+        return binding.stream_order_probe(key, (far + image, far + image + 4096), (far, far + 16), (far + out, far + out + 4096),
+                                          2, 28.0, 0.0, 148)
+    assert probe(1 << 20, 2 << 20) == 0
+    assert call(lib, name, struct, stream=key, **args) == binding.OK
+    assert probe(2 << 20, 3 << 20) == 1

@@ -320,3 +320,38 @@ def test_norm_gradients_of_long_rows(T, D, dtype, gate, rows, by, pad):
     n.check_backward(n.run_backward(use_dr=False), use_dr=False)
     n.check_backward(n.run_backward(use_dx=False), use_dx=False)
     assert block.status() == (0, 0)
+
+
+def test_an_empty_call_between_two_convolutions_keeps_them_in_order():
+    """The same with calls of zero length, which launch nothing: the second convolution follows the first."""
+    B, C, K, H = 64, 64, 128, 14
+    g = gen(12)
+    image = normal(g, (H + 2, H + 2, C, B), BF16)
+    f1, f2 = normal(g, (C, 3, 3, C), BF16, (9 * C) ** -0.5), normal(g, (K, 1, 1, C), BF16, C ** -0.5)
+    e = Ffn(0, 128, 256)
+    a, sa, b, sb = fp8_operands(2, 128, 128)
+    no, row = torch.empty((0, 128), dtype=BF16, device="cuda"), torch.empty((0, 1), device="cuda")
+    between = (lambda: e.forward(True), lambda: block.fp8_product(a[:0], sa[:0], b, sb, no),
+               lambda: block.residual_norm_backward(None, no, no, torch.empty_like(no)),
+               lambda: block.quantize_blocks(no, torch.empty((0, 128), dtype=E4M3, device="cuda"), row))
+    middles = [torch.empty((C, H, H, B), dtype=BF16, device="cuda") for _ in range(12)]
+
+    def chain(sync):
+        outs = []
+        for mid in middles:
+            mid.zero_()
+        torch.cuda.synchronize()
+        for i, mid in enumerate(middles):
+            out = torch.zeros((K, H, H, B), dtype=BF16, device="cuda")
+            for one in (lambda: binding.conv_forward(image, f1, mid, B, C, C, H, H, 3, 3), between[i % 4],
+                        lambda: binding.conv_forward(mid.view(H, H, C, B), f2, out, B, C, K, H, H, 1, 1)):
+                one()
+                if sync:
+                    torch.cuda.synchronize()
+            outs.append(out)
+        torch.cuda.synchronize()
+        return outs
+    want = chain(True)
+    for _ in range(3):
+        for x, y in zip(want, chain(False)):
+            assert torch.equal(x, y)
