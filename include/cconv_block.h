@@ -25,8 +25,9 @@
  * 256-byte aligned, of at least the size that the matching *_workspace function gives for the same
  * arguments; its contents do not matter before or after a call, and calls that may run at the same
  * time need workspaces of their own.  Outputs must not overlap inputs, each other or the workspace,
- * but for the two cases named below.  Calls are asynchronous on `cuda_stream`, ordered with the
- * stream's other work like any kernel, allocate nothing, and may be captured in a CUDA graph.
+ * but for the two cases named below, where an output may be one input itself (address and strides).
+ * Calls are asynchronous on `cuda_stream`, ordered with the stream's other work like any kernel,
+ * allocate nothing, and may be captured in a CUDA graph.
  *
  * Errors: CCONV_OK (0) or a negative code as in cconv.h; nothing throws, aborts or traps.  Lengths
  * may be zero (the result is then empty, gradients of weights are zero).

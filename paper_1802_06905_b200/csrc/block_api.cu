@@ -58,17 +58,24 @@ struct Bytes {
     const int64_t d = ((o.lo - lo) % pitch + pitch) % pitch;  // column slices of one array do not meet
     return d < width || d + o.width > pitch;
   }
+  bool operator==(const Bytes& o) const { return lo == o.lo && hi == o.hi && pitch == o.pitch && width == o.width; }
 };
 
 // Collects the byte ranges that a call reads and writes, and checks each operand on the way.
 class Operands {
  public:
   bool ok = true;
-  // An operand of rows x cols elements.  `rows_ok_zero_stride`: inputs may repeat rows and columns.
-  void in(const cconv_matrix& m, int64_t rows, int64_t cols, int es) { add(m, rows, cols, es, false); }
-  void out(const cconv_matrix& m, int64_t rows, int64_t cols, int es) { add(m, rows, cols, es, true); }
-  void in(const void* v, int64_t n, int es) { in(vec(v, n), 1, n, es); }
-  void out(const void* v, int64_t n, int es) { out(vec(v, n), 1, n, es); }
+  // An operand of rows x cols elements, or a vector; inputs may repeat rows and columns.  Its number, or -1 if it
+  // has no element.
+  int in(const cconv_matrix& m, int64_t rows, int64_t cols, int es) { return add(m, rows, cols, es, false); }
+  int out(const cconv_matrix& m, int64_t rows, int64_t cols, int es) { return add(m, rows, cols, es, true); }
+  int in(const void* v, int64_t n, int es) { return in(vec(v, n), 1, n, es); }
+  int out(const void* v, int64_t n, int es) { return out(vec(v, n), 1, n, es); }
+  // The result `out` may be written in the place of `in`, if they are one and the same matrix (numbers from above).
+  void may_be_one(int in, int out) {
+    in_ = in;
+    out_ = out;
+  }
   void workspace(void* p, uint64_t have, int64_t need) {
     if (need == 0) return;
     if (!p || (reinterpret_cast<uintptr_t>(p) & 255u) || have < uint64_t(need)) {
@@ -94,13 +101,12 @@ class Operands {
     if (block_launches() != before) note(stream, sms);
     return rc;
   }
-  // No output meets another output or an input; `same` names a pair that may be one matrix.
-  bool distinct(const void* same_in = nullptr, const void* same_out = nullptr) const {
+  // No output meets another output or an input, but for the pair that may be one.
+  bool distinct() const {
     for (int i = 0; i < n_; ++i)
       for (int j = 0; j < n_; ++j) {
         if (i == j || !written_[i] || (written_[j] && j < i)) continue;
-        if (same_in && same_in == same_out && range_[i].lo == same_out && range_[j].lo == same_in && !written_[j])
-          continue;
+        if (i == out_ && j == in_ && range_[i] == range_[j]) continue;
         if (range_[i].meets(range_[j])) return false;
       }
     return ok;
@@ -117,21 +123,22 @@ class Operands {
     note_call(stream, c, Overlap::kInputsEarly, sms);
   }
   static cconv_matrix vec(const void* v, int64_t n) { return cconv_matrix{const_cast<void*>(v), n, 1}; }
-  void push(Bytes b, bool written) {
+  int push(Bytes b, bool written) {
     range_[n_] = b;
-    written_[n_++] = written;
+    written_[n_] = written;
+    return n_++;
   }
-  void add(const cconv_matrix& m, int64_t rows, int64_t cols, int es, bool written) {
-    if (rows == 0 || cols == 0) return;  // nothing is touched
+  int add(const cconv_matrix& m, int64_t rows, int64_t cols, int es, bool written) {
+    if (rows == 0 || cols == 0) return -1;  // nothing is touched
     if (!m.data || (reinterpret_cast<uintptr_t>(m.data) & uintptr_t(es - 1)) || m.row_stride < 0 || m.col_stride < 0 ||
         m.row_stride > kMaxStride || m.col_stride > kMaxStride) {
       ok = false;
-      return;
+      return -1;
     }
     const double last = double(rows - 1) * double(m.row_stride) + double(cols - 1) * double(m.col_stride);
     if (last > 4.0e18 / es) {
       ok = false;
-      return;
+      return -1;
     }
     if (written) {
       // distinct elements: one stride steps over the whole extent of the other
@@ -145,11 +152,11 @@ class Operands {
     const int64_t wr = ((cols - 1) * m.col_stride + 1) * es, wc = ((rows - 1) * m.row_stride + 1) * es;
     if (rows > 1 && m.row_stride * es >= wr) b.pitch = m.row_stride * es, b.width = wr;
     else if (cols > 1 && m.col_stride * es >= wc) b.pitch = m.col_stride * es, b.width = wc;
-    push(b, written);
+    return push(b, written);
   }
   Bytes range_[24];
   bool written_[24] = {};
-  int n_ = 0;
+  int n_ = 0, in_ = -1, out_ = -1;
 };
 
 bool length_ok(int64_t n) { return n >= 0 && n < kMaxLength; }
@@ -359,15 +366,14 @@ int cconv_residual_norm_forward(const cconv_residual_norm_args* args, void* cuda
       return CCONV_EINVAL;
     if (a.T && a.D && ((!a.block.data && (a.gate.data || a.w_post)) || (!a.norm_out.data && a.w_pre))) return CCONV_EINVAL;
     Operands o;
-    o.in(a.resid, a.T, a.D, es);
+    const int resid = o.in(a.resid, a.T, a.D, es);
     if (a.block.data) o.in(a.block, a.T, a.D, es);
     if (a.gate.data) o.in(a.gate, gate_rows(a), a.D, es);
     if (a.w_post) o.in(a.w_post, a.D, es);
     if (a.w_pre) o.in(a.w_pre, a.D, es);
-    o.out(a.resid_out, a.T, a.D, es);
+    o.may_be_one(resid, o.out(a.resid_out, a.T, a.D, es));
     if (a.norm_out.data) o.out(a.norm_out, a.T, a.D, es);
-    const bool same = a.resid.row_stride == a.resid_out.row_stride;
-    if (!o.distinct(same ? a.resid.data : nullptr, a.resid_out.data)) return CCONV_EINVAL;
+    if (!o.distinct()) return CCONV_EINVAL;
     if (!o.writes()) return CCONV_OK;
     const int sms = block_sm_count();
     if (sms < 0) return sms;
@@ -410,21 +416,19 @@ int cconv_residual_norm_backward(const cconv_residual_norm_args* args, void* cud
     if (a.w_post) o.in(a.w_post, a.D, es);
     if (a.w_pre) o.in(a.w_pre, a.D, es);
     if (a.dnorm_out.data) o.in(a.resid_out, a.T, a.D, es);
-    if (a.dresid_out.data) o.in(a.dresid_out, a.T, a.D, es);
+    const int direct = a.dresid_out.data ? o.in(a.dresid_out, a.T, a.D, es) : -1;
     if (a.dnorm_out.data) o.in(a.dnorm_out, a.T, a.D, es);
-    o.out(a.dresid, a.T, a.D, es);
+    o.may_be_one(direct, o.out(a.dresid, a.T, a.D, es));
     if (a.dblock.data) o.out(a.dblock, a.T, a.D, es);
     if (a.dgate.data) o.out(a.dgate, gate_rows(a), a.D, es);
     if (a.dw_post) o.out(a.dw_post, a.D, es);
     if (a.dw_pre) o.out(a.dw_pre, a.D, es);
-    const bool same = a.dresid_out.row_stride == a.dresid.row_stride;
-    const void* same_in = same ? a.dresid_out.data : nullptr;
-    if (!o.distinct(same_in, a.dresid.data)) return CCONV_EINVAL;
+    if (!o.distinct()) return CCONV_EINVAL;
     if (!o.writes()) return CCONV_OK;
     const int sms = block_sm_count();
     if (sms < 0) return sms;
     o.workspace(a.workspace, a.workspace_bytes, norm_workspace(a, sms));
-    if (!o.distinct(same_in, a.dresid.data)) return CCONV_EINVAL;
+    if (!o.distinct()) return CCONV_EINVAL;
     cudaStream_t s = static_cast<cudaStream_t>(cuda_stream);
     if (a.T == 0) {
       return o.run(cuda_stream, sms, [&]() -> int {

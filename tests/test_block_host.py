@@ -204,3 +204,37 @@ def test_a_call_without_results_leaves_the_stream_alone(lib, name, struct, args)
     assert probe(1 << 20, 2 << 20) == 0
     assert call(lib, name, struct, stream=key, **args) == binding.OK
     assert probe(2 << 20, 3 << 20) == 1
+
+
+FORWARD_IN_PLACE = dict(T=8, D=256, scale=1.0, eps=1e-6, resid=at(1), resid_out=at(1), norm_out=at(2), block=at(3))
+BACKWARD_IN_PLACE = dict(T=8, D=256, scale=1.0, eps=1e-6, resid_out=at(1), dnorm_out=at(2), dresid_out=at(3), dresid=at(3),
+                         block=at(4), dblock=at(5))
+
+
+@pytest.mark.parametrize("name,args,bad", [
+    ("forward", FORWARD_IN_PLACE, dict(block=at(1, 0))),                        # row 0 for every token
+    ("forward", FORWARD_IN_PLACE, dict(block=at(1))),
+    ("forward", FORWARD_IN_PLACE, dict(gate=at(1))),
+    ("forward", FORWARD_IN_PLACE, dict(gate=at(1), rows_per_gate=2)),
+    ("forward", FORWARD_IN_PLACE, dict(w_post=1 << 20)),
+    ("forward", FORWARD_IN_PLACE, dict(w_pre=1 << 20)),
+    ("forward", FORWARD_IN_PLACE, dict(resid=at(1, 0))),
+    ("forward", FORWARD_IN_PLACE, dict(resid=at(1, 512))),
+    ("forward", FORWARD_IN_PLACE, dict(norm_out=at(1))),
+    ("backward", BACKWARD_IN_PLACE, dict(resid_out=at(3, 0))),
+    ("backward", BACKWARD_IN_PLACE, dict(dnorm_out=at(3, 512))),
+    ("backward", BACKWARD_IN_PLACE, dict(dnorm_out=at(3))),
+    ("backward", BACKWARD_IN_PLACE, dict(block=at(3, 0))),
+    ("backward", BACKWARD_IN_PLACE, dict(gate=at(3), dgate=at(6))),
+    ("backward", BACKWARD_IN_PLACE, dict(w_post=3 << 20, dw_post=6 << 20)),
+    ("backward", BACKWARD_IN_PLACE, dict(w_pre=3 << 20, dw_pre=6 << 20)),
+    ("backward", BACKWARD_IN_PLACE, dict(dresid_out=at(3, 0))),
+])
+def test_only_the_named_matrix_may_be_written_in_place(lib, name, args, bad):
+    entry = "cconv_residual_norm_" + name
+    assert call(lib, entry, "cconv_residual_norm_args", **{**args, **bad}) == binding.EINVAL
+    import torch
+    if not torch.cuda.is_available():  # in place as the header allows it: goes on to the device
+        assert call(lib, entry, "cconv_residual_norm_args", **args) in (binding.ECUDA, binding.EUNSUPPORTED)
+        one = {k: (v[0], 7, 1) if isinstance(v, tuple) and k != "norm_out" else v for k, v in args.items()}
+        assert call(lib, entry, "cconv_residual_norm_args", **{**one, "T": 1}) in (binding.ECUDA, binding.EUNSUPPORTED)
