@@ -2,6 +2,7 @@
 // layout, launches.  Nothing here allocates or synchronises (cconv_block_status synchronises).
 #include <cmath>
 #include <cstring>
+#include <numeric>
 #include <string>
 
 #include "block.h"
@@ -48,17 +49,23 @@ namespace {
 constexpr int64_t kMaxLength = (int64_t(1) << 31) - 1024;  // of one dimension: coordinates of tiles are 32 bits
 constexpr int64_t kMaxStride = int64_t(1) << 40;
 
-// The bytes of an operand: [lo, hi), and where they are rows at a pitch, `width` bytes of every `pitch`.
+// The bytes of an operand: [lo, hi), and where they are rows at a pitch, `width` bytes of every `pitch`; its
+// elements of `unit` bytes begin multiples of `step` bytes behind lo (0: it is one element).
 struct Bytes {
   const char *lo = nullptr, *hi = nullptr;
-  int64_t pitch = 0, width = 0;
+  int64_t pitch = 0, width = 0, unit = 1, step = 1;
+  // Whether b, which repeats every `period` bytes like this, lies beside these `mine` bytes of each period.
+  bool beside(const Bytes& b, int64_t period, int64_t mine, int64_t its) const {
+    const int64_t d = ((b.lo - lo) % period + period) % period;
+    return d >= mine && d + its <= period;
+  }
   bool meets(const Bytes& o) const {
     if (lo >= o.hi || o.lo >= hi) return false;
-    if (pitch == 0 || pitch != o.pitch) return true;
-    const int64_t d = ((o.lo - lo) % pitch + pitch) % pitch;  // column slices of one array do not meet
-    return d < width || d + o.width > pitch;
+    if (pitch && pitch == o.pitch && beside(o, pitch, width, o.width)) return false;  // column slices of one array
+    const int64_t each = std::gcd(step, o.step);
+    return each == 0 || !beside(o, each, unit, o.unit);  // columns of one array in turn
   }
-  bool operator==(const Bytes& o) const { return lo == o.lo && hi == o.hi && pitch == o.pitch && width == o.width; }
+  bool operator==(const Bytes& o) const { return lo == o.lo && hi == o.hi && pitch == o.pitch && width == o.width && step == o.step; }
 };
 
 // Collects the byte ranges that a call reads and writes, and checks each operand on the way.
@@ -82,7 +89,7 @@ class Operands {
       ok = false;
       return;
     }
-    push({static_cast<const char*>(p), static_cast<const char*>(p) + need, 0, 0}, true);
+    push({static_cast<const char*>(p), static_cast<const char*>(p) + need}, true);
   }
   // Whether any result has an element.  A call without one launches nothing and needs no device.
   bool writes() const {
@@ -148,7 +155,8 @@ class Operands {
       if (!rows_outer && !cols_outer) ok = false;
     }
     const char* lo = static_cast<const char*>(m.data);
-    Bytes b{lo, lo + ((rows - 1) * m.row_stride + (cols - 1) * m.col_stride + 1) * es, 0, 0};
+    Bytes b{lo, lo + ((rows - 1) * m.row_stride + (cols - 1) * m.col_stride + 1) * es, 0, 0, es,
+            std::gcd(rows > 1 ? m.row_stride * es : 0, cols > 1 ? m.col_stride * es : 0)};
     const int64_t wr = ((cols - 1) * m.col_stride + 1) * es, wc = ((rows - 1) * m.row_stride + 1) * es;
     if (rows > 1 && m.row_stride * es >= wr) b.pitch = m.row_stride * es, b.width = wr;
     else if (cols > 1 && m.col_stride * es >= wc) b.pitch = m.col_stride * es, b.width = wc;

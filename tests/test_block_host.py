@@ -238,3 +238,21 @@ def test_only_the_named_matrix_may_be_written_in_place(lib, name, args, bad):
         assert call(lib, entry, "cconv_residual_norm_args", **args) in (binding.ECUDA, binding.EUNSUPPORTED)
         one = {k: (v[0], 7, 1) if isinstance(v, tuple) and k != "norm_out" else v for k, v in args.items()}
         assert call(lib, entry, "cconv_residual_norm_args", **{**one, "T": 1}) in (binding.ECUDA, binding.EUNSUPPORTED)
+
+
+def test_columns_of_one_array_in_turn_are_distinct(lib):
+    """gate_pre in the even columns of an array and up_pre in the odd ones; likewise in turn by threes, with rows
+    of any pitch, and by rows.  Those that share an element are refused."""
+    f = lib.cconv_ffn_forward
+    f.restype, f.argtypes = ctypes.c_int, [ctypes.c_void_p, ctypes.c_void_p]
+    a = 1 << 26
+    import torch
+    for gate, up in (((a, 64, 2), (a + 2, 64, 2)), ((a + 2, 64, 2), (a, 64, 2)), ((a, 96, 3), (a + 4, 96, 3)),
+                     ((a, 64, 2), (a + 128 + 2, 128, 2)), ((a, 2, 8), (a + 2, 2, 8)), ((a, 1, 8), (a + 8, 1, 8))):
+        s = ffn(lib, gate_pre=gate, up_pre=up)
+        if not torch.cuda.is_available():
+            assert f(ctypes.addressof(s), None) in (binding.ECUDA, binding.EUNSUPPORTED), (gate, up)
+    for gate, up in (((a, 64, 2), (a + 4, 64, 2)), ((a, 64, 2), (a + 2, 65, 2)), ((a, 64, 2), (a + 2, 64, 1)),
+                     ((a, 96, 3), (a + 2, 64, 2)), ((a, 64, 2), (a, 64, 2)), ((a, 2, 8), (a + 4, 2, 8))):
+        s = ffn(lib, gate_pre=gate, up_pre=up)
+        assert f(ctypes.addressof(s), None) == binding.EINVAL, (gate, up)

@@ -355,3 +355,13 @@ def test_an_empty_call_between_two_convolutions_keeps_them_in_order():
     for _ in range(3):
         for x, y in zip(want, chain(False)):
             assert torch.equal(x, y)
+
+
+def test_pre_activations_in_the_columns_of_one_array_in_turn():
+    for T, D, F in ((3, 72, 136), (40, 72, 136), (300, 72, 136)):
+        f = Ffn(T, D, F)
+        both, out = poisoned((T, 2 * F), BF16), poisoned((T, D), BF16)
+        block.ffn_forward(f.x, f.wg, f.wu, f.wd, out, gate_pre=both[:, ::2], up_pre=both[:, 1::2])
+        f.check_forward(out, both[:, ::2], both[:, 1::2], "in turn")
+        f.g, f.u = both[:, ::2], both[:, 1::2]
+        f.check_backward(*f.backward(), "in turn")
