@@ -75,7 +75,8 @@ typedef struct {
 } cconv_ffn_args;
 
 /* Bytes of workspace that the call with these arguments needs (>= 0), or a negative code.  Only the
- * sizes, types, strides and alignment of the addresses matter; nothing is dereferenced. */
+ * sizes, types, strides and alignment of the addresses matter (NULL is aligned, but for gate_pre and
+ * up_pre of the forward call, which it makes absent); nothing is dereferenced. */
 int64_t cconv_ffn_forward_workspace(const cconv_ffn_args* args);
 int64_t cconv_ffn_backward_workspace(const cconv_ffn_args* args);
 int cconv_ffn_forward(const cconv_ffn_args* args, void* cuda_stream);

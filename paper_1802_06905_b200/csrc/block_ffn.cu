@@ -67,7 +67,7 @@ void forward(Steps& st, const cconv_ffn_args& a) {
     Launch l = launch_of(a, p, kGated);
     l.save = gate_pre.p != nullptr;
     choose_cut(&l, sms, false);
-    const Mat to[3] = {h, gate_pre, up_pre};
+    const Mat to[3] = {h, l.save ? gate_pre : Mat(), l.save ? up_pre : Mat()};
     st.launch(l, to);
   }
   if (few_down) {
@@ -92,7 +92,7 @@ void backward(Steps& st, const cconv_ffn_args& a) {
   const Mat dout(a.dout), x(a.x);
   {
     Product p = product(T, F, D);
-    p.a[0] = st.operand(dout, T, D);
+    p.a[0] = st.operand(dout, T, D, false, &a.dout);
     p.b[0] = st.operand(Mat(a.w_down).t(), F, D);
     p.in[0] = st.readable(a.gate_pre, T, F);
     p.in[1] = st.readable(a.up_pre, T, F);
@@ -111,7 +111,7 @@ void backward(Steps& st, const cconv_ffn_args& a) {
   ps[1].a[0] = in_place(dg.t(), F, T);
   ps[2].a[0] = in_place(du.t(), F, T);
   ps[1].b[0] = ps[2].b[0] = st.operand(x.t(), D, T);
-  ps[3].a[0] = st.operand(dout.t(), D, T);
+  ps[3].a[0] = st.operand(dout.t(), D, T, false, &a.dout);
   ps[3].b[0] = in_place(h.t(), F, T);
 
   // each by itself, with its own cut

@@ -55,24 +55,20 @@ class Steps {
   }
 
   // An operand of a product (rows x k) as it lies, or a copy of it: in its own order, where the product takes that
-  // and the copies need not transpose, else with k contiguous.  A matrix that is copied in one order serves
-  // for both (dout and its transpose).
-  Operand copied(const Mat& m, int64_t rows, int64_t k, bool want_kmajor) {
+  // and the copies need not transpose, else with k contiguous.  `of` names the argument that `m` is, or is the
+  // transpose of (null: used once): one copy of it in one order serves both.  (By the argument and not by the
+  // address, so that the workspace does not depend on which arguments share one.)
+  Operand copied(const Mat& m, int64_t rows, int64_t k, bool want_kmajor, const void* of) {
     const bool kmajor = want_kmajor || es_ != 2 || m.rs != 1 || m.cs == 1;
     const Mat from = kmajor ? m : m.t();
     const int64_t outer = kmajor ? rows : k, inner = kmajor ? k : rows;
     Mat to;
-    for (const Copy& c : copies_)
-      if (m.p && c.from.p == from.p && c.from.rs == from.rs && c.from.cs == from.cs && c.rows == outer && c.cols == inner) to = c.to;
+    for (const Made& c : made_)
+      if (of && c.of == of && c.rows == outer && c.cols == inner && c.rs == from.rs && c.cs == from.cs) to = c.to;
     if (!to.rs) {
       to = scratch(outer, inner, es_);
       copy(from, to, outer, inner, es_);
-      Copy c;
-      c.from = from;
-      c.to = to;
-      c.rows = outer;
-      c.cols = inner;
-      copies_.push_back(c);
+      made_.push_back({of, outer, inner, from.rs, from.cs, to});
     }
     Operand o;
     o.p = to.p;
@@ -82,15 +78,15 @@ class Steps {
     o.k = k;
     return o;
   }
-  Operand operand(const Mat& m, int64_t rows, int64_t k, bool want_kmajor = false) {
+  Operand operand(const Mat& m, int64_t rows, int64_t k, bool want_kmajor = false, const void* of = nullptr) {
     Operand o;
-    return operand_in_place(m, rows, k, es_, !want_kmajor && es_ == 2, &o) ? o : copied(m, rows, k, want_kmajor);
+    return operand_in_place(m, rows, k, es_, !want_kmajor && es_ == 2, &o) ? o : copied(m, rows, k, want_kmajor, of);
   }
   // Two operands of one product, in the same order.
   void operands(const Mat& a, const Mat& b, int64_t rows, int64_t k, Operand* oa, Operand* ob) {
     *oa = operand(a, rows, k);
     *ob = operand(b, rows, k, oa->kmajor);
-    if (oa->kmajor != ob->kmajor) *oa = copied(a, rows, k, true);
+    if (oa->kmajor != ob->kmajor) *oa = copied(a, rows, k, true, nullptr);
   }
   // A matrix that is read row by row.
   Mat readable(const cconv_matrix& m, int64_t rows, int64_t cols) {
@@ -101,14 +97,15 @@ class Steps {
     return to;
   }
 
-  // Adds a launch.  `to[i]` is where out[i] of the i-th product (or of the only one) belongs; what the
-  // copy engine cannot write there in place goes to the workspace first.
+  // Adds a launch.  `to[i]` is where out[i] of the i-th product (or of the only one) belongs (Mat(): nowhere; an
+  // address may be null while the workspace is measured); what the copy engine cannot write there in place goes
+  // to the workspace first.
   void launch(Launch l, const Mat* to) {
     struct Move { Mat from, to; int64_t M, N; };
     std::vector<Move> moves;
     const int es = type_bytes(dtype_);
     for (int i = 0; i < (l.count > 1 ? l.count : 3); ++i) {
-      if (!to[i].p) continue;
+      if (!to[i].p && !to[i].rs && !to[i].cs) continue;
       Product& p = l.of[l.count > 1 ? i : 0];
       Mat& out = p.out[l.count > 1 ? 0 : i];
       out = to[i];
@@ -139,7 +136,13 @@ class Steps {
   Carver ws_;
   const int sms_, es_, dtype_;
   std::vector<Step> steps_;
-  std::vector<Copy> pending_, copies_;  // to be launched; made for operands
+  std::vector<Copy> pending_;  // to be launched
+  struct Made {                // a copy of an operand
+    const void* of;
+    int64_t rows, cols, rs, cs;
+    Mat to;
+  };
+  std::vector<Made> made_;
 };
 
 }  // namespace cconv

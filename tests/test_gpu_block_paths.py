@@ -1,9 +1,12 @@
 """The feed-forward sub-block where its pieces meet: every cut of a product, offsets past 32 bits, the order of
 a stream that convolutions share, other devices' streams, and the command that runs all of it together."""
+import ctypes
+
 import pytest
 import torch
 
 from paper_1802_06905_b200 import binding, block
+from test_block_host import struct_of
 from test_gpu_block import BF16, E4M3, FP16, FP32, Ffn, Norm, act64, close, fp8_check, fp8_operands, gen, normal, poisoned
 
 pytestmark = pytest.mark.gpu
@@ -365,3 +368,36 @@ def test_pre_activations_in_the_columns_of_one_array_in_turn():
         f.check_forward(out, both[:, ::2], both[:, 1::2], "in turn")
         f.g, f.u = both[:, ::2], both[:, 1::2]
         f.check_backward(*f.backward(), "in turn")
+
+
+def workspace(name, struct, addresses, matrices, **sizes):
+    s = struct_of(struct)()
+    for k, v in sizes.items():
+        setattr(s, k, v)
+    for i, (k, (rs, cs)) in enumerate(matrices.items()):
+        m = getattr(s, k)
+        m.data, m.row_stride, m.col_stride = addresses(i), rs, cs
+    f = getattr(binding.load_library(), name)
+    f.restype, f.argtypes = ctypes.c_int64, [ctypes.c_void_p]
+    return f(ctypes.addressof(s))
+
+
+@pytest.mark.parametrize("T", [2, 40, 333, 3000])
+@pytest.mark.parametrize("step", [1, 2])
+def test_the_workspace_does_not_depend_on_which_addresses_are_equal(T, step):
+    """A query with one placeholder for every matrix, or with none, gives what the call needs: odd sizes, so that
+    every operand is copied, and results that go through the workspace too."""
+    far, same, none = (lambda i: (i + 1) << 30), (lambda i: 1 << 30), (lambda i: None)
+    # T = D and D = F too: then matrices of different arguments have equal shapes and strides
+    for D, F in ((T if T % 2 else T + 1, 263), (263, 263)):
+        fd, td, tf, df = (D * step, step), (D * step, step), (F * step, step), (F * step, step)
+        for name, m in (
+                ("cconv_ffn_forward_workspace", dict(x=td, w_gate=fd, w_up=fd, w_down=df, out=td)),
+                ("cconv_ffn_backward_workspace", dict(x=td, dout=td, w_gate=fd, w_up=fd, w_down=df, gate_pre=tf, up_pre=tf, dx=td,
+                                                      dw_gate=fd, dw_up=fd, dw_down=df))):
+            sizes = [workspace(name, "cconv_ffn_args", a, m, T=T, D=D, F=F, dtype=block.TYPE_BF16) for a in (far, same, none)]
+            assert sizes[0] > 0 and sizes[0] == sizes[1] == sizes[2], (name, sizes)
+    m = dict(a=(D * step, step), b=(D * step, step), a_scale=(99, 1), b_scale=(99, 1), c=(F * step, step))
+    sizes = [workspace("cconv_fp8_product_workspace", "cconv_fp8_product_args", a, m, M=T, N=F, K=D, dtype=block.TYPE_BF16)
+             for a in (far, same, none)]
+    assert sizes[0] > 0 and sizes[0] == sizes[1] == sizes[2], sizes
