@@ -401,3 +401,74 @@ def test_the_workspace_does_not_depend_on_which_addresses_are_equal(T, step):
     sizes = [workspace("cconv_fp8_product_workspace", "cconv_fp8_product_args", a, m, M=T, N=F, K=D, dtype=block.TYPE_BF16)
              for a in (far, same, none)]
     assert sizes[0] > 0 and sizes[0] == sizes[1] == sizes[2], sizes
+
+
+def tail_inputs(act, dtype, T, F):
+    """T x F pre-activations over both tails, to where the exponential's argument reaches 85, and that argument."""
+    far = {"silu": 85.0, "gelu": 13.0, "gelu_tanh": 9.8, "relu": 9.0}[act]
+    far = min(far, 9.0) if dtype is FP16 else far
+    g = ((torch.rand((T, F), generator=gen(T + F), device="cuda") * 2 - 1) * far).to(dtype)
+    v = g.double()
+    z = {"silu": v, "gelu": v * v / 2, "gelu_tanh": 2 * (2 / torch.pi) ** 0.5 * (v + 0.044715 * v ** 3), "relu": 0 * v}[act]
+    return g, z.abs()
+
+
+def act64_in_the_tails(name, g):
+    """a(g), a'(g) and the first of the two terms that a' adds, in 64 bits without a difference from 1 (as 1 + tanh
+    and 1 + erf are, which leave nothing of values below 1e-16)."""
+    if name == "silu":
+        s, rest = torch.sigmoid(g), torch.sigmoid(-g)
+        return g * s, s + g * s * rest, s
+    if name == "gelu":
+        cdf = torch.special.erfc(-g * 0.5 ** 0.5) / 2
+        return g * cdf, cdf + g * torch.exp(-g * g / 2) / (2 * torch.pi) ** 0.5, cdf
+    if name == "gelu_tanh":
+        k = 2 * (2 / torch.pi) ** 0.5
+        s, rest = (torch.sigmoid(sign * k * (g + 0.044715 * g ** 3)) for sign in (1, -1))
+        return g * s, s + g * s * rest * k * (1 + 3 * 0.044715 * g * g), s
+    on = (g > 0).double()
+    return g * on, on, on
+
+
+# The hidden values reach the result one by one: w_gate and w_down are identities, u is 512 everywhere.  The fast
+# exponential is off by 2 + 1.2 |z| units, its argument's roundings by up to 2.5 |z|, the rest by fewer than 14.
+@pytest.mark.parametrize("act", ["silu", "gelu", "gelu_tanh", "relu"])
+@pytest.mark.parametrize("dtype", [BF16, FP16])
+@pytest.mark.parametrize("T", [2, 16, 100, 300])
+def test_hidden_values_are_right_relative_to_themselves(act, dtype, T):
+    F, D, u = 64, 128, {BF16: 2.0 ** -8, FP16: 2.0 ** -11}[dtype]
+    g, z = tail_inputs(act, dtype, T, F)
+    x = torch.zeros((T, D), device="cuda", dtype=dtype)
+    x[:, :F], x[:, F] = g, 512.0
+    wg, wu, wd = (torch.zeros(s, device="cuda", dtype=dtype) for s in ((F, D), (F, D), (D, F)))
+    wg[:, :F], wd[:F], wu[:, F] = torch.eye(F, device="cuda"), torch.eye(F, device="cuda"), 1.0
+    out = poisoned((T, D), dtype)
+    block.ffn_forward(x, wg, wu, wd, out, act=block.ACTS[act])
+    h = 512 * act64_in_the_tails(act, g.double())[0]
+    tiny = 2.0 ** -24 if dtype is FP16 else 1e-36
+    close(out[:, :F], h, 1.01 * (u + 2.0 ** -23 * (16 + 4 * z)) * h.abs() + tiny, f"{act} of {T}")
+    assert (out[:, F:] == 0).all()
+
+
+@pytest.mark.parametrize("act", ["silu", "gelu", "gelu_tanh", "relu"])
+@pytest.mark.parametrize("dtype", [BF16, FP16])
+@pytest.mark.parametrize("T", [16, 128, 320])
+def test_hidden_gradients_are_right_relative_to_themselves(act, dtype, T):
+    """As many tokens as channels, dout and x identities: dw_down = h, dw_up = (dL/du)^T, dw_gate = (dL/dg)^T, where
+    dL/dh = w_down = 512.  dL/dg adds two terms, relative to whose sizes it is right."""
+    F, D, u = 64, T, {BF16: 2.0 ** -8, FP16: 2.0 ** -11}[dtype]
+    g, z = tail_inputs(act, dtype, T, F)
+    eye, up = torch.eye(T, device="cuda").to(dtype), torch.full((T, F), 2.0, device="cuda").to(dtype)
+    wg, wu = torch.zeros((F, D), device="cuda", dtype=dtype), torch.zeros((F, D), device="cuda", dtype=dtype)
+    wd = torch.full((D, F), 512.0, device="cuda").to(dtype)
+    dx, dwg, dwu, dwd = poisoned((T, D), dtype), poisoned((F, D), dtype), poisoned((F, D), dtype), poisoned((D, F), dtype)
+    block.ffn_backward(eye, eye, wg, wu, wd, g, up, dx, dwg, dwu, dwd, act=block.ACTS[act])
+    v = g.double()
+    a, da, share = act64_in_the_tails(act, v)
+    size = share.abs() + (da - share).abs()
+    tiny = 2.0 ** -24 if dtype is FP16 else 1e-35
+    off = 2.0 ** -23 * (16 + 4 * z)
+    close(dwd, 2 * a, 1.01 * (u + off) * 2 * a.abs() + tiny, act + " h")
+    close(dwu.t(), 512 * a, 1.01 * (u + off) * 512 * a.abs() + tiny, act + " dL/du")
+    close(dwg.t(), 1024 * da, 1.01 * 1024 * (u * da.abs() + off * size) + tiny, act + " dL/dg")
+    assert (dx == 0).all()
