@@ -2,9 +2,9 @@
 //
 //   forward    n = y rho_y w_post,  r' = scale r + gate n,  x = r' rho_r w_pre,
 //              rho_v = 1 / sqrt(mean(v^2) + eps)
-//   backward   e = dx w_pre,  S = dr' + rho_r e - r' rho_r^3 mean(e r')       (dL/dr', all of it)
+//   backward   e = dx w_pre,  S = dr' + rho_r (e - r^ mean(e r^)),  r^ = r' rho_r      (dL/dr', all of it)
 //              dr = scale S,  dgate = sum_t S n,  dn = gate S
-//              f = dn w_post,  dy = rho_y f - y rho_y^3 mean(f y)
+//              f = dn w_post,  dy = rho_y (f - y^ mean(f y^)),  y^ = y rho_y
 //              dw_post = sum_t dn y rho_y,  dw_pre = sum_t dx r' rho_r
 //
 // Both directions read every [T][D] array once and write every output once; a row stays in registers
@@ -563,7 +563,7 @@ __global__ void __launch_bounds__(kThreads ? kThreads : 512, 512 / (kThreads ? k
       }
       const float2 q = row_sum2(srr, ser);
       const float rho = rsqrtf(q.x * inv_d + p.eps);
-      const float k = rho * rho * rho * (q.y * inv_d);
+      const float k = rho * (rho * (q.y * inv_d));  // (rho^3 would leave the range that rho itself is well within)
       // (read again: the reduction would hold them in registers that the sums need)
       load_across<kThreads, kRing>(r, row_r, D, 0.0f);
       load_across<kThreads, kRing>(x, row_x, D, 0.0f);
@@ -571,8 +571,9 @@ __global__ void __launch_bounds__(kThreads ? kThreads : 512, 512 / (kThreads ? k
       load_across<kThreads, kRing>(s, row_d, D, 0.0f);
 #pragma unroll
       for (int v = 0; v < NV; ++v) {
-        s[v] += rho * (x[v] * w[v]) - k * r[v];
-        s_pre[v] += x[v] * (r[v] * rho);
+        const float rhat = r[v] * rho;
+        s[v] += rho * (x[v] * w[v]) - k * rhat;
+        s_pre[v] += x[v] * rhat;
       }
     } else {
       load_across<kThreads, kRing>(s, row_d, D, 0.0f);
@@ -593,13 +594,14 @@ __global__ void __launch_bounds__(kThreads ? kThreads : 512, 512 / (kThreads ? k
     if (w_post) {
       const float2 q = row_sum2(syy, sfy);
       rho = rsqrtf(q.x * inv_d + p.eps);
-      k = rho * rho * rho * (q.y * inv_d);
+      k = rho * (rho * (q.y * inv_d));
     }
 #pragma unroll
     for (int v = 0; v < NV; ++v) {
       const int c = A::column(v);
-      s_group[v] += s[v] * (y[v] * rho);
-      if (A::inside(v, D)) to_y[c] = from_f32<T>(rho * (s[v] * gw[v]) - k * y[v]);
+      const float yhat = y[v] * rho, f = s[v] * gw[v];
+      s_group[v] += s[v] * yhat;
+      if (A::inside(v, D)) to_y[c] = from_f32<T>(rho * f - k * yhat);
     }
   }
   if (t < row1 || dead) {  // let the copies that are on their way land
@@ -805,7 +807,7 @@ __global__ void __launch_bounds__(512) cconv_residual_norm_backward_ring_kernel(
       }
       const float2 q = block_sum2(sum_of(srr), sum_of(ser), smem, buf);
       const float rho1 = rsqrtf(q.x * inv_d + p.eps);
-      const float k1 = -rho1 * rho1 * rho1 * (q.y * inv_d);
+      const float k1 = -rho1 * (rho1 * (q.y * inv_d));
       const uint64_t rho = pair_of(rho1, rho1), k = pair_of(k1, k1);
 #pragma unroll
       for (int v = 0; v < NV; ++v) {
@@ -814,8 +816,9 @@ __global__ void __launch_bounds__(512) cconv_residual_norm_backward_ring_kernel(
         get(has_dres, row_d, v, s[v], 0);
 #pragma unroll
         for (int i = 0; i < P; ++i) {
-          s[v][i] = fma2(x[v][i], mul2(w[i], rho), fma2(r[v][i], k, s[v][i]));
-          s_pre[v][i] = fma2(x[v][i], mul2(r[v][i], rho), s_pre[v][i]);
+          const uint64_t rhat = mul2(r[v][i], rho);
+          s[v][i] = fma2(x[v][i], mul2(w[i], rho), fma2(rhat, k, s[v][i]));
+          s_pre[v][i] = fma2(x[v][i], rhat, s_pre[v][i]);
         }
       }
     } else {
@@ -840,7 +843,7 @@ __global__ void __launch_bounds__(512) cconv_residual_norm_backward_ring_kernel(
     if (has_post) {
       const float2 q = block_sum2(sum_of(syy), sum_of(sfy), smem, buf);
       const float rho1 = rsqrtf(q.x * inv_d + p.eps);
-      const float k1 = -rho1 * rho1 * rho1 * (q.y * inv_d);
+      const float k1 = -rho1 * (rho1 * (q.y * inv_d));
       rho = pair_of(rho1, rho1);
       k = pair_of(k1, k1);
     }
@@ -849,8 +852,9 @@ __global__ void __launch_bounds__(512) cconv_residual_norm_backward_ring_kernel(
       uint64_t o[P];
 #pragma unroll
       for (int i = 0; i < P; ++i) {
-        s_group[v][i] = fma2(s[v][i], mul2(y[v][i], rho), s_group[v][i]);
-        o[i] = fma2(y[v][i], k, mul2(rho, mul2(s[v][i], gw[v][i])));
+        const uint64_t yhat = mul2(y[v][i], rho), f = mul2(s[v][i], gw[v][i]);
+        s_group[v][i] = fma2(s[v][i], yhat, s_group[v][i]);
+        o[i] = fma2(yhat, k, mul2(rho, f));
       }
       if (inside(v)) put_pairs<T>(dblock + t * p.dblock_rs + (v * nt + tid) * E, o);
     }
@@ -1037,11 +1041,11 @@ __global__ void __launch_bounds__(512) cconv_residual_norm_backward_long_kernel(
       }
       const float2 q = block_sum2(srr, ser, smem, buf);
       rho = rsqrtf(q.x * inv_d + p.eps);
-      k = rho * rho * rho * (q.y * inv_d);
+      k = rho * (rho * (q.y * inv_d));
     }
     auto grad = [&](int c) {
       float s = fd ? to_f32(fd[c]) : 0.0f;
-      if (fx) s += rho * (w_pre ? to_f32(fx[c]) * to_f32(w_pre[c]) : to_f32(fx[c])) - k * to_f32(fr[c]);
+      if (fx) s += rho * (w_pre ? to_f32(fx[c]) * to_f32(w_pre[c]) : to_f32(fx[c])) - k * (to_f32(fr[c]) * rho);
       return s;
     };
     float rho_y = 1.0f, ky = 0.0f;
@@ -1054,7 +1058,7 @@ __global__ void __launch_bounds__(512) cconv_residual_norm_backward_long_kernel(
       }
       const float2 q = block_sum2(syy, sfy, smem, buf);
       rho_y = rsqrtf(q.x * inv_d + p.eps);
-      ky = rho_y * rho_y * rho_y * (q.y * inv_d);
+      ky = rho_y * (rho_y * (q.y * inv_d));
     }
     // a thread owns the columns c = threadIdx.x (mod blockDim.x) in every sweep, of all arrays
     for (int c = threadIdx.x; c < p.D; c += blockDim.x) {
@@ -1069,7 +1073,7 @@ __global__ void __launch_bounds__(512) cconv_residual_norm_backward_long_kernel(
           if (whole && ends) dgate[group * p.dgate_rs + c] = from_f32<T>(sum);
         }
         part[p.D + c] += dn * yhat;
-        dblock[t * p.dblock_rs + c] = from_f32<T>(w_post ? rho_y * (dn * to_f32(w_post[c])) - ky * to_f32(fy[c]) : dn);
+        dblock[t * p.dblock_rs + c] = from_f32<T>(w_post ? rho_y * (dn * to_f32(w_post[c])) - ky * yhat : dn);
       }
       dresid[t * p.dresid_rs + c] = from_f32<T>(p.scale * s);
     }

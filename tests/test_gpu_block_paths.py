@@ -472,3 +472,26 @@ def test_hidden_gradients_are_right_relative_to_themselves(act, dtype, T):
     close(dwu.t(), 512 * a, 1.01 * (u + off) * 512 * a.abs() + tiny, act + " dL/du")
     close(dwg.t(), 1024 * da, 1.01 * 1024 * (u * da.abs() + off * size) + tiny, act + " dL/dg")
     assert (dx == 0).all()
+
+
+# every backward kernel: wide rows, rows that begin anywhere (few, many), rows that clusters share, longer ones
+EVERY_NORM_KERNEL = [(5, 256), (700, 1024), (3, 251), (2400, 1001), (6, 9999), (1, 12001)]
+
+
+@pytest.mark.parametrize("T,D", EVERY_NORM_KERNEL)
+def test_norm_gradients_of_rows_of_any_size(T, D):
+    """Values of 1e15 (rho^3 is below the least fp32 number), of 1e-14 and 0 under an eps of 1e-30 (it is above
+    the largest): the bound is relative, as for rows near 1."""
+    for dtype in (FP32, BF16):
+        n = Norm(T, D, dtype, "all")
+        n.r, n.y = n.r * 1e15, n.y * 1e15
+        n.check_backward(n.run_backward(use_dr=False), use_dr=False, what="large")
+        n = Norm(T, D, dtype, blk=False, eps=1e-30)
+        n.r = n.r * 1e-14
+        n.r[T - 1] = 0
+        n.check_backward(n.run_backward(use_dr=False), use_dr=False, what="small")
+        n = Norm(T, D, dtype, "all", eps=1e-30)
+        n.y = n.y * 1e-14
+        n.y[T - 1] = 0
+        n.check_backward(n.run_backward(), what="small block")
+    assert block.status() == (0, 0)
