@@ -601,7 +601,7 @@ __global__ void __launch_bounds__(kThreads ? kThreads : 512, 512 / (kThreads ? k
       const int c = A::column(v);
       const float yhat = y[v] * rho, f = s[v] * gw[v];
       s_group[v] += s[v] * yhat;
-      if (A::inside(v, D)) to_y[c] = from_f32<T>(rho * f - k * yhat);
+      if (A::inside(v, D)) to_y[c] = from_f32<T>(w_post ? rho * f - k * yhat : f);
     }
   }
   if (t < row1 || dead) {  // let the copies that are on their way land
@@ -854,7 +854,7 @@ __global__ void __launch_bounds__(512) cconv_residual_norm_backward_ring_kernel(
       for (int i = 0; i < P; ++i) {
         const uint64_t yhat = mul2(y[v][i], rho), f = mul2(s[v][i], gw[v][i]);
         s_group[v][i] = fma2(s[v][i], yhat, s_group[v][i]);
-        o[i] = fma2(yhat, k, mul2(rho, f));
+        o[i] = has_post ? fma2(yhat, k, mul2(rho, f)) : f;
       }
       if (inside(v)) put_pairs<T>(dblock + t * p.dblock_rs + (v * nt + tid) * E, o);
     }

@@ -495,3 +495,12 @@ def test_norm_gradients_of_rows_of_any_size(T, D):
         n.y[T - 1] = 0
         n.check_backward(n.run_backward(), what="small block")
     assert block.status() == (0, 0)
+
+
+@pytest.mark.parametrize("T,D", EVERY_NORM_KERNEL)
+def test_without_a_norm_the_block_s_gradient_does_not_depend_on_the_block(T, D):
+    n = Norm(T, D, BF16, "all", post=False)
+    want = n.run_backward(use_dx=False)
+    n.y[0, 1], n.y[0, 2], n.y[T - 1, 3] = float("inf"), float("nan"), float("-inf")
+    got = n.run_backward(use_dx=False)
+    assert torch.equal(got[0], want[0]) and torch.equal(got[1], want[1])
