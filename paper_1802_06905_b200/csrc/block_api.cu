@@ -417,7 +417,9 @@ int cconv_residual_norm_backward(const cconv_residual_norm_args* args, void* cud
       if (!a.dnorm_out.data && !a.dresid_out.data) return CCONV_EINVAL;
     }
     if (a.D && (!a.gate.data != !a.dgate.data || !a.w_post != !a.dw_post)) return CCONV_EINVAL;
-    if (a.D && (a.w_pre && (a.dnorm_out.data || a.T == 0)) != (a.dw_pre != nullptr)) return CCONV_EINVAL;
+    // (without tokens dnorm_out may be given with no address, or absent: dw_pre is zeroed if it is there)
+    if (a.D && a.dw_pre && !a.w_pre) return CCONV_EINVAL;
+    if (a.T && a.D && (a.w_pre && a.dnorm_out.data) != (a.dw_pre != nullptr)) return CCONV_EINVAL;
     Operands o;
     if (a.block.data) o.in(a.block, a.T, a.D, es);
     if (a.gate.data) o.in(a.gate, gate_rows(a), a.D, es);

@@ -256,3 +256,13 @@ def test_columns_of_one_array_in_turn_are_distinct(lib):
                      ((a, 96, 3), (a + 2, 64, 2)), ((a, 64, 2), (a, 64, 2)), ((a, 2, 8), (a + 4, 2, 8))):
         s = ffn(lib, gate_pre=gate, up_pre=up)
         assert f(ctypes.addressof(s), None) == binding.EINVAL, (gate, up)
+
+
+def test_without_tokens_the_second_norm_s_gradient_may_be_absent(lib):
+    """dw_pre belongs to dnorm_out, which may be absent; of no tokens neither has an address."""
+    none = dict(T=0, D=256, scale=1.0, eps=1e-6, dresid=at(1))
+    assert call(lib, "cconv_residual_norm_backward", "cconv_residual_norm_args", **none, w_pre=2 << 20) == binding.OK
+    assert call(lib, "cconv_residual_norm_backward", "cconv_residual_norm_args", **none, dw_pre=2 << 20) == binding.EINVAL
+    for more in (dict(w_pre=2 << 20, dresid_out=at(3), dw_pre=4 << 20), dict(w_pre=2 << 20, dnorm_out=at(3), resid_out=at(5)),
+                 dict(dnorm_out=at(3), resid_out=at(5), dw_pre=4 << 20)):
+        assert call(lib, "cconv_residual_norm_backward", "cconv_residual_norm_args", **{**none, "T": 4}, **more) == binding.EINVAL
