@@ -2,10 +2,11 @@
 //
 //   forward    n = y rho_y w_post,  r' = scale r + gate n,  x = r' rho_r w_pre,
 //              rho_v = 1 / sqrt(mean(v^2) + eps)
-//   backward   e = dx w_pre,  S = dr' + rho_r (e - r^ mean(e r^)),  r^ = r' rho_r      (dL/dr', all of it)
+//   backward   e = dx w_pre,  S = dr' + rho_r e - r' rho_r^3 mean(e r')       (dL/dr', all of it)
 //              dr = scale S,  dgate = sum_t S n,  dn = gate S
-//              f = dn w_post,  dy = rho_y (f - y^ mean(f y^)),  y^ = y rho_y
+//              f = dn w_post,  dy = rho_y f - y rho_y^3 mean(f y)
 //              dw_post = sum_t dn y rho_y,  dw_pre = sum_t dx r' rho_r
+//   (rho^3 mean is formed from the mean on, a rho at a time: rho^3 alone leaves fp32's range for rows of 1e13 or an eps of 1e-26)
 //
 // Both directions read every [T][D] array once and write every output once; a row stays in registers
 // between its two reductions (over y, then over r'; backward: over r' and e, then over y and f), so
@@ -77,7 +78,6 @@ __device__ __forceinline__ float2 block_sum2(float a, float b, float2 (*smem)[32
 }
 
 // Block b of the kernels that take neighbouring rows has the rows [T b / nb, T (b+1) / nb).
-template <typename T>
 __device__ __forceinline__ int64_t first_row(const NormParams& p, int64_t b) {
   return p.T * b / p.nb;
 }
@@ -342,7 +342,7 @@ __global__ void __launch_bounds__(kThreads) cconv_residual_norm_narrow_kernel(co
   using A = Across<NV, kThreads>;
   const int tid = threadIdx.x;
   const float inv_d = 1.0f / float(p.D);
-  const int64_t row0 = first_row<T>(p, blockIdx.x), row1 = first_row<T>(p, blockIdx.x + 1);
+  const int64_t row0 = first_row(p, blockIdx.x), row1 = first_row(p, blockIdx.x + 1);
   const int64_t per = p.rows_per_gate ? p.rows_per_gate : p.T;
   const RowRing<T, 2> rows = {{static_cast<const T*>(p.resid), block}, {p.resid_rs, p.block_rs}, p.T, row0, row1,
                               uint32_t(p.D * sizeof(T)), p.ring_slot, smem_u32(ring), smem_u32(full), uint32_t(p.ring_rows)};
@@ -448,7 +448,7 @@ __global__ void __launch_bounds__(kThreads ? kThreads : 512, 512 / (kThreads ? k
   T* dgate = static_cast<T*>(p.dgate) + c0;
   const int tid = threadIdx.x;
   const float inv_d = 1.0f / float(p.D);
-  const int64_t row0 = first_row<T>(p, b), row1 = first_row<T>(p, b + 1);
+  const int64_t row0 = first_row(p, b), row1 = first_row(p, b + 1);
   const int64_t per = p.rows_per_gate ? p.rows_per_gate : p.T;
   float* part = p.part + int64_t(b) * 4 * p.D + c0;
   int buf = 0, shares_of = 0;
@@ -563,7 +563,7 @@ __global__ void __launch_bounds__(kThreads ? kThreads : 512, 512 / (kThreads ? k
       }
       const float2 q = row_sum2(srr, ser);
       const float rho = rsqrtf(q.x * inv_d + p.eps);
-      const float k = rho * (rho * (q.y * inv_d));  // (rho^3 would leave the range that rho itself is well within)
+      const float k = rho * (rho * (rho * (q.y * inv_d)));
       // (read again: the reduction would hold them in registers that the sums need)
       load_across<kThreads, kRing>(r, row_r, D, 0.0f);
       load_across<kThreads, kRing>(x, row_x, D, 0.0f);
@@ -571,9 +571,8 @@ __global__ void __launch_bounds__(kThreads ? kThreads : 512, 512 / (kThreads ? k
       load_across<kThreads, kRing>(s, row_d, D, 0.0f);
 #pragma unroll
       for (int v = 0; v < NV; ++v) {
-        const float rhat = r[v] * rho;
-        s[v] += rho * (x[v] * w[v]) - k * rhat;
-        s_pre[v] += x[v] * rhat;
+        s[v] += rho * (x[v] * w[v]) - k * r[v];
+        s_pre[v] += x[v] * (r[v] * rho);
       }
     } else {
       load_across<kThreads, kRing>(s, row_d, D, 0.0f);
@@ -594,14 +593,14 @@ __global__ void __launch_bounds__(kThreads ? kThreads : 512, 512 / (kThreads ? k
     if (w_post) {
       const float2 q = row_sum2(syy, sfy);
       rho = rsqrtf(q.x * inv_d + p.eps);
-      k = rho * (rho * (q.y * inv_d));
+      k = rho * (rho * (rho * (q.y * inv_d)));
     }
 #pragma unroll
     for (int v = 0; v < NV; ++v) {
       const int c = A::column(v);
-      const float yhat = y[v] * rho, f = s[v] * gw[v];
-      s_group[v] += s[v] * yhat;
-      if (A::inside(v, D)) to_y[c] = from_f32<T>(w_post ? rho * f - k * yhat : f);
+      const float f = s[v] * gw[v];
+      s_group[v] += s[v] * (y[v] * rho);
+      if (A::inside(v, D)) to_y[c] = from_f32<T>(w_post ? rho * f - k * y[v] : f);  // (y may be infinite)
     }
   }
   if (t < row1 || dead) {  // let the copies that are on their way land
@@ -661,8 +660,10 @@ __device__ __forceinline__ void put_pairs(void* to, const uint64_t (&f)[16 / siz
 // Wide rows: a ring in shared memory that bulk copies fill several rows ahead, so that no registers are
 // held for what is on its way; 16 bytes of a row a thread and access, NV of them.  The arithmetic runs on
 // pairs (8.5 operations an element instead of 17: with single ones issue slots, not HBM, set the pace).
-// kAll: every array is given and the accesses cover the row exactly, as in a training step.
-template <typename T, int NV, bool kAll>
+// kAll: every array is given and the accesses cover the row exactly, as in a training step.  kPost: the block is
+// normed (without, its gradient may not touch its values, which may be infinite; chosen at run time instead, 8192 x
+// 6000 bf16 takes 169 us, not 164).
+template <typename T, int NV, bool kAll, bool kPost>
 __global__ void __launch_bounds__(512) cconv_residual_norm_backward_ring_kernel(const NormParams p) {
   extern __shared__ __align__(128) uint8_t ring[];
   __shared__ float2 smem[2][32];
@@ -682,10 +683,10 @@ __global__ void __launch_bounds__(512) cconv_residual_norm_backward_ring_kernel(
   T* dgate = static_cast<T*>(p.dgate);
   const int nt = blockDim.x, tid = threadIdx.x;
   const bool has_dx = kAll || dx, has_dres = kAll || dres, has_block = kAll || block;
-  const bool has_pre = kAll || w_pre, has_post = kAll || w_post, has_gate = kAll || gate;
+  const bool has_pre = kAll || w_pre, has_gate = kAll || gate;
   auto inside = [&](int v) { return kAll || (v * nt + tid) * E < p.D; };
   const float inv_d = 1.0f / float(p.D);
-  const int64_t row0 = first_row<T>(p, blockIdx.x), row1 = first_row<T>(p, blockIdx.x + 1);
+  const int64_t row0 = first_row(p, blockIdx.x), row1 = first_row(p, blockIdx.x + 1);
   const int64_t per = p.rows_per_gate ? p.rows_per_gate : p.T;
   float* part = p.part + int64_t(blockIdx.x) * 4 * p.D;
   const uint32_t row_bytes = uint32_t(p.D) * sizeof(T), ring0 = smem_u32(ring), full0 = smem_u32(full);
@@ -719,7 +720,7 @@ __global__ void __launch_bounds__(512) cconv_residual_norm_backward_ring_kernel(
     for (int v = 0; v < NV; ++v) {
       uint64_t fg[P], fw[P];
       get(has_gate, gate + group * p.gate_rs, v, fg, one);
-      get(has_post, w_post, v, fw, one);
+      get(kPost, w_post, v, fw, one);
 #pragma unroll
       for (int i = 0; i < P; ++i) gw[v][i] = mul2(fg[i], fw[i]);
     }
@@ -732,7 +733,7 @@ __global__ void __launch_bounds__(512) cconv_residual_norm_backward_ring_kernel(
       const int c = (v * nt + tid) * E;
       uint64_t fg[P], fw[P];
       get(has_gate, gate + group * p.gate_rs, v, fg, one);
-      get(has_post, w_post, v, fw, one);
+      get(kPost, w_post, v, fw, one);
 #pragma unroll
       for (int i = 0; i < P; ++i) {
         if (inside(v)) {
@@ -807,7 +808,7 @@ __global__ void __launch_bounds__(512) cconv_residual_norm_backward_ring_kernel(
       }
       const float2 q = block_sum2(sum_of(srr), sum_of(ser), smem, buf);
       const float rho1 = rsqrtf(q.x * inv_d + p.eps);
-      const float k1 = -rho1 * (rho1 * (q.y * inv_d));
+      const float k1 = q.y * -inv_d * rho1 * rho1 * rho1;
       const uint64_t rho = pair_of(rho1, rho1), k = pair_of(k1, k1);
 #pragma unroll
       for (int v = 0; v < NV; ++v) {
@@ -816,9 +817,8 @@ __global__ void __launch_bounds__(512) cconv_residual_norm_backward_ring_kernel(
         get(has_dres, row_d, v, s[v], 0);
 #pragma unroll
         for (int i = 0; i < P; ++i) {
-          const uint64_t rhat = mul2(r[v][i], rho);
-          s[v][i] = fma2(x[v][i], mul2(w[i], rho), fma2(rhat, k, s[v][i]));
-          s_pre[v][i] = fma2(x[v][i], rhat, s_pre[v][i]);
+          s[v][i] = fma2(x[v][i], mul2(w[i], rho), fma2(r[v][i], k, s[v][i]));
+          s_pre[v][i] = fma2(x[v][i], mul2(r[v][i], rho), s_pre[v][i]);
         }
       }
     } else {
@@ -840,10 +840,10 @@ __global__ void __launch_bounds__(512) cconv_residual_norm_backward_ring_kernel(
     }
     if (!has_block) continue;
     uint64_t rho = one, k = 0;
-    if (has_post) {
+    if (kPost) {
       const float2 q = block_sum2(sum_of(syy), sum_of(sfy), smem, buf);
       const float rho1 = rsqrtf(q.x * inv_d + p.eps);
-      const float k1 = -rho1 * (rho1 * (q.y * inv_d));
+      const float k1 = q.y * -inv_d * rho1 * rho1 * rho1;
       rho = pair_of(rho1, rho1);
       k = pair_of(k1, k1);
     }
@@ -852,9 +852,9 @@ __global__ void __launch_bounds__(512) cconv_residual_norm_backward_ring_kernel(
       uint64_t o[P];
 #pragma unroll
       for (int i = 0; i < P; ++i) {
-        const uint64_t yhat = mul2(y[v][i], rho), f = mul2(s[v][i], gw[v][i]);
-        s_group[v][i] = fma2(s[v][i], yhat, s_group[v][i]);
-        o[i] = has_post ? fma2(yhat, k, mul2(rho, f)) : f;
+        s_group[v][i] = fma2(s[v][i], kPost ? mul2(y[v][i], rho) : y[v][i], s_group[v][i]);
+        o[i] = mul2(s[v][i], gw[v][i]);
+        if (kPost) o[i] = fma2(y[v][i], k, mul2(rho, o[i]));
       }
       if (inside(v)) put_pairs<T>(dblock + t * p.dblock_rs + (v * nt + tid) * E, o);
     }
@@ -901,7 +901,7 @@ __global__ void __launch_bounds__(512) cconv_residual_norm_ring_kernel(const Nor
   const bool has_block = kAll || block, has_post = kAll || w_post, has_norm = kAll || norm_out;
   auto inside = [&](int v) { return kAll || (v * nt + tid) * E < p.D; };
   const float inv_d = 1.0f / float(p.D);
-  const int64_t row0 = first_row<T>(p, blockIdx.x), row1 = first_row<T>(p, blockIdx.x + 1);
+  const int64_t row0 = first_row(p, blockIdx.x), row1 = first_row(p, blockIdx.x + 1);
   const int64_t per = p.rows_per_gate ? p.rows_per_gate : p.T;
   const uint32_t row_bytes = uint32_t(p.D) * sizeof(T), ring0 = smem_u32(ring), full0 = smem_u32(full);
   const uint64_t one = pair_of(1.0f, 1.0f), scale = pair_of(p.scale, p.scale);
@@ -1013,7 +1013,7 @@ __global__ void __launch_bounds__(512) cconv_residual_norm_backward_long_kernel(
   T* dblock = static_cast<T*>(p.dblock);
   T* dgate = static_cast<T*>(p.dgate);
   const float inv_d = 1.0f / float(p.D);
-  const int64_t row0 = first_row<T>(p, blockIdx.x), row1 = first_row<T>(p, blockIdx.x + 1);
+  const int64_t row0 = first_row(p, blockIdx.x), row1 = first_row(p, blockIdx.x + 1);
   const int64_t per = p.rows_per_gate ? p.rows_per_gate : p.T;
   float* part = p.part + int64_t(blockIdx.x) * 4 * p.D;
   float* whole_sum = p.part + (int64_t(p.nb) * 4 + blockIdx.x) * p.D;
@@ -1041,11 +1041,11 @@ __global__ void __launch_bounds__(512) cconv_residual_norm_backward_long_kernel(
       }
       const float2 q = block_sum2(srr, ser, smem, buf);
       rho = rsqrtf(q.x * inv_d + p.eps);
-      k = rho * (rho * (q.y * inv_d));
+      k = rho * (rho * (rho * (q.y * inv_d)));
     }
     auto grad = [&](int c) {
       float s = fd ? to_f32(fd[c]) : 0.0f;
-      if (fx) s += rho * (w_pre ? to_f32(fx[c]) * to_f32(w_pre[c]) : to_f32(fx[c])) - k * (to_f32(fr[c]) * rho);
+      if (fx) s += rho * (w_pre ? to_f32(fx[c]) * to_f32(w_pre[c]) : to_f32(fx[c])) - k * to_f32(fr[c]);
       return s;
     };
     float rho_y = 1.0f, ky = 0.0f;
@@ -1058,7 +1058,7 @@ __global__ void __launch_bounds__(512) cconv_residual_norm_backward_long_kernel(
       }
       const float2 q = block_sum2(syy, sfy, smem, buf);
       rho_y = rsqrtf(q.x * inv_d + p.eps);
-      ky = rho_y * (rho_y * (q.y * inv_d));
+      ky = rho_y * (rho_y * (rho_y * (q.y * inv_d)));
     }
     // a thread owns the columns c = threadIdx.x (mod blockDim.x) in every sweep, of all arrays
     for (int c = threadIdx.x; c < p.D; c += blockDim.x) {
@@ -1073,7 +1073,7 @@ __global__ void __launch_bounds__(512) cconv_residual_norm_backward_long_kernel(
           if (whole && ends) dgate[group * p.dgate_rs + c] = from_f32<T>(sum);
         }
         part[p.D + c] += dn * yhat;
-        dblock[t * p.dblock_rs + c] = from_f32<T>(w_post ? rho_y * (dn * to_f32(w_post[c])) - ky * yhat : dn);
+        dblock[t * p.dblock_rs + c] = from_f32<T>(w_post ? rho_y * (dn * to_f32(w_post[c])) - ky * to_f32(fy[c]) : dn);
       }
       dresid[t * p.dresid_rs + c] = from_f32<T>(p.scale * s);
     }
@@ -1104,7 +1104,7 @@ __global__ void __launch_bounds__(512) cconv_residual_norm_sums_kernel(const Nor
   if (blockIdx.y >= 2) {
     // every block has a row (nb <= T); row t lies in block ceil((t + 1) nb / T) - 1
     const int i = int(blockIdx.y) - 2;
-    group = p.sums_by_group ? i : (first_row<T>(p, i + 1) - 1) / per;
+    group = p.sums_by_group ? i : (first_row(p, i + 1) - 1) / per;
     const int64_t g0 = group * per, g1 = g0 + per < p.T ? g0 + per : p.T;
     b0 = int(((g0 + 1) * p.nb + p.T - 1) / p.T) - 1;
     b1 = int((g1 * p.nb + p.T - 1) / p.T) - 1;
@@ -1121,7 +1121,7 @@ __global__ void __launch_bounds__(512) cconv_residual_norm_sums_kernel(const Nor
     if (blockIdx.y >= 2) {
       // the group's rows are the last group of its first block and the first of the others, unless they
       // begin that block
-      const bool last = first_row<T>(p, b0) / per != group;
+      const bool last = first_row(p, b0) / per != group;
       from = p.part + 2 * int64_t(p.D) + c;
       if (last && slice == 0) s = load(from + b0 * step + p.D);
       b0 += last;
@@ -1314,14 +1314,20 @@ cudaError_t launch_forward(NormParams p, int sms, cudaStream_t s) {
   return launch_forward_nv<T, 1, 16>(p, threads, grid, s);
 }
 
-template <typename T, int NV, bool kAll>
-cudaError_t launch_ring(NormParams p, int threads, cudaStream_t s) {
-  auto f = cconv_residual_norm_backward_ring_kernel<T, NV, kAll>;
+template <typename T, int NV, bool kAll, bool kPost>
+cudaError_t launch_ring_as(NormParams p, int threads, cudaStream_t s) {
+  auto f = cconv_residual_norm_backward_ring_kernel<T, NV, kAll, kPost>;
   static bool ready[64] = {};
   const cudaError_t e = allow_ring(f, ready);
   if (e != cudaSuccess) return e;
   p.ring_rows = int(std::min<int64_t>(8, ring_rows(p.D, sizeof(T), blocks_an_sm(p.D, sizeof(T)))));
   return launch(f, dim3(unsigned(p.nb)), threads, size_t(p.D) * (size_t(p.ring_rows) * 4 * sizeof(T) + 4), 1, s, p);
+}
+
+template <typename T, int NV>
+cudaError_t launch_ring(const NormParams& p, bool all, int threads, cudaStream_t s) {
+  if (all) return launch_ring_as<T, NV, true, true>(p, threads, s);
+  return p.w_post ? launch_ring_as<T, NV, false, true>(p, threads, s) : launch_ring_as<T, NV, false, false>(p, threads, s);
 }
 
 template <typename T, int NV>
@@ -1404,9 +1410,9 @@ cudaError_t launch_backward(NormParams p, cudaStream_t s) {
     e = launch(cconv_residual_norm_backward_long_kernel<T>, dim3(unsigned(p.nb)), 512, 0, 1, s, p);
   } else if (w) {
     constexpr int kMost = 16 / kWide;
-    if (sh.nv == 1) e = all ? launch_ring<T, 1, true>(p, sh.threads, s) : launch_ring<T, 1, false>(p, sh.threads, s);
-    else if (sh.nv == 2) e = all ? launch_ring<T, 2, true>(p, sh.threads, s) : launch_ring<T, 2, false>(p, sh.threads, s);
-    else e = all ? launch_ring<T, kMost, true>(p, sh.threads, s) : launch_ring<T, kMost, false>(p, sh.threads, s);
+    if (sh.nv == 1) e = launch_ring<T, 1>(p, all, sh.threads, s);
+    else if (sh.nv == 2) e = launch_ring<T, 2>(p, all, sh.threads, s);
+    else e = launch_ring<T, kMost>(p, all, sh.threads, s);
   } else {
     if (sh.nv == 1) e = launch_plain<T, 1>(p, sh.threads, s);
     else if (sh.nv == 2) e = launch_plain<T, 2>(p, sh.threads, s);
