@@ -68,8 +68,7 @@ struct PairParams {
   uint32_t a_stage, stage_bytes; // room of a stage's A; of the whole stage
   uint32_t pieces;              // staged by an epilogue warp
   int paired, act, save;
-  int direct;  // results straight to memory (cut)
-  // direct: where results go and come from (in elements)
+  // cut: where results go and come from (in elements)
   char* out[3];
   int64_t out_rs[3], out_cs[3];
   const char* in[2];
@@ -197,7 +196,7 @@ __device__ __forceinline__ void unstage32(uint32_t base, int r, int c0, float (&
 
 // Pieces that an epilogue warp stages.
 int pieces_of(const Launch& l) {
-  if (l.direct) return 0;
+  if (l.cut()) return 0;
   return l.epilogue == kStore ? 2 : l.epilogue == kScaled || (l.epilogue == kGated && !l.save) ? 1 : 3;
 }
 // Scales of 8-bit rows that an epilogue warp keeps: 16 blocks of k of its 32 rows and of its columns
@@ -507,14 +506,14 @@ __global__ void __launch_bounds__(kThreads, 1) cconv_pair_product_kernel(
         if (lane == 0) mbar_arrive_cluster(tempty0 + 8 * buf);
       };
       if constexpr (!kEightBit) {
-        if (p.direct) {
+        if (p.splits > 1) {  // cut: results straight to memory
           // Columns go in pieces of 32; the pair `owner` finishes `each` neighbouring ones (of both
           // g and u when paired).  The two halves of the warps take turns.
           if (!wait_sums()) break;
           const int all = p.paired ? 4 : o.block_n >> 5, each = all / p.splits, sent = p.paired ? 2 * each : each;
           const int row = q * 32 + lane;
-          if (p.splits > 1) cluster_sync_all();  // every pair's operands are used up: their place takes the pieces
-          for (int i = half; p.splits > 1 && i < all; i += 2) {
+          cluster_sync_all();  // every pair's operands are used up: their place takes the pieces
+          for (int i = half; i < all; i += 2) {
             const int owner = i / each;
             if (owner == share) continue;
             const uint32_t to = cluster_map_shared(base, uint32_t(2 * owner) + rank) +
@@ -530,7 +529,7 @@ __global__ void __launch_bounds__(kThreads, 1) cconv_pair_product_kernel(
               }
             }
           }
-          if (p.splits > 1) cluster_sync_all();  // all pieces have come
+          cluster_sync_all();  // all pieces have come
           met = true;
           for (int i = share * each + half; i < (share + 1) * each; i += 2) {
             const int local = i - share * each;
@@ -542,13 +541,13 @@ __global__ void __launch_bounds__(kThreads, 1) cconv_pair_product_kernel(
               const int n = cols - c * 8;
               float f[8];
               load_sums8(acc + i * 32 + c * 8, f);
-              if (p.splits > 1) join8(base, row, c, p.splits, share, sent, local, f);
+              join8(base, row, c, p.splits, share, sent, local, f);
               if constexpr (kEpi == kStore) {
                 write8<T>(p.out[0], p.out_rs[0], p.out_cs[0], r, at, n, f);
               } else if constexpr (kEpi == kGated) {
                 float u[8];
                 load_sums8(acc + 128 + i * 32 + c * 8, u);
-                if (p.splits > 1) join8(base, row, c, p.splits, share, sent, each + local, u);
+                join8(base, row, c, p.splits, share, sent, each + local, u);
                 if (p.save) {
                   write8<T>(p.out[1], p.out_rs[1], p.out_cs[1], r, at, n, f);
                   write8<T>(p.out[2], p.out_rs[2], p.out_cs[2], r, at, n, u);
@@ -735,13 +734,13 @@ __global__ void __launch_bounds__(kThreads, 1) cconv_pair_product_kernel(
             f[2 * i + 1] = v.y;
           }
         };
-        if (p.direct) {  // as above, with the sums in registers
+        if (p.splits > 1) {  // as above, with the sums in registers
           const int each = (o.block_n >> 5) / p.splits, row = q * 32 + lane, first = half * (cols >> 5);
-          if (p.splits > 1) cluster_sync_all();
+          cluster_sync_all();
 #pragma unroll
           for (int c = 0; c < 4; ++c) {
             const int i = first + c, owner = i / each;
-            if (p.splits > 1 && c * 32 < cols && owner != share) {
+            if (c * 32 < cols && owner != share) {
               const uint32_t to = cluster_map_shared(base, uint32_t(2 * owner) + rank) +
                                   uint32_t((share < owner ? share : share - 1) * each + i - owner * each) * kShareBytes;
 #pragma unroll
@@ -752,7 +751,7 @@ __global__ void __launch_bounds__(kThreads, 1) cconv_pair_product_kernel(
               }
             }
           }
-          if (p.splits > 1) cluster_sync_all();
+          cluster_sync_all();
           met = true;
 #pragma unroll
           for (int c = 0; c < 4; ++c) {
@@ -764,7 +763,7 @@ __global__ void __launch_bounds__(kThreads, 1) cconv_pair_product_kernel(
               for (int e = 0; e < 4; ++e) {
                 float f[8];
                 piece8(c * 4 + e, f);
-                if (p.splits > 1) join8(base, row, e, p.splits, share, each, i - share * each, f);
+                join8(base, row, e, p.splits, share, each, i - share * each, f);
                 write8<T>(p.out[0], p.out_rs[0], p.out_cs[0], r, col + e * 8, n - e * 8, f);
               }
             }
@@ -896,7 +895,7 @@ int run_as(const Launch& l, int sms, cudaStream_t s) {
       if (j == 0 || p.segments) rc = encode_operand(&m.a[j], p.a[j], kEight ? 1 : 2, l.dtype, a_rows_of(p));
       if (rc == CCONV_OK && (j == 0 || p.segments || p.paired)) rc = encode_operand(&m.b[j], p.b[j], kEight ? 1 : 2, l.dtype, p.block_n / 2);
     }
-    if (rc == CCONV_OK && !l.direct) rc = encode_map(&m.out, p.out[0].p, es, l.dtype, p.N, p.M, p.out[0].rs, 128 / es, 32);
+    if (rc == CCONV_OK && !l.cut()) rc = encode_map(&m.out, p.out[0].p, es, l.dtype, p.N, p.M, p.out[0].rs, 128 / es, 32);
     if (rc != CCONV_OK) return rc;
   }
   const Product& p = l.of[0];
@@ -912,12 +911,11 @@ int run_as(const Launch& l, int sms, cudaStream_t s) {
   if constexpr (kEpi == kGated || kEpi == kGatedBackward) {
     CUtensorMap* more_maps[4] = {&maps.out1, &maps.out2, &maps.in[0], &maps.in[1]};
     const Mat* mats[4] = {&p.out[1], &p.out[2], &p.in[0], &p.in[1]};
-    for (int i = 0; i < 4 && !l.direct; ++i)
+    for (int i = 0; i < 4 && !l.cut(); ++i)
       if (mats[i]->p && (rc = encode_map(more_maps[i], mats[i]->p, es, l.dtype, p.N, p.M, mats[i]->rs, 64, 32))) return rc;
   }
   q.a_stage = a_most;
   q.stage_bytes = a_most + b_most;
-  q.direct = l.direct;
   q.pieces = uint32_t(pieces_of(l));
   q.stages = stages_of(l, a_most, b_most);
   q.paired = p.paired;
@@ -1125,7 +1123,6 @@ void cut(Launch* l, int block_n, int splits) {
   Product& p = l->of[0];
   p.block_n = block_n;
   l->splits = splits;
-  l->direct = splits > 1;
 }
 }  // namespace
 

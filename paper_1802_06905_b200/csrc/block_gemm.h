@@ -27,7 +27,7 @@ struct Product {
   Operand a[2], b[2];
   bool segments = false, paired = false;
   int64_t M = 0, N = 0, K = 0;  // paired: N = rows of b[0]
-  Mat out[3], in[2];            // `in` row-major; unless direct, all row-major and in place for the copy engine
+  Mat out[3], in[2];            // `in` row-major; unless cut, all row-major and in place for the copy engine
   int block_n = 256;            // columns of a tile: 256, 128 or (kStore, B k-contiguous) 64
 };
 
@@ -36,10 +36,10 @@ struct Launch {
   int count = 1;                // more than one: kStore, uncut
   int epilogue = kStore;
   int splits = 1;               // pairs that share a tile, each a part of k: 1, 2 or 4
-  bool direct = false;          // results go straight to any layout (where cut)
   int dtype = 0, act = 0;
   bool save = false;
   Mat row_scale, col_scale;     // kScaled: scale (row, kb) of A, (row / 128, kb) of B
+  bool cut() const { return splits > 1; }  // results then go straight to any layout
 };
 
 int run_products(const Launch& l, int sms, cudaStream_t s);

@@ -110,7 +110,7 @@ class Steps {
       Mat& out = p.out[l.count > 1 ? 0 : i];
       out = to[i];
       Operand o;
-      if (l.direct) continue;  // written straight to any layout
+      if (l.cut()) continue;  // written straight to any layout
       if (operand_in_place(to[i], p.M, p.N, es, false, &o)) {
         out = Mat(o.p, o.pitch, 1);
       } else {

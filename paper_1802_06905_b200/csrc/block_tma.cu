@@ -6,25 +6,6 @@
 #include "host_setup.h"
 
 namespace cconv {
-namespace {
-
-using EncodeFn = CUresult (*)(CUtensorMap*, CUtensorMapDataType, cuuint32_t, void*, const cuuint64_t*, const cuuint64_t*,
-                              const cuuint32_t*, const cuuint32_t*, CUtensorMapInterleave, CUtensorMapSwizzle,
-                              CUtensorMapL2promotion, CUtensorMapFloatOOBfill);
-
-EncodeFn encode_fn() {
-  static EncodeFn fn = [] {
-    void* p = nullptr;
-    cudaDriverEntryPointQueryResult q;
-    if (cudaGetDriverEntryPoint("cuTensorMapEncodeTiled", &p, cudaEnableDefault, &q) != cudaSuccess ||
-        q != cudaDriverEntryPointSuccess)
-      p = nullptr;
-    return reinterpret_cast<EncodeFn>(p);
-  }();
-  return fn;
-}
-
-}  // namespace
 
 bool operand_in_place(const Mat& m, int64_t rows, int64_t k, int es, bool allow_row_major, Operand* o) {
   o->p = m.p;
@@ -50,7 +31,7 @@ bool operand_in_place(const Mat& m, int64_t rows, int64_t k, int es, bool allow_
 
 int encode_map(CUtensorMap* tm, const void* p, int es, int dtype, int64_t inner, int64_t outer, int64_t pitch,
                int box_inner, int box_outer) {
-  EncodeFn enc = encode_fn();
+  EncodeTiledFn enc = encode_tiled_fn();
   if (!enc) {
     set_last_cuda_error("cuTensorMapEncodeTiled is not available from this driver");
     return CCONV_ECUDA;

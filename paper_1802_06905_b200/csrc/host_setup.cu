@@ -12,16 +12,6 @@
 
 namespace cconv {
 
-namespace {
-
-thread_local std::string g_last_cuda_error;
-
-typedef CUresult (*EncodeTiledFn)(CUtensorMap*, CUtensorMapDataType, cuuint32_t, void*,
-                                  const cuuint64_t*, const cuuint64_t*, const cuuint32_t*,
-                                  const cuuint32_t*, CUtensorMapInterleave, CUtensorMapSwizzle,
-                                  CUtensorMapL2promotion, CUtensorMapFloatOOBfill);
-
-// The driver is reached through the runtime so that the library loads on machines without one.
 EncodeTiledFn encode_tiled_fn() {
   static EncodeTiledFn fn = [] {
     void* p = nullptr;
@@ -34,6 +24,10 @@ EncodeTiledFn encode_tiled_fn() {
   }();
   return fn;
 }
+
+namespace {
+
+thread_local std::string g_last_cuda_error;
 
 int env_int(const char* name, int dflt) {
   const char* v = std::getenv(name);

@@ -13,6 +13,14 @@ namespace cconv {
 void set_last_cuda_error(const std::string& msg);  // per host thread
 const char* last_cuda_error();
 
+// cuTensorMapEncodeTiled, or null.  The driver is reached through the runtime so that the library loads on
+// machines without one.
+typedef CUresult (*EncodeTiledFn)(CUtensorMap*, CUtensorMapDataType, cuuint32_t, void*,
+                                  const cuuint64_t*, const cuuint64_t*, const cuuint32_t*,
+                                  const cuuint32_t*, CUtensorMapInterleave, CUtensorMapSwizzle,
+                                  CUtensorMapL2promotion, CUtensorMapFloatOOBfill);
+EncodeTiledFn encode_tiled_fn();
+
 // Everything cconv_halo_kernel needs to know about a shape and its tile (descriptors included).
 void build_halo_params(const Dims& d, const HaloTile& t, HaloKernelParams* p);
 
