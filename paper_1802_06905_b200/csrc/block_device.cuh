@@ -82,7 +82,7 @@ __device__ __forceinline__ float activation_of(float g, float& da) {
     return g * phi;
   } else if constexpr (kAct == CCONV_ACT_GELU_TANH) {
     const float k = 1.5957691216057308f;  // 2 sqrt(2/pi)
-    const float g2 = g * g;
+    const float g2 = fminf(g * g, 1e12f);  // s is 0 or 1 long before: no infinity that s (1 - s) = 0 would multiply
     const float s = __fdividef(1.0f, 1.0f + __expf(-k * (g + 0.044715f * g * g2)));
     if (kDerivative) da = s + g * s * (1.0f - s) * k * (1.0f + 0.134145f * g2);
     return g * s;

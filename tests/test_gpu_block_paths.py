@@ -504,3 +504,20 @@ def test_without_a_norm_the_block_s_gradient_does_not_depend_on_the_block(T, D):
     n.y[0, 1], n.y[0, 2], n.y[T - 1, 3] = float("inf"), float("nan"), float("-inf")
     got = n.run_backward(use_dx=False)
     assert torch.equal(got[0], want[0]) and torch.equal(got[1], want[1])
+
+
+@pytest.mark.parametrize("act", ["silu", "gelu", "gelu_tanh", "relu"])
+def test_pre_activations_of_any_finite_size(act):
+    """Up to the ends of bf16's range every activation is g or 0, and its derivative 1 or 0."""
+    T, F = 64, 64
+    g = torch.cat([s * 10.0 ** torch.arange(3.0, 35.0, device="cuda") for s in (1, -1)]).to(BF16).expand(T, F).contiguous()
+    eye = torch.eye(T, device="cuda").to(BF16)
+    up = torch.full((T, F), 2.0, device="cuda").to(BF16)
+    wd, none = torch.ones((T, F), device="cuda").to(BF16), torch.zeros((F, T), device="cuda").to(BF16)
+    dx, dwg, dwu, dwd = poisoned((T, T), BF16), poisoned((F, T), BF16), poisoned((F, T), BF16), poisoned((T, F), BF16)
+    block.ffn_backward(eye, eye, none, none, wd, g, up, dx, dwg, dwu, dwd, act=block.ACTS[act])
+    on = (g > 0).double()
+    # (products with the identity add zeros: values are exact but for their own rounding, 1 of them 2^-8)
+    close(dwd, 2 * g.double() * on, 2.0 ** -8 * 2 * g.double().abs() * on, act + " h")
+    close(dwu.t(), g.double() * on, 2.0 ** -8 * g.double().abs() * on, act + " dL/du")
+    close(dwg.t(), 2 * on, 2.0 ** -7 * on, act + " dL/dg")
