@@ -6,7 +6,7 @@
  *   feed-forward    y = (act(x Wg^T) * (x Wu^T)) Wd^T                     and its gradients
  *   residual norm   r' = scale r + gate * norm(y) * w_post,  x = norm(r') * w_pre   and its gradients
  *                   norm(v) = v / sqrt(mean(v^2) + eps), over the D channels of a token
- *   8-bit product   C[m,n] = sum_kb sa[m,kb] sb[n/128,kb] sum_{k in block kb} A[m,k] B[n,k]
+ *   8-bit product   C[m,n] = sum_kb (sa[m,kb] sb[n/128,kb]) sum_{k in block kb} A[m,k] B[n,k]
  *   quantisation    8-bit values (e4m3) and a scale for each 1 x 128 or 128 x 128 block
  *
  * Matrices are given by the address of element (0,0) and two strides in elements.  Strides of inputs
@@ -18,7 +18,9 @@
  * Everything is computed from values in 32 bits: products accumulate, norms and sums of gradients are
  * held in fp32, and each output is rounded once to its type.  The hidden activations h = act(g) * u
  * and the gradients of the pre-activations, which are operands of the tensor cores, are rounded to
- * the type in between.  Results do not depend on timing: no sum is formed by atomics.
+ * the type in between (fp16: infinite beyond 65504); forward calls of up to 4 tokens whose operands are
+ * read in place keep what the rounding of h left.  The last bits of a token's result may so depend on
+ * how many tokens share its call.  They do not depend on timing: no sum is formed by atomics.
  *
  * Ownership: all pointers are DEVICE pointers of the current device, owned by the caller; a NULL
  * `data` stands for an absent matrix where the text allows one.  The workspace is device memory,
@@ -26,6 +28,8 @@
  * arguments; its contents do not matter before or after a call, and calls that may run at the same
  * time need workspaces of their own.  Outputs must not overlap inputs, each other or the workspace,
  * but for the two cases named below, where an output may be one input itself (address and strides).
+ * (Slices of one array, and columns that lie in it in turn, are told from overlaps by pitch and strides;
+ * operands that interleave in other ways are refused.)
  * Calls are asynchronous on `cuda_stream`, ordered with the stream's other work like any kernel,
  * allocate nothing, and may be captured in a CUDA graph.
  *

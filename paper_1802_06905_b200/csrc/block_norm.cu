@@ -8,10 +8,12 @@
 //              dw_post = sum_t dn y rho_y,  dw_pre = sum_t dx r' rho_r
 //   (rho^3 mean is formed from the mean on, a rho at a time: rho^3 alone leaves fp32's range for rows of 1e13 or an eps of 1e-26)
 //
-// Both directions read every [T][D] array once and write every output once; a row stays in registers
-// between its two reductions (over y, then over r'; backward: over r' and e, then over y and f), so
-// they are bound by HBM.  Measured, 16384 x 4096 bf16 with 8 gates: forward 89.5 us, 6.0 TB/s (4 arrays once: 82 us
-// at the rate of a copy); backward 149 us, 5.4 TB/s (6 arrays: 123 us), 135 of them the first kernel.  One token
+// Both directions read every [T][D] array once from memory and write every output once; a row stays on chip, in
+// registers or in shared memory, between its two reductions (over y, then over r'; backward: over r' and e, then
+// over y and f), so they are bound by HBM.  That holds forward up to 16384 channels, and backward up to 65536 where a
+// block or a cluster of them has room for the row; the *_long_ kernels, for the rest, read a row once for
+// each sweep over it.  Measured, 16384 x 4096 bf16 with 8 gates: forward 89.5 us, 6.0 TB/s (4 arrays once: 82 us
+// at the rate of a copy); backward 147 us, 5.5 TB/s (6 arrays: 123 us), 135 of them the first kernel.  One token
 // of 4096 channels: 2.5 us on the device.
 #include <algorithm>
 #include <type_traits>
@@ -415,11 +417,11 @@ __global__ void __launch_bounds__(kThreads) cconv_residual_norm_narrow_kernel(co
 // rows is complete there and written at once.
 // Rows that are not wide (an odd length, pitch or address): element v nt + tid is the thread's, so that the
 // narrow accesses of a warp are neighbours.  kThreads: rows come through the ring above, and a block's size is
-// known when compiled, which leaves accesses no address arithmetic of their own (16384 x 4095 bf16: 260 us, and 490
+// known when compiled, which leaves accesses no address arithmetic of their own (16384 x 4095 bf16: 259 us, and 490
 // with a size known at the launch); 0: straight from global memory, where rows are few or the ring has no room for
 // two (1118 us).  kCluster: rows too long for one block's registers are shared by the 2, 4 or 8 blocks of a
 // cluster, a range of columns each, which exchange their sums through distributed shared memory (4096 x 16384
-// bf16: 357 us; with sums in memory, cconv_residual_norm_backward_long_kernel, 2860 us).
+// bf16: 345 us; with sums in memory, cconv_residual_norm_backward_long_kernel, 2860 us).
 constexpr int kMostParts = 8;
 template <typename T, int NV, int kThreads, bool kCluster = false>
 __global__ void __launch_bounds__(kThreads ? kThreads : 512, 512 / (kThreads ? kThreads : 512)) cconv_residual_norm_backward_kernel(const NormParams p) {
