@@ -111,7 +111,9 @@ class Steps {
       out = to[i];
       Operand o;
       if (l.cut()) continue;  // written straight to any layout
-      if (operand_in_place(to[i], p.M, p.N, es, false, &o)) {
+      // (the copy engine stops a store at the row's last 16 bytes, not at its last element: a row that ends within
+      // them would take zeros behind its end)
+      if (p.N * es % 16 == 0 && operand_in_place(to[i], p.M, p.N, es, false, &o)) {
         out = Mat(o.p, o.pitch, 1);
       } else {
         out = scratch(p.M, p.N, es);

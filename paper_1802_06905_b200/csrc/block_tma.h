@@ -23,7 +23,8 @@ struct Operand {
 bool operand_in_place(const Mat& m, int64_t rows, int64_t k, int es, bool allow_row_major, Operand* o);
 
 // 2-D tensor map: `inner` contiguous elements by `outer` rows at `pitch` elements; a box of box_inner x
-// box_outer with 128-byte swizzle (box_inner * es = 128).  es: 1 (e4m3), 2 (bf16 or fp16 by dtype).
+// box_outer with 128-byte swizzle (box_inner * es = 128).  es: 1 (e4m3), 2 (bf16 or fp16 by dtype).  Loads read zeros
+// past `inner`; stores write the whole 16 bytes that `inner` ends in.
 int encode_map(CUtensorMap* tm, const void* p, int es, int dtype, int64_t inner, int64_t outer, int64_t pitch,
                int box_inner, int box_outer);
 

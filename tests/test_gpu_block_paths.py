@@ -521,3 +521,73 @@ def test_pre_activations_of_any_finite_size(act):
     close(dwd, 2 * g.double() * on, 2.0 ** -8 * 2 * g.double().abs() * on, act + " h")
     close(dwu.t(), g.double() * on, 2.0 ** -8 * g.double().abs() * on, act + " dL/du")
     close(dwg.t(), 2 * on, 2.0 ** -7 * on, act + " dL/dg")
+
+
+def embedded(shape, dtype, pad, above=1, left=0):
+    """A result inside a larger array, from a 16-byte boundary on and at a pitch of 16 bytes where `pad` allows."""
+    big = torch.full((shape[0] + above + 1, left + shape[1] + pad), 5.0, device="cuda").to(dtype)
+    return big, big[above:above + shape[0], left:left + shape[1]]
+
+
+def pitch_to(n, unit):
+    return -n % unit + unit
+
+
+# rows that end within 16 bytes, with the next row or another array right behind them
+@pytest.mark.parametrize("T,D,F", [(1, 69, 133), (6, 1, 5), (20, 69, 133), (70, 129, 63), (260, 257, 131), (700, 65, 1021)])
+@pytest.mark.parametrize("dtype", [BF16, FP16])
+def test_ffn_results_of_any_length_leave_their_surroundings(T, D, F, dtype):
+    f = Ffn(T, D, F, dtype)
+    for left in (0, 8):
+        bufs = [embedded(s, dtype, pitch_to(s[1], 8), left=left) for s in ((T, D), (T, F), (T, F))]
+        for save in (True, False):
+            block.ffn_forward(f.x, f.wg, f.wu, f.wd, bufs[0][1], gate_pre=bufs[1][1] if save else None,
+                              up_pre=bufs[2][1] if save else None)
+            f.check_forward(bufs[0][1], *((bufs[1][1], bufs[2][1]) if save else (None, None)))
+            for big, v in bufs:
+                v.fill_(5.0)
+                assert (big == 5.0).all()
+        bufs = [embedded(s, dtype, pitch_to(s[1], 8), left=left) for s in ((T, D), (F, D), (F, D), (D, F))]
+        block.ffn_backward(f.dy, f.x, f.wg, f.wu, f.wd, f.g, f.u, *[v for _, v in bufs])
+        f.check_backward(*[v for _, v in bufs])
+        for big, v in bufs:
+            v.fill_(5.0)
+            assert (big == 5.0).all()
+
+
+@pytest.mark.parametrize("M,N,K", [(1, 345, 897), (3, 5, 128), (40, 133, 256), (232, 1, 1), (600, 1021, 384)])
+@pytest.mark.parametrize("dtype,unit", [(BF16, 8), (FP16, 8), (FP32, 4)])
+def test_fp8_results_of_any_length_leave_their_surroundings(M, N, K, dtype, unit):
+    a, sa, b, sb = fp8_operands(M, N, K)
+    for left in (0, unit):
+        big, v = embedded((M, N), dtype, pitch_to(N, unit), left=left)
+        block.fp8_product(a, sa, b, sb, v)
+        fp8_check(a, sa, b, sb, v)
+        v.fill_(5.0)
+        assert (big == 5.0).all()
+
+
+def test_norms_and_values_in_8_bits_of_any_length_leave_their_surroundings():
+    for T, D in ((3, 69), (40, 1001), (2500, 1001), (6, 8201), (2, 20001), (2500, 260)):
+        for dtype in (BF16, FP32):
+            n = Norm(T, D, dtype, "groups", max(1, T // 3))
+            (big, v), (big2, v2) = embedded((T, D), dtype, pitch_to(D, 8)), embedded((T, D), dtype, pitch_to(D, 8))
+            n.check(*n.run(out=v, xout=v2))
+            want = n.run_backward()
+            (big3, v3), (big4, v4), (big5, v5) = (embedded(t.shape, dtype, pitch_to(D, 8)) for t in (want[0], want[1], want[3]))
+            vectors = [torch.full((D + 16,), 5.0, device="cuda").to(dtype) for _ in range(2)]
+            block.residual_norm_backward(n.dr, n.dx, n.o, v3, block=n.y, dblock=v4, w_post=n.wpost, dw_post=vectors[0][8:8 + D],
+                                         gate=n.gate, dgate=v5, w_pre=n.wpre, dw_pre=vectors[1][8:8 + D], rows_per_gate=n.rows,
+                                         scale=n.scale, eps=n.eps)
+            n.check_backward((v3, v4, vectors[0][8:8 + D], v5, vectors[1][8:8 + D]))
+            for whole, part in ((big, v), (big2, v2), (big3, v3), (big4, v4), (big5, v5), *((t, t[8:8 + D]) for t in vectors)):
+                part.fill_(5.0)
+                assert (whole == 5.0).all()
+        x = normal(gen(T), (T, D), BF16)
+        for rows in (1, 128):
+            bytes_, q = embedded((T, D), torch.int8, pitch_to(D, 8))
+            big, s = embedded((-(-T // rows), -(-D // 128)), FP32, 4)
+            block.quantize_blocks(x, q.view(E4M3), s, block_rows=rows)
+            q.fill_(5)
+            s.fill_(5.0)
+            assert (bytes_ == 5).all() and (big == 5.0).all()
