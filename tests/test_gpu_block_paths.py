@@ -1,6 +1,7 @@
 """The feed-forward sub-block where its pieces meet: every cut of a product, offsets past 32 bits, the order of
 a stream that convolutions share, other devices' streams, and the command that runs all of it together."""
 import ctypes
+import random
 
 import pytest
 import torch
@@ -591,3 +592,59 @@ def test_norms_and_values_in_8_bits_of_any_length_leave_their_surroundings():
             q.fill_(5)
             s.fill_(5.0)
             assert (bytes_ == 5).all() and (big == 5.0).all()
+
+
+def test_random_sequences_with_convolutions_run_in_order(monkeypatch):
+    """Calls of every kind, empty ones among them, over five buffers that they read and write in turn: without
+    synchronisation bit for bit what they give with a synchronisation after each.  (Convolutions that have to wait
+    would take another kernel, which rounds otherwise; the switch keeps them on one.)"""
+    monkeypatch.setenv("CCONV_WAIT_TWIN", "0")
+    rng = random.Random(4)
+    B, C, H, D = 64, 64, 13, 208
+    n, g = H * H * C * B, gen(21)
+    f3, f1 = normal(g, (C, 3, 3, C), BF16, (9 * C) ** -0.5), normal(g, (C, 1, 1, C), BF16, C ** -0.5)
+    wg, wu, wd, w = normal(g, (320, D), BF16, D ** -0.5), normal(g, (320, D), BF16, D ** -0.5), normal(g, (D, 320), BF16, 0.06), normal(g, (D,), BF16)
+    w8, s8 = torch.empty((D, D), dtype=E4M3, device="cuda"), torch.empty((2, 2), device="cuda")
+    block.quantize_blocks(normal(g, (D, D), BF16, D ** -0.5), w8, s8, block_rows=128)
+    start = [normal(g, (n,), BF16) for _ in range(5)]
+    kinds = ("conv3", "conv1", "conv1", "ffn", "ffn", "norm", "in place", "backward", "fp8", "quantize", "empty", "torch")
+
+    def run(calls, sync):
+        bufs = [t.clone() for t in start]
+        q, s, dw = torch.zeros((n // D, D), dtype=E4M3, device="cuda"), torch.zeros((n // D, 2), device="cuda"), torch.zeros_like(w)
+        torch.cuda.synchronize()
+        for kind, i, j, k, T, at in calls:
+            a, b, c = (bufs[m][at:at + T * D].view(T, D) for m in (i, j, k))
+            x, y = bufs[i].view(H, H, C, B), bufs[j]
+            if kind == "conv3":
+                binding.conv_forward(x, f3, y[:11 * 11 * C * B].view(C, 11, 11, B), B, C, C, 11, 11, 3, 3)
+            elif kind == "conv1":
+                binding.conv_forward(x, f1, y.view(C, H, H, B), B, C, C, H, H, 1, 1)
+            elif kind == "ffn":
+                block.ffn_forward(a, wg, wu, wd, b)
+            elif kind == "norm":
+                block.residual_norm_forward(a, b, c, w_pre=w, scale=0.5)
+            elif kind == "in place":
+                block.residual_norm_forward(a, a, b, block=c, w_post=w, w_pre=w, scale=0.5)
+            elif kind == "backward":
+                block.residual_norm_backward(a, b, c, a, w_pre=w, dw_pre=dw, scale=0.25)
+            elif kind == "quantize":
+                block.quantize_blocks(a, q[:T], s[:T])
+            elif kind == "fp8":
+                block.fp8_product(q[:T], s[:T], w8, s8, b)
+            elif kind == "empty":
+                block.ffn_forward(a[:0], wg, wu, wd, b[:0])
+            else:
+                b.copy_(a * 0.5)
+            if sync:
+                torch.cuda.synchronize()
+        torch.cuda.synchronize()
+        return [*bufs, q.view(torch.uint8), s, dw]
+    for _ in range(100):
+        calls = [(rng.choice(kinds), *rng.sample(range(5), 3), rng.choice([1, 3, 16, 40, 300, 1500, n // D - 40]), rng.choice([0, 8, 8192]))
+                 for _ in range(rng.randint(5, 30))]
+        want = run(calls, True)
+        for _ in range(2):
+            for x, y in zip(want, run(calls, False)):
+                assert torch.equal(x.view(torch.uint8), y.view(torch.uint8)), calls
+    assert block.status() == (0, 0)
