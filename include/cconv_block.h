@@ -8,6 +8,7 @@
  *                   norm(v) = v / sqrt(mean(v^2) + eps), over the D channels of a token
  *   8-bit product   C[m,n] = sum_kb (sa[m,kb] sb[n/128,kb]) sum_{k in block kb} A[m,k] B[n,k]
  *   quantisation    8-bit values (e4m3) and a scale for each 1 x 128 or 128 x 128 block
+ *   norm in 8 bits  the residual norm whose x is written as 8-bit values and scales
  *
  * Matrices are given by the address of element (0,0) and two strides in elements.  Strides of inputs
  * are any non-negative numbers (0 repeats a row or column); the elements of an output are distinct.
@@ -116,6 +117,17 @@ typedef struct {
 int64_t cconv_residual_norm_backward_workspace(const cconv_residual_norm_args* args);
 int cconv_residual_norm_forward(const cconv_residual_norm_args* args, void* cuda_stream);
 int cconv_residual_norm_backward(const cconv_residual_norm_args* args, void* cuda_stream);
+
+/* The forward call with x in 8 bits, a scale for each 128 channels of a token, as cconv_quantize_blocks gives
+ * them for x before its rounding to `dtype`: scale = max|x| / 448, q = x / scale.  norm.norm_out (x rounded to
+ * `dtype`) may be given too; resid_out as in the forward call. */
+typedef struct {
+  cconv_residual_norm_args norm; /* its forward operands; the others and the workspace are not looked at */
+  cconv_matrix q;                /* out: [T][D] e4m3, column stride 1 */
+  cconv_matrix q_scale;          /* out: [T][ceil(D/128)] fp32, any strides */
+} cconv_residual_norm_quantize_args;
+
+int cconv_residual_norm_quantize(const cconv_residual_norm_quantize_args* args, void* cuda_stream);
 
 /* ---- product in 8-bit floating point with a scale for each block of 128 ------------------------ */
 typedef struct {

@@ -2,6 +2,7 @@
 
     ffn_forward / ffn_backward                        y = (act(x Wg^T) * (x Wu^T)) Wd^T
     residual_norm_forward / residual_norm_backward    r' = scale r + gate norm(y) w_post, x = norm(r') w_pre
+    residual_norm_quantize                            the same with x in 8 bits and scales
     fp8_product                                       8-bit operands with a scale for each block of 128
     quantize_blocks                                   the 8-bit values and the scales
 
@@ -28,6 +29,7 @@ _TYPES = {torch.bfloat16: TYPE_BF16, torch.float16: TYPE_FP16, torch.float32: TY
 EXPORTS = (
     "cconv_ffn_forward_workspace", "cconv_ffn_backward_workspace", "cconv_ffn_forward", "cconv_ffn_backward",
     "cconv_residual_norm_backward_workspace", "cconv_residual_norm_forward", "cconv_residual_norm_backward",
+    "cconv_residual_norm_quantize",
     "cconv_fp8_product_workspace", "cconv_fp8_product", "cconv_quantize_blocks", "cconv_block_status",
 )
 
@@ -38,6 +40,7 @@ _FFN = struct.Struct("qqqii" + _MAT * 12)
 _NORM = struct.Struct("qqiffxxxxq" + _MAT * 3 + "PP" + _MAT * 7 + "PP")
 _FP8 = struct.Struct("qqqii" + _MAT * 5)
 _QUANT = struct.Struct("qqii" + _MAT * 3)
+_TWO = struct.Struct(_MAT * 2)  # behind the norm's, in the call with 8-bit results
 _SPACE = struct.Struct("PQ")
 _NO_SPACE = _SPACE.pack(0, 0)
 _NONE = (0, 0, 0)
@@ -224,6 +227,19 @@ def _gate(gate, T, D, rows_per_gate, dt, dev, name):
     return _row(gate, (groups, D), dt, dev, name)
 
 
+def _norm_forward_args(resid, resid_out, norm_out, block, w_post, gate, w_pre, rows_per_gate, scale, eps):
+    dtype, dev = _type(resid, "resid")
+    shape = T, D = resid.shape
+    dt = resid.dtype
+    return _NORM.pack(
+        T, D, dtype, scale, eps, rows_per_gate, *_row(resid, shape, dt, dev, "resid"),
+        *(_NONE if block is None else _row(block, shape, dt, dev, "block")),
+        *_gate(gate, T, D, rows_per_gate, dt, dev, "gate"), _vec(w_post, D, dt, dev, "w_post"),
+        _vec(w_pre, D, dt, dev, "w_pre"), *_row(resid_out, shape, dt, dev, "resid_out"),
+        *(_NONE if norm_out is None else _row(norm_out, shape, dt, dev, "norm_out")),
+        0, 0, 0, 0, 0, 0, 0, 0, 0, 0, 0, 0, 0, 0, 0, 0, 0) + _NO_SPACE, dev
+
+
 def residual_norm_forward(resid, resid_out, norm_out=None, block=None, w_post=None, gate=None, w_pre=None,
                           rows_per_gate=0, scale=1.0, eps=1e-6, stream=None):
     """cconv_residual_norm_forward: resid_out = scale resid + gate norm(block) w_post and
@@ -233,18 +249,24 @@ def residual_norm_forward(resid, resid_out, norm_out=None, block=None, w_post=No
     residual is scaled; without ``w_post`` the block is not normed; without ``gate`` it counts in full;
     without ``norm_out`` there is no second norm.  ``gate`` [ceil(T / rows_per_gate), D] has a row for
     each ``rows_per_gate`` tokens (0: one row for all).  ``resid_out`` may be ``resid``."""
-    dtype, dev = _type(resid, "resid")
-    shape = T, D = resid.shape
-    dt = resid.dtype
-    args = _NORM.pack(
-        T, D, dtype, scale, eps, rows_per_gate, *_row(resid, shape, dt, dev, "resid"),
-        *(_NONE if block is None else _row(block, shape, dt, dev, "block")),
-        *_gate(gate, T, D, rows_per_gate, dt, dev, "gate"), _vec(w_post, D, dt, dev, "w_post"),
-        _vec(w_pre, D, dt, dev, "w_pre"), *_row(resid_out, shape, dt, dev, "resid_out"),
-        *(_NONE if norm_out is None else _row(norm_out, shape, dt, dev, "norm_out")),
-        0, 0, 0, 0, 0, 0, 0, 0, 0, 0, 0, 0, 0, 0, 0, 0, 0)
-    _call("cconv_residual_norm_forward", args + _NO_SPACE, dev, stream)
+    args, dev = _norm_forward_args(resid, resid_out, norm_out, block, w_post, gate, w_pre, rows_per_gate, scale, eps)
+    _call("cconv_residual_norm_forward", args, dev, stream)
     return resid_out, norm_out
+
+
+def residual_norm_quantize(resid, resid_out, q, q_scale, norm_out=None, block=None, w_post=None, gate=None, w_pre=None,
+                           rows_per_gate=0, scale=1.0, eps=1e-6, stream=None):
+    """cconv_residual_norm_quantize: residual_norm_forward whose x = norm(resid_out before its rounding) w_pre is
+    written as float8_e4m3fn values ``q`` [T, D] (contiguous rows) and fp32 scales ``q_scale`` [T, ceil(D/128)].
+
+    q = x / q_scale and q_scale = max|x| / 448 as quantize_blocks gives them, for x before its rounding to the
+    type.  ``norm_out``, if given, gets x rounded to the type.  Everything else as residual_norm_forward."""
+    args, dev = _norm_forward_args(resid, resid_out, norm_out, block, w_post, gate, w_pre, rows_per_gate, scale, eps)
+    T, D = resid.shape
+    args += _TWO.pack(*_row(q, (T, D), torch.float8_e4m3fn, dev, "q"),
+                      *_mat(q_scale, (T, (D + 127) // 128), torch.float32, dev, "q_scale"))
+    _call("cconv_residual_norm_quantize", args, dev, stream)
+    return resid_out, q, q_scale
 
 
 def _norm_backward_args(dresid_out, dnorm_out, resid_out, dresid, block, dblock, w_post, dw_post, gate, dgate, w_pre,

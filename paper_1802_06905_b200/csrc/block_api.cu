@@ -276,6 +276,51 @@ int64_t norm_workspace(const cconv_residual_norm_args& a, int sms) {
   return round_up64(nb * 5 * a.D * 4, 256);
 }
 
+// The forward call; with q and q_scale the second norm's result goes there in 8 bits.
+int norm_forward(cconv_residual_norm_args a, const cconv_matrix* q, const cconv_matrix* q_scale, void* cuda_stream) {
+  if (!norm_sizes_ok(a)) return CCONV_EINVAL;
+  const int es = type_bytes(a.dtype);
+  a.resid = same_row(a.resid, a.T, a.D);
+  a.block = same_row(a.block, a.T, a.D);
+  a.gate = same_row(a.gate, gate_rows(a), a.D);
+  a.resid_out = same_row(a.resid_out, a.T, a.D);
+  a.norm_out = same_row(a.norm_out, a.T, a.D);
+  if (!unit(a.resid, a.D) || !unit(a.block, a.D) || !unit(a.gate, a.D) || !unit(a.resid_out, a.D) || !unit(a.norm_out, a.D))
+    return CCONV_EINVAL;
+  if (a.T && a.D && ((!a.block.data && (a.gate.data || a.w_post)) || (!a.norm_out.data && !q && a.w_pre))) return CCONV_EINVAL;
+  Operands o;
+  const int resid = o.in(a.resid, a.T, a.D, es);
+  if (a.block.data) o.in(a.block, a.T, a.D, es);
+  if (a.gate.data) o.in(a.gate, gate_rows(a), a.D, es);
+  if (a.w_post) o.in(a.w_post, a.D, es);
+  if (a.w_pre) o.in(a.w_pre, a.D, es);
+  o.may_be_one(resid, o.out(a.resid_out, a.T, a.D, es));
+  if (a.norm_out.data) o.out(a.norm_out, a.T, a.D, es);
+  cconv_matrix values{}, scales{};
+  if (q) {
+    values = same_row(*q, a.T, a.D);
+    scales = same_row(*q_scale, a.T, cdiv64(a.D, 128));
+    if (!unit(values, a.D)) return CCONV_EINVAL;
+    o.out(values, a.T, a.D, 1);
+    o.out(scales, a.T, cdiv64(a.D, 128), 4);
+  }
+  if (!o.distinct()) return CCONV_EINVAL;
+  if (!o.writes()) return CCONV_OK;
+  const int sms = block_sm_count();
+  if (sms < 0) return sms;
+  NormParams p = norm_params(a);
+  p.q = static_cast<uint8_t*>(values.data); p.q_rs = values.row_stride;
+  p.q_scale = static_cast<float*>(scales.data); p.q_scale_rs = scales.row_stride; p.q_scale_cs = scales.col_stride;
+  const int rc = block_status_word(&p.status);
+  if (rc != CCONV_OK) return rc;
+  p.limit_ns = block_wait_limit_ns();
+  return o.run(cuda_stream, sms, [&] {
+    cudaStream_t s = static_cast<cudaStream_t>(cuda_stream);
+    return block_cuda_error(q ? run_norm_quantize(p, a.dtype, sms, s) : run_norm_forward(p, a.dtype, sms, s),
+                            "cconv_residual_norm_forward");
+  });
+}
+
 bool fp8_sizes_ok(const cconv_fp8_product_args& a) {
   return length_ok(a.M) && length_ok(a.N) && length_ok(a.K) && a.dtype >= CCONV_TYPE_BF16 &&
          a.dtype <= CCONV_TYPE_FP32 && a.reserved == 0 && double(a.M) * a.N < 1e15 && double(a.M) * a.K < 1e15 &&
@@ -361,38 +406,12 @@ int64_t cconv_residual_norm_backward_workspace(const cconv_residual_norm_args* a
 }
 
 int cconv_residual_norm_forward(const cconv_residual_norm_args* args, void* cuda_stream) {
+  return guarded([&]() -> int { return args ? norm_forward(*args, nullptr, nullptr, cuda_stream) : CCONV_EINVAL; });
+}
+
+int cconv_residual_norm_quantize(const cconv_residual_norm_quantize_args* args, void* cuda_stream) {
   return guarded([&]() -> int {
-    if (!args || !norm_sizes_ok(*args)) return CCONV_EINVAL;
-    cconv_residual_norm_args a = *args;
-    const int es = type_bytes(a.dtype);
-    a.resid = same_row(a.resid, a.T, a.D);
-    a.block = same_row(a.block, a.T, a.D);
-    a.gate = same_row(a.gate, gate_rows(a), a.D);
-    a.resid_out = same_row(a.resid_out, a.T, a.D);
-    a.norm_out = same_row(a.norm_out, a.T, a.D);
-    if (!unit(a.resid, a.D) || !unit(a.block, a.D) || !unit(a.gate, a.D) || !unit(a.resid_out, a.D) || !unit(a.norm_out, a.D))
-      return CCONV_EINVAL;
-    if (a.T && a.D && ((!a.block.data && (a.gate.data || a.w_post)) || (!a.norm_out.data && a.w_pre))) return CCONV_EINVAL;
-    Operands o;
-    const int resid = o.in(a.resid, a.T, a.D, es);
-    if (a.block.data) o.in(a.block, a.T, a.D, es);
-    if (a.gate.data) o.in(a.gate, gate_rows(a), a.D, es);
-    if (a.w_post) o.in(a.w_post, a.D, es);
-    if (a.w_pre) o.in(a.w_pre, a.D, es);
-    o.may_be_one(resid, o.out(a.resid_out, a.T, a.D, es));
-    if (a.norm_out.data) o.out(a.norm_out, a.T, a.D, es);
-    if (!o.distinct()) return CCONV_EINVAL;
-    if (!o.writes()) return CCONV_OK;
-    const int sms = block_sm_count();
-    if (sms < 0) return sms;
-    NormParams p = norm_params(a);
-    const int rc = block_status_word(&p.status);
-    if (rc != CCONV_OK) return rc;
-    p.limit_ns = block_wait_limit_ns();
-    return o.run(cuda_stream, sms, [&] {
-      return block_cuda_error(run_norm_forward(p, a.dtype, sms, static_cast<cudaStream_t>(cuda_stream)),
-                              "cconv_residual_norm_forward");
-    });
+    return args ? norm_forward(args->norm, &args->q, &args->q_scale, cuda_stream) : CCONV_EINVAL;
   });
 }
 

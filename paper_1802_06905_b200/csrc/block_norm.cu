@@ -15,399 +15,11 @@
 // each sweep over it.  Measured, 16384 x 4096 bf16 with 8 gates: forward 89.5 us, 6.0 TB/s (4 arrays once: 82 us
 // at the rate of a copy); backward 147 us, 5.5 TB/s (6 arrays: 123 us), 135 of them the first kernel.  One token
 // of 4096 channels: 2.5 us on the device.
-#include <algorithm>
-#include <type_traits>
-
-#include "block.h"
-#include "block_device.cuh"
-#include "block_launch.h"
-#include "block_norm.h"
-#include "host_setup.h"
-#include "ptx_sm100.cuh"
+#include "block_norm.cuh"
+#include "block_norm_forward.cuh"
 
 namespace cconv {
 namespace {
-
-// E elements of type T that are loaded and stored together.
-template <typename T, int E>
-struct Vec;
-template <typename T>
-struct Vec<T, 8> {  // 16-bit types
-  uint4 w;
-  __device__ __forceinline__ void load(const T* p) { w = *reinterpret_cast<const uint4*>(p); }
-  __device__ __forceinline__ void zero() { w = make_uint4(0, 0, 0, 0); }
-  __device__ __forceinline__ void get(float (&f)[8]) const {
-    const float2 a = unpack2<T>(w.x), b = unpack2<T>(w.y), c = unpack2<T>(w.z), d = unpack2<T>(w.w);
-    f[0] = a.x; f[1] = a.y; f[2] = b.x; f[3] = b.y; f[4] = c.x; f[5] = c.y; f[6] = d.x; f[7] = d.y;
-  }
-  static __device__ __forceinline__ void store(T* p, const float (&f)[8]) {
-    *reinterpret_cast<uint4*>(p) = make_uint4(pack2<T>(f[0], f[1]), pack2<T>(f[2], f[3]),
-                                              pack2<T>(f[4], f[5]), pack2<T>(f[6], f[7]));
-  }
-};
-template <>
-struct Vec<float, 4> {
-  float4 w;
-  __device__ __forceinline__ void load(const float* p) { w = *reinterpret_cast<const float4*>(p); }
-  __device__ __forceinline__ void zero() { w = make_float4(0, 0, 0, 0); }
-  __device__ __forceinline__ void get(float (&f)[4]) const { f[0] = w.x; f[1] = w.y; f[2] = w.z; f[3] = w.w; }
-  static __device__ __forceinline__ void store(float* p, const float (&f)[4]) {
-    *reinterpret_cast<float4*>(p) = make_float4(f[0], f[1], f[2], f[3]);
-  }
-};
-template <typename T>
-struct Vec<T, 1> {
-  T w;
-  __device__ __forceinline__ void load(const T* p) { w = *p; }
-  __device__ __forceinline__ void zero() { w = from_f32<T>(0.0f); }
-  __device__ __forceinline__ void get(float (&f)[1]) const { f[0] = to_f32(w); }
-  static __device__ __forceinline__ void store(T* p, const float (&f)[1]) { *p = from_f32<T>(f[0]); }
-};
-
-// Sums of two values over the block, the same in every thread.  `buf` alternates between calls, so
-// that one barrier a call is enough.
-__device__ __forceinline__ float2 block_sum2(float a, float b, float2 (*smem)[32], int& buf) {
-  a = warp_sum(a);
-  b = warp_sum(b);
-  const int warps = blockDim.x >> 5;
-  if (warps == 1) return make_float2(a, b);
-  if ((threadIdx.x & 31) == 0) smem[buf][threadIdx.x >> 5] = make_float2(a, b);
-  __syncthreads();
-  const int lane = threadIdx.x & 31;
-  const float2 v = lane < warps ? smem[buf][lane] : make_float2(0.0f, 0.0f);
-  buf ^= 1;
-  return make_float2(warp_sum(v.x), warp_sum(v.y));
-}
-
-// Block b of the kernels that take neighbouring rows has the rows [T b / nb, T (b+1) / nb).
-__device__ __forceinline__ int64_t first_row(const NormParams& p, int64_t b) {
-  return p.T * b / p.nb;
-}
-
-// A ring in shared memory for rows that begin anywhere: a bulk copy brings the 16-byte pieces that a row lies
-// in, so that its first element lies as far behind the slot's start as in memory behind a multiple of 16.  Pieces
-// that reach out of the whole array (of its first and last row) stay behind; complete() fetches their elements.
-template <typename T, int kArrays>
-struct RowRing {
-  struct Span {
-    uintptr_t row, end, lo, hi;  // of the row; of the pieces that are copied
-  };
-  const T* base[kArrays];  // null: absent
-  int64_t rs[kArrays];
-  int64_t rows_of_all, row0, row1;
-  uint32_t row_bytes, slot, ring0, full0, stages;
-
-  __device__ __forceinline__ Span span(int a, int64_t t) const {
-    Span s;
-    const uintptr_t first = reinterpret_cast<uintptr_t>(base[a]);
-    s.row = first + uintptr_t(t * rs[a]) * sizeof(T);
-    s.end = s.row + row_bytes;
-    s.lo = s.row & ~uintptr_t(15);
-    s.hi = (s.end + 15) & ~uintptr_t(15);
-    if (s.lo < first) s.lo += 16;
-    if (s.hi > first + uintptr_t((rows_of_all - 1) * rs[a]) * sizeof(T) + row_bytes) s.hi -= 16;
-    return s;
-  }
-  __device__ __forceinline__ void copy(int64_t t) const {  // one thread
-    const uint32_t st = uint32_t(t - row0) % stages, bar = full0 + 8 * st, to = ring0 + st * kArrays * slot;
-    uint32_t bytes = 0;
-#pragma unroll
-    for (int a = 0; a < kArrays; ++a) {
-      if (!base[a]) continue;
-      const Span s = span(a, t);
-      bytes += uint32_t(s.hi - s.lo);
-    }
-    mbar_arrive_expect_tx(bar, bytes);
-#pragma unroll
-    for (int a = 0; a < kArrays; ++a) {
-      if (!base[a]) continue;
-      const Span s = span(a, t);
-      bulk_load(to + a * slot + uint32_t(s.lo - (s.row & ~uintptr_t(15))), reinterpret_cast<const void*>(s.lo),
-                uint32_t(s.hi - s.lo), bar);
-    }
-  }
-  __device__ __forceinline__ void begin() const {  // one thread
-    for (uint32_t i = 0; i < stages; ++i) mbar_init(full0 + 8 * i, 1);
-    fence_barrier_init();
-    for (int64_t t = row0; t < row1 && t < row0 + int64_t(stages); ++t) copy(t);
-  }
-  // Array a of row t, which lies in stage st.
-  __device__ __forceinline__ T* row(uint8_t* ring, int a, uint32_t st, int64_t t) const {
-    const uintptr_t at = reinterpret_cast<uintptr_t>(base[a] + t * rs[a]);
-    return reinterpret_cast<T*>(ring + (st * kArrays + a) * slot + (at & 15));
-  }
-  // All threads, once the copies of row t have landed.
-  __device__ __forceinline__ void complete(uint8_t* ring, uint32_t st, int64_t t) const {
-    if (t != 0 && t != rows_of_all - 1) return;
-#pragma unroll
-    for (int a = 0; a < kArrays; ++a) {
-      if (!base[a]) continue;
-      const Span s = span(a, t);
-      const uint32_t n = row_bytes / sizeof(T), head = s.lo > s.row ? uint32_t(s.lo - s.row) / sizeof(T) : 0,
-                     tail = s.end > s.hi ? uint32_t(s.end - s.hi) / sizeof(T) : 0;
-      if (threadIdx.x < head) row(ring, a, st, t)[threadIdx.x] = base[a][t * rs[a] + threadIdx.x];
-      if (threadIdx.x < tail) row(ring, a, st, t)[n - 1 - threadIdx.x] = base[a][t * rs[a] + n - 1 - threadIdx.x];
-    }
-    fence_proxy_async_smem();  // the next copy into the slot comes after
-    __syncthreads();
-  }
-};
-
-// Rows of which a thread takes the elements v nt + tid.  kThreads: the threads of a block, if known when compiled;
-// a row then has more than kThreads NV 2/3 elements (NV = 12 and 16), so that most need no comparison.
-template <int NV, int kThreads>
-struct Across {
-  static constexpr int kSure = kThreads && NV > 8 ? NV - 4 : 0;  // elements that every thread has
-  static __device__ __forceinline__ int nt() { return kThreads ? kThreads : blockDim.x; }
-  static __device__ __forceinline__ int column(int v) { return v * nt() + int(threadIdx.x); }
-  static __device__ __forceinline__ bool inside(int v, int D) { return v < kSure || column(v) < D; }
-};
-// Elements of a row (`otherwise` where it ends, or where there is none): loads without conditions, so that all are on
-// their way together.  kSpare: memory goes on behind the row.
-template <int kThreads, bool kSpare, typename T, int NV>
-__device__ __forceinline__ void load_across(float (&f)[NV], const T* from, int D, float otherwise) {
-  using A = Across<NV, kThreads>;
-  if (from) {
-    T raw[NV];
-#pragma unroll
-    for (int v = 0; v < NV; ++v) raw[v] = from[kSpare || v < A::kSure ? A::column(v) : min(A::column(v), D - 1)];
-#pragma unroll
-    for (int v = 0; v < NV; ++v) f[v] = A::inside(v, D) ? to_f32(raw[v]) : otherwise;
-  } else {
-#pragma unroll
-    for (int v = 0; v < NV; ++v) f[v] = otherwise;
-  }
-}
-
-// ---- forward -----------------------------------------------------------------------------------
-// A block a row (and the row gridDim.x further on, ...): few rows, whose latency counts, or rows that are not
-// wide.  Everything that a row needs is asked for before its first reduction (one row of 4096: 2.5 us).
-template <typename T, int E, int NV>
-__global__ void __launch_bounds__(1024) cconv_residual_norm_kernel(const NormParams p) {
-  __shared__ float2 smem[2][32];
-  start_in_order();
-  using V = Vec<T, E>;
-  const T* resid = static_cast<const T*>(p.resid);  // may be resid_out
-  const T* __restrict__ block = static_cast<const T*>(p.block);
-  const T* __restrict__ gate = static_cast<const T*>(p.gate);
-  const T* __restrict__ w_post = static_cast<const T*>(p.w_post);
-  const T* __restrict__ w_pre = static_cast<const T*>(p.w_pre);
-  T* resid_out = static_cast<T*>(p.resid_out);
-  T* norm_out = static_cast<T*>(p.norm_out);
-  const int nt = blockDim.x, tid = threadIdx.x;
-  const float inv_d = 1.0f / float(p.D);
-  int buf = 0;
-  V vpost[NV], vpre[NV];
-  auto fetch = [&](V& v, const T* from, int c) {
-    v.zero();
-    if (from && c < p.D) v.load(from + c);
-  };
-#pragma unroll
-  for (int v = 0; v < NV; ++v) {
-    fetch(vpost[v], w_post, (v * nt + tid) * E);
-    fetch(vpre[v], w_pre, (v * nt + tid) * E);
-  }
-  for (int64_t t = blockIdx.x; t < p.T; t += gridDim.x) {
-    const T* row_r = resid + t * p.resid_rs;
-    const T* row_y = block ? block + t * p.block_rs : nullptr;
-    const T* row_g = gate ? gate + (p.rows_per_gate ? t / p.rows_per_gate : 0) * p.gate_rs : nullptr;
-    V r[NV], y[NV], g[NV];
-#pragma unroll
-    for (int v = 0; v < NV; ++v) {
-      const int c = (v * nt + tid) * E;
-      fetch(r[v], row_r, c);
-      fetch(y[v], row_y, c);
-      fetch(g[v], row_g, c);
-    }
-    float rho = 1.0f;
-    if (block && w_post) {
-      float ss = 0.0f;
-#pragma unroll
-      for (int v = 0; v < NV; ++v) {
-        float f[E];
-        y[v].get(f);
-#pragma unroll
-        for (int i = 0; i < E; ++i) ss += f[i] * f[i];
-      }
-      rho = rsqrtf(block_sum2(ss, 0.0f, smem, buf).x * inv_d + p.eps);
-    }
-    float o[NV][E], ss = 0.0f;
-#pragma unroll
-    for (int v = 0; v < NV; ++v) {
-      const int c = (v * nt + tid) * E;
-      float f[E];
-      r[v].get(o[v]);
-      y[v].get(f);
-      if (w_post) {
-        float w[E];
-        vpost[v].get(w);
-#pragma unroll
-        for (int i = 0; i < E; ++i) f[i] *= rho * w[i];
-      }
-      if (gate) {
-        float w[E];
-        g[v].get(w);
-#pragma unroll
-        for (int i = 0; i < E; ++i) f[i] *= w[i];
-      }
-#pragma unroll
-      for (int i = 0; i < E; ++i) {
-        o[v][i] = p.scale * o[v][i] + f[i];
-        ss += o[v][i] * o[v][i];
-      }
-      if (c < p.D) V::store(resid_out + t * p.resid_out_rs + c, o[v]);
-    }
-    if (!norm_out) continue;
-    rho = rsqrtf(block_sum2(ss, 0.0f, smem, buf).x * inv_d + p.eps);
-#pragma unroll
-    for (int v = 0; v < NV; ++v) {
-      const int c = (v * nt + tid) * E;
-      float w[E];
-      vpre[v].get(w);
-#pragma unroll
-      for (int i = 0; i < E; ++i) o[v][i] *= w_pre ? rho * w[i] : rho;
-      if (c < p.D) V::store(norm_out + t * p.norm_out_rs + c, o[v]);
-    }
-  }
-}
-
-// Rows too long for registers: the row is read again in each of the three sweeps (from L2, which sets the pace:
-// nothing of a row is kept on chip but its sums, so that any length works).
-template <typename T>
-__global__ void __launch_bounds__(1024) cconv_residual_norm_long_kernel(const NormParams p) {
-  __shared__ float2 smem[2][32];
-  start_in_order();
-  const T* resid = static_cast<const T*>(p.resid);
-  const T* block = static_cast<const T*>(p.block);
-  const T* gate = static_cast<const T*>(p.gate);
-  const T* w_post = static_cast<const T*>(p.w_post);
-  const T* w_pre = static_cast<const T*>(p.w_pre);
-  T* resid_out = static_cast<T*>(p.resid_out);
-  T* norm_out = static_cast<T*>(p.norm_out);
-  const float inv_d = 1.0f / float(p.D);
-  int buf = 0;
-  for (int64_t t = blockIdx.x; t < p.T; t += gridDim.x) {
-    const T* r = resid + t * p.resid_rs;
-    const T* y = block ? block + t * p.block_rs : nullptr;
-    const T* g = gate ? gate + (p.rows_per_gate ? t / p.rows_per_gate : 0) * p.gate_rs : nullptr;
-    float rho_y = 1.0f;
-    if (y && w_post) {
-      float ss = 0.0f;
-      for (int c = threadIdx.x; c < p.D; c += blockDim.x) {
-        const float f = to_f32(y[c]);
-        ss += f * f;
-      }
-      rho_y = rsqrtf(block_sum2(ss, 0.0f, smem, buf).x * inv_d + p.eps);
-    }
-    auto out = [&](int c) {
-      float o = p.scale * to_f32(r[c]);
-      if (y) {
-        float n = to_f32(y[c]);
-        if (w_post) n *= rho_y * to_f32(w_post[c]);
-        if (g) n *= to_f32(g[c]);
-        o += n;
-      }
-      return o;
-    };
-    float rho_r = 1.0f;
-    if (norm_out) {
-      float ss = 0.0f;
-      for (int c = threadIdx.x; c < p.D; c += blockDim.x) {
-        const float o = out(c);
-        ss += o * o;
-      }
-      rho_r = rsqrtf(block_sum2(ss, 0.0f, smem, buf).x * inv_d + p.eps);
-    }
-    for (int c = threadIdx.x; c < p.D; c += blockDim.x) {
-      const float o = out(c);
-      resid_out[t * p.resid_out_rs + c] = from_f32<T>(o);
-      if (norm_out) norm_out[t * p.norm_out_rs + c] = from_f32<T>(w_pre ? o * rho_r * to_f32(w_pre[c]) : o * rho_r);
-    }
-  }
-}
-
-// Many rows that are not wide, through the ring above (16384 x 4095 bf16: 131 us, 224 with a block size known at
-// the launch; with a block a row and everything from global memory 516 us).
-template <typename T, int NV, int kThreads>
-__global__ void __launch_bounds__(kThreads) cconv_residual_norm_narrow_kernel(const NormParams p) {
-  extern __shared__ __align__(128) uint8_t ring[];
-  __shared__ float2 smem[2][32];
-  __shared__ __align__(8) uint64_t full[8];
-  __shared__ int abort_flag;
-  start_in_order();
-  const T* block = static_cast<const T*>(p.block);
-  const T* __restrict__ gate = static_cast<const T*>(p.gate);
-  const T* __restrict__ w_post = static_cast<const T*>(p.w_post);
-  const T* __restrict__ w_pre = static_cast<const T*>(p.w_pre);
-  T* resid_out = static_cast<T*>(p.resid_out);
-  T* norm_out = static_cast<T*>(p.norm_out);
-  using A = Across<NV, kThreads>;
-  const int tid = threadIdx.x;
-  const float inv_d = 1.0f / float(p.D);
-  const int64_t row0 = first_row(p, blockIdx.x), row1 = first_row(p, blockIdx.x + 1);
-  const int64_t per = p.rows_per_gate ? p.rows_per_gate : p.T;
-  const RowRing<T, 2> rows = {{static_cast<const T*>(p.resid), block}, {p.resid_rs, p.block_rs}, p.T, row0, row1,
-                              uint32_t(p.D * sizeof(T)), p.ring_slot, smem_u32(ring), smem_u32(full), uint32_t(p.ring_rows)};
-  if (tid == 0) {
-    abort_flag = 0;
-    rows.begin();
-  }
-  __syncthreads();
-  float gw[NV], wpre[NV];  // gate * w_post of the current group; w_pre
-  load_across<kThreads, false>(wpre, w_pre, p.D, 1.0f);
-  int64_t group_end = row0;
-  uint32_t st = 0, phase = 0;
-  int buf = 0;
-  int64_t t = row0;
-  for (; t < row1; ++t) {
-    if (t == group_end || t == row0) {
-      const int64_t group = t / per;
-      group_end = (group + 1) * per;
-      float g[NV];
-      load_across<kThreads, false>(g, gate ? gate + group * p.gate_rs : nullptr, p.D, 1.0f);
-      load_across<kThreads, false>(gw, w_post, p.D, 1.0f);
-#pragma unroll
-      for (int v = 0; v < NV; ++v) gw[v] *= g[v];
-    }
-    const bool ok = mbar_wait(rows.full0 + 8 * st, phase, &abort_flag, p.status, kStatProducerWait, p.limit_ns);
-    // every thread is past the row before: its place in the ring is free
-    if (!__syncthreads_and(ok)) break;
-    if (tid == 0 && t > row0 && t - 1 + p.ring_rows < row1) rows.copy(t - 1 + p.ring_rows);
-    rows.complete(ring, st, t);
-    const T* row_r = rows.row(ring, 0, st, t);
-    const T* row_y = block ? rows.row(ring, 1, st, t) : nullptr;
-    if (++st == uint32_t(p.ring_rows)) st = 0, phase ^= 1;
-    float rho = 1.0f, ss = 0.0f;
-    float o[NV];
-    load_across<kThreads, true>(o, row_y, p.D, 0.0f);
-    if (block && w_post) {
-#pragma unroll
-      for (int v = 0; v < NV; ++v) ss += o[v] * o[v];
-      rho = rsqrtf(block_sum2(ss, 0.0f, smem, buf).x * inv_d + p.eps);
-      ss = 0.0f;
-    }
-    float r[NV];
-    load_across<kThreads, true>(r, row_r, p.D, 0.0f);
-    T* to = resid_out + t * p.resid_out_rs;
-#pragma unroll
-    for (int v = 0; v < NV; ++v) {
-      o[v] = p.scale * r[v] + o[v] * (rho * gw[v]);
-      ss += o[v] * o[v];
-      if (A::inside(v, p.D)) to[A::column(v)] = from_f32<T>(o[v]);
-    }
-    if (!norm_out) continue;
-    rho = rsqrtf(block_sum2(ss, 0.0f, smem, buf).x * inv_d + p.eps);
-    to = norm_out + t * p.norm_out_rs;
-#pragma unroll
-    for (int v = 0; v < NV; ++v)
-      if (A::inside(v, p.D)) to[A::column(v)] = from_f32<T>(o[v] * (rho * wpre[v]));
-  }
-  if (t < row1) {  // a copy did not come in time: let those on their way land
-    const uint64_t t0 = globaltimer_ns();
-    while (globaltimer_ns() - t0 < 200000) {
-    }
-  }
-}
 
 // ---- backward ----------------------------------------------------------------------------------
 // A block takes its rows in order and keeps its share of the column sums
@@ -617,46 +229,6 @@ __global__ void __launch_bounds__(kThreads ? kThreads : 512, 512 / (kThreads ? k
     const int c = A::column(v);
     if (A::inside(v, D)) part[c] = s_pre[v];
   }
-}
-
-__device__ __forceinline__ float sum_of(uint64_t v) {
-  const float2 f = halves_of(v);
-  return f.x + f.y;
-}
-// 16 bytes of elements as pairs, and back.
-template <typename T>
-__device__ __forceinline__ void get_pairs(const void* from, uint64_t (&f)[16 / sizeof(T) / 2]) {
-  const uint4 w = *static_cast<const uint4*>(from);
-  const uint32_t a[4] = {w.x, w.y, w.z, w.w};
-  if constexpr (sizeof(T) == 4) {
-    f[0] = pair_of(__uint_as_float(a[0]), __uint_as_float(a[1]));
-    f[1] = pair_of(__uint_as_float(a[2]), __uint_as_float(a[3]));
-  } else {
-#pragma unroll
-    for (int i = 0; i < 4; ++i) {
-      const float2 v = unpack2<T>(a[i]);
-      f[i] = pair_of(v.x, v.y);
-    }
-  }
-}
-template <typename T>
-__device__ __forceinline__ void put_pairs(void* to, const uint64_t (&f)[16 / sizeof(T) / 2]) {
-  uint32_t a[4];
-  if constexpr (sizeof(T) == 4) {
-#pragma unroll
-    for (int i = 0; i < 2; ++i) {
-      const float2 v = halves_of(f[i]);
-      a[2 * i] = __float_as_uint(v.x);
-      a[2 * i + 1] = __float_as_uint(v.y);
-    }
-  } else {
-#pragma unroll
-    for (int i = 0; i < 4; ++i) {
-      const float2 v = halves_of(f[i]);
-      a[i] = pack2<T>(v.x, v.y);
-    }
-  }
-  *static_cast<uint4*>(to) = make_uint4(a[0], a[1], a[2], a[3]);
 }
 
 // Wide rows: a ring in shared memory that bulk copies fill several rows ahead, so that no registers are
@@ -882,122 +454,6 @@ __global__ void __launch_bounds__(512) cconv_residual_norm_backward_ring_kernel(
   }
 }
 
-// The forward direction of many wide rows, the same way: r and y through a ring, pairs of operations, the
-// weights in registers.
-template <typename T, int NV, bool kAll>
-__global__ void __launch_bounds__(512) cconv_residual_norm_ring_kernel(const NormParams p) {
-  extern __shared__ __align__(128) uint8_t ring[];
-  __shared__ float2 smem[2][32];
-  __shared__ __align__(8) uint64_t full[8];
-  __shared__ int abort_flag;
-  start_in_order();
-  constexpr int E = 16 / int(sizeof(T)), P = E / 2;
-  const T* resid = static_cast<const T*>(p.resid);  // may be resid_out
-  const T* block = static_cast<const T*>(p.block);
-  const T* __restrict__ gate = static_cast<const T*>(p.gate);
-  const T* __restrict__ w_post = static_cast<const T*>(p.w_post);
-  const T* __restrict__ w_pre = static_cast<const T*>(p.w_pre);
-  T* resid_out = static_cast<T*>(p.resid_out);
-  T* norm_out = static_cast<T*>(p.norm_out);
-  const int nt = blockDim.x, tid = threadIdx.x;
-  const bool has_block = kAll || block, has_post = kAll || w_post, has_norm = kAll || norm_out;
-  auto inside = [&](int v) { return kAll || (v * nt + tid) * E < p.D; };
-  const float inv_d = 1.0f / float(p.D);
-  const int64_t row0 = first_row(p, blockIdx.x), row1 = first_row(p, blockIdx.x + 1);
-  const int64_t per = p.rows_per_gate ? p.rows_per_gate : p.T;
-  const uint32_t row_bytes = uint32_t(p.D) * sizeof(T), ring0 = smem_u32(ring), full0 = smem_u32(full);
-  const uint64_t one = pair_of(1.0f, 1.0f), scale = pair_of(p.scale, p.scale);
-  int buf = 0;
-  auto get = [&](bool given, const T* from, int v, uint64_t (&f)[P], uint64_t otherwise) {
-    if (given && inside(v)) {
-      get_pairs<T>(from + (v * nt + tid) * E, f);
-    } else {
-#pragma unroll
-      for (int i = 0; i < P; ++i) f[i] = otherwise;
-    }
-  };
-  auto copy_row = [&](int64_t t) {
-    const uint32_t st = uint32_t(t - row0) % uint32_t(p.ring_rows), bar = full0 + 8 * st;
-    const uint32_t to = ring0 + st * 2 * row_bytes;
-    mbar_arrive_expect_tx(bar, row_bytes * (has_block ? 2u : 1u));
-    bulk_load(to, resid + t * p.resid_rs, row_bytes, bar);
-    if (has_block) bulk_load(to + row_bytes, block + t * p.block_rs, row_bytes, bar);
-  };
-  if (tid == 0) {
-    abort_flag = 0;
-    for (int i = 0; i < p.ring_rows; ++i) mbar_init(full0 + 8 * i, 1);
-    fence_barrier_init();
-    for (int64_t t = row0; t < row1 && t < row0 + p.ring_rows; ++t) copy_row(t);
-  }
-  __syncthreads();
-  uint64_t gw[NV][P], wpre[NV][P];  // gate * w_post of the current group; w_pre
-#pragma unroll
-  for (int v = 0; v < NV; ++v) get(kAll || w_pre, w_pre, v, wpre[v], one);
-  int64_t group_end = row0;
-  uint32_t st = 0, phase = 0;
-  int64_t t = row0;
-  for (; t < row1; ++t) {
-    if (t == group_end || t == row0) {
-      const int64_t group = t / per;
-      group_end = (group + 1) * per;
-#pragma unroll
-      for (int v = 0; v < NV; ++v) {
-        uint64_t fg[P];
-        get(kAll || gate, gate + group * p.gate_rs, v, fg, one);
-        get(has_post, w_post, v, gw[v], one);
-#pragma unroll
-        for (int i = 0; i < P; ++i) gw[v][i] = mul2(gw[v][i], fg[i]);
-      }
-    }
-    const bool ok = mbar_wait(full0 + 8 * st, phase, &abort_flag, p.status, kStatProducerWait, p.limit_ns);
-    // every thread is past the row before: its place in the ring is free
-    if (!__syncthreads_and(ok)) break;
-    if (tid == 0 && t > row0 && t - 1 + p.ring_rows < row1) copy_row(t - 1 + p.ring_rows);
-    const T* row_r = reinterpret_cast<const T*>(ring + st * 2 * row_bytes);
-    const T* row_y = row_r + p.D;
-    if (++st == uint32_t(p.ring_rows)) st = 0, phase ^= 1;
-    uint64_t o[NV][P], sum = 0;
-    float rho1 = 1.0f;
-    if (has_block) {
-#pragma unroll
-      for (int v = 0; v < NV; ++v) {
-        get(true, row_y, v, o[v], 0);
-#pragma unroll
-        for (int i = 0; i < P; ++i) sum = fma2(o[v][i], o[v][i], sum);
-      }
-      if (has_post) rho1 = rsqrtf(block_sum2(sum_of(sum), 0.0f, smem, buf).x * inv_d + p.eps);
-    }
-    uint64_t rho = pair_of(rho1, rho1);
-    sum = 0;
-#pragma unroll
-    for (int v = 0; v < NV; ++v) {
-      uint64_t r[P];
-      get(true, row_r, v, r, 0);
-#pragma unroll
-      for (int i = 0; i < P; ++i) {
-        r[i] = mul2(scale, r[i]);
-        o[v][i] = has_block ? fma2(o[v][i], mul2(rho, gw[v][i]), r[i]) : r[i];
-        sum = fma2(o[v][i], o[v][i], sum);
-      }
-      if (inside(v)) put_pairs<T>(resid_out + t * p.resid_out_rs + (v * nt + tid) * E, o[v]);
-    }
-    if (!has_norm) continue;
-    rho1 = rsqrtf(block_sum2(sum_of(sum), 0.0f, smem, buf).x * inv_d + p.eps);
-    rho = pair_of(rho1, rho1);
-#pragma unroll
-    for (int v = 0; v < NV; ++v) {
-#pragma unroll
-      for (int i = 0; i < P; ++i) o[v][i] = mul2(o[v][i], mul2(rho, wpre[v][i]));
-      if (inside(v)) put_pairs<T>(norm_out + t * p.norm_out_rs + (v * nt + tid) * E, o[v]);
-    }
-  }
-  if (t < row1) {  // a copy did not come in time: let those on their way land
-    const uint64_t t0 = globaltimer_ns();
-    while (globaltimer_ns() - t0 < 200000) {
-    }
-  }
-}
-
 // Rows too long for registers: column sums live in the partial table (5 rows a block here; the fifth
 // holds the sums of a gate group that is complete within the block until it is written).
 template <typename T>
@@ -1149,173 +605,6 @@ __global__ void __launch_bounds__(512) cconv_residual_norm_sums_kernel(const Nor
   }
 }
 
-// Shared memory of an SM for the rings of the backward blocks on it, and what a block has besides (its own
-// few KB, and the sums of dw_post).
-constexpr int64_t kRingSmem = 216 * 1024, kRingOwn = 2048;
-int64_t ring_rows(int64_t D, int es, int64_t blocks) {
-  return (kRingSmem / blocks / 1024 * 1024 - kRingOwn - 4 * D) / (4 * D * es);
-}
-// Backward blocks that share an SM: about 512 threads of 16 elements, so that one block's row covers the
-// other's reductions while the table of partial sums stays small against the arrays (at D = 4096, bf16:
-// two blocks of 256 threads; with 8 elements a thread, two blocks of 512, it took 1.4 times as long); fewer where a
-// ring of each would not hold two rows.
-int64_t blocks_an_sm(int64_t D, int es) {
-  const int64_t threads = std::max<int64_t>(32, std::min<int64_t>(512, round_up64(cdiv64(D, 16), 32)));
-  int64_t n = std::min<int64_t>(16, 512 / threads);
-  while (n > 1 && ring_rows(D, es, n) < 2) --n;
-  return n;
-}
-
-// Threads a block and accesses a thread for rows of D elements taken E at a time: at most `held`
-// elements a thread, whole warps, one access a thread as long as that leaves `few` threads or fewer.
-struct Shape {
-  int threads, nv;
-};
-Shape shape_of(int64_t D, int E, int held, int most, int few = 256) {
-  const int64_t acc = cdiv64(D, E);
-  int nv = 1;
-  while (nv * E < held && acc > int64_t(nv) * few) nv *= 2;
-  const int64_t threads = round_up64(cdiv64(acc, nv), 32);
-  return threads <= most ? Shape{int(threads), nv} : Shape{0, 0};
-}
-
-bool wide(const NormParams& p, int es, bool backward) {
-  const int E = 16 / es;
-  if (p.D % E) return false;
-  uintptr_t all = 0;
-  int64_t strides = 0;
-  auto add = [&](const void* q, int64_t rs) {
-    if (!q) return;
-    all |= reinterpret_cast<uintptr_t>(q);
-    strides |= rs * es;
-  };
-  add(p.block, p.block_rs);
-  add(p.gate, p.gate_rs);
-  add(p.w_post, 0);
-  add(p.w_pre, 0);
-  add(p.resid_out, p.resid_out_rs);
-  if (backward) {
-    add(p.dresid_out, p.dresid_out_rs);
-    add(p.dnorm_out, p.dnorm_out_rs);
-    add(p.dresid, p.dresid_rs);
-    add(p.dblock, p.dblock_rs);
-    add(p.dgate, p.dgate_rs);
-  } else {
-    add(p.resid, p.resid_rs);
-    add(p.norm_out, p.norm_out_rs);
-  }
-  return ((all | uintptr_t(strides)) & 15u) == 0;
-}
-
-template <typename F>
-cudaError_t allow_ring(F f, bool (&ready)[64]) {
-  int dev = 0;
-  cudaError_t e = cudaGetDevice(&dev);
-  if (e != cudaSuccess) return e;
-  if (!__atomic_load_n(&ready[dev & 63], __ATOMIC_ACQUIRE)) {
-    e = cudaFuncSetAttribute(f, cudaFuncAttributeMaxDynamicSharedMemorySize, int(kRingSmem));
-    if (e != cudaSuccess) return e;
-    __atomic_store_n(&ready[dev & 63], true, __ATOMIC_RELEASE);
-  }
-  return cudaSuccess;
-}
-
-template <typename T, int E, int NV>
-cudaError_t launch_forward_nv(const NormParams& p, int threads, int64_t grid, cudaStream_t s) {
-  return launch(cconv_residual_norm_kernel<T, E, NV>, dim3(unsigned(grid)), threads, 0, 1, s, p);
-}
-
-template <typename T, int NV, bool kAll>
-cudaError_t launch_forward_ring(const NormParams& p, int threads, cudaStream_t s) {
-  auto f = cconv_residual_norm_ring_kernel<T, NV, kAll>;
-  static bool ready[64] = {};
-  const cudaError_t e = allow_ring(f, ready);
-  if (e != cudaSuccess) return e;
-  return launch(f, dim3(unsigned(p.nb)), threads, size_t(p.D) * p.ring_rows * 2 * sizeof(T), 1, s, p);
-}
-
-// Shared memory of a row of one array in the ring of rows that begin anywhere.
-int64_t narrow_slot(int64_t row_bytes) { return round_up64(row_bytes, 16) + 16; }
-// Threads and elements a thread there: 64 to 512 threads, 12 or 16 elements (8 where D is at most 512).
-Shape narrow_shape(int64_t D) {
-  if (D <= 512) return {64, 8};
-  for (int threads = 64; threads <= 512; threads *= 2) {
-    if (D <= threads * 12) return {threads, 12};
-    if (D <= threads * 16) return {threads, 16};
-  }
-  return {0, 0};
-}
-// Calls f with the shape's numbers as constants: f(elements, threads).
-template <typename F>
-cudaError_t with_narrow_shape(const Shape& n, F f) {
-  auto elements = [&](auto threads) {
-    if (n.nv == 12) return f(std::integral_constant<int, 12>(), threads);
-    return f(std::integral_constant<int, 16>(), threads);
-  };
-  if (n.nv == 8) return f(std::integral_constant<int, 8>(), std::integral_constant<int, 64>());
-  if (n.threads == 64) return elements(std::integral_constant<int, 64>());
-  if (n.threads == 128) return elements(std::integral_constant<int, 128>());
-  if (n.threads == 256) return elements(std::integral_constant<int, 256>());
-  return elements(std::integral_constant<int, 512>());
-}
-// Whether the rows of an array can go through it: none but the first and last touch its ends.
-bool narrow_fits(const void* q, int64_t rs, const NormParams& p, int es) {
-  return !q || (rs * es >= 16 && p.D * es >= 64);
-}
-
-template <typename T>
-cudaError_t launch_forward(NormParams p, int sms, cudaStream_t s) {
-  constexpr int kWide = 16 / int(sizeof(T)), kMost = 16 / kWide;
-  const bool w = wide(p, sizeof(T), false);
-  const Shape sh = shape_of(p.D, w ? kWide : 1, 16, 1024);
-  const int threads = sh.threads ? sh.threads : 1024;
-  // Many wide rows: blocks of about 1024 threads an SM go through rows of their own, fewer where their rings
-  // would not hold two rows each.
-  int64_t an_sm = std::max(1, std::min(16, 1024 / threads));
-  auto rows = [&](int64_t blocks) { return (kRingSmem / blocks / 1024 * 1024 - kRingOwn) / (2 * p.D * int64_t(sizeof(T))); };
-  while (an_sm > 1 && rows(an_sm) < 2) --an_sm;
-  if (w && sh.threads && sh.threads <= 512 && rows(an_sm) >= 2 && p.T >= 4 * an_sm * sms) {
-    p.nb = int(an_sm * sms);
-    p.ring_rows = int(std::min<int64_t>(8, rows(an_sm)));
-    const bool all = p.block && p.w_post && p.w_pre && p.gate && p.norm_out && p.D == int64_t(sh.threads) * sh.nv * kWide;
-    if (sh.nv == 1) return all ? launch_forward_ring<T, 1, true>(p, threads, s) : launch_forward_ring<T, 1, false>(p, threads, s);
-    if (sh.nv == 2) return all ? launch_forward_ring<T, 2, true>(p, threads, s) : launch_forward_ring<T, 2, false>(p, threads, s);
-    return all ? launch_forward_ring<T, kMost, true>(p, threads, s) : launch_forward_ring<T, kMost, false>(p, threads, s);
-  }
-  const int64_t grid = std::min<int64_t>(p.T, int64_t(sms) * std::max(1, std::min(32, 1024 / threads)));
-  if (!sh.threads) return launch(cconv_residual_norm_long_kernel<T>, dim3(unsigned(grid)), threads, 0, 1, s, p);
-  if (w) {
-    if (sh.nv == 1) return launch_forward_nv<T, kWide, 1>(p, threads, grid, s);
-    if (sh.nv == 2) return launch_forward_nv<T, kWide, 2>(p, threads, grid, s);
-    return launch_forward_nv<T, kWide, kMost>(p, threads, grid, s);
-  }
-  // many rows that are not wide: the same with their own ring
-  const Shape n = narrow_shape(p.D);
-  if (n.threads && narrow_fits(p.resid, p.resid_rs, p, sizeof(T)) && narrow_fits(p.block, p.block_rs, p, sizeof(T))) {
-    const int64_t es = sizeof(T), slot = narrow_slot(p.D * es), spare = n.threads * n.nv * es;
-    an_sm = 1024 / n.threads;
-    auto narrow_rows = [&](int64_t blocks) { return (kRingSmem / blocks / 1024 * 1024 - kRingOwn - spare) / (2 * slot); };
-    while (an_sm > 1 && narrow_rows(an_sm) < 2) --an_sm;
-    if (narrow_rows(an_sm) >= 2 && p.T >= 4 * an_sm * sms) {
-      p.nb = int(an_sm * sms);
-      p.ring_rows = int(std::min<int64_t>(8, narrow_rows(an_sm)));
-      p.ring_slot = uint32_t(slot);
-      return with_narrow_shape(n, [&](auto nv, auto nt) {
-        auto f = cconv_residual_norm_narrow_kernel<T, decltype(nv)::value, decltype(nt)::value>;
-        static bool ready[64] = {};
-        const cudaError_t e = allow_ring(f, ready);
-        if (e != cudaSuccess) return e;
-        return launch(f, dim3(unsigned(p.nb)), nt, size_t(p.ring_rows) * 2 * slot + spare, 1, s, p);
-      });
-    }
-  }
-  if (sh.nv == 1) return launch_forward_nv<T, 1, 1>(p, threads, grid, s);
-  if (sh.nv == 2) return launch_forward_nv<T, 1, 2>(p, threads, grid, s);
-  if (sh.nv == 4) return launch_forward_nv<T, 1, 4>(p, threads, grid, s);
-  if (sh.nv == 8) return launch_forward_nv<T, 1, 8>(p, threads, grid, s);
-  return launch_forward_nv<T, 1, 16>(p, threads, grid, s);
-}
-
 template <typename T, int NV, bool kAll, bool kPost>
 cudaError_t launch_ring_as(NormParams p, int threads, cudaStream_t s) {
   auto f = cconv_residual_norm_backward_ring_kernel<T, NV, kAll, kPost>;
@@ -1440,9 +729,9 @@ int norm_backward_blocks(int64_t T, int64_t D, int es, int sms) {
 }
 
 cudaError_t run_norm_forward(const NormParams& p, int dtype, int sms, cudaStream_t s) {
-  if (dtype == CCONV_TYPE_BF16) return launch_forward<__nv_bfloat16>(p, sms, s);
-  if (dtype == CCONV_TYPE_FP16) return launch_forward<__half>(p, sms, s);
-  return launch_forward<float>(p, sms, s);
+  if (dtype == CCONV_TYPE_BF16) return launch_forward<__nv_bfloat16, false>(p, sms, s);
+  if (dtype == CCONV_TYPE_FP16) return launch_forward<__half, false>(p, sms, s);
+  return launch_forward<float, false>(p, sms, s);
 }
 
 cudaError_t run_norm_backward(const NormParams& p, int dtype, cudaStream_t s) {

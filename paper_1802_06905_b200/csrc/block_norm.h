@@ -22,11 +22,16 @@ struct NormParams {
   uint32_t ring_slot;  // bytes of a row of one array there, where rows begin anywhere
   int* status;      // where a bounded wait that ran out is noted
   uint64_t limit_ns;
+  uint8_t* q;       // 8-bit results: norm_out's values (before their rounding) over the scale of their 128 channels
+  float* q_scale;
+  int64_t q_rs, q_scale_rs, q_scale_cs;
   float* part;  // backward: [nb][4][D], and [nb][D] more for rows that registers cannot hold
 };
 
 int norm_backward_blocks(int64_t T, int64_t D, int es, int sms);
 cudaError_t run_norm_forward(const NormParams& p, int dtype, int sms, cudaStream_t s);
+// The same with the second norm's result in 8 bits (p.q, p.q_scale; p.norm_out may be there too).
+cudaError_t run_norm_quantize(const NormParams& p, int dtype, int sms, cudaStream_t s);
 cudaError_t run_norm_backward(const NormParams& p, int dtype, cudaStream_t s);
 
 }  // namespace cconv
