@@ -8,6 +8,7 @@
  *                   norm(v) = v / sqrt(mean(v^2) + eps), over the D channels of a token
  *   8-bit product   C[m,n] = sum_kb (sa[m,kb] sb[n/128,kb]) sum_{k in block kb} A[m,k] B[n,k]
  *   quantisation    8-bit values (e4m3) and a scale for each 1 x 128 or 128 x 128 block
+ *   4-bit product   C[m,n] = sum_g s[n,g] sum_{k in group g} (q[n,k] - z[n,g]) X[m,k], and the quantiser of its weights
  *   norm in 8 bits  the residual norm whose x is written as 8-bit values and scales
  *
  * Matrices are given by the address of element (0,0) and two strides in elements.  Strides of inputs
@@ -160,6 +161,49 @@ typedef struct {
 } cconv_quantize_args;
 
 int cconv_quantize_blocks(const cconv_quantize_args* args, void* cuda_stream);
+
+/* ---- product with 4-bit weights and a scale for each group of a row --------------------------------
+ *   C[m,n] = sum_g scale[n,g] sum_{k in group g} (q[n,k] - zero[n,g]) X[m,k],   group g: k / group = g
+ * Element 2j of a row of q is the low half of byte j, element 2j + 1 its high half; what lies behind K in the last
+ * byte does not matter.  A token that holds an infinity or a NaN gives infinities or NaN.
+ * Up to 64 tokens, sums are of q and X as they are, in fp32, and scaled in fp32; with more, the weights
+ * scale (q - zero) are rounded to `dtype` first, as operands of the tensor cores. */
+typedef struct {
+  int64_t M, N, K;
+  int32_t dtype;       /* CCONV_TYPE_BF16 or _FP16, of X and C */
+  int32_t scale_dtype; /* CCONV_TYPE_*, of the scales */
+  int32_t group;       /* 32, 64 or 128 */
+  int32_t reserved;    /* 0 */
+  cconv_matrix x;      /* [M][K] */
+  cconv_matrix q;      /* [N][ceil(K/2)] bytes */
+  cconv_matrix scale;  /* [N][ceil(K/group)] */
+  cconv_matrix zero;   /* [N][ceil(K/group)] bytes, 0 to 15 in their low halves; absent: 8 */
+  cconv_matrix c;      /* out: [M][N] */
+  void* workspace;
+  uint64_t workspace_bytes;
+} cconv_int4_product_args;
+
+int64_t cconv_int4_product_workspace(const cconv_int4_product_args* args);
+int cconv_int4_product(const cconv_int4_product_args* args, void* cuda_stream);
+
+/* Weights in 4 bits, in fp32 up to the last rounding; s' = s rounded to scale_dtype, quotients nearest, ties to even:
+ *   zero absent  s = max|w| / 7 over the group,          q = 8 + clamp(rint(w / s'), -8, 7)
+ *   zero given   s = (max(w, 0) - min(w, 0)) / 15,       zero = clamp(rint(-min(w, 0) / s'), 0, 15),
+ *                                                        q = clamp(rint(w / s') + zero, 0, 15)
+ * Where s' is 0 or not finite, q and zero are 8 throughout; a group that holds an infinity or a NaN has scale NaN.
+ * The half byte behind an odd K is 0. */
+typedef struct {
+  int64_t N, K;
+  int32_t dtype; /* CCONV_TYPE_*, of w */
+  int32_t scale_dtype, group;
+  int32_t reserved;   /* 0 */
+  cconv_matrix w;     /* in: [N][K] */
+  cconv_matrix q;     /* out: [N][ceil(K/2)] bytes */
+  cconv_matrix scale; /* out: [N][ceil(K/group)] */
+  cconv_matrix zero;  /* out: [N][ceil(K/group)] bytes; absent: see above */
+} cconv_quantize_groups_args;
+
+int cconv_quantize_groups(const cconv_quantize_groups_args* args, void* cuda_stream);
 
 /* Synchronises `cuda_stream`, reads the status word that the product kernels of the current device
  * share and clears it: CCONV_OK, CCONV_EDEVICE_TIMEOUT (a bounded wait on the device ran out; the

@@ -5,6 +5,8 @@
     residual_norm_quantize                            the same with x in 8 bits and scales
     fp8_product                                       8-bit operands with a scale for each block of 128
     quantize_blocks                                   the 8-bit values and the scales
+    int4_product                                      4-bit weights with a scale for each group of a row
+    quantize_groups                                   those weights, scales and zero points
 
 Argument marshalling only: every step runs in ``libcconv.so``.  Results go to tensors that the caller
 gives.  Calls are asynchronous on ``stream`` (default: the current stream of the operands' device).
@@ -30,7 +32,8 @@ EXPORTS = (
     "cconv_ffn_forward_workspace", "cconv_ffn_backward_workspace", "cconv_ffn_forward", "cconv_ffn_backward",
     "cconv_residual_norm_backward_workspace", "cconv_residual_norm_forward", "cconv_residual_norm_backward",
     "cconv_residual_norm_quantize",
-    "cconv_fp8_product_workspace", "cconv_fp8_product", "cconv_quantize_blocks", "cconv_block_status",
+    "cconv_fp8_product_workspace", "cconv_fp8_product", "cconv_quantize_blocks", "cconv_int4_product_workspace",
+    "cconv_int4_product", "cconv_quantize_groups", "cconv_block_status",
 )
 
 # The argument structures of the C ABI, field for field (P: address, q: 64-bit, i: 32-bit, f: float), without
@@ -40,6 +43,8 @@ _FFN = struct.Struct("qqqii" + _MAT * 12)
 _NORM = struct.Struct("qqiffxxxxq" + _MAT * 3 + "PP" + _MAT * 7 + "PP")
 _FP8 = struct.Struct("qqqii" + _MAT * 5)
 _QUANT = struct.Struct("qqii" + _MAT * 3)
+_INT4 = struct.Struct("qqqiiii" + _MAT * 5)
+_GROUPS = struct.Struct("qqiiii" + _MAT * 4)
 _TWO = struct.Struct(_MAT * 2)  # behind the norm's, in the call with 8-bit results
 _SPACE = struct.Struct("PQ")
 _NO_SPACE = _SPACE.pack(0, 0)
@@ -350,6 +355,64 @@ def quantize_blocks(x, q, scale, block_rows=1, stream=None):
                        *_mat(scale, (-(-T // block_rows), -(-D // 128)), torch.float32, dev, "scale"))
     _call("cconv_quantize_blocks", args, dev, stream)
     return q, scale
+
+
+# ---- 4-bit weights -----------------------------------------------------------------------------------
+
+def _scale_type(scale):
+    ty = _TYPES.get(scale.dtype)
+    if ty is None:
+        raise ValueError(f"scale has type {scale.dtype}; supported: {', '.join(str(d) for d in _TYPES)}")
+    return ty
+
+
+def _group(group):
+    if group not in (32, 64, 128):
+        raise ValueError(f"group must be 32, 64 or 128, got {group}")
+
+
+def _int4_args(x, q, scale, out, zero, group):
+    dtype, dev = _type(x, "x", _HALF_TYPES)
+    M, K = x.shape
+    _group(group)
+    if q.dim() != 2:
+        raise ValueError(f"q must be a matrix, got shape {tuple(q.shape)}")
+    N, groups, u8 = q.shape[0], (K + group - 1) // group, torch.uint8
+    return _INT4.pack(M, N, K, dtype, _scale_type(scale), group, 0, x.data_ptr(), *x.stride(),
+                      *_mat(q, (N, (K + 1) // 2), u8, dev, "q"), *_mat(scale, (N, groups), scale.dtype, dev, "scale"),
+                      *(_NONE if zero is None else _mat(zero, (N, groups), u8, dev, "zero")),
+                      *_mat(out, (M, N), x.dtype, dev, "out")), dev
+
+
+def int4_product_workspace(x, q, scale, out, zero=None, group=128):
+    """cconv_int4_product_workspace: bytes of workspace of the call with these tensors."""
+    args, dev = _int4_args(x, q, scale, out, zero, group)
+    return _need("cconv_int4_product_workspace", args, dev)
+
+
+def int4_product(x, q, scale, out, zero=None, group=128, workspace=None, stream=None):
+    """cconv_int4_product: out[m,n] = sum_g scale[n,g] sum_{k in group g} (q[n,k] - zero[n,g]) x[m,k].
+
+    x [M, K], out [M, N] bf16 or fp16; q [N, ceil(K/2)] uint8, element 2j of a row in the low half of byte j; scale
+    [N, ceil(K/group)] bf16, fp16 or fp32; zero of the same shape, uint8 of 0 to 15 (None: 8 throughout); group 32, 64 or
+    128; any strides.  With more than 64 tokens the weights scale (q - zero) are rounded to x's type."""
+    args, dev = _int4_args(x, q, scale, out, zero, group)
+    _call_with_space("cconv_int4_product", "cconv_int4_product_workspace", args, dev, workspace, stream)
+    return out
+
+
+def quantize_groups(w, q, scale, zero=None, group=128, stream=None):
+    """cconv_quantize_groups: the 4-bit values q [N, ceil(K/2)] (uint8, two a byte) and scales [N, ceil(K/group)]
+    of w [N, K], bf16, fp16 or fp32 each; with ``zero`` (uint8, as scale) a group's range need not be symmetric."""
+    dtype, dev = _type(w, "w")
+    N, K = w.shape
+    _group(group)
+    groups, u8 = (K + group - 1) // group, torch.uint8
+    args = _GROUPS.pack(N, K, dtype, _scale_type(scale), group, 0, w.data_ptr(), *w.stride(),
+                        *_mat(q, (N, (K + 1) // 2), u8, dev, "q"), *_mat(scale, (N, groups), scale.dtype, dev, "scale"),
+                        *(_NONE if zero is None else _mat(zero, (N, groups), u8, dev, "zero")))
+    _call("cconv_quantize_groups", args, dev, stream)
+    return q, scale, zero
 
 
 def status(stream=None):

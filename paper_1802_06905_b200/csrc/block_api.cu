@@ -9,6 +9,7 @@
 #include "block_ffn.h"
 #include "block_fp8.h"
 #include "block_gemm.h"
+#include "block_int4.h"
 #include "block_norm.h"
 #include "block_quant.h"
 #include "host_setup.h"
@@ -327,6 +328,15 @@ bool fp8_sizes_ok(const cconv_fp8_product_args& a) {
          double(a.N) * a.K < 1e15;
 }
 
+bool group_ok(int32_t group) { return group == 32 || group == 64 || group == 128; }
+bool type_ok(int32_t t) { return t >= CCONV_TYPE_BF16 && t <= CCONV_TYPE_FP32; }
+bool int4_sizes_ok(const cconv_int4_product_args& a) {
+  return length_ok(a.M) && length_ok(a.N) && length_ok(a.K) && (a.dtype == CCONV_TYPE_BF16 || a.dtype == CCONV_TYPE_FP16) &&
+         type_ok(a.scale_dtype) && group_ok(a.group) && a.reserved == 0 && double(a.M) * a.N < 1e15 &&
+         double(a.M) * a.K < 1e15 && double(a.N) * a.K < 1e15;
+}
+bool int4_empty(const cconv_int4_product_args& a) { return a.M == 0 || a.N == 0 || a.K == 0; }
+
 bool fp8_empty(const cconv_fp8_product_args& a) { return a.M == 0 || a.N == 0 || a.K == 0; }
 
 }  // namespace
@@ -536,6 +546,62 @@ int cconv_quantize_blocks(const cconv_quantize_args* args, void* cuda_stream) {
     return o.run(cuda_stream, sms, [&] {
       return block_cuda_error(run_quantize(p, a.dtype, a.block_rows, sms, static_cast<cudaStream_t>(cuda_stream)),
                               "cconv_quantize_blocks");
+    });
+  });
+}
+
+int64_t cconv_int4_product_workspace(const cconv_int4_product_args* args) {
+  return guarded([&]() -> int64_t {
+    if (!args || !int4_sizes_ok(*args)) return CCONV_EINVAL;
+    const int sms = block_sm_count();
+    if (sms < 0) return sms;
+    return int4_empty(*args) ? 0 : int4_workspace(*args, sms);
+  });
+}
+
+int cconv_int4_product(const cconv_int4_product_args* args, void* cuda_stream) {
+  return guarded([&]() -> int {
+    if (!args || !int4_sizes_ok(*args)) return CCONV_EINVAL;
+    const cconv_int4_product_args& a = *args;
+    const int64_t groups = cdiv64(a.K, a.group);
+    Operands o;
+    o.in(a.x, a.M, a.K, 2);
+    o.in(a.q, a.N, cdiv64(a.K, 2), 1);
+    o.in(a.scale, a.N, groups, type_bytes(a.scale_dtype));
+    if (a.zero.data) o.in(a.zero, a.N, groups, 1);
+    o.out(a.c, a.M, a.N, 2);
+    if (!o.distinct()) return CCONV_EINVAL;
+    if (!o.writes()) return CCONV_OK;
+    const int sms = block_sm_count();
+    if (sms < 0) return sms;
+    o.workspace(a.workspace, a.workspace_bytes, int4_empty(a) ? 0 : int4_workspace(a, sms));
+    if (!o.distinct()) return CCONV_EINVAL;
+    cudaStream_t s = static_cast<cudaStream_t>(cuda_stream);
+    return o.run(cuda_stream, sms, [&] {
+      return int4_empty(a) ? block_cuda_error(zero_out(a.c, a.M, a.N, 2, s), "cconv_int4_product") : run_int4(a, sms, s);
+    });
+  });
+}
+
+int cconv_quantize_groups(const cconv_quantize_groups_args* args, void* cuda_stream) {
+  return guarded([&]() -> int {
+    if (!args) return CCONV_EINVAL;
+    const cconv_quantize_groups_args& a = *args;
+    if (!length_ok(a.N) || !length_ok(a.K) || !type_ok(a.dtype) || !type_ok(a.scale_dtype) || !group_ok(a.group) ||
+        a.reserved != 0 || double(a.N) * a.K >= 1e15)
+      return CCONV_EINVAL;
+    const int64_t groups = cdiv64(a.K, a.group);
+    Operands o;
+    o.in(a.w, a.N, a.K, type_bytes(a.dtype));
+    o.out(a.q, a.N, cdiv64(a.K, 2), 1);
+    o.out(a.scale, a.N, groups, type_bytes(a.scale_dtype));
+    if (a.zero.data) o.out(a.zero, a.N, groups, 1);
+    if (!o.distinct()) return CCONV_EINVAL;
+    if (!o.writes()) return CCONV_OK;
+    const int sms = block_sm_count();
+    if (sms < 0) return sms;
+    return o.run(cuda_stream, sms, [&] {
+      return block_cuda_error(run_quantize_groups(a, static_cast<cudaStream_t>(cuda_stream)), "cconv_quantize_groups");
     });
   });
 }

@@ -30,5 +30,19 @@ cudaError_t launch(F f, dim3 grid, int threads, size_t smem, int cluster, cudaSt
   return e;
 }
 
+// Lets a kernel have `bytes` of dynamic shared memory on the current device (`ready`: the kernel's, by device).
+template <typename F>
+cudaError_t allow_smem(F f, bool (&ready)[64], int bytes) {
+  int dev = 0;
+  cudaError_t e = cudaGetDevice(&dev);
+  if (e != cudaSuccess) return e;
+  if (!__atomic_load_n(&ready[dev & 63], __ATOMIC_ACQUIRE)) {
+    e = cudaFuncSetAttribute(f, cudaFuncAttributeMaxDynamicSharedMemorySize, bytes);
+    if (e != cudaSuccess) return e;
+    __atomic_store_n(&ready[dev & 63], true, __ATOMIC_RELEASE);
+  }
+  return cudaSuccess;
+}
+
 }  // namespace
 }  // namespace cconv

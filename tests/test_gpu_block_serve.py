@@ -1,4 +1,5 @@
-"""The operators that serve the feed-forward sub-block against plain 64-bit forms: norms with 8-bit results.
+"""The operators that serve the feed-forward sub-block against plain 64-bit forms: norms with 8-bit results,
+products with 4-bit weights and their quantiser.
 
 Tolerances.  u is a type's unit roundoff, eps / 2 (bf16 2^-8, fp16 2^-11, fp32 2^-24, e4m3 2^-4).  Sums of n products
 in fp32 are off by at most (n + 16) 2^-23 of the sum of the products' sizes.  A result's own rounding adds u of its
@@ -163,3 +164,203 @@ def test_norm_in_8_bits_of_nothing():
         block.residual_norm_quantize(e, torch.empty_like(e), torch.empty((T, D), device="cuda", dtype=E4M3),
                                      torch.empty((T, -(-D // 128)), device="cuda"))
     torch.cuda.synchronize()
+
+
+# ---- 4-bit weights --------------------------------------------------------------------------------
+
+U8 = torch.uint8
+
+
+class Int4:
+    """Random codes, scales, zero points and tokens; exact values and tolerances."""
+
+    def __init__(self, M, N, K, group=128, dtype=BF16, scale=None, zero=False, seed=0):
+        g = gen(seed + 3 * M + 5 * N + 7 * K + group)
+        self.M, self.N, self.K, self.group, self.dtype = M, N, K, group, dtype
+        groups = -(-K // group)
+        self.x = normal(g, (M, K), dtype)
+        self.q = torch.randint(0, 256, (N, -(-K // 2)), generator=g, device="cuda", dtype=U8)
+        self.scale = (torch.exp(0.3 * normal(g, (N, groups), FP32)) * (0.2 * max(K, 1) ** -0.5)).to(scale or dtype)
+        # (the upper halves of the bytes do not count)
+        self.zero = torch.randint(0, 256, (N, groups), generator=g, device="cuda", dtype=U8) if zero else None
+
+    def run(self, out=None, **kw):
+        out = poisoned((self.M, self.N), self.dtype) if out is None else out
+        return block.int4_product(self.x, self.q, self.scale, out, zero=self.zero, group=self.group, **kw)
+
+    def weights(self):
+        """q, z and s of every element, in 64 bits."""
+        at = torch.arange(self.K, device="cuda")
+        q = (self.q[:, at // 2].int() >> (4 * (at % 2)) & 15).double()
+        z = torch.full_like(q, 8.0) if self.zero is None else (self.zero.int() & 15).double()[:, at // self.group]
+        return q, z, self.scale.double()[:, at // self.group]
+
+    def check(self, out, what=""):
+        q, z, s = self.weights()
+        x, u = self.x.double(), U[self.dtype]
+        w = s * (q - z)
+        c = x @ w.T
+        if self.M <= 64:  # sums of 16 + q and 16 + z
+            e = sum_err(self.K) * (x.abs() @ (s.abs() * (32 + q + z)).T)
+        else:             # weights rounded to the type
+            e = (u + sum_err(self.K)) * (x.abs() @ w.abs().T) + 2.0 ** -25 * x.abs().sum(1, keepdim=True)
+        close(out, c, 1.01 * (e + u * c.abs()) + TINY[self.dtype], what)
+
+
+INT4_SHAPES = [(1, 64, 64), (1, 1, 1), (2, 16, 128), (3, 17, 33), (1, 4096, 1024), (4, 33, 256), (5, 130, 1000), (8, 4800, 384),
+               (9, 100, 4200), (16, 5000, 520), (17, 48, 96), (23, 75, 2056), (33, 129, 130), (64, 200, 640), (65, 256, 256),
+               (130, 72, 1001), (300, 513, 320), (1, 8192, 8192), (64, 31, 16416)]
+
+
+@pytest.mark.parametrize("M,N,K", INT4_SHAPES)
+@pytest.mark.parametrize("group", [32, 64, 128])
+@pytest.mark.parametrize("dtype", [BF16, FP16])
+def test_int4_product(M, N, K, group, dtype):
+    scale = (dtype, FP32, BF16, FP16)[(M + N + K + group // 32) % 4]
+    for zero in (False, True):
+        c = Int4(M, N, K, group, dtype, scale, zero)
+        c.check(c.run(), f"{M}x{N}x{K} group {group} zero {zero}")
+    assert block.status() == (0, 0)
+
+
+@pytest.mark.parametrize("M", [1, 3, 12, 40, 100])
+@pytest.mark.parametrize("K", [256, 264, 300])
+def test_int4_strided_operands(M, K):
+    c = Int4(M, 72, K, 32, BF16, zero=True)
+
+    def transposed(t):
+        return t.t().contiguous().t()
+
+    def shifted(by, pad):
+        def f(t):
+            big = torch.full((t.shape[0], t.shape[1] + pad), 9, device="cuda").to(t.dtype)
+            big[:, by:by + t.shape[1]] = t
+            return big[:, by:by + t.shape[1]]
+        return f
+
+    def every_other(t):
+        big = torch.full((t.shape[0], 2 * t.shape[1]), 9, device="cuda").to(t.dtype)
+        big[:, ::2] = t
+        return big[:, ::2]
+    exp = c.run()
+    for store in (transposed, shifted(0, 16), shifted(4, 8), shifted(8, 24), shifted(1, 3), every_other):
+        h = Int4(M, 72, K, 32, BF16, zero=True)
+        for name in ("x", "q", "scale", "zero"):
+            setattr(h, name, store(getattr(c, name)))
+        big = torch.full((M + 2, 80), 7.0, device="cuda", dtype=BF16)
+        out = big[1:M + 1, 3:75]
+        h.run(out=out)
+        assert torch.equal(out, exp)  # the same sums in the same order
+        big[1:M + 1, 3:75] = 7.0
+        assert (big == 7.0).all()
+        wide = torch.full((72, M), 7.0, device="cuda", dtype=BF16)
+        assert torch.equal(h.run(out=wide.t()), exp)
+
+
+def test_int4_rows_with_a_shared_token_and_shared_weights():
+    c = Int4(5, 40, 320, 64, FP16)
+    c.x = c.x[:1].expand(5, 320)
+    c.q, c.scale = c.q[:1].expand(40, 160), c.scale[:1].expand(40, 5)
+    c.check(c.run(), "broadcast")
+
+
+def test_int4_of_nothing():
+    for M, N, K in ((0, 8, 64), (3, 0, 64), (3, 8, 0)):
+        c = Int4(M, N, K)
+        assert (c.run() == 0).all()
+
+
+def test_int4_infinities_and_nan():
+    for M in (4, 100):
+        c = Int4(M, 64, 512)
+        c.x[1, 7] = float("inf")
+        c.x[2, 300] = float("nan")
+        c.scale[9, 2] = float("nan")
+        out = c.run()
+        bad = ~torch.isfinite(out)
+        assert bad[2].all() and bad[:, 9].all()
+        bad[1:3], bad[:, 9] = False, False
+        assert not bad.any()
+
+
+def test_int4_offsets_beyond_32_bits():
+    """Rows so far apart that their offsets pass 2^32 bytes."""
+    N, K = 3, 256
+    c = Int4(2, N, K)
+    big = torch.empty(3 * (1 << 31) + 256, device="cuda", dtype=U8)
+    q = big.as_strided((N, K // 2), (1 << 31, 1))
+    q.copy_(c.q)
+    exp = c.run()
+    c.q = q
+    assert torch.equal(c.run(), exp)
+    c.x = c.x.repeat(40, 1)
+    c.M = 80
+    c.check(c.run(), "many tokens")
+
+
+def quantized(w, group, zero, stype):
+    """The definition, operation by operation in fp32."""
+    N, K = w.shape
+    groups = -(-K // group)
+    f = torch.nn.functional.pad(w.float(), (0, groups * group - K)).reshape(N, groups, group)
+    if zero:
+        lo, hi = f.amin(2, keepdim=True).clamp(max=0), f.amax(2, keepdim=True).clamp(min=0)
+        s = (hi - lo) / torch.full_like(lo, 15.0)
+    else:
+        s = f.abs().amax(2, keepdim=True) / torch.full((N, groups, 1), 7.0, device="cuda")
+    s = torch.where(torch.isfinite(f).all(2, keepdim=True), s, float("nan"))
+    st = s.to(stype)
+    sf = st.float()
+    ok = torch.isfinite(sf) & (sf > 0)
+    by = torch.where(ok, sf, 1.0)
+    z = (-lo / by).round().clamp(0, 15) if zero else torch.full_like(sf, 8.0)
+    q = ((f / by).round() + z).clamp(0, 15)
+    z = torch.where(ok, z, 8.0)
+    q = torch.where(ok, q, 8.0).reshape(N, -1)[:, :K].to(torch.int32)
+    q = torch.nn.functional.pad(q, (0, K % 2))
+    return (q[:, ::2] | q[:, 1::2] << 4).to(U8), st[:, :, 0], z[:, :, 0].to(U8)
+
+
+@pytest.mark.parametrize("N,K", [(1, 1), (3, 32), (5, 33), (17, 256), (64, 1000), (9, 2048), (2, 5001), (70000, 40)])
+@pytest.mark.parametrize("dtype", [BF16, FP16, FP32])
+@pytest.mark.parametrize("zero", [False, True])
+def test_quantize_groups(N, K, dtype, zero):
+    g = gen(N + K)
+    w = normal(g, (N, K), dtype, 0.02) + (0.01 if zero else 0)
+    if N > 3:
+        w[1] = 0
+        w[2, : min(K, 40)] = 0.5
+        w[3, K // 2] = float("inf")
+        w[3, 0] = float("nan")
+    for group in (32, 64, 128):
+        for stype in (BF16, FP16, FP32):
+            groups = -(-K // group)
+            q = torch.full((N, -(-K // 2)), 77, device="cuda", dtype=U8)
+            s = poisoned((N, groups), stype)
+            z = torch.full((N, groups), 99, device="cuda", dtype=U8) if zero else None
+            block.quantize_groups(w, q, s, zero=z, group=group)
+            eq, es, ez = quantized(w, group, zero, stype)
+            assert torch.equal(torch.nan_to_num(s, nan=-1), torch.nan_to_num(es, nan=-1))
+            assert torch.equal(q, eq)
+            assert z is None or torch.equal(z, ez)
+
+
+def test_quantize_groups_strided_and_back():
+    w = normal(gen(4), (100, 330), FP32, 0.1)
+    q0, s0, z0 = quantized(w, 32, True, BF16)
+    store = torch.zeros((330, 100), device="cuda").t()
+    store.copy_(w)
+    q, s, z = (torch.zeros((c, 100), device="cuda", dtype=t).t() for c, t in ((165, U8), (11, BF16), (11, U8)))
+    block.quantize_groups(store, q, s, zero=z, group=32)
+    assert torch.equal(q, q0) and torch.equal(s, s0) and torch.equal(z, z0)
+    # what the product makes of them is within half a step of w, and the scale's and zero point's rounding
+    out = poisoned((330, 100), BF16)
+    block.int4_product(torch.eye(330, device="cuda", dtype=BF16), q, s, out, zero=z, group=32)
+    step = s.double().repeat_interleave(32, 1)[:, :330]
+    close(out.t(), w.double(), 1.1 * step + 2.0 ** -7 * w.double().abs(), "back")
+
+
+def test_quantize_groups_of_nothing():
+    for N, K in ((0, 64), (4, 0)):
+        block.quantize_groups(torch.empty((N, K), device="cuda"), torch.empty((N, K // 2), device="cuda", dtype=U8),
+                              torch.empty((N, -(-K // 128)), device="cuda"))
