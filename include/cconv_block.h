@@ -9,6 +9,7 @@
  *   8-bit product   C[m,n] = sum_kb (sa[m,kb] sb[n/128,kb]) sum_{k in block kb} A[m,k] B[n,k]
  *   quantisation    8-bit values (e4m3) and a scale for each 1 x 128 or 128 x 128 block
  *   4-bit product   C[m,n] = sum_g s[n,g] sum_{k in group g} (q[n,k] - z[n,g]) X[m,k], and the quantiser of its weights
+ *   clipping        norm over all elements of a list of gradients, and factor = min(1, max_norm / (norm + eps))
  *   norm in 8 bits  the residual norm whose x is written as 8-bit values and scales
  *
  * Matrices are given by the address of element (0,0) and two strides in elements.  Strides of inputs
@@ -204,6 +205,34 @@ typedef struct {
 } cconv_quantize_groups_args;
 
 int cconv_quantize_groups(const cconv_quantize_groups_args* args, void* cuda_stream);
+
+/* ---- the norm of a list of gradients, and clipping -------------------------------------------------
+ * norm = sqrt(sum of squares over all elements), the sum in 64 bits, rounded to fp32; every element times
+ * min(1, max_norm / (norm + eps)), in fp32, rounded to its type.  A norm that is infinite makes the factor 0, one that is
+ * NaN makes every element NaN.  Tensors of more than two dimensions are lists of rows where their strides allow. */
+typedef struct {
+  void* data;
+  int64_t rows, cols, row_stride, col_stride; /* strides in elements */
+  int32_t dtype;                              /* CCONV_TYPE_* */
+  int32_t reserved;                           /* 0 */
+} cconv_tensor;
+
+typedef struct {
+  int64_t count;
+  const cconv_tensor* grads; /* HOST array of `count`, read during the call */
+  const cconv_tensor* outs;  /* HOST array: where results go, rows, cols and types as in grads; NULL: in place.  Every
+                                out is apart from all gradients, or all of its own one */
+  float max_norm, eps;       /* max_norm >= 0, eps >= 0, not both 0 */
+  int32_t norm_given;        /* 1: `norm` holds the norm (of this list and others, say) and is read, not written */
+  int32_t reserved;          /* 0 */
+  void* norm;                /* fp32, one element */
+  void* workspace;           /* none needed where the norm is given */
+  uint64_t workspace_bytes;
+} cconv_clip_args;
+
+int64_t cconv_clip_workspace(const cconv_clip_args* args);
+int cconv_gradient_norm(const cconv_clip_args* args, void* cuda_stream); /* writes `norm`; reads grads and workspace only */
+int cconv_clip_gradients(const cconv_clip_args* args, void* cuda_stream);
 
 /* Synchronises `cuda_stream`, reads the status word that the product kernels of the current device
  * share and clears it: CCONV_OK, CCONV_EDEVICE_TIMEOUT (a bounded wait on the device ran out; the

@@ -7,6 +7,7 @@
     quantize_blocks                                   the 8-bit values and the scales
     int4_product                                      4-bit weights with a scale for each group of a row
     quantize_groups                                   those weights, scales and zero points
+    gradient_norm, clip_gradients                     the norm over a list of gradients, and their clipping
 
 Argument marshalling only: every step runs in ``libcconv.so``.  Results go to tensors that the caller
 gives.  Calls are asynchronous on ``stream`` (default: the current stream of the operands' device).
@@ -33,7 +34,8 @@ EXPORTS = (
     "cconv_residual_norm_backward_workspace", "cconv_residual_norm_forward", "cconv_residual_norm_backward",
     "cconv_residual_norm_quantize",
     "cconv_fp8_product_workspace", "cconv_fp8_product", "cconv_quantize_blocks", "cconv_int4_product_workspace",
-    "cconv_int4_product", "cconv_quantize_groups", "cconv_block_status",
+    "cconv_int4_product", "cconv_quantize_groups", "cconv_clip_workspace",
+    "cconv_gradient_norm", "cconv_clip_gradients", "cconv_block_status",
 )
 
 # The argument structures of the C ABI, field for field (P: address, q: 64-bit, i: 32-bit, f: float), without
@@ -45,6 +47,8 @@ _FP8 = struct.Struct("qqqii" + _MAT * 5)
 _QUANT = struct.Struct("qqii" + _MAT * 3)
 _INT4 = struct.Struct("qqqiiii" + _MAT * 5)
 _GROUPS = struct.Struct("qqiiii" + _MAT * 4)
+_TENSOR = struct.Struct("Pqqqqii")
+_CLIP = struct.Struct("qPPffiiP")
 _TWO = struct.Struct(_MAT * 2)  # behind the norm's, in the call with 8-bit results
 _SPACE = struct.Struct("PQ")
 _NO_SPACE = _SPACE.pack(0, 0)
@@ -413,6 +417,90 @@ def quantize_groups(w, q, scale, zero=None, group=128, stream=None):
                         *(_NONE if zero is None else _mat(zero, (N, groups), u8, dev, "zero")))
     _call("cconv_quantize_groups", args, dev, stream)
     return q, scale, zero
+
+
+# ---- the norm of a list of gradients, and clipping ----------------------------------------------------
+
+def _as_rows(t, name):
+    """(rows, cols, row stride, col stride) of a tensor's elements, taken in the order of its strides."""
+    if t.is_contiguous():
+        return 1, t.numel(), t.numel(), 1
+    dims = []  # (size, stride), outer ones first, neighbours that follow one another merged
+    for size, stride in sorted(((n, st) for n, st in zip(t.shape, t.stride()) if n > 1), key=lambda d: -d[1]):
+        if dims and dims[-1][1] == size * stride:
+            dims[-1] = (dims[-1][0] * size, stride)
+        else:
+            dims.append((size, stride))
+    if len(dims) > 2:
+        raise ValueError(f"{name}: a tensor of shape {tuple(t.shape)} and strides {t.stride()} is no list of rows")
+    dims = [(1, t.numel())] * (2 - len(dims)) + dims
+    return dims[0][0], dims[1][0], dims[0][1], dims[1][1]
+
+
+class TensorList:
+    """A list of tensors of one device as the library takes it, for lists that several calls share: gradients that
+    a program keeps from step to step.  It holds the tensors; their storage, shapes and strides must not change."""
+
+    def __init__(self, tensors, name="tensors"):
+        self.tensors = list(tensors)
+        if not self.tensors:
+            raise ValueError(f"{name} must hold at least one tensor")
+        self.device = self.tensors[0].get_device()
+        packed = []
+        for i, t in enumerate(self.tensors):
+            ty = _TYPES.get(t.dtype)
+            if ty is None or t.get_device() != self.device or self.device < 0:
+                raise ValueError(f"{name}[{i}] must be a bf16, fp16 or fp32 tensor on one CUDA device, got {t.dtype} on {t.device}")
+            packed.append(_TENSOR.pack(t.data_ptr(), *_as_rows(t, f"{name}[{i}]"), ty, 0))
+        # of tensors of the same layout the elements correspond in the order above
+        self.layout = [(t.dtype, t.shape, None if t.is_contiguous() else t.stride()) for t in self.tensors]
+        self._array = ctypes.create_string_buffer(b"".join(packed))
+        self.address, self.count = ctypes.addressof(self._array), len(packed)
+
+    def __len__(self):
+        return self.count
+
+
+def _tensor_list(tensors, name):
+    return tensors if isinstance(tensors, TensorList) else TensorList(tensors, name)
+
+
+def _clip_args(grads, outs, max_norm, eps, norm_given, norm):
+    if outs is not None and (outs.device != grads.device or outs.layout != grads.layout):
+        raise ValueError("outs must have the types, shapes, strides and device of grads")
+    return _CLIP.pack(grads.count, grads.address, 0 if outs is None else outs.address, max_norm, eps, norm_given, 0,
+                      _vec(norm, 1, torch.float32, grads.device, "norm"))
+
+
+def clip_workspace(grads):
+    """cconv_clip_workspace: bytes of workspace of gradient_norm and clip_gradients with these tensors."""
+    grads = _tensor_list(grads, "grads")
+    return _need("cconv_clip_workspace", _CLIP.pack(grads.count, grads.address, 0, 1.0, 0.0, 0, 0, 0), grads.device)
+
+
+def gradient_norm(grads, norm, workspace=None, stream=None):
+    """cconv_gradient_norm: norm[0] = sqrt of the sum of squares over all elements of ``grads``.
+
+    ``grads``: a list of bf16, fp16 and fp32 tensors of one device, or a TensorList; ``norm``: fp32 [1]."""
+    grads = _tensor_list(grads, "grads")
+    args = _clip_args(grads, None, 1.0, 0.0, 0, norm)
+    _call_with_space("cconv_gradient_norm", "cconv_clip_workspace", args, grads.device, workspace, stream)
+    return norm
+
+
+def clip_gradients(grads, max_norm, norm, outs=None, eps=1e-6, norm_given=False, workspace=None, stream=None):
+    """cconv_clip_gradients: every gradient times min(1, max_norm / (norm + eps)), in place or to ``outs``.
+
+    ``grads``, ``outs``: lists of tensors, or TensorLists; ``norm`` (fp32 [1]) gets the norm over all of them, or,
+    with ``norm_given``, holds it: that of other ranks' gradients too, say.  Nothing waits for the host."""
+    grads = _tensor_list(grads, "grads")
+    outs = None if outs is None else _tensor_list(outs, "outs")
+    args = _clip_args(grads, outs, max_norm, eps, int(norm_given), norm)
+    if norm_given:
+        _call("cconv_clip_gradients", args + _NO_SPACE, grads.device, stream)
+    else:
+        _call_with_space("cconv_clip_gradients", "cconv_clip_workspace", args, grads.device, workspace, stream)
+    return norm
 
 
 def status(stream=None):

@@ -1,11 +1,14 @@
 // Entry points of the feed-forward sub-block (include/cconv_block.h): checks of arguments, workspace
 // layout, launches.  Nothing here allocates or synchronises (cconv_block_status synchronises).
+#include <algorithm>
 #include <cmath>
 #include <cstring>
 #include <numeric>
 #include <string>
+#include <vector>
 
 #include "block.h"
+#include "block_clip.h"
 #include "block_ffn.h"
 #include "block_fp8.h"
 #include "block_gemm.h"
@@ -68,6 +71,31 @@ struct Bytes {
   }
   bool operator==(const Bytes& o) const { return lo == o.lo && hi == o.hi && pitch == o.pitch && width == o.width && step == o.step; }
 };
+
+// The bytes of an operand of rows x cols > 0 elements; whether they can be an operand's (of a result: are distinct).
+bool bytes_of(const cconv_matrix& m, int64_t rows, int64_t cols, int es, bool written, Bytes* out) {
+  if (!m.data || (reinterpret_cast<uintptr_t>(m.data) & uintptr_t(es - 1)) || m.row_stride < 0 || m.col_stride < 0 ||
+      m.row_stride > kMaxStride || m.col_stride > kMaxStride)
+    return false;
+  const double last = double(rows - 1) * double(m.row_stride) + double(cols - 1) * double(m.col_stride);
+  if (last > 4.0e18 / es) return false;
+  bool ok = true;
+  if (written) {
+    // distinct elements: one stride steps over the whole extent of the other
+    const int64_t r = m.row_stride, c = m.col_stride;
+    const bool rows_outer = (rows == 1 || r > (cols - 1) * c) && (cols == 1 || c > 0);
+    const bool cols_outer = (cols == 1 || c > (rows - 1) * r) && (rows == 1 || r > 0);
+    ok = rows_outer || cols_outer;
+  }
+  const char* lo = static_cast<const char*>(m.data);
+  Bytes b{lo, lo + ((rows - 1) * m.row_stride + (cols - 1) * m.col_stride + 1) * es, 0, 0, es,
+          std::gcd(rows > 1 ? m.row_stride * es : 0, cols > 1 ? m.col_stride * es : 0)};
+  const int64_t wr = ((cols - 1) * m.col_stride + 1) * es, wc = ((rows - 1) * m.row_stride + 1) * es;
+  if (rows > 1 && m.row_stride * es >= wr) b.pitch = m.row_stride * es, b.width = wr;
+  else if (cols > 1 && m.col_stride * es >= wc) b.pitch = m.col_stride * es, b.width = wc;
+  *out = b;
+  return ok;
+}
 
 // Collects the byte ranges that a call reads and writes, and checks each operand on the way.
 class Operands {
@@ -138,29 +166,9 @@ class Operands {
   }
   int add(const cconv_matrix& m, int64_t rows, int64_t cols, int es, bool written) {
     if (rows == 0 || cols == 0) return -1;  // nothing is touched
-    if (!m.data || (reinterpret_cast<uintptr_t>(m.data) & uintptr_t(es - 1)) || m.row_stride < 0 || m.col_stride < 0 ||
-        m.row_stride > kMaxStride || m.col_stride > kMaxStride) {
-      ok = false;
-      return -1;
-    }
-    const double last = double(rows - 1) * double(m.row_stride) + double(cols - 1) * double(m.col_stride);
-    if (last > 4.0e18 / es) {
-      ok = false;
-      return -1;
-    }
-    if (written) {
-      // distinct elements: one stride steps over the whole extent of the other
-      const int64_t r = m.row_stride, c = m.col_stride;
-      const bool rows_outer = (rows == 1 || r > (cols - 1) * c) && (cols == 1 || c > 0);
-      const bool cols_outer = (cols == 1 || c > (rows - 1) * r) && (rows == 1 || r > 0);
-      if (!rows_outer && !cols_outer) ok = false;
-    }
-    const char* lo = static_cast<const char*>(m.data);
-    Bytes b{lo, lo + ((rows - 1) * m.row_stride + (cols - 1) * m.col_stride + 1) * es, 0, 0, es,
-            std::gcd(rows > 1 ? m.row_stride * es : 0, cols > 1 ? m.col_stride * es : 0)};
-    const int64_t wr = ((cols - 1) * m.col_stride + 1) * es, wc = ((rows - 1) * m.row_stride + 1) * es;
-    if (rows > 1 && m.row_stride * es >= wr) b.pitch = m.row_stride * es, b.width = wr;
-    else if (cols > 1 && m.col_stride * es >= wc) b.pitch = m.col_stride * es, b.width = wc;
+    Bytes b;
+    if (!bytes_of(m, rows, cols, es, written, &b)) ok = false;
+    if (!b.lo) return -1;
     return push(b, written);
   }
   Bytes range_[24];
@@ -328,8 +336,112 @@ bool fp8_sizes_ok(const cconv_fp8_product_args& a) {
          double(a.N) * a.K < 1e15;
 }
 
-bool group_ok(int32_t group) { return group == 32 || group == 64 || group == 128; }
 bool type_ok(int32_t t) { return t >= CCONV_TYPE_BF16 && t <= CCONV_TYPE_FP32; }
+
+// ---- clipping ------------------------------------------------------------------------------------
+constexpr int64_t kMostTensors = 1 << 20;
+
+bool clip_sizes_ok(const cconv_clip_args& a, bool clips) {
+  if (a.count < 0 || a.count > kMostTensors || (a.count && !a.grads) || a.reserved != 0 || a.norm_given < 0 || a.norm_given > 1)
+    return false;
+  if (clips && (!(a.max_norm >= 0) || !(a.eps >= 0) || !std::isfinite(a.eps) || !(a.max_norm + a.eps > 0))) return false;
+  double all = 0;
+  for (int64_t i = 0; i < a.count; ++i) {
+    const cconv_tensor& g = a.grads[i];
+    if (g.rows < 0 || g.cols < 0 || !type_ok(g.dtype) || g.reserved != 0) return false;
+    all += double(g.rows) * double(g.cols);
+    if (clips && a.outs) {
+      const cconv_tensor& o = a.outs[i];
+      if (o.rows != g.rows || o.cols != g.cols || o.dtype != g.dtype || o.reserved != 0) return false;
+    }
+  }
+  return all < 1e15;
+}
+
+cconv_matrix matrix_of(const cconv_tensor& t) {
+  return cconv_matrix{t.data, t.rows > 1 ? t.row_stride : t.cols, t.cols > 1 ? t.col_stride : 1};
+}
+
+// The operands of a call of any number of tensors: checked, told from one another in the order of their addresses,
+// and noted in the stream's bookkeeping.
+class Tensors {
+ public:
+  bool ok = true;
+  void add(const cconv_matrix& m, int64_t rows, int64_t cols, int es, bool written, int64_t of) {
+    if (rows == 0 || cols == 0) return;
+    Entry e{{}, written, of};
+    if (!bytes_of(m, rows, cols, es, written, &e.bytes)) ok = false;
+    else all_.push_back(e);
+  }
+  // No result meets anything but its own gradient (`of` equal) lying in the very same place.
+  bool distinct() {
+    std::sort(all_.begin(), all_.end(), [](const Entry& a, const Entry& b) { return a.bytes.lo < b.bytes.lo; });
+    std::vector<const Entry*> open;  // those that reach beyond the current one's start
+    for (const Entry& e : all_) {
+      size_t kept = 0;
+      for (const Entry* o : open) {
+        if (o->bytes.hi <= e.bytes.lo) continue;
+        open[kept++] = o;
+        if (!o->written && !e.written) continue;
+        if (o->of == e.of && o->written != e.written && o->bytes == e.bytes) continue;
+        if (o->bytes.meets(e.bytes)) return false;
+      }
+      open.resize(kept);
+      open.push_back(&e);
+    }
+    return ok;
+  }
+  void note(void* stream, int sms) const {
+    CallSpans c;
+    for (const Entry& e : all_) {
+      Span& s = e.written ? c.out : c.image;
+      if (!s.lo || e.bytes.lo < s.lo) s.lo = e.bytes.lo;
+      if (!s.hi || e.bytes.hi > s.hi) s.hi = e.bytes.hi;
+    }
+    note_call(stream, c, Overlap::kInputsEarly, sms);
+  }
+
+ private:
+  struct Entry {
+    Bytes bytes;
+    bool written;
+    int64_t of;  // the tensor's number
+  };
+  std::vector<Entry> all_;
+};
+
+int clip_call(const cconv_clip_args& a, bool clips, void* cuda_stream) {
+  if (!clip_sizes_ok(a, clips)) return CCONV_EINVAL;
+  const bool sums = !clips || !a.norm_given;
+  bool any = false;
+  Tensors o;
+  for (int64_t i = 0; i < a.count; ++i) {
+    const cconv_tensor& g = a.grads[i];
+    const int es = type_bytes(g.dtype);
+    any |= g.rows && g.cols;
+    o.add(matrix_of(g), g.rows, g.cols, es, clips && !a.outs, i);
+    if (clips && a.outs) o.add(matrix_of(a.outs[i]), g.rows, g.cols, es, true, i);
+  }
+  o.add(cconv_matrix{a.norm, 1, 1}, 1, 1, 4, sums, -1);
+  if (!o.distinct()) return CCONV_EINVAL;
+  if (!any && !sums) return CCONV_OK;
+  const int sms = block_sm_count();
+  if (sms < 0) return sms;
+  const int64_t need = sums ? clip_workspace(a, sms) : 0;
+  if (need) {
+    if (!a.workspace || (reinterpret_cast<uintptr_t>(a.workspace) & 255u) || a.workspace_bytes < uint64_t(need)) return CCONV_EINVAL;
+    o.add(cconv_matrix{a.workspace, need, 1}, 1, need, 1, true, -2);
+    if (!o.distinct()) return CCONV_EINVAL;
+  }
+  cudaStream_t s = static_cast<cudaStream_t>(cuda_stream);
+  const int64_t before = block_launches();
+  int rc = sums && any ? run_square_sums(a, sms, s) : CCONV_OK;
+  if (rc == CCONV_OK) rc = clips && any ? run_clip(a, sms, s) : run_norm_of_sums(a, sms, s);
+  if (block_launches() != before) o.note(cuda_stream, sms);
+  return rc;
+}
+
+bool group_ok(int32_t group) { return group == 32 || group == 64 || group == 128; }
 bool int4_sizes_ok(const cconv_int4_product_args& a) {
   return length_ok(a.M) && length_ok(a.N) && length_ok(a.K) && (a.dtype == CCONV_TYPE_BF16 || a.dtype == CCONV_TYPE_FP16) &&
          type_ok(a.scale_dtype) && group_ok(a.group) && a.reserved == 0 && double(a.M) * a.N < 1e15 &&
@@ -604,6 +716,23 @@ int cconv_quantize_groups(const cconv_quantize_groups_args* args, void* cuda_str
       return block_cuda_error(run_quantize_groups(a, static_cast<cudaStream_t>(cuda_stream)), "cconv_quantize_groups");
     });
   });
+}
+
+int64_t cconv_clip_workspace(const cconv_clip_args* args) {
+  return guarded([&]() -> int64_t {
+    if (!args || !clip_sizes_ok(*args, false)) return CCONV_EINVAL;
+    const int sms = block_sm_count();
+    if (sms < 0) return sms;
+    return clip_workspace(*args, sms);
+  });
+}
+
+int cconv_gradient_norm(const cconv_clip_args* args, void* cuda_stream) {
+  return guarded([&]() -> int { return args ? clip_call(*args, false, cuda_stream) : CCONV_EINVAL; });
+}
+
+int cconv_clip_gradients(const cconv_clip_args* args, void* cuda_stream) {
+  return guarded([&]() -> int { return args ? clip_call(*args, true, cuda_stream) : CCONV_EINVAL; });
 }
 
 int cconv_block_status(void* cuda_stream, int* detail_out) {

@@ -364,3 +364,147 @@ def test_quantize_groups_of_nothing():
     for N, K in ((0, 64), (4, 0)):
         block.quantize_groups(torch.empty((N, K), device="cuda"), torch.empty((N, K // 2), device="cuda", dtype=U8),
                               torch.empty((N, -(-K // 128)), device="cuda"))
+
+
+# ---- the norm of a list of gradients, and clipping --------------------------------------------------
+
+def gradients(shapes, seed=0, scale=0.02):
+    g = gen(seed)
+    return [normal(g, shape, dtype, scale) for shape, dtype in shapes]
+
+
+def norm64(ts):
+    return sum(t.double().square().sum().item() for t in ts) ** 0.5
+
+
+def check_clipped(outs, grads, norm, max_norm, eps=1e-6, what=""):
+    """Squares in fp32 over at most 34 elements, then 64 bits: 40 2^-24 of the sum, half of that of its root."""
+    exact = norm64(grads)
+    assert abs(norm.item() - exact) <= 24 * 2.0 ** -24 * exact, (what, norm.item(), exact)
+    factor = min(1.0, max_norm / (exact + eps))
+    for o, g in zip(outs, grads):
+        assert o.dtype == g.dtype and o.shape == g.shape
+        v = g.double() * factor
+        close(o, v, v.abs() * (U[g.dtype] * 1.01 + 30 * 2.0 ** -24) + 2.0 ** -25 * (g.dtype == FP16) + 1e-45, what)
+
+
+LISTS = [[((1,), FP32)], [((7,), BF16), ((0,), FP32), ((3, 5), FP16)], [((1000, 1000), BF16)], [((300, 700), FP32), ((700,), FP32)],
+         [((256, 700), BF16), ((700, 256), FP16), ((256,), FP32)] * 17, [((33,), FP32)] * 700, [((4096, 4097), FP16), ((5, 3, 7, 11), BF16)],
+         [((2, 8191), BF16), ((1, 8193), BF16), ((1, 4095), FP32), ((1, 4097), FP32)]]
+
+
+@pytest.mark.parametrize("shapes", LISTS, ids=range(len(LISTS)))
+@pytest.mark.parametrize("part", [0.25, 4.0])
+def test_clip_gradients(shapes, part):
+    grads = gradients(shapes)
+    exact = norm64(grads)
+    norm = poisoned((1,), FP32)
+    outs = [poisoned(g.shape, g.dtype) for g in grads]
+    block.clip_gradients(grads, part * exact, norm, outs=outs)
+    check_clipped(outs, grads, norm, part * exact, what="outs")
+    alone = poisoned((1,), FP32)
+    block.gradient_norm(grads, alone)
+    assert torch.equal(alone, norm)
+    # in place, the list made once; and with the norm given
+    mine = [g.clone() for g in grads]
+    lst = block.TensorList(mine)
+    norm2 = poisoned((1,), FP32)
+    block.clip_gradients(lst, part * exact, norm2)
+    assert torch.equal(norm2, norm)
+    for a, b in zip(mine, outs):
+        assert torch.equal(a, b)
+    more = [poisoned(g.shape, g.dtype) for g in grads]
+    block.clip_gradients(grads, part * exact, norm, outs=more, norm_given=True)
+    for a, b in zip(more, outs):
+        assert torch.equal(a, b)
+
+
+def test_clip_views_of_a_buffer_that_begin_anywhere():
+    flat = normal(gen(5), (200001,), BF16)
+    cuts = [0, 1, 4, 17, 1000, 9192, 9193, 30000, 131072, 200001]
+    out = torch.full_like(flat, 7.0)
+    # results two elements further on than the gradients: no common alignment
+    target = torch.full((200005,), 7.0, device="cuda", dtype=BF16)
+    grads = [flat[a:b] for a, b in zip(cuts, cuts[1:])]
+    norm = poisoned((1,), FP32)
+    block.clip_gradients(grads, 1.0, norm, outs=[target[a + 3:b + 3] for a, b in zip(cuts, cuts[1:])])
+    check_clipped([target[3:200004]], [flat], norm, 1.0)
+    assert (target[:3] == 7).all() and target[200004] == 7
+    block.clip_gradients(grads[1:-1], 1.0, norm, outs=[out[a:b] for a, b in zip(cuts, cuts[1:])][1:-1])
+    assert out[0] == 7 and (out[131072:] == 7).all() and not (out[1:131072] == 7).any()
+
+
+def test_clip_strided_tensors():
+    g = gen(6)
+    whole = [normal(g, s, t) for s, t in (((64, 3000), BF16), ((500, 40), FP32), ((6, 4, 10, 8), FP16), ((90, 70), BF16))]
+    views = [whole[0][:, 7:2900], whole[1][::2, ::3], whole[2].permute(0, 3, 1, 2), whole[3].t()]
+    before = [w.clone() for w in whole]
+    copies = [v.clone() for v in views]
+    norm = poisoned((1,), FP32)
+    m = 0.5 * norm64(copies)
+    block.clip_gradients(views, m, norm)
+    check_clipped(views, copies, norm, m)
+    for w, b, v in zip(whole, before, ((slice(None), slice(7, 2900)), (slice(None, None, 2), slice(None, None, 3)))):
+        w, b = w.clone(), b.clone()
+        w[v], b[v] = 0, 0
+        assert torch.equal(w, b)  # what lies between stays
+
+
+def test_clip_extreme_values():
+    for value, dtype in ((1e30, FP32), (3e38, BF16), (1e-30, FP32), (1e-38, BF16), (6e-8, FP16), (6e4, FP16)):
+        x = torch.full((70001,), value, device="cuda").to(dtype)
+        v = x[0].item()
+        norm = poisoned((1,), FP32)
+        block.gradient_norm([x], norm)
+        exact = abs(v) * 70001 ** 0.5
+        if exact > 3.4e38:
+            assert norm.item() == float("inf")
+        else:
+            assert abs(norm.item() - exact) <= 2.0 ** -19 * exact + 1e-45, (value, dtype)
+    zeros = [torch.zeros(5000, device="cuda"), torch.zeros(3, device="cuda", dtype=BF16)]
+    block.clip_gradients(zeros, 1.0, norm)
+    assert norm.item() == 0 and all((z == 0).all() for z in zeros)
+    # one element of 1e-20 among zeros
+    zeros[0][4321] = 1e-25
+    block.gradient_norm(zeros, norm)
+    assert abs(norm.item() - 1e-25) < 1e-31
+
+
+def test_clip_infinities_and_nan():
+    a, b = torch.ones(9000, device="cuda", dtype=BF16), torch.ones(100, device="cuda")
+    a[5] = float("inf")
+    norm = poisoned((1,), FP32)
+    block.clip_gradients([a, b], 1.0, norm)
+    assert norm.item() == float("inf")
+    assert torch.isnan(a[5]) and (a[6:] == 0).all() and (b == 0).all()
+    a, b = torch.ones(9000, device="cuda", dtype=BF16), torch.ones(100, device="cuda")
+    a[5] = float("nan")
+    block.clip_gradients([a, b], 1.0, norm)
+    assert torch.isnan(norm).all() and torch.isnan(a).all() and torch.isnan(b).all()
+
+
+def test_clip_of_nothing():
+    norm = poisoned((1,), FP32)
+    block.clip_gradients([torch.empty(0, device="cuda"), torch.empty((3, 0), device="cuda")], 1.0, norm)
+    assert norm.item() == 0
+    block.gradient_norm([torch.empty(0, device="cuda")], norm.fill_(3))
+    assert norm.item() == 0
+
+
+def test_clip_refuses_results_that_meet_others():
+    a = torch.ones(100, device="cuda")
+    norm = poisoned((1,), FP32)
+    for grads, outs in (([a, a], None), ([a[:60], a[50:]], None), ([a[:50]], [a[10:60]]), ([a[:1]], [norm])):
+        with pytest.raises(block.CconvError):
+            block.clip_gradients(grads, 1.0, norm, outs=outs)
+    block.clip_gradients([a, a], 1.0, norm, outs=[torch.empty_like(a), torch.empty_like(a)])  # read twice: counted twice
+    assert abs(norm.item() - 200 ** 0.5) < 1e-5
+    with pytest.raises(ValueError):
+        block.clip_gradients([a], 1.0, norm, outs=[a[:50]])
+    with pytest.raises(ValueError):
+        block.TensorList([a, torch.ones(3)])
+    with pytest.raises(ValueError):
+        block.TensorList([torch.ones((4, 4, 4), device="cuda")[::2, ::2, ::2]])
+    for bad in (-1.0, float("nan")):
+        with pytest.raises(block.CconvError):
+            block.clip_gradients([a], bad, norm)
