@@ -9,6 +9,7 @@
  *   8-bit product   C[m,n] = sum_kb (sa[m,kb] sb[n/128,kb]) sum_{k in block kb} A[m,k] B[n,k]
  *   quantisation    8-bit values (e4m3) and a scale for each 1 x 128 or 128 x 128 block
  *   4-bit product   C[m,n] = sum_g s[n,g] sum_{k in group g} (q[n,k] - z[n,g]) X[m,k], and the quantiser of its weights
+ *   mixture         y = sum_j p_j ffn_{e_j}(x) over the k of E experts that a router scores highest, for a few tokens
  *   clipping        norm over all elements of a list of gradients, and factor = min(1, max_norm / (norm + eps))
  *   norm in 8 bits  the residual norm whose x is written as 8-bit values and scales
  *
@@ -205,6 +206,33 @@ typedef struct {
 } cconv_quantize_groups_args;
 
 int cconv_quantize_groups(const cconv_quantize_groups_args* args, void* cuda_stream);
+
+/* ---- mixture of experts, for a few tokens --------------------------------------------------------
+ * logits = x Wr^T; token t goes through the top_k experts of the largest logits, in falling order (of equal ones the
+ * lower number first; a NaN counts as the lowest), with weights p = softmax over them (normalize 1) or over all
+ * experts (normalize 0):   out[t] = sum_j p_j (act(x Wg_e^T) * (x Wu_e^T)) Wd_e^T,  e = ids[t][j].
+ * Without a router ids and weights are read instead; numbers that are no expert's add nothing (those of other
+ * ranks, say), and an expert that a token names twice counts with both weights.
+ * The weights of each expert in use are read once for 64 tokens; calls of more run 64 at a time. */
+typedef struct {
+  int64_t T, D, F, E;  /* E at most 1024, T at most 2^20 */
+  int32_t dtype;       /* CCONV_TYPE_BF16 or _FP16, of x, the weights' matrices and out */
+  int32_t act, top_k;  /* top_k: 1 to 32, at most E where there is a router */
+  int32_t normalize;   /* 0 or 1 */
+  cconv_matrix x;      /* [T][D] */
+  cconv_matrix router; /* [E][D]; absent: see above */
+  cconv_matrix w_gate, w_up; /* [F][D] of expert 0 */
+  cconv_matrix w_down;       /* [D][F] of expert 0 */
+  int64_t gate_stride, up_stride, down_stride; /* elements from an expert's matrix to the next one's */
+  cconv_matrix ids;    /* [T][top_k] int32; out with a router, in without */
+  cconv_matrix weights; /* [T][top_k] fp32; out with a router, in without */
+  cconv_matrix out;    /* out: [T][D] */
+  void* workspace;
+  uint64_t workspace_bytes;
+} cconv_moe_args;
+
+int64_t cconv_moe_workspace(const cconv_moe_args* args); /* (a router of NULL is absent) */
+int cconv_moe_forward(const cconv_moe_args* args, void* cuda_stream);
 
 /* ---- the norm of a list of gradients, and clipping -------------------------------------------------
  * norm = sqrt(sum of squares over all elements), the sum in 64 bits, rounded to fp32; every element times

@@ -7,6 +7,7 @@
     quantize_blocks                                   the 8-bit values and the scales
     int4_product                                      4-bit weights with a scale for each group of a row
     quantize_groups                                   those weights, scales and zero points
+    moe_forward                                       a mixture-of-experts layer for a few tokens
     gradient_norm, clip_gradients                     the norm over a list of gradients, and their clipping
 
 Argument marshalling only: every step runs in ``libcconv.so``.  Results go to tensors that the caller
@@ -34,7 +35,8 @@ EXPORTS = (
     "cconv_residual_norm_backward_workspace", "cconv_residual_norm_forward", "cconv_residual_norm_backward",
     "cconv_residual_norm_quantize",
     "cconv_fp8_product_workspace", "cconv_fp8_product", "cconv_quantize_blocks", "cconv_int4_product_workspace",
-    "cconv_int4_product", "cconv_quantize_groups", "cconv_clip_workspace",
+    "cconv_int4_product", "cconv_quantize_groups", "cconv_moe_workspace",
+    "cconv_moe_forward", "cconv_clip_workspace",
     "cconv_gradient_norm", "cconv_clip_gradients", "cconv_block_status",
 )
 
@@ -47,6 +49,7 @@ _FP8 = struct.Struct("qqqii" + _MAT * 5)
 _QUANT = struct.Struct("qqii" + _MAT * 3)
 _INT4 = struct.Struct("qqqiiii" + _MAT * 5)
 _GROUPS = struct.Struct("qqiiii" + _MAT * 4)
+_MOE = struct.Struct("qqqqiiii" + _MAT * 5 + "qqq" + _MAT * 3)
 _TENSOR = struct.Struct("Pqqqqii")
 _CLIP = struct.Struct("qPPffiiP")
 _TWO = struct.Struct(_MAT * 2)  # behind the norm's, in the call with 8-bit results
@@ -417,6 +420,54 @@ def quantize_groups(w, q, scale, zero=None, group=128, stream=None):
                         *(_NONE if zero is None else _mat(zero, (N, groups), u8, dev, "zero")))
     _call("cconv_quantize_groups", args, dev, stream)
     return q, scale, zero
+
+
+# ---- mixture of experts ------------------------------------------------------------------------------
+
+def _experts(t, shape, dtype, dev, name):
+    """((address, row stride, column stride) of expert 0's matrix, elements to the next one's), checked."""
+    if t.dtype is not dtype or t.get_device() != dev or t.shape != shape:
+        raise ValueError(f"{name} must be a {dtype} tensor of shape {tuple(shape)} on cuda:{dev}, "
+                         f"got {t.dtype} {tuple(t.shape)} on {t.device}")
+    expert, rows, cols = t.stride()
+    return (t.data_ptr(), rows, cols), expert
+
+
+def _moe_args(x, w_router, w_gate, w_up, w_down, out, ids, weights, act, normalize):
+    dtype, dev = _type(x, "x", _HALF_TYPES)
+    T, D = x.shape
+    if w_gate.dim() != 3:
+        raise ValueError(f"w_gate must have the dimensions experts, hidden channels, channels, got shape {tuple(w_gate.shape)}")
+    E, F, dt = w_gate.shape[0], w_gate.shape[1], x.dtype
+    if ids.dim() != 2 or ids.shape[1] < 1:
+        raise ValueError(f"ids must be a matrix with a column for each choice, got shape {tuple(ids.shape)}")
+    top_k = ids.shape[1]
+    gate, gate_stride = _experts(w_gate, (E, F, D), dt, dev, "w_gate")
+    up, up_stride = _experts(w_up, (E, F, D), dt, dev, "w_up")
+    down, down_stride = _experts(w_down, (E, D, F), dt, dev, "w_down")
+    return _MOE.pack(T, D, F, E, dtype, act, top_k, int(normalize), x.data_ptr(), *x.stride(),
+                     *(_NONE if w_router is None else _mat(w_router, (E, D), dt, dev, "w_router")), *gate, *up, *down,
+                     gate_stride, up_stride, down_stride, *_mat(ids, (T, top_k), torch.int32, dev, "ids"),
+                     *_mat(weights, (T, top_k), torch.float32, dev, "weights"), *_mat(out, (T, D), dt, dev, "out")), dev
+
+
+def moe_workspace(x, w_router, w_gate, w_up, w_down, out, ids, weights, act=ACT_SILU, normalize=True):
+    """cconv_moe_workspace: bytes of workspace of the call with these tensors."""
+    args, dev = _moe_args(x, w_router, w_gate, w_up, w_down, out, ids, weights, act, normalize)
+    return _need("cconv_moe_workspace", args, dev)
+
+
+def moe_forward(x, w_router, w_gate, w_up, w_down, out, ids, weights, act=ACT_SILU, normalize=True, workspace=None,
+                stream=None):
+    """cconv_moe_forward: out[t] = sum_j weights[t,j] (act(x Wg_e^T) * (x Wu_e^T)) Wd_e^T,  e = ids[t,j].
+
+    x, out [T, D]; w_gate, w_up [E, F, D]; w_down [E, D, F]; bf16 or fp16, any strides.  With ``w_router`` [E, D], ids
+    (int32 [T, k]) and weights (fp32 [T, k]) are written: the k experts of the largest x w_router^T in falling order
+    (of equal ones the lower number first) and the softmax over them (``normalize``) or over all experts.  Without
+    (None) they are read: numbers outside 0 .. E - 1 add nothing.  Made for a few tokens: 64 at a time."""
+    args, dev = _moe_args(x, w_router, w_gate, w_up, w_down, out, ids, weights, act, normalize)
+    _call_with_space("cconv_moe_forward", "cconv_moe_workspace", args, dev, workspace, stream)
+    return out, ids, weights
 
 
 # ---- the norm of a list of gradients, and clipping ----------------------------------------------------

@@ -13,6 +13,7 @@
 #include "block_fp8.h"
 #include "block_gemm.h"
 #include "block_int4.h"
+#include "block_moe.h"
 #include "block_norm.h"
 #include "block_quant.h"
 #include "host_setup.h"
@@ -441,6 +442,27 @@ int clip_call(const cconv_clip_args& a, bool clips, void* cuda_stream) {
   return rc;
 }
 
+// ---- mixture of experts --------------------------------------------------------------------------
+bool moe_sizes_ok(const cconv_moe_args& a) {
+  return a.T >= 0 && a.T <= (1 << 20) && length_ok(a.D) && length_ok(a.F) && a.E >= 0 && a.E <= kMostExperts &&
+         (a.dtype == CCONV_TYPE_BF16 || a.dtype == CCONV_TYPE_FP16) && a.act >= CCONV_ACT_SILU && a.act <= CCONV_ACT_RELU &&
+         a.top_k >= 1 && a.top_k <= kMostChosen && (a.normalize == 0 || a.normalize == 1) &&
+         (!a.router.data || a.top_k <= a.E || a.T == 0) && double(a.D) * a.F < 1e12 && double(a.T) * a.D < 1e15 &&
+         double(a.T) * a.F < 1e13;
+}
+bool moe_empty(const cconv_moe_args& a) { return a.T == 0 || a.D == 0 || a.F == 0 || a.E == 0; }
+// Whether anything but zeros comes of the call: without hidden channels the router still chooses.
+bool moe_runs(const cconv_moe_args& a) { return a.T && a.D && a.E && (a.F || a.router.data); }
+// The matrices of all experts as one vector of their elements' hull; false if it is none.
+bool experts_ok(const cconv_matrix& m, int64_t stride, int64_t rows, int64_t cols, int64_t experts, int64_t* n) {
+  for (int64_t s : {m.row_stride, m.col_stride, stride})
+    if (s < 0 || s > kMaxStride) return false;
+  const double last = double(rows - 1) * m.row_stride + double(cols - 1) * m.col_stride + double(experts - 1) * stride;
+  if (last > 2.0e18) return false;
+  *n = (rows - 1) * m.row_stride + (cols - 1) * m.col_stride + (experts - 1) * stride + 1;
+  return true;
+}
+
 bool group_ok(int32_t group) { return group == 32 || group == 64 || group == 128; }
 bool int4_sizes_ok(const cconv_int4_product_args& a) {
   return length_ok(a.M) && length_ok(a.N) && length_ok(a.K) && (a.dtype == CCONV_TYPE_BF16 || a.dtype == CCONV_TYPE_FP16) &&
@@ -714,6 +736,60 @@ int cconv_quantize_groups(const cconv_quantize_groups_args* args, void* cuda_str
     if (sms < 0) return sms;
     return o.run(cuda_stream, sms, [&] {
       return block_cuda_error(run_quantize_groups(a, static_cast<cudaStream_t>(cuda_stream)), "cconv_quantize_groups");
+    });
+  });
+}
+
+int64_t cconv_moe_workspace(const cconv_moe_args* args) {
+  return guarded([&]() -> int64_t {
+    if (!args || !moe_sizes_ok(*args)) return CCONV_EINVAL;
+    const int sms = block_sm_count();
+    if (sms < 0) return sms;
+    return moe_runs(*args) ? moe_workspace(*args, sms) : 0;
+  });
+}
+
+int cconv_moe_forward(const cconv_moe_args* args, void* cuda_stream) {
+  return guarded([&]() -> int {
+    if (!args || !moe_sizes_ok(*args)) return CCONV_EINVAL;
+    const cconv_moe_args& a = *args;
+    const bool routes = a.router.data != nullptr;
+    // (a router that must choose among no experts, or from no channels, has nothing to choose by)
+    if (routes && a.T && (a.E == 0 || a.D == 0)) return CCONV_EINVAL;
+    Operands o;
+    o.in(a.x, a.T, a.D, 2);
+    if (routes) o.in(a.router, a.E, a.D, 2);
+    if (!moe_empty(a)) {
+      int64_t n[3];
+      if (!experts_ok(a.w_gate, a.gate_stride, a.F, a.D, a.E, &n[0]) || !experts_ok(a.w_up, a.up_stride, a.F, a.D, a.E, &n[1]) ||
+          !experts_ok(a.w_down, a.down_stride, a.D, a.F, a.E, &n[2]))
+        return CCONV_EINVAL;
+      o.in(a.w_gate.data, n[0], 2);
+      o.in(a.w_up.data, n[1], 2);
+      o.in(a.w_down.data, n[2], 2);
+    }
+    if (routes) {
+      o.out(a.ids, a.T, a.top_k, 4);
+      o.out(a.weights, a.T, a.top_k, 4);
+    } else {
+      o.in(a.ids, a.T, a.top_k, 4);
+      o.in(a.weights, a.T, a.top_k, 4);
+    }
+    o.out(a.out, a.T, a.D, 2);
+    if (!o.distinct()) return CCONV_EINVAL;
+    if (!o.writes()) return CCONV_OK;
+    const int sms = block_sm_count();
+    if (sms < 0) return sms;
+    o.workspace(a.workspace, a.workspace_bytes, moe_runs(a) ? moe_workspace(a, sms) : 0);
+    if (!o.distinct()) return CCONV_EINVAL;
+    cudaStream_t s = static_cast<cudaStream_t>(cuda_stream);
+    return o.run(cuda_stream, sms, [&]() -> int {
+      if (moe_runs(a)) {
+        const int rc = run_moe(a, sms, s);
+        if (rc != CCONV_OK) return rc;
+      }
+      if (moe_empty(a)) BLOCK_CUDA(zero_out(a.out, a.T, a.D, 2, s));
+      return CCONV_OK;
     });
   });
 }

@@ -1,5 +1,5 @@
 """The operators that serve the feed-forward sub-block against plain 64-bit forms: norms with 8-bit results,
-products with 4-bit weights and their quantiser.
+products with 4-bit weights and their quantiser, clipping, mixtures of experts.
 
 Tolerances.  u is a type's unit roundoff, eps / 2 (bf16 2^-8, fp16 2^-11, fp32 2^-24, e4m3 2^-4).  Sums of n products
 in fp32 are off by at most (n + 16) 2^-23 of the sum of the products' sizes.  A result's own rounding adds u of its
@@ -508,3 +508,189 @@ def test_clip_refuses_results_that_meet_others():
     for bad in (-1.0, float("nan")):
         with pytest.raises(block.CconvError):
             block.clip_gradients([a], bad, norm)
+
+
+# ---- mixture of experts -----------------------------------------------------------------------------
+
+class Moe:
+    """A layer's operands, exact values and tolerances."""
+
+    def __init__(self, T, D, F, E, k, dtype=BF16, act="silu", normalize=True, seed=0):
+        g = gen(seed + T + 3 * D + 5 * F + 7 * E + 11 * k)
+        self.T, self.D, self.F, self.E, self.k, self.dtype, self.act, self.normalize = T, D, F, E, k, dtype, act, normalize
+        self.x = normal(g, (T, D), dtype)
+        self.router = normal(g, (E, D), dtype, max(D, 1) ** -0.5)
+        self.wg, self.wu = (normal(g, (E, F, D), dtype, max(D, 1) ** -0.5) for _ in range(2))
+        self.wd = normal(g, (E, D, F), dtype, max(F, 1) ** -0.5)
+
+    def run(self, ids=None, weights=None, out=None, **kw):
+        routed = ids is None
+        out = poisoned((self.T, self.D), self.dtype) if out is None else out
+        ids = torch.full((self.T, self.k), -7, device="cuda", dtype=torch.int32) if routed else ids
+        weights = poisoned((self.T, self.k), FP32) if weights is None else weights
+        return block.moe_forward(self.x, self.router if routed else None, self.wg, self.wu, self.wd, out, ids, weights,
+                                 act=block.ACTS[self.act], normalize=self.normalize, **kw)
+
+    def check_routes(self, ids, weights, what=""):
+        x, r = self.x.double(), self.router.double()
+        logits = x @ r.T
+        e = sum_err(self.D) * (x.abs() @ r.abs().T).amax(1, keepdim=True)
+        assert (ids >= 0).all() and (ids < self.E).all(), what
+        assert all(len(set(row)) == self.k for row in ids.tolist()), what
+        got = logits.gather(1, ids.long())
+        best = logits.sort(1, descending=True)[0][:, :self.k]
+        assert ((got - best).abs() <= 2 * e).all(), what  # the right ones, in order, but for ties within the sums' rounding
+        p = torch.softmax(got if self.normalize else logits, 1)
+        p = p if self.normalize else p.gather(1, ids.long())
+        # a shift of e in every logit changes p by 2 e of itself; the exponential, the sum and the quotient
+        close(weights, p, p * (2 * e * 1.01 + (self.E + 40) * 2.0 ** -23), what + " weights")
+
+    def check_out(self, out, ids, weights, what=""):
+        from test_gpu_block import act64
+        u = U[self.dtype]
+        y = torch.zeros((self.T, self.D), device="cuda", dtype=torch.float64)
+        ey = torch.zeros_like(y)
+        x = self.x.double()
+        for e in range(self.E):
+            w = (weights.double() * (ids == e)).sum(1)
+            rows = (ids == e).any(1).nonzero()[:, 0]
+            if not len(rows):
+                continue
+            xs, wg, wu, wd = x[rows], self.wg[e].double(), self.wu[e].double(), self.wd[e].double()
+            g, v = xs @ wg.T, xs @ wu.T
+            eg, ev = sum_err(self.D) * (xs.abs() @ wg.abs().T), sum_err(self.D) * (xs.abs() @ wu.abs().T)
+            a, _ = act64(self.act, g)
+            h = a * v
+            # as the feed-forward block's; h in two parts is rounded to u^2
+            eh = 1.13 * eg * (v.abs() + ev) + (a.abs() + 1e-6) * ev + 2.0 ** -20 * (h.abs() + g.abs() * v.abs()) + u * u * h.abs() + TINY[self.dtype]
+            p = w[rows, None]
+            y[rows] += p * (h @ wd.T)
+            ey[rows] += p.abs() * (eh @ wd.abs().T + sum_err(2 * self.F + 2 * self.k) * (h.abs() @ wd.abs().T))
+        close(out, y, 1.01 * (ey + u * y.abs()) + TINY[self.dtype], what + " out")
+
+
+MOE_SHAPES = [(1, 64, 64, 4, 2), (1, 2048, 1024, 64, 8), (2, 8, 8, 1, 1), (3, 72, 40, 5, 5), (5, 1000, 1304, 10, 3), (7, 65, 33, 6, 2),
+              (8, 512, 136, 16, 4), (9, 130, 264, 3, 1), (16, 256, 96, 40, 6), (17, 1, 1, 9, 3), (31, 384, 200, 128, 8),
+              (33, 96, 120, 7, 7), (64, 512, 256, 20, 4), (65, 128, 72, 12, 3), (130, 64, 136, 4, 2), (4, 4800, 64, 8, 2),
+              (6, 40, 16, 1000, 32), (40, 66, 34, 300, 5)]
+
+
+@pytest.mark.parametrize("T,D,F,E,k", MOE_SHAPES)
+@pytest.mark.parametrize("dtype", [BF16, FP16])
+def test_moe_forward(T, D, F, E, k, dtype):
+    act = ["silu", "gelu", "gelu_tanh", "relu"][(T + D) % 4]
+    m = Moe(T, D, F, E, k, dtype, act, normalize=(T + F) % 2 == 0)
+    out, ids, weights = m.run()
+    what = f"{T}x{D}x{F} {k} of {E}"
+    m.check_routes(ids, weights, what)
+    m.check_out(out, ids, weights, what)
+    # the same choice given: the same result
+    again, _, _ = m.run(ids=ids, weights=weights)
+    assert torch.equal(again, out)
+
+
+def test_moe_ties_and_order():
+    """Whole numbers, so that scores are exact and many are equal: the lower number goes first."""
+    g = gen(9)
+    m = Moe(40, 64, 32, 24, 6)
+    m.x = torch.randint(-2, 3, (40, 64), generator=g, device="cuda").to(BF16)
+    m.router = torch.randint(-1, 2, (24, 64), generator=g, device="cuda").to(BF16)
+    m.x[3] = 0
+    m.router[5] = m.router[4]
+    out, ids, weights = m.run()
+    logits = m.x.double() @ m.router.double().T
+    assert torch.equal(ids.long(), torch.sort(logits, dim=1, descending=True, stable=True)[1][:, :6])
+    assert ids[3].tolist() == list(range(6)) and torch.allclose(weights[3], torch.full((6,), 1 / 6, device="cuda"))
+    m.check_out(out, ids, weights)
+
+
+def test_moe_given_choices():
+    """Numbers that are no expert's, experts named twice, negative and zero weights, one expert for all, none for some."""
+    g = gen(10)
+    for T in (1, 6, 40, 70):
+        m = Moe(T, 128, 72, 8, 5)
+        ids = torch.randint(-3, 11, (T, 5), generator=g, device="cuda", dtype=torch.int32)
+        weights = normal(g, (T, 5), FP32)
+        weights[0, 1] = 0
+        ids[T // 2] = 3
+        if T > 1:
+            ids[1] = -1
+        out, _, _ = m.run(ids=ids, weights=weights)
+        m.check_out(out, ids, weights, f"T {T}")
+        assert T == 1 or (out[1] == 0).all()
+        ids.fill_(7)
+        m.check_out(m.run(ids=ids, weights=weights)[0], ids, weights, "one expert")
+        ids.fill_(1 << 30)
+        assert (m.run(ids=ids, weights=weights)[0] == 0).all()
+
+
+@pytest.mark.parametrize("T", [1, 5, 70])
+@pytest.mark.parametrize("D,F", [(128, 96), (100, 60), (51, 33)])
+def test_moe_strided_operands(T, D, F):
+    m = Moe(T, D, F, 6, 3, FP16)
+    exp = m.run()
+
+    def transposed(t):
+        return t.transpose(-1, -2).contiguous().transpose(-1, -2)
+
+    def padded(by, pad):
+        def f(t):
+            big = torch.full((*t.shape[:-1], t.shape[-1] + pad), 9.0, device="cuda", dtype=t.dtype)
+            big[..., by:by + t.shape[-1]] = t
+            return big[..., by:by + t.shape[-1]]
+        return f
+
+    def experts_inside(t):  # experts next to one another for each row
+        return t.transpose(0, 1).contiguous().transpose(0, 1) if t.dim() == 3 else t
+    for store in (transposed, padded(8, 16), padded(2, 4), padded(1, 3), experts_inside):
+        h = Moe(T, D, F, 6, 3, FP16)
+        for name in ("x", "router", "wg", "wu", "wd"):
+            setattr(h, name, store(getattr(m, name)))
+        big = torch.full((T + 1, D + 3), 7.0, device="cuda", dtype=FP16)
+        ids = torch.full((3, T), -1, device="cuda", dtype=torch.int32).t()
+        got = block.moe_forward(h.x, h.router, h.wg, h.wu, h.wd, big[1:, 2:D + 2], ids, torch.empty((3, T), device="cuda").t())
+        for a, b in zip(got, exp):
+            assert torch.equal(a, b)
+        big[1:, 2:D + 2] = 7.0
+        assert (big == 7).all()
+    # gate and up as halves of one array, which may lie in different orders
+    both = torch.cat([m.wg, m.wu], 1)
+    m.wg, m.wu = both[:, :F], both[:, F:]
+    assert torch.equal(m.run()[0], exp[0])
+    m.wu = transposed(m.wu)
+    assert torch.equal(m.run()[0], exp[0])
+
+
+def test_moe_of_nothing():
+    m = Moe(4, 32, 0, 6, 2)
+    out, ids, weights = m.run()
+    assert (out == 0).all()
+    m.check_routes(ids, weights)
+    for T, D, F, E in ((0, 32, 16, 6), (3, 0, 16, 6), (3, 32, 16, 0), (3, 32, 0, 4)):
+        m = Moe(T, D, F, E, 2)
+        out, _, _ = m.run(ids=torch.zeros((T, 2), device="cuda", dtype=torch.int32), weights=torch.ones((T, 2), device="cuda"))
+        assert (out == 0).all()
+
+
+def test_moe_infinities_and_nan():
+    m = Moe(6, 64, 48, 5, 2)
+    exp, _, _ = m.run()
+    m.x[2, 5] = float("nan")
+    out, ids, weights = m.run()
+    assert torch.isnan(out[2]).all() and torch.isnan(weights[2]).all() and ids[2].tolist() == [0, 1]
+    keep = [0, 1, 3, 4, 5]
+    assert torch.equal(out[keep], exp[keep])  # (a token's neighbours do not notice)
+
+
+def test_moe_offsets_beyond_32_bits():
+    """Experts so far apart that their offsets pass 2^32 bytes."""
+    m = Moe(3, 64, 16, 4, 4)
+    exp = m.run()[0]
+    big = torch.empty(3 * (1 << 31) + 64 * 16, device="cuda", dtype=BF16)
+    for name in ("wg", "wu", "wd"):
+        t = getattr(m, name)
+        far = big.as_strided(t.shape, (1 << 31, t.shape[2], 1))
+        far.copy_(t)
+        old, _ = t, setattr(m, name, far)
+        assert torch.equal(m.run()[0], exp), name
+        setattr(m, name, old)
