@@ -6,11 +6,10 @@
 //
 // What bounds it is HBM: the weights of the experts in use, each read once for all tokens that chose it.  Three
 // launches, which follow one another without a gap (a kernel is put in place while the one in front ends):
-//   router   one cluster of eight blocks for 64 tokens: logits, a barrier, the choice
-//   gate/up  tiles of 8 hidden channels of an expert in use, its tokens gathered as columns; h in two 16-bit parts,
-//            whose sum has twice the type's precision
-//   down     tiles of 16 or 8 channels through all experts in use; a column is a token, so that the weighted sums of
-//            all its experts stay in one accumulator, added up in the order of the experts
+//   router   one cluster of eight blocks for 64 tokens: scores, a barrier, the choice
+//   gate/up  tiles of 8 hidden channels of an expert in use, its tokens gathered as columns, 8 or 16 at a time; h in
+//            two 16-bit parts, whose sum has twice the type's precision
+//   down     tiles of 16 channels through all experts in use, in one block or shared by a cluster
 // Both weight kernels build the lists of who goes where themselves from the choice (a microsecond less than to wait
 // for a kernel that would), stream weights through rings in shared memory, one a warp, and multiply by warp-wide
 // matrix instructions (m16n8): tcgen05 would want tiles that a few tokens leave almost empty.
@@ -30,7 +29,7 @@ namespace cconv {
 namespace {
 
 constexpr int kTokens = 64;  // of a launch of the weight kernels
-constexpr int kWarps = 8, kStages = 4, kUnitBytes = 2048;
+constexpr int kWarps = 8;
 constexpr int kRouterBlocks = 8, kRouterWarps = 16;
 
 struct MoeParams {
@@ -40,7 +39,6 @@ struct MoeParams {
   int T, E, k, act, dtype, normalize;
   const char* router;  // rows readable like x's
   int64_t router_rs;
-  float* logits;       // [T][E]
   int* ids; int64_t ids_rs, ids_cs;
   float* weights; int64_t weights_rs, weights_cs;
   // expert matrices: element strides
@@ -64,76 +62,118 @@ __device__ __forceinline__ uint64_t warp_max(uint64_t v) {
   const uint32_t lo = __reduce_max_sync(0xffffffffu, uint32_t(v >> 32) == hi ? uint32_t(v) : 0u);
   return uint64_t(hi) << 32 | lo;
 }
+__device__ __forceinline__ float load_cluster(uint32_t at) {
+  float v;
+  asm volatile("ld.shared::cluster.f32 %0, [%1];" : "=f"(v) : "r"(at) : "memory");
+  return v;
+}
 
-// Experts are dealt to the blocks of the cluster in neighbouring ranges; a block's warps share the channels.  Then each
-// warp of the cluster chooses for tokens of its own.
+// Channels are dealt to the blocks of the cluster, and a block's share of them and 16 experts at a time to its warps:
+// with the usual sizes a warp's loads are all on their way at once.  Partial scores [slice][token][expert] lie in
+// shared memory, a block adds its own up, and the warp that chooses for a token adds up the blocks'.
 template <typename T, int kNt>
-__global__ void __launch_bounds__(kRouterWarps * 32) cconv_moe_router_kernel(const MoeParams p) {
-  __shared__ float sums[kRouterWarps][128];
+__global__ void __launch_bounds__(kRouterWarps * 32) cconv_moe_router_kernel(const MoeParams p, const int chunk) {
+  extern __shared__ __align__(128) uint8_t smem[];
+  float* const part = reinterpret_cast<float*>(smem);
   start_in_order();
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, g = lane >> 2, q = lane & 3;
-  const int rank = int(cluster_ctarank()), t0 = int(blockIdx.x / kRouterBlocks) * kTokens, tokens = min(kTokens, p.T - t0);
-  const int per = (p.E + kRouterBlocks - 1) / kRouterBlocks, e0 = rank * per, e1 = min(p.E, e0 + per);
-  for (int m = e0; m < e1; m += 16) {
-    const char* r0 = p.router + int64_t(min(m + g, p.E - 1)) * p.router_rs;
-    const char* r1 = p.router + int64_t(min(m + g + 8, p.E - 1)) * p.router_rs;
-    float acc[kNt][4] = {};
-    const int64_t units = (p.x_k + 31) / 32;
-#pragma unroll 2
-    for (int64_t u = warp; u < units; u += kRouterWarps) {
-      const int64_t k0 = u * 32 + q * 8;
-      const bool in = k0 < p.x_k;
-      const uint4 none = make_uint4(0, 0, 0, 0);
-      const uint4 a0 = in ? *reinterpret_cast<const uint4*>(r0 + k0 * 2) : none;
-      const uint4 a1 = in ? *reinterpret_cast<const uint4*>(r1 + k0 * 2) : none;
+  const int rank = int(cluster_ctarank()), t0 = int(blockIdx.x / kRouterBlocks) * chunk, tokens = min(chunk, p.T - t0);
+  const int groups = (p.E + 15) / 16, slices = groups >= kRouterWarps ? 1 : kRouterWarps / groups;
+  const int units = int((p.x_k + 31) / 32), all = slices * kRouterBlocks, slice = warp / groups;
+  if (slice < slices) {
+    // of the cluster's slices, this warp's
+    const int mine = rank * slices + slice, u0 = int(int64_t(units) * mine / all), u1 = int(int64_t(units) * (mine + 1) / all);
+    for (int m = slices == 1 ? warp : warp % groups; m < groups; m += kRouterWarps) {
+      const char* r0 = p.router + int64_t(min(16 * m + g, p.E - 1)) * p.router_rs;
+      const char* r1 = p.router + int64_t(min(16 * m + g + 8, p.E - 1)) * p.router_rs;
+      float acc[kNt][4] = {};
+#pragma unroll 4
+      for (int u = u0; u < u1; ++u) {
+        const int64_t k0 = int64_t(u) * 32 + q * 8;
+        const bool in = k0 < p.x_k;
+        const uint4 none = make_uint4(0, 0, 0, 0);
+        const uint4 a0 = in ? *reinterpret_cast<const uint4*>(r0 + k0 * 2) : none;
+        const uint4 a1 = in ? *reinterpret_cast<const uint4*>(r1 + k0 * 2) : none;
 #pragma unroll
-      for (int e = 0; e < kNt; ++e) {
-        const int t = 8 * e + g;
-        const uint4 v = in && t < tokens ? *reinterpret_cast<const uint4*>(p.x + int64_t(t0 + t) * p.x_rs + k0 * 2) : none;
-        mma16<T>(acc[e], a0.x, a1.x, a0.y, a1.y, v.x, v.y);
-        mma16<T>(acc[e], a0.z, a1.z, a0.w, a1.w, v.z, v.w);
+        for (int e = 0; e < kNt; ++e) {
+          const int t = 8 * e + g;
+          const uint4 v = in && t < tokens ? *reinterpret_cast<const uint4*>(p.x + int64_t(t0 + t) * p.x_rs + k0 * 2) : none;
+          mma16<T>(acc[e], a0.x, a1.x, a0.y, a1.y, v.x, v.y);
+          mma16<T>(acc[e], a0.z, a1.z, a0.w, a1.w, v.z, v.w);
+        }
       }
+#pragma unroll
+      for (int e = 0; e < kNt; ++e)
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+          const int row = 16 * m + g + (i >> 1) * 8, t = 8 * e + 2 * q + (i & 1);
+          if (row < p.E && t < tokens) part[(slice * tokens + t) * p.E + row] = acc[e][i];
+        }
     }
-#pragma unroll
-    for (int e = 0; e < kNt; ++e) {
-      if (8 * e >= tokens) break;
-      __syncthreads();
-#pragma unroll
-      for (int i = 0; i < 4; ++i) sums[warp][i * 32 + lane] = acc[e][i];
-      __syncthreads();
-      if (threadIdx.x < 128) {
-        float s = 0.0f;
-#pragma unroll
-        for (int w = 0; w < kRouterWarps; ++w) s += sums[w][threadIdx.x];
-        const int i = threadIdx.x >> 5;
-        const int row = m + g + (i >> 1) * 8, t = 8 * e + 2 * q + (i & 1);
-        if (row < e1 && t < tokens) p.logits[int64_t(t0 + t) * p.E + row] = s;
-      }
+  }
+  __syncthreads();
+  if (slices > 1) {
+    for (int i = threadIdx.x; i < tokens * p.E; i += kRouterWarps * 32) {
+      float v = part[i];
+      for (int o = 1; o < slices; ++o) v += part[o * tokens * p.E + i];
+      part[i] = v;
     }
   }
   cluster_sync_all();
-  for (int t = rank * kRouterWarps + warp; t < tokens; t += kRouterBlocks * kRouterWarps) {
-    const float* row = p.logits + int64_t(t0 + t) * p.E;
+  for (int t = rank + kRouterBlocks * warp; t < tokens; t += kRouterBlocks * kRouterWarps) {
+    // the token's scores, whole: the first of each lane's in registers, the others back in this block's memory
+    float* const row = part + t * p.E;
+    float score[4];
+    const uint32_t at = smem_u32(row);
+    for (int e = lane, i = 0; e < p.E; e += 32, ++i) {
+      float v[kRouterBlocks], sum = 0.0f;
+#pragma unroll
+      for (int r = 0; r < kRouterBlocks; ++r) v[r] = load_cluster(cluster_map_shared(at + e * 4, r));
+#pragma unroll
+      for (int r = 0; r < kRouterBlocks; ++r) sum += v[r];
+      if (i < 4) {
+#pragma unroll
+        for (int j = 0; j < 4; ++j) score[j] = i == j ? sum : score[j];
+      } else {
+        row[e] = sum;  // (no other block reads this token's scores)
+      }
+    }
+    uint64_t key[4];
+#pragma unroll
+    for (int j = 0; j < 4; ++j) key[j] = 32 * j + lane < p.E ? rank_of(score[j], 32 * j + lane) : 0;
     uint64_t before = ~uint64_t(0);
     float mine = 0.0f, largest = 0.0f;  // lane j: the j-th choice's score
     int id = 0;
     for (int j = 0; j < p.k; ++j) {
       uint64_t best = 0;
-      for (int e = lane; e < p.E; e += 32) {
+#pragma unroll
+      for (int i = 0; i < 4; ++i)
+        if (key[i] < before && key[i] > best) best = key[i];
+      for (int e = lane + 128; e < p.E; e += 32) {
         const uint64_t r = rank_of(row[e], e);
         if (r < before && r > best) best = r;
       }
       before = warp_max(best);
-      const int e = int(~uint32_t(before));
-      const float score = row[e];
-      if (j == 0) largest = score;
-      if (lane == j) mine = score, id = e;
+      const int e = int(~uint32_t(before)), place = e >> 5;
+      float v = 0.0f;
+      if (place >= 4) {
+        v = (e & 31) == lane ? row[e] : 0.0f;
+      } else {
+#pragma unroll
+        for (int i = 0; i < 4; ++i) v = place == i ? score[i] : v;
+      }
+      v = __shfl_sync(0xffffffffu, v, e & 31);
+      if (j == 0) largest = v;
+      if (lane == j) mine = v, id = e;
     }
     float sum = 0.0f;
     if (p.normalize) {
       sum = lane < p.k ? expf(mine - largest) : 0.0f;
     } else {
-      for (int e = lane; e < p.E; e += 32) sum += expf(row[e] - largest);
+#pragma unroll
+      for (int i = 0; i < 4; ++i)
+        if (32 * i + lane < p.E) sum += expf(score[i] - largest);
+      for (int e = lane + 128; e < p.E; e += 32) sum += expf(row[e] - largest);
     }
     sum = warp_sum(sum);
     if (lane < p.k) {
@@ -141,33 +181,38 @@ __global__ void __launch_bounds__(kRouterWarps * 32) cconv_moe_router_kernel(con
       p.weights[int64_t(t0 + t) * p.weights_rs + lane * p.weights_cs] = __fdiv_rn(expf(mine - largest), sum);
     }
   }
+  cluster_sync_all();  // no block leaves while others read its scores
 }
 
 // ---- who goes where --------------------------------------------------------------------------------
-// Of the tokens of a launch, in shared memory: the experts in use in ascending order, each with the set of its tokens
-// and where their pairs (token, choice) begin in `pairs`, ascending by token.  An expert that a token names twice counts
-// once, with both weights; numbers that are no expert's count for nothing.
+// Of the tokens of a launch, in shared memory: the pairs (token, choice) in the order of experts, of an expert
+// ascending by token, in groups of up to `most` of one expert.  An expert that a token names twice counts once, with
+// both weights; numbers that are no expert's count for nothing.
 struct Routes {
-  uint64_t* tokens;   // [used]: bit t
-  uint16_t* expert;   // [used]
-  uint16_t* first;    // [used]
+  uint64_t* tokens;   // [E]: bit t
+  float* weight;      // [pairs], as `pairs` (down kernel)
+  uint16_t *first_of;  // [E]
   uint16_t* pairs;    // [pairs]: t k + j
-  float* weight;      // [t k + j] (down kernel)
-  int used;
+  uint16_t *expert, *first;  // [groups]
+  uint8_t* count;     // [groups]
+  int groups;
 };
-constexpr int routes_bytes(int E, int pairs, bool weights) {
-  return E * 8 + E * 4 + (pairs + 1) / 2 * 4 + (weights ? pairs * 4 : 0);
+constexpr __host__ __device__ int most_groups(int E, int pairs, int most) { return (E < pairs ? E : pairs) + pairs / most; }
+constexpr int routes_bytes(int E, int pairs, int most, bool weights) {
+  return E * 10 + pairs * (weights ? 6 : 2) + most_groups(E, pairs, most) * 5 + 16;
 }
 
 template <bool kWeights>
-__device__ __forceinline__ Routes routes_of(const MoeParams& p, uint8_t* smem, int* scratch) {
+__device__ __forceinline__ Routes routes_of(const MoeParams& p, uint8_t* smem, int* scratch, int most) {
   const int E = p.E, pairs = p.T * p.k, tid = threadIdx.x, nt = kWarps * 32;
   Routes r;
   r.tokens = reinterpret_cast<uint64_t*>(smem);
   r.weight = reinterpret_cast<float*>(r.tokens + E);
-  r.expert = reinterpret_cast<uint16_t*>(r.weight + (kWeights ? pairs : 0));
-  r.first = r.expert + E;
-  r.pairs = r.first + E;
+  r.first_of = reinterpret_cast<uint16_t*>(r.weight + (kWeights ? pairs : 0));
+  r.pairs = r.first_of + E;
+  r.expert = r.pairs + pairs;
+  r.first = r.expert + most_groups(E, pairs, most);
+  r.count = reinterpret_cast<uint8_t*>(r.first + most_groups(E, pairs, most));
   for (int e = tid; e < E; e += nt) r.tokens[e] = 0;
   __syncthreads();
   auto id_of = [&](int t, int j) { return __ldg(p.ids + t * p.ids_rs + j * p.ids_cs); };
@@ -176,17 +221,17 @@ __device__ __forceinline__ Routes routes_of(const MoeParams& p, uint8_t* smem, i
     if (e >= 0 && e < E) atomicOr(reinterpret_cast<unsigned long long*>(r.tokens + e), 1ull << t);
   }
   __syncthreads();
-  // places of the experts in use: at most 1024 experts, 4 a thread, all threads' counts added up by the warps
-  uint64_t mine[4];
-  int n = 0, entries = 0;
+  // groups and pairs in front of each expert's: at most 1024 experts, 4 a thread
+  int n[4], groups = 0, entries = 0;
 #pragma unroll
   for (int i = 0; i < 4; ++i) {
     const int e = tid * 4 + i;
-    mine[i] = e < E ? r.tokens[e] : 0;
-    n += mine[i] != 0;
-    entries += __popcll(mine[i]);
+    n[i] = e < E ? __popcll(r.tokens[e]) : 0;
+    groups += (n[i] + most - 1) / most;
+    entries += n[i];
   }
-  int both = n | entries << 16, incl = both;  // (at most 1024 and 2048)
+  const int both = groups | entries << 16;  // (at most 1536 and 2048)
+  int incl = both;
 #pragma unroll
   for (int o = 1; o < 32; o <<= 1) {
     const int v = __shfl_up_sync(0xffffffffu, incl, o);
@@ -200,157 +245,172 @@ __device__ __forceinline__ Routes routes_of(const MoeParams& p, uint8_t* smem, i
     if (w < (tid >> 5)) base += scratch[w];
     total += scratch[w];
   }
-  r.used = total & 0xffff;
+  r.groups = total & 0xffff;
   int at = base & 0xffff, first = base >> 16;
 #pragma unroll
   for (int i = 0; i < 4; ++i) {
-    if (mine[i] == 0) continue;
-    r.tokens[at] = mine[i];  // (every thread has read its own; at <= its first)
-    r.expert[at] = uint16_t(tid * 4 + i);
-    r.first[at] = uint16_t(first);
-    ++at;
-    first += __popcll(mine[i]);
+    const int e = tid * 4 + i;
+    if (n[i]) r.first_of[e] = uint16_t(first);
+    for (int c = 0; c < n[i]; c += most, ++at) {
+      r.expert[at] = uint16_t(e);
+      r.first[at] = uint16_t(first + c);
+      r.count[at] = uint8_t(min(most, n[i] - c));
+    }
+    first += n[i];
   }
   __syncthreads();
   for (int i = tid; i < pairs; i += nt) {
     const int t = i / p.k, j = i - t * p.k, e = id_of(t, j);
     if (e < 0 || e >= E) continue;
     bool again = false;
-    for (int o = 0; o < j; ++o) again |= id_of(t, o) == e;
+    float w = kWeights ? __ldg(p.weights + t * p.weights_rs + j * p.weights_cs) : 0.0f;
+    for (int o = 0; o < p.k; ++o) {
+      if (o == j || id_of(t, o) != e) continue;
+      again |= o < j;
+      if (kWeights) w += __ldg(p.weights + t * p.weights_rs + o * p.weights_cs);
+    }
     if (again) continue;
-    int lo = 0, hi = r.used - 1;  // e's place
-    while (lo < hi) {
-      const int mid = (lo + hi) >> 1;
-      if (r.expert[mid] < e) lo = mid + 1;
-      else hi = mid;
-    }
-    r.pairs[r.first[lo] + __popcll(r.tokens[lo] & ((1ull << t) - 1))] = uint16_t(i);
-    if (kWeights) {
-      float w = 0.0f;
-      for (int o = j; o < p.k; ++o)
-        if (id_of(t, o) == e) w += __ldg(p.weights + t * p.weights_rs + o * p.weights_cs);
-      r.weight[i] = w;
-    }
+    const int to = r.first_of[e] + __popcll(r.tokens[e] & ((1ull << t) - 1));
+    r.pairs[to] = uint16_t(i);
+    if (kWeights) r.weight[to] = w;
   }
   __syncthreads();
   return r;
 }
 
-// ---- weights through a ring -------------------------------------------------------------------------
-// A unit is 16 segments of 128 bytes; segments of odd number have their halves swapped, so that the 16-byte words that
-// eight lanes read together lie in different banks.
+// ---- weights and tokens through a ring ---------------------------------------------------------------
+// A unit is segments of 128 bytes: 16 of weights' rows, then a column each.  Segments of odd number have their halves
+// swapped, so that the 16-byte words that eight lanes read together lie in different banks.
 __device__ __forceinline__ uint32_t place(int segment, int byte) { return segment * 128 + (byte ^ ((segment & 1) << 6)); }
 
-// Copies a unit: segment s is 64 elements from at(s), of which those before left(s) are there and the others zeros.
-template <int kBytes, typename At, typename Left>
-__device__ __forceinline__ void copy_unit_by(uint32_t to, int lane, At at, Left left) {
+// kBytes, or zeros, to shared memory, not waited for.
+template <int kBytes>
+__device__ __forceinline__ void copy_piece(uint32_t to, const char* from, bool there) {
+  const uint32_t n = there ? kBytes : 0;
+  if constexpr (kBytes == 16)
+    asm volatile("cp.async.cg.shared.global [%0], [%1], 16, %2;" ::"r"(to), "l"(from), "r"(n) : "memory");
+  else
+    asm volatile("cp.async.ca.shared.global [%0], [%1], %2, %3;" ::"r"(to), "l"(from), "n"(kBytes), "r"(n) : "memory");
+}
+// Copies the weights: segment s is 64 elements from at(s), of which the first `left` are there and the others zeros.
+template <int kBytes, typename At>
+__device__ __forceinline__ void copy_rows_by(uint32_t to, int lane, int left, At at) {
   constexpr int kAcross = 128 / kBytes;
 #pragma unroll
-  for (int i = 0; i < kUnitBytes / 32 / kBytes; ++i) {
+  for (int i = 0; i < 16 * kAcross / 32; ++i) {
     const int c = i * 32 + lane, seg = c / kAcross, off = c % kAcross * kBytes;
+    const bool there = off < left * 2;
     const char* from = at(seg);
-    const bool there = off < left(seg) * 2;
-    const uint32_t n = there ? kBytes : 0;
-    if constexpr (kBytes == 16)
-      asm volatile("cp.async.cg.shared.global [%0], [%1], 16, %2;" ::"r"(to + place(seg, off)), "l"(there ? from + off : from), "r"(n) : "memory");
-    else
-      asm volatile("cp.async.ca.shared.global [%0], [%1], %2, %3;" ::"r"(to + place(seg, off)), "l"(there ? from + off : from), "n"(kBytes), "r"(n) : "memory");
+    copy_piece<kBytes>(to + place(seg, off), there ? from + off : from, there);
   }
 }
-template <typename At, typename Left, typename Step>
-__device__ __forceinline__ void copy_unit(uint8_t* ring, int piece, int lane, At at, Left left, Step step) {
+template <typename At, typename Step>
+__device__ __forceinline__ void copy_rows(uint8_t* ring, int piece, int lane, int left, At at, Step step) {
   const uint32_t to = smem_u32(ring);
   if (piece == 16) {
-    copy_unit_by<16>(to, lane, at, left);
+    copy_rows_by<16>(to, lane, left, at);
   } else if (piece == 4) {
-    copy_unit_by<4>(to, lane, at, left);
+    copy_rows_by<4>(to, lane, left, at);
   } else {
     // element by element, step(s) apart
     for (int seg = 0; seg < 16; ++seg) {
       const uint16_t* from = reinterpret_cast<const uint16_t*>(at(seg));
-      const int64_t n = left(seg), cs = step(seg);
+      const int64_t cs = step(seg);
 #pragma unroll
       for (int i = 0; i < 2; ++i) {
         const int e = i * 32 + lane;
-        *reinterpret_cast<uint16_t*>(ring + place(seg, e * 2)) = e < n ? __ldg(from + e * cs) : uint16_t(0);
+        *reinterpret_cast<uint16_t*>(ring + place(seg, e * 2)) = e < left ? __ldg(from + e * cs) : uint16_t(0);
       }
     }
   }
 }
+// Copies `count` columns to the segments from `segment` on: column c is 64 elements from at(c), `left` of them there.
+template <int kMost, typename At>
+__device__ __forceinline__ void copy_columns(uint32_t to, int segment, int lane, int count, int left, At at) {
+#pragma unroll
+  for (int i = 0; i < kMost * 8 / 32; ++i) {
+    const int c = i * 4 + (lane >> 3), off = (lane & 7) * 16;
+    if (c >= count) continue;
+    const bool there = off < left * 2;
+    const char* from = at(c);
+    copy_piece<16>(to + place(segment + c, off), there ? from + off : from, there);
+  }
+}
 __device__ __forceinline__ void commit_copies() { asm volatile("cp.async.commit_group;" ::: "memory"); }
+template <int kStages>
 __device__ __forceinline__ void wait_for_unit() {
   asm volatile("cp.async.wait_group %0;" ::"n"(kStages - 1) : "memory");
   __syncwarp();
 }
-__device__ __forceinline__ uint4 load_16(const char* p) { return *reinterpret_cast<const uint4*>(p); }
+__device__ __forceinline__ uint4 words_at(const uint8_t* unit, int segment, int byte) {
+  return *reinterpret_cast<const uint4*>(unit + place(segment, byte));
+}
+__device__ __forceinline__ int left_of(int64_t length, int64_t from) { return int(min(max(length - from, int64_t(0)), int64_t(64))); }
 
 // ---- gate and up ------------------------------------------------------------------------------------
-// Block b takes the items b, b + gridDim.x, ... of (expert in use, 8 hidden channels); its warps share the channels in
+// Block b takes the items b, b + gridDim.x, ... of (group, 8 hidden channels); its warps share the channels in
 // units of 64.  Rows 0 to 7 of a tile are the gate's, rows 8 to 15 the up projection's.
 template <typename T, int kNt>
+struct GateUp {
+  static constexpr int kStages = kNt == 1 ? 4 : 3, kUnitBytes = 2048 + kNt * 1024, kColumns = 8 * kNt;
+  static constexpr int kRing = kWarps * kStages * kUnitBytes, kSmem = kRing + kWarps * kNt * 512;
+};
+template <typename T, int kNt>
 __global__ void __launch_bounds__(kWarps * 32, 2) cconv_moe_gate_up_kernel(const MoeParams p) {
+  using S = GateUp<T, kNt>;
   extern __shared__ __align__(128) uint8_t smem[];
   __shared__ int scratch[kWarps];
-  float(*const sums)[128] = reinterpret_cast<float(*)[128]>(smem + kWarps * kStages * kUnitBytes);  // [kNt * kWarps]
+  float(*const sums)[128] = reinterpret_cast<float(*)[128]>(smem + S::kRing);  // [kNt * kWarps]
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, g = lane >> 2, q = lane & 3;
-  uint8_t* const ring = smem + warp * (kStages * kUnitBytes);
+  uint8_t* const ring = smem + warp * (S::kStages * S::kUnitBytes);
   start_in_order();
-  const Routes r = routes_of<false>(p, smem + kWarps * (kStages * kUnitBytes + kNt * 512), scratch);
+  const Routes r = routes_of<false>(p, smem + S::kSmem, scratch, S::kColumns);
   const int tiles = int((p.F + 7) / 8);
   const int units = int((p.D + 63) / 64), per = (units + kWarps - 1) / kWarps, u0 = warp * per;
-  const int64_t items = int64_t(r.used) * tiles, stride = gridDim.x;
+  const int64_t items = int64_t(r.groups) * tiles, stride = gridDim.x;
   const int64_t mine = int64_t(blockIdx.x) < items ? (items - 1 - blockIdx.x) / stride + 1 : 0;
 
-  // (an item's place and tile, kept without divisions)
-  const int step_place = int(stride / tiles), step_tile = int(stride % tiles);
-  int lplace = int(blockIdx.x / tiles), ltile = int(blockIdx.x % tiles), lu = 0;
+  // (an item's group and tile, kept without divisions)
+  const int step_group = int(stride / tiles), step_tile = int(stride % tiles);
+  int lgroup = int(blockIdx.x / tiles), ltile = int(blockIdx.x % tiles), lu = 0;
   auto load = [&](int stage) {
     const int unit = u0 + lu;
-    if (lplace < r.used && unit < units) {
-      const int64_t e = r.expert[lplace], k0 = int64_t(unit) * 64;
-      copy_unit(ring + stage * kUnitBytes, p.piece_in, lane, [&](int seg) {
+    if (lgroup < r.groups && unit < units) {
+      uint8_t* const to = ring + stage * S::kUnitBytes;
+      const int64_t e = r.expert[lgroup], k0 = int64_t(unit) * 64;
+      copy_rows(to, p.piece_in, lane, left_of(p.D, k0), [&](int seg) {
         const int64_t f = min(int64_t(ltile) * 8 + (seg & 7), p.F - 1);
         return seg < 8 ? p.w_gate + (e * p.gate_es + f * p.gate_rs + k0 * p.gate_cs) * 2
                        : p.w_up + (e * p.up_es + f * p.up_rs + k0 * p.up_cs) * 2;
-      }, [&](int) { return p.D - k0; }, [&](int seg) { return seg < 8 ? p.gate_cs : p.up_cs; });
+      }, [&](int seg) { return seg < 8 ? p.gate_cs : p.up_cs; });
+      const int first = r.first[lgroup];
+      copy_columns<S::kColumns>(smem_u32(to), 16, lane, r.count[lgroup], left_of(p.x_k, k0),
+                                [&](int c) { return p.x + int64_t(r.pairs[first + c] / p.k) * p.x_rs + k0 * 2; });
     }
     commit_copies();
     if (++lu == per) {
       lu = 0;
       ltile += step_tile;
-      lplace += step_place;
-      if (ltile >= tiles) ltile -= tiles, ++lplace;
+      lgroup += step_group;
+      if (ltile >= tiles) ltile -= tiles, ++lgroup;
     }
   };
-#pragma unroll
-  for (int i = 0; i < kStages; ++i) load(i);
+  for (int i = 0; i < S::kStages; ++i) load(i);
 
-  int pl = int(blockIdx.x / tiles), tile = int(blockIdx.x % tiles), step = 0;
+  int group = int(blockIdx.x / tiles), tile = int(blockIdx.x % tiles), step = 0;
   float acc[kNt][4] = {};
-  const char* row[kNt];  // the tokens of this lane's columns
-  int count = 0, first = 0;
-  auto start_item = [&]() {
-    count = __popcll(r.tokens[pl]);
-    first = r.first[pl];
-#pragma unroll
-    for (int e = 0; e < kNt; ++e) row[e] = p.x + int64_t(r.pairs[first + min(8 * e + g, count - 1)] / p.k) * p.x_rs + q * 16;
-  };
   auto use = [&](int stage) {
-    if (step == 0) start_item();
-    const int unit = u0 + step;
-    wait_for_unit();
+    const int count = r.count[group], unit = u0 + step;
+    wait_for_unit<S::kStages>();
     if (unit < units) {
-      const uint8_t* from = ring + stage * kUnitBytes;
+      const uint8_t* from = ring + stage * S::kUnitBytes;
 #pragma unroll
       for (int i = 0; i < 2; ++i) {
-        const int64_t k0 = int64_t(unit) * 64 + i * 32;
-        const uint4 a0 = *reinterpret_cast<const uint4*>(from + place(g, i * 64 + q * 16));
-        const uint4 a1 = *reinterpret_cast<const uint4*>(from + place(g + 8, i * 64 + q * 16));
+        const uint4 a0 = words_at(from, g, i * 64 + q * 16), a1 = words_at(from, g + 8, i * 64 + q * 16);
 #pragma unroll
         for (int e = 0; e < kNt; ++e) {
           if (8 * e >= count) break;
-          uint4 v = make_uint4(0, 0, 0, 0);
-          if (8 * e + g < count && k0 + q * 8 < p.x_k) v = load_16(row[e] + k0 * 2);
+          const uint4 v = words_at(from, 16 + 8 * e + g, i * 64 + q * 16);  // (columns behind the last: whatever lies there)
           mma16<T>(acc[e], a0.x, a1.x, a0.y, a1.y, v.x, v.y);
           mma16<T>(acc[e], a0.z, a1.z, a0.w, a1.w, v.z, v.w);
         }
@@ -364,7 +424,7 @@ __global__ void __launch_bounds__(kWarps * 32, 2) cconv_moe_gate_up_kernel(const
     for (int e = 0; e < kNt; ++e)
 #pragma unroll
       for (int i = 0; i < 4; ++i) {
-        if (8 * e < count) sums[e * kWarps + warp][i * 32 + lane] = acc[e][i];
+        sums[e * kWarps + warp][i * 32 + lane] = acc[e][i];
         acc[e][i] = 0.0f;
       }
     __syncthreads();
@@ -378,7 +438,7 @@ __global__ void __launch_bounds__(kWarps * 32, 2) cconv_moe_gate_up_kernel(const
         u[0] += part[w][at + 64];
       }
       gate(p.act, a, u);
-      const int64_t channel = int64_t(tile) * 8 + f, to = int64_t(r.pairs[first + c]) * p.h_rs + channel;
+      const int64_t channel = int64_t(tile) * 8 + f, to = int64_t(r.pairs[r.first[group] + c]) * p.h_rs + channel;
       if (channel >= p.F) a[0] = 0.0f;  // the rest of the row's last 16 bytes
       const T hi = from_f32<T>(a[0]);
       reinterpret_cast<T*>(p.h)[to] = hi;
@@ -386,198 +446,227 @@ __global__ void __launch_bounds__(kWarps * 32, 2) cconv_moe_gate_up_kernel(const
       reinterpret_cast<T*>(p.h_lo)[to] = from_f32<T>(isfinite(to_f32(hi)) ? a[0] - to_f32(hi) : 0.0f);
     }
     tile += step_tile;
-    pl += step_place;
-    if (tile >= tiles) tile -= tiles, ++pl;
+    group += step_group;
+    if (tile >= tiles) tile -= tiles, ++group;
   };
   const int64_t total = mine * per;
   int stage = 0;
   for (int64_t it = 0; it < total; ++it) {
     use(stage);
     load(stage);
-    stage = (stage + 1) % kStages;
+    if (++stage == S::kStages) stage = 0;
   }
 }
 
 // ---- down -------------------------------------------------------------------------------------------
-// Block b takes the tiles b, b + gridDim.x, ... of kRows channels, each through all experts in use; its warps share
-// the hidden channels in units of 64 (16 rows) or 128 (8 rows, whose second halves are segments 8 to 15).
-template <typename T, int kNt, int kRows>
-__global__ void __launch_bounds__(kWarps * 32, 2) cconv_moe_down_kernel(const MoeParams p, const int early) {
+// Cluster c of `parts` blocks takes the tiles c, c + clusters, ... of 16 channels, each through all groups; the (group,
+// 64 hidden channels) of a tile are dealt evenly to the cluster's warps, in order.  Columns are a group's tokens, the
+// first parts of h in kNt tiles of them and the second parts in kNt more.  Each warp adds its groups' sums, times their
+// weights, to sums of its own [token][16] in shared memory; those of the warps, and then of the blocks, are added up in order.
+template <typename T, int kNt>
+struct Down {
+  static constexpr int kUnitBytes = 2048 + kNt * 2048, kTokens = 8 * kNt;
+  static int ring(int stages) { return kWarps * stages * kUnitBytes; }
+};
+template <typename T, int kNt, int kStages>
+__global__ void __launch_bounds__(kWarps * 32, 2) cconv_moe_down_kernel(const MoeParams p, const int parts) {
+  using S = Down<T, kNt>;
   extern __shared__ __align__(128) uint8_t smem[];
   __shared__ int scratch[kWarps];
-  float(*const sums)[128] = reinterpret_cast<float(*)[128]>(smem + kWarps * kStages * kUnitBytes);
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, g = lane >> 2, q = lane & 3;
-  uint8_t* const ring = smem + warp * (kStages * kUnitBytes);
-  constexpr int kUnit = kRows == 16 ? 64 : 128;
-  const int tiles = int((p.D + kRows - 1) / kRows);
-  const int units = int((p.F + kUnit - 1) / kUnit), per = (units + kWarps - 1) / kWarps, u0 = warp * per;
+  uint8_t* const ring = smem + warp * (kStages * S::kUnitBytes);
+  float* const all = reinterpret_cast<float*>(smem + kWarps * kStages * S::kUnitBytes);  // [kWarps][T][16]
+  float* const mine = all + warp * p.T * 16;
+  const int tiles = int((p.D + 15) / 16), clusters = int(gridDim.x) / parts;
+  const int rank = int(blockIdx.x) % parts, first_tile = int(blockIdx.x) / parts;
+  const int units = int((p.F + 63) / 64);
 
   // Behind the gate and up kernel of the same call, which lets this one in only once everything before the call and the
   // router are complete, the choice and the weights are there already; h is waited for below.
-  if (!early) start_in_order();
-  const Routes r = routes_of<true>(p, smem + kWarps * (kStages * kUnitBytes + kNt * 512), scratch);
-  int lt = blockIdx.x, lplace = 0, lu = 0;
-  auto load = [&](int stage) {
-    const int unit = u0 + lu;
-    if (lt < tiles && lplace < r.used && unit < units) {
-      const int64_t e = r.expert[lplace], k0 = int64_t(unit) * kUnit;
-      auto part = [&](int seg) { return k0 + (kRows == 8 ? seg >> 3 << 6 : 0); };
-      copy_unit(ring + stage * kUnitBytes, p.piece_out, lane, [&](int seg) {
-        const int64_t d = min(int64_t(lt) * kRows + (seg & (kRows - 1)), p.D - 1), k = part(seg);
-        return p.w_down + (e * p.down_es + d * p.down_rs + (k < p.F ? k : 0) * p.down_cs) * 2;
-      }, [&](int seg) { return p.F - part(seg); }, [&](int) { return p.down_cs; });
-    }
-    commit_copies();
-    if (++lu == per) {
-      lu = 0;
-      if (++lplace >= r.used) lplace = 0, lt += gridDim.x;
+  const Routes r = routes_of<true>(p, smem + kWarps * (kStages * S::kUnitBytes + p.T * 64), scratch, S::kTokens);
+  const int64_t work = int64_t(r.groups) * units;
+  const int64_t w0 = work * (rank * kWarps + warp) / (parts * kWarps), w1 = work * (rank * kWarps + warp + 1) / (parts * kWarps);
+  const int each = int(w1 - w0), group0 = units ? int(w0 / units) : 0, unit0 = int(w0 - int64_t(group0) * units);
+
+  // weights, and tokens once they are there
+  int lt = first_tile, lgroup = group0, lunit = unit0, ln = 0;
+  auto load_weights = [&](int stage, int tile, int group, int unit) {
+    const int64_t e = r.expert[group], k0 = int64_t(unit) * 64;
+    copy_rows(ring + stage * S::kUnitBytes, p.piece_out, lane, left_of(p.F, k0), [&](int seg) {
+      const int64_t d = min(int64_t(tile) * 16 + seg, p.D - 1);
+      return p.w_down + (e * p.down_es + d * p.down_rs + k0 * p.down_cs) * 2;
+    }, [&](int) { return p.down_cs; });
+  };
+  auto load_tokens = [&](int stage, int group, int unit) {
+    const uint32_t to = smem_u32(ring + stage * S::kUnitBytes);
+    const int64_t k0 = int64_t(unit) * 64;
+    const int count = r.count[group], first = r.first[group], left = left_of(p.h_rs, k0);
+    copy_columns<S::kTokens>(to, 16, lane, count, left, [&](int c) { return p.h + (r.pairs[first + c] * p.h_rs + k0) * 2; });
+    copy_columns<S::kTokens>(to, 16 + S::kTokens, lane, count, left, [&](int c) { return p.h_lo + (r.pairs[first + c] * p.h_rs + k0) * 2; });
+  };
+  auto next = [&](int& tile, int& group, int& unit, int& n) {
+    if (++n == each) {
+      n = 0;
+      group = group0;
+      unit = unit0;
+      tile += clusters;
+    } else if (++unit == units) {
+      unit = 0;
+      ++group;
     }
   };
-#pragma unroll
-  for (int i = 0; i < kStages; ++i) load(i);
-  if (early) start_in_order();
-
-  int pl = 0, step = 0;
-  float acc[kNt][4] = {}, d[kNt][4] = {};
-  int64_t row[kNt];  // where h of this lane's tokens begins; -1: they have not chosen the expert
-  uint64_t tokens = 0;
-  int first = 0;
-  auto pair_of_token = [&](int t) { return r.pairs[first + __popcll(tokens & ((1ull << t) - 1))]; };
-  auto use = [&](int stage) {
-    if (step == 0) {
-      tokens = r.tokens[pl];
-      first = r.first[pl];
-#pragma unroll
-      for (int e = 0; e < kNt; ++e) {
-        const int t = 8 * e + g;
-        row[e] = tokens >> t & 1 ? int64_t(pair_of_token(t)) * p.h_rs * 2 + q * 16 : -1;
-      }
+  {
+    int tt = lt, tg = lgroup, tu = lunit, tn = ln;
+    for (int i = 0; i < kStages; ++i) {
+      if (each && lt < tiles) load_weights(i, lt, lgroup, lunit);
+      next(lt, lgroup, lunit, ln);
     }
-    const int unit = u0 + step;
-    wait_for_unit();
-    if (unit < units) {
-      const uint8_t* from = ring + stage * kUnitBytes;
+    start_in_order();
+    for (int i = 0; i < kStages; ++i) {
+      if (each && tt < tiles) load_tokens(i, tg, tu);
+      commit_copies();  // (the first commit takes in the weights of all stages)
+      next(tt, tg, tu, tn);
+    }
+  }
+  int stage = 0;
+  for (int tile = first_tile; tile < tiles; tile += clusters) {
+    for (int i = lane; i < p.T * 16; i += 32) mine[i] = 0.0f;
+    __syncwarp();
+    float d[2 * kNt][4] = {};
+    int group = group0, unit = unit0;
+    for (int n = 0; n < each; ++n) {
+      const int count = r.count[group];
+      wait_for_unit<kStages>();
+      const uint8_t* from = ring + stage * S::kUnitBytes;
 #pragma unroll
-      for (int i = 0; i < kUnit / 32; ++i) {
-        const int64_t k0 = int64_t(unit) * kUnit + i * 32;
-        uint4 a0, a1;
-        if constexpr (kRows == 16) {
-          a0 = *reinterpret_cast<const uint4*>(from + place(g, i * 64 + q * 16));
-          a1 = *reinterpret_cast<const uint4*>(from + place(g + 8, i * 64 + q * 16));
-        } else {
-          a0 = *reinterpret_cast<const uint4*>(from + place(g + (i >> 1) * 8, (i & 1) * 64 + q * 16));
-          a1 = make_uint4(0, 0, 0, 0);
-        }
+      for (int i = 0; i < 2; ++i) {
+        const uint4 a0 = words_at(from, g, i * 64 + q * 16), a1 = words_at(from, g + 8, i * 64 + q * 16);
 #pragma unroll
-        for (int e = 0; e < kNt; ++e) {
-          if ((tokens >> (8 * e) & 0xff) == 0) continue;
-          uint4 v = make_uint4(0, 0, 0, 0), w = v;
-          if (row[e] >= 0 && k0 + q * 8 < p.h_rs) {
-            v = load_16(p.h + row[e] + k0 * 2);
-            w = load_16(p.h_lo + row[e] + k0 * 2);
-          }
+        for (int e = 0; e < 2 * kNt; ++e) {
+          if (8 * (e % kNt) >= count) continue;
+          const uint4 v = words_at(from, 16 + 8 * e + g, i * 64 + q * 16);
           mma16<T>(d[e], a0.x, a1.x, a0.y, a1.y, v.x, v.y);
           mma16<T>(d[e], a0.z, a1.z, a0.w, a1.w, v.z, v.w);
-          mma16<T>(d[e], a0.x, a1.x, a0.y, a1.y, w.x, w.y);
-          mma16<T>(d[e], a0.z, a1.z, a0.w, a1.w, w.z, w.w);
         }
       }
-    }
-    __syncwarp();
-    if (++step < per) return;
-    step = 0;
-    // the expert's share, times the weights of this lane's columns
+      __syncwarp();
+      if (lt < tiles) {
+        load_weights(stage, lt, lgroup, lunit);
+        load_tokens(stage, lgroup, lunit);
+      }
+      commit_copies();
+      next(lt, lgroup, lunit, ln);
+      if (++stage == kStages) stage = 0;
+      if (++unit == units || n + 1 == each) {
+        // the group's share: this lane's columns are tokens 2q and 2q + 1 of eight
+        const int first = r.first[group];
 #pragma unroll
-    for (int e = 0; e < kNt; ++e) {
-      if ((tokens >> (8 * e) & 0xff) == 0) continue;
+        for (int e = 0; e < kNt; ++e)
 #pragma unroll
-      for (int c = 0; c < 2; ++c) {
-        const int t = 8 * e + 2 * q + c;
-        if (tokens >> t & 1) {
-          const float w = r.weight[pair_of_token(t)];
-          acc[e][c] += w * d[e][c];
-          acc[e][2 + c] += w * d[e][2 + c];
-        }
-        d[e][c] = d[e][2 + c] = 0.0f;
+          for (int c = 0; c < 2; ++c) {
+            const int column = 8 * e + 2 * q + c;
+            if (column < count) {
+              const float w = r.weight[first + column];
+              float* to = mine + r.pairs[first + column] / p.k * 16 + g;
+              to[0] += w * (d[e][c] + d[kNt + e][c]);
+              to[8] += w * (d[e][2 + c] + d[kNt + e][2 + c]);
+            }
+            d[e][c] = d[kNt + e][c] = d[e][2 + c] = d[kNt + e][2 + c] = 0.0f;
+          }
+        __syncwarp();
+        unit = 0;
+        ++group;
       }
     }
-    ++pl;
-  };
-  int stage = 0;
-  for (int tile = blockIdx.x; tile < tiles; tile += gridDim.x) {
-    pl = 0;
-    const int total = r.used * per;
-    for (int it = 0; it < total; ++it) {
-      use(stage);
-      load(stage);
-      stage = (stage + 1) % kStages;
-    }
-    __syncthreads();  // the sums before have been read
-#pragma unroll
-    for (int e = 0; e < kNt; ++e)
-#pragma unroll
-      for (int i = 0; i < 4; ++i) {
-        sums[e * kWarps + warp][i * 32 + lane] = acc[e][i];
-        acc[e][i] = 0.0f;
-      }
     __syncthreads();
-    for (int i = threadIdx.x; i < kRows * p.T; i += kWarps * 32) {
-      const int rr = i % kRows, t = i / kRows;
-      const int64_t channel = int64_t(tile) * kRows + rr;
-      if (channel >= p.D) continue;
-      const int at = ((rr >> 3) * 2 + (t & 1)) * 32 + (rr & 7) * 4 + ((t & 7) >> 1);
-      const float(*part)[128] = sums + (t >> 3) * kWarps;
+    const int outputs = p.T * 16;
+    for (int i = threadIdx.x; i < outputs; i += kWarps * 32) {
       float s = 0.0f;
 #pragma unroll
-      for (int w = 0; w < kWarps; ++w) s += part[w][at];
-      static_cast<T*>(const_cast<void*>(p.out.p))[t * p.out.rs + channel * p.out.cs] = from_f32<T>(s);
+      for (int w = 0; w < kWarps; ++w) s += all[w * outputs + i];
+      if (parts == 1) {
+        const int64_t channel = int64_t(tile) * 16 + (i & 15);
+        if (channel < p.D) static_cast<T*>(const_cast<void*>(p.out.p))[(i >> 4) * p.out.rs + channel * p.out.cs] = from_f32<T>(s);
+      } else {
+        all[i] = s;
+      }
     }
+    if (parts == 1) {
+      __syncthreads();
+      continue;
+    }
+    cluster_sync_all();
+    for (int i = threadIdx.x + rank * kWarps * 32; i < outputs; i += parts * kWarps * 32) {
+      float s = 0.0f;
+      for (int b = 0; b < parts; ++b) s += load_cluster(cluster_map_shared(smem_u32(all + i), b));
+      const int64_t channel = int64_t(tile) * 16 + (i & 15);
+      if (channel < p.D) static_cast<T*>(const_cast<void*>(p.out.p))[(i >> 4) * p.out.rs + channel * p.out.cs] = from_f32<T>(s);
+    }
+    cluster_sync_all();  // the sums have been read
   }
 }
 
 // ---- launches ---------------------------------------------------------------------------------------
-template <typename T, int kNt>
-cudaError_t launch_router(const MoeParams& p, cudaStream_t s) {
-  const dim3 grid(unsigned(cdiv64(p.T, kTokens) * kRouterBlocks));
-  return launch(cconv_moe_router_kernel<T, kNt>, grid, kRouterWarps * 32, 0, kRouterBlocks, s, p);
-}
-
-constexpr int kRing = kWarps * kStages * kUnitBytes;
-int smem_of(const MoeParams& p, int nt, bool weights) { return kRing + kWarps * nt * 512 + routes_bytes(p.E, p.T * p.k, weights); }
-constexpr int kMostSmem = kRing + kWarps * 8 * 512 + routes_bytes(int(kMostExperts), kTokens * int(kMostChosen), true);
+constexpr int kMostShared = 200 * 1024;  // of a block here
 
 template <typename T, int kNt>
-cudaError_t launch_gate_up(const MoeParams& p, int sms, cudaStream_t s) {
-  auto f = cconv_moe_gate_up_kernel<T, kNt>;
+cudaError_t launch_router(const MoeParams& p, int chunk, cudaStream_t s) {
+  auto f = cconv_moe_router_kernel<T, kNt>;
   static bool ready[64] = {};
-  const cudaError_t e = allow_smem(f, ready, kMostSmem);
+  const cudaError_t e = allow_smem(f, ready, kMostShared);
   if (e != cudaSuccess) return e;
-  const int64_t most = std::min<int64_t>(p.E, int64_t(p.T) * p.k) * cdiv64(p.F, 8);
-  return launch(f, dim3(unsigned(std::min<int64_t>(most, 2 * sms))), kWarps * 32, smem_of(p, kNt, false), 1, s, p);
+  const int groups = int(cdiv64(p.E, 16)), slices = groups >= kRouterWarps ? 1 : kRouterWarps / groups;
+  const dim3 grid(unsigned(cdiv64(p.T, chunk) * kRouterBlocks));
+  return launch(f, grid, kRouterWarps * 32, size_t(slices) * chunk * p.E * 4, kRouterBlocks, s, p, chunk);
 }
-template <typename T, int kNt, int kRows>
-cudaError_t launch_down_rows(const MoeParams& p, int sms, cudaStream_t s) {
-  auto f = cconv_moe_down_kernel<T, kNt, kRows>;
-  static bool ready[64] = {};
-  const cudaError_t e = allow_smem(f, ready, kMostSmem);
-  if (e != cudaSuccess) return e;
-  return launch(f, dim3(unsigned(std::min<int64_t>(cdiv64(p.D, kRows), 2 * sms))), kWarps * 32, smem_of(p, kNt, true), 1, s, p, 1);
-}
-template <typename T, int kNt>
-cudaError_t launch_down(const MoeParams& p, int sms, cudaStream_t s) {
-  // 16 rows a tile where that leaves no SM with less than two blocks
-  return cdiv64(p.D, 16) >= 2 * sms ? launch_down_rows<T, kNt, 16>(p, sms, s) : launch_down_rows<T, kNt, 8>(p, sms, s);
-}
-// Calls f(T(), columns of 8) for the call's type and T tokens, at most 64.
+// Calls f(T(), columns of 8) for the call's type and at most 64 tokens.
 template <typename F>
-cudaError_t with_columns(int dtype, int64_t T, F f) {
+cudaError_t with_columns(int dtype, int64_t tokens, F f) {
   auto columns = [&](auto type) {
-    if (T <= 8) return f(type, std::integral_constant<int, 1>());
-    if (T <= 16) return f(type, std::integral_constant<int, 2>());
-    if (T <= 32) return f(type, std::integral_constant<int, 4>());
+    if (tokens <= 8) return f(type, std::integral_constant<int, 1>());
+    if (tokens <= 16) return f(type, std::integral_constant<int, 2>());
+    if (tokens <= 32) return f(type, std::integral_constant<int, 4>());
     return f(type, std::integral_constant<int, 8>());
   };
   return dtype == CCONV_TYPE_BF16 ? columns(__nv_bfloat16()) : columns(__half());
+}
+// Tokens that choose together: as many as leave their scores room in shared memory.
+int router_tokens(int64_t T, int64_t E) { return int(std::min<int64_t>(std::min<int64_t>(T, kTokens), std::max<int64_t>(8, 16384 / E))); }
+
+template <typename T, int kNt>
+cudaError_t launch_gate_up(const MoeParams& p, int sms, cudaStream_t s) {
+  using S = GateUp<T, kNt>;
+  auto f = cconv_moe_gate_up_kernel<T, kNt>;
+  static bool ready[64] = {};
+  const cudaError_t e = allow_smem(f, ready, kMostShared);
+  if (e != cudaSuccess) return e;
+  const int pairs = p.T * p.k;
+  const int64_t most = most_groups(p.E, pairs, S::kColumns) * cdiv64(p.F, 8);
+  return launch(f, dim3(unsigned(std::min<int64_t>(most, 2 * sms))), kWarps * 32,
+                S::kSmem + routes_bytes(p.E, pairs, S::kColumns, false), 1, s, p);
+}
+template <typename T, int kNt, int kStages>
+cudaError_t launch_down_as(const MoeParams& p, int sms, cudaStream_t s) {
+  using S = Down<T, kNt>;
+  auto f = cconv_moe_down_kernel<T, kNt, kStages>;
+  static bool ready[64] = {};
+  const cudaError_t e = allow_smem(f, ready, kMostShared);
+  if (e != cudaSuccess) return e;
+  // blocks that share a tile, so that every SM has two
+  const int64_t tiles = cdiv64(p.D, 16);
+  const int parts = tiles * 2 > 2 * sms ? 1 : tiles * 4 > 2 * sms ? 2 : tiles * 8 > 2 * sms ? 4 : 8;
+  const int64_t clusters = std::min<int64_t>(tiles, 2 * sms / parts);
+  return launch(f, dim3(unsigned(clusters * parts)), kWarps * 32,
+                S::ring(kStages) + kWarps * p.T * 64 + routes_bytes(p.E, p.T * p.k, S::kTokens, true), parts, s, p, parts);
+}
+template <typename T>
+cudaError_t launch_layer(const MoeParams& p, int sms, cudaStream_t s) {
+  // columns for 8 tokens of an expert, or for 16 where most have more than 8
+  const bool many = int64_t(p.T) * p.k > 6 * int64_t(p.E) && p.T > 8;
+  const cudaError_t e = many ? launch_gate_up<T, 2>(p, sms, s) : launch_gate_up<T, 1>(p, sms, s);
+  if (e != cudaSuccess) return e;
+  if (many) return launch_down_as<T, 2, 2>(p, sms, s);
+  return p.T <= 16 ? launch_down_as<T, 1, 3>(p, sms, s) : launch_down_as<T, 1, 2>(p, sms, s);
 }
 
 // Bytes that rows of an expert's matrix can be copied in.
@@ -640,11 +729,12 @@ void plan(Steps& st, const cconv_moe_args& a) {
     const Mat router = padded(st, a.router, a.E, a.D, &k);
     p.router = static_cast<const char*>(router.p);
     p.router_rs = router.rs * 2;
-    p.logits = static_cast<float*>(const_cast<void*>(st.scratch(a.T, a.E, 4).p));
     MoeParams r = p;
     r.T = int(a.T);
     st.add([=](cudaStream_t s) {
-      return block_cuda_error(with_columns(r.dtype, r.T, [&](auto type, auto nt) { return launch_router<decltype(type), decltype(nt)::value>(r, s); }),
+      const int chunk = router_tokens(r.T, r.E);
+      return block_cuda_error(with_columns(r.dtype, chunk, [&](auto type, auto nt) {
+        return launch_router<decltype(type), decltype(nt)::value>(r, chunk, s); }),
                               "cconv_moe_router_kernel");
     });
   }
@@ -656,10 +746,8 @@ void plan(Steps& st, const cconv_moe_args& a) {
     c.weights += t0 * c.weights_rs;
     c.out.p = static_cast<const char*>(c.out.p) + t0 * c.out.rs * 2;
     st.add([=](cudaStream_t s) {
-      cudaError_t e = with_columns(c.dtype, c.T, [&](auto type, auto nt) { return launch_gate_up<decltype(type), decltype(nt)::value>(c, sms, s); });
-      if (e == cudaSuccess)
-        e = with_columns(c.dtype, c.T, [&](auto type, auto nt) { return launch_down<decltype(type), decltype(nt)::value>(c, sms, s); });
-      return block_cuda_error(e, "cconv_moe_forward");
+      return block_cuda_error(c.dtype == CCONV_TYPE_BF16 ? launch_layer<__nv_bfloat16>(c, sms, s) : launch_layer<__half>(c, sms, s),
+                              "cconv_moe_forward");
     });
   }
 }
