@@ -195,11 +195,12 @@ struct Routes {
   uint16_t* pairs;    // [pairs]: t k + j
   uint16_t *expert, *first;  // [groups]
   uint8_t* count;     // [groups]
+  uint8_t* token;     // [pairs], as `pairs`: t
   int groups;
 };
 constexpr __host__ __device__ int most_groups(int E, int pairs, int most) { return (E < pairs ? E : pairs) + pairs / most; }
 constexpr int routes_bytes(int E, int pairs, int most, bool weights) {
-  return E * 10 + pairs * (weights ? 6 : 2) + most_groups(E, pairs, most) * 5 + 16;
+  return E * 10 + pairs * (weights ? 7 : 3) + most_groups(E, pairs, most) * 5 + 16;
 }
 
 template <bool kWeights>
@@ -213,6 +214,7 @@ __device__ __forceinline__ Routes routes_of(const MoeParams& p, uint8_t* smem, i
   r.expert = r.pairs + pairs;
   r.first = r.expert + most_groups(E, pairs, most);
   r.count = reinterpret_cast<uint8_t*>(r.first + most_groups(E, pairs, most));
+  r.token = r.count + most_groups(E, pairs, most);
   for (int e = tid; e < E; e += nt) r.tokens[e] = 0;
   __syncthreads();
   auto id_of = [&](int t, int j) { return __ldg(p.ids + t * p.ids_rs + j * p.ids_cs); };
@@ -272,6 +274,7 @@ __device__ __forceinline__ Routes routes_of(const MoeParams& p, uint8_t* smem, i
     if (again) continue;
     const int to = r.first_of[e] + __popcll(r.tokens[e] & ((1ull << t) - 1));
     r.pairs[to] = uint16_t(i);
+    r.token[to] = uint8_t(t);
     if (kWeights) r.weight[to] = w;
   }
   __syncthreads();
@@ -292,48 +295,34 @@ __device__ __forceinline__ void copy_piece(uint32_t to, const char* from, bool t
   else
     asm volatile("cp.async.ca.shared.global [%0], [%1], %2, %3;" ::"r"(to), "l"(from), "n"(kBytes), "r"(n) : "memory");
 }
-// Copies the weights: segment s is 64 elements from at(s), of which the first `left` are there and the others zeros.
-template <int kBytes, typename At>
-__device__ __forceinline__ void copy_rows_by(uint32_t to, int lane, int left, At at) {
-  constexpr int kAcross = 128 / kBytes;
+// Copies 16 bytes that every lane names of 4 rows (or columns) each, 128 bytes of 4 neighbouring rows an instruction;
+// lane l's go to the word l % 8 of the rows l / 8, l / 8 + 4, ... of those from `segment` on.  Of columns, the first `count`.
+template <int kEach>
+__device__ __forceinline__ void copy_16(uint32_t to, int segment, int lane, const char* const (&from)[kEach], uint32_t at, bool there,
+                                        int count) {
 #pragma unroll
-  for (int i = 0; i < 16 * kAcross / 32; ++i) {
-    const int c = i * 32 + lane, seg = c / kAcross, off = c % kAcross * kBytes;
-    const bool there = off < left * 2;
-    const char* from = at(seg);
-    copy_piece<kBytes>(to + place(seg, off), there ? from + off : from, there);
-  }
+  for (int i = 0; i < kEach; ++i)
+    if (i * 4 + (lane >> 3) < count) copy_piece<16>(to + place(segment + i * 4 + (lane >> 3), (lane & 7) * 16), from[i] + at, there);
 }
+// The weights where rows do not lie on 16 bytes: segment s is 64 elements from at(s), step(s) apart, of which the first
+// `left` are there and the others zeros.
 template <typename At, typename Step>
 __device__ __forceinline__ void copy_rows(uint8_t* ring, int piece, int lane, int left, At at, Step step) {
-  const uint32_t to = smem_u32(ring);
-  if (piece == 16) {
-    copy_rows_by<16>(to, lane, left, at);
-  } else if (piece == 4) {
-    copy_rows_by<4>(to, lane, left, at);
-  } else {
-    // element by element, step(s) apart
+  if (piece == 4) {
     for (int seg = 0; seg < 16; ++seg) {
-      const uint16_t* from = reinterpret_cast<const uint16_t*>(at(seg));
-      const int64_t cs = step(seg);
-#pragma unroll
-      for (int i = 0; i < 2; ++i) {
-        const int e = i * 32 + lane;
-        *reinterpret_cast<uint16_t*>(ring + place(seg, e * 2)) = e < left ? __ldg(from + e * cs) : uint16_t(0);
-      }
+      const bool there = lane * 4 < left * 2;
+      copy_piece<4>(smem_u32(ring) + place(seg, lane * 4), at(seg) + (there ? lane * 4 : 0), there);
     }
+    return;
   }
-}
-// Copies `count` columns to the segments from `segment` on: column c is 64 elements from at(c), `left` of them there.
-template <int kMost, typename At>
-__device__ __forceinline__ void copy_columns(uint32_t to, int segment, int lane, int count, int left, At at) {
+  for (int seg = 0; seg < 16; ++seg) {
+    const uint16_t* from = reinterpret_cast<const uint16_t*>(at(seg));
+    const int64_t cs = step(seg);
 #pragma unroll
-  for (int i = 0; i < kMost * 8 / 32; ++i) {
-    const int c = i * 4 + (lane >> 3), off = (lane & 7) * 16;
-    if (c >= count) continue;
-    const bool there = off < left * 2;
-    const char* from = at(c);
-    copy_piece<16>(to + place(segment + c, off), there ? from + off : from, there);
+    for (int i = 0; i < 2; ++i) {
+      const int e = i * 32 + lane;
+      *reinterpret_cast<uint16_t*>(ring + place(seg, e * 2)) = e < left ? __ldg(from + e * cs) : uint16_t(0);
+    }
   }
 }
 __device__ __forceinline__ void commit_copies() { asm volatile("cp.async.commit_group;" ::: "memory"); }
@@ -372,20 +361,38 @@ __global__ void __launch_bounds__(kWarps * 32, 2) cconv_moe_gate_up_kernel(const
 
   // (an item's group and tile, kept without divisions)
   const int step_group = int(stride / tiles), step_tile = int(stride % tiles);
-  int lgroup = int(blockIdx.x / tiles), ltile = int(blockIdx.x % tiles), lu = 0;
+  int lgroup = int(blockIdx.x / tiles), ltile = int(blockIdx.x % tiles), lu = 0, lcount = 0;
+  const char *rows[4], *columns[2 * kNt];  // of the item: what this lane copies of
+  auto row_of = [&](int64_t e, int seg) {
+    const int64_t f = min(int64_t(ltile) * 8 + (seg & 7), p.F - 1);
+    return seg < 8 ? p.w_gate + (e * p.gate_es + f * p.gate_rs) * 2 : p.w_up + (e * p.up_es + f * p.up_rs) * 2;
+  };
+  auto aim = [&]() {
+    if (lgroup >= r.groups) return;
+    const int64_t e = r.expert[lgroup];
+    const int first = r.first[lgroup];
+    lcount = r.count[lgroup];
+    if (p.piece_in == 16) {
+#pragma unroll
+      for (int i = 0; i < 4; ++i) rows[i] = row_of(e, i * 4 + (lane >> 3));
+    }
+#pragma unroll
+    for (int i = 0; i < 2 * kNt; ++i) columns[i] = p.x + int64_t(r.token[first + min(i * 4 + (lane >> 3), lcount - 1)]) * p.x_rs;
+  };
+  const uint32_t row_bytes = uint32_t(p.D) * 2, column_bytes = uint32_t(p.x_k) * 2;
   auto load = [&](int stage) {
     const int unit = u0 + lu;
     if (lgroup < r.groups && unit < units) {
       uint8_t* const to = ring + stage * S::kUnitBytes;
-      const int64_t e = r.expert[lgroup], k0 = int64_t(unit) * 64;
-      copy_rows(to, p.piece_in, lane, left_of(p.D, k0), [&](int seg) {
-        const int64_t f = min(int64_t(ltile) * 8 + (seg & 7), p.F - 1);
-        return seg < 8 ? p.w_gate + (e * p.gate_es + f * p.gate_rs + k0 * p.gate_cs) * 2
-                       : p.w_up + (e * p.up_es + f * p.up_rs + k0 * p.up_cs) * 2;
-      }, [&](int seg) { return seg < 8 ? p.gate_cs : p.up_cs; });
-      const int first = r.first[lgroup];
-      copy_columns<S::kColumns>(smem_u32(to), 16, lane, r.count[lgroup], left_of(p.x_k, k0),
-                                [&](int c) { return p.x + int64_t(r.pairs[first + c] / p.k) * p.x_rs + k0 * 2; });
+      const uint32_t at = uint32_t(unit) * 128 + (lane & 7) * 16;
+      if (p.piece_in == 16) {
+        copy_16(smem_u32(to), 0, lane, rows, at < row_bytes ? at : 0, at < row_bytes, 16);
+      } else {
+        const int64_t e = r.expert[lgroup], k0 = int64_t(unit) * 64;
+        copy_rows(to, p.piece_in, lane, left_of(p.D, k0), [&](int seg) { return row_of(e, seg) + k0 * (seg < 8 ? p.gate_cs : p.up_cs) * 2; },
+                  [&](int seg) { return seg < 8 ? p.gate_cs : p.up_cs; });
+      }
+      copy_16(smem_u32(to), 16, lane, columns, at < column_bytes ? at : 0, at < column_bytes, lcount);
     }
     commit_copies();
     if (++lu == per) {
@@ -393,8 +400,10 @@ __global__ void __launch_bounds__(kWarps * 32, 2) cconv_moe_gate_up_kernel(const
       ltile += step_tile;
       lgroup += step_group;
       if (ltile >= tiles) ltile -= tiles, ++lgroup;
+      aim();
     }
   };
+  aim();
   for (int i = 0; i < S::kStages; ++i) load(i);
 
   int group = int(blockIdx.x / tiles), tile = int(blockIdx.x % tiles), step = 0;
@@ -489,45 +498,69 @@ __global__ void __launch_bounds__(kWarps * 32, 2) cconv_moe_down_kernel(const Mo
   const int each = int(w1 - w0), group0 = units ? int(w0 / units) : 0, unit0 = int(w0 - int64_t(group0) * units);
 
   // weights, and tokens once they are there
-  int lt = first_tile, lgroup = group0, lunit = unit0, ln = 0;
-  auto load_weights = [&](int stage, int tile, int group, int unit) {
-    const int64_t e = r.expert[group], k0 = int64_t(unit) * 64;
-    copy_rows(ring + stage * S::kUnitBytes, p.piece_out, lane, left_of(p.F, k0), [&](int seg) {
-      const int64_t d = min(int64_t(tile) * 16 + seg, p.D - 1);
-      return p.w_down + (e * p.down_es + d * p.down_rs + k0 * p.down_cs) * 2;
-    }, [&](int) { return p.down_cs; });
+  int lt = first_tile, lgroup = group0, lunit = unit0, ln = 0, lcount = 0;
+  const char *rows[4], *highs[2 * kNt], *lows[2 * kNt];  // of the tile and group: what this lane copies of
+  const uint32_t row_bytes = uint32_t(p.F) * 2, column_bytes = uint32_t(p.h_rs) * 2;
+  auto row_of = [&](int64_t e, int seg) {
+    return p.w_down + (e * p.down_es + min(int64_t(lt) * 16 + seg, p.D - 1) * p.down_rs) * 2;
   };
-  auto load_tokens = [&](int stage, int group, int unit) {
-    const uint32_t to = smem_u32(ring + stage * S::kUnitBytes);
-    const int64_t k0 = int64_t(unit) * 64;
-    const int count = r.count[group], first = r.first[group], left = left_of(p.h_rs, k0);
-    copy_columns<S::kTokens>(to, 16, lane, count, left, [&](int c) { return p.h + (r.pairs[first + c] * p.h_rs + k0) * 2; });
-    copy_columns<S::kTokens>(to, 16 + S::kTokens, lane, count, left, [&](int c) { return p.h_lo + (r.pairs[first + c] * p.h_rs + k0) * 2; });
-  };
-  auto next = [&](int& tile, int& group, int& unit, int& n) {
-    if (++n == each) {
-      n = 0;
-      group = group0;
-      unit = unit0;
-      tile += clusters;
-    } else if (++unit == units) {
-      unit = 0;
-      ++group;
+  auto aim = [&]() {
+    if (lgroup >= r.groups) return;
+    const int first = r.first[lgroup];
+    lcount = r.count[lgroup];
+    if (p.piece_out == 16) {
+      const int64_t e = r.expert[lgroup];
+#pragma unroll
+      for (int i = 0; i < 4; ++i) rows[i] = row_of(e, i * 4 + (lane >> 3));
+    }
+#pragma unroll
+    for (int i = 0; i < 2 * kNt; ++i) {
+      const int64_t h = int64_t(r.pairs[first + min(i * 4 + (lane >> 3), lcount - 1)]) * column_bytes;
+      highs[i] = p.h + h;
+      lows[i] = p.h_lo + h;
     }
   };
-  {
-    int tt = lt, tg = lgroup, tu = lunit, tn = ln;
+  auto load_weights = [&](int stage) {
+    uint8_t* const to = ring + stage * S::kUnitBytes;
+    if (p.piece_out == 16) {
+      const uint32_t at = uint32_t(lunit) * 128 + (lane & 7) * 16;
+      copy_16(smem_u32(to), 0, lane, rows, at < row_bytes ? at : 0, at < row_bytes, 16);
+    } else {
+      const int64_t e = r.expert[lgroup], k0 = int64_t(lunit) * 64;
+      copy_rows(to, p.piece_out, lane, left_of(p.F, k0), [&](int seg) { return row_of(e, seg) + k0 * p.down_cs * 2; },
+                [&](int) { return p.down_cs; });
+    }
+  };
+  auto load_tokens = [&](int stage) {
+    const uint32_t to = smem_u32(ring + stage * S::kUnitBytes), at = uint32_t(lunit) * 128 + (lane & 7) * 16;
+    copy_16(to, 16, lane, highs, at < column_bytes ? at : 0, at < column_bytes, lcount);
+    copy_16(to, 16 + S::kTokens, lane, lows, at < column_bytes ? at : 0, at < column_bytes, lcount);
+  };
+  auto next = [&]() {
+    if (++ln == each) {
+      ln = 0;
+      lgroup = group0;
+      lunit = unit0;
+      lt += clusters;
+      aim();
+    } else if (++lunit == units) {
+      lunit = 0;
+      ++lgroup;
+      aim();
+    }
+  };
+  auto fill = [&](auto load, auto commit) {
+    lt = first_tile, lgroup = group0, lunit = unit0, ln = 0;
+    aim();
     for (int i = 0; i < kStages; ++i) {
-      if (each && lt < tiles) load_weights(i, lt, lgroup, lunit);
-      next(lt, lgroup, lunit, ln);
+      if (each && lt < tiles) load(i);
+      commit();
+      next();
     }
-    start_in_order();
-    for (int i = 0; i < kStages; ++i) {
-      if (each && tt < tiles) load_tokens(i, tg, tu);
-      commit_copies();  // (the first commit takes in the weights of all stages)
-      next(tt, tg, tu, tn);
-    }
-  }
+  };
+  fill(load_weights, [] {});
+  start_in_order();
+  fill(load_tokens, [] { commit_copies(); });  // (the first takes in the weights of all stages)
   int stage = 0;
   for (int tile = first_tile; tile < tiles; tile += clusters) {
     for (int i = lane; i < p.T * 16; i += 32) mine[i] = 0.0f;
@@ -551,11 +584,11 @@ __global__ void __launch_bounds__(kWarps * 32, 2) cconv_moe_down_kernel(const Mo
       }
       __syncwarp();
       if (lt < tiles) {
-        load_weights(stage, lt, lgroup, lunit);
-        load_tokens(stage, lgroup, lunit);
+        load_weights(stage);
+        load_tokens(stage);
       }
       commit_copies();
-      next(lt, lgroup, lunit, ln);
+      next();
       if (++stage == kStages) stage = 0;
       if (++unit == units || n + 1 == each) {
         // the group's share: this lane's columns are tokens 2q and 2q + 1 of eight
@@ -567,7 +600,7 @@ __global__ void __launch_bounds__(kWarps * 32, 2) cconv_moe_down_kernel(const Mo
             const int column = 8 * e + 2 * q + c;
             if (column < count) {
               const float w = r.weight[first + column];
-              float* to = mine + r.pairs[first + column] / p.k * 16 + g;
+              float* to = mine + r.token[first + column] * 16 + g;
               to[0] += w * (d[e][c] + d[kNt + e][c]);
               to[8] += w * (d[e][2 + c] + d[kNt + e][2 + c]);
             }
