@@ -70,8 +70,6 @@ __device__ __forceinline__ float scale_of(uint32_t raw, int dtype) {
   return __half2float(__ushort_as_half(uint16_t(raw)));
 }
 
-constexpr int kStages = 4;
-
 // kBytes of a row (from global memory, or zeros) to shared memory, not waited for.
 template <int kBytes>
 __device__ __forceinline__ void copy_piece(uint32_t to, const char* from, bool there) {
@@ -81,94 +79,131 @@ __device__ __forceinline__ void copy_piece(uint32_t to, const char* from, bool t
   else
     asm volatile("cp.async.ca.shared.global [%0], [%1], %2, %3;" ::"r"(to), "l"(from), "n"(kBytes), "r"(n) : "memory");
 }
+__device__ __forceinline__ void commit_copies() { asm volatile("cp.async.commit_group;" ::: "memory"); }
+template <int kLeft>
+__device__ __forceinline__ void wait_for_copies() { asm volatile("cp.async.wait_group %0;" ::"n"(kLeft) : "memory"); }
 
-// A block takes tiles of 16 kMt rows, blockIdx.x and every gridDim.x-th after it, and 8 kNt tokens (blockIdx.y); its
-// warps share k in units of 128.  Each warp copies its units to a ring of its own in shared memory, four ahead, also
-// across tiles: where a block has a tile or two, all that it reads is on its way at once.  Pieces of 16 bytes of a
-// row change places by the row, so that the words that a warp reads together lie in different banks.  Scales come
-// with the unit into registers, a fourth of them to each of the four lanes that share a row.
-template <typename T, int kGroups, int kNt, int kMt>
+// Where byte `byte` of a row of nibbles (64 bytes a unit) or of a token (256 bytes a unit) lies in shared memory: 16-byte
+// pieces change places by the row, so that what a warp reads together lies in different banks.
+__device__ __forceinline__ uint32_t row_place(int row, int byte) { return row * 64 + (byte ^ ((row >> 1 & 3) << 4)); }
+__device__ __forceinline__ uint32_t token_place(int token, int byte) { return token * 256 + (byte ^ ((token & 1) << 6)); }
+
+// Copies a unit of 8 kEach rows of nibbles: row_of(r) is where row r begins.
+template <int kEach, typename Row>
+__device__ __forceinline__ void copy_rows(uint32_t to, int lane, const Int4Params& p, const char* const (&rows)[kEach], int unit, Row row_of) {
+  if (p.piece == 16) {  // (rows: those of this lane)
+    const int64_t at = int64_t(unit) * 64 + (lane & 3) * 16;
+    const bool there = at < p.w_bytes;
+#pragma unroll
+    for (int i = 0; i < kEach; ++i) copy_piece<16>(to + row_place(i * 8 + (lane >> 2), (lane & 3) * 16), rows[i] + (there ? at : 0), there);
+    return;
+  }
+  auto pieces = [&](auto bytes) {
+    constexpr int kBytes = decltype(bytes)::value, kAcross = 64 / kBytes;
+#pragma unroll 4
+    for (int c = lane; c < 8 * kEach * kAcross; c += 32) {
+      const int r = c / kAcross, off = c % kAcross * kBytes;
+      const int64_t at = int64_t(unit) * 64 + off;
+      const bool there = at < p.w_bytes;
+      copy_piece<kBytes>(to + row_place(r, off), row_of(r) + (there ? at : 0), there);
+    }
+  };
+  if (p.piece == 8) pieces(std::integral_constant<int, 8>());
+  else pieces(std::integral_constant<int, 4>());
+}
+
+// Up to 8 tokens.  A block takes tiles of 16 kMt rows, blockIdx.x and every gridDim.x-th after it; its warps share k in
+// units of 128.  Each warp copies its units, weights and tokens, to a ring of its own in shared memory, also across
+// tiles: where a block has a tile or two, nearly all that it reads is on its way at once.  Scales come with the unit into
+// registers, a fourth of them to each of the four lanes that share a row.
+constexpr int kStages = 3;
+template <typename T, int kGroups, int kMt>
 __global__ void __launch_bounds__(kWarps * 32, 2) cconv_int4_kernel(const Int4Params p) {
   constexpr int kRows = 2 * kMt;  // rows of a lane
-  constexpr int kScales = (kRows * kGroups + 3) / 4, kUnitBytes = 16 * kMt * 64;
+  constexpr int kScales = (kRows * kGroups + 3) / 4, kWeightBytes = 16 * kMt * 64;
   extern __shared__ __align__(128) uint8_t smem[];
-  float(*const sums)[128] = reinterpret_cast<float(*)[128]>(smem);  // [kMt * kNt * kWarps]
+  float(*const sums)[128] = reinterpret_cast<float(*)[128]>(smem);  // [kMt * kWarps]
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, g = lane >> 2, q = lane & 3;
-  const uint8_t* const ring = smem + kMt * kNt * kWarps * 512 + warp * (kStages * kUnitBytes);
+  const int unit_bytes = kWeightBytes + p.M * 256;
+  const uint8_t* const ring = smem + kMt * kWarps * 512 + warp * (kStages * unit_bytes);
   const uint32_t ring_at = smem_u32(ring);
   const int tiles = int((p.N + 16 * kMt - 1) / (16 * kMt));
   const int u0 = warp * p.per;
   const int mine = int(blockIdx.x) < tiles ? (tiles - 1 - int(blockIdx.x)) / int(gridDim.x) + 1 : 0;
-  const int t0 = blockIdx.y * 8 * kNt;
   const int64_t last = p.N - 1;
 
   uint32_t scale[kStages][kScales], zero[kStages][kScales];
   int lt = blockIdx.x, lu = 0;
-  auto copy_unit = [&](auto bytes, uint32_t to, int unit) {
-    constexpr int kBytes = decltype(bytes)::value, kAcross = 64 / kBytes;
+  const char *rows[kRows], *scales[kScales];  // of the tile: what this lane copies of, and its scales' rows
+  const uint8_t* zeros[kScales];
+  const int scale_bytes = p.scale_dtype == CCONV_TYPE_FP32 ? 4 : 2;
+  auto row_of = [&](int r) { return p.w + min(int64_t(lt) * (16 * kMt) + r, last) * p.w_rs; };
+  // scale number j of a unit: group j / kRows, row j % kRows; lane q has those with j % 4 = q
+  auto aim = [&]() {
 #pragma unroll
-    for (int i = 0; i < kUnitBytes / 32 / kBytes; ++i) {
-      const int c = i * 32 + lane, r = c / kAcross, off = c % kAcross * kBytes;
-      const int64_t row = min(int64_t(lt) * (16 * kMt) + r, last), at = int64_t(unit) * 64 + off;
-      const bool there = at < p.w_bytes;
-      copy_piece<kBytes>(to + r * 64 + (off ^ ((r >> 1 & 3) << 4)), p.w + row * p.w_rs + (there ? at : 0), there);
+    for (int i = 0; i < kRows; ++i) rows[i] = row_of(i * 8 + (lane >> 2));
+#pragma unroll
+    for (int i = 0; i < kScales; ++i) {
+      const int64_t r = min(int64_t(lt) * (16 * kMt) + g + 8 * ((4 * i + q) % kRows), last);
+      scales[i] = p.scale + r * p.s_rs * scale_bytes;
+      zeros[i] = p.zero + r * p.z_rs;
     }
   };
   auto load = [&](int stage, uint32_t (&s)[kScales], uint32_t (&z)[kScales]) {
     const int unit = u0 + lu;
     if (lt < tiles && unit < p.units) {
-      const uint32_t to = ring_at + stage * kUnitBytes;
-      if (p.piece == 16) copy_unit(std::integral_constant<int, 16>(), to, unit);
-      else if (p.piece == 8) copy_unit(std::integral_constant<int, 8>(), to, unit);
-      else copy_unit(std::integral_constant<int, 4>(), to, unit);
-      // scale number j of the unit: group j / kRows, row j % kRows; lane q has those with j % 4 = q
+      const uint32_t to = ring_at + stage * unit_bytes;
+      copy_rows(to, lane, p, rows, unit, row_of);
+      const int64_t k0 = int64_t(unit) * 128 + (lane & 15) * 8;
+      const bool there = k0 < p.x_k;
+      for (int t = lane >> 4; t < p.M; t += 2)
+        copy_piece<16>(to + kWeightBytes + token_place(t, (lane & 15) * 16), p.x + t * p.x_rs + (there ? k0 * 2 : 0), there);
 #pragma unroll
       for (int i = 0; i < kScales; ++i) {
-        const int j = 4 * i + q;
-        const int64_t r = min(int64_t(lt) * (16 * kMt) + g + 8 * (j % kRows), last), grp = min(unit * kGroups + j / kRows, p.groups - 1);
-        s[i] = load_scale(p.scale, p.scale_dtype, r * p.s_rs + grp * p.s_cs);
-        if (p.zero) z[i] = __ldg(p.zero + r * p.z_rs + grp * p.z_cs);
+        const int64_t grp = min(unit * kGroups + (4 * i + q) / kRows, p.groups - 1);
+        s[i] = load_scale(scales[i], p.scale_dtype, grp * p.s_cs);
+        if (p.zero) z[i] = __ldg(zeros[i] + grp * p.z_cs);
       }
     }
-    asm volatile("cp.async.commit_group;" ::: "memory");
-    if (++lu == p.per) lu = 0, lt += gridDim.x;
+    commit_copies();
+    if (++lu == p.per) {
+      lu = 0;
+      lt += gridDim.x;
+      aim();
+    }
   };
 
   start_in_order();
+  aim();
 #pragma unroll
   for (int i = 0; i < kStages; ++i) load(i, scale[i], zero[i]);
 
-  float acc[kMt][kNt][4] = {};
+  float acc[kMt][4] = {};
   int tile = blockIdx.x, step = 0;
   auto use = [&](int stage, const uint32_t (&s)[kScales], const uint32_t (&z)[kScales]) {
     const int unit = u0 + step;
-    asm volatile("cp.async.wait_group %0;" ::"n"(kStages - 1) : "memory");
+    wait_for_copies<kStages - 1>();
     __syncwarp();
     if (unit < p.units) {
-      const uint8_t* const from = ring + stage * kUnitBytes + g * 64 + q * 4;
-      float d[kMt][kNt][4] = {}, sum[kNt][4] = {};
+      const uint8_t* const from = ring + stage * unit_bytes;
+      float d[kMt][4] = {}, sum[4] = {};
 #pragma unroll
       for (int i = 0; i < 4; ++i) {
-        const int64_t k0 = int64_t(unit) * 128 + i * 32 + q * 8;
         uint32_t w[kRows];
 #pragma unroll
-        for (int r = 0; r < kRows; ++r) w[r] = *reinterpret_cast<const uint32_t*>(from + r * 512 + ((i ^ (g >> 1)) << 4));
+        for (int r = 0; r < kRows; ++r) w[r] = *reinterpret_cast<const uint32_t*>(from + row_place(g + 8 * r, i * 16 + q * 4));
+        // (a column behind the last token repeats it and goes nowhere)
+        const uint4 v = *reinterpret_cast<const uint4*>(from + kWeightBytes + token_place(min(g, p.M - 1), i * 64 + q * 16));
+        const uint32_t x0 = __byte_perm(v.x, v.z, 0x5410), x1 = __byte_perm(v.x, v.z, 0x7632);
+        const uint32_t x2 = __byte_perm(v.y, v.w, 0x5410), x3 = __byte_perm(v.y, v.w, 0x7632);
+        constexpr uint32_t one = Code<T>::kOnes;
+        mma16<T>(sum, one, one, one, one, x0, x1);
+        mma16<T>(sum, one, one, one, one, x2, x3);
 #pragma unroll
-        for (int e = 0; e < kNt; ++e) {
-          const int token = t0 + 8 * e + g;
-          uint4 v = make_uint4(0, 0, 0, 0);
-          if (token < p.M && k0 < p.x_k) v = *reinterpret_cast<const uint4*>(p.x + token * p.x_rs + k0 * 2);
-          const uint32_t x0 = __byte_perm(v.x, v.z, 0x5410), x1 = __byte_perm(v.x, v.z, 0x7632);
-          const uint32_t x2 = __byte_perm(v.y, v.w, 0x5410), x3 = __byte_perm(v.y, v.w, 0x7632);
-          constexpr uint32_t one = Code<T>::kOnes;
-          mma16<T>(sum[e], one, one, one, one, x0, x1);
-          mma16<T>(sum[e], one, one, one, one, x2, x3);
-#pragma unroll
-          for (int m = 0; m < kMt; ++m) {
-            const uint32_t lo = w[2 * m], hi = w[2 * m + 1];
-            mma16<T>(d[m][e], two_of<T, 0>(lo), two_of<T, 0>(hi), two_of<T, 1>(lo), two_of<T, 1>(hi), x0, x1);
-            mma16<T>(d[m][e], two_of<T, 2>(lo), two_of<T, 2>(hi), two_of<T, 3>(lo), two_of<T, 3>(hi), x2, x3);
-          }
+        for (int m = 0; m < kMt; ++m) {
+          const uint32_t lo = w[2 * m], hi = w[2 * m + 1];
+          mma16<T>(d[m], two_of<T, 0>(lo), two_of<T, 0>(hi), two_of<T, 1>(lo), two_of<T, 1>(hi), x0, x1);
+          mma16<T>(d[m], two_of<T, 2>(lo), two_of<T, 2>(hi), two_of<T, 3>(lo), two_of<T, 3>(hi), x2, x3);
         }
         if ((i + 1) % (4 / kGroups) == 0) {  // a group's sums are complete: scaled and added up
 #pragma unroll
@@ -177,18 +212,14 @@ __global__ void __launch_bounds__(kWarps * 32, 2) cconv_int4_kernel(const Int4Pa
             const float by = scale_of(__shfl_sync(0xffffffffu, s[j / 4], lane_of), p.scale_dtype);
             const float zp = p.zero ? 16.0f + float(__shfl_sync(0xffffffffu, z[j / 4], lane_of) & 15u) : 24.0f;
 #pragma unroll
-            for (int e = 0; e < kNt; ++e)
-#pragma unroll
-              for (int c = 0; c < 2; ++c) {
-                float& f = d[r >> 1][e][(r & 1) * 2 + c];
-                acc[r >> 1][e][(r & 1) * 2 + c] += by * (f - zp * sum[e][c]);
-                f = 0.0f;
-              }
+            for (int c = 0; c < 2; ++c) {
+              float& f = d[r >> 1][(r & 1) * 2 + c];
+              acc[r >> 1][(r & 1) * 2 + c] += by * (f - zp * sum[c]);
+              f = 0.0f;
+            }
           }
 #pragma unroll
-          for (int e = 0; e < kNt; ++e)
-#pragma unroll
-            for (int c = 0; c < 4; ++c) sum[e][c] = 0.0f;
+          for (int c = 0; c < 4; ++c) sum[c] = 0.0f;
         }
       }
     }
@@ -199,24 +230,22 @@ __global__ void __launch_bounds__(kWarps * 32, 2) cconv_int4_kernel(const Int4Pa
 #pragma unroll
     for (int m = 0; m < kMt; ++m)
 #pragma unroll
-      for (int e = 0; e < kNt; ++e)
-#pragma unroll
-        for (int i = 0; i < 4; ++i) {
-          sums[(m * kNt + e) * kWarps + warp][i * 32 + lane] = acc[m][e][i];
-          acc[m][e][i] = 0.0f;
-        }
+      for (int i = 0; i < 4; ++i) {
+        sums[m * kWarps + warp][i * 32 + lane] = acc[m][i];
+        acc[m][i] = 0.0f;
+      }
     __syncthreads();
     const int64_t n0 = int64_t(tile) * (16 * kMt);
-    for (int i = threadIdx.x; i < 128 * kMt * kNt; i += kWarps * 32) {
+    for (int i = threadIdx.x; i < 16 * kMt * p.M; i += kWarps * 32) {
       // (neighbouring threads: neighbouring rows)
       const int r = i % (16 * kMt), t = i / (16 * kMt), rr = r & 15;
-      if (t0 + t < p.M && n0 + r < p.N) {
-        const float(*part)[128] = sums + ((r >> 4) * kNt + (t >> 3)) * kWarps;
-        const int at = ((rr >> 3) * 2 + (t & 1)) * 32 + (rr & 7) * 4 + ((t & 7) >> 1);
+      if (n0 + r < p.N) {
+        const float(*part)[128] = sums + (r >> 4) * kWarps;
+        const int at = ((rr >> 3) * 2 + (t & 1)) * 32 + (rr & 7) * 4 + (t >> 1);
         float f = 0.0f;
 #pragma unroll
         for (int w = 0; w < kWarps; ++w) f += part[w][at];
-        static_cast<T*>(const_cast<void*>(p.out.p))[(t0 + t) * p.out.rs + (n0 + r) * p.out.cs] = from_f32<T>(f);
+        static_cast<T*>(const_cast<void*>(p.out.p))[t * p.out.rs + (n0 + r) * p.out.cs] = from_f32<T>(f);
       }
     }
     tile += gridDim.x;
@@ -231,6 +260,168 @@ __global__ void __launch_bounds__(kWarps * 32, 2) cconv_int4_kernel(const Int4Pa
       }
     }
   }
+}
+
+// q - z as pairs of 16-bit numbers, of neighbouring nibbles: bytes that hold a nibble each become the lower bytes of
+// 128 + q (bf16) or 1024 + q (fp16), from which 128 + z or 1024 + z (`bias`) is taken off, exactly.
+template <typename T>
+struct High {
+  static constexpr uint32_t kByte = 0x43434343u, kBase = 0x43004300u;
+};
+template <>
+struct High<__half> {
+  static constexpr uint32_t kByte = 0x64646464u, kBase = 0x64006400u;
+};
+template <typename T>
+__device__ __forceinline__ uint32_t minus2(uint32_t a, uint32_t b);
+template <>
+__device__ __forceinline__ uint32_t minus2<__nv_bfloat16>(uint32_t a, uint32_t b) {
+  const __nv_bfloat162 v = __hsub2(*reinterpret_cast<const __nv_bfloat162*>(&a), *reinterpret_cast<const __nv_bfloat162*>(&b));
+  return *reinterpret_cast<const uint32_t*>(&v);
+}
+template <>
+__device__ __forceinline__ uint32_t minus2<__half>(uint32_t a, uint32_t b) {
+  const __half2 v = __hsub2(*reinterpret_cast<const __half2*>(&a), *reinterpret_cast<const __half2*>(&b));
+  return *reinterpret_cast<const uint32_t*>(&v);
+}
+template <typename T>
+__device__ __forceinline__ void pairs_of(uint32_t v, uint32_t bias, uint32_t (&w)[4]) {
+  const uint32_t even = v & 0x0f0f0f0fu, odd = v >> 4 & 0x0f0f0f0fu;
+  const uint32_t lo = __byte_perm(even, odd, 0x5140), hi = __byte_perm(even, odd, 0x7362);
+  w[0] = minus2<T>(__byte_perm(lo, High<T>::kByte, 0x4140), bias);
+  w[1] = minus2<T>(__byte_perm(lo, High<T>::kByte, 0x4342), bias);
+  w[2] = minus2<T>(__byte_perm(hi, High<T>::kByte, 0x4140), bias);
+  w[3] = minus2<T>(__byte_perm(hi, High<T>::kByte, 0x4342), bias);
+}
+
+// 9 to 64 tokens: their words, not the weights, would fill the shared memory's bandwidth if each warp fetched its own.  So
+// the warps of a block share the tokens of a unit and take 16 rows each; a cluster of `parts` blocks shares k, and
+// adds up its sums through distributed shared memory in a fixed order.
+template <typename T, int kGroups, int kNt>
+__global__ void __launch_bounds__(kWarps * 32, 2) cconv_int4_tokens_kernel(const Int4Params p, const int parts) {
+  constexpr int kScales = (2 * kGroups + 3) / 4, kRowsBytes = 16 * 64, kWeightBytes = kWarps * kRowsBytes;
+  constexpr int kUnitBytes = kWeightBytes + 8 * kNt * 256;
+  extern __shared__ __align__(128) uint8_t smem[];
+  const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, g = lane >> 2, q = lane & 3;
+  const int rank = int(blockIdx.x) % parts;
+  const int64_t n0 = int64_t(blockIdx.x) / parts * (16 * kWarps), row0 = n0 + warp * 16, last = p.N - 1;
+  const int u0 = int(int64_t(p.units) * rank / parts), u1 = int(int64_t(p.units) * (rank + 1) / parts);
+  const char *rows[2], *scales[kScales];
+  const uint8_t* zeros[kScales];
+  const int scale_bytes = p.scale_dtype == CCONV_TYPE_FP32 ? 4 : 2;
+  auto row_of = [&](int r) { return p.w + min(row0 + r, last) * p.w_rs; };
+#pragma unroll
+  for (int i = 0; i < 2; ++i) rows[i] = row_of(i * 8 + (lane >> 2));
+  // scale number j of a unit: group j / 2, row j % 2; lane q has those with j % 4 = q
+#pragma unroll
+  for (int i = 0; i < kScales; ++i) {
+    const int64_t r = min(row0 + g + 8 * (q % 2), last);
+    scales[i] = p.scale + r * p.s_rs * scale_bytes;
+    zeros[i] = p.zero + r * p.z_rs;
+  }
+  uint32_t scale[kStages][kScales], zero[kStages][kScales];
+  auto load = [&](int stage, int unit, uint32_t (&s)[kScales], uint32_t (&z)[kScales]) {
+    if (unit < u1) {
+      const uint32_t to = smem_u32(smem) + stage * kUnitBytes;
+      copy_rows(to + warp * kRowsBytes, lane, p, rows, unit, row_of);
+      const int64_t k0 = int64_t(unit) * 128 + (lane & 15) * 8;
+      const bool there = k0 < p.x_k;
+#pragma unroll
+      for (int i = 0; i < kNt / 2 + (kNt == 1); ++i) {
+        const int t = i * 16 + int(threadIdx.x >> 4);
+        if (t < p.M) copy_piece<16>(to + kWeightBytes + token_place(t, (lane & 15) * 16), p.x + t * p.x_rs + (there ? k0 * 2 : 0), there);
+      }
+#pragma unroll
+      for (int i = 0; i < kScales; ++i) {
+        const int64_t grp = min(unit * kGroups + (4 * i + q) / 2, p.groups - 1);
+        s[i] = load_scale(scales[i], p.scale_dtype, grp * p.s_cs);
+        if (p.zero) z[i] = __ldg(zeros[i] + grp * p.z_cs);
+      }
+    }
+    commit_copies();
+  };
+
+  start_in_order();
+#pragma unroll
+  for (int i = 0; i < kStages - 1; ++i) load(i, u0 + i, scale[i], zero[i]);
+  float acc[kNt][4] = {};
+  auto use = [&](int stage, const uint32_t (&s)[kScales], const uint32_t (&z)[kScales]) {
+    const uint8_t* const from = smem + stage * kUnitBytes;
+    float d[kNt][4] = {};
+    uint32_t bias[2];
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+      if (i % (4 / kGroups) == 0) {
+#pragma unroll
+        for (int r = 0; r < 2; ++r) {
+          const int j = i * kGroups / 4 * 2 + r;
+          const uint32_t zp = p.zero ? __shfl_sync(0xffffffffu, z[j / 4], (lane & 28) | (j & 3)) & 15u : 8u;
+          bias[r] = High<T>::kBase | zp * 0x10001u;
+        }
+      }
+      uint32_t lo[4], hi[4];
+      pairs_of<T>(*reinterpret_cast<const uint32_t*>(from + warp * kRowsBytes + row_place(g, i * 16 + q * 4)), bias[0], lo);
+      pairs_of<T>(*reinterpret_cast<const uint32_t*>(from + warp * kRowsBytes + row_place(g + 8, i * 16 + q * 4)), bias[1], hi);
+#pragma unroll
+      for (int e = 0; e < kNt; ++e) {
+        if (8 * e >= p.M) break;
+        // (columns behind the last token: whatever lies there, for sums that go nowhere)
+        const uint4 v = *reinterpret_cast<const uint4*>(from + kWeightBytes + token_place(8 * e + g, i * 64 + q * 16));
+        mma16<T>(d[e], lo[0], hi[0], lo[1], hi[1], v.x, v.y);
+        mma16<T>(d[e], lo[2], hi[2], lo[3], hi[3], v.z, v.w);
+      }
+      if ((i + 1) % (4 / kGroups) == 0) {
+#pragma unroll
+        for (int r = 0; r < 2; ++r) {
+          const int j = i * kGroups / 4 * 2 + r;
+          const float by = scale_of(__shfl_sync(0xffffffffu, s[j / 4], (lane & 28) | (j & 3)), p.scale_dtype);
+#pragma unroll
+          for (int e = 0; e < kNt; ++e)
+#pragma unroll
+            for (int c = 0; c < 2; ++c) {
+              acc[e][r * 2 + c] += by * d[e][r * 2 + c];
+              d[e][r * 2 + c] = 0.0f;
+            }
+        }
+      }
+    }
+  };
+  for (int u = u0; u < u1; u += kStages) {
+#pragma unroll
+    for (int i = 0; i < kStages; ++i) {
+      if (u + i >= u1) break;
+      wait_for_copies<kStages - 2>();
+      __syncthreads();  // the unit is there for all, and the one before has been read by all
+      constexpr int kBehind = kStages - 1;
+      load((i + kBehind) % kStages, u + i + kBehind, scale[(i + kBehind) % kStages], zero[(i + kBehind) % kStages]);
+      use(i, scale[i], zero[i]);
+    }
+  }
+  __syncthreads();
+  // sums as [token][row] in the ring's place
+  float* const sums = reinterpret_cast<float*>(smem);
+  constexpr int kPitch = 16 * kWarps + 4;
+#pragma unroll
+  for (int e = 0; e < kNt; ++e)
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+      const int t = 8 * e + 2 * q + (i & 1);
+      if (t < p.M) sums[t * kPitch + warp * 16 + g + (i >> 1) * 8] = acc[e][i];
+    }
+  if (parts > 1) cluster_sync_all();
+  else __syncthreads();
+  for (int i = threadIdx.x + rank * kWarps * 32; i < p.M * 16 * kWarps; i += parts * kWarps * 32) {
+    const int r = i % (16 * kWarps), t = i / (16 * kWarps);
+    float f = 0.0f;
+    if (parts > 1) {
+      const uint32_t at = smem_u32(sums + t * kPitch + r);
+      for (int b = 0; b < parts; ++b) f += load_cluster(cluster_map_shared(at, b));
+    } else {
+      f = sums[t * kPitch + r];
+    }
+    if (n0 + r < p.N) static_cast<T*>(const_cast<void*>(p.out.p))[t * p.out.rs + (n0 + r) * p.out.cs] = from_f32<T>(f);
+  }
+  if (parts > 1) cluster_sync_all();  // no block leaves while others read its sums
 }
 
 // The weights as numbers of the operands' type, for products of many tokens: 8 neighbours of a row a thread.
@@ -270,25 +461,34 @@ __global__ void __launch_bounds__(256) cconv_int4_expand_kernel(const ExpandPara
   }
 }
 
-template <typename T, int kGroups, int kNt, int kMt>
+template <typename T, int kGroups, int kMt>
 cudaError_t launch_rows(const Int4Params& p, int sms, cudaStream_t s) {
-  auto f = cconv_int4_kernel<T, kGroups, kNt, kMt>;
-  constexpr int kSmem = kMt * kNt * kWarps * 512 + kWarps * kStages * 16 * kMt * 64;
+  auto f = cconv_int4_kernel<T, kGroups, kMt>;
   static bool ready[64] = {};
-  if (kSmem > 48 * 1024) {
-    const cudaError_t e = allow_smem(f, ready, kSmem);
-    if (e != cudaSuccess) return e;
-  }
-  const dim3 grid(unsigned(std::min<int64_t>(cdiv64(p.N, 16 * kMt), 2 * sms)), unsigned(cdiv64(p.M, 8 * kNt)));
-  return launch(f, grid, kWarps * 32, kSmem, 1, s, p);
+  const cudaError_t e = allow_smem(f, ready, kMt * kWarps * 512 + kWarps * kStages * (16 * kMt * 64 + 8 * 256));
+  if (e != cudaSuccess) return e;
+  const dim3 grid(unsigned(std::min<int64_t>(cdiv64(p.N, 16 * kMt), 2 * sms)));
+  return launch(f, grid, kWarps * 32, size_t(kMt * kWarps * 512 + kWarps * kStages * (16 * kMt * 64 + p.M * 256)), 1, s, p);
+}
+template <typename T, int kGroups, int kNt>
+cudaError_t launch_shared(const Int4Params& p, int sms, cudaStream_t s) {
+  auto f = cconv_int4_tokens_kernel<T, kGroups, kNt>;
+  constexpr int kSmem = std::max(kStages * (kWarps * 16 * 64 + 8 * kNt * 256), 8 * kNt * (16 * kWarps + 4) * 4);
+  static bool ready[64] = {};
+  const cudaError_t e = allow_smem(f, ready, kSmem);
+  if (e != cudaSuccess) return e;
+  const int64_t tiles = cdiv64(p.N, 16 * kWarps);
+  int parts = 1;
+  while (parts < 8 && 2 * parts <= p.units && tiles * parts < sms + sms / 2) parts *= 2;
+  return launch(f, dim3(unsigned(tiles * parts)), kWarps * 32, kSmem, parts, s, p, parts);
 }
 template <typename T, int kGroups>
 cudaError_t launch_tokens(const Int4Params& p, int sms, cudaStream_t s) {
+  if (p.M > 32) return launch_shared<T, kGroups, 8>(p, sms, s);
+  if (p.M > 16) return launch_shared<T, kGroups, 4>(p, sms, s);
+  if (p.M > 8) return launch_shared<T, kGroups, 2>(p, sms, s);
   // 32 rows a tile where that leaves no SM idle
-  const bool two = cdiv64(p.N, 32) >= sms;
-  if (p.M <= 8) return two ? launch_rows<T, kGroups, 1, 2>(p, sms, s) : launch_rows<T, kGroups, 1, 1>(p, sms, s);
-  if (p.M <= 16) return two ? launch_rows<T, kGroups, 2, 2>(p, sms, s) : launch_rows<T, kGroups, 2, 1>(p, sms, s);
-  return launch_rows<T, kGroups, 4, 1>(p, sms, s);  // (32 rows by 32 tokens need more registers than there are)
+  return cdiv64(p.N, 32) >= sms ? launch_rows<T, kGroups, 2>(p, sms, s) : launch_rows<T, kGroups, 1>(p, sms, s);
 }
 template <typename T>
 cudaError_t launch_few(const Int4Params& p, int group, int sms, cudaStream_t s) {

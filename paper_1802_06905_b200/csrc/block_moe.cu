@@ -62,12 +62,6 @@ __device__ __forceinline__ uint64_t warp_max(uint64_t v) {
   const uint32_t lo = __reduce_max_sync(0xffffffffu, uint32_t(v >> 32) == hi ? uint32_t(v) : 0u);
   return uint64_t(hi) << 32 | lo;
 }
-__device__ __forceinline__ float load_cluster(uint32_t at) {
-  float v;
-  asm volatile("ld.shared::cluster.f32 %0, [%1];" : "=f"(v) : "r"(at) : "memory");
-  return v;
-}
-
 // Channels are dealt to the blocks of the cluster, and a block's share of them and 16 experts at a time to its warps:
 // with the usual sizes a warp's loads are all on their way at once.  Partial scores [slice][token][expert] lie in
 // shared memory, a block adds its own up, and the warp that chooses for a token adds up the blocks'.
