@@ -7,7 +7,7 @@
 // second goes through each block's share backwards, so that what the first read last comes out of L2.
 // Where nothing is to be done in place (factor 1) the second pass ends after the sums.
 //
-// Squares are added up in fp32 over the 16 or 32 elements that a thread has of a piece, which go on in 64 bits.  Where
+// Squares are added up in fp32 over the 16 to 64 elements that a thread has of a piece, which go on in 64 bits.  Where
 // fp32 cannot hold them (elements beyond 1e18, or all below 1e-15) the elements are squared in 64 bits.
 #include "block_clip.h"
 
@@ -19,10 +19,10 @@
 namespace cconv {
 namespace {
 
-constexpr int kThreads = 256, kPieceBytes = 16384, kBlocksAnSm = 8;
+constexpr int kThreads = 256, kBlocksAnSm = 4;
 
-// A tensor as rows of elements.  Pieces are 16384 bytes of a row or, where rows are short or elements apart
-// (`scattered`), as many elements in the order of rows.
+// A tensor as rows of elements.  Pieces are kVectors x 16 bytes a thread of a row or, where rows are short or elements
+// apart (`scattered`), as many elements in the order of rows.
 struct Item {
   const void* p;
   void* out;
@@ -57,7 +57,7 @@ __device__ __forceinline__ double block_sum(double v) {
   return s;
 }
 
-// What a thread has of a piece: up to 4 accesses of 16 bytes, and one element in front of and behind them.
+// What a thread has of a piece: up to kVectors accesses of 16 bytes, and one element in front of and behind them.
 template <typename T>
 struct Piece {
   static constexpr int E = 16 / int(sizeof(T));
@@ -87,21 +87,21 @@ __device__ __forceinline__ void unpack16(const uint4& w, float (&f)[16 / sizeof(
 }
 
 // The sum of squares of what a thread has of a piece, in 64 bits where fp32 cannot hold it.
-template <typename T>
+template <typename T, int kVectors>
 __device__ __forceinline__ double squares(const Piece<T>& piece) {
   constexpr int E = Piece<T>::E;
   const int tid = threadIdx.x;
   const uint4* v = reinterpret_cast<const uint4*>(piece.from + piece.head);
-  uint4 w[4];
+  uint4 w[kVectors];
 #pragma unroll
-  for (int i = 0; i < 4; ++i) w[i] = i * kThreads + tid < piece.vectors ? __ldcg(v + i * kThreads + tid) : make_uint4(0, 0, 0, 0);
+  for (int i = 0; i < kVectors; ++i) w[i] = i * kThreads + tid < piece.vectors ? __ldcg(v + i * kThreads + tid) : make_uint4(0, 0, 0, 0);
   float ends[2] = {0.0f, 0.0f};
   if (tid < piece.head) ends[0] = to_f32(piece.from[tid]);
   if (tid < piece.tail) ends[1] = to_f32(piece.from[piece.head + piece.vectors * E + tid]);
   float s[2] = {ends[0] * ends[0], ends[1] * ends[1]};
   uint32_t any = (__float_as_uint(ends[0]) | __float_as_uint(ends[1])) << 1;
 #pragma unroll
-  for (int i = 0; i < 4; ++i) {
+  for (int i = 0; i < kVectors; ++i) {
     float f[E];
     unpack16<T>(w[i], f);
 #pragma unroll
@@ -112,7 +112,7 @@ __device__ __forceinline__ double squares(const Piece<T>& piece) {
   if ((all > 1e-30f && all < 1e37f) || any == 0) return double(all);
   double exact = double(ends[0]) * double(ends[0]) + double(ends[1]) * double(ends[1]);
 #pragma unroll 1
-  for (int i = 0; i < 4; ++i) {
+  for (int i = 0; i < kVectors; ++i) {
     if (i * kThreads + tid >= piece.vectors) break;
     float f[E];
     unpack16<T>(__ldcg(v + i * kThreads + tid), f);
@@ -134,11 +134,11 @@ __device__ __forceinline__ int item_of(const Table<N>& t, int64_t piece) {
   return lo;
 }
 
-constexpr __host__ __device__ int piece_elements(int dtype) { return kPieceBytes / (dtype == CCONV_TYPE_FP32 ? 4 : 2); }
+constexpr int piece_elements(int vectors, int dtype) { return kThreads * 16 * vectors / (dtype == CCONV_TYPE_FP32 ? 4 : 2); }
 
-template <typename T>
+template <typename T, int kVectors>
 __device__ __forceinline__ double item_squares(const Item& it, int64_t piece) {
-  constexpr int kElements = kPieceBytes / int(sizeof(T));
+  constexpr int kElements = kThreads * 16 * kVectors / int(sizeof(T));
   const T* p = static_cast<const T*>(it.p);
   if (it.scattered) {
     double s = 0.0;
@@ -149,11 +149,11 @@ __device__ __forceinline__ double item_squares(const Item& it, int64_t piece) {
     }
     return s;
   }
-  const int64_t row = piece / it.row_pieces, c = piece % it.row_pieces * kElements;
-  return squares<T>(Piece<T>(p + row * it.rs + c, min(it.cols - c, int64_t(kElements))));
+  const int64_t row = it.rows == 1 ? 0 : piece / it.row_pieces, c = (piece - row * it.row_pieces) * kElements;
+  return squares<T, kVectors>(Piece<T>(p + row * it.rs + c, min(it.cols - c, int64_t(kElements))));
 }
 
-template <int N>
+template <int N, int kVectors>
 __global__ void __launch_bounds__(kThreads, kBlocksAnSm) cconv_square_sums_kernel(const __grid_constant__ Table<N> t, double* sums) {
   start_in_order();
   const int64_t p0 = t.pieces * blockIdx.x / gridDim.x, p1 = t.pieces * (blockIdx.x + 1) / gridDim.x;
@@ -162,9 +162,9 @@ __global__ void __launch_bounds__(kThreads, kBlocksAnSm) cconv_square_sums_kerne
   for (int64_t p = p0; p < p1; ++p) {
     while (at + 1 < t.count && t.item[at + 1].first <= p) ++at;
     const Item& it = t.item[at];
-    if (it.dtype == CCONV_TYPE_BF16) s += item_squares<__nv_bfloat16>(it, p - it.first);
-    else if (it.dtype == CCONV_TYPE_FP16) s += item_squares<__half>(it, p - it.first);
-    else s += item_squares<float>(it, p - it.first);
+    if (it.dtype == CCONV_TYPE_BF16) s += item_squares<__nv_bfloat16, kVectors>(it, p - it.first);
+    else if (it.dtype == CCONV_TYPE_FP16) s += item_squares<__half, kVectors>(it, p - it.first);
+    else s += item_squares<float, kVectors>(it, p - it.first);
   }
   s = block_sum(s);
   if (threadIdx.x == 0) sums[blockIdx.x] = s;
@@ -182,9 +182,9 @@ __global__ void __launch_bounds__(kThreads) cconv_norm_of_sums_kernel(const doub
   if (threadIdx.x == 0) *norm = v;
 }
 
-template <typename T>
+template <typename T, int kVectors>
 __device__ __forceinline__ void item_scale(const Item& it, int64_t piece, float by) {
-  constexpr int kElements = kPieceBytes / int(sizeof(T)), E = 16 / int(sizeof(T));
+  constexpr int kElements = kThreads * 16 * kVectors / int(sizeof(T)), E = 16 / int(sizeof(T));
   const T* p = static_cast<const T*>(it.p);
   T* out = static_cast<T*>(it.out);
   const int tid = threadIdx.x;
@@ -196,13 +196,13 @@ __device__ __forceinline__ void item_scale(const Item& it, int64_t piece, float 
     }
     return;
   }
-  const int64_t row = piece / it.row_pieces, c = piece % it.row_pieces * kElements;
+  const int64_t row = it.rows == 1 ? 0 : piece / it.row_pieces, c = (piece - row * it.row_pieces) * kElements;
   const Piece<T> from(p + row * it.rs + c, min(it.cols - c, int64_t(kElements)));
   T* to = out + row * it.out_rs + c;
   const uint4* v = reinterpret_cast<const uint4*>(from.from + from.head);
-  uint4 w[4];
+  uint4 w[kVectors];
 #pragma unroll
-  for (int i = 0; i < 4; ++i)
+  for (int i = 0; i < kVectors; ++i)
     if (i * kThreads + tid < from.vectors) w[i] = __ldcg(v + i * kThreads + tid);
   if (tid < from.head) to[tid] = from_f32<T>(by * to_f32(from.from[tid]));
   const int behind = from.head + from.vectors * E + tid;
@@ -210,7 +210,7 @@ __device__ __forceinline__ void item_scale(const Item& it, int64_t piece, float 
   to += from.head;
   const bool wide = (reinterpret_cast<uintptr_t>(to) & 15) == 0;
 #pragma unroll
-  for (int i = 0; i < 4; ++i) {
+  for (int i = 0; i < kVectors; ++i) {
     const int at = i * kThreads + tid;
     if (at >= from.vectors) break;
     float f[E];
@@ -232,7 +232,7 @@ __device__ __forceinline__ void item_scale(const Item& it, int64_t piece, float 
   }
 }
 
-template <int N>
+template <int N, int kVectors>
 __global__ void __launch_bounds__(kThreads, kBlocksAnSm) cconv_clip_kernel(const __grid_constant__ Table<N> t, const ClipParams c) {
   start_in_order();
   const float norm = c.blocks ? norm_of(c.sums, c.blocks) : *c.norm;
@@ -246,9 +246,9 @@ __global__ void __launch_bounds__(kThreads, kBlocksAnSm) cconv_clip_kernel(const
   for (int64_t p = p1 - 1; p >= p0; --p) {
     while (t.item[at].first > p) --at;
     const Item& it = t.item[at];
-    if (it.dtype == CCONV_TYPE_BF16) item_scale<__nv_bfloat16>(it, p - it.first, by);
-    else if (it.dtype == CCONV_TYPE_FP16) item_scale<__half>(it, p - it.first, by);
-    else item_scale<float>(it, p - it.first, by);
+    if (it.dtype == CCONV_TYPE_BF16) item_scale<__nv_bfloat16, kVectors>(it, p - it.first, by);
+    else if (it.dtype == CCONV_TYPE_FP16) item_scale<__half, kVectors>(it, p - it.first, by);
+    else item_scale<float, kVectors>(it, p - it.first, by);
   }
 }
 
@@ -256,14 +256,21 @@ __global__ void __launch_bounds__(kThreads, kBlocksAnSm) cconv_clip_kernel(const
 // Tables go with the launch: 40 tensors in the 4 KB that every launch has room for, 320 in the 32 KB that it may take.
 constexpr int kFewItems = 40, kMostItems = 320;
 
-int64_t pieces_of(const cconv_tensor& t, bool scattered) {
-  const int64_t n = piece_elements(t.dtype);
+int64_t pieces_of(const cconv_tensor& t, int vectors, bool scattered) {
+  const int64_t n = piece_elements(vectors, t.dtype);
   return scattered ? cdiv64(t.rows * t.cols, n) : t.rows * cdiv64(t.cols, n);
+}
+
+// 8 accesses a thread and piece where there is work for all SMs all the same, else 4.
+int vectors_of(const cconv_clip_args& a, int sms) {
+  double bytes = 0;
+  for (int64_t i = 0; i < a.count; ++i) bytes += double(a.grads[i].rows) * a.grads[i].cols * type_bytes(a.grads[i].dtype);
+  return bytes >= 4.0 * sms * kBlocksAnSm * kThreads * 128 ? 8 : 4;
 }
 
 // Calls f(table, its number) for the tables of the call.
 template <typename F>
-int with_tables(const cconv_clip_args& a, F f) {
+int with_tables(const cconv_clip_args& a, int vectors, F f) {
   Table<kMostItems> t;
   t.count = 0;
   t.pieces = 0;
@@ -297,11 +304,11 @@ int with_tables(const cconv_clip_args& a, F f) {
     it.rs = g.row_stride; it.cs = g.col_stride;
     it.out_rs = o.row_stride; it.out_cs = o.col_stride;
     it.dtype = g.dtype;
-    it.row_pieces = cdiv64(g.cols, piece_elements(g.dtype));
+    it.row_pieces = cdiv64(g.cols, piece_elements(vectors, g.dtype));
     // short rows would leave most of a block idle
     it.scattered = (g.cols > 1 && (g.col_stride != 1 || o.col_stride != 1)) || (g.rows > 1 && g.cols < 1024);
     it.first = t.pieces;
-    t.pieces += pieces_of(g, it.scattered);
+    t.pieces += pieces_of(g, vectors, it.scattered);
     if (t.count == kMostItems) {
       const cudaError_t e = send();
       if (e != cudaSuccess) return block_cuda_error(e, "clipping");
@@ -315,7 +322,7 @@ int blocks_of(int64_t pieces, int sms) { return int(std::min<int64_t>(pieces, in
 // Partial sums of the call: as many as there are blocks in all its launches.
 int sums_of(const cconv_clip_args& a, int sms) {
   int n = 0;
-  with_tables(a, [&](const auto& t, int) {
+  with_tables(a, vectors_of(a, sms), [&](const auto& t, int) {
     n += blocks_of(t.pieces, sms);
     return cudaSuccess;
   });
@@ -328,13 +335,14 @@ int64_t clip_workspace(const cconv_clip_args& a, int sms) { return round_up64(in
 
 int run_square_sums(const cconv_clip_args& a, int sms, cudaStream_t s) {
   double* to = static_cast<double*>(a.workspace);
-  return with_tables(a, [&](const auto& t, int) {
+  const int vectors = vectors_of(a, sms);
+  return with_tables(a, vectors, [&](const auto& t, int) {
     const int n = blocks_of(t.pieces, sms);
     double* mine = to;
     to += n;
+    constexpr int kItems = sizeof(t) == sizeof(Table<kFewItems>) ? kFewItems : kMostItems;
     auto go = [&](auto f) { return launch(f, dim3(unsigned(n)), kThreads, 0, 1, s, t, mine); };
-    if constexpr (sizeof(t) == sizeof(Table<kFewItems>)) return go(cconv_square_sums_kernel<kFewItems>);
-    else return go(cconv_square_sums_kernel<kMostItems>);
+    return vectors == 8 ? go(cconv_square_sums_kernel<kItems, 8>) : go(cconv_square_sums_kernel<kItems, 4>);
   });
 }
 
@@ -351,12 +359,13 @@ int run_clip(const cconv_clip_args& a, int sms, cudaStream_t s) {
   c.max_norm = a.max_norm;
   c.eps = a.eps;
   c.in_place = a.outs == nullptr;
-  return with_tables(a, [&](const auto& t, int number) {
+  const int vectors = vectors_of(a, sms);
+  return with_tables(a, vectors, [&](const auto& t, int number) {
     c.first_launch = number == 0;
     const int n = blocks_of(t.pieces, sms);
+    constexpr int kItems = sizeof(t) == sizeof(Table<kFewItems>) ? kFewItems : kMostItems;
     auto go = [&](auto f) { return launch(f, dim3(unsigned(n)), kThreads, 0, 1, s, t, c); };
-    if constexpr (sizeof(t) == sizeof(Table<kFewItems>)) return go(cconv_clip_kernel<kFewItems>);
-    else return go(cconv_clip_kernel<kMostItems>);
+    return vectors == 8 ? go(cconv_clip_kernel<kItems, 8>) : go(cconv_clip_kernel<kItems, 4>);
   });
 }
 

@@ -3,13 +3,10 @@
 //   C[m][n] = sum_g s[n][g] sum_{k in g} (q[n][k] - z[n][g]) x[m][k]
 //           = sum_g s[n][g] (sum_k (16 + q) x - (16 + z) sum_k x)
 //
-// Few tokens: the weights are read once, through shared memory into warp-wide matrix instructions.  16 + q
-// is a 16-bit number whose mantissa starts with the four bits, so that a shift and a logical operation make two of
-// them; a group's sums come out of the matrix instructions, those of x beside them (rows of ones), and are scaled and
-// added up in fp32.  16 + q against q - z costs a factor of 5 in the sums' rounding, 2^-21 in place of 2^-23.
-//
-// A word holds k = 0 .. 7 in its nibbles; the two that one shift brings in place are four apart, so x's pairs are
-// taken four apart too.
+// Few tokens: the weights are read once, into warp-wide matrix instructions, a group's sums come out of these and are scaled and added up in fp32.  Up to 8 tokens, 16 + q is the number that is multiplied: its mantissa starts with the four
+// bits, so that a shift and a logical operation make two of them (6 operations for two where q - z is formed).  That costs
+// a factor of 5 in the sums' rounding.  A word holds k = 0 .. 7 in its nibbles; the two that one shift brings in
+// place are four apart, so x's pairs are taken four apart too.
 #include "block_int4.h"
 
 #include <algorithm>
@@ -33,12 +30,12 @@ struct Code;  // a nibble as the number 16 + q
 template <>
 struct Code<__nv_bfloat16> {
   static constexpr int kAt = 3;
-  static constexpr uint32_t kMask = 0x00780078u, kBase = 0x41804180u, kOnes = 0x3f803f80u;
+  static constexpr uint32_t kMask = 0x00780078u, kBase = 0x41804180u;
 };
 template <>
 struct Code<__half> {
   static constexpr int kAt = 6;
-  static constexpr uint32_t kMask = 0x03c003c0u, kBase = 0x4c004c00u, kOnes = 0x3c003c00u;
+  static constexpr uint32_t kMask = 0x03c003c0u, kBase = 0x4c004c00u;
 };
 // 16 + q of nibbles i and i + 4.
 template <typename T, int i>
@@ -51,12 +48,17 @@ __device__ __forceinline__ uint32_t two_of(uint32_t v) {
 struct Int4Params {
   const char *x, *w;  // tokens by k; rows of nibbles
   int64_t x_rs, w_rs;  // bytes
+  const char* w_end;   // behind the last row
   const char* scale;
   const uint8_t* zero;
   int64_t s_rs, s_cs, z_rs, z_cs;  // elements
-  int64_t N, x_k, w_bytes;  // x_k, w_bytes: of a row that may be read, multiples of 8 elements and of a piece
-  int M, scale_dtype, piece, groups;
-  int units, per;  // of 128 of k; of a warp
+  int64_t N;
+  uint32_t x_bytes;  // of a token that may be read, a multiple of 16
+  int M, scale_dtype, groups;
+  uint32_t w_bytes;  // of a row
+  uint32_t lies;     // bits in which rows' addresses and lengths differ from multiples of 16 bytes (of 4 they are)
+  int shifted;       // rows do not all begin at multiples of 16 bytes
+  int units, per;    // of 128 of k; of a warp
   Mat out;
 };
 
@@ -83,149 +85,227 @@ __device__ __forceinline__ void commit_copies() { asm volatile("cp.async.commit_
 template <int kLeft>
 __device__ __forceinline__ void wait_for_copies() { asm volatile("cp.async.wait_group %0;" ::"n"(kLeft) : "memory"); }
 
-// Where byte `byte` of a row of nibbles (64 bytes a unit) or of a token (256 bytes a unit) lies in shared memory: 16-byte
-// pieces change places by the row, so that what a warp reads together lies in different banks.
-__device__ __forceinline__ uint32_t row_place(int row, int byte) { return row * 64 + (byte ^ ((row >> 1 & 3) << 4)); }
+// Where byte `byte` of a row of nibbles or of a token (256 bytes a unit) lies in shared memory.  A row has five pieces
+// of 16 bytes: its 64 of a unit may begin within the first.  What a warp reads together lies in different banks: rows are
+// 20 words apart, and the halves of a token's 256 bytes change places by the token.
+constexpr int kRowPitch = 80;
+__device__ __forceinline__ uint32_t row_place(int row, int byte) { return row * kRowPitch + byte; }
 __device__ __forceinline__ uint32_t token_place(int token, int byte) { return token * 256 + (byte ^ ((token & 1) << 6)); }
 
-// Copies a unit of 8 kEach rows of nibbles: row_of(r) is where row r begins.
-template <int kEach, typename Row>
-__device__ __forceinline__ void copy_rows(uint32_t to, int lane, const Int4Params& p, const char* const (&rows)[kEach], int unit, Row row_of) {
-  if (p.piece == 16) {  // (rows: those of this lane)
-    const int64_t at = int64_t(unit) * 64 + (lane & 3) * 16;
-    const bool there = at < p.w_bytes;
-#pragma unroll
-    for (int i = 0; i < kEach; ++i) copy_piece<16>(to + row_place(i * 8 + (lane >> 2), (lane & 3) * 16), rows[i] + (there ? at : 0), there);
-    return;
+// 16 bytes of a row, but for those outside the whole array, where it ends within them (word by word then).
+__device__ __forceinline__ void copy_inside(uint32_t to, const char* from, const Int4Params& p) {
+  if (from >= p.w && from + 16 <= p.w_end) {
+    copy_piece<16>(to, from, true);
+  } else {
+#pragma unroll 1
+    for (int i = 0; i < 16; i += 4)
+      if (from + i >= p.w && from + i < p.w_end) copy_piece<4>(to + i, from + i, true);
   }
-  auto pieces = [&](auto bytes) {
-    constexpr int kBytes = decltype(bytes)::value, kAcross = 64 / kBytes;
-#pragma unroll 4
-    for (int c = lane; c < 8 * kEach * kAcross; c += 32) {
-      const int r = c / kAcross, off = c % kAcross * kBytes;
-      const int64_t at = int64_t(unit) * 64 + off;
-      const bool there = at < p.w_bytes;
-      copy_piece<kBytes>(to + row_place(r, off), row_of(r) + (there ? at : 0), there);
-    }
-  };
-  if (p.piece == 8) pieces(std::integral_constant<int, 8>());
-  else pieces(std::integral_constant<int, 4>());
 }
 
-// Up to 8 tokens.  A block takes tiles of 16 kMt rows, blockIdx.x and every gridDim.x-th after it; its warps share k in
-// units of 128.  Each warp copies its units, weights and tokens, to a ring of its own in shared memory, also across
-// tiles: where a block has a tile or two, nearly all that it reads is on its way at once.  Scales come with the unit into
-// registers, a fourth of them to each of the four lanes that share a row.
-constexpr int kStages = 3;
-template <typename T, int kGroups, int kMt>
-__global__ void __launch_bounds__(kWarps * 32, 2) cconv_int4_kernel(const Int4Params p) {
-  constexpr int kRows = 2 * kMt;  // rows of a lane
-  constexpr int kScales = (kRows * kGroups + 3) / 4, kWeightBytes = 16 * kMt * 64;
-  extern __shared__ __align__(128) uint8_t smem[];
-  float(*const sums)[128] = reinterpret_cast<float(*)[128]>(smem);  // [kMt * kWarps]
-  const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, g = lane >> 2, q = lane & 3;
-  const int unit_bytes = kWeightBytes + p.M * 256;
-  const uint8_t* const ring = smem + kMt * kWarps * 512 + warp * (kStages * unit_bytes);
-  const uint32_t ring_at = smem_u32(ring);
-  const int tiles = int((p.N + 16 * kMt - 1) / (16 * kMt));
-  const int u0 = warp * p.per;
-  const int mine = int(blockIdx.x) < tiles ? (tiles - 1 - int(blockIdx.x)) / int(gridDim.x) + 1 : 0;
-  const int64_t last = p.N - 1;
+// The rows of nibbles that a warp copies a unit of: 8 kEach neighbouring ones.
+template <int kEach>
+struct RowCopies {
+  const char* rows[kEach];  // of this lane's rows, from the multiple of 16 bytes that it begins behind
+  const char* tail;         // of row `lane`: a fifth piece
+  static __device__ __forceinline__ const char* aligned(const char* q) {
+    return reinterpret_cast<const char*>(reinterpret_cast<uintptr_t>(q) & ~uintptr_t(15));
+  }
+  __device__ __forceinline__ void aim(const Int4Params& p, int64_t row0, int lane) {
+    const int64_t last = p.N - 1;
+#pragma unroll
+    for (int i = 0; i < kEach; ++i) rows[i] = aligned(p.w + min(row0 + i * 8 + (lane >> 2), last) * p.w_rs) + (lane & 3) * 16;
+    tail = aligned(p.w + min(row0 + lane, last) * p.w_rs) + 64;
+  }
+  __device__ __forceinline__ void copy(const Int4Params& p, uint32_t to, int lane, int unit) const {
+    const int64_t at = int64_t(unit) * 64;
+#pragma unroll
+    for (int i = 0; i < kEach; ++i) copy_inside(to + row_place(i * 8 + (lane >> 2), (lane & 3) * 16), rows[i] + at, p);
+    if (p.shifted && lane < 8 * kEach) copy_inside(to + row_place(lane, 64), tail + at, p);
+  }
+};
 
-  uint32_t scale[kStages][kScales], zero[kStages][kScales];
-  int lt = blockIdx.x, lu = 0;
-  const char *rows[kRows], *scales[kScales];  // of the tile: what this lane copies of, and its scales' rows
-  const uint8_t* zeros[kScales];
-  const int scale_bytes = p.scale_dtype == CCONV_TYPE_FP32 ? 4 : 2;
-  auto row_of = [&](int r) { return p.w + min(int64_t(lt) * (16 * kMt) + r, last) * p.w_rs; };
-  // scale number j of a unit: group j / kRows, row j % kRows; lane q has those with j % 4 = q
-  auto aim = [&]() {
+// The scales (and zero points) of a unit of kGroups groups and of kRows rows, g + 8 r, that four lanes share: value j is of
+// group j / kRows and row j % kRows; lane q of the four has those with j % 4 = q, and gives them to the others.
+template <int kGroups, int kRows>
+struct Scales {
+  static constexpr int kOwn = (kRows * kGroups + 3) / 4;
+  uint32_t raw[kOwn], zero[kOwn];  // as they come
+};
+template <int kGroups, int kRows>
+struct ScaleRows {
+  using Own = Scales<kGroups, kRows>;
+  const char* at[Own::kOwn];
+  const uint8_t* zero_at[Own::kOwn];
+  __device__ __forceinline__ void aim(const Int4Params& p, int64_t row0, int lane) {  // row0: of g = 0
+    const int es = p.scale_dtype == CCONV_TYPE_FP32 ? 4 : 2;
 #pragma unroll
-    for (int i = 0; i < kRows; ++i) rows[i] = row_of(i * 8 + (lane >> 2));
-#pragma unroll
-    for (int i = 0; i < kScales; ++i) {
-      const int64_t r = min(int64_t(lt) * (16 * kMt) + g + 8 * ((4 * i + q) % kRows), last);
-      scales[i] = p.scale + r * p.s_rs * scale_bytes;
-      zeros[i] = p.zero + r * p.z_rs;
+    for (int i = 0; i < Own::kOwn; ++i) {
+      const int64_t r = min(row0 + (lane >> 2) + 8 * ((4 * i + (lane & 3)) % kRows), p.N - 1);
+      at[i] = p.scale + r * p.s_rs * es;
+      zero_at[i] = p.zero + r * p.z_rs;
     }
-  };
-  auto load = [&](int stage, uint32_t (&s)[kScales], uint32_t (&z)[kScales]) {
-    const int unit = u0 + lu;
-    if (lt < tiles && unit < p.units) {
-      const uint32_t to = ring_at + stage * unit_bytes;
-      copy_rows(to, lane, p, rows, unit, row_of);
-      const int64_t k0 = int64_t(unit) * 128 + (lane & 15) * 8;
-      const bool there = k0 < p.x_k;
-      for (int t = lane >> 4; t < p.M; t += 2)
-        copy_piece<16>(to + kWeightBytes + token_place(t, (lane & 15) * 16), p.x + t * p.x_rs + (there ? k0 * 2 : 0), there);
+  }
+  __device__ __forceinline__ void load(const Int4Params& p, int lane, int unit, Own& s) const {
 #pragma unroll
-      for (int i = 0; i < kScales; ++i) {
-        const int64_t grp = min(unit * kGroups + (4 * i + q) / kRows, p.groups - 1);
-        s[i] = load_scale(scales[i], p.scale_dtype, grp * p.s_cs);
-        if (p.zero) z[i] = __ldg(zeros[i] + grp * p.z_cs);
+    for (int i = 0; i < Own::kOwn; ++i) {
+      const int64_t group = unit * kGroups + (4 * i + (lane & 3)) / kRows;
+      s.raw[i] = s.zero[i] = 0;  // (behind the last group: nothing times nothing)
+      if (group < p.groups && (kRows * kGroups >= 4 || (lane & 3) < kRows * kGroups)) {
+        s.raw[i] = load_scale(at[i], p.scale_dtype, group * p.s_cs);
+        if (p.zero) s.zero[i] = __ldg(zero_at[i] + group * p.z_cs);
       }
     }
-    commit_copies();
-    if (++lu == p.per) {
-      lu = 0;
-      lt += gridDim.x;
-      aim();
+  }
+};
+// The current unit's.
+template <int kGroups, int kRows>
+struct ScaleValues {
+  using Own = Scales<kGroups, kRows>;
+  float by[Own::kOwn], low[Own::kOwn];  // scale; zero point
+  __device__ __forceinline__ ScaleValues(const Int4Params& p, const Own& s) {
+#pragma unroll
+    for (int i = 0; i < Own::kOwn; ++i) {
+      by[i] = scale_of(s.raw[i], p.scale_dtype);
+      low[i] = p.zero ? float(s.zero[i] & 15u) : 8.0f;
     }
+  }
+  __device__ __forceinline__ float scale(int group, int r, int lane) const {
+    const int j = group * kRows + r;
+    return __shfl_sync(0xffffffffu, by[j / 4], (lane & 28) | (j & 3));
+  }
+  __device__ __forceinline__ float zero_point(const Int4Params& p, int group, int r, int lane) const {
+    const int j = group * kRows + r;
+    return p.zero ? __shfl_sync(0xffffffffu, low[j / 4], (lane & 28) | (j & 3)) : 8.0f;
+  }
+};
+
+// Up to 8 tokens: all of them lie in shared memory, in the order in which the matrix instructions take them, with the
+// sums of each group beside them; weights go straight into the registers that multiply them.  A block takes tiles of 16
+// kMt rows, blockIdx.x and every gridDim.x-th after it; its warps share k in units of 128, of which a batch is on its way
+// while the one before is multiplied, also across tiles.  Of a unit, lane q of the four that share a row takes the
+// words of kWords neighbours: no more k than a group has between the four.
+template <typename T, int kWords, int kGroups, int kMt>
+__global__ void __launch_bounds__(kWarps * 32, 2) cconv_int4_kernel(const Int4Params p) {
+  // rows of a lane; loads of a unit; units of a batch (32 words a lane, or 16 where scales take registers too)
+  constexpr int kRows = 2 * kMt, kSteps = 4 / kWords, kUnits = (kGroups == 1 ? 4 : 2) / kMt;
+  extern __shared__ __align__(128) uint8_t smem[];
+  __shared__ float sums[kMt * kWarps][128];
+  uint4* const tokens = reinterpret_cast<uint4*>(smem);  // [unit][word][token][lane of four]
+  float* const totals = reinterpret_cast<float*>(smem + p.units * p.M * 256);  // [unit][group][token]
+  const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, g = lane >> 2, q = lane & 3;
+  const int tiles = int((p.N + 16 * kMt - 1) / (16 * kMt));
+  const int u0 = warp * p.per, u1 = min(p.units, u0 + p.per), batches = (p.per + kUnits - 1) / kUnits;
+  const int mine = int(blockIdx.x) < tiles ? (tiles - 1 - int(blockIdx.x)) / int(gridDim.x) + 1 : 0;
+
+  struct Batch {
+    Words<kWords> w[kUnits][kSteps][kRows];
+    Scales<kGroups, kRows> scales[kUnits];
+  } b[2];
+  const char* rows[kRows];
+  ScaleRows<kGroups, kRows> scale_rows;
+  int lt = blockIdx.x, lb = 0;
+  auto load = [&](Batch& a) {
+    if (lt < tiles) {
+      if (lb == 0) {
+        const int64_t row0 = int64_t(lt) * (16 * kMt);
+        rows[0] = p.w + min(row0 + g, p.N - 1) * p.w_rs + q * (4 * kWords);
+#pragma unroll
+        for (int r = 1; r < kRows; ++r)
+          rows[r] = row0 + 16 * kMt <= p.N ? rows[r - 1] + 8 * p.w_rs : p.w + min(row0 + g + 8 * r, p.N - 1) * p.w_rs + q * (4 * kWords);
+        scale_rows.aim(p, row0, lane);
+      }
+#pragma unroll
+      for (int u = 0; u < kUnits; ++u) {
+        const int unit = u0 + lb * kUnits + u;
+        const uint32_t at = uint32_t(unit) * 64;
+#pragma unroll
+        for (int i = 0; i < kSteps; ++i) {
+          const bool in = unit < u1 && at + (i * 4 + q) * (4 * kWords) < p.w_bytes;
+#pragma unroll
+          for (int r = 0; r < kRows; ++r) {
+            if (in) a.w[u][i][r].load(rows[r] + at + i * 16 * kWords);
+            else a.w[u][i][r].zero();
+          }
+        }
+        if (unit < u1) scale_rows.load(p, lane, unit, a.scales[u]);
+      }
+    }
+    if (++lb == batches) lb = 0, lt += gridDim.x;
   };
 
   start_in_order();
-  aim();
-#pragma unroll
-  for (int i = 0; i < kStages; ++i) load(i, scale[i], zero[i]);
-
-  float acc[kMt][4] = {};
-  int tile = blockIdx.x, step = 0;
-  auto use = [&](int stage, const uint32_t (&s)[kScales], const uint32_t (&z)[kScales]) {
-    const int unit = u0 + step;
-    wait_for_copies<kStages - 1>();
-    __syncwarp();
-    if (unit < p.units) {
-      const uint8_t* const from = ring + stage * unit_bytes;
-      float d[kMt][4] = {}, sum[4] = {};
+  load(b[0]);
+  {
+    // The tokens: eight neighbours of k a thread, four times at once (each alone would wait for memory); the lanes that
+    // have a group's add up their sums.
+    const int pieces = p.units * 16, all = pieces * p.M;  // (pieces: a multiple of 16, whole groups)
+    const unsigned half = (threadIdx.x & 16) ? 0xffff0000u : 0xffffu;
+    for (int c0 = threadIdx.x; c0 < all; c0 += 4 * kWarps * 32) {
+      uint4 v[4];
+      int at[4];  // piece | token << 28
 #pragma unroll
       for (int i = 0; i < 4; ++i) {
-        uint32_t w[kRows];
+        const int c = c0 + i * kWarps * 32, t = c / pieces, piece = c - t * pieces;
+        at[i] = piece | t << 28;
+        v[i] = make_uint4(0, 0, 0, 0);
+        if (c < all && uint32_t(piece) * 16 < p.x_bytes) v[i] = *reinterpret_cast<const uint4*>(p.x + t * p.x_rs + uint32_t(piece) * 16);
+      }
 #pragma unroll
-        for (int r = 0; r < kRows; ++r) w[r] = *reinterpret_cast<const uint32_t*>(from + row_place(g + 8 * r, i * 16 + q * 4));
-        // (a column behind the last token repeats it and goes nowhere)
-        const uint4 v = *reinterpret_cast<const uint4*>(from + kWeightBytes + token_place(min(g, p.M - 1), i * 64 + q * 16));
-        const uint32_t x0 = __byte_perm(v.x, v.z, 0x5410), x1 = __byte_perm(v.x, v.z, 0x7632);
-        const uint32_t x2 = __byte_perm(v.y, v.w, 0x5410), x3 = __byte_perm(v.y, v.w, 0x7632);
-        constexpr uint32_t one = Code<T>::kOnes;
-        mma16<T>(sum, one, one, one, one, x0, x1);
-        mma16<T>(sum, one, one, one, one, x2, x3);
+      for (int i = 0; i < 4; ++i) {
+        if (c0 + i * kWarps * 32 >= all) break;  // (16 threads together)
+        const int t = at[i] >> 28, unit = (at[i] & 0xfffffff) >> 4, in = at[i] & 15;
+        const int word = in / (4 * kWords) * kWords + in % kWords, four = in / kWords & 3;
+        tokens[((unit * 4 + word) * p.M + t) * 4 + four] =
+            make_uint4(__byte_perm(v[i].x, v[i].z, 0x5410), __byte_perm(v[i].x, v[i].z, 0x7632), __byte_perm(v[i].y, v[i].w, 0x5410),
+                       __byte_perm(v[i].y, v[i].w, 0x7632));
+        const float2 f0 = unpack2<T>(v[i].x), f1 = unpack2<T>(v[i].y), f2 = unpack2<T>(v[i].z), f3 = unpack2<T>(v[i].w);
+        float sum = ((f0.x + f0.y) + (f1.x + f1.y)) + ((f2.x + f2.y) + (f3.x + f3.y));
 #pragma unroll
-        for (int m = 0; m < kMt; ++m) {
-          const uint32_t lo = w[2 * m], hi = w[2 * m + 1];
-          mma16<T>(d[m], two_of<T, 0>(lo), two_of<T, 0>(hi), two_of<T, 1>(lo), two_of<T, 1>(hi), x0, x1);
-          mma16<T>(d[m], two_of<T, 2>(lo), two_of<T, 2>(hi), two_of<T, 3>(lo), two_of<T, 3>(hi), x2, x3);
-        }
-        if ((i + 1) % (4 / kGroups) == 0) {  // a group's sums are complete: scaled and added up
+        for (int o = 1; o < 16 / kGroups; o <<= 1) sum += __shfl_xor_sync(half, sum, o);
+        if (in % (16 / kGroups) == 0) totals[(unit * kGroups + in / (16 / kGroups)) * p.M + t] = sum;
+      }
+    }
+  }
+  __syncthreads();
+
+  float acc[kMt][4] = {};
+  const int token = min(g, p.M - 1), t0 = min(2 * q, p.M - 1), t1 = min(2 * q + 1, p.M - 1);  // (columns behind the last go nowhere)
+  int tile = blockIdx.x, batch = 0;
+  auto use = [&](Batch& a) {
 #pragma unroll
-          for (int r = 0; r < kRows; ++r) {
-            const int j = i * kGroups / 4 * kRows + r, lane_of = (lane & 28) | (j & 3);
-            const float by = scale_of(__shfl_sync(0xffffffffu, s[j / 4], lane_of), p.scale_dtype);
-            const float zp = p.zero ? 16.0f + float(__shfl_sync(0xffffffffu, z[j / 4], lane_of) & 15u) : 24.0f;
+    for (int u = 0; u < kUnits; ++u) {
+      const int unit = u0 + batch * kUnits + u;
+      if (unit < u1) {
+        const ScaleValues<kGroups, kRows> values(p, a.scales[u]);
+        float d[kMt][4] = {};
 #pragma unroll
-            for (int c = 0; c < 2; ++c) {
-              float& f = d[r >> 1][(r & 1) * 2 + c];
-              acc[r >> 1][(r & 1) * 2 + c] += by * (f - zp * sum[c]);
-              f = 0.0f;
+        for (int j = 0; j < 4; ++j) {
+          const uint4 x = tokens[((unit * 4 + j) * p.M + token) * 4 + q];
+#pragma unroll
+          for (int m = 0; m < kMt; ++m) {
+            const uint32_t lo = a.w[u][j / kWords][2 * m].w[j % kWords], hi = a.w[u][j / kWords][2 * m + 1].w[j % kWords];
+            mma16<T>(d[m], two_of<T, 0>(lo), two_of<T, 0>(hi), two_of<T, 1>(lo), two_of<T, 1>(hi), x.x, x.y);
+            mma16<T>(d[m], two_of<T, 2>(lo), two_of<T, 2>(hi), two_of<T, 3>(lo), two_of<T, 3>(hi), x.z, x.w);
+          }
+          if ((j + 1) % (4 / kGroups) == 0) {  // a group's sums are complete: scaled and added up
+            const int group = j * kGroups / 4;
+            const float s0 = totals[(unit * kGroups + group) * p.M + t0], s1 = totals[(unit * kGroups + group) * p.M + t1];
+#pragma unroll
+            for (int r = 0; r < kRows; ++r) {
+              const float by = values.scale(group, r, lane), zp = 16.0f + values.zero_point(p, group, r, lane);
+              float& f0 = d[r >> 1][(r & 1) * 2];
+              float& f1 = d[r >> 1][(r & 1) * 2 + 1];
+              acc[r >> 1][(r & 1) * 2] += by * (f0 - zp * s0);
+              acc[r >> 1][(r & 1) * 2 + 1] += by * (f1 - zp * s1);
+              f0 = f1 = 0.0f;
             }
           }
-#pragma unroll
-          for (int c = 0; c < 4; ++c) sum[c] = 0.0f;
         }
       }
     }
-    __syncwarp();  // the stage may be filled again
-    if (++step < p.per) return;
-    step = 0;
+    if (++batch < batches) return;
+    batch = 0;
     __syncthreads();  // the tile before has been read
 #pragma unroll
     for (int m = 0; m < kMt; ++m)
@@ -236,31 +316,30 @@ __global__ void __launch_bounds__(kWarps * 32, 2) cconv_int4_kernel(const Int4Pa
       }
     __syncthreads();
     const int64_t n0 = int64_t(tile) * (16 * kMt);
-    for (int i = threadIdx.x; i < 16 * kMt * p.M; i += kWarps * 32) {
+    if (int(threadIdx.x) < 16 * kMt * p.M) {
       // (neighbouring threads: neighbouring rows)
-      const int r = i % (16 * kMt), t = i / (16 * kMt), rr = r & 15;
-      if (n0 + r < p.N) {
-        const float(*part)[128] = sums + (r >> 4) * kWarps;
-        const int at = ((rr >> 3) * 2 + (t & 1)) * 32 + (rr & 7) * 4 + (t >> 1);
-        float f = 0.0f;
+      const int r = threadIdx.x % (16 * kMt), t = threadIdx.x / (16 * kMt), rr = r & 15;
+      const float(*part)[128] = sums + (r >> 4) * kWarps;
+      const int at = ((rr >> 3) * 2 + (t & 1)) * 32 + (rr & 7) * 4 + (t >> 1);
+      float f = 0.0f;
 #pragma unroll
-        for (int w = 0; w < kWarps; ++w) f += part[w][at];
-        static_cast<T*>(const_cast<void*>(p.out.p))[t * p.out.rs + (n0 + r) * p.out.cs] = from_f32<T>(f);
-      }
+      for (int w = 0; w < kWarps; ++w) f += part[w][at];
+      if (n0 + r < p.N) static_cast<T*>(const_cast<void*>(p.out.p))[t * p.out.rs + (n0 + r) * p.out.cs] = from_f32<T>(f);
     }
     tile += gridDim.x;
   };
-  const int total = mine * p.per;
-  for (int it = 0; it < total; it += kStages) {
-#pragma unroll
-    for (int i = 0; i < kStages; ++i) {
-      if (it + i < total) {
-        use(i, scale[i], zero[i]);
-        load(i, scale[i], zero[i]);
-      }
+  const int total = mine * batches;
+  for (int it = 0; it < total; it += 2) {
+    load(b[1]);
+    use(b[0]);
+    if (it + 1 < total) {
+      load(b[0]);
+      use(b[1]);
     }
   }
 }
+
+constexpr int kStages = 3;
 
 // q - z as pairs of 16-bit numbers, of neighbouring nibbles: bytes that hold a nibble each become the lower bytes of
 // 128 + q (bf16) or 1024 + q (fp16), from which 128 + z or 1024 + z (`bias`) is taken off, exactly.
@@ -294,87 +373,82 @@ __device__ __forceinline__ void pairs_of(uint32_t v, uint32_t bias, uint32_t (&w
   w[3] = minus2<T>(__byte_perm(hi, High<T>::kByte, 0x4342), bias);
 }
 
-// 9 to 64 tokens: their words, not the weights, would fill the shared memory's bandwidth if each warp fetched its own.  So
+// 5 to 64 tokens: their words, not the weights, would fill the shared memory's bandwidth if each warp fetched its own.  So
 // the warps of a block share the tokens of a unit and take 16 rows each; a cluster of `parts` blocks shares k, and
 // adds up its sums through distributed shared memory in a fixed order.
+template <int kNt>
+constexpr int kSharedUnit = 16 * kWarps * kRowPitch + 8 * kNt * 256;
 template <typename T, int kGroups, int kNt>
 __global__ void __launch_bounds__(kWarps * 32, 2) cconv_int4_tokens_kernel(const Int4Params p, const int parts) {
-  constexpr int kScales = (2 * kGroups + 3) / 4, kRowsBytes = 16 * 64, kWeightBytes = kWarps * kRowsBytes;
-  constexpr int kUnitBytes = kWeightBytes + 8 * kNt * 256;
+  constexpr int kUnitBytes = kSharedUnit<kNt>, kWeightBytes = 16 * kWarps * kRowPitch;
   extern __shared__ __align__(128) uint8_t smem[];
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, g = lane >> 2, q = lane & 3;
   const int rank = int(blockIdx.x) % parts;
-  const int64_t n0 = int64_t(blockIdx.x) / parts * (16 * kWarps), row0 = n0 + warp * 16, last = p.N - 1;
+  const int64_t n0 = int64_t(blockIdx.x) / parts * (16 * kWarps), row0 = n0 + warp * 16;
   const int u0 = int(int64_t(p.units) * rank / parts), u1 = int(int64_t(p.units) * (rank + 1) / parts);
-  const char *rows[2], *scales[kScales];
-  const uint8_t* zeros[kScales];
-  const int scale_bytes = p.scale_dtype == CCONV_TYPE_FP32 ? 4 : 2;
-  auto row_of = [&](int r) { return p.w + min(row0 + r, last) * p.w_rs; };
-#pragma unroll
-  for (int i = 0; i < 2; ++i) rows[i] = row_of(i * 8 + (lane >> 2));
-  // scale number j of a unit: group j / 2, row j % 2; lane q has those with j % 4 = q
-#pragma unroll
-  for (int i = 0; i < kScales; ++i) {
-    const int64_t r = min(row0 + g + 8 * (q % 2), last);
-    scales[i] = p.scale + r * p.s_rs * scale_bytes;
-    zeros[i] = p.zero + r * p.z_rs;
-  }
-  uint32_t scale[kStages][kScales], zero[kStages][kScales];
-  auto load = [&](int stage, int unit, uint32_t (&s)[kScales], uint32_t (&z)[kScales]) {
+  const int token = int(threadIdx.x >> 4);
+  const char* const token_from = p.x + token * p.x_rs;
+  const uint32_t token_at = smem_u32(smem) + kWeightBytes + token_place(token, (lane & 15) * 16);
+  RowCopies<2> rows;
+  rows.aim(p, row0, lane);
+  ScaleRows<kGroups, 2> scale_rows;
+  scale_rows.aim(p, row0, lane);
+  Scales<kGroups, 2> scales;
+  auto load = [&](int stage, int unit) {
     if (unit < u1) {
-      const uint32_t to = smem_u32(smem) + stage * kUnitBytes;
-      copy_rows(to + warp * kRowsBytes, lane, p, rows, unit, row_of);
-      const int64_t k0 = int64_t(unit) * 128 + (lane & 15) * 8;
-      const bool there = k0 < p.x_k;
+      rows.copy(p, smem_u32(smem) + stage * kUnitBytes + warp * (16 * kRowPitch), lane, unit);
+      const uint32_t at = uint32_t(unit) * 256 + (lane & 15) * 16;
+      const bool there = at < p.x_bytes;
 #pragma unroll
-      for (int i = 0; i < kNt / 2 + (kNt == 1); ++i) {
-        const int t = i * 16 + int(threadIdx.x >> 4);
-        if (t < p.M) copy_piece<16>(to + kWeightBytes + token_place(t, (lane & 15) * 16), p.x + t * p.x_rs + (there ? k0 * 2 : 0), there);
-      }
-#pragma unroll
-      for (int i = 0; i < kScales; ++i) {
-        const int64_t grp = min(unit * kGroups + (4 * i + q) / 2, p.groups - 1);
-        s[i] = load_scale(scales[i], p.scale_dtype, grp * p.s_cs);
-        if (p.zero) z[i] = __ldg(zeros[i] + grp * p.z_cs);
-      }
+      for (int i = 0; i < kNt / 2; ++i)
+        if (i * 16 + token < p.M) copy_piece<16>(token_at + stage * kUnitBytes + i * 4096, token_from + i * 16 * p.x_rs + (there ? at : 0), there);
     }
     commit_copies();
   };
 
   start_in_order();
+  for (int i = 0; i < kStages - 1; ++i) load(i, u0 + i);
+  if (u0 < u1) scale_rows.load(p, lane, u0, scales);
+  uint32_t word[2];
 #pragma unroll
-  for (int i = 0; i < kStages - 1; ++i) load(i, u0 + i, scale[i], zero[i]);
+  for (int r = 0; r < 2; ++r)
+    word[r] = row_place(warp * 16 + g + 8 * r,
+                        int((reinterpret_cast<uintptr_t>(p.w) + uint64_t(min(row0 + g + 8 * r, p.N - 1) * p.w_rs)) & 15) + q * 4);
+  const uint32_t x_word[2] = {kWeightBytes + token_place(g, q * 16), kWeightBytes + token_place(g, 64 + q * 16)};
   float acc[kNt][4] = {};
-  auto use = [&](int stage, const uint32_t (&s)[kScales], const uint32_t (&z)[kScales]) {
+  int stage = 0;
+  for (int unit = u0; unit < u1; ++unit) {
+    const ScaleValues<kGroups, 2> values(p, scales);
+    if (unit + 1 < u1) scale_rows.load(p, lane, unit + 1, scales);
+    wait_for_copies<kStages - 2>();
+    __syncthreads();  // the unit is there for all, and the one before has been read by all
+    load(stage == 0 ? kStages - 1 : stage - 1, unit + kStages - 1);
     const uint8_t* const from = smem + stage * kUnitBytes;
+    if (++stage == kStages) stage = 0;
     float d[kNt][4] = {};
     uint32_t bias[2];
 #pragma unroll
     for (int i = 0; i < 4; ++i) {
       if (i % (4 / kGroups) == 0) {
 #pragma unroll
-        for (int r = 0; r < 2; ++r) {
-          const int j = i * kGroups / 4 * 2 + r;
-          const uint32_t zp = p.zero ? __shfl_sync(0xffffffffu, z[j / 4], (lane & 28) | (j & 3)) & 15u : 8u;
-          bias[r] = High<T>::kBase | zp * 0x10001u;
-        }
+        for (int r = 0; r < 2; ++r)
+          bias[r] = High<T>::kBase | uint32_t(int(values.zero_point(p, i * kGroups / 4, r, lane))) * 0x10001u;
       }
       uint32_t lo[4], hi[4];
-      pairs_of<T>(*reinterpret_cast<const uint32_t*>(from + warp * kRowsBytes + row_place(g, i * 16 + q * 4)), bias[0], lo);
-      pairs_of<T>(*reinterpret_cast<const uint32_t*>(from + warp * kRowsBytes + row_place(g + 8, i * 16 + q * 4)), bias[1], hi);
+      pairs_of<T>(*reinterpret_cast<const uint32_t*>(from + word[0] + i * 16), bias[0], lo);
+      pairs_of<T>(*reinterpret_cast<const uint32_t*>(from + word[1] + i * 16), bias[1], hi);
 #pragma unroll
       for (int e = 0; e < kNt; ++e) {
         if (8 * e >= p.M) break;
         // (columns behind the last token: whatever lies there, for sums that go nowhere)
-        const uint4 v = *reinterpret_cast<const uint4*>(from + kWeightBytes + token_place(8 * e + g, i * 64 + q * 16));
+        const uint4 v = *reinterpret_cast<const uint4*>(from + x_word[i & 1] + (i >> 1) * 128 + e * 2048);
         mma16<T>(d[e], lo[0], hi[0], lo[1], hi[1], v.x, v.y);
         mma16<T>(d[e], lo[2], hi[2], lo[3], hi[3], v.z, v.w);
       }
       if ((i + 1) % (4 / kGroups) == 0) {
 #pragma unroll
         for (int r = 0; r < 2; ++r) {
-          const int j = i * kGroups / 4 * 2 + r;
-          const float by = scale_of(__shfl_sync(0xffffffffu, s[j / 4], (lane & 28) | (j & 3)), p.scale_dtype);
+          const float by = values.scale(i * kGroups / 4, r, lane);
 #pragma unroll
           for (int e = 0; e < kNt; ++e)
 #pragma unroll
@@ -384,17 +458,6 @@ __global__ void __launch_bounds__(kWarps * 32, 2) cconv_int4_tokens_kernel(const
             }
         }
       }
-    }
-  };
-  for (int u = u0; u < u1; u += kStages) {
-#pragma unroll
-    for (int i = 0; i < kStages; ++i) {
-      if (u + i >= u1) break;
-      wait_for_copies<kStages - 2>();
-      __syncthreads();  // the unit is there for all, and the one before has been read by all
-      constexpr int kBehind = kStages - 1;
-      load((i + kBehind) % kStages, u + i + kBehind, scale[(i + kBehind) % kStages], zero[(i + kBehind) % kStages]);
-      use(i, scale[i], zero[i]);
     }
   }
   __syncthreads();
@@ -461,19 +524,21 @@ __global__ void __launch_bounds__(256) cconv_int4_expand_kernel(const ExpandPara
   }
 }
 
-template <typename T, int kGroups, int kMt>
+constexpr int kMostTokenBytes = 96 * 1024;  // of shared memory, so that two blocks share an SM
+
+template <typename T, int kWords, int kGroups, int kMt>
 cudaError_t launch_rows(const Int4Params& p, int sms, cudaStream_t s) {
-  auto f = cconv_int4_kernel<T, kGroups, kMt>;
+  auto f = cconv_int4_kernel<T, kWords, kGroups, kMt>;
   static bool ready[64] = {};
-  const cudaError_t e = allow_smem(f, ready, kMt * kWarps * 512 + kWarps * kStages * (16 * kMt * 64 + 8 * 256));
+  const cudaError_t e = allow_smem(f, ready, kMostTokenBytes);
   if (e != cudaSuccess) return e;
   const dim3 grid(unsigned(std::min<int64_t>(cdiv64(p.N, 16 * kMt), 2 * sms)));
-  return launch(f, grid, kWarps * 32, size_t(kMt * kWarps * 512 + kWarps * kStages * (16 * kMt * 64 + p.M * 256)), 1, s, p);
+  return launch(f, grid, kWarps * 32, size_t(p.units) * p.M * (256 + kGroups * 4), 1, s, p);
 }
 template <typename T, int kGroups, int kNt>
 cudaError_t launch_shared(const Int4Params& p, int sms, cudaStream_t s) {
   auto f = cconv_int4_tokens_kernel<T, kGroups, kNt>;
-  constexpr int kSmem = std::max(kStages * (kWarps * 16 * 64 + 8 * kNt * 256), 8 * kNt * (16 * kWarps + 4) * 4);
+  constexpr int kSmem = std::max(kStages * kSharedUnit<kNt>, 8 * kNt * (16 * kWarps + 4) * 4);
   static bool ready[64] = {};
   const cudaError_t e = allow_smem(f, ready, kSmem);
   if (e != cudaSuccess) return e;
@@ -482,13 +547,26 @@ cudaError_t launch_shared(const Int4Params& p, int sms, cudaStream_t s) {
   while (parts < 8 && 2 * parts <= p.units && tiles * parts < sms + sms / 2) parts *= 2;
   return launch(f, dim3(unsigned(tiles * parts)), kWarps * 32, kSmem, parts, s, p, parts);
 }
+template <typename T, int kWords, int kGroups>
+cudaError_t launch_words(const Int4Params& p, int sms, cudaStream_t s) {
+  // 32 rows a tile where that leaves no SM idle
+  return cdiv64(p.N, 32) >= sms ? launch_rows<T, kWords, kGroups, 2>(p, sms, s) : launch_rows<T, kWords, kGroups, 1>(p, sms, s);
+}
 template <typename T, int kGroups>
 cudaError_t launch_tokens(const Int4Params& p, int sms, cudaStream_t s) {
   if (p.M > 32) return launch_shared<T, kGroups, 8>(p, sms, s);
   if (p.M > 16) return launch_shared<T, kGroups, 4>(p, sms, s);
-  if (p.M > 8) return launch_shared<T, kGroups, 2>(p, sms, s);
-  // 32 rows a tile where that leaves no SM idle
-  return cdiv64(p.N, 32) >= sms ? launch_rows<T, kGroups, 2>(p, sms, s) : launch_rows<T, kGroups, 1>(p, sms, s);
+  // What a block makes of 5 to 8 tokens takes longer than its tile's weights, but for small matrices, whose time is that of a
+  // launch: 8 tokens 4096 x 4096 10.0 against 7.5 us, 2048 x 2048 4.8 against 5.9; 4 tokens 8192 x 4096 11.5 against 12.
+  const bool own = p.M <= 4 || (p.M <= 8 && p.units * p.M <= 128);
+  if (!own || int64_t(p.units) * p.M * (256 + kGroups * 4) > kMostTokenBytes) return launch_shared<T, kGroups, 2>(p, sms, s);
+  constexpr int kWords = 4 / kGroups;  // that four lanes may have of a group
+  const int most = (p.lies & 15) == 0 ? 4 : (p.lies & 7) == 0 ? 2 : 1;
+  if constexpr (kWords == 4)
+    if (most == 4) return launch_words<T, 4, kGroups>(p, sms, s);
+  if constexpr (kWords >= 2)
+    if (most >= 2) return launch_words<T, 2, kGroups>(p, sms, s);
+  return launch_words<T, 1, kGroups>(p, sms, s);
 }
 template <typename T>
 cudaError_t launch_few(const Int4Params& p, int group, int sms, cudaStream_t s) {
@@ -512,15 +590,14 @@ void plan(Steps& st, const cconv_int4_product_args& a) {
     at = 0;
     st.copy(Mat(a.q), w, N, row, 1);
   }
-  const uintptr_t lies = at | uintptr_t(w_bytes);
   if (M <= kFewTokensInt4) {
     Int4Params p{};
     Mat x(a.x);
-    p.x_k = K;
+    p.x_bytes = uint32_t(K) * 2;
     if (!few_readable(x, M, K, 2)) {
       // (zeros behind a row's end, for k beyond K of its last word)
       const Mat to = st.scratch(M, K, 2);
-      p.x_k = to.rs;
+      p.x_bytes = uint32_t(to.rs) * 2;
       if (K % 8) {
         const int64_t bytes = M * to.rs * 2;
         st.add([=](cudaStream_t s) {
@@ -536,7 +613,10 @@ void plan(Steps& st, const cconv_int4_product_args& a) {
     p.x_rs = x.rs * 2;
     p.w = static_cast<const char*>(w.p);
     p.w_rs = w.rs;
-    p.w_bytes = w_bytes;
+    p.w_end = p.w + (N - 1) * w.rs + w_bytes;
+    p.shifted = (at & 15) != 0;
+    p.w_bytes = uint32_t(w_bytes);
+    p.lies = uint32_t((at | uintptr_t(w_bytes)) & 15);
     p.scale = static_cast<const char*>(a.scale.data);
     p.s_rs = a.scale.row_stride; p.s_cs = a.scale.col_stride;
     p.zero = static_cast<const uint8_t*>(a.zero.data);
@@ -544,7 +624,6 @@ void plan(Steps& st, const cconv_int4_product_args& a) {
     p.N = N;
     p.M = int(M);
     p.scale_dtype = a.scale_dtype;
-    p.piece = (lies & 15) == 0 ? 16 : (lies & 7) == 0 ? 8 : 4;
     p.groups = int(cdiv64(K, group));
     p.units = int(cdiv64(K, 128));
     p.per = int(cdiv64(p.units, kWarps));
