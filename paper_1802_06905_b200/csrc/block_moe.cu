@@ -50,18 +50,18 @@ struct MoeParams {
   Mat out;
 };
 
+__device__ __forceinline__ uint4 load_16(const char* p) { return *reinterpret_cast<const uint4*>(p); }
+
 // ---- router --------------------------------------------------------------------------------------
-// Order of scores: larger first, then the lower index; NaN last.
-__device__ __forceinline__ uint64_t rank_of(float v, int e) {
+// A score as a number of the same order, NaN below all others; 0 is none.
+__device__ __forceinline__ uint32_t key_of(float v) {
   const uint32_t b = __float_as_uint(v);
-  const uint32_t up = v != v ? 0u : (b & 0x80000000u) ? ~b : b | 0x80000000u;
-  return uint64_t(up) << 32 | uint32_t(~e);
+  return v != v ? 1u : (b & 0x80000000u) ? ~b : b | 0x80000000u;
 }
-__device__ __forceinline__ uint64_t warp_max(uint64_t v) {
-  const uint32_t hi = __reduce_max_sync(0xffffffffu, uint32_t(v >> 32));
-  const uint32_t lo = __reduce_max_sync(0xffffffffu, uint32_t(v >> 32) == hi ? uint32_t(v) : 0u);
-  return uint64_t(hi) << 32 | lo;
+__device__ __forceinline__ float score_of(uint32_t key) {  // (key 1: a NaN too)
+  return __uint_as_float((key & 0x80000000u) ? key ^ 0x80000000u : ~key);
 }
+
 // Channels are dealt to the blocks of the cluster, and a block's share of them and 16 experts at a time to its warps:
 // with the usual sizes a warp's loads are all on their way at once.  Partial scores [slice][token][expert] lie in
 // shared memory, a block adds its own up, and the warp that chooses for a token adds up the blocks'.
@@ -81,20 +81,30 @@ __global__ void __launch_bounds__(kRouterWarps * 32) cconv_moe_router_kernel(con
       const char* r0 = p.router + int64_t(min(16 * m + g, p.E - 1)) * p.router_rs;
       const char* r1 = p.router + int64_t(min(16 * m + g + 8, p.E - 1)) * p.router_rs;
       float acc[kNt][4] = {};
-#pragma unroll 4
-      for (int u = u0; u < u1; ++u) {
-        const int64_t k0 = int64_t(u) * 32 + q * 8;
-        const bool in = k0 < p.x_k;
-        const uint4 none = make_uint4(0, 0, 0, 0);
-        const uint4 a0 = in ? *reinterpret_cast<const uint4*>(r0 + k0 * 2) : none;
-        const uint4 a1 = in ? *reinterpret_cast<const uint4*>(r1 + k0 * 2) : none;
+      // kBatch units at once: with the usual sizes they are all that the warp has, and wait for memory together
+      constexpr int kBatch = kNt == 1 ? 4 : kNt <= 4 ? 2 : 1;
+      const uint4 none = make_uint4(0, 0, 0, 0);
+      for (int first = u0; first < u1; first += kBatch) {
+        uint4 a0[kBatch], a1[kBatch], v[kBatch][kNt];
 #pragma unroll
-        for (int e = 0; e < kNt; ++e) {
-          const int t = 8 * e + g;
-          const uint4 v = in && t < tokens ? *reinterpret_cast<const uint4*>(p.x + int64_t(t0 + t) * p.x_rs + k0 * 2) : none;
-          mma16<T>(acc[e], a0.x, a1.x, a0.y, a1.y, v.x, v.y);
-          mma16<T>(acc[e], a0.z, a1.z, a0.w, a1.w, v.z, v.w);
+        for (int u = 0; u < kBatch; ++u) {
+          const int64_t k0 = int64_t(first + u) * 32 + q * 8;
+          const bool in = first + u < u1 && k0 < p.x_k;
+          a0[u] = in ? load_16(r0 + k0 * 2) : none;
+          a1[u] = in ? load_16(r1 + k0 * 2) : none;
+#pragma unroll
+          for (int e = 0; e < kNt; ++e) {
+            const int t = 8 * e + g;
+            v[u][e] = in && t < tokens ? load_16(p.x + int64_t(t0 + t) * p.x_rs + k0 * 2) : none;
+          }
         }
+#pragma unroll
+        for (int u = 0; u < kBatch; ++u)
+#pragma unroll
+          for (int e = 0; e < kNt; ++e) {
+            mma16<T>(acc[e], a0[u].x, a1[u].x, a0[u].y, a1[u].y, v[u][e].x, v[u][e].y);
+            mma16<T>(acc[e], a0[u].z, a1[u].z, a0[u].w, a1[u].w, v[u][e].z, v[u][e].w);
+          }
       }
 #pragma unroll
       for (int e = 0; e < kNt; ++e)
@@ -116,8 +126,8 @@ __global__ void __launch_bounds__(kRouterWarps * 32) cconv_moe_router_kernel(con
   cluster_sync_all();
   for (int t = rank + kRouterBlocks * warp; t < tokens; t += kRouterBlocks * kRouterWarps) {
     // the token's scores, whole: the first of each lane's in registers, the others back in this block's memory
-    float* const row = part + t * p.E;
-    float score[4];
+    uint32_t* const row = reinterpret_cast<uint32_t*>(part + t * p.E);
+    uint32_t key[4] = {}, top = 0;
     const uint32_t at = smem_u32(row);
     for (int e = lane, i = 0; e < p.E; e += 32, ++i) {
       float v[kRouterBlocks], sum = 0.0f;
@@ -125,50 +135,40 @@ __global__ void __launch_bounds__(kRouterWarps * 32) cconv_moe_router_kernel(con
       for (int r = 0; r < kRouterBlocks; ++r) v[r] = load_cluster(cluster_map_shared(at + e * 4, r));
 #pragma unroll
       for (int r = 0; r < kRouterBlocks; ++r) sum += v[r];
-      if (i < 4) {
+      const uint32_t k = key_of(sum);
+      top = max(top, k);
 #pragma unroll
-        for (int j = 0; j < 4; ++j) score[j] = i == j ? sum : score[j];
-      } else {
-        row[e] = sum;  // (no other block reads this token's scores)
-      }
+      for (int j = 0; j < 4; ++j) key[j] = i == j ? k : key[j];
+      if (i >= 4) row[e] = k;  // (no other block reads this token's scores)
     }
-    uint64_t key[4];
+    const float largest = score_of(__reduce_max_sync(0xffffffffu, top));
+    float sum = 0.0f;
+    if (!p.normalize) {
 #pragma unroll
-    for (int j = 0; j < 4; ++j) key[j] = 32 * j + lane < p.E ? rank_of(score[j], 32 * j + lane) : 0;
-    uint64_t before = ~uint64_t(0);
-    float mine = 0.0f, largest = 0.0f;  // lane j: the j-th choice's score
+      for (int i = 0; i < 4; ++i)
+        if (key[i]) sum += expf(score_of(key[i]) - largest);
+      for (int e = lane + 128; e < p.E; e += 32) sum += expf(score_of(row[e]) - largest);
+    }
+    // The largest k times; of equal ones the lowest number, which leaves the others behind.
+    float mine = 0.0f;  // lane j: the j-th choice's score
     int id = 0;
     for (int j = 0; j < p.k; ++j) {
-      uint64_t best = 0;
+      uint32_t best = max(max(key[0], key[1]), max(key[2], key[3]));
+      for (int e = lane + 128; e < p.E; e += 32) best = max(best, row[e]);
+      best = __reduce_max_sync(0xffffffffu, best);
+      uint32_t first = ~0u;
+      for (int e = lane + 128; e < p.E && first == ~0u; e += 32) first = row[e] == best ? e : ~0u;
 #pragma unroll
-      for (int i = 0; i < 4; ++i)
-        if (key[i] < before && key[i] > best) best = key[i];
-      for (int e = lane + 128; e < p.E; e += 32) {
-        const uint64_t r = rank_of(row[e], e);
-        if (r < before && r > best) best = r;
+      for (int i = 3; i >= 0; --i) first = key[i] == best ? 32 * i + lane : first;
+      const uint32_t e = __reduce_min_sync(0xffffffffu, first);
+      if (first == e) {  // this lane's: gone
+#pragma unroll
+        for (int i = 0; i < 4; ++i) key[i] = int(e) == 32 * i + lane ? 0 : key[i];
+        if (e >= 128) row[e] = 0;
       }
-      before = warp_max(best);
-      const int e = int(~uint32_t(before)), place = e >> 5;
-      float v = 0.0f;
-      if (place >= 4) {
-        v = (e & 31) == lane ? row[e] : 0.0f;
-      } else {
-#pragma unroll
-        for (int i = 0; i < 4; ++i) v = place == i ? score[i] : v;
-      }
-      v = __shfl_sync(0xffffffffu, v, e & 31);
-      if (j == 0) largest = v;
-      if (lane == j) mine = v, id = e;
+      if (lane == j) mine = score_of(best), id = int(e);
     }
-    float sum = 0.0f;
-    if (p.normalize) {
-      sum = lane < p.k ? expf(mine - largest) : 0.0f;
-    } else {
-#pragma unroll
-      for (int i = 0; i < 4; ++i)
-        if (32 * i + lane < p.E) sum += expf(score[i] - largest);
-      for (int e = lane + 128; e < p.E; e += 32) sum += expf(row[e] - largest);
-    }
+    if (p.normalize) sum = lane < p.k ? expf(mine - largest) : 0.0f;
     sum = warp_sum(sum);
     if (lane < p.k) {
       p.ids[int64_t(t0 + t) * p.ids_rs + lane * p.ids_cs] = id;
@@ -209,9 +209,39 @@ __device__ __forceinline__ Routes routes_of(const MoeParams& p, uint8_t* smem, i
   r.first = r.expert + most_groups(E, pairs, most);
   r.count = reinterpret_cast<uint8_t*>(r.first + most_groups(E, pairs, most));
   r.token = r.count + most_groups(E, pairs, most);
+  auto id_of = [&](int t, int j) { return __ldg(p.ids + t * p.ids_rs + j * p.ids_cs); };
+  if (p.T == 1) {  // a group a choice, in their order: a microsecond less than the general way
+    if (tid < 32) {
+      const int id = tid < p.k ? id_of(0, tid) : -1;
+      const bool valid = id >= 0 && id < E;
+      const uint32_t same = __match_any_sync(0xffffffffu, valid ? id : -1 - tid);
+      const bool first = valid && __ffs(int(same)) - 1 == tid;
+      const uint32_t all = __ballot_sync(0xffffffffu, first);
+      float w = 0.0f;
+      if (kWeights) {
+        const float own = valid ? __ldg(p.weights + tid * p.weights_cs) : 0.0f;
+        for (int j = 0; j < p.k; ++j) {
+          const float v = __shfl_sync(0xffffffffu, own, j);
+          if (same >> j & 1) w += v;
+        }
+      }
+      if (first) {
+        const int at = __popc(all & ((1u << tid) - 1));
+        r.expert[at] = uint16_t(id);
+        r.first[at] = uint16_t(at);
+        r.count[at] = 1;
+        r.pairs[at] = uint16_t(tid);
+        r.token[at] = 0;
+        if (kWeights) r.weight[at] = w;
+      }
+      if (tid == 0) scratch[0] = __popc(all);
+    }
+    __syncthreads();
+    r.groups = scratch[0];
+    return r;
+  }
   for (int e = tid; e < E; e += nt) r.tokens[e] = 0;
   __syncthreads();
-  auto id_of = [&](int t, int j) { return __ldg(p.ids + t * p.ids_rs + j * p.ids_cs); };
   for (int i = tid; i < pairs; i += nt) {
     const int t = i / p.k, e = id_of(t, i - t * p.k);
     if (e >= 0 && e < E) atomicOr(reinterpret_cast<unsigned long long*>(r.tokens + e), 1ull << t);
@@ -355,7 +385,7 @@ __global__ void __launch_bounds__(kWarps * 32, 2) cconv_moe_gate_up_kernel(const
 
   // (an item's group and tile, kept without divisions)
   const int step_group = int(stride / tiles), step_tile = int(stride % tiles);
-  int lgroup = int(blockIdx.x / tiles), ltile = int(blockIdx.x % tiles), lu = 0, lcount = 0;
+  int lgroup = int(blockIdx.x) / tiles, ltile = int(blockIdx.x) % tiles, lu = 0, lcount = 0;
   const char *rows[4], *columns[2 * kNt];  // of the item: what this lane copies of
   auto row_of = [&](int64_t e, int seg) {
     const int64_t f = min(int64_t(ltile) * 8 + (seg & 7), p.F - 1);
@@ -400,7 +430,7 @@ __global__ void __launch_bounds__(kWarps * 32, 2) cconv_moe_gate_up_kernel(const
   aim();
   for (int i = 0; i < S::kStages; ++i) load(i);
 
-  int group = int(blockIdx.x / tiles), tile = int(blockIdx.x % tiles), step = 0;
+  int group = int(blockIdx.x) / tiles, tile = int(blockIdx.x) % tiles, step = 0;
   float acc[kNt][4] = {};
   auto use = [&](int stage) {
     const int count = r.count[group], unit = u0 + step;
