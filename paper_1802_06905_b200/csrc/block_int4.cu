@@ -37,12 +37,13 @@ struct Code<__half> {
   static constexpr int kAt = 6;
   static constexpr uint32_t kMask = 0x03c003c0u, kBase = 0x4c004c00u;
 };
-// 16 + q of nibbles i and i + 4.
+// 16 + q of nibbles i and i + 4.  `base` is kBase as a number that is not known when compiled: mask and base are then one
+// operation (with two constants they are two).
 template <typename T, int i>
-__device__ __forceinline__ uint32_t two_of(uint32_t v) {
+__device__ __forceinline__ uint32_t two_of(uint32_t v, uint32_t base) {
   constexpr int kShift = Code<T>::kAt - 4 * i;
   const uint32_t at = kShift >= 0 ? v << (kShift & 31) : v >> (-kShift & 31);
-  return (at & Code<T>::kMask) | Code<T>::kBase;
+  return (at & Code<T>::kMask) | base;
 }
 
 struct Int4Params {
@@ -57,6 +58,7 @@ struct Int4Params {
   int M, scale_dtype, groups;
   uint32_t w_bytes;  // of a row
   uint32_t lies;     // bits in which rows' addresses and lengths differ from multiples of 16 bytes (of 4 they are)
+  uint32_t base;     // Code<T>::kBase
   int shifted;       // rows do not all begin at multiples of 16 bytes
   int units, per;    // of 128 of k; of a warp
   Mat out;
@@ -285,8 +287,8 @@ __global__ void __launch_bounds__(kWarps * 32, 2) cconv_int4_kernel(const Int4Pa
 #pragma unroll
           for (int m = 0; m < kMt; ++m) {
             const uint32_t lo = a.w[u][j / kWords][2 * m].w[j % kWords], hi = a.w[u][j / kWords][2 * m + 1].w[j % kWords];
-            mma16<T>(d[m], two_of<T, 0>(lo), two_of<T, 0>(hi), two_of<T, 1>(lo), two_of<T, 1>(hi), x.x, x.y);
-            mma16<T>(d[m], two_of<T, 2>(lo), two_of<T, 2>(hi), two_of<T, 3>(lo), two_of<T, 3>(hi), x.z, x.w);
+            mma16<T>(d[m], two_of<T, 0>(lo, p.base), two_of<T, 0>(hi, p.base), two_of<T, 1>(lo, p.base), two_of<T, 1>(hi, p.base), x.x, x.y);
+            mma16<T>(d[m], two_of<T, 2>(lo, p.base), two_of<T, 2>(hi, p.base), two_of<T, 3>(lo, p.base), two_of<T, 3>(hi, p.base), x.z, x.w);
           }
           if ((j + 1) % (4 / kGroups) == 0) {  // a group's sums are complete: scaled and added up
             const int group = j * kGroups / 4;
@@ -487,39 +489,75 @@ __global__ void __launch_bounds__(kWarps * 32, 2) cconv_int4_tokens_kernel(const
   if (parts > 1) cluster_sync_all();  // no block leaves while others read its sums
 }
 
-// The weights as numbers of the operands' type, for products of many tokens: 8 neighbours of a row a thread.
+// The weights as numbers of the operands' type, for products of many tokens: 8 or 16 neighbours of a row a thread, 4 rows.
+// Bound by the store of 2 bytes a weight, where scales are of that type too (one rounding, of an exact product, a pair).
 struct ExpandParams {
   const char *w, *scale;
   const uint8_t* zero;
   void* to;
   int64_t w_rs, s_rs, s_cs, z_rs, z_cs, to_rs, N, K;
-  int scale_dtype, group;
+  int scale_dtype, group_shift;  // 1 << group_shift words a group
 };
-constexpr int kExpandRows = 8;
 template <typename T>
-__global__ void __launch_bounds__(256) cconv_int4_expand_kernel(const ExpandParams p) {
+__device__ __forceinline__ uint32_t times2(uint32_t a, uint32_t b);
+template <>
+__device__ __forceinline__ uint32_t times2<__nv_bfloat16>(uint32_t a, uint32_t b) {
+  const __nv_bfloat162 v = __hmul2(*reinterpret_cast<const __nv_bfloat162*>(&a), *reinterpret_cast<const __nv_bfloat162*>(&b));
+  return *reinterpret_cast<const uint32_t*>(&v);
+}
+template <>
+__device__ __forceinline__ uint32_t times2<__half>(uint32_t a, uint32_t b) {
+  const __half2 v = __hmul2(*reinterpret_cast<const __half2*>(&a), *reinterpret_cast<const __half2*>(&b));
+  return *reinterpret_cast<const uint32_t*>(&v);
+}
+constexpr int kExpandRows = 4;
+// kWords neighbouring words a thread (2 where that keeps to multiples of 32 bytes, which go in one store); kSame: scales
+// are of the type T.
+template <typename T, int kWords, bool kSame>
+__global__ void __launch_bounds__(256, 4) cconv_int4_expand_kernel(const ExpandParams p) {
   start_in_order();
-  const int64_t words = (p.K + 7) / 8, i = int64_t(blockIdx.x) * 256 + threadIdx.x;
+  const uint32_t words = uint32_t((p.K + 7) / 8), i = (blockIdx.x * 256 + threadIdx.x) * kWords;
   if (i >= words) return;
-  const int64_t grp = i * 8 / p.group, last = p.N - 1;
+  const int64_t grp = i >> p.group_shift;
+  const int es = kSame || p.scale_dtype != CCONV_TYPE_FP32 ? 2 : 4;
+  const int64_t scale_step = p.s_rs * es, to_step = p.to_rs * int64_t(sizeof(T));
   for (int64_t n0 = int64_t(blockIdx.y) * kExpandRows; n0 < p.N; n0 += int64_t(gridDim.y) * kExpandRows) {
-    uint32_t v[kExpandRows], s[kExpandRows], z[kExpandRows];
+    const int rows = int(min(p.N - n0, int64_t(kExpandRows)));
+    const char* w_at = p.w + n0 * p.w_rs + i * 4;
+    const char* s_at = p.scale + (n0 * p.s_rs + grp * p.s_cs) * es;
+    const uint8_t* z_at = p.zero + n0 * p.z_rs + grp * p.z_cs;
+    char* to = static_cast<char*>(p.to) + n0 * to_step + i * 16;
+    Words<kWords> v[kExpandRows];
+    uint32_t s[kExpandRows], z[kExpandRows];
 #pragma unroll
-    for (int r = 0; r < kExpandRows; ++r) {
-      const int64_t n = min(n0 + r, last);
-      v[r] = __ldg(reinterpret_cast<const uint32_t*>(p.w + n * p.w_rs) + i);
-      s[r] = load_scale(p.scale, p.scale_dtype, n * p.s_rs + grp * p.s_cs);
-      z[r] = p.zero ? __ldg(p.zero + n * p.z_rs + grp * p.z_cs) & 15u : 8u;
+    for (int r = 0; r < kExpandRows; ++r, w_at += p.w_rs, s_at += scale_step, z_at += p.z_rs) {
+      z[r] = 8;
+      if (r >= rows) break;
+      v[r].load(w_at);
+      if (es == 2) s[r] = __ldg(reinterpret_cast<const uint16_t*>(s_at));
+      else s[r] = __ldg(reinterpret_cast<const uint32_t*>(s_at));
+      if (p.zero) z[r] = __ldg(z_at) & 15u;
     }
 #pragma unroll
-    for (int r = 0; r < kExpandRows; ++r) {
-      if (n0 + r > last) break;
-      const float by = scale_of(s[r], p.scale_dtype);
-      float f[8];
+    for (int r = 0; r < kExpandRows; ++r, to += to_step) {
+      if (r >= rows) break;
+      uint32_t w[kWords][4];
 #pragma unroll
-      for (int j = 0; j < 8; ++j) f[j] = by * float(int(v[r] >> (4 * j) & 15u) - int(z[r]));
-      T* to = static_cast<T*>(p.to) + (n0 + r) * p.to_rs + i * 8;
-      *reinterpret_cast<uint4*>(to) = make_uint4(pack2<T>(f[0], f[1]), pack2<T>(f[2], f[3]), pack2<T>(f[4], f[5]), pack2<T>(f[6], f[7]));
+      for (int k = 0; k < kWords; ++k) {
+        pairs_of<T>(v[r].w[k], High<T>::kBase | z[r] * 0x10001u, w[k]);
+#pragma unroll
+        for (int j = 0; j < 4; ++j) {
+          if constexpr (kSame) {
+            w[k][j] = times2<T>(w[k][j], s[r] * 0x10001u);
+          } else {
+            const float by = scale_of(s[r], p.scale_dtype);
+            const float2 f = unpack2<T>(w[k][j]);
+            w[k][j] = pack2<T>(by * f.x, by * f.y);
+          }
+        }
+      }
+      if constexpr (kWords == 2) st_global_v8(to, w[0][0], w[0][1], w[0][2], w[0][3], w[1][0], w[1][1], w[1][2], w[1][3]);
+      else *reinterpret_cast<uint4*>(to) = make_uint4(w[0][0], w[0][1], w[0][2], w[0][3]);
     }
   }
 }
@@ -628,6 +666,7 @@ void plan(Steps& st, const cconv_int4_product_args& a) {
     p.units = int(cdiv64(K, 128));
     p.per = int(cdiv64(p.units, kWarps));
     p.out = Mat(a.c);
+    p.base = dtype == CCONV_TYPE_BF16 ? Code<__nv_bfloat16>::kBase : Code<__half>::kBase;
     st.add([=](cudaStream_t s) {
       return block_cuda_error(dtype == CCONV_TYPE_BF16 ? launch_few<__nv_bfloat16>(p, group, sms, s)
                                                        : launch_few<__half>(p, group, sms, s),
@@ -648,12 +687,17 @@ void plan(Steps& st, const cconv_int4_product_args& a) {
   p.N = N;
   p.K = K;
   p.scale_dtype = a.scale_dtype;
-  p.group = group;
+  p.group_shift = group == 32 ? 2 : group == 64 ? 3 : 4;
+  const bool two = K % 16 == 0 && (at & 7) == 0;
   st.add([=](cudaStream_t s) {
-    const dim3 grid(unsigned(cdiv64(cdiv64(K, 8), 256)), unsigned(std::min<int64_t>(cdiv64(N, kExpandRows), 65535)));
-    return block_cuda_error(dtype == CCONV_TYPE_BF16 ? launch(cconv_int4_expand_kernel<__nv_bfloat16>, grid, 256, 0, 1, s, p)
-                                                     : launch(cconv_int4_expand_kernel<__half>, grid, 256, 0, 1, s, p),
-                            "cconv_int4_expand_kernel");
+    const dim3 grid(unsigned(cdiv64(K, two ? 4096 : 2048)), unsigned(std::min<int64_t>(cdiv64(N, kExpandRows), 65535)));
+    auto go = [&](auto f) { return block_cuda_error(launch(f, grid, 256, 0, 1, s, p), "cconv_int4_expand_kernel"); };
+    auto of = [&](auto type) {
+      using T = decltype(type);
+      if (p.scale_dtype == dtype) return two ? go(cconv_int4_expand_kernel<T, 2, true>) : go(cconv_int4_expand_kernel<T, 1, true>);
+      return two ? go(cconv_int4_expand_kernel<T, 2, false>) : go(cconv_int4_expand_kernel<T, 1, false>);
+    };
+    return dtype == CCONV_TYPE_BF16 ? of(__nv_bfloat16()) : of(__half());
   });
   Launch l;
   l.epilogue = kStore;
