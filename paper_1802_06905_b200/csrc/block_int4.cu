@@ -3,10 +3,14 @@
 //   C[m][n] = sum_g s[n][g] sum_{k in g} (q[n][k] - z[n][g]) x[m][k]
 //           = sum_g s[n][g] (sum_k (16 + q) x - (16 + z) sum_k x)
 //
-// Few tokens: the weights are read once, into warp-wide matrix instructions, a group's sums come out of these and are scaled and added up in fp32.  Up to 8 tokens, 16 + q is the number that is multiplied: its mantissa starts with the four
-// bits, so that a shift and a logical operation make two of them (6 operations for two where q - z is formed).  That costs
-// a factor of 5 in the sums' rounding.  A word holds k = 0 .. 7 in its nibbles; the two that one shift brings in
+// Few tokens: the weights are read once, into warp-wide matrix instructions; a group's sums come out of these, and are
+// scaled and added up in fp32.  For one or two tokens 16 + q is the number that is multiplied: its mantissa starts with the
+// four bits, so that a shift and a logical operation make two of them (6 operations for two where q - z is formed).  That
+// costs a factor of 5 in the sums' rounding.  A word holds k = 0 .. 7 in its nibbles; the two that one shift brings in
 // place are four apart, so x's pairs are taken four apart too.
+//
+// What bounds it is the issue of instructions: 8192 x 4096, one token, 17 MB of weights: 7.7 us (2.6 at the rate of a
+// copy), 420 instructions of a warp for 4096 weights, half of them of pipes that take one every other clock.
 #include "block_int4.h"
 
 #include <algorithm>
@@ -110,20 +114,29 @@ template <int kEach>
 struct RowCopies {
   const char* rows[kEach];  // of this lane's rows, from the multiple of 16 bytes that it begins behind
   const char* tail;         // of row `lane`: a fifth piece
+  bool first, last;         // whether the array's first or last row is among them
   static __device__ __forceinline__ const char* aligned(const char* q) {
     return reinterpret_cast<const char*>(reinterpret_cast<uintptr_t>(q) & ~uintptr_t(15));
   }
   __device__ __forceinline__ void aim(const Int4Params& p, int64_t row0, int lane) {
-    const int64_t last = p.N - 1;
+    const int64_t end = p.N - 1;
 #pragma unroll
-    for (int i = 0; i < kEach; ++i) rows[i] = aligned(p.w + min(row0 + i * 8 + (lane >> 2), last) * p.w_rs) + (lane & 3) * 16;
-    tail = aligned(p.w + min(row0 + lane, last) * p.w_rs) + 64;
+    for (int i = 0; i < kEach; ++i) rows[i] = aligned(p.w + min(row0 + i * 8 + (lane >> 2), end) * p.w_rs) + (lane & 3) * 16;
+    tail = aligned(p.w + min(row0 + lane, end) * p.w_rs) + 64;
+    first = row0 == 0;
+    last = row0 + 8 * kEach > end;
   }
   __device__ __forceinline__ void copy(const Int4Params& p, uint32_t to, int lane, int unit) const {
-    const int64_t at = int64_t(unit) * 64;
+    const uint32_t at = uint32_t(unit) * 64;
+    if ((first && unit == 0) || (last && unit >= p.units - 2)) {  // pieces that may reach out of the array
+#pragma unroll 1
+      for (int i = 0; i < kEach; ++i) copy_inside(to + row_place(i * 8 + (lane >> 2), (lane & 3) * 16), rows[i] + at, p);
+      if (p.shifted && lane < 8 * kEach) copy_inside(to + row_place(lane, 64), tail + at, p);
+      return;
+    }
 #pragma unroll
-    for (int i = 0; i < kEach; ++i) copy_inside(to + row_place(i * 8 + (lane >> 2), (lane & 3) * 16), rows[i] + at, p);
-    if (p.shifted && lane < 8 * kEach) copy_inside(to + row_place(lane, 64), tail + at, p);
+    for (int i = 0; i < kEach; ++i) copy_piece<16>(to + row_place(i * 8 + (lane >> 2), (lane & 3) * 16), rows[i] + at, true);
+    if (p.shifted && lane < 8 * kEach) copy_piece<16>(to + row_place(lane, 64), tail + at, true);
   }
 };
 
@@ -164,25 +177,26 @@ struct ScaleRows {
 template <int kGroups, int kRows>
 struct ScaleValues {
   using Own = Scales<kGroups, kRows>;
-  float by[Own::kOwn], low[Own::kOwn];  // scale; zero point
+  float by[Own::kOwn];       // scale
+  uint32_t low[Own::kOwn];  // zero point
   __device__ __forceinline__ ScaleValues(const Int4Params& p, const Own& s) {
 #pragma unroll
     for (int i = 0; i < Own::kOwn; ++i) {
       by[i] = scale_of(s.raw[i], p.scale_dtype);
-      low[i] = p.zero ? float(s.zero[i] & 15u) : 8.0f;
+      low[i] = s.zero[i] & 15u;
     }
   }
   __device__ __forceinline__ float scale(int group, int r, int lane) const {
     const int j = group * kRows + r;
     return __shfl_sync(0xffffffffu, by[j / 4], (lane & 28) | (j & 3));
   }
-  __device__ __forceinline__ float zero_point(const Int4Params& p, int group, int r, int lane) const {
+  __device__ __forceinline__ uint32_t zero_point(const Int4Params& p, int group, int r, int lane) const {
     const int j = group * kRows + r;
-    return p.zero ? __shfl_sync(0xffffffffu, low[j / 4], (lane & 28) | (j & 3)) : 8.0f;
+    return p.zero ? __shfl_sync(0xffffffffu, low[j / 4], (lane & 28) | (j & 3)) : 8u;
   }
 };
 
-// Up to 8 tokens: all of them lie in shared memory, in the order in which the matrix instructions take them, with the
+// One or two tokens, and up to 8 of small matrices: all of them lie in shared memory, in the order in which the matrix instructions take them, with the
 // sums of each group beside them; weights go straight into the registers that multiply them.  A block takes tiles of 16
 // kMt rows, blockIdx.x and every gridDim.x-th after it; its warps share k in units of 128, of which a batch is on its way
 // while the one before is multiplied, also across tiles.  Of a unit, lane q of the four that share a row takes the
@@ -295,7 +309,7 @@ __global__ void __launch_bounds__(kWarps * 32, 2) cconv_int4_kernel(const Int4Pa
             const float s0 = totals[(unit * kGroups + group) * p.M + t0], s1 = totals[(unit * kGroups + group) * p.M + t1];
 #pragma unroll
             for (int r = 0; r < kRows; ++r) {
-              const float by = values.scale(group, r, lane), zp = 16.0f + values.zero_point(p, group, r, lane);
+              const float by = values.scale(group, r, lane), zp = 16.0f + float(values.zero_point(p, group, r, lane));
               float& f0 = d[r >> 1][(r & 1) * 2];
               float& f1 = d[r >> 1][(r & 1) * 2 + 1];
               acc[r >> 1][(r & 1) * 2] += by * (f0 - zp * s0);
@@ -375,7 +389,7 @@ __device__ __forceinline__ void pairs_of(uint32_t v, uint32_t bias, uint32_t (&w
   w[3] = minus2<T>(__byte_perm(hi, High<T>::kByte, 0x4342), bias);
 }
 
-// 5 to 64 tokens: their words, not the weights, would fill the shared memory's bandwidth if each warp fetched its own.  So
+// Up to 64 tokens: their words, not the weights, would fill the shared memory's bandwidth if each warp fetched its own.  So
 // the warps of a block share the tokens of a unit and take 16 rows each; a cluster of `parts` blocks shares k, and
 // adds up its sums through distributed shared memory in a fixed order.
 template <int kNt>
@@ -402,7 +416,7 @@ __global__ void __launch_bounds__(kWarps * 32, 2) cconv_int4_tokens_kernel(const
       const uint32_t at = uint32_t(unit) * 256 + (lane & 15) * 16;
       const bool there = at < p.x_bytes;
 #pragma unroll
-      for (int i = 0; i < kNt / 2; ++i)
+      for (int i = 0; i < (kNt + 1) / 2; ++i)
         if (i * 16 + token < p.M) copy_piece<16>(token_at + stage * kUnitBytes + i * 4096, token_from + i * 16 * p.x_rs + (there ? at : 0), there);
     }
     commit_copies();
@@ -434,14 +448,13 @@ __global__ void __launch_bounds__(kWarps * 32, 2) cconv_int4_tokens_kernel(const
       if (i % (4 / kGroups) == 0) {
 #pragma unroll
         for (int r = 0; r < 2; ++r)
-          bias[r] = High<T>::kBase | uint32_t(int(values.zero_point(p, i * kGroups / 4, r, lane))) * 0x10001u;
+          bias[r] = High<T>::kBase | values.zero_point(p, i * kGroups / 4, r, lane) * 0x10001u;
       }
       uint32_t lo[4], hi[4];
       pairs_of<T>(*reinterpret_cast<const uint32_t*>(from + word[0] + i * 16), bias[0], lo);
       pairs_of<T>(*reinterpret_cast<const uint32_t*>(from + word[1] + i * 16), bias[1], hi);
 #pragma unroll
       for (int e = 0; e < kNt; ++e) {
-        if (8 * e >= p.M) break;
         // (columns behind the last token: whatever lies there, for sums that go nowhere)
         const uint4 v = *reinterpret_cast<const uint4*>(from + x_word[i & 1] + (i >> 1) * 128 + e * 2048);
         mma16<T>(d[e], lo[0], hi[0], lo[1], hi[1], v.x, v.y);
@@ -568,22 +581,25 @@ template <typename T, int kWords, int kGroups, int kMt>
 cudaError_t launch_rows(const Int4Params& p, int sms, cudaStream_t s) {
   auto f = cconv_int4_kernel<T, kWords, kGroups, kMt>;
   static bool ready[64] = {};
-  const cudaError_t e = allow_smem(f, ready, kMostTokenBytes);
+  const cudaError_t e = allow_smem(f, ready, kSpreadSmem);
   if (e != cudaSuccess) return e;
   const dim3 grid(unsigned(std::min<int64_t>(cdiv64(p.N, 16 * kMt), 2 * sms)));
-  return launch(f, grid, kWarps * 32, size_t(p.units) * p.M * (256 + kGroups * 4), 1, s, p);
+  return launch(f, grid, kWarps * 32, size_t(spread_smem(grid.x, sms, p.units * p.M * (256 + kGroups * 4))), 1, s, p);
 }
 template <typename T, int kGroups, int kNt>
 cudaError_t launch_shared(const Int4Params& p, int sms, cudaStream_t s) {
   auto f = cconv_int4_tokens_kernel<T, kGroups, kNt>;
   constexpr int kSmem = std::max(kStages * kSharedUnit<kNt>, 8 * kNt * (16 * kWarps + 4) * 4);
   static bool ready[64] = {};
-  const cudaError_t e = allow_smem(f, ready, kSmem);
+  const cudaError_t e = allow_smem(f, ready, std::max(kSmem, kSpreadSmem));
   if (e != cudaSuccess) return e;
   const int64_t tiles = cdiv64(p.N, 16 * kWarps);
+  // As many parts as leave every block its place at once, two an SM (a group of SMs has places for whole clusters: not
+  // quite all): 5000 x 4200, 23 tokens in 8 parts 19.7 us, in 4 parts 15.
   int parts = 1;
-  while (parts < 8 && 2 * parts <= p.units && tiles * parts < sms + sms / 2) parts *= 2;
-  return launch(f, dim3(unsigned(tiles * parts)), kWarps * 32, kSmem, parts, s, p, parts);
+  while (parts < 8 && 2 * parts <= p.units && 2 * tiles * parts <= 2 * sms - sms / 4) parts *= 2;
+  const int64_t blocks = tiles * parts, apart = parts > 1 ? std::max<int64_t>(blocks, sms + 1) : blocks;
+  return launch(f, dim3(unsigned(blocks)), kWarps * 32, size_t(spread_smem(apart, sms, kSmem)), parts, s, p, parts);
 }
 template <typename T, int kWords, int kGroups>
 cudaError_t launch_words(const Int4Params& p, int sms, cudaStream_t s) {
@@ -592,12 +608,15 @@ cudaError_t launch_words(const Int4Params& p, int sms, cudaStream_t s) {
 }
 template <typename T, int kGroups>
 cudaError_t launch_tokens(const Int4Params& p, int sms, cudaStream_t s) {
-  if (p.M > 32) return launch_shared<T, kGroups, 8>(p, sms, s);
-  if (p.M > 16) return launch_shared<T, kGroups, 4>(p, sms, s);
-  // What a block makes of 5 to 8 tokens takes longer than its tile's weights, but for small matrices, whose time is that of a
-  // launch: 8 tokens 4096 x 4096 10.0 against 7.5 us, 2048 x 2048 4.8 against 5.9; 4 tokens 8192 x 4096 11.5 against 12.
-  const bool own = p.M <= 4 || (p.M <= 8 && p.units * p.M <= 128);
-  if (!own || int64_t(p.units) * p.M * (256 + kGroups * 4) > kMostTokenBytes) return launch_shared<T, kGroups, 2>(p, sms, s);
+  if (p.M > 48) return launch_shared<T, kGroups, 8>(p, sms, s);
+  if (p.M > 32) return launch_shared<T, kGroups, 6>(p, sms, s);
+  if (p.M > 24) return launch_shared<T, kGroups, 4>(p, sms, s);
+  if (p.M > 16) return launch_shared<T, kGroups, 3>(p, sms, s);
+  if (p.M > 8) return launch_shared<T, kGroups, 2>(p, sms, s);
+  // What each block makes of the tokens for itself takes longer than its tile's weights once they are several, but for
+  // small matrices: 8 tokens 4096 x 4096 8.4 against 6.7 us shared, 2048 x 2048 4.8 against 5.6.
+  const bool own = p.M <= 2 || p.units * p.M <= 128;
+  if (!own || int64_t(p.units) * p.M * (256 + kGroups * 4) > kMostTokenBytes) return launch_shared<T, kGroups, 1>(p, sms, s);
   constexpr int kWords = 4 / kGroups;  // that four lanes may have of a group
   const int most = (p.lies & 15) == 0 ? 4 : (p.lies & 7) == 0 ? 2 : 1;
   if constexpr (kWords == 4)

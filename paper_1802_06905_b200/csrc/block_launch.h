@@ -2,6 +2,8 @@
 #pragma once
 #include <cuda_runtime.h>
 
+#include <algorithm>
+
 #include "block.h"
 
 namespace cconv {
@@ -42,6 +44,15 @@ cudaError_t allow_smem(F f, bool (&ready)[64], int bytes) {
     __atomic_store_n(&ready[dev & 63], true, __ATOMIC_RELEASE);
   }
   return cudaSuccess;
+}
+
+// Shared memory to ask for, at least `need`, so that no SM takes more than its share of `blocks`: what is left is filled
+// up before other SMs get any (256 blocks of which three fit an SM may lie on 86 of them).
+constexpr int kSpreadSmem = 115 * 1024;  // at most
+inline int spread_smem(int64_t blocks, int sms, int need) {
+  const int64_t each = std::max<int64_t>(1, cdiv64(blocks, sms));
+  // (an SM has 228 KB, 1 KB a block of it for itself)
+  return std::max(need, int(228 / (each + 1)) * 1024);
 }
 
 }  // namespace
