@@ -504,7 +504,7 @@ class TensorList:
                 raise ValueError(f"{name}[{i}] must be a bf16, fp16 or fp32 tensor on one CUDA device, got {t.dtype} on {t.device}")
             packed.append(_TENSOR.pack(t.data_ptr(), *_as_rows(t, f"{name}[{i}]"), ty, 0))
         # of tensors of the same layout the elements correspond in the order above
-        self.layout = [(t.dtype, t.shape, None if t.is_contiguous() else t.stride()) for t in self.tensors]
+        self.layout = repr([(str(t.dtype), tuple(t.shape), t.is_contiguous() or t.stride()) for t in self.tensors])
         self._array = ctypes.create_string_buffer(b"".join(packed))
         self.address, self.count = ctypes.addressof(self._array), len(packed)
 

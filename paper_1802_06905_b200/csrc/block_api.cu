@@ -368,6 +368,7 @@ cconv_matrix matrix_of(const cconv_tensor& t) {
 class Tensors {
  public:
   bool ok = true;
+  explicit Tensors(size_t n) { all_.reserve(n); }
   void add(const cconv_matrix& m, int64_t rows, int64_t cols, int es, bool written, int64_t of) {
     if (rows == 0 || cols == 0) return;
     Entry e{{}, written, of};
@@ -376,9 +377,13 @@ class Tensors {
   }
   // No result meets anything but its own gradient (`of` equal) lying in the very same place.
   bool distinct() {
-    std::sort(all_.begin(), all_.end(), [](const Entry& a, const Entry& b) { return a.bytes.lo < b.bytes.lo; });
+    std::vector<std::pair<const char*, const Entry*>> order;
+    order.reserve(all_.size());
+    for (const Entry& e : all_) order.emplace_back(e.bytes.lo, &e);
+    std::sort(order.begin(), order.end());
     std::vector<const Entry*> open;  // those that reach beyond the current one's start
-    for (const Entry& e : all_) {
+    for (const auto& at : order) {
+      const Entry& e = *at.second;
       size_t kept = 0;
       for (const Entry* o : open) {
         if (o->bytes.hi <= e.bytes.lo) continue;
@@ -415,7 +420,7 @@ int clip_call(const cconv_clip_args& a, bool clips, void* cuda_stream) {
   if (!clip_sizes_ok(a, clips)) return CCONV_EINVAL;
   const bool sums = !clips || !a.norm_given;
   bool any = false;
-  Tensors o;
+  Tensors o(size_t(a.count) * 2 + 2);
   for (int64_t i = 0; i < a.count; ++i) {
     const cconv_tensor& g = a.grads[i];
     const int es = type_bytes(g.dtype);
@@ -432,12 +437,12 @@ int clip_call(const cconv_clip_args& a, bool clips, void* cuda_stream) {
   if (need) {
     if (!a.workspace || (reinterpret_cast<uintptr_t>(a.workspace) & 255u) || a.workspace_bytes < uint64_t(need)) return CCONV_EINVAL;
     o.add(cconv_matrix{a.workspace, need, 1}, 1, need, 1, true, -2);
-    if (!o.distinct()) return CCONV_EINVAL;
   }
+  if (!o.distinct()) return CCONV_EINVAL;
   cudaStream_t s = static_cast<cudaStream_t>(cuda_stream);
   const int64_t before = block_launches();
-  int rc = sums && any ? run_square_sums(a, sms, s) : CCONV_OK;
-  if (rc == CCONV_OK) rc = clips && any ? run_clip(a, sms, s) : run_norm_of_sums(a, sms, s);
+  int n = 0, rc = sums && any ? run_square_sums(a, sms, &n, s) : CCONV_OK;
+  if (rc == CCONV_OK) rc = clips && any ? run_clip(a, sms, n, s) : run_norm_of_sums(a, n, s);
   if (block_launches() != before) o.note(cuda_stream, sms);
   return rc;
 }

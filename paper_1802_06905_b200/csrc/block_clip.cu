@@ -319,42 +319,39 @@ int with_tables(const cconv_clip_args& a, int vectors, F f) {
 
 int blocks_of(int64_t pieces, int sms) { return int(std::min<int64_t>(pieces, int64_t(sms) * kBlocksAnSm)); }
 
-// Partial sums of the call: as many as there are blocks in all its launches.
-int sums_of(const cconv_clip_args& a, int sms) {
-  int n = 0;
-  with_tables(a, vectors_of(a, sms), [&](const auto& t, int) {
-    n += blocks_of(t.pieces, sms);
-    return cudaSuccess;
-  });
-  return n;
-}
 
 }  // namespace
 
-int64_t clip_workspace(const cconv_clip_args& a, int sms) { return round_up64(int64_t(sums_of(a, sms)) * 8, 256); }
+// (room for every launch's partial sums at their most)
+int64_t clip_workspace(const cconv_clip_args& a, int sms) {
+  return round_up64(std::max<int64_t>(1, cdiv64(a.count, kMostItems)) * sms * kBlocksAnSm * 8, 256);
+}
 
-int run_square_sums(const cconv_clip_args& a, int sms, cudaStream_t s) {
+
+int run_square_sums(const cconv_clip_args& a, int sms, int* sums, cudaStream_t s) {
+  *sums = 0;
   double* to = static_cast<double*>(a.workspace);
   const int vectors = vectors_of(a, sms);
   return with_tables(a, vectors, [&](const auto& t, int) {
     const int n = blocks_of(t.pieces, sms);
     double* mine = to;
     to += n;
+    *sums += n;
     constexpr int kItems = sizeof(t) == sizeof(Table<kFewItems>) ? kFewItems : kMostItems;
     auto go = [&](auto f) { return launch(f, dim3(unsigned(n)), kThreads, 0, 1, s, t, mine); };
     return vectors == 8 ? go(cconv_square_sums_kernel<kItems, 8>) : go(cconv_square_sums_kernel<kItems, 4>);
   });
 }
 
-int run_norm_of_sums(const cconv_clip_args& a, int sms, cudaStream_t s) {
+int run_norm_of_sums(const cconv_clip_args& a, int sums, cudaStream_t s) {
   return block_cuda_error(launch(cconv_norm_of_sums_kernel, dim3(1), kThreads, 0, 1, s, static_cast<const double*>(a.workspace),
-                                 sums_of(a, sms), static_cast<float*>(a.norm)), "cconv_norm_of_sums_kernel");
+                                 sums, static_cast<float*>(a.norm)), "cconv_norm_of_sums_kernel");
 }
 
-int run_clip(const cconv_clip_args& a, int sms, cudaStream_t s) {
+int run_clip(const cconv_clip_args& a, int sms, int sums, cudaStream_t s) {
   ClipParams c{};
   c.sums = static_cast<double*>(a.workspace);
-  c.blocks = a.norm_given ? 0 : sums_of(a, sms);
+  c.blocks = a.norm_given ? 0 : sums;
   c.norm = static_cast<float*>(a.norm);
   c.max_norm = a.max_norm;
   c.eps = a.eps;

@@ -58,30 +58,43 @@ __device__ __forceinline__ void put_quantized(const NormParams& p, int64_t t, in
 }
 
 // Of a row whose element v nt + tid is the thread's (NV a thread, zeros behind the row): the maxima of 32 neighbours
-// meet in shared memory (`maxima`, a word for each 32 columns of the row, even rows and odd ones apart).
-template <int NV>
+// meet in shared memory, a thread for each 128 columns makes the scale and its reciprocal of them, and all take those
+// (each element with divisions of its own: 16384 x 4095 bf16 435 us).
+template <int kColumns>
+struct AcrossScales {
+  uint32_t maxima[kColumns / 32];
+  float2 scale[(kColumns + 127) / 128];  // and its reciprocal, 0 where quotients are divisions
+};
+template <int NV, int kColumns>
 __device__ __forceinline__ void put_quantized_across(const NormParams& p, int64_t t, int nt, const float (&f)[NV],
-                                                     uint32_t* maxima) {
+                                                     AcrossScales<kColumns>& shared) {
+  const int tid = threadIdx.x, last = (p.D - 1) >> 5;
 #pragma unroll
   for (int v = 0; v < NV; ++v) {
-    const int c = v * nt + int(threadIdx.x);
+    const int c = v * nt + tid;
     const uint32_t m = __reduce_max_sync(0xffffffffu, size_of(f[v]));
-    if ((threadIdx.x & 31) == 0 && c < p.D) maxima[c >> 5] = m;
+    if ((tid & 31) == 0 && c < p.D) shared.maxima[c >> 5] = m;
   }
   __syncthreads();
-  const int last = (p.D - 1) >> 5;
+  for (int b = tid; b * 128 < p.D; b += nt) {
+    uint32_t m = shared.maxima[4 * b];
+#pragma unroll
+    for (int i = 1; i < 4; ++i) m = max(m, shared.maxima[min(4 * b + i, last)]);
+    const float scale = __fdiv_rn(__uint_as_float(m), kMax);
+    const bool quick = scale > 1e-25f && scale < 1e25f;
+    shared.scale[b] = make_float2(scale, quick ? __fdiv_rn(1.0f, scale) : 0.0f);
+    p.q_scale[t * p.q_scale_rs + b * p.q_scale_cs] = scale;
+  }
+  __syncthreads();
 #pragma unroll
   for (int v = 0; v < NV; ++v) {
-    const int c = v * nt + int(threadIdx.x);
+    const int c = v * nt + tid;
     if (c >= p.D) break;
-    const int first = c >> 7 << 2;
-    uint32_t m = maxima[first];
-#pragma unroll
-    for (int i = 1; i < 4; ++i) m = max(m, maxima[min(first + i, last)]);
-    const float scale = __fdiv_rn(__uint_as_float(m), kMax);
-    const float q = __fdiv_rn(f[v], scale == 0.0f ? 1.0f : scale);
+    const float2 s = shared.scale[c >> 7];
+    float q = f[v] * s.y;
+    q = fmaf(fmaf(q, -s.x, f[v]), s.y, q);
+    if (s.y == 0.0f) q = __fdiv_rn(f[v], s.x == 0.0f ? 1.0f : s.x);
     p.q[t * p.q_rs + c] = uint8_t(e4m3x4(pair_of(q, 0.0f), 0));
-    if ((c & 127) == 0) p.q_scale[t * p.q_scale_rs + (c >> 7) * p.q_scale_cs] = scale;
   }
 }
 template <int N>
@@ -95,7 +108,7 @@ __device__ __forceinline__ void as_pairs(const float (&f)[N], uint64_t (&o)[N / 
 template <typename T, int E, int NV, bool kQuant>
 __global__ void __launch_bounds__(1024) cconv_residual_norm_kernel(const NormParams p) {
   __shared__ float2 smem[2][32];
-  __shared__ uint32_t maxima[2][kQuant && E == 1 ? 512 : 1];
+  __shared__ AcrossScales<kQuant && E == 1 ? NV * 1024 : 32> across;
   start_in_order();
   using V = Vec<T, E>;
   const T* resid = static_cast<const T*>(p.resid);  // may be resid_out
@@ -107,7 +120,7 @@ __global__ void __launch_bounds__(1024) cconv_residual_norm_kernel(const NormPar
   T* norm_out = static_cast<T*>(p.norm_out);
   const int nt = blockDim.x, tid = threadIdx.x;
   const float inv_d = 1.0f / float(p.D);
-  int buf = 0, odd = 0;
+  int buf = 0;
   V vpost[NV], vpre[NV];
   auto fetch = [&](V& v, const T* from, int c) {
     v.zero();
@@ -188,8 +201,7 @@ __global__ void __launch_bounds__(1024) cconv_residual_norm_kernel(const NormPar
       float f[NV];
 #pragma unroll
       for (int v = 0; v < NV; ++v) f[v] = o[v][0];
-      put_quantized_across(p, t, nt, f, maxima[odd]);
-      odd ^= 1;
+      put_quantized_across(p, t, nt, f, across);
     }
   }
 }
@@ -279,9 +291,9 @@ __global__ void __launch_bounds__(1024) cconv_residual_norm_long_kernel(const No
 // Many rows that are not wide, through the ring above (16384 x 4095 bf16: 131 us, 224 with a block size known at
 // the launch; with a block a row and everything from global memory 516 us).
 template <typename T, int NV, int kThreads, bool kQuant>
-__global__ void __launch_bounds__(kThreads) cconv_residual_norm_narrow_kernel(const NormParams p) {
+__global__ void __launch_bounds__(kThreads, kQuant ? 512 / kThreads : 1) cconv_residual_norm_narrow_kernel(const NormParams p) {
   extern __shared__ __align__(128) uint8_t ring[];
-  __shared__ uint32_t maxima[2][kQuant ? NV * kThreads / 32 : 1];
+  __shared__ AcrossScales<kQuant ? NV * kThreads : 32> across;
   __shared__ float2 smem[2][32];
   __shared__ __align__(8) uint64_t full[8];
   __shared__ int abort_flag;
@@ -357,7 +369,7 @@ __global__ void __launch_bounds__(kThreads) cconv_residual_norm_narrow_kernel(co
     if constexpr (kQuant) {
 #pragma unroll
       for (int v = 0; v < NV; ++v) o[v] = A::inside(v, p.D) ? o[v] * (rho * wpre[v]) : 0.0f;
-      put_quantized_across(p, t, kThreads, o, maxima[t & 1]);
+      put_quantized_across(p, t, kThreads, o, across);
     }
   }
   if (t < row1) {  // a copy did not come in time: let those on their way land
@@ -369,8 +381,9 @@ __global__ void __launch_bounds__(kThreads) cconv_residual_norm_narrow_kernel(co
 
 // The forward direction of many wide rows, the same way: r and y through a ring, pairs of operations, the
 // weights in registers.
+// (8-bit results: the registers that 1024 threads of an SM may have, which the others keep to of themselves.)
 template <typename T, int NV, bool kAll, bool kQuant>
-__global__ void __launch_bounds__(512) cconv_residual_norm_ring_kernel(const NormParams p) {
+__global__ void __launch_bounds__(512, kQuant ? 2 : 1) cconv_residual_norm_ring_kernel(const NormParams p) {
   extern __shared__ __align__(128) uint8_t ring[];
   __shared__ float2 smem[2][32];
   __shared__ __align__(8) uint64_t full[8];
