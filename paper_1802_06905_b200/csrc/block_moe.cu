@@ -64,11 +64,13 @@ __device__ __forceinline__ float score_of(uint32_t key) {  // (key 1: a NaN too)
 
 // Channels are dealt to the blocks of the cluster, and a block's share of them and 16 experts at a time to its warps:
 // with the usual sizes a warp's loads are all on their way at once.  Partial scores [slice][token][expert] lie in
-// shared memory, a block adds its own up, and the warp that chooses for a token adds up the blocks'.
+// shared memory; a block adds its own up and sends them to the block that chooses for the token (t % 8), whose warps
+// add up the blocks' [block][t / 8][expert].
 template <typename T, int kNt>
 __global__ void __launch_bounds__(kRouterWarps * 32) cconv_moe_router_kernel(const MoeParams p, const int chunk) {
   extern __shared__ __align__(128) uint8_t smem[];
   float* const part = reinterpret_cast<float*>(smem);
+  cluster_arrive();
   start_in_order();
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, g = lane >> 2, q = lane & 3;
   const int rank = int(cluster_ctarank()), t0 = int(blockIdx.x / kRouterBlocks) * chunk, tokens = min(chunk, p.T - t0);
@@ -115,31 +117,31 @@ __global__ void __launch_bounds__(kRouterWarps * 32) cconv_moe_router_kernel(con
         }
     }
   }
+  float* const inbox = part + slices * chunk * p.E;
+  const int own = (tokens + kRouterBlocks - 1) / kRouterBlocks * p.E;  // scores from one block
   __syncthreads();
-  if (slices > 1) {
-    for (int i = threadIdx.x; i < tokens * p.E; i += kRouterWarps * 32) {
-      float v = part[i];
-      for (int o = 1; o < slices; ++o) v += part[o * tokens * p.E + i];
-      part[i] = v;
-    }
+  cluster_wait();  // every block of the cluster is there
+  for (int i = threadIdx.x; i < tokens * p.E; i += kRouterWarps * 32) {
+    const int t = i / p.E, e = i - t * p.E;
+    float v = part[i];
+    for (int o = 1; o < slices; ++o) v += part[o * tokens * p.E + i];
+    store_cluster(cluster_map_shared(smem_u32(inbox + rank * own + t / kRouterBlocks * p.E + e), t % kRouterBlocks), v);
   }
   cluster_sync_all();
   for (int t = rank + kRouterBlocks * warp; t < tokens; t += kRouterBlocks * kRouterWarps) {
-    // the token's scores, whole: the first of each lane's in registers, the others back in this block's memory
-    uint32_t* const row = reinterpret_cast<uint32_t*>(part + t * p.E);
+    // the token's scores, whole: the first of each lane's in registers, the others back in memory
+    const float* const from = inbox + t / kRouterBlocks * p.E;
+    uint32_t* const row = reinterpret_cast<uint32_t*>(inbox + t / kRouterBlocks * p.E);
     uint32_t key[4] = {}, top = 0;
-    const uint32_t at = smem_u32(row);
     for (int e = lane, i = 0; e < p.E; e += 32, ++i) {
-      float v[kRouterBlocks], sum = 0.0f;
+      float sum = 0.0f;
 #pragma unroll
-      for (int r = 0; r < kRouterBlocks; ++r) v[r] = load_cluster(cluster_map_shared(at + e * 4, r));
-#pragma unroll
-      for (int r = 0; r < kRouterBlocks; ++r) sum += v[r];
+      for (int r = 0; r < kRouterBlocks; ++r) sum += from[r * own + e];
       const uint32_t k = key_of(sum);
       top = max(top, k);
 #pragma unroll
       for (int j = 0; j < 4; ++j) key[j] = i == j ? k : key[j];
-      if (i >= 4) row[e] = k;  // (no other block reads this token's scores)
+      if (i >= 4) row[e] = k;
     }
     const float largest = score_of(__reduce_max_sync(0xffffffffu, top));
     float sum = 0.0f;
@@ -175,7 +177,6 @@ __global__ void __launch_bounds__(kRouterWarps * 32) cconv_moe_router_kernel(con
       p.weights[int64_t(t0 + t) * p.weights_rs + lane * p.weights_cs] = __fdiv_rn(expf(mine - largest), sum);
     }
   }
-  cluster_sync_all();  // no block leaves while others read its scores
 }
 
 // ---- who goes where --------------------------------------------------------------------------------
@@ -210,31 +211,54 @@ __device__ __forceinline__ Routes routes_of(const MoeParams& p, uint8_t* smem, i
   r.count = reinterpret_cast<uint8_t*>(r.first + most_groups(E, pairs, most));
   r.token = r.count + most_groups(E, pairs, most);
   auto id_of = [&](int t, int j) { return __ldg(p.ids + t * p.ids_rs + j * p.ids_cs); };
-  if (p.T == 1) {  // a group a choice, in their order: a microsecond less than the general way
+  if (pairs <= 32) {  // one warp, a lane a pair: a kernel a microsecond and a half shorter than the general way
     if (tid < 32) {
-      const int id = tid < p.k ? id_of(0, tid) : -1;
+      const uint32_t whole = 0xffffffffu;
+      const int t = tid / p.k, id = tid < pairs ? id_of(t, tid - t * p.k) : -1;
       const bool valid = id >= 0 && id < E;
-      const uint32_t same = __match_any_sync(0xffffffffu, valid ? id : -1 - tid);
-      const bool first = valid && __ffs(int(same)) - 1 == tid;
-      const uint32_t all = __ballot_sync(0xffffffffu, first);
+      const int key = valid ? id * kTokens + t : -1 - tid;
+      const uint32_t same = __match_any_sync(whole, key);
+      const bool counts = valid && __ffs(int(same)) - 1 == tid;
       float w = 0.0f;
       if (kWeights) {
-        const float own = valid ? __ldg(p.weights + tid * p.weights_cs) : 0.0f;
-        for (int j = 0; j < p.k; ++j) {
-          const float v = __shfl_sync(0xffffffffu, own, j);
+        const float own = valid ? __ldg(p.weights + t * p.weights_rs + (tid - t * p.k) * p.weights_cs) : 0.0f;
+        for (int j = 0; j < pairs; ++j) {
+          const float v = __shfl_sync(whole, own, j);
           if (same >> j & 1) w += v;
         }
       }
-      if (first) {
-        const int at = __popc(all & ((1u << tid) - 1));
-        r.expert[at] = uint16_t(id);
-        r.first[at] = uint16_t(at);
-        r.count[at] = 1;
+      // places: pairs in front, of the same expert (`in`) and of others; one token's experts stay in their order
+      const uint32_t real = __ballot_sync(whole, counts), mates = __match_any_sync(whole, counts ? id : -1 - tid);
+      int at = __popc(real & ((1u << tid) - 1)), in = 0, group = at;
+      if (p.T > 1) {
+        at = 0;
+        for (int j = 0; j < pairs; ++j) {
+          const int other = __shfl_sync(whole, key, j);
+          const bool front = (real >> j & 1) && other < key;
+          at += front;
+          in += front && (mates >> j & 1);
+        }
+      }
+      const bool starts = counts && in % most == 0;
+      const uint32_t heads = __ballot_sync(whole, starts);
+      if (p.T > 1) {
+        group = 0;
+        for (int j = 0; j < pairs; ++j) {
+          const int other = __shfl_sync(whole, at, j);
+          group += (heads >> j & 1) && other < at;
+        }
+      }
+      if (counts) {
         r.pairs[at] = uint16_t(tid);
-        r.token[at] = 0;
+        r.token[at] = uint8_t(t);
         if (kWeights) r.weight[at] = w;
       }
-      if (tid == 0) scratch[0] = __popc(all);
+      if (starts) {
+        r.expert[group] = uint16_t(id);
+        r.first[group] = uint16_t(at);
+        r.count[group] = uint8_t(min(most, __popc(mates) - in));
+      }
+      if (tid == 0) scratch[0] = __popc(heads);
     }
     __syncthreads();
     r.groups = scratch[0];
@@ -495,12 +519,15 @@ __global__ void __launch_bounds__(kWarps * 32, 2) cconv_moe_gate_up_kernel(const
 // Cluster c of `parts` blocks takes the tiles c, c + clusters, ... of 16 channels, each through all groups; the (group,
 // 64 hidden channels) of a tile are dealt evenly to the cluster's warps, in order.  Columns are a group's tokens, the
 // first parts of h in kNt tiles of them and the second parts in kNt more.  Each warp adds its groups' sums, times their
-// weights, to sums of its own [token][16] in shared memory; those of the warps, and then of the blocks, are added up in order.
+// weights, to sums of its own [token][16] in shared memory; those of the warps are added up in order, sent to the block
+// that writes them (block r of n has the r-th of n neighbours), and there the blocks' in order.
 template <typename T, int kNt>
 struct Down {
   static constexpr int kUnitBytes = 2048 + kNt * 2048, kTokens = 8 * kNt;
   static int ring(int stages) { return kWarps * stages * kUnitBytes; }
 };
+// What the blocks of a cluster send one of them of a tile, in multiples of 8 bytes.
+constexpr __host__ __device__ int box_bytes(int T, int parts) { return ((T * 16 + parts - 1) / parts * parts + 1) / 2 * 8; }
 template <typename T, int kNt, int kStages>
 __global__ void __launch_bounds__(kWarps * 32, 2) cconv_moe_down_kernel(const MoeParams p, const int parts) {
   using S = Down<T, kNt>;
@@ -513,10 +540,11 @@ __global__ void __launch_bounds__(kWarps * 32, 2) cconv_moe_down_kernel(const Mo
   const int tiles = int((p.D + 15) / 16), clusters = int(gridDim.x) / parts;
   const int rank = int(blockIdx.x) % parts, first_tile = int(blockIdx.x) / parts;
   const int units = int((p.F + 63) / 64);
+  if (parts > 1) cluster_arrive();
 
   // Behind the gate and up kernel of the same call, which lets this one in only once everything before the call and the
   // router are complete, the choice and the weights are there already; h is waited for below.
-  const Routes r = routes_of<true>(p, smem + kWarps * (kStages * S::kUnitBytes + p.T * 64), scratch, S::kTokens);
+  const Routes r = routes_of<true>(p, smem + kWarps * (kStages * S::kUnitBytes + p.T * 64) + 2 * box_bytes(p.T, parts), scratch, S::kTokens);
   const int64_t work = int64_t(r.groups) * units;
   const int64_t w0 = work * (rank * kWarps + warp) / (parts * kWarps), w1 = work * (rank * kWarps + warp + 1) / (parts * kWarps);
   const int each = int(w1 - w0), group0 = units ? int(w0 / units) : 0, unit0 = int(w0 - int64_t(group0) * units);
@@ -585,6 +613,13 @@ __global__ void __launch_bounds__(kWarps * 32, 2) cconv_moe_down_kernel(const Mo
   fill(load_weights, [] {});
   start_in_order();
   fill(load_tokens, [] { commit_copies(); });  // (the first takes in the weights of all stages)
+  if (parts > 1) cluster_wait();  // every block of the cluster is there
+  const int outputs = p.T * 16, share = (outputs + parts - 1) / parts;
+  float *const boxes = all + kWarps * outputs, *box = boxes;  // [2][parts][share]
+  auto put_out = [&](int tile, int i, float v) {
+    const int64_t channel = int64_t(tile) * 16 + (i & 15);
+    if (channel < p.D) static_cast<T*>(const_cast<void*>(p.out.p))[(i >> 4) * p.out.rs + channel * p.out.cs] = from_f32<T>(v);
+  };
   int stage = 0;
   for (int tile = first_tile; tile < tiles; tile += clusters) {
     for (int i = lane; i < p.T * 16; i += 32) mine[i] = 0.0f;
@@ -636,30 +671,25 @@ __global__ void __launch_bounds__(kWarps * 32, 2) cconv_moe_down_kernel(const Mo
       }
     }
     __syncthreads();
-    const int outputs = p.T * 16;
     for (int i = threadIdx.x; i < outputs; i += kWarps * 32) {
       float s = 0.0f;
 #pragma unroll
       for (int w = 0; w < kWarps; ++w) s += all[w * outputs + i];
-      if (parts == 1) {
-        const int64_t channel = int64_t(tile) * 16 + (i & 15);
-        if (channel < p.D) static_cast<T*>(const_cast<void*>(p.out.p))[(i >> 4) * p.out.rs + channel * p.out.cs] = from_f32<T>(s);
-      } else {
-        all[i] = s;
-      }
+      if (parts == 1) put_out(tile, i, s);
+      else store_cluster(cluster_map_shared(smem_u32(box + rank * share + i / parts), i % parts), s);
     }
     if (parts == 1) {
       __syncthreads();
       continue;
     }
+    // (one meeting a tile: what is sent for the next but one comes after the next tile's, and so after these are read)
     cluster_sync_all();
-    for (int i = threadIdx.x + rank * kWarps * 32; i < outputs; i += parts * kWarps * 32) {
+    for (int i = threadIdx.x * parts + rank; i < outputs; i += parts * kWarps * 32) {
       float s = 0.0f;
-      for (int b = 0; b < parts; ++b) s += load_cluster(cluster_map_shared(smem_u32(all + i), b));
-      const int64_t channel = int64_t(tile) * 16 + (i & 15);
-      if (channel < p.D) static_cast<T*>(const_cast<void*>(p.out.p))[(i >> 4) * p.out.rs + channel * p.out.cs] = from_f32<T>(s);
+      for (int b = 0; b < parts; ++b) s += box[b * share + i / parts];
+      put_out(tile, i, s);
     }
-    cluster_sync_all();  // the sums have been read
+    box = box == boxes ? boxes + parts * share : boxes;
   }
 }
 
@@ -674,7 +704,8 @@ cudaError_t launch_router(const MoeParams& p, int chunk, cudaStream_t s) {
   if (e != cudaSuccess) return e;
   const int groups = int(cdiv64(p.E, 16)), slices = groups >= kRouterWarps ? 1 : kRouterWarps / groups;
   const dim3 grid(unsigned(cdiv64(p.T, chunk) * kRouterBlocks));
-  return launch(f, grid, kRouterWarps * 32, size_t(slices) * chunk * p.E * 4, kRouterBlocks, s, p, chunk);
+  const int64_t scores = int64_t(slices) * chunk + round_up64(chunk, kRouterBlocks);
+  return launch(f, grid, kRouterWarps * 32, size_t(scores * p.E * 4), kRouterBlocks, s, p, chunk);
 }
 // Calls f(T(), columns of 8) for the call's type and at most 64 tokens.
 template <typename F>
@@ -714,7 +745,7 @@ cudaError_t launch_down_as(const MoeParams& p, int sms, cudaStream_t s) {
   const int parts = tiles * 2 > 2 * sms ? 1 : tiles * 4 > 2 * sms ? 2 : tiles * 8 > 2 * sms ? 4 : 8;
   const int64_t clusters = std::min<int64_t>(tiles, 2 * sms / parts);
   return launch(f, dim3(unsigned(clusters * parts)), kWarps * 32,
-                S::ring(kStages) + kWarps * p.T * 64 + routes_bytes(p.E, p.T * p.k, S::kTokens, true), parts, s, p, parts);
+                S::ring(kStages) + kWarps * p.T * 64 + 2 * box_bytes(p.T, parts) + routes_bytes(p.E, p.T * p.k, S::kTokens, true), parts, s, p, parts);
 }
 template <typename T>
 cudaError_t launch_layer(const MoeParams& p, int sms, cudaStream_t s) {

@@ -514,6 +514,12 @@ __device__ __forceinline__ uint32_t cluster_ctarank() {
 }
 // Hardware barrier over all threads of all CTAs of the cluster; release/acquire orders the
 // distributed-shared-memory stores issued before it against the loads issued after it.
+__device__ __forceinline__ void cluster_arrive() {
+  asm volatile("barrier.cluster.arrive.release.aligned;" ::: "memory");
+}
+__device__ __forceinline__ void cluster_wait() {
+  asm volatile("barrier.cluster.wait.acquire.aligned;" ::: "memory");
+}
 __device__ __forceinline__ void cluster_sync_all() {
   asm volatile("barrier.cluster.arrive.release.aligned;" ::: "memory");
   asm volatile("barrier.cluster.wait.acquire.aligned;" ::: "memory");
@@ -523,6 +529,9 @@ __device__ __forceinline__ uint32_t cluster_map_shared(uint32_t local, uint32_t 
   uint32_t r;
   asm volatile("mapa.shared::cluster.u32 %0, %1, %2;" : "=r"(r) : "r"(local), "r"(rank));
   return r;
+}
+__device__ __forceinline__ void store_cluster(uint32_t addr, float v) {
+  asm volatile("st.shared::cluster.f32 [%0], %1;" ::"r"(addr), "f"(v) : "memory");
 }
 __device__ __forceinline__ float load_cluster(uint32_t addr) {
   float v;
