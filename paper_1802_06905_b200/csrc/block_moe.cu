@@ -195,7 +195,7 @@ struct Routes {
 };
 constexpr __host__ __device__ int most_groups(int E, int pairs, int most) { return (E < pairs ? E : pairs) + pairs / most; }
 constexpr int routes_bytes(int E, int pairs, int most, bool weights) {
-  return E * 10 + pairs * (weights ? 7 : 3) + most_groups(E, pairs, most) * 5 + 16;
+  return E * 10 + pairs * (weights ? 13 : 5) + most_groups(E, pairs, most) * 5 + 16;
 }
 
 template <bool kWeights>
@@ -204,7 +204,9 @@ __device__ __forceinline__ Routes routes_of(const MoeParams& p, uint8_t* smem, i
   Routes r;
   r.tokens = reinterpret_cast<uint64_t*>(smem);
   r.weight = reinterpret_cast<float*>(r.tokens + E);
-  r.first_of = reinterpret_cast<uint16_t*>(r.weight + (kWeights ? pairs : 0));
+  float* const given = r.weight + (kWeights ? pairs : 0);  // [pairs]: the weights as they are given
+  int16_t* const ids = reinterpret_cast<int16_t*>(given + (kWeights ? pairs : 0));  // [pairs]: the experts, -1: none
+  r.first_of = reinterpret_cast<uint16_t*>(ids + pairs);
   r.pairs = r.first_of + E;
   r.expert = r.pairs + pairs;
   r.first = r.expert + most_groups(E, pairs, most);
@@ -268,6 +270,8 @@ __device__ __forceinline__ Routes routes_of(const MoeParams& p, uint8_t* smem, i
   __syncthreads();
   for (int i = tid; i < pairs; i += nt) {
     const int t = i / p.k, e = id_of(t, i - t * p.k);
+    if (kWeights) given[i] = __ldg(p.weights + t * p.weights_rs + (i - t * p.k) * p.weights_cs);
+    ids[i] = int16_t(e >= 0 && e < E ? e : -1);
     if (e >= 0 && e < E) atomicOr(reinterpret_cast<unsigned long long*>(r.tokens + e), 1ull << t);
   }
   __syncthreads();
@@ -310,14 +314,14 @@ __device__ __forceinline__ Routes routes_of(const MoeParams& p, uint8_t* smem, i
   }
   __syncthreads();
   for (int i = tid; i < pairs; i += nt) {
-    const int t = i / p.k, j = i - t * p.k, e = id_of(t, j);
-    if (e < 0 || e >= E) continue;
+    const int t = i / p.k, j = i - t * p.k, e = ids[i];
+    if (e < 0) continue;
     bool again = false;
-    float w = kWeights ? __ldg(p.weights + t * p.weights_rs + j * p.weights_cs) : 0.0f;
+    float w = kWeights ? given[i] : 0.0f;
     for (int o = 0; o < p.k; ++o) {
-      if (o == j || id_of(t, o) != e) continue;
+      if (o == j || ids[t * p.k + o] != e) continue;
       again |= o < j;
-      if (kWeights) w += __ldg(p.weights + t * p.weights_rs + o * p.weights_cs);
+      if (kWeights) w += given[t * p.k + o];
     }
     if (again) continue;
     const int to = r.first_of[e] + __popcll(r.tokens[e] & ((1ull << t) - 1));
@@ -385,14 +389,15 @@ __device__ __forceinline__ uint4 words_at(const uint8_t* unit, int segment, int 
 __device__ __forceinline__ int left_of(int64_t length, int64_t from) { return int(min(max(length - from, int64_t(0)), int64_t(64))); }
 
 // ---- gate and up ------------------------------------------------------------------------------------
-// Block b takes the items b, b + gridDim.x, ... of (group, 8 hidden channels); its warps share the channels in
-// units of 64.  Rows 0 to 7 of a tile are the gate's, rows 8 to 15 the up projection's.
+// Team b of kTeam warps (a block or, where channels are few, less) takes the items b, b + teams, ... of (group, 8 hidden
+// channels), which its warps share in units of 64 channels.  Rows 0 to 7 of a tile are the gate's, rows 8 to 15 the up
+// projection's.
 template <typename T, int kNt>
 struct GateUp {
   static constexpr int kStages = kNt == 1 ? 4 : 3, kUnitBytes = 2048 + kNt * 1024, kColumns = 8 * kNt;
   static constexpr int kRing = kWarps * kStages * kUnitBytes, kSmem = kRing + kWarps * kNt * 512;
 };
-template <typename T, int kNt>
+template <typename T, int kNt, int kTeam>
 __global__ void __launch_bounds__(kWarps * 32, 2) cconv_moe_gate_up_kernel(const MoeParams p) {
   using S = GateUp<T, kNt>;
   extern __shared__ __align__(128) uint8_t smem[];
@@ -403,13 +408,20 @@ __global__ void __launch_bounds__(kWarps * 32, 2) cconv_moe_gate_up_kernel(const
   start_in_order();
   const Routes r = routes_of<false>(p, smem + S::kSmem, scratch, S::kColumns);
   const int tiles = int((p.F + 7) / 8);
-  const int units = int((p.D + 63) / 64), per = (units + kWarps - 1) / kWarps, u0 = warp * per;
-  const int64_t items = int64_t(r.groups) * tiles, stride = gridDim.x;
-  const int64_t mine = int64_t(blockIdx.x) < items ? (items - 1 - blockIdx.x) / stride + 1 : 0;
+  constexpr int kTeams = kWarps / kTeam;
+  // (teams of a block are gridDim.x apart, so that a last round spreads over the SMs)
+  const int team = int(blockIdx.x) + warp / kTeam * int(gridDim.x), member = warp % kTeam, thread = threadIdx.x % (kTeam * 32);
+  auto team_sync = [&]() {
+    if constexpr (kTeams == 1) __syncthreads();
+    else asm volatile("bar.sync %0, %1;" ::"r"(1 + warp / kTeam), "n"(kTeam * 32) : "memory");
+  };
+  const int units = int((p.D + 63) / 64), per = (units + kTeam - 1) / kTeam, u0 = member * per;
+  const int64_t items = int64_t(r.groups) * tiles, stride = int64_t(gridDim.x) * kTeams;
+  const int64_t mine = team < items ? (items - 1 - team) / stride + 1 : 0;
 
   // (an item's group and tile, kept without divisions)
   const int step_group = int(stride / tiles), step_tile = int(stride % tiles);
-  int lgroup = int(blockIdx.x) / tiles, ltile = int(blockIdx.x) % tiles, lu = 0, lcount = 0;
+  int lgroup = team / tiles, ltile = team % tiles, lu = 0, lcount = 0;
   const char *rows[4], *columns[2 * kNt];  // of the item: what this lane copies of
   auto row_of = [&](int64_t e, int seg) {
     const int64_t f = min(int64_t(ltile) * 8 + (seg & 7), p.F - 1);
@@ -454,7 +466,7 @@ __global__ void __launch_bounds__(kWarps * 32, 2) cconv_moe_gate_up_kernel(const
   aim();
   for (int i = 0; i < S::kStages; ++i) load(i);
 
-  int group = int(blockIdx.x) / tiles, tile = int(blockIdx.x) % tiles, step = 0;
+  int group = team / tiles, tile = team % tiles, step = 0;
   float acc[kNt][4] = {};
   auto use = [&](int stage) {
     const int count = r.count[group], unit = u0 + step;
@@ -476,7 +488,7 @@ __global__ void __launch_bounds__(kWarps * 32, 2) cconv_moe_gate_up_kernel(const
     __syncwarp();
     if (++step < per) return;
     step = 0;
-    __syncthreads();  // the sums before have been read
+    team_sync();  // the sums before have been read
 #pragma unroll
     for (int e = 0; e < kNt; ++e)
 #pragma unroll
@@ -484,13 +496,13 @@ __global__ void __launch_bounds__(kWarps * 32, 2) cconv_moe_gate_up_kernel(const
         sums[e * kWarps + warp][i * 32 + lane] = acc[e][i];
         acc[e][i] = 0.0f;
       }
-    __syncthreads();
-    for (int i = threadIdx.x; i < 8 * count; i += kWarps * 32) {
+    team_sync();
+    for (int i = thread; i < 8 * count; i += kTeam * 32) {
       const int f = i & 7, c = i >> 3, at = (c & 1) * 32 + f * 4 + ((c & 7) >> 1);
-      const float(*part)[128] = sums + (c >> 3) * kWarps;
+      const float(*part)[128] = sums + (c >> 3) * kWarps + (warp - member);
       float a[1] = {0.0f}, u[1] = {0.0f};
 #pragma unroll
-      for (int w = 0; w < kWarps; ++w) {
+      for (int w = 0; w < kTeam; ++w) {
         a[0] += part[w][at];
         u[0] += part[w][at + 64];
       }
@@ -721,17 +733,22 @@ cudaError_t with_columns(int dtype, int64_t tokens, F f) {
 // Tokens that choose together: as many as leave their scores room in shared memory.
 int router_tokens(int64_t T, int64_t E) { return int(std::min<int64_t>(std::min<int64_t>(T, kTokens), std::max<int64_t>(8, 16384 / E))); }
 
-template <typename T, int kNt>
-cudaError_t launch_gate_up(const MoeParams& p, int sms, cudaStream_t s) {
+template <typename T, int kNt, int kTeam>
+cudaError_t launch_gate_up_as(const MoeParams& p, int sms, cudaStream_t s) {
   using S = GateUp<T, kNt>;
-  auto f = cconv_moe_gate_up_kernel<T, kNt>;
+  auto f = cconv_moe_gate_up_kernel<T, kNt, kTeam>;
   static bool ready[64] = {};
   const cudaError_t e = allow_smem(f, ready, kMostShared);
   if (e != cudaSuccess) return e;
   const int pairs = p.T * p.k;
-  const int64_t most = most_groups(p.E, pairs, S::kColumns) * cdiv64(p.F, 8);
+  const int64_t most = cdiv64(most_groups(p.E, pairs, S::kColumns) * cdiv64(p.F, 8), kWarps / kTeam);
   return launch(f, dim3(unsigned(std::min<int64_t>(most, 2 * sms))), kWarps * 32,
                 S::kSmem + routes_bytes(p.E, pairs, S::kColumns, false), 1, s, p);
+}
+constexpr int64_t kFewChannels = 768;  // 576 channels: 32.1 against 34.8 us with teams of 8, 1000: 27.1 against 26.6
+template <typename T, int kNt>
+cudaError_t launch_gate_up(const MoeParams& p, int sms, cudaStream_t s) {
+  return p.D <= kFewChannels ? launch_gate_up_as<T, kNt, 2>(p, sms, s) : launch_gate_up_as<T, kNt, 8>(p, sms, s);
 }
 template <typename T, int kNt, int kStages>
 cudaError_t launch_down_as(const MoeParams& p, int sms, cudaStream_t s) {
