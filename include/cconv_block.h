@@ -215,7 +215,7 @@ int cconv_quantize_groups(const cconv_quantize_groups_args* args, void* cuda_str
  * ranks, say), and an expert that a token names twice counts with both weights.
  * The weights of each expert in use are read once for 64 tokens; calls of more run 64 at a time. */
 typedef struct {
-  int64_t T, D, F, E;  /* E at most 1024, T at most 2^20 */
+  int64_t T, D, F, E;  /* E at most 1024, T at most 2^20, D and F at most 2^29 */
   int32_t dtype;       /* CCONV_TYPE_BF16 or _FP16, of x, the weights' matrices and out */
   int32_t act, top_k;  /* top_k: 1 to 32, at most E where there is a router */
   int32_t normalize;   /* 0 or 1 */

@@ -14,11 +14,11 @@ HERE = os.path.dirname(os.path.abspath(__file__))
 CSRC = os.path.join(HERE, "csrc")
 LIB = os.path.join(HERE, "libcconv.so")
 SOURCES = ["kernels.cu", "direct_kernel.cu", "stem_kernel.cu", "api.cu", "host_setup.cu", "noalloc.cu", "pool.cu", "planner.cpp",
-           "block_api.cu", "block_clip.cu", "block_few.cu", "block_ffn.cu", "block_fp8.cu", "block_gemm.cu", "block_int4.cu", "block_moe.cu", "block_tma.cu", "block_norm.cu", "block_norm_quant.cu",
+           "block_api.cu", "block_clip.cu", "block_few.cu", "block_ffn.cu", "block_fp8.cu", "block_gemm.cu", "block_int4.cu", "block_moe.cu", "block_pad.cu", "block_tma.cu", "block_norm.cu", "block_norm_quant.cu",
            "block_quant.cu"]
 HEADERS = ["kernels.h", "planner.h", "host_setup.h", "ptx_sm100.cuh", "direct_issue.cuh",
            "block.h", "block_device.cuh", "block_few.h", "block_ffn.h", "block_fp8.h", "block_launch.h", "block_steps.h", "block_gemm.h", "block_tma.h", "pair_sm100.cuh", "block_norm.h", "block_norm.cuh", "block_norm_forward.cuh",
-           "block_clip.h", "block_e4m3.cuh", "block_int4.h", "block_mma.cuh", "block_moe.h", "block_quant.h",
+           "block_clip.h", "block_e4m3.cuh", "block_int4.h", "block_mma.cuh", "block_moe.h", "block_pad.h", "block_quant.h",
            os.path.join("..", "..", "include", "cconv_block.h"), os.path.join("..", "..", "include", "cconv.h")]
 
 

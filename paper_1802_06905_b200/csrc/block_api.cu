@@ -449,7 +449,7 @@ int clip_call(const cconv_clip_args& a, bool clips, void* cuda_stream) {
 
 // ---- mixture of experts --------------------------------------------------------------------------
 bool moe_sizes_ok(const cconv_moe_args& a) {
-  return a.T >= 0 && a.T <= (1 << 20) && length_ok(a.D) && length_ok(a.F) && a.E >= 0 && a.E <= kMostExperts &&
+  return a.T >= 0 && a.T <= (1 << 20) && a.D >= 0 && a.D <= (1 << 29) && a.F >= 0 && a.F <= (1 << 29) && a.E >= 0 && a.E <= kMostExperts &&
          (a.dtype == CCONV_TYPE_BF16 || a.dtype == CCONV_TYPE_FP16) && a.act >= CCONV_ACT_SILU && a.act <= CCONV_ACT_RELU &&
          a.top_k >= 1 && a.top_k <= kMostChosen && (a.normalize == 0 || a.normalize == 1) &&
          (!a.router.data || a.top_k <= a.E || a.T == 0) && double(a.D) * a.F < 1e12 && double(a.T) * a.D < 1e15 &&

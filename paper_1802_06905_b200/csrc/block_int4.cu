@@ -17,10 +17,10 @@
 #include <type_traits>
 
 #include "block_device.cuh"
-#include "block_few.h"
 #include "block_gemm.h"
 #include "block_launch.h"
 #include "block_mma.cuh"
+#include "block_pad.h"
 #include "block_steps.h"
 #include "ptx_sm100.cuh"
 
@@ -649,23 +649,11 @@ void plan(Steps& st, const cconv_int4_product_args& a) {
   }
   if (M <= kFewTokensInt4) {
     Int4Params p{};
-    Mat x(a.x);
-    p.x_bytes = uint32_t(K) * 2;
-    if (!few_readable(x, M, K, 2)) {
-      // (zeros behind a row's end, for k beyond K of its last word)
-      const Mat to = st.scratch(M, K, 2);
-      p.x_bytes = uint32_t(to.rs) * 2;
-      if (K % 8) {
-        const int64_t bytes = M * to.rs * 2;
-        st.add([=](cudaStream_t s) {
-          const cudaError_t e = cudaMemsetAsync(const_cast<void*>(to.p), 0, size_t(bytes), s);
-          block_launches() += e == cudaSuccess;
-          return block_cuda_error(e, "cconv_int4_product");
-        });
-      }
-      st.copy(x, to, M, K, 2);
-      x = to;
-    }
+    int64_t readable = 0;
+    Padded padded;
+    const Mat x = padded.readable(st, a.x, M, K, &readable);
+    padded.add(st);
+    p.x_bytes = uint32_t(readable) * 2;
     p.x = static_cast<const char*>(x.p);
     p.x_rs = x.rs * 2;
     p.w = static_cast<const char*>(w.p);

@@ -19,9 +19,9 @@
 #include <type_traits>
 
 #include "block_device.cuh"
-#include "block_few.h"
 #include "block_launch.h"
 #include "block_mma.cuh"
+#include "block_pad.h"
 #include "block_steps.h"
 #include "ptx_sm100.cuh"
 
@@ -44,7 +44,7 @@ struct MoeParams {
   // expert matrices: element strides
   const char *w_gate, *w_up, *w_down;
   int64_t gate_es, gate_rs, gate_cs, up_es, up_rs, up_cs, down_es, down_rs, down_cs;
-  int piece_in, piece_out;  // bytes that rows of gate and up, and of down, can be copied in (2: element by element)
+  int piece_in, piece_out;  // of gate and up, and of down: see piece_of
   char *h, *h_lo;           // [T k][h_rs] elements
   int64_t h_rs;
   Mat out;
@@ -356,17 +356,10 @@ __device__ __forceinline__ void copy_16(uint32_t to, int segment, int lane, cons
   for (int i = 0; i < kEach; ++i)
     if (i * 4 + (lane >> 3) < count) copy_piece<16>(to + place(segment + i * 4 + (lane >> 3), (lane & 7) * 16), from[i] + at, there);
 }
-// The weights where rows do not lie on 16 bytes: segment s is 64 elements from at(s), step(s) apart, of which the first
-// `left` are there and the others zeros.
+// The weights where a row's elements lie step(s) apart: segment s is 64 elements from at(s), of which the first `left`
+// are there and the others zeros.
 template <typename At, typename Step>
-__device__ __forceinline__ void copy_rows(uint8_t* ring, int piece, int lane, int left, At at, Step step) {
-  if (piece == 4) {
-    for (int seg = 0; seg < 16; ++seg) {
-      const bool there = lane * 4 < left * 2;
-      copy_piece<4>(smem_u32(ring) + place(seg, lane * 4), at(seg) + (there ? lane * 4 : 0), there);
-    }
-    return;
-  }
+__device__ __forceinline__ void copy_elements(uint8_t* ring, int lane, int left, At at, Step step) {
   for (int seg = 0; seg < 16; ++seg) {
     const uint16_t* from = reinterpret_cast<const uint16_t*>(at(seg));
     const int64_t cs = step(seg);
@@ -377,6 +370,38 @@ __device__ __forceinline__ void copy_rows(uint8_t* ring, int piece, int lane, in
     }
   }
 }
+// The weights where rows begin at any multiple of 2 bytes: pieces of 16 bytes from the multiple of 16 that they begin
+// at or behind, so that a row lies up to 14 bytes behind its segment's start and ends in a ninth piece (`kNinths`).  (That
+// multiple lies in the row's allocation, which begins at one itself; behind a row's end nothing is read.)
+constexpr int kNinths = 2048;  // where the ninth pieces lie in a unit: behind the weights
+struct OddRows {
+  // of rows l / 8, l / 8 + 4, ... (l: the lane) the lane's piece of eight, of row l the ninth; and the bytes from there to
+  // the row's end
+  const char *at[4], *ninth;
+  uint32_t left[4], ninth_left;
+  template <typename Row>
+  __device__ __forceinline__ void aim(int lane, uint32_t row_bytes, Row row_of) {
+    auto piece = [&](const char* row, int byte, uint32_t* left) {
+      const uint32_t behind = uint32_t(reinterpret_cast<uintptr_t>(row)) & 15u;
+      *left = row_bytes + behind - byte;  // (may lie behind the end: below zero)
+      return row - behind + byte;
+    };
+#pragma unroll
+    for (int i = 0; i < 4; ++i) at[i] = piece(row_of(i * 4 + (lane >> 3)), (lane & 7) * 16, &left[i]);
+    ninth = piece(row_of(lane & 15), 128, &ninth_left);
+  }
+  // The unit that begins `from` bytes behind the rows' first elements.
+  __device__ __forceinline__ void copy(uint8_t* unit, int lane, uint32_t from) const {
+    auto put = [&](uint32_t to, const char* p, uint32_t left) {
+      const uint32_t bytes = uint32_t(max(0, min(16, int(left - from))));
+      asm volatile("cp.async.cg.shared.global [%0], [%1], 16, %2;" ::"r"(to), "l"(p + (bytes ? int64_t(from) : 0)), "r"(bytes) : "memory");
+    };
+    const uint32_t to = smem_u32(unit);
+#pragma unroll
+    for (int i = 0; i < 4; ++i) put(to + place(i * 4 + (lane >> 3), (lane & 7) * 16), at[i], left[i]);
+    if (lane < 16) put(to + kNinths + lane * 16, ninth, ninth_left);
+  }
+};
 __device__ __forceinline__ void commit_copies() { asm volatile("cp.async.commit_group;" ::: "memory"); }
 template <int kStages>
 __device__ __forceinline__ void wait_for_unit() {
@@ -386,20 +411,36 @@ __device__ __forceinline__ void wait_for_unit() {
 __device__ __forceinline__ uint4 words_at(const uint8_t* unit, int segment, int byte) {
   return *reinterpret_cast<const uint4*>(unit + place(segment, byte));
 }
+// The same of weights that OddRows brought; behind: bytes from the segment's start to the row.
+__device__ __forceinline__ uint4 odd_words_at(const uint8_t* unit, int segment, int byte, uint32_t behind) {
+  const uint4 a = words_at(unit, segment, byte);
+  const uint4 b = *reinterpret_cast<const uint4*>(byte == 112 ? unit + kNinths + segment * 16 : unit + place(segment, byte + 16));
+  uint32_t w[8] = {a.x, a.y, a.z, a.w, b.x, b.y, b.z, b.w};
+  const bool two = behind & 8, one = behind & 4;
+#pragma unroll
+  for (int i = 0; i < 6; ++i) w[i] = two ? w[i + 2] : w[i];
+#pragma unroll
+  for (int i = 0; i < 5; ++i) w[i] = one ? w[i + 1] : w[i];
+  const uint32_t bits = (behind & 2) * 8;
+  return make_uint4(__funnelshift_r(w[0], w[1], bits), __funnelshift_r(w[1], w[2], bits), __funnelshift_r(w[2], w[3], bits),
+                    __funnelshift_r(w[3], w[4], bits));
+}
+__device__ __forceinline__ uint32_t behind_16(const char* row) { return uint32_t(reinterpret_cast<uintptr_t>(row)) & 15u; }
 __device__ __forceinline__ int left_of(int64_t length, int64_t from) { return int(min(max(length - from, int64_t(0)), int64_t(64))); }
 
 // ---- gate and up ------------------------------------------------------------------------------------
 // Team b of kTeam warps (a block or, where channels are few, less) takes the items b, b + teams, ... of (group, 8 hidden
 // channels), which its warps share in units of 64 channels.  Rows 0 to 7 of a tile are the gate's, rows 8 to 15 the up
 // projection's.
-template <typename T, int kNt>
+template <typename T, int kNt, bool kOdd>
 struct GateUp {
-  static constexpr int kStages = kNt == 1 ? 4 : 3, kUnitBytes = 2048 + kNt * 1024, kColumns = 8 * kNt;
+  static constexpr int kFirst = kOdd ? 18 : 16;  // the columns' first segment
+  static constexpr int kStages = kNt == 1 ? 4 : 3, kUnitBytes = kFirst * 128 + kNt * 1024, kColumns = 8 * kNt;
   static constexpr int kRing = kWarps * kStages * kUnitBytes, kSmem = kRing + kWarps * kNt * 512;
 };
-template <typename T, int kNt, int kTeam>
+template <typename T, int kNt, int kTeam, bool kOdd>
 __global__ void __launch_bounds__(kWarps * 32, 2) cconv_moe_gate_up_kernel(const MoeParams p) {
-  using S = GateUp<T, kNt>;
+  using S = GateUp<T, kNt, kOdd>;
   extern __shared__ __align__(128) uint8_t smem[];
   __shared__ int scratch[kWarps];
   float(*const sums)[128] = reinterpret_cast<float(*)[128]>(smem + S::kRing);  // [kNt * kWarps]
@@ -423,16 +464,19 @@ __global__ void __launch_bounds__(kWarps * 32, 2) cconv_moe_gate_up_kernel(const
   const int step_group = int(stride / tiles), step_tile = int(stride % tiles);
   int lgroup = team / tiles, ltile = team % tiles, lu = 0, lcount = 0;
   const char *rows[4], *columns[2 * kNt];  // of the item: what this lane copies of
-  auto row_of = [&](int64_t e, int seg) {
-    const int64_t f = min(int64_t(ltile) * 8 + (seg & 7), p.F - 1);
+  auto row_at = [&](int64_t e, int tile, int seg) {
+    const int64_t f = min(int64_t(tile) * 8 + (seg & 7), p.F - 1);
     return seg < 8 ? p.w_gate + (e * p.gate_es + f * p.gate_rs) * 2 : p.w_up + (e * p.up_es + f * p.up_rs) * 2;
   };
+  OddRows odd;
+  auto row_of = [&](int64_t e, int seg) { return row_at(e, ltile, seg); };
   auto aim = [&]() {
     if (lgroup >= r.groups) return;
     const int64_t e = r.expert[lgroup];
     const int first = r.first[lgroup];
     lcount = r.count[lgroup];
-    if (p.piece_in == 16) {
+    if constexpr (kOdd) odd.aim(lane, uint32_t(p.D) * 2, [&](int seg) { return row_of(e, seg); });
+    if (!kOdd && p.piece_in == 16) {
 #pragma unroll
       for (int i = 0; i < 4; ++i) rows[i] = row_of(e, i * 4 + (lane >> 3));
     }
@@ -445,14 +489,16 @@ __global__ void __launch_bounds__(kWarps * 32, 2) cconv_moe_gate_up_kernel(const
     if (lgroup < r.groups && unit < units) {
       uint8_t* const to = ring + stage * S::kUnitBytes;
       const uint32_t at = uint32_t(unit) * 128 + (lane & 7) * 16;
-      if (p.piece_in == 16) {
+      if constexpr (kOdd) {
+        odd.copy(to, lane, uint32_t(unit) * 128);
+      } else if (p.piece_in == 16) {
         copy_16(smem_u32(to), 0, lane, rows, at < row_bytes ? at : 0, at < row_bytes, 16);
       } else {
         const int64_t e = r.expert[lgroup], k0 = int64_t(unit) * 64;
-        copy_rows(to, p.piece_in, lane, left_of(p.D, k0), [&](int seg) { return row_of(e, seg) + k0 * (seg < 8 ? p.gate_cs : p.up_cs) * 2; },
+        copy_elements(to, lane, left_of(p.D, k0), [&](int seg) { return row_of(e, seg) + k0 * (seg < 8 ? p.gate_cs : p.up_cs) * 2; },
                   [&](int seg) { return seg < 8 ? p.gate_cs : p.up_cs; });
       }
-      copy_16(smem_u32(to), 16, lane, columns, at < column_bytes ? at : 0, at < column_bytes, lcount);
+      copy_16(smem_u32(to), S::kFirst, lane, columns, at < column_bytes ? at : 0, at < column_bytes, lcount);
     }
     commit_copies();
     if (++lu == per) {
@@ -468,18 +514,25 @@ __global__ void __launch_bounds__(kWarps * 32, 2) cconv_moe_gate_up_kernel(const
 
   int group = team / tiles, tile = team % tiles, step = 0;
   float acc[kNt][4] = {};
+  uint32_t behind[2] = {0, 0};  // of this lane's rows (kOdd)
   auto use = [&](int stage) {
     const int count = r.count[group], unit = u0 + step;
+    if (kOdd && step == 0) {
+      const int64_t e = r.expert[group];
+      behind[0] = behind_16(row_at(e, tile, g)), behind[1] = behind_16(row_at(e, tile, g + 8));
+    }
     wait_for_unit<S::kStages>();
     if (unit < units) {
       const uint8_t* from = ring + stage * S::kUnitBytes;
 #pragma unroll
       for (int i = 0; i < 2; ++i) {
-        const uint4 a0 = words_at(from, g, i * 64 + q * 16), a1 = words_at(from, g + 8, i * 64 + q * 16);
+        const int at = i * 64 + q * 16;
+        const uint4 a0 = kOdd ? odd_words_at(from, g, at, behind[0]) : words_at(from, g, at);
+        const uint4 a1 = kOdd ? odd_words_at(from, g + 8, at, behind[1]) : words_at(from, g + 8, at);
 #pragma unroll
         for (int e = 0; e < kNt; ++e) {
           if (8 * e >= count) break;
-          const uint4 v = words_at(from, 16 + 8 * e + g, i * 64 + q * 16);  // (columns behind the last: whatever lies there)
+          const uint4 v = words_at(from, S::kFirst + 8 * e + g, at);  // (columns behind the last: whatever lies there)
           mma16<T>(acc[e], a0.x, a1.x, a0.y, a1.y, v.x, v.y);
           mma16<T>(acc[e], a0.z, a1.z, a0.w, a1.w, v.z, v.w);
         }
@@ -533,16 +586,17 @@ __global__ void __launch_bounds__(kWarps * 32, 2) cconv_moe_gate_up_kernel(const
 // first parts of h in kNt tiles of them and the second parts in kNt more.  Each warp adds its groups' sums, times their
 // weights, to sums of its own [token][16] in shared memory; those of the warps are added up in order, sent to the block
 // that writes them (block r of n has the r-th of n neighbours), and there the blocks' in order.
-template <typename T, int kNt>
+template <typename T, int kNt, bool kOdd>
 struct Down {
-  static constexpr int kUnitBytes = 2048 + kNt * 2048, kTokens = 8 * kNt;
+  static constexpr int kFirst = kOdd ? 18 : 16;  // the columns' first segment
+  static constexpr int kUnitBytes = kFirst * 128 + kNt * 2048, kTokens = 8 * kNt;
   static int ring(int stages) { return kWarps * stages * kUnitBytes; }
 };
 // What the blocks of a cluster send one of them of a tile, in multiples of 8 bytes.
 constexpr __host__ __device__ int box_bytes(int T, int parts) { return ((T * 16 + parts - 1) / parts * parts + 1) / 2 * 8; }
-template <typename T, int kNt, int kStages>
+template <typename T, int kNt, int kStages, bool kOdd>
 __global__ void __launch_bounds__(kWarps * 32, 2) cconv_moe_down_kernel(const MoeParams p, const int parts) {
-  using S = Down<T, kNt>;
+  using S = Down<T, kNt, kOdd>;
   extern __shared__ __align__(128) uint8_t smem[];
   __shared__ int scratch[kWarps];
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, g = lane >> 2, q = lane & 3;
@@ -565,14 +619,17 @@ __global__ void __launch_bounds__(kWarps * 32, 2) cconv_moe_down_kernel(const Mo
   int lt = first_tile, lgroup = group0, lunit = unit0, ln = 0, lcount = 0;
   const char *rows[4], *highs[2 * kNt], *lows[2 * kNt];  // of the tile and group: what this lane copies of
   const uint32_t row_bytes = uint32_t(p.F) * 2, column_bytes = uint32_t(p.h_rs) * 2;
-  auto row_of = [&](int64_t e, int seg) {
-    return p.w_down + (e * p.down_es + min(int64_t(lt) * 16 + seg, p.D - 1) * p.down_rs) * 2;
+  auto row_at = [&](int64_t e, int tile, int seg) {
+    return p.w_down + (e * p.down_es + min(int64_t(tile) * 16 + seg, p.D - 1) * p.down_rs) * 2;
   };
+  OddRows odd;
+  auto row_of = [&](int64_t e, int seg) { return row_at(e, lt, seg); };
   auto aim = [&]() {
     if (lgroup >= r.groups) return;
     const int first = r.first[lgroup];
     lcount = r.count[lgroup];
-    if (p.piece_out == 16) {
+    if constexpr (kOdd) odd.aim(lane, uint32_t(p.F) * 2, [&](int seg) { return row_of(r.expert[lgroup], seg); });
+    if (!kOdd && p.piece_out == 16) {
       const int64_t e = r.expert[lgroup];
 #pragma unroll
       for (int i = 0; i < 4; ++i) rows[i] = row_of(e, i * 4 + (lane >> 3));
@@ -586,19 +643,21 @@ __global__ void __launch_bounds__(kWarps * 32, 2) cconv_moe_down_kernel(const Mo
   };
   auto load_weights = [&](int stage) {
     uint8_t* const to = ring + stage * S::kUnitBytes;
-    if (p.piece_out == 16) {
+    if constexpr (kOdd) {
+      odd.copy(to, lane, uint32_t(lunit) * 128);
+    } else if (p.piece_out == 16) {
       const uint32_t at = uint32_t(lunit) * 128 + (lane & 7) * 16;
       copy_16(smem_u32(to), 0, lane, rows, at < row_bytes ? at : 0, at < row_bytes, 16);
     } else {
       const int64_t e = r.expert[lgroup], k0 = int64_t(lunit) * 64;
-      copy_rows(to, p.piece_out, lane, left_of(p.F, k0), [&](int seg) { return row_of(e, seg) + k0 * p.down_cs * 2; },
+      copy_elements(to, lane, left_of(p.F, k0), [&](int seg) { return row_of(e, seg) + k0 * p.down_cs * 2; },
                 [&](int) { return p.down_cs; });
     }
   };
   auto load_tokens = [&](int stage) {
     const uint32_t to = smem_u32(ring + stage * S::kUnitBytes), at = uint32_t(lunit) * 128 + (lane & 7) * 16;
-    copy_16(to, 16, lane, highs, at < column_bytes ? at : 0, at < column_bytes, lcount);
-    copy_16(to, 16 + S::kTokens, lane, lows, at < column_bytes ? at : 0, at < column_bytes, lcount);
+    copy_16(to, S::kFirst, lane, highs, at < column_bytes ? at : 0, at < column_bytes, lcount);
+    copy_16(to, S::kFirst + S::kTokens, lane, lows, at < column_bytes ? at : 0, at < column_bytes, lcount);
   };
   auto next = [&]() {
     if (++ln == each) {
@@ -638,17 +697,24 @@ __global__ void __launch_bounds__(kWarps * 32, 2) cconv_moe_down_kernel(const Mo
     __syncwarp();
     float d[2 * kNt][4] = {};
     int group = group0, unit = unit0;
+    uint32_t behind[2] = {0, 0};  // of this lane's rows (kOdd)
     for (int n = 0; n < each; ++n) {
       const int count = r.count[group];
+      if (kOdd && (n == 0 || unit == 0)) {
+        const int64_t e = r.expert[group];
+        behind[0] = behind_16(row_at(e, tile, g)), behind[1] = behind_16(row_at(e, tile, g + 8));
+      }
       wait_for_unit<kStages>();
       const uint8_t* from = ring + stage * S::kUnitBytes;
 #pragma unroll
       for (int i = 0; i < 2; ++i) {
-        const uint4 a0 = words_at(from, g, i * 64 + q * 16), a1 = words_at(from, g + 8, i * 64 + q * 16);
+        const int at = i * 64 + q * 16;
+        const uint4 a0 = kOdd ? odd_words_at(from, g, at, behind[0]) : words_at(from, g, at);
+        const uint4 a1 = kOdd ? odd_words_at(from, g + 8, at, behind[1]) : words_at(from, g + 8, at);
 #pragma unroll
         for (int e = 0; e < 2 * kNt; ++e) {
           if (8 * (e % kNt) >= count) continue;
-          const uint4 v = words_at(from, 16 + 8 * e + g, i * 64 + q * 16);
+          const uint4 v = words_at(from, S::kFirst + 8 * e + g, at);
           mma16<T>(d[e], a0.x, a1.x, a0.y, a1.y, v.x, v.y);
           mma16<T>(d[e], a0.z, a1.z, a0.w, a1.w, v.z, v.w);
         }
@@ -733,10 +799,10 @@ cudaError_t with_columns(int dtype, int64_t tokens, F f) {
 // Tokens that choose together: as many as leave their scores room in shared memory.
 int router_tokens(int64_t T, int64_t E) { return int(std::min<int64_t>(std::min<int64_t>(T, kTokens), std::max<int64_t>(8, 16384 / E))); }
 
-template <typename T, int kNt, int kTeam>
+template <typename T, int kNt, int kTeam, bool kOdd>
 cudaError_t launch_gate_up_as(const MoeParams& p, int sms, cudaStream_t s) {
-  using S = GateUp<T, kNt>;
-  auto f = cconv_moe_gate_up_kernel<T, kNt, kTeam>;
+  using S = GateUp<T, kNt, kOdd>;
+  auto f = cconv_moe_gate_up_kernel<T, kNt, kTeam, kOdd>;
   static bool ready[64] = {};
   const cudaError_t e = allow_smem(f, ready, kMostShared);
   if (e != cudaSuccess) return e;
@@ -748,12 +814,14 @@ cudaError_t launch_gate_up_as(const MoeParams& p, int sms, cudaStream_t s) {
 constexpr int64_t kFewChannels = 768;  // 576 channels: 32.1 against 34.8 us with teams of 8, 1000: 27.1 against 26.6
 template <typename T, int kNt>
 cudaError_t launch_gate_up(const MoeParams& p, int sms, cudaStream_t s) {
-  return p.D <= kFewChannels ? launch_gate_up_as<T, kNt, 2>(p, sms, s) : launch_gate_up_as<T, kNt, 8>(p, sms, s);
+  const bool few = p.D <= kFewChannels;
+  if (p.piece_in == 2) return few ? launch_gate_up_as<T, kNt, 2, true>(p, sms, s) : launch_gate_up_as<T, kNt, 8, true>(p, sms, s);
+  return few ? launch_gate_up_as<T, kNt, 2, false>(p, sms, s) : launch_gate_up_as<T, kNt, 8, false>(p, sms, s);
 }
-template <typename T, int kNt, int kStages>
-cudaError_t launch_down_as(const MoeParams& p, int sms, cudaStream_t s) {
-  using S = Down<T, kNt>;
-  auto f = cconv_moe_down_kernel<T, kNt, kStages>;
+template <typename T, int kNt, int kStages, bool kOdd>
+cudaError_t launch_down_odd(const MoeParams& p, int sms, cudaStream_t s) {
+  using S = Down<T, kNt, kOdd>;
+  auto f = cconv_moe_down_kernel<T, kNt, kStages, kOdd>;
   static bool ready[64] = {};
   const cudaError_t e = allow_smem(f, ready, kMostShared);
   if (e != cudaSuccess) return e;
@@ -763,6 +831,10 @@ cudaError_t launch_down_as(const MoeParams& p, int sms, cudaStream_t s) {
   const int64_t clusters = std::min<int64_t>(tiles, 2 * sms / parts);
   return launch(f, dim3(unsigned(clusters * parts)), kWarps * 32,
                 S::ring(kStages) + kWarps * p.T * 64 + 2 * box_bytes(p.T, parts) + routes_bytes(p.E, p.T * p.k, S::kTokens, true), parts, s, p, parts);
+}
+template <typename T, int kNt, int kStages>
+cudaError_t launch_down_as(const MoeParams& p, int sms, cudaStream_t s) {
+  return p.piece_out == 2 ? launch_down_odd<T, kNt, kStages, true>(p, sms, s) : launch_down_odd<T, kNt, kStages, false>(p, sms, s);
 }
 template <typename T>
 cudaError_t launch_layer(const MoeParams& p, int sms, cudaStream_t s) {
@@ -774,36 +846,19 @@ cudaError_t launch_layer(const MoeParams& p, int sms, cudaStream_t s) {
   return p.T <= 16 ? launch_down_as<T, 1, 3>(p, sms, s) : launch_down_as<T, 1, 2>(p, sms, s);
 }
 
-// Bytes that rows of an expert's matrix can be copied in.
+// Bytes that rows of an expert's matrix begin at multiples of: 16 (and end there), 2, or 1: elements lie apart.
 int piece_of(const cconv_matrix& m, int64_t expert_stride, int64_t rows, int64_t cols, int64_t experts) {
-  if (m.col_stride != 1 && cols > 1) return 2;
+  if (m.col_stride != 1 && cols > 1) return 1;
   const uintptr_t lies = reinterpret_cast<uintptr_t>(m.data) | uintptr_t(rows > 1 ? m.row_stride * 2 : 0) |
                          uintptr_t(experts > 1 ? expert_stride * 2 : 0) | uintptr_t(cols * 2);
-  return (lies & 15) == 0 ? 16 : (lies & 3) == 0 ? 4 : 2;
-}
-
-// Rows that 16 bytes at a time can be read from, with zeros behind K; *k: elements that may be read.
-Mat padded(Steps& st, const cconv_matrix& m, int64_t rows, int64_t K, int64_t* k) {
-  *k = K;
-  if (few_readable(Mat(m), rows, K, 2)) return Mat(m);
-  const Mat to = st.scratch(rows, K, 2);
-  *k = to.rs;
-  if (K % 8) {
-    const int64_t bytes = rows * to.rs * 2;
-    st.add([=](cudaStream_t s) {
-      const cudaError_t e = cudaMemsetAsync(const_cast<void*>(to.p), 0, size_t(bytes), s);
-      block_launches() += e == cudaSuccess;
-      return block_cuda_error(e, "cconv_moe_forward");
-    });
-  }
-  st.copy(Mat(m), to, rows, K, 2);
-  return to;
+  return (lies & 15) == 0 ? 16 : 2;
 }
 
 void plan(Steps& st, const cconv_moe_args& a) {
   const int sms = st.sms();
   MoeParams p{};
-  const Mat x = padded(st, a.x, a.T, a.D, &p.x_k);
+  Padded padded;
+  const Mat x = padded.readable(st, a.x, a.T, a.D, &p.x_k);
   p.x = static_cast<const char*>(x.p);
   p.x_rs = x.rs * 2;
   p.D = a.D;
@@ -831,9 +886,12 @@ void plan(Steps& st, const cconv_moe_args& a) {
   p.out = Mat(a.out);
   if (a.router.data) {
     int64_t k = 0;
-    const Mat router = padded(st, a.router, a.E, a.D, &k);
+    const Mat router = padded.readable(st, a.router, a.E, a.D, &k);
     p.router = static_cast<const char*>(router.p);
     p.router_rs = router.rs * 2;
+  }
+  padded.add(st);
+  if (a.router.data) {
     MoeParams r = p;
     r.T = int(a.T);
     st.add([=](cudaStream_t s) {

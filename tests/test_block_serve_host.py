@@ -98,7 +98,7 @@ MOE = ("cconv_moe_forward", "cconv_moe_args",
     (GROUPS, dict(dtype=3)), (GROUPS, dict(scale_dtype=-1)), (GROUPS, dict(group=48)), (GROUPS, dict(reserved=7)), (GROUPS, dict(N=-3)),
     (GROUPS, dict(q=at(1, 128))), (GROUPS, dict(scale=at(2, 2))), (GROUPS, dict(zero=at(3, 2))), (GROUPS, dict(q=(2 << 20, 64, 1))),
     (GROUPS, dict(w=(0, 256, 1))), (GROUPS, dict(scale=((3 << 20) + 1, 2, 1))),
-    (MOE, dict(T=-1)), (MOE, dict(T=(1 << 20) + 1)), (MOE, dict(E=1025)), (MOE, dict(E=-1)), (MOE, dict(dtype=2)), (MOE, dict(act=4)),
+    (MOE, dict(T=-1)), (MOE, dict(T=(1 << 20) + 1)), (MOE, dict(E=1025)), (MOE, dict(D=(1 << 29) + 1)), (MOE, dict(F=(1 << 29) + 1)), (MOE, dict(E=-1)), (MOE, dict(dtype=2)), (MOE, dict(act=4)),
     (MOE, dict(top_k=0)), (MOE, dict(top_k=33)), (MOE, dict(top_k=9)), (MOE, dict(normalize=2)), (MOE, dict(x=(0, 64, 1))),
     (MOE, dict(w_gate=(0, 64, 1))), (MOE, dict(w_up=((4 << 20) + 1, 64, 1))), (MOE, dict(w_down=(5 << 20, -1, 1))),
     (MOE, dict(gate_stride=-1)), (MOE, dict(up_stride=1 << 41)), (MOE, dict(ids=(0, 2, 1))), (MOE, dict(ids=((6 << 20) + 2, 2, 1))),

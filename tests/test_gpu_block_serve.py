@@ -694,3 +694,26 @@ def test_moe_offsets_beyond_32_bits():
         old, _ = t, setattr(m, name, far)
         assert torch.equal(m.run()[0], exp), name
         setattr(m, name, old)
+
+
+@pytest.mark.parametrize("T", [1, 4, 20])
+@pytest.mark.parametrize("D,F", [(64, 64), (63, 65), (33, 127), (40, 66), (129, 191), (70, 1)])
+def test_moe_rows_keep_their_neighbours_out(T, D, F):
+    """An infinity in one row of the last matrix reaches its channel alone: nothing of a row's neighbours, which lie
+    right in front of it and behind it, enters its sums, wherever rows begin."""
+    for at in (0, 1, 2):
+        m = Moe(T, D, F, 3, 2)
+        store = torch.zeros(at + 3 * D * F, device="cuda", dtype=BF16)
+        wd = store[at:].view(3, D, F)
+        wd.copy_(m.wd)
+        m.wd = wd
+        exp, ids, weights = m.run()
+        m.check_out(exp, ids, weights, "plain")
+        for d in (0, D // 2, D - 1):
+            for f in (0, F - 1):
+                old = wd[:, d, f].clone()
+                wd[:, d, f] = float("inf")
+                out = m.run()[0]
+                others = [c for c in range(D) if c != d]
+                assert torch.equal(out[:, others], exp[:, others]) and not torch.isfinite(out[:, d]).any()
+                wd[:, d, f] = old
