@@ -237,7 +237,7 @@ int cconv_moe_forward(const cconv_moe_args* args, void* cuda_stream);
 /* ---- the norm of a list of gradients, and clipping -------------------------------------------------
  * norm = sqrt(sum of squares over all elements), the sum in 64 bits, rounded to fp32; every element times
  * min(1, max_norm / (norm + eps)), in fp32, rounded to its type.  A norm that is infinite makes the factor 0, one that is
- * NaN makes every element NaN.  Tensors of more than two dimensions are lists of rows where their strides allow. */
+ * NaN, or as infinite as max_norm, makes every element NaN.  Tensors of more than two dimensions are lists of rows where their strides allow. */
 typedef struct {
   void* data;
   int64_t rows, cols, row_stride, col_stride; /* strides in elements */

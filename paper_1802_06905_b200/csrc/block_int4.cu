@@ -114,7 +114,7 @@ template <int kEach>
 struct RowCopies {
   const char* rows[kEach];  // of this lane's rows, from the multiple of 16 bytes that it begins behind
   const char* tail;         // of row `lane`: a fifth piece
-  bool first, last;         // whether the array's first or last row is among them
+  bool first, last;         // whether their first or last pieces may reach out of the array
   static __device__ __forceinline__ const char* aligned(const char* q) {
     return reinterpret_cast<const char*>(reinterpret_cast<uintptr_t>(q) & ~uintptr_t(15));
   }
@@ -123,12 +123,13 @@ struct RowCopies {
 #pragma unroll
     for (int i = 0; i < kEach; ++i) rows[i] = aligned(p.w + min(row0 + i * 8 + (lane >> 2), end) * p.w_rs) + (lane & 3) * 16;
     tail = aligned(p.w + min(row0 + lane, end) * p.w_rs) + 64;
-    first = row0 == 0;
-    last = row0 + 8 * kEach > end;
+    // (rows may be shorter than a unit, or all the same one: the last tile's are not the only ones)
+    first = aligned(p.w + min(row0, end) * p.w_rs) < p.w;
+    last = p.w + min(row0 + 8 * kEach - 1, end) * p.w_rs + int64_t(p.units) * 64 + 16 > p.w_end;
   }
   __device__ __forceinline__ void copy(const Int4Params& p, uint32_t to, int lane, int unit) const {
     const uint32_t at = uint32_t(unit) * 64;
-    if ((first && unit == 0) || (last && unit >= p.units - 2)) {  // pieces that may reach out of the array
+    if ((first && unit == 0) || (last && unit >= p.units - 2)) {
 #pragma unroll 1
       for (int i = 0; i < kEach; ++i) copy_inside(to + row_place(i * 8 + (lane >> 2), (lane & 3) * 16), rows[i] + at, p);
       if (p.shifted && lane < 8 * kEach) copy_inside(to + row_place(lane, 64), tail + at, p);

@@ -338,14 +338,9 @@ __device__ __forceinline__ Routes routes_of(const MoeParams& p, uint8_t* smem, i
 // swapped, so that the 16-byte words that eight lanes read together lie in different banks.
 __device__ __forceinline__ uint32_t place(int segment, int byte) { return segment * 128 + (byte ^ ((segment & 1) << 6)); }
 
-// kBytes, or zeros, to shared memory, not waited for.
-template <int kBytes>
-__device__ __forceinline__ void copy_piece(uint32_t to, const char* from, bool there) {
-  const uint32_t n = there ? kBytes : 0;
-  if constexpr (kBytes == 16)
-    asm volatile("cp.async.cg.shared.global [%0], [%1], 16, %2;" ::"r"(to), "l"(from), "r"(n) : "memory");
-  else
-    asm volatile("cp.async.ca.shared.global [%0], [%1], %2, %3;" ::"r"(to), "l"(from), "n"(kBytes), "r"(n) : "memory");
+// 16 bytes, of which the first n are from memory and the others zeros, to shared memory, not waited for.
+__device__ __forceinline__ void copy_piece(uint32_t to, const char* from, uint32_t n) {
+  asm volatile("cp.async.cg.shared.global [%0], [%1], 16, %2;" ::"r"(to), "l"(from), "r"(n) : "memory");
 }
 // Copies 16 bytes that every lane names of 4 rows (or columns) each, 128 bytes of 4 neighbouring rows an instruction;
 // lane l's go to the word l % 8 of the rows l / 8, l / 8 + 4, ... of those from `segment` on.  Of columns, the first `count`.
@@ -354,7 +349,7 @@ __device__ __forceinline__ void copy_16(uint32_t to, int segment, int lane, cons
                                         int count) {
 #pragma unroll
   for (int i = 0; i < kEach; ++i)
-    if (i * 4 + (lane >> 3) < count) copy_piece<16>(to + place(segment + i * 4 + (lane >> 3), (lane & 7) * 16), from[i] + at, there);
+    if (i * 4 + (lane >> 3) < count) copy_piece(to + place(segment + i * 4 + (lane >> 3), (lane & 7) * 16), from[i] + at, there ? 16 : 0);
 }
 // The weights where a row's elements lie step(s) apart: segment s is 64 elements from at(s), of which the first `left`
 // are there and the others zeros.
@@ -394,7 +389,7 @@ struct OddRows {
   __device__ __forceinline__ void copy(uint8_t* unit, int lane, uint32_t from) const {
     auto put = [&](uint32_t to, const char* p, uint32_t left) {
       const uint32_t bytes = uint32_t(max(0, min(16, int(left - from))));
-      asm volatile("cp.async.cg.shared.global [%0], [%1], 16, %2;" ::"r"(to), "l"(p + (bytes ? int64_t(from) : 0)), "r"(bytes) : "memory");
+      copy_piece(to, p + (bytes ? int64_t(from) : 0), bytes);
     };
     const uint32_t to = smem_u32(unit);
 #pragma unroll

@@ -264,6 +264,19 @@ def test_int4_rows_with_a_shared_token_and_shared_weights():
     c.check(c.run(), "broadcast")
 
 
+@pytest.mark.parametrize("M", [9, 40])
+@pytest.mark.parametrize("N,K", [(34, 8), (34, 24), (18, 136), (50, 264), (129, 40)])
+def test_int4_short_rows(M, N, K):
+    """Rows of less than the bytes that are read of one at once, side by side, overlapping and all the same."""
+    c = Int4(M, N, K, 32, BF16, zero=True)
+    c.check(c.run(), "side by side")
+    bytes_ = K // 2
+    flat = c.q.reshape(-1)
+    for pitch in (4, 0):
+        c.q = flat[4:].as_strided((N, bytes_), (pitch, 1), 4) if (N - 1) * pitch + bytes_ + 4 <= flat.numel() else c.q
+        c.check(c.run(), f"{pitch} bytes apart")
+
+
 def test_int4_of_nothing():
     for M, N, K in ((0, 8, 64), (3, 0, 64), (3, 8, 0)):
         c = Int4(M, N, K)
@@ -481,6 +494,16 @@ def test_clip_infinities_and_nan():
     a[5] = float("nan")
     block.clip_gradients([a, b], 1.0, norm)
     assert torch.isnan(norm).all() and torch.isnan(a).all() and torch.isnan(b).all()
+
+
+def test_clip_without_a_limit():
+    a = torch.full((5000,), 3.0, device="cuda", dtype=BF16)
+    norm = poisoned((1,), FP32)
+    block.clip_gradients([a], float("inf"), norm)
+    assert abs(norm.item() - 3.0 * 5000 ** 0.5) < 1e-3 and (a == 3.0).all()
+    a[7] = float("inf")
+    block.clip_gradients([a], float("inf"), norm)  # the formula's quotient is none
+    assert norm.item() == float("inf") and torch.isnan(a).all()
 
 
 def test_clip_of_nothing():
