@@ -14,6 +14,7 @@
 #include "block_int4.h"
 
 #include <algorithm>
+#include <atomic>
 #include <type_traits>
 
 #include "block_device.cuh"
@@ -595,10 +596,17 @@ cudaError_t launch_shared(const Int4Params& p, int sms, cudaStream_t s) {
   const cudaError_t e = allow_smem(f, ready, std::max(kSmem, kSpreadSmem));
   if (e != cudaSuccess) return e;
   const int64_t tiles = cdiv64(p.N, 16 * kWarps);
-  // As many parts as leave every block its place at once, two an SM (a group of SMs has places for whole clusters: not
-  // quite all): 5000 x 4200, 23 tokens in 8 parts 19.7 us, in 4 parts 15.
+  // As many parts as leave every block its place at once, two an SM.  A cluster lies in one group of SMs, whose number
+  // differs, so that the device is asked: 40 tiles (5000 x 4200, 23 tokens) in 4 parts 16.5 us, in 6 13.2, in 7, which do
+  // not fit, 20.  (Not quite all places, while the kernel in front may still have some: 55 tiles in 5 parts 14 us, in 4 12.5.)
+  static std::atomic<int> places[64][9];
   int parts = 1;
-  while (parts < 8 && 2 * parts <= p.units && 2 * tiles * parts <= 2 * sms - sms / 4) parts *= 2;
+  for (int n = 2; n <= 8 && n <= p.units && tiles * n <= 2 * sms - sms / 4; ++n) {
+    int at_once = 0;
+    const cudaError_t e = clusters_at_once(f, kWarps * 32, std::max(kSmem, spread_smem(2, 1, 0)), n, places, &at_once);
+    if (e != cudaSuccess) return e;
+    if (tiles <= at_once) parts = n;
+  }
   const int64_t blocks = tiles * parts, apart = parts > 1 ? std::max<int64_t>(blocks, sms + 1) : blocks;
   return launch(f, dim3(unsigned(blocks)), kWarps * 32, size_t(spread_smem(apart, sms, kSmem)), parts, s, p, parts);
 }

@@ -3,6 +3,7 @@
 #include <cuda_runtime.h>
 
 #include <algorithm>
+#include <atomic>
 
 #include "block.h"
 
@@ -44,6 +45,32 @@ cudaError_t allow_smem(F f, bool (&ready)[64], int bytes) {
     __atomic_store_n(&ready[dev & 63], true, __ATOMIC_RELEASE);
   }
   return cudaSuccess;
+}
+
+// How many clusters of `size` (2 to 8) blocks of f the current device holds at once (`known`: the kernel's, by device and size,
+// one more than the number).
+template <typename F>
+cudaError_t clusters_at_once(F f, int threads, int smem, int size, std::atomic<int> (&known)[64][9], int* n) {
+  int dev = 0;
+  cudaError_t e = cudaGetDevice(&dev);
+  if (e != cudaSuccess) return e;
+  std::atomic<int>& at = known[dev & 63][size];
+  *n = at.load(std::memory_order_relaxed) - 1;
+  if (*n >= 0) return cudaSuccess;
+  cudaLaunchConfig_t cfg = {};
+  cfg.gridDim = dim3(unsigned(size));
+  cfg.blockDim = dim3(unsigned(threads));
+  cfg.dynamicSmemBytes = size_t(smem);
+  cudaLaunchAttribute attr[1];
+  attr[0].id = cudaLaunchAttributeClusterDimension;
+  attr[0].val.clusterDim.x = unsigned(size);
+  attr[0].val.clusterDim.y = 1;
+  attr[0].val.clusterDim.z = 1;
+  cfg.attrs = attr;
+  cfg.numAttrs = 1;
+  e = cudaOccupancyMaxActiveClusters(n, f, &cfg);
+  if (e == cudaSuccess) at.store(*n + 1, std::memory_order_relaxed);
+  return e;
 }
 
 // Shared memory to ask for, at least `need`, so that no SM takes more than its share of `blocks`: what is left is filled
