@@ -64,6 +64,19 @@ __device__ __forceinline__ float2 block_sum2(float a, float b, float2 (*smem)[32
   return make_float2(warp_sum(v.x), warp_sum(v.y));
 }
 
+// The same of one value.
+__device__ __forceinline__ float block_sum1(float a, float2 (*smem)[32], int& buf) {
+  a = warp_sum(a);
+  const int warps = blockDim.x >> 5;
+  if (warps == 1) return a;
+  float* const sums = reinterpret_cast<float*>(smem[buf]);
+  if ((threadIdx.x & 31) == 0) sums[threadIdx.x >> 5] = a;
+  __syncthreads();
+  const int lane = threadIdx.x & 31;
+  buf ^= 1;
+  return warp_sum(lane < warps ? sums[lane] : 0.0f);
+}
+
 // Block b of the kernels that take neighbouring rows has the rows [T b / nb, T (b+1) / nb).
 __device__ __forceinline__ int64_t first_row(const NormParams& p, int64_t b) {
   return p.T * b / p.nb;

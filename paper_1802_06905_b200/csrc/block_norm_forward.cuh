@@ -32,6 +32,7 @@ __device__ __forceinline__ void put_quantized(const NormParams& p, int64_t t, in
   uint32_t size = size_of(m);
 #pragma unroll
   for (int o = kLanes / 2; o > 0; o >>= 1) size = max(size, __shfl_xor_sync(0xffffffffu, size, o));
+  if (!inside) return;  // (a warp of zeros behind the row would divide: 16384 x 5376 221 us)
   m = __uint_as_float(size);
   float scale = m * (1.0f / kMax);
   if (m > 1e-22f && m < 1e25f) {
@@ -47,10 +48,11 @@ __device__ __forceinline__ void put_quantized(const NormParams& p, int64_t t, in
     }
   } else {
     scale = __fdiv_rn(m, kMax);
+    if (scale != 0.0f) {
 #pragma unroll
-    for (int i = 0; i < P; ++i) f[i] = divide_pair(f[i], scale == 0.0f ? 1.0f : scale);
+      for (int i = 0; i < P; ++i) f[i] = divide_pair(f[i], scale);
+    }
   }
-  if (!inside) return;
   if ((c & 127) == 0) p.q_scale[t * p.q_scale_rs + (c >> 7) * p.q_scale_cs] = scale;
   uint8_t* to = p.q + t * p.q_rs + c;
   if constexpr (P == 4) *reinterpret_cast<uint2*>(to) = make_uint2(e4m3x4(f[0], f[1]), e4m3x4(f[2], f[3]));
@@ -93,7 +95,7 @@ __device__ __forceinline__ void put_quantized_across(const NormParams& p, int64_
     const float2 s = shared.scale[c >> 7];
     float q = f[v] * s.y;
     q = fmaf(fmaf(q, -s.x, f[v]), s.y, q);
-    if (s.y == 0.0f) q = __fdiv_rn(f[v], s.x == 0.0f ? 1.0f : s.x);
+    if (s.y == 0.0f) q = s.x == 0.0f ? f[v] : __fdiv_rn(f[v], s.x);
     p.q[t * p.q_rs + c] = uint8_t(e4m3x4(pair_of(q, 0.0f), 0));
   }
 }
@@ -153,7 +155,7 @@ __global__ void __launch_bounds__(1024) cconv_residual_norm_kernel(const NormPar
 #pragma unroll
         for (int i = 0; i < E; ++i) ss += f[i] * f[i];
       }
-      rho = rsqrtf(block_sum2(ss, 0.0f, smem, buf).x * inv_d + p.eps);
+      rho = rsqrtf(block_sum1(ss, smem, buf) * inv_d + p.eps);
     }
     float o[NV][E], ss = 0.0f;
 #pragma unroll
@@ -182,7 +184,7 @@ __global__ void __launch_bounds__(1024) cconv_residual_norm_kernel(const NormPar
       if (c < p.D) V::store(resid_out + t * p.resid_out_rs + c, o[v]);
     }
     if (!kQuant && !norm_out) continue;
-    rho = rsqrtf(block_sum2(ss, 0.0f, smem, buf).x * inv_d + p.eps);
+    rho = rsqrtf(block_sum1(ss, smem, buf) * inv_d + p.eps);
 #pragma unroll
     for (int v = 0; v < NV; ++v) {
       const int c = (v * nt + tid) * E;
@@ -233,7 +235,7 @@ __global__ void __launch_bounds__(1024) cconv_residual_norm_long_kernel(const No
         const float f = to_f32(y[c]);
         ss += f * f;
       }
-      rho_y = rsqrtf(block_sum2(ss, 0.0f, smem, buf).x * inv_d + p.eps);
+      rho_y = rsqrtf(block_sum1(ss, smem, buf) * inv_d + p.eps);
     }
     auto out = [&](int c) {
       float o = p.scale * to_f32(r[c]);
@@ -252,7 +254,7 @@ __global__ void __launch_bounds__(1024) cconv_residual_norm_long_kernel(const No
         const float o = out(c);
         ss += o * o;
       }
-      rho_r = rsqrtf(block_sum2(ss, 0.0f, smem, buf).x * inv_d + p.eps);
+      rho_r = rsqrtf(block_sum1(ss, smem, buf) * inv_d + p.eps);
     }
     if constexpr (kQuant) {
       // all threads take the same number of columns; a block of 128 lies within four warps of one of them
@@ -346,7 +348,7 @@ __global__ void __launch_bounds__(kThreads, kQuant ? 512 / kThreads : 1) cconv_r
     if (block && w_post) {
 #pragma unroll
       for (int v = 0; v < NV; ++v) ss += o[v] * o[v];
-      rho = rsqrtf(block_sum2(ss, 0.0f, smem, buf).x * inv_d + p.eps);
+      rho = rsqrtf(block_sum1(ss, smem, buf) * inv_d + p.eps);
       ss = 0.0f;
     }
     float r[NV];
@@ -359,7 +361,7 @@ __global__ void __launch_bounds__(kThreads, kQuant ? 512 / kThreads : 1) cconv_r
       if (A::inside(v, p.D)) to[A::column(v)] = from_f32<T>(o[v]);
     }
     if (!kQuant && !norm_out) continue;
-    rho = rsqrtf(block_sum2(ss, 0.0f, smem, buf).x * inv_d + p.eps);
+    rho = rsqrtf(block_sum1(ss, smem, buf) * inv_d + p.eps);
     to = norm_out + t * p.norm_out_rs;
     if (!kQuant || norm_out) {
 #pragma unroll
@@ -382,7 +384,8 @@ __global__ void __launch_bounds__(kThreads, kQuant ? 512 / kThreads : 1) cconv_r
 // The forward direction of many wide rows, the same way: r and y through a ring, pairs of operations, the
 // weights in registers.
 // (8-bit results: the registers that 1024 threads of an SM may have, which the others keep to of themselves.)
-template <typename T, int NV, bool kAll, bool kQuant>
+// kAll: every operand is there; kExact: and every access of every thread lies in the row.
+template <typename T, int NV, bool kAll, bool kExact, bool kQuant>
 __global__ void __launch_bounds__(512, kQuant ? 2 : 1) cconv_residual_norm_ring_kernel(const NormParams p) {
   extern __shared__ __align__(128) uint8_t ring[];
   __shared__ float2 smem[2][32];
@@ -399,7 +402,7 @@ __global__ void __launch_bounds__(512, kQuant ? 2 : 1) cconv_residual_norm_ring_
   T* norm_out = static_cast<T*>(p.norm_out);
   const int nt = blockDim.x, tid = threadIdx.x;
   const bool has_block = kAll || block, has_post = kAll || w_post, has_norm = (kAll && !kQuant) || norm_out;
-  auto inside = [&](int v) { return kAll || (v * nt + tid) * E < p.D; };
+  auto inside = [&](int v) { return kExact || (v * nt + tid) * E < p.D; };
   const float inv_d = 1.0f / float(p.D);
   const int64_t row0 = first_row(p, blockIdx.x), row1 = first_row(p, blockIdx.x + 1);
   const int64_t per = p.rows_per_gate ? p.rows_per_gate : p.T;
@@ -463,7 +466,7 @@ __global__ void __launch_bounds__(512, kQuant ? 2 : 1) cconv_residual_norm_ring_
 #pragma unroll
         for (int i = 0; i < P; ++i) sum = fma2(o[v][i], o[v][i], sum);
       }
-      if (has_post) rho1 = rsqrtf(block_sum2(sum_of(sum), 0.0f, smem, buf).x * inv_d + p.eps);
+      if (has_post) rho1 = rsqrtf(block_sum1(sum_of(sum), smem, buf) * inv_d + p.eps);
     }
     uint64_t rho = pair_of(rho1, rho1);
     sum = 0;
@@ -480,7 +483,7 @@ __global__ void __launch_bounds__(512, kQuant ? 2 : 1) cconv_residual_norm_ring_
       if (inside(v)) put_pairs<T>(resid_out + t * p.resid_out_rs + (v * nt + tid) * E, o[v]);
     }
     if (!kQuant && !has_norm) continue;
-    rho1 = rsqrtf(block_sum2(sum_of(sum), 0.0f, smem, buf).x * inv_d + p.eps);
+    rho1 = rsqrtf(block_sum1(sum_of(sum), smem, buf) * inv_d + p.eps);
     rho = pair_of(rho1, rho1);
 #pragma unroll
     for (int v = 0; v < NV; ++v) {
@@ -503,13 +506,21 @@ cudaError_t launch_forward_nv(const NormParams& p, int threads, int64_t grid, cu
   return launch(cconv_residual_norm_kernel<T, E, NV, kQuant>, dim3(unsigned(grid)), threads, 0, 1, s, p);
 }
 
-template <typename T, int NV, bool kAll, bool kQuant>
-cudaError_t launch_forward_ring(const NormParams& p, int threads, cudaStream_t s) {
-  auto f = cconv_residual_norm_ring_kernel<T, NV, kAll, kQuant>;
+template <typename T, int NV, bool kAll, bool kExact, bool kQuant>
+cudaError_t launch_forward_ring_as(const NormParams& p, int threads, cudaStream_t s) {
+  auto f = cconv_residual_norm_ring_kernel<T, NV, kAll, kExact, kQuant>;
   static bool ready[64] = {};
   const cudaError_t e = allow_ring(f, ready);
   if (e != cudaSuccess) return e;
   return launch(f, dim3(unsigned(p.nb)), threads, size_t(p.D) * p.ring_rows * 2 * sizeof(T), 1, s, p);
+}
+
+template <typename T, int NV, bool kQuant>
+cudaError_t launch_forward_ring(const NormParams& p, int threads, cudaStream_t s) {
+  const bool all = p.block && p.w_post && p.w_pre && p.gate && (kQuant || p.norm_out);
+  if (!all) return launch_forward_ring_as<T, NV, false, false, kQuant>(p, threads, s);
+  if (p.D * int64_t(sizeof(T)) != int64_t(threads) * NV * 16) return launch_forward_ring_as<T, NV, true, false, kQuant>(p, threads, s);
+  return launch_forward_ring_as<T, NV, true, true, kQuant>(p, threads, s);
 }
 
 template <typename T, bool kQuant>
@@ -527,10 +538,9 @@ cudaError_t launch_forward(NormParams p, int sms, cudaStream_t s) {
   if (w && sh.threads && sh.threads <= 512 && rows(an_sm) >= 2 && p.T >= 4 * an_sm * sms) {
     p.nb = int(an_sm * sms);
     p.ring_rows = int(std::min<int64_t>(8, rows(an_sm)));
-    const bool all = p.block && p.w_post && p.w_pre && p.gate && (kQuant || p.norm_out) && p.D == int64_t(sh.threads) * sh.nv * kWide;
-    if (sh.nv == 1) return all ? launch_forward_ring<T, 1, true, kQuant>(p, threads, s) : launch_forward_ring<T, 1, false, kQuant>(p, threads, s);
-    if (sh.nv == 2) return all ? launch_forward_ring<T, 2, true, kQuant>(p, threads, s) : launch_forward_ring<T, 2, false, kQuant>(p, threads, s);
-    return all ? launch_forward_ring<T, kMost, true, kQuant>(p, threads, s) : launch_forward_ring<T, kMost, false, kQuant>(p, threads, s);
+    if (sh.nv == 1) return launch_forward_ring<T, 1, kQuant>(p, threads, s);
+    if (sh.nv == 2) return launch_forward_ring<T, 2, kQuant>(p, threads, s);
+    return launch_forward_ring<T, kMost, kQuant>(p, threads, s);
   }
   const int64_t grid = std::min<int64_t>(p.T, int64_t(sms) * std::max(1, std::min(32, 1024 / threads)));
   if (!sh.threads) return launch(cconv_residual_norm_long_kernel<T, kQuant>, dim3(unsigned(grid)), threads, 0, 1, s, p);
