@@ -155,7 +155,7 @@ struct RowRing {
 // a row then has more than kThreads NV 2/3 elements (NV = 12 and 16), so that most need no comparison.
 template <int NV, int kThreads>
 struct Across {
-  static constexpr int kSure = kThreads && NV > 8 ? NV - 4 : 0;  // elements that every thread has
+  static constexpr int kSure = kThreads && NV > 8 ? NV - 4 : kThreads > 64 ? NV / 2 : 0;  // elements that every thread has
   static __device__ __forceinline__ int nt() { return kThreads ? kThreads : blockDim.x; }
   static __device__ __forceinline__ int column(int v) { return v * nt() + int(threadIdx.x); }
   static __device__ __forceinline__ bool inside(int v, int D) { return v < kSure || column(v) < D; }
@@ -311,6 +311,24 @@ cudaError_t with_narrow_shape(const Shape& n, F f) {
   if (n.threads == 128) return elements(std::integral_constant<int, 128>());
   if (n.threads == 256) return elements(std::integral_constant<int, 256>());
   return elements(std::integral_constant<int, 512>());
+}
+// The same for 8-bit results: 8 elements a thread as long as that is enough, so that 1024 threads share an SM.
+inline Shape narrow_quant_shape(int64_t D) {
+  for (int threads : {64, 128, 192, 256, 384, 512})
+    if (D <= threads * 8) return {threads, 8};
+  return narrow_shape(D);
+}
+template <typename F>
+cudaError_t with_narrow_quant_shape(const Shape& n, F f) {
+  auto eight = [&](auto threads) { return f(std::integral_constant<int, 8>(), threads); };
+  if (n.nv == 12) return f(std::integral_constant<int, 12>(), std::integral_constant<int, 512>());
+  if (n.nv == 16) return f(std::integral_constant<int, 16>(), std::integral_constant<int, 512>());
+  if (n.threads == 64) return eight(std::integral_constant<int, 64>());
+  if (n.threads == 128) return eight(std::integral_constant<int, 128>());
+  if (n.threads == 192) return eight(std::integral_constant<int, 192>());
+  if (n.threads == 256) return eight(std::integral_constant<int, 256>());
+  if (n.threads == 384) return eight(std::integral_constant<int, 384>());
+  return eight(std::integral_constant<int, 512>());
 }
 // Whether the rows of an array can go through it: none but the first and last touch its ends.
 inline bool narrow_fits(const void* q, int64_t rs, const NormParams& p, int es) {

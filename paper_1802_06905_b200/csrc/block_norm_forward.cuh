@@ -292,8 +292,9 @@ __global__ void __launch_bounds__(1024) cconv_residual_norm_long_kernel(const No
 
 // Many rows that are not wide, through the ring above (16384 x 4095 bf16: 131 us, 224 with a block size known at
 // the launch; with a block a row and everything from global memory 516 us).
+constexpr int narrow_threads(int nv) { return nv == 8 ? 1024 : 512; }  // of an SM, of 8-bit results
 template <typename T, int NV, int kThreads, bool kQuant>
-__global__ void __launch_bounds__(kThreads, kQuant ? 512 / kThreads : 1) cconv_residual_norm_narrow_kernel(const NormParams p) {
+__global__ void __launch_bounds__(kThreads, kQuant ? narrow_threads(NV) / kThreads : 1) cconv_residual_norm_narrow_kernel(const NormParams p) {
   extern __shared__ __align__(128) uint8_t ring[];
   __shared__ AcrossScales<kQuant ? NV * kThreads : 32> across;
   __shared__ float2 smem[2][32];
@@ -552,23 +553,25 @@ cudaError_t launch_forward(NormParams p, int sms, cudaStream_t s) {
     return launch_forward_nv<T, kWide, kMost, kQuant>(p, threads, grid, s);
   }
   // many rows that are not wide: the same with their own ring
-  const Shape n = narrow_shape(p.D);
+  const Shape n = kQuant ? narrow_quant_shape(p.D) : narrow_shape(p.D);
   if (n.threads && narrow_fits(p.resid, p.resid_rs, p, sizeof(T)) && narrow_fits(p.block, p.block_rs, p, sizeof(T))) {
     const int64_t es = sizeof(T), slot = narrow_slot(p.D * es), spare = n.threads * n.nv * es;
-    an_sm = 1024 / n.threads;
+    an_sm = (kQuant ? narrow_threads(n.nv) : 1024) / n.threads;
     auto narrow_rows = [&](int64_t blocks) { return (kRingSmem / blocks / 1024 * 1024 - kRingOwn - spare) / (2 * slot); };
     while (an_sm > 1 && narrow_rows(an_sm) < 2) --an_sm;
     if (narrow_rows(an_sm) >= 2 && p.T >= 4 * an_sm * sms) {
       p.nb = int(an_sm * sms);
       p.ring_rows = int(std::min<int64_t>(8, narrow_rows(an_sm)));
       p.ring_slot = uint32_t(slot);
-      return with_narrow_shape(n, [&](auto nv, auto nt) {
+      auto go = [&](auto nv, auto nt) {
         auto f = cconv_residual_norm_narrow_kernel<T, decltype(nv)::value, decltype(nt)::value, kQuant>;
         static bool ready[64] = {};
         const cudaError_t e = allow_ring(f, ready);
         if (e != cudaSuccess) return e;
         return launch(f, dim3(unsigned(p.nb)), nt, size_t(p.ring_rows) * 2 * slot + spare, 1, s, p);
-      });
+      };
+      if constexpr (kQuant) return with_narrow_quant_shape(n, go);
+      else return with_narrow_shape(n, go);
     }
   }
   if (sh.nv == 1) return launch_forward_nv<T, 1, 1, kQuant>(p, threads, grid, s);
