@@ -292,9 +292,11 @@ __global__ void __launch_bounds__(1024) cconv_residual_norm_long_kernel(const No
 
 // Many rows that are not wide, through the ring above (16384 x 4095 bf16: 131 us, 224 with a block size known at
 // the launch; with a block a row and everything from global memory 516 us).
+// (Blocks an SM that the compiler keeps registers for: without 8-bit results none are named.  Naming one is no lower
+// limit but leave to take 104 to 131 registers instead of 72 to 109: 16384 x 4095 192 us, 16384 x 2047 76 instead of 62.)
 constexpr int narrow_threads(int nv) { return nv == 8 ? 1024 : 512; }  // of an SM, of 8-bit results
 template <typename T, int NV, int kThreads, bool kQuant>
-__global__ void __launch_bounds__(kThreads, kQuant ? narrow_threads(NV) / kThreads : 1) cconv_residual_norm_narrow_kernel(const NormParams p) {
+__global__ void __launch_bounds__(kThreads, kQuant ? narrow_threads(NV) / kThreads : 0) cconv_residual_norm_narrow_kernel(const NormParams p) {
   extern __shared__ __align__(128) uint8_t ring[];
   __shared__ AcrossScales<kQuant ? NV * kThreads : 32> across;
   __shared__ float2 smem[2][32];
@@ -384,10 +386,13 @@ __global__ void __launch_bounds__(kThreads, kQuant ? narrow_threads(NV) / kThrea
 
 // The forward direction of many wide rows, the same way: r and y through a ring, pairs of operations, the
 // weights in registers.
-// (8-bit results: the registers that 1024 threads of an SM may have, which the others keep to of themselves.)
+// (8-bit results: the registers that 1024 threads of an SM may have.  Others take up to 84, or with kRoomy, for blocks of
+// at most 256 threads of which two share an SM all the same, up to 96: 16384 x 4080 bf16 89 instead of 99 us, 8192 x 2048
+// fp32 47.4 instead of 48.6; where every access lies in the row of 16-bit elements they do not pay, 16384 x 4096 94 instead
+// of 92, and larger blocks would lose their neighbour, 16384 x 5376 154 instead of 135.)
 // kAll: every operand is there; kExact: and every access of every thread lies in the row.
-template <typename T, int NV, bool kAll, bool kExact, bool kQuant>
-__global__ void __launch_bounds__(512, kQuant ? 2 : 1) cconv_residual_norm_ring_kernel(const NormParams p) {
+template <typename T, int NV, bool kAll, bool kExact, bool kRoomy, bool kQuant>
+__global__ void __launch_bounds__(kRoomy ? 256 : 512, kQuant || kRoomy ? 2 : 0) cconv_residual_norm_ring_kernel(const NormParams p) {
   extern __shared__ __align__(128) uint8_t ring[];
   __shared__ float2 smem[2][32];
   __shared__ __align__(8) uint64_t full[8];
@@ -507,9 +512,9 @@ cudaError_t launch_forward_nv(const NormParams& p, int threads, int64_t grid, cu
   return launch(cconv_residual_norm_kernel<T, E, NV, kQuant>, dim3(unsigned(grid)), threads, 0, 1, s, p);
 }
 
-template <typename T, int NV, bool kAll, bool kExact, bool kQuant>
+template <typename T, int NV, bool kAll, bool kExact, bool kRoomy, bool kQuant>
 cudaError_t launch_forward_ring_as(const NormParams& p, int threads, cudaStream_t s) {
-  auto f = cconv_residual_norm_ring_kernel<T, NV, kAll, kExact, kQuant>;
+  auto f = cconv_residual_norm_ring_kernel<T, NV, kAll, kExact, kRoomy, kQuant>;
   static bool ready[64] = {};
   const cudaError_t e = allow_ring(f, ready);
   if (e != cudaSuccess) return e;
@@ -519,9 +524,19 @@ cudaError_t launch_forward_ring_as(const NormParams& p, int threads, cudaStream_
 template <typename T, int NV, bool kQuant>
 cudaError_t launch_forward_ring(const NormParams& p, int threads, cudaStream_t s) {
   const bool all = p.block && p.w_post && p.w_pre && p.gate && (kQuant || p.norm_out);
-  if (!all) return launch_forward_ring_as<T, NV, false, false, kQuant>(p, threads, s);
-  if (p.D * int64_t(sizeof(T)) != int64_t(threads) * NV * 16) return launch_forward_ring_as<T, NV, true, false, kQuant>(p, threads, s);
-  return launch_forward_ring_as<T, NV, true, true, kQuant>(p, threads, s);
+  if (!all) return launch_forward_ring_as<T, NV, false, false, false, kQuant>(p, threads, s);
+  const bool exact = p.D * int64_t(sizeof(T)) == int64_t(threads) * NV * 16;
+  // more than 256 threads come with 16 elements a thread alone
+  constexpr bool kMayBeLarge = kQuant || NV * 16 / int(sizeof(T)) == 16, kRoomyExact = !kQuant && sizeof(T) == 4;
+  if constexpr (kMayBeLarge) {
+    if (kQuant || threads > 256)
+      return exact ? launch_forward_ring_as<T, NV, true, true, false, kQuant>(p, threads, s)
+                   : launch_forward_ring_as<T, NV, true, false, false, kQuant>(p, threads, s);
+  }
+  if constexpr (!kQuant) {
+    if (!exact) return launch_forward_ring_as<T, NV, true, false, true, kQuant>(p, threads, s);
+    return launch_forward_ring_as<T, NV, true, true, kRoomyExact, kQuant>(p, threads, s);
+  }
 }
 
 template <typename T, bool kQuant>

@@ -1,0 +1,39 @@
+"""Calls of the sub-block whose kernels were once slowed down by a change that left their results as they were: times
+against a neighbour's in the same process.  The limits lie in the middle between the two measured ratios (B200)."""
+import pytest
+import torch
+
+from paper_1802_06905_b200 import block
+from test_gpu_block import BF16, gen, normal
+
+pytestmark = pytest.mark.gpu
+
+
+def pace(calls, n=20, rounds=7):
+    """The least time of n calls of each, measured in turn."""
+    best = [float("inf")] * len(calls)
+    for _ in range(rounds):
+        for i, call in enumerate(calls):
+            a, b = torch.cuda.Event(enable_timing=True), torch.cuda.Event(enable_timing=True)
+            torch.cuda.synchronize()
+            a.record()
+            for _ in range(n):
+                call()
+            b.record()
+            b.synchronize()
+            best[i] = min(best[i], a.elapsed_time(b))
+    return best
+
+
+def forward_norm(T, D):
+    g = gen(T + D)
+    resid, y, w = normal(g, (T, D), BF16), normal(g, (T, D), BF16), normal(g, (D,), BF16)
+    gate = normal(g, (-(-T // 2048), D), BF16)
+    out, x = torch.empty_like(resid), torch.empty_like(resid)
+    return lambda: block.residual_norm_forward(resid, out, x, block=y, w_post=w, gate=gate, w_pre=w, rows_per_gate=2048)
+
+
+@pytest.mark.parametrize("D,limit", [(4095, 1.72), (2047, 1.36)])  # 2.04 and 1.50 with too few blocks an SM, 1.41 and 1.22
+def test_rows_that_begin_anywhere_keep_their_pace(D, limit):
+    odd, even = pace([forward_norm(16384, D), forward_norm(16384, D + 1)])
+    assert odd < limit * even, (odd, even)
