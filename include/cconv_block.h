@@ -169,7 +169,8 @@ int cconv_quantize_blocks(const cconv_quantize_args* args, void* cuda_stream);
  * Element 2j of a row of q is the low half of byte j, element 2j + 1 its high half; what lies behind K in the last
  * byte does not matter.  A token that holds an infinity or a NaN gives infinities or NaN.
  * Up to 64 tokens, sums are of q and X as they are, in fp32, and scaled in fp32; with more, the weights
- * scale (q - zero) are rounded to `dtype` first, as operands of the tensor cores. */
+ * scale (q - zero) are rounded to the precision of `dtype` first, as operands of the tensor cores (fp16: not to its range;
+ * a row's groups whose scale is below 2^-24 of its largest lose bits, 2^-31 of that one at most). */
 typedef struct {
   int64_t M, N, K;
   int32_t dtype;       /* CCONV_TYPE_BF16 or _FP16, of X and C */

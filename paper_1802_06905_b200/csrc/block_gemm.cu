@@ -73,7 +73,7 @@ struct PairParams {
   int64_t out_rs[3], out_cs[3];
   const char* in[2];
   int64_t in_rs[2];
-  // 8-bit: scale of row r (of 128 rows of B) and k block kb
+  // 8-bit: scale of row r (of 128 rows of B) and k block kb.  kColumns: col_scale of column n
   const float *row_scale, *col_scale;
   int64_t row_rs, row_ks, col_rs, col_ks;
   int* status;
@@ -197,7 +197,7 @@ __device__ __forceinline__ void unstage32(uint32_t base, int r, int c0, float (&
 // Pieces that an epilogue warp stages.
 int pieces_of(const Launch& l) {
   if (l.cut()) return 0;
-  return l.epilogue == kStore ? 2 : l.epilogue == kScaled || (l.epilogue == kGated && !l.save) ? 1 : 3;
+  return l.epilogue == kStore || l.epilogue == kColumns ? 2 : l.epilogue == kScaled || (l.epilogue == kGated && !l.save) ? 1 : 3;
 }
 // Scales of 8-bit rows that an epilogue warp keeps: 16 blocks of k of its 32 rows and of its columns
 // (row 32), the 16 in use and the next 16; a pitch of 17 words keeps the lanes on different banks.
@@ -286,6 +286,15 @@ __device__ __forceinline__ void write8(char* base, int64_t rs, int64_t cs, int64
 #pragma unroll
     for (int i = 0; i < 8; ++i)
       if (i < n) to[i * cs] = from_f32<T>(f[i]);
+  }
+}
+// Columns' sums times their factors (the same in every lane).
+template <int N>
+__device__ __forceinline__ void scale_columns(float (&f)[N], const float* by) {
+#pragma unroll
+  for (int i = 0; i < N; i += 4) {
+    const float4 v = __ldg(reinterpret_cast<const float4*>(by + i));
+    f[i] *= v.x, f[i + 1] *= v.y, f[i + 2] *= v.z, f[i + 3] *= v.w;
   }
 }
 template <typename T>
@@ -542,7 +551,8 @@ __global__ void __launch_bounds__(kThreads, 1) cconv_pair_product_kernel(
               float f[8];
               load_sums8(acc + i * 32 + c * 8, f);
               join8(base, row, c, p.splits, share, sent, local, f);
-              if constexpr (kEpi == kStore) {
+              if constexpr (kEpi == kStore || kEpi == kColumns) {
+                if constexpr (kEpi == kColumns) scale_columns(f, p.col_scale + at);
                 write8<T>(p.out[0], p.out_rs[0], p.out_cs[0], r, at, n, f);
               } else if constexpr (kEpi == kGated) {
                 float u[8];
@@ -568,7 +578,7 @@ __global__ void __launch_bounds__(kThreads, 1) cconv_pair_product_kernel(
           break;  // there is one tile
         }
       }
-      if constexpr (kEpi == kStore) {
+      if constexpr (kEpi == kStore || kEpi == kColumns) {
         if (!wait_sums()) break;
         const int cols = o.block_n >> 1;
         for (int c = 0; c < cols; c += 64) {
@@ -582,6 +592,11 @@ __global__ void __launch_bounds__(kThreads, 1) cconv_pair_product_kernel(
           load_sums(acc + at, f);
           load_sums(acc + at + 32, g);
           if (c + 64 >= cols) release_sums();
+          if constexpr (kEpi == kColumns) {
+            const float* by = p.col_scale + tl.n * int64_t(o.block_n) + at;
+            scale_columns(f, by);
+            scale_columns(g, by + 32);
+          }
           const uint32_t to = mine + piece * kBoxBytes;
           if (lane == 0) bulk_wait_group_read<1>();
           __syncwarp();
@@ -929,8 +944,9 @@ int run_as(const Launch& l, int sms, cudaStream_t s) {
   q.col_ks = l.col_scale.cs;
   q.limit_ns = block_wait_limit_ns();
   cudaError_t e;
-  if (l.dtype == CCONV_TYPE_BF16) e = launch_pair<kEpi, __nv_bfloat16>(maps, q, sms, s);
-  else if (l.dtype == CCONV_TYPE_FP16) e = launch_pair<kEpi, __half>(maps, q, sms, s);
+  if (l.dtype == CCONV_TYPE_FP16) e = launch_pair<kEpi, __half>(maps, q, sms, s);
+  else if constexpr (kEpi == kColumns) return CCONV_EUNSUPPORTED;
+  else if (l.dtype == CCONV_TYPE_BF16) e = launch_pair<kEpi, __nv_bfloat16>(maps, q, sms, s);
   else if constexpr (kEight) e = launch_pair<kEpi, float>(maps, q, sms, s);
   else return CCONV_EUNSUPPORTED;
   return block_cuda_error(e, "cconv_pair_product_kernel");
@@ -1153,6 +1169,7 @@ void choose_cut(Launch* l, int sms, bool few_columns) {
 
 int run_products(const Launch& l, int sms, cudaStream_t s) {
   if (l.epilogue == kStore) return run_as<kStore>(l, sms, s);
+  if (l.epilogue == kColumns) return run_as<kColumns>(l, sms, s);
   if (l.epilogue == kGated) return run_as<kGated>(l, sms, s);
   if (l.epilogue == kGatedBackward) return run_as<kGatedBackward>(l, sms, s);
   return run_as<kScaled>(l, sms, s);

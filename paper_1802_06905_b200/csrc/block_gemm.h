@@ -16,6 +16,7 @@ enum : int {
   kGated = 1,          // columns are pairs g, u: out[0] = act(g) * u, and out[1] = g, out[2] = u if saved
   kGatedBackward = 2,  // sums are dh; in[0] = g, in[1] = u: out[0] = dg, out[1] = du, out[2] = h
   kScaled = 3,         // 8-bit operands, sums of each block of 128 scaled: out[0]
+  kColumns = 4,        // fp16: out[0], column n times col_scale[n]
 };
 
 constexpr int kMostProducts = 4;  // of one launch
@@ -28,7 +29,7 @@ struct Product {
   bool segments = false, paired = false;
   int64_t M = 0, N = 0, K = 0;  // paired: N = rows of b[0]
   Mat out[3], in[2];            // `in` row-major; unless cut, all row-major and in place for the copy engine
-  int block_n = 256;            // columns of a tile: 256, 128 or (kStore, B k-contiguous) 64
+  int block_n = 256;            // columns of a tile: 256, 128 or (kStore and kColumns, B k-contiguous) 64
 };
 
 struct Launch {
@@ -38,7 +39,9 @@ struct Launch {
   int splits = 1;               // pairs that share a tile, each a part of k: 1, 2 or 4
   int dtype = 0, act = 0;
   bool save = false;
-  Mat row_scale, col_scale;     // kScaled: scale (row, kb) of A, (row / 128, kb) of B
+  // kScaled: scale (row, kb) of A, (row / 128, kb) of B.  kColumns: col_scale of every column of every tile, 32-byte
+  // aligned (room for N rounded up to 256)
+  Mat row_scale, col_scale;
   bool cut() const { return splits > 1; }  // results then go straight to any layout
 };
 

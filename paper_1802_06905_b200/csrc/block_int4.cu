@@ -506,11 +506,16 @@ __global__ void __launch_bounds__(kWarps * 32, 2) cconv_int4_tokens_kernel(const
 
 // The weights as numbers of the operands' type, for products of many tokens: 8 or 16 neighbours of a row a thread, 4 rows.
 // Bound by the store of 2 bytes a weight, where scales are of that type too (one rounding, of an exact product, a pair).
+// The rounding is to the operands' precision: the tensor cores take nothing finer of that type.  Its range is bf16's, which
+// is the scales' own; in fp16 weights would leave it from scales of 4367 on and lose bits below 6e-5, so that there a row
+// is divided by a power of two that brings its largest scale to [2^10, 2^11) (times 15: below 2^15), and the product's
+// columns are multiplied by it in fp32.  What a row's small groups lose to fp16's smallest step is 2^-31 of its largest scale.
 struct ExpandParams {
   const char *w, *scale;
   const uint8_t* zero;
   void* to;
   int64_t w_rs, s_rs, s_cs, z_rs, z_cs, to_rs, N, K;
+  const float* power;  // [N], of fp16 weights
   int scale_dtype, group_shift;  // 1 << group_shift words a group
 };
 template <typename T>
@@ -526,10 +531,29 @@ __device__ __forceinline__ uint32_t times2<__half>(uint32_t a, uint32_t b) {
   return *reinterpret_cast<const uint32_t*>(&v);
 }
 constexpr int kExpandRows = 4;
+// The power of two of each row, a warp a row.  Scales that are not finite are not looked at: their weights stay so.  (From
+// 2^-100 on both it and its inverse are normal numbers; smaller scales give results that round to 0.)
+__global__ void __launch_bounds__(256) cconv_int4_row_powers_kernel(const char* scale, int scale_dtype, int64_t s_rs, int64_t s_cs,
+                                                                    int64_t N, int groups, float* power) {
+  start_in_order();
+  const int lane = threadIdx.x & 31;
+  for (int64_t n = int64_t(blockIdx.x) * 8 + (threadIdx.x >> 5); n < N; n += int64_t(gridDim.x) * 8) {
+    uint32_t most = 0;
+    for (int i = lane; i < groups; i += 32) {
+      const uint32_t size = __float_as_uint(scale_of(load_scale(scale, scale_dtype, n * s_rs + i * s_cs), scale_dtype)) & 0x7fffffffu;
+      if (size < 0x7f800000u) most = max(most, size);
+    }
+    most = __reduce_max_sync(0xffffffffu, most);
+    const int e = most ? max(ilogbf(__uint_as_float(most)) - 10, -100) : 0;
+    if (lane == 0) power[n] = __uint_as_float(uint32_t(127 + e) << 23);
+  }
+}
+__device__ __forceinline__ float inverse_of_power(float v) { return __uint_as_float((254u << 23) - __float_as_uint(v)); }
 // kWords neighbouring words a thread (2 where that keeps to multiples of 32 bytes, which go in one store); kSame: scales
 // are of the type T.
 template <typename T, int kWords, bool kSame>
 __global__ void __launch_bounds__(256, 4) cconv_int4_expand_kernel(const ExpandParams p) {
+  constexpr bool kPowers = std::is_same<T, __half>::value;
   start_in_order();
   const uint32_t words = uint32_t((p.K + 7) / 8), i = (blockIdx.x * 256 + threadIdx.x) * kWords;
   if (i >= words) return;
@@ -544,6 +568,7 @@ __global__ void __launch_bounds__(256, 4) cconv_int4_expand_kernel(const ExpandP
     char* to = static_cast<char*>(p.to) + n0 * to_step + i * 16;
     Words<kWords> v[kExpandRows];
     uint32_t s[kExpandRows], z[kExpandRows];
+    float power[kExpandRows];
 #pragma unroll
     for (int r = 0; r < kExpandRows; ++r, w_at += p.w_rs, s_at += scale_step, z_at += p.z_rs) {
       z[r] = 8;
@@ -552,10 +577,13 @@ __global__ void __launch_bounds__(256, 4) cconv_int4_expand_kernel(const ExpandP
       if (es == 2) s[r] = __ldg(reinterpret_cast<const uint16_t*>(s_at));
       else s[r] = __ldg(reinterpret_cast<const uint32_t*>(s_at));
       if (p.zero) z[r] = __ldg(z_at) & 15u;
+      if (kPowers) power[r] = __ldg(p.power + n0 + r);
     }
 #pragma unroll
     for (int r = 0; r < kExpandRows; ++r, to += to_step) {
       if (r >= rows) break;
+      const float times = kPowers ? inverse_of_power(power[r]) : 1.0f;
+      if (kPowers && kSame) s[r] = __half_as_ushort(__float2half_rn(scale_of(s[r], CCONV_TYPE_FP16) * times));
       uint32_t w[kWords][4];
 #pragma unroll
       for (int k = 0; k < kWords; ++k) {
@@ -565,7 +593,7 @@ __global__ void __launch_bounds__(256, 4) cconv_int4_expand_kernel(const ExpandP
           if constexpr (kSame) {
             w[k][j] = times2<T>(w[k][j], s[r] * 0x10001u);
           } else {
-            const float by = scale_of(s[r], p.scale_dtype);
+            const float by = scale_of(s[r], p.scale_dtype) * times;
             const float2 f = unpack2<T>(w[k][j]);
             w[k][j] = pack2<T>(by * f.x, by * f.y);
           }
@@ -705,6 +733,16 @@ void plan(Steps& st, const cconv_int4_product_args& a) {
   p.scale_dtype = a.scale_dtype;
   p.group_shift = group == 32 ? 2 : group == 64 ? 3 : 4;
   const bool two = K % 16 == 0 && (at & 7) == 0;
+  Mat powers;
+  if (dtype == CCONV_TYPE_FP16) {
+    powers = st.scratch(1, round_up64(N, 256), 4);
+    p.power = static_cast<const float*>(powers.p);
+    st.add([=](cudaStream_t s) {
+      const dim3 grid(unsigned(std::min<int64_t>(cdiv64(N, 8), 65535)));
+      return block_cuda_error(launch(cconv_int4_row_powers_kernel, grid, 256, 0, 1, s, p.scale, p.scale_dtype, p.s_rs, p.s_cs, N,
+                                     int(cdiv64(K, group)), const_cast<float*>(p.power)), "cconv_int4_row_powers_kernel");
+    });
+  }
   st.add([=](cudaStream_t s) {
     const dim3 grid(unsigned(cdiv64(K, two ? 4096 : 2048)), unsigned(std::min<int64_t>(cdiv64(N, kExpandRows), 65535)));
     auto go = [&](auto f) { return block_cuda_error(launch(f, grid, 256, 0, 1, s, p), "cconv_int4_expand_kernel"); };
@@ -716,7 +754,8 @@ void plan(Steps& st, const cconv_int4_product_args& a) {
     return dtype == CCONV_TYPE_BF16 ? of(__nv_bfloat16()) : of(__half());
   });
   Launch l;
-  l.epilogue = kStore;
+  l.epilogue = dtype == CCONV_TYPE_FP16 ? kColumns : kStore;
+  l.col_scale = powers;
   l.dtype = dtype;
   l.of[0].M = M;
   l.of[0].N = N;
