@@ -288,11 +288,10 @@ __device__ __forceinline__ void write8(char* base, int64_t rs, int64_t cs, int64
       if (i < n) to[i * cs] = from_f32<T>(f[i]);
   }
 }
-// Columns' sums times their factors (the same in every lane).
-template <int N>
-__device__ __forceinline__ void scale_columns(float (&f)[N], const float* by) {
+// Eight columns' sums times their factors (the same in every lane).
+__device__ __forceinline__ void scale_columns(float (&f)[8], const float* by) {
 #pragma unroll
-  for (int i = 0; i < N; i += 4) {
+  for (int i = 0; i < 8; i += 4) {
     const float4 v = __ldg(reinterpret_cast<const float4*>(by + i));
     f[i] *= v.x, f[i + 1] *= v.y, f[i + 2] *= v.z, f[i + 3] *= v.w;
   }
@@ -579,8 +578,15 @@ __global__ void __launch_bounds__(kThreads, 1) cconv_pair_product_kernel(
         }
       }
       if constexpr (kEpi == kStore || kEpi == kColumns) {
-        if (!wait_sums()) break;
         const int cols = o.block_n >> 1;
+        float by[4] = {};  // kColumns: a lane's of each 32 columns, here before the sums are
+        if constexpr (kEpi == kColumns) {
+          const float* from = p.col_scale + tl.n * int64_t(o.block_n) + (cols < 64 ? 0 : half * cols) + lane;
+#pragma unroll
+          for (int j = 0; j < 4; ++j)
+            if (j * 32 < max(cols, 64)) by[j] = __ldg(from + j * 32);
+        }
+        if (!wait_sums()) break;
         for (int c = 0; c < cols; c += 64) {
           const bool narrow = cols < 64;  // 64 columns a tile: one half of the warps takes them all
           if (narrow && half) {
@@ -593,9 +599,12 @@ __global__ void __launch_bounds__(kThreads, 1) cconv_pair_product_kernel(
           load_sums(acc + at + 32, g);
           if (c + 64 >= cols) release_sums();
           if constexpr (kEpi == kColumns) {
-            const float* by = p.col_scale + tl.n * int64_t(o.block_n) + at;
-            scale_columns(f, by);
-            scale_columns(g, by + 32);
+            const float by_f = c == 0 ? by[0] : by[2], by_g = c == 0 ? by[1] : by[3];
+#pragma unroll
+            for (int i = 0; i < 32; ++i) {
+              f[i] *= __shfl_sync(0xffffffffu, by_f, i);
+              g[i] *= __shfl_sync(0xffffffffu, by_g, i);
+            }
           }
           const uint32_t to = mine + piece * kBoxBytes;
           if (lane == 0) bulk_wait_group_read<1>();

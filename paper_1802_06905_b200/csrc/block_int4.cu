@@ -515,7 +515,8 @@ struct ExpandParams {
   const uint8_t* zero;
   void* to;
   int64_t w_rs, s_rs, s_cs, z_rs, z_cs, to_rs, N, K;
-  const float* power;  // [N], of fp16 weights
+  float* power;  // [N], written: of fp16 weights
+  int groups;
   int scale_dtype, group_shift;  // 1 << group_shift words a group
 };
 template <typename T>
@@ -531,22 +532,17 @@ __device__ __forceinline__ uint32_t times2<__half>(uint32_t a, uint32_t b) {
   return *reinterpret_cast<const uint32_t*>(&v);
 }
 constexpr int kExpandRows = 4;
-// The power of two of each row, a warp a row.  Scales that are not finite are not looked at: their weights stay so.  (From
-// 2^-100 on both it and its inverse are normal numbers; smaller scales give results that round to 0.)
-__global__ void __launch_bounds__(256) cconv_int4_row_powers_kernel(const char* scale, int scale_dtype, int64_t s_rs, int64_t s_cs,
-                                                                    int64_t N, int groups, float* power) {
-  start_in_order();
-  const int lane = threadIdx.x & 31;
-  for (int64_t n = int64_t(blockIdx.x) * 8 + (threadIdx.x >> 5); n < N; n += int64_t(gridDim.x) * 8) {
-    uint32_t most = 0;
-    for (int i = lane; i < groups; i += 32) {
-      const uint32_t size = __float_as_uint(scale_of(load_scale(scale, scale_dtype, n * s_rs + i * s_cs), scale_dtype)) & 0x7fffffffu;
-      if (size < 0x7f800000u) most = max(most, size);
-    }
-    most = __reduce_max_sync(0xffffffffu, most);
-    const int e = most ? max(ilogbf(__uint_as_float(most)) - 10, -100) : 0;
-    if (lane == 0) power[n] = __uint_as_float(uint32_t(127 + e) << 23);
+// A row's power of two, by a warp.  Scales that are not finite are not looked at: their weights stay so.  (From 2^-100 on
+// both it and its inverse are normal numbers; smaller scales give results that round to 0.)
+__device__ __forceinline__ float power_of_row(const char* scale, int scale_dtype, int64_t s_cs, int groups) {
+  uint32_t most = 0;
+  for (int i = threadIdx.x & 31; i < groups; i += 32) {
+    const uint32_t size = __float_as_uint(scale_of(load_scale(scale, scale_dtype, i * s_cs), scale_dtype)) & 0x7fffffffu;
+    if (size < 0x7f800000u) most = max(most, size);
   }
+  most = __reduce_max_sync(0xffffffffu, most);
+  const int e = most ? max(ilogbf(__uint_as_float(most)) - 10, -100) : 0;
+  return __uint_as_float(uint32_t(127 + e) << 23);
 }
 __device__ __forceinline__ float inverse_of_power(float v) { return __uint_as_float((254u << 23) - __float_as_uint(v)); }
 // kWords neighbouring words a thread (2 where that keeps to multiples of 32 bytes, which go in one store); kSame: scales
@@ -554,9 +550,12 @@ __device__ __forceinline__ float inverse_of_power(float v) { return __uint_as_fl
 template <typename T, int kWords, bool kSame>
 __global__ void __launch_bounds__(256, 4) cconv_int4_expand_kernel(const ExpandParams p) {
   constexpr bool kPowers = std::is_same<T, __half>::value;
+  __shared__ float inverse[2][kExpandRows];
   start_in_order();
   const uint32_t words = uint32_t((p.K + 7) / 8), i = (blockIdx.x * 256 + threadIdx.x) * kWords;
-  if (i >= words) return;
+  const bool inside = i < words;
+  if (!kPowers && !inside) return;
+  int turn = 0;
   const int64_t grp = i >> p.group_shift;
   const int es = kSame || p.scale_dtype != CCONV_TYPE_FP32 ? 2 : 4;
   const int64_t scale_step = p.s_rs * es, to_step = p.to_rs * int64_t(sizeof(T));
@@ -568,21 +567,30 @@ __global__ void __launch_bounds__(256, 4) cconv_int4_expand_kernel(const ExpandP
     char* to = static_cast<char*>(p.to) + n0 * to_step + i * 16;
     Words<kWords> v[kExpandRows];
     uint32_t s[kExpandRows], z[kExpandRows];
-    float power[kExpandRows];
 #pragma unroll
     for (int r = 0; r < kExpandRows; ++r, w_at += p.w_rs, s_at += scale_step, z_at += p.z_rs) {
       z[r] = 8;
-      if (r >= rows) break;
+      if (r >= rows || !inside) break;
       v[r].load(w_at);
       if (es == 2) s[r] = __ldg(reinterpret_cast<const uint16_t*>(s_at));
       else s[r] = __ldg(reinterpret_cast<const uint32_t*>(s_at));
       if (p.zero) z[r] = __ldg(z_at) & 15u;
-      if (kPowers) power[r] = __ldg(p.power + n0 + r);
+    }
+    if constexpr (kPowers) {
+      const int warp = threadIdx.x >> 5;
+      if (warp < rows) {  // (warps 0 to 3)
+        const float power = power_of_row(p.scale + (n0 + warp) * scale_step, p.scale_dtype, p.s_cs, p.groups);
+        if ((threadIdx.x & 31) == 0) {
+          inverse[turn][warp] = inverse_of_power(power);
+          if (blockIdx.x == 0) p.power[n0 + warp] = power;
+        }
+      }
+      __syncthreads();  // (the next rows' go to the other half, which all have read by the barrier after)
     }
 #pragma unroll
     for (int r = 0; r < kExpandRows; ++r, to += to_step) {
-      if (r >= rows) break;
-      const float times = kPowers ? inverse_of_power(power[r]) : 1.0f;
+      if (r >= rows || !inside) break;
+      const float times = kPowers ? inverse[turn][r] : 1.0f;
       if (kPowers && kSame) s[r] = __half_as_ushort(__float2half_rn(scale_of(s[r], CCONV_TYPE_FP16) * times));
       uint32_t w[kWords][4];
 #pragma unroll
@@ -602,6 +610,7 @@ __global__ void __launch_bounds__(256, 4) cconv_int4_expand_kernel(const ExpandP
       if constexpr (kWords == 2) st_global_v8(to, w[0][0], w[0][1], w[0][2], w[0][3], w[1][0], w[1][1], w[1][2], w[1][3]);
       else *reinterpret_cast<uint4*>(to) = make_uint4(w[0][0], w[0][1], w[0][2], w[0][3]);
     }
+    turn ^= 1;
   }
 }
 
@@ -731,17 +740,13 @@ void plan(Steps& st, const cconv_int4_product_args& a) {
   p.N = N;
   p.K = K;
   p.scale_dtype = a.scale_dtype;
+  p.groups = int(cdiv64(K, group));
   p.group_shift = group == 32 ? 2 : group == 64 ? 3 : 4;
   const bool two = K % 16 == 0 && (at & 7) == 0;
   Mat powers;
   if (dtype == CCONV_TYPE_FP16) {
     powers = st.scratch(1, round_up64(N, 256), 4);
-    p.power = static_cast<const float*>(powers.p);
-    st.add([=](cudaStream_t s) {
-      const dim3 grid(unsigned(std::min<int64_t>(cdiv64(N, 8), 65535)));
-      return block_cuda_error(launch(cconv_int4_row_powers_kernel, grid, 256, 0, 1, s, p.scale, p.scale_dtype, p.s_rs, p.s_cs, N,
-                                     int(cdiv64(K, group)), const_cast<float*>(p.power)), "cconv_int4_row_powers_kernel");
-    });
+    p.power = static_cast<float*>(const_cast<void*>(powers.p));
   }
   st.add([=](cudaStream_t s) {
     const dim3 grid(unsigned(cdiv64(K, two ? 4096 : 2048)), unsigned(std::min<int64_t>(cdiv64(N, kExpandRows), 65535)));

@@ -102,3 +102,9 @@ def test_int4_in_fp16_into_strided_results():
         assert (big == 7.0).all()
         wide = poisoned((N, M), FP16)
         check_fp16(c, c.run(out=wide.t()), "transposed")
+
+
+def test_int4_in_fp16_with_more_rows_than_a_launch_has_blocks():
+    c = Int4(66, 4 * 65535 + 90, 48, 32, FP16, FP32, zero=True)
+    c.scale = (c.scale.double() * 10.0 ** (torch.arange(c.N, device="cuda", dtype=torch.float64) % 9 - 5)[:, None]).to(FP32)
+    check_fp16(c, c.run(), "many rows")
