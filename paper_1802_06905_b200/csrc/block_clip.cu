@@ -3,7 +3,8 @@
 //   norm = sqrt(sum of squares),  factor = min(1, max_norm / (norm + eps)),  out = factor gradient
 //
 // Two passes, since the factor needs every element: the first reads and leaves a partial sum a block, the
-// second adds those up (every block for itself, in a fixed order), reads again and writes.  Both are bound by HBM.  The
+// second adds those up (every block of its first launch for itself, in a fixed order; where tensors are so many that
+// there are more launches, those read the norm that the first has left), reads again and writes.  Both are bound by HBM.  The
 // second goes through each block's share backwards, so that what the first read last comes out of L2.
 // Where nothing is to be done in place (factor 1) the second pass ends after the sums.
 //
@@ -38,10 +39,10 @@ struct Table {
 };
 struct ClipParams {
   double* sums;    // partial sums of squares
-  int blocks;      // of them; 0: the norm is given
+  int blocks;      // of them; 0: the norm is there already
   float* norm;
   float max_norm, eps;
-  int in_place, first_launch;
+  int in_place;
 };
 
 __device__ __forceinline__ double block_sum(double v) {
@@ -236,7 +237,7 @@ template <int N, int kVectors>
 __global__ void __launch_bounds__(kThreads, kBlocksAnSm) cconv_clip_kernel(const __grid_constant__ Table<N> t, const ClipParams c) {
   start_in_order();
   const float norm = c.blocks ? norm_of(c.sums, c.blocks) : *c.norm;
-  if (c.blocks && c.first_launch && blockIdx.x == 0 && threadIdx.x == 0) *c.norm = norm;
+  if (c.blocks && blockIdx.x == 0 && threadIdx.x == 0) *c.norm = norm;
   const float ratio = __fdiv_rn(c.max_norm, norm + c.eps);
   const float by = ratio >= 1.0f ? 1.0f : ratio;  // (NaN stays)
   if (by == 1.0f && c.in_place) return;
@@ -351,14 +352,13 @@ int run_norm_of_sums(const cconv_clip_args& a, int sums, cudaStream_t s) {
 int run_clip(const cconv_clip_args& a, int sms, int sums, cudaStream_t s) {
   ClipParams c{};
   c.sums = static_cast<double*>(a.workspace);
-  c.blocks = a.norm_given ? 0 : sums;
   c.norm = static_cast<float*>(a.norm);
   c.max_norm = a.max_norm;
   c.eps = a.eps;
   c.in_place = a.outs == nullptr;
   const int vectors = vectors_of(a, sms);
   return with_tables(a, vectors, [&](const auto& t, int number) {
-    c.first_launch = number == 0;
+    c.blocks = a.norm_given || number > 0 ? 0 : sums;
     const int n = blocks_of(t.pieces, sms);
     constexpr int kItems = sizeof(t) == sizeof(Table<kFewItems>) ? kFewItems : kMostItems;
     auto go = [&](auto f) { return launch(f, dim3(unsigned(n)), kThreads, 0, 1, s, t, c); };
