@@ -587,8 +587,9 @@ struct Down {
   static constexpr int kUnitBytes = kFirst * 128 + kNt * 2048, kTokens = 8 * kNt;
   static int ring(int stages) { return kWarps * stages * kUnitBytes; }
 };
-// What the blocks of a cluster send one of them of a tile, in multiples of 8 bytes.
-constexpr __host__ __device__ int box_bytes(int T, int parts) { return ((T * 16 + parts - 1) / parts * parts + 1) / 2 * 8; }
+// What the blocks of a cluster send one of them of a tile, in multiples of 8 bytes.  (A tile that is shared is its
+// cluster's only one: parts of 2 and more are chosen where the device has a cluster for each tile.)
+constexpr __host__ __device__ int box_bytes(int T, int parts) { return parts == 1 ? 0 : ((T * 16 + parts - 1) / parts * parts + 1) / 2 * 8; }
 template <typename T, int kNt, int kStages, bool kOdd>
 __global__ void __launch_bounds__(kWarps * 32, 2) cconv_moe_down_kernel(const MoeParams p, const int parts) {
   using S = Down<T, kNt, kOdd>;
@@ -605,7 +606,7 @@ __global__ void __launch_bounds__(kWarps * 32, 2) cconv_moe_down_kernel(const Mo
 
   // Behind the gate and up kernel of the same call, which lets this one in only once everything before the call and the
   // router are complete, the choice and the weights are there already; h is waited for below.
-  const Routes r = routes_of<true>(p, smem + kWarps * (kStages * S::kUnitBytes + p.T * 64) + 2 * box_bytes(p.T, parts), scratch, S::kTokens);
+  const Routes r = routes_of<true>(p, smem + kWarps * (kStages * S::kUnitBytes + p.T * 64) + box_bytes(p.T, parts), scratch, S::kTokens);
   const int64_t work = int64_t(r.groups) * units;
   const int64_t w0 = work * (rank * kWarps + warp) / (parts * kWarps), w1 = work * (rank * kWarps + warp + 1) / (parts * kWarps);
   const int each = int(w1 - w0), group0 = units ? int(w0 / units) : 0, unit0 = int(w0 - int64_t(group0) * units);
@@ -681,7 +682,7 @@ __global__ void __launch_bounds__(kWarps * 32, 2) cconv_moe_down_kernel(const Mo
   fill(load_tokens, [] { commit_copies(); });  // (the first takes in the weights of all stages)
   if (parts > 1) cluster_wait();  // every block of the cluster is there
   const int outputs = p.T * 16, share = (outputs + parts - 1) / parts;
-  float *const boxes = all + kWarps * outputs, *box = boxes;  // [2][parts][share]
+  float* const box = all + kWarps * outputs;  // [parts][share]
   auto put_out = [&](int tile, int i, float v) {
     const int64_t channel = int64_t(tile) * 16 + (i & 15);
     if (channel < p.D) static_cast<T*>(const_cast<void*>(p.out.p))[(i >> 4) * p.out.rs + channel * p.out.cs] = from_f32<T>(v);
@@ -755,14 +756,12 @@ __global__ void __launch_bounds__(kWarps * 32, 2) cconv_moe_down_kernel(const Mo
       __syncthreads();
       continue;
     }
-    // (one meeting a tile: what is sent for the next but one comes after the next tile's, and so after these are read)
     cluster_sync_all();
     for (int i = threadIdx.x * parts + rank; i < outputs; i += parts * kWarps * 32) {
       float s = 0.0f;
       for (int b = 0; b < parts; ++b) s += box[b * share + i / parts];
       put_out(tile, i, s);
     }
-    box = box == boxes ? boxes + parts * share : boxes;
   }
 }
 
@@ -823,9 +822,9 @@ cudaError_t launch_down_odd(const MoeParams& p, int sms, cudaStream_t s) {
   // blocks that share a tile, so that every SM has two
   const int64_t tiles = cdiv64(p.D, 16);
   const int parts = tiles * 2 > 2 * sms ? 1 : tiles * 4 > 2 * sms ? 2 : tiles * 8 > 2 * sms ? 4 : 8;
-  const int64_t clusters = std::min<int64_t>(tiles, 2 * sms / parts);
-  return launch(f, dim3(unsigned(clusters * parts)), kWarps * 32,
-                S::ring(kStages) + kWarps * p.T * 64 + 2 * box_bytes(p.T, parts) + routes_bytes(p.E, p.T * p.k, S::kTokens, true), parts, s, p, parts);
+  const int64_t blocks = parts == 1 ? std::min<int64_t>(tiles, 2 * sms) : tiles * parts;
+  return launch(f, dim3(unsigned(blocks)), kWarps * 32,
+                S::ring(kStages) + kWarps * p.T * 64 + box_bytes(p.T, parts) + routes_bytes(p.E, p.T * p.k, S::kTokens, true), parts, s, p, parts);
 }
 template <typename T, int kNt, int kStages>
 cudaError_t launch_down_as(const MoeParams& p, int sms, cudaStream_t s) {
