@@ -8,9 +8,10 @@ type's normal range half of its smallest step.
 import pytest
 import torch
 
+import test_gpu_block_serve as serve
 from paper_1802_06905_b200 import block
 from test_gpu_block import BF16, FP16, FP32, TINY, U, close, gen, normal, poisoned, sum_err
-from test_gpu_block_serve import Int4
+from test_gpu_block_serve import Int4, Moe
 
 pytestmark = pytest.mark.gpu
 
@@ -108,3 +109,187 @@ def test_int4_in_fp16_with_more_rows_than_a_launch_has_blocks():
     c = Int4(66, 4 * 65535 + 90, 48, 32, FP16, FP32, zero=True)
     c.scale = (c.scale.double() * 10.0 ** (torch.arange(c.N, device="cuda", dtype=torch.float64) % 9 - 5)[:, None]).to(FP32)
     check_fp16(c, c.run(), "many rows")
+
+
+# ---- 4-bit products known to the last bit ------------------------------------------------------------
+
+def integers(g, low, high, shape, dtype):
+    return torch.randint(low, high + 1, shape, generator=g, device="cuda").to(dtype)
+
+
+def exact_int4(M, N, K, group, dtype, scale, zero):
+    """Tokens of whole numbers up to 3 and scales that are powers of two from 1/8 to 1: in units of 1/8, sums of (q - z) s x
+    are whole numbers below 45 8 K (K up to 16416: 2^22.5), and a group's of (16 + q) x below 2^14, so that fp32 holds each
+    without rounding in whatever order they are added up; and weights are numbers of 4 bits and a sign."""
+    c = Int4(M, N, K, group, dtype, scale, zero)
+    g = gen(M + N + K + group)
+    c.x = integers(g, -3, 3, (M, K), dtype)
+    c.scale = (2.0 ** -integers(g, 0, 3, c.scale.shape, FP32)).to(scale)
+    return c
+
+
+# own tokens: one tile a block and several (more than 296 tiles of 16 or 32 rows), rows that begin at multiples of 16, 8 and 4
+# bytes; 3 to 8 tokens shared; every number of token tiles; few and many units for a cluster; expanded
+EXACT = [(1, 20011, 256), (2, 20011, 264), (1, 20011, 272), (2, 9500, 1040), (1, 20011, 4096), (8, 12000, 128), (1, 300, 8192), (2, 77, 16416),
+         (3, 300, 4096), (7, 4096, 4096), (8, 5000, 5120), (4, 129, 8192), (5, 40, 16416), (3, 1000, 5130), (6, 2000, 2056),
+         (9, 700, 4096), (16, 1000, 5120), (17, 129, 8192), (23, 5000, 4200), (31, 64, 1024), (40, 129, 16416), (48, 700, 4100), (64, 31, 16416),
+         (64, 1030, 2048), (65, 130, 4096), (300, 513, 1000), (2060, 300, 264)]
+
+
+@pytest.mark.parametrize("M,N,K", EXACT)
+@pytest.mark.parametrize("dtype", [BF16, FP16])
+def test_int4_products_of_whole_numbers(M, N, K, dtype):
+    for group in (32, 64, 128):
+        for scale, zero in ((dtype, False), (FP32, True)):
+            c = exact_int4(M, N, K, group, dtype, scale, zero)
+            out = c.run()
+            q, z, s = c.weights()
+            exact = c.x.double() @ (s * (q - z)).T
+            assert torch.equal(out, exact.to(FP32).to(dtype)), (group, scale, zero)
+    assert block.status() == (0, 0)
+
+
+@pytest.mark.parametrize("M,N,K", [(1, 1000, 8192), (2, 20011, 1024), (5, 1000, 5120), (8, 300, 4096), (23, 1000, 4200), (64, 100, 16416),
+                                   (65, 1000, 4096), (400, 300, 4096), (1, 100, 60000), (2, 64, 40000), (8, 64, 60000)])
+@pytest.mark.parametrize("dtype", [BF16, FP16])
+def test_int4_errors_are_the_result_s_rounding(M, N, K, dtype):
+    """Of random operands, relative to the result's norm: a result rounded once is off by r, the sums' errors are far below
+    it (K 2^-24 of their terms' root sum of squares at worst, which 16 + q makes five times as large: 2^-8 r in fp16 at
+    K = 4096) and add a tenth at most; with more than 64 tokens each weight is rounded as well, by the same share: r sqrt 2."""
+    for group, zero in ((32, True), (128, False)):
+        c = Int4(M, N, K, group, dtype, None, zero)
+        out = c.run().double()
+        q, z, s = c.weights()
+        exact = c.x.double() @ (s * (q - z)).T
+        rounding = (exact.to(dtype).double() - exact).norm()
+        assert (out - exact).norm() <= (1.1 if M <= 64 else 1.55) * rounding
+
+
+# ---- mixtures known to the last bit ----------------------------------------------------------------------
+
+def exact_moe(T, D, F, E, k, dtype):
+    """Whole numbers as tokens (up to 2) and as weights of gate and up (up to 1), sixteenths as weights of down, relu, and
+    powers of two from 1/4 to 1 as the choices' weights: h is a whole number, of more bits than the type has, but for
+    |h| <= 65504 no more than two numbers of it hold; everything else is a whole number in units of 1/64."""
+    m = Moe(T, D, F, E, k, dtype, "relu")
+    g = gen(T + D + F + E)
+    m.x = integers(g, -2, 2, (T, D), dtype)
+    thin = min(1.0, 700.0 / D)  # (the share of weights that are not zeros, which keeps h in range)
+    keep = lambda t: t * (torch.rand(t.shape, generator=g, device="cuda") < thin)  # noqa: E731
+    m.wg, m.wu = (keep(integers(g, -1, 1, (E, F, D), dtype)) for _ in range(2))
+    m.wd = integers(g, -1, 1, (E, D, F), dtype) / 16
+    ids = torch.stack([torch.randperm(E, generator=g, device="cuda")[:k] for _ in range(T)]).to(torch.int32)
+    weights = 2.0 ** -integers(g, 0, 2, (T, k), FP32) * integers(g, 0, 1, (T, k), FP32).mul_(2).sub_(1)
+    return m, ids, weights
+
+
+def exact_moe_result(m, ids, weights):
+    x = m.x.double()
+    y, size, h_most, h_bits = torch.zeros((m.T, m.D), device="cuda", dtype=torch.float64), 0, 0, False
+    for e in range(m.E):
+        w = (weights.double() * (ids == e)).sum(1, keepdim=True)
+        h = (x @ m.wg[e].double().T).clamp(min=0) * (x @ m.wu[e].double().T)
+        h_most = max(h_most, h.abs().max().item())
+        h_bits |= bool((h.to(m.dtype).double() != h).any())
+        y += w * (h @ m.wd[e].double().T)
+        size = size + w.abs() * (h.abs() @ m.wd[e].double().abs().T)
+    assert h_most <= 65504 and size.max().item() * 64 < 2 ** 24  # nothing on the way is rounded
+    return y, h_bits
+
+
+# every number of columns and of warps a team, tiles shared by 8, 4, 2 and 1 blocks, rows that begin at multiples of 16 and of 2
+# bytes, lists of up to 32 pairs and of more, several launches
+EXACT_MOE = [(1, 2048, 1024, 64, 8), (5, 1000, 1304, 10, 3), (32, 2048, 256, 32, 4), (33, 1024, 136, 4, 2), (40, 1001, 66, 4, 3), (64, 4096, 72, 8, 2),
+             (20, 2400, 64, 2, 2), (20, 2401, 63, 2, 2), (33, 1300, 136, 4, 2), (33, 1301, 65, 4, 2), (40, 200, 33, 3, 2), (64, 700, 200, 8, 2),
+             (16, 2500, 96, 40, 6), (64, 904, 264, 128, 4), (9, 4801, 40, 16, 2), (130, 1000, 200, 4, 2), (70, 1001, 65, 4, 2), (64, 8, 8, 1, 1),
+             (17, 1, 1, 2, 2), (4, 2047, 1023, 8, 2), (64, 1500, 1100, 2, 1), (12, 800, 2048, 64, 8),
+             (64, 64, 16, 1024, 32), (64, 65, 17, 300, 32), (64, 2401, 9, 300, 32)]
+
+
+@pytest.mark.parametrize("T,D,F,E,k", EXACT_MOE)
+@pytest.mark.parametrize("dtype", [BF16, FP16])
+def test_moe_of_whole_numbers(T, D, F, E, k, dtype):
+    m, ids, weights = exact_moe(T, D, F, E, k, dtype)
+    out = m.run(ids=ids, weights=weights)[0]
+    y, h_bits = exact_moe_result(m, ids, weights)
+    assert torch.equal(out, y.to(FP32).to(dtype))
+    # the second part of h counts (fp16 holds whole numbers up to 2048 in one)
+    assert h_bits or D < 500 or dtype is FP16
+
+
+@pytest.mark.parametrize("T,D,F,E,k", [(9, 1000, 64, 4, 2), (40, 1024, 72, 4, 2), (33, 136, 2000, 5, 2)])
+def test_moe_of_whole_numbers_whose_elements_lie_apart(T, D, F, E, k):
+    m, ids, weights = exact_moe(T, D, F, E, k, BF16)
+    y, _ = exact_moe_result(m, ids, weights)
+    for names in (("wg",), ("wu",), ("wd",), ("wg", "wu", "wd")):
+        h, _, _ = exact_moe(T, D, F, E, k, BF16)
+        for name in names:
+            setattr(h, name, getattr(m, name).transpose(1, 2).contiguous().transpose(1, 2))
+        assert torch.equal(h.run(ids=ids, weights=weights)[0], y.to(FP32).to(BF16)), names
+
+
+@pytest.mark.parametrize("T,D,F,E,k", [(1, 2048, 1024, 64, 8), (5, 1000, 1304, 10, 3), (64, 1024, 512, 8, 2), (40, 1001, 333, 4, 3)])
+@pytest.mark.parametrize("dtype", [BF16, FP16])
+def test_moe_errors_are_the_result_s_rounding(T, D, F, E, k, dtype):
+    """Of random operands, relative to the result's norm: h in two parts, the activation (2e-6) and the sums are all some
+    hundred times more exact than the result's rounding in bf16 and some ten times in fp16, and add a tenth at most."""
+    m = Moe(T, D, F, E, k, dtype)
+    out, ids, weights = m.run()
+    m.check_routes(ids, weights)
+    x, y = m.x.double(), torch.zeros((T, D), device="cuda", dtype=torch.float64)
+    for e in range(E):
+        w = (weights.double() * (ids == e)).sum(1, keepdim=True)
+        g = x @ m.wg[e].double().T
+        y += w * ((g * torch.sigmoid(g) * (x @ m.wu[e].double().T)) @ m.wd[e].double().T)
+    assert (out.double() - y).norm() <= 1.1 * (y.to(dtype).double() - y).norm()
+
+
+# ---- norms in 8 bits: a case for each kernel that many rows choose ------------------------------------------
+
+# (rows for each block of 64, 128, 192, 256, 384 and 512 threads, of 8, 12 and 16 elements a thread)
+NARROW = [(9600, 65), (9600, 333), (9500, 511), (4800, 1001), (3000, 1501), (2400, 2047), (1200, 2501), (1300, 4001), (1250, 4095), (700, 5001),
+          (650, 7001)]
+# every operand there, rows that do not fill a block; 1 and 2 accesses a thread (fp32: up to 4)
+RAGGED = [(4802, 1016), (1000, 2056), (1204, 5376), (1207, 5376)]
+
+
+@pytest.mark.parametrize("T,D", NARROW + RAGGED)
+@pytest.mark.parametrize("dtype", [BF16, FP16, FP32])
+def test_norm_in_8_bits_of_many_rows(T, D, dtype):
+    serve.test_norm_in_8_bits(T, D, dtype)
+
+
+@pytest.mark.parametrize("T,D", NARROW[1:] + RAGGED)  # (its elements lie in the first two blocks of 128)
+def test_norm_in_8_bits_of_many_rows_with_zeros_infinities_and_nan(T, D):
+    serve.test_norm_in_8_bits_of_zeros_infinities_and_nan(T, D)
+
+
+@pytest.mark.parametrize("T,D", NARROW)
+@pytest.mark.parametrize("dtype", [BF16, FP32])
+def test_norm_in_8_bits_of_many_rows_in_place_and_strided(T, D, dtype):
+    serve.test_norm_in_8_bits_in_place_and_strided(T, D, dtype)
+
+
+@pytest.mark.parametrize("T,D", NARROW + RAGGED)
+@pytest.mark.parametrize("dtype", [BF16, FP16])
+def test_norm_in_8_bits_values_are_the_nearest(T, D, dtype):
+    """Against x / scale in 64 bits, with every operand there: the nearest e4m3 value, but where x / scale lies within its own
+    error of the middle between two.
+
+    That error: a sum of squares has at most 16 terms a thread and ten additions in a tree, 27 roundings of 2^-24, which the
+    root halves; with the mean, eps and the root itself rho is within 2^-19 of itself.  n = y rho w_post gate is so within
+    (2^-19 + 3 2^-24) |n|, r' = base + n within that and 2^-23 |base| + 2^-24 |r'|, however little of them is left in
+    r'; x = r' rho w_pre adds (2^-19 + 2 2^-24) |x|, the quotient 2^-23: together less than 2^-18 |x| (1 + (|base| + |n|) / |r'|)."""
+    n = serve.Norm(T, D, dtype, gate=max(1, T // 3))
+    out, q, s = n.run()
+    r, _, x, _ = n.exact()
+    base = n.scale * n.resid.double()
+    v = (x / s.double().repeat_interleave(128, 1)[:, :D].clamp(min=1e-300)).clamp(-448, 448)
+    parts = (base.abs() + (r - base).abs()) / r.abs().clamp(min=1e-300)
+    m, e = torch.frexp(v)
+    step = torch.ldexp(torch.ones_like(v), (e - 4).clamp(min=-9))
+    nearest = torch.round(v / step) * step
+    middle = ((v / step).abs() % 1 - 0.5).abs() * step  # distance from there
+    off = q.double() != nearest
+    assert not (off & (middle > 2.0 ** -18 * v.abs() * (1 + parts))).any()
+    assert ((q.double() - nearest).abs()[off] <= 1.01 * step[off]).all()
