@@ -168,7 +168,8 @@ int cconv_quantize_blocks(const cconv_quantize_args* args, void* cuda_stream);
  *   C[m,n] = sum_g scale[n,g] sum_{k in group g} (q[n,k] - zero[n,g]) X[m,k],   group g: k / group = g
  * Element 2j of a row of q is the low half of byte j, element 2j + 1 its high half; what lies behind K in the last
  * byte does not matter.  A token that holds an infinity or a NaN gives infinities or NaN.
- * Up to 64 tokens, sums are of q and X as they are, in fp32, and scaled in fp32; with more, the weights
+ * Up to 64 tokens, sums are of q and X as they are, in fp32, and scaled in fp32 (of one or two tokens, and up to 8 of small
+ * matrices, as sums of (16 + q) X less (16 + zero) times that of X: fp32's rounding is then of these); with more, the weights
  * scale (q - zero) are rounded to the precision of `dtype` first, as operands of the tensor cores (fp16: not to its range;
  * a row's groups whose scale is below 2^-24 of its largest lose bits, 2^-31 of that one at most). */
 typedef struct {
@@ -214,6 +215,7 @@ int cconv_quantize_groups(const cconv_quantize_groups_args* args, void* cuda_str
  * experts (normalize 0):   out[t] = sum_j p_j (act(x Wg_e^T) * (x Wu_e^T)) Wd_e^T,  e = ids[t][j].
  * Without a router ids and weights are read instead; numbers that are no expert's add nothing (those of other
  * ranks, say), and an expert that a token names twice counts with both weights.
+ * h = act(x Wg_e^T) * (x Wu_e^T) is held as the sum of two numbers of `dtype`: twice its precision, and its range.
  * The weights of each expert in use are read once for 64 tokens; calls of more run 64 at a time. */
 typedef struct {
   int64_t T, D, F, E;  /* E at most 1024, T at most 2^20, D and F at most 2^29 */
@@ -236,7 +238,8 @@ int64_t cconv_moe_workspace(const cconv_moe_args* args); /* (a router of NULL is
 int cconv_moe_forward(const cconv_moe_args* args, void* cuda_stream);
 
 /* ---- the norm of a list of gradients, and clipping -------------------------------------------------
- * norm = sqrt(sum of squares over all elements), the sum in 64 bits, rounded to fp32; every element times
+ * norm = sqrt(sum of squares over all elements), the sum in 64 bits (but for up to 66 neighbours' in fp32, where that holds
+ * them), rounded to fp32; every element times
  * min(1, max_norm / (norm + eps)), in fp32, rounded to its type.  A norm that is infinite makes the factor 0, one that is
  * NaN, or as infinite as max_norm, makes every element NaN.  Tensors of more than two dimensions are lists of rows where their strides allow. */
 typedef struct {

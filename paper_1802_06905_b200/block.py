@@ -402,7 +402,7 @@ def int4_product(x, q, scale, out, zero=None, group=128, workspace=None, stream=
 
     x [M, K], out [M, N] bf16 or fp16; q [N, ceil(K/2)] uint8, element 2j of a row in the low half of byte j; scale
     [N, ceil(K/group)] bf16, fp16 or fp32; zero of the same shape, uint8 of 0 to 15 (None: 8 throughout); group 32, 64 or
-    128; any strides.  With more than 64 tokens the weights scale (q - zero) are rounded to x's type."""
+    128; any strides.  With more than 64 tokens the weights scale (q - zero) are rounded to the precision of x's type."""
     args, dev = _int4_args(x, q, scale, out, zero, group)
     _call_with_space("cconv_int4_product", "cconv_int4_product_workspace", args, dev, workspace, stream)
     return out
@@ -543,7 +543,8 @@ def clip_gradients(grads, max_norm, norm, outs=None, eps=1e-6, norm_given=False,
     """cconv_clip_gradients: every gradient times min(1, max_norm / (norm + eps)), in place or to ``outs``.
 
     ``grads``, ``outs``: lists of tensors, or TensorLists; ``norm`` (fp32 [1]) gets the norm over all of them, or,
-    with ``norm_given``, holds it: that of other ranks' gradients too, say.  Nothing waits for the host."""
+    with ``norm_given``, holds it: that of other ranks' gradients too, say.  Nothing waits for the host.  A list is described
+    anew in each call (1.5 to 2 us a tensor on the host); a program that keeps its gradients makes a TensorList of them."""
     grads = _tensor_list(grads, "grads")
     outs = None if outs is None else _tensor_list(outs, "outs")
     args = _clip_args(grads, outs, max_norm, eps, int(norm_given), norm)

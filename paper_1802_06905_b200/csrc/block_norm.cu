@@ -12,7 +12,7 @@
 // registers or in shared memory, between its two reductions (over y, then over r'; backward: over r' and e, then
 // over y and f), so they are bound by HBM.  That holds forward up to 16384 channels, and backward up to 65536 where a
 // block or a cluster of them has room for the row; the *_long_ kernels, for the rest, read a row once for
-// each sweep over it.  Measured, 16384 x 4096 bf16 with 8 gates: forward 89.5 us, 6.0 TB/s (4 arrays once: 82 us
+// each sweep over it.  Measured, 16384 x 4096 bf16 with 8 gates: forward 89.5 to 92 us, 5.9 TB/s (4 arrays once: 82 us
 // at the rate of a copy); backward 147 us, 5.5 TB/s (6 arrays: 123 us), 135 of them the first kernel.  One token
 // of 4096 channels: 2.5 us on the device.
 #include "block_norm.cuh"

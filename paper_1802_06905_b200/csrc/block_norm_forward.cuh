@@ -293,7 +293,7 @@ __global__ void __launch_bounds__(1024) cconv_residual_norm_long_kernel(const No
   }
 }
 
-// Many rows that are not wide, through a ring for rows that begin anywhere (16384 x 4095 bf16: 131 us, 224 with a block size known at
+// Many rows that are not wide, through a ring for rows that begin anywhere (16384 x 4095 bf16: 127 us, 224 with a block size known at
 // the launch; with a block a row and everything from global memory 516 us).
 // (Blocks an SM that the compiler keeps registers for: without 8-bit results none are named.  Naming one is no lower
 // limit but leave to take 104 to 131 registers instead of 72 to 109: 16384 x 4095 192 us, 16384 x 2047 76 instead of 62.)
