@@ -111,6 +111,43 @@ def test_int4_in_fp16_with_more_rows_than_a_launch_has_blocks():
     check_fp16(c, c.run(), "many rows")
 
 
+def test_int4_in_fp16_captured_and_on_two_streams():
+    """The rows' powers of two are the workspace's, of each call its own; a workspace of just the size, whatever it holds."""
+    cs = []
+    for i, (M, N, K) in enumerate(((65, 333, 520), (300, 1024, 512), (80, 77, 2050))):
+        c = Int4(M, N, K, 64, FP16, FP32, zero=True, seed=i)
+        c.scale = (c.scale.double() * 10.0 ** (torch.arange(N, device="cuda", dtype=torch.float64) % 7 - 4)[:, None]).to(FP32)
+        cs.append(c)
+    want = [c.run() for c in cs]
+    for c, w in zip(cs, want):
+        check_fp16(c, w, "alone")
+        n = block.int4_product_workspace(c.x, c.q, c.scale, w, zero=c.zero, group=64)
+        for byte in (0, 255):
+            space = torch.full((n + 4096,), byte, device="cuda", dtype=torch.uint8)
+            assert torch.equal(c.run(workspace=space[:n]), w) and (space[n:] == byte).all()
+    streams, got = [torch.cuda.Stream(), torch.cuda.Stream()], []
+    torch.cuda.synchronize()
+    for i in range(30):
+        with torch.cuda.stream(streams[i % 2]):
+            got.append((i % 3, cs[i % 3].run()))
+    torch.cuda.synchronize()
+    assert all(torch.equal(out, want[i]) for i, out in got)
+    graphs = []
+    for c in cs:
+        g = torch.cuda.CUDAGraph()
+        with torch.cuda.graph(g, stream=streams[0]):
+            graphs.append((g, c.run()))
+    for c in cs:
+        c.scale.mul_(1e-3)
+    torch.cuda.synchronize()
+    for _ in range(2):
+        for (g, out), c in zip(graphs, cs):
+            g.replay()
+    torch.cuda.synchronize()
+    for (g, out), c in zip(graphs, cs):
+        assert torch.equal(out, c.run())
+
+
 # ---- 4-bit products known to the last bit ------------------------------------------------------------
 
 def integers(g, low, high, shape, dtype):
@@ -293,3 +330,49 @@ def test_norm_in_8_bits_values_are_the_nearest(T, D, dtype):
     off = q.double() != nearest
     assert not (off & (middle > 2.0 ** -18 * v.abs() * (1 + parts))).any()
     assert ((q.double() - nearest).abs()[off] <= 1.01 * step[off]).all()
+
+
+# ---- sizes beyond 32 bits ------------------------------------------------------------------------------------
+
+def test_int4_products_beyond_32_bits():
+    """Weights of more than 2^32 bytes for few tokens; expanded ones of more than 2^32 bytes for many."""
+    g = gen(77)
+    for M, N, K, dtype in ((1, 150001, 60000, BF16), (20, 150001, 60000, BF16), (66, 40001, 60000, FP16)):
+        q = torch.randint(0, 256, (N, K // 2), generator=g, device="cuda", dtype=torch.uint8)
+        x, scale = integers(g, -1, 1, (M, K), dtype), (2.0 ** -integers(g, 0, 1, (N, -(-K // 128)), FP32)).to(dtype)
+        out = block.int4_product(x, q, scale, poisoned((M, N), dtype))
+        at = torch.cat([torch.arange(40, device="cuda"), torch.randint(0, N, (100,), generator=g, device="cuda"), torch.arange(N - 40, N, device="cuda")])
+        k = torch.arange(K, device="cuda")
+        w = ((q[at][:, k // 2].int() >> (4 * (k % 2)) & 15) - 8).double() * scale[at].double()[:, k // 128]
+        assert torch.equal(out[:, at], (x.double() @ w.T).to(FP32).to(dtype))
+        assert torch.isfinite(out).all()
+
+
+def test_norm_in_8_bits_beyond_32_bits():
+    T, D = 1 << 20, 4104
+    r = torch.empty((T, D), device="cuda", dtype=BF16)
+    for i in range(0, T, 1 << 17):
+        r[i:i + (1 << 17)].normal_(generator=gen(i))
+    out, q, s = torch.empty_like(r), torch.empty((T, D), device="cuda", dtype=serve.E4M3), poisoned((T, 33), FP32)
+    block.residual_norm_quantize(r, out, q, s)
+    for rows in (slice(0, 50), slice(T // 2 - 25, T // 2 + 25), slice(T - 50, T)):
+        assert torch.equal(out[rows], r[rows])
+        x = r[rows].double()
+        x = x / (x.square().mean(1, keepdim=True) + serve.EPS).sqrt()
+        sc = s[rows].double().repeat_interleave(128, 1)[:, :D]
+        close(s[rows], torch.nn.functional.pad(x, (0, 120)).reshape(50, 33, 128).abs().amax(2) / 448, 2.0 ** -17 * s[rows].double(), "scales")
+        close(q[rows].double() * sc, x, x.abs() * (2.0 ** -4 + 2.0 ** -17) + 2.0 ** -10 * sc, "values")
+    assert torch.isfinite(s).all()
+
+
+def test_clipping_beyond_32_bits():
+    n = (1 << 32) + 12347
+    t = torch.full((n,), 0.5, device="cuda", dtype=BF16)
+    t[-3:] = 64.0
+    norm = poisoned((1,), FP32)
+    exact = ((n - 3) * 0.25 + 3 * 4096.0) ** 0.5
+    block.clip_gradients([t], exact / 4, norm)
+    assert abs(norm.item() - exact) <= 24 * 2.0 ** -24 * exact
+    # a quarter, but for eps and the norm's rounding: within a rounding to bf16
+    for part, v in ((t[:1 << 20], 0.125), (t[1 << 31:(1 << 31) + 4096], 0.125), (t[(1 << 32) - 4096:-3], 0.125), (t[-3:], 16.0)):
+        assert ((part.double() - v).abs() <= 2.0 ** -8 * v).all()
